@@ -91,6 +91,23 @@ typedef struct {
  * and frees the cache on its own device, whichever device is current.
  * Errors: INVALID, UNSUPPORTED, OOM (host), CUDA. */
 pe_status pe_cache_create(const pe_cache_config *cfg, pe_cache **out);
+
+/* The same cache with K and V held in 8 bits: e4m3 codes with one power-of-two
+ * scale for each (layer, page, kv-head), for K and for V.  With a the largest
+ * magnitude of a page's tokens there, the scale's exponent e is the least
+ * integer with a <= 448 * 2^e (at least -126, at most 119: larger magnitudes
+ * than 448 * 2^119 become that; -126 where a = 0); a value is held as
+ * code * 2^e, code = x * 2^-e rounded to e4m3, nearest, ties to even.
+ * Every call takes and gives bf16 as before and keeps its meaning on the values
+ * held.  Appending to a partly filled page quantises that page again from its
+ * kept values and the new tokens.  e4m3 has no infinity: a token whose K or V
+ * holds an infinity or NaN for a kv-head is held as NaN there, and every query
+ * row that sees it gets NaN; rows that do not see it are not affected.
+ * k_pool and v_pool must be NULL (INVALID otherwise).  Device memory: half of
+ * a bf16 cache's pools, 2 bytes a page, kv-head and layer for the scales, and
+ * one layer's pools in bf16, into which calls that attend many queries unpack
+ * the layer they need.  Errors as pe_cache_create. */
+pe_status pe_cache_create_q8(const pe_cache_config *cfg, pe_cache **out);
 pe_status pe_cache_destroy(pe_cache *cache);
 
 /* New empty sequence (len 0); the lowest free slot id is returned.  OOM if none. */
@@ -171,6 +188,59 @@ pe_status pe_replay_attn_batch(pe_cache *cache, int32_t n, const int32_t *seqs, 
                                const void *Q_packed, const int32_t *cu_q, void *out, int32_t num_q_heads,
                                float softmax_scale, void *stream);
 
+/* pe_replay_attn_batch that also keeps account of what the keys drew: for
+ * every key j of sequence i, weights[i * weights_stride + j] grows by the sum
+ * over the sequence's q-heads and its queries of this call of the key's softmax
+ * weight (0 for a query that does not see the key).  weights: device fp32, rows
+ * of weights_stride >= the sequence's length entries; entries past the length
+ * and rows of sequences without queries are not touched.  Held and summed in
+ * 32 bits, in an order that does not depend on timing.  `out` as in
+ * pe_replay_attn_batch (the same values).  weights must not overlap Q or out.
+ * Errors: those of pe_replay_attn_batch; INVALID (weights null or not 4-byte
+ * aligned), RANGE (weights_stride below a length; n_q x num_q_heads x 4 bytes
+ * above the cache's workspace). */
+pe_status pe_replay_attn_weights_batch(pe_cache *cache, int32_t n, const int32_t *seqs, int32_t layer,
+                                       const void *Q_packed, const int32_t *cu_q, void *out, int32_t num_q_heads,
+                                       float softmax_scale, float *weights, int64_t weights_stride, void *stream);
+
+/* The values the cache holds: tokens [begins[i], begins[i] + cu_tokens[i+1] -
+ * cu_tokens[i]) of sequence i into rows [cu_tokens[i], cu_tokens[i+1]) of
+ * K_out / V_out, device bf16 [L][cu_tokens[n]][Hkv][d] (16-byte aligned);
+ * seqs, begins (int64) and cu_tokens (from 0, non-decreasing) are host arrays.
+ * A sequence may appear more than once.  On an 8-bit cache a value is code *
+ * 2^e, exact in bf16 down to its smallest normal number; a token held as NaN
+ * reads as NaN in K and V.  Errors: INVALID, RANGE (tokens past a length),
+ * UNSUPPORTED (host-only cache), CUDA. */
+pe_status pe_read_kv_batch(pe_cache *cache, int32_t n, const int32_t *seqs, const int64_t *begins,
+                           const int32_t *cu_tokens, void *K_out, void *V_out, void *stream);
+
+/* Eviction by accumulated attention weight.  Sequence i of length T comes down
+ * to keep[i] tokens (all it has, if fewer): its first `sinks` and last `recent`
+ * positions, and of the others the ones with the largest weights[i *
+ * weights_stride + j] (device fp32, as pe_replay_attn_weights_batch fills it;
+ * ties go to the lowest position, NaN counts below every number).  The kept
+ * tokens keep their order and become positions 0 .. keep[i]-1 of the sequence,
+ * in every layer; later calls (crop, append, attention, checkpoints) use the new
+ * positions.  kept[i * kept_stride + r] (device int32, kept_stride >= every
+ * sequence's new length) receives the old position of new position r, -1 up to
+ * kept_stride past them; the weights move along, and their entries from the
+ * new length up to T become 0.  A sequence with keep[i] >= T stays as it is.
+ * Pages that hold sinks only stay in place.  The others are copied into pages
+ * popped (ascending logical order, sequence by sequence) before the old pages
+ * lose their references (descending logical order), so that many must be free;
+ * an 8-bit cache quantises each new page from the values it receives.
+ * Checkpoints past the sinks are dropped; the recomputation counter stays.
+ * Everything runs on `stream`, without a wait for the device.  All-or-nothing,
+ * a sequence may appear once.  On a host-only cache only the bookkeeping runs
+ * (weights and kept unused).
+ * Errors: INVALID (unknown or repeated sequence, negative keep / sinks / recent,
+ * sinks + recent above a keep[i] < T, null or misaligned weights or kept), RANGE
+ * (a stride too small), OOM, CUDA (the weights are then as before, kept is
+ * not defined). */
+pe_status pe_evict_batch(pe_cache *cache, int32_t n, const int32_t *seqs, const int32_t *keep, int32_t sinks,
+                         int32_t recent, float *weights, int64_t weights_stride, int32_t *kept, int64_t kept_stride,
+                         void *stream);
+
 /* ---- Replay with the indep split (Sec. 4.5, the T - tau + 1 paragraph;
  * Sec. 4.1 methods B7 and B5').  Post-target turns whose content is the same
  * in the counterfactual world are re-prefilled, many positions per pass;
@@ -249,8 +319,12 @@ pe_status pe_page_refs(const pe_cache *cache, int32_t *out, int32_t cap);
  * into host `out`, after all work on `stream`; for checking the mirror. */
 pe_status pe_seq_device_page_table(pe_cache *cache, int32_t seq, int32_t *out, int32_t cap, void *stream);
 
-/* Device pool pointers (for reading pool contents back). */
+/* Device pool pointers (for reading pool contents back): bf16, or an 8-bit
+ * cache's codes [L][num_pages][Hkv][ps][d]. */
 pe_status pe_cache_pools(const pe_cache *cache, void **k_pool, void **v_pool);
+/* An 8-bit cache's scale exponents, device int8 [L][num_pages][Hkv][2] (K, V);
+ * UNSUPPORTED on a bf16 cache. */
+pe_status pe_cache_scales(const pe_cache *cache, void **exponents);
 
 /* Options: "splitkv" = -1 (auto, default) / 0 (never) / 1 (always);
  * "num_splits" = 0 (auto) or the split count; "debug_poison" = 0/1: crop

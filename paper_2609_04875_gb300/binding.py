@@ -32,6 +32,7 @@ EXPORTED = [
     "pe_seq_checkpoints", "pe_page_refs", "pe_prov_create", "pe_prov_destroy", "pe_prov_add",
     "pe_prov_locate_source", "pe_prov_taint_closure", "pe_prov_first_entry", "pe_replay_schedule",
     "pe_replay_rounds", "pe_attn_plan_persistent", "pe_attn_plan_launches", "pe_last_error", "pe_version",
+    "pe_cache_create_q8", "pe_cache_scales", "pe_read_kv_batch", "pe_replay_attn_weights_batch", "pe_evict_batch",
 ]
 
 # Turn kinds and replay policies of pe_replay_schedule (pe.h).
@@ -100,6 +101,11 @@ _sigs = {
     "pe_replay_rounds": [_P, _I32, _I32P, _I32, _I32P, _I32P, _P, _P, _P, _P, _I32, ctypes.c_float, _P],
     "pe_attn_plan_persistent": [_P, _I32, _I32P, _I32P, _I32, _I32, _I32P, _I32P, _I32P, _I32, _I32P, _I32,
                                 _I32P, _I32],
+    "pe_cache_create_q8": [ctypes.POINTER(_Config), ctypes.POINTER(_P)],
+    "pe_cache_scales": [_P, ctypes.POINTER(_P)],
+    "pe_read_kv_batch": [_P, _I32, _I32P, _I64P, _I32P, _P, _P, _P],
+    "pe_replay_attn_weights_batch": [_P, _I32, _I32P, _I32, _P, _I32P, _P, _I32, ctypes.c_float, _P, _I64, _P],
+    "pe_evict_batch": [_P, _I32, _I32P, _I32P, _I32, _I32, _P, _I64, _P, _I64, _P],
     "pe_attn_plan_launches": [_P, _I32, _I32P, _I32P, _I32, _I32, _I64P, _I64, _I64P],
 }
 for _name, _args in _sigs.items():
@@ -220,12 +226,17 @@ class PagedKVCache:
     ``k_pool`` / ``v_pool``: optional caller-owned CUDA tensors of shape
     [L][num_pages][Hkv][page_size][d] (bf16); otherwise the library allocates.
     ``host_only=True`` keeps only the host bookkeeping (no device memory).
+    ``kv_bits=8``: K and V are held as e4m3 codes with one power-of-two scale
+    for each page, kv-head and layer (pe_cache_create_q8); every call takes and
+    gives bf16 as before.
     A device cache lives on the CUDA device current at construction; its calls
     must be made with that device current, on tensors that live there.
     """
 
     def __init__(self, num_layers, num_kv_heads, head_dim, page_size, num_pages, max_seqs, max_pages_per_seq,
-                 init_free_order=None, k_pool=None, v_pool=None, host_only=False, workspace_bytes=0):
+                 init_free_order=None, k_pool=None, v_pool=None, host_only=False, workspace_bytes=0, kv_bits=16):
+        if kv_bits not in (8, 16):
+            raise ValueError("kv_bits must be 8 or 16")
         cfg = _Config()
         cfg.num_layers, cfg.num_kv_heads, cfg.head_dim = num_layers, num_kv_heads, head_dim
         cfg.page_size, cfg.num_pages, cfg.max_seqs = page_size, num_pages, max_seqs
@@ -253,8 +264,10 @@ class PagedKVCache:
         self.page_size, self.num_pages, self.max_seqs = page_size, num_pages, max_seqs
         self.max_pages_per_seq = max_pages_per_seq
         self.host_only = host_only
+        self.kv_bits = kv_bits
         h = ctypes.c_void_p()
-        _check(_lib.pe_cache_create(ctypes.byref(cfg), ctypes.byref(h)))
+        create = _lib.pe_cache_create_q8 if kv_bits == 8 else _lib.pe_cache_create
+        _check(create(ctypes.byref(cfg), ctypes.byref(h)))
         self._h = h
         self._default_scale = 1.0 / math.sqrt(head_dim)  # (after the library has refused any but 64 and 128)
 
@@ -413,6 +426,90 @@ class PagedKVCache:
                                          _i32_array(cu_q), self._ptr(out, "out"), shape[1], scale,
                                          self._s(stream)))
         return out
+
+    def replay_attn_weights_batch(self, seqs, layer, Q, cu_q, weights, out=None, softmax_scale=None, stream=None):
+        """replay_attn_batch, and each key's softmax weight, summed over the
+        sequence's queries and q-heads, added to ``weights``: CUDA float32
+        [len(seqs)][>= the longest length], columns contiguous."""
+        shape = Q.shape
+        if len(shape) != 3 or shape[2] != self.head_dim or shape[0] != cu_q[-1]:
+            raise ValueError("Q must be [cu_q[-1]][Hq][d]")
+        _same_shape(out, Q)
+        if out is None:
+            import torch
+            out = torch.empty_like(Q)
+        scale = self._default_scale if softmax_scale is None else float(softmax_scale)
+        ptr, stride = self._weights(weights, seqs)
+        _check(_lib.pe_replay_attn_weights_batch(self._h, len(seqs), _i32_array(seqs), layer, self._ptr(Q, "Q"),
+                                                 _i32_array(cu_q), self._ptr(out, "out"), shape[1], scale, ptr, stride,
+                                                 self._s(stream)))
+        return out
+
+    def _rows(self, t, name, dtype, n):
+        """(address, row stride) of a CUDA tensor of n rows with contiguous columns."""
+        import torch
+        if t.dtype is not getattr(torch, dtype):
+            raise TypeError(f"{name} must be {dtype}")
+        if not t.is_cuda:
+            raise TypeError(f"{name} must be a CUDA tensor")
+        if t.get_device() != self._device:
+            raise ValueError(f"{name} is on cuda:{t.get_device()}, the cache on cuda:{self._device}")
+        if t.dim() != 2 or t.shape[0] != n or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise ValueError(f"{name} must be [{n}][columns], columns contiguous")
+        if n > 1 and t.stride(0) < t.shape[1]:
+            raise ValueError(f"{name}: rows overlap")
+        return t.data_ptr(), t.stride(0) if n > 1 else t.shape[1]
+
+    def _weights(self, t, seqs):
+        """The same for weights: the library checks the sequences' lengths against the row stride, which is the
+        number of columns unless the rows are parts of longer ones."""
+        ptr, stride = self._rows(t, "weights", "float32", len(seqs))
+        if stride != t.shape[1] and max(self.seq_info(s)[0] for s in seqs) > t.shape[1]:
+            raise ValueError("weights: a sequence is longer than a row")
+        return ptr, stride
+
+    # -- reading back, eviction --------------------------------------------------
+    def read_kv_batch(self, seqs, begins, cu_tokens, stream=None):
+        """(K, V): bf16 [L][cu_tokens[-1]][Hkv][d], rows cu_tokens[i]:cu_tokens[i+1] the values the cache holds for
+        seqs[i]'s tokens from begins[i] on."""
+        import torch
+        if len(begins) != len(seqs) or len(cu_tokens) != len(seqs) + 1:
+            raise ValueError("begins and cu_tokens must match seqs")
+        if self.host_only:
+            raise ValueError("a host-only cache holds no K and V")
+        K = torch.empty((self.num_layers, cu_tokens[-1], self.num_kv_heads, self.head_dim), dtype=torch.bfloat16,
+                        device=f"cuda:{self._device}")
+        V = torch.empty_like(K)
+        _check(_lib.pe_read_kv_batch(self._h, len(seqs), _i32_array(seqs), _i64_array(begins), _i32_array(cu_tokens),
+                                     K.data_ptr(), V.data_ptr(), self._s(stream)))
+        return K, V
+
+    def read_kv(self, seq, begin=0, n=None, stream=None):
+        """(K, V) of one sequence's tokens [begin, begin + n) (to its end by default)."""
+        n = self.seq_info(seq)[0] - begin if n is None else n
+        return self.read_kv_batch([seq], [begin], [0, n], stream)
+
+    def evict_batch(self, seqs, keep, weights=None, sinks=0, recent=0, kept=None, stream=None):
+        """pe_evict_batch: sequence i keeps keep[i] positions (all it has, if fewer): its first ``sinks``, its last
+        ``recent`` and the others of largest ``weights[i]`` (CUDA float32 [len(seqs)][>= length], compacted in
+        place).  Returns ``kept``, int32 [len(seqs)][max(keep)]: the positions kept, ascending, -1 past them.
+        Host-only caches take no tensors."""
+        if len(keep) != len(seqs):
+            raise ValueError("keep must match seqs")
+        if self.host_only:
+            _check(_lib.pe_evict_batch(self._h, len(seqs), _i32_array(seqs), _i32_array(keep), int(sinks), int(recent),
+                                       None, 0, None, 0, self._s(stream)))
+            return None
+        import torch
+        w, w_stride = self._weights(weights, seqs)
+        if kept is None:
+            kept = torch.empty((len(seqs), max(0, *keep) if len(keep) else 0), dtype=torch.int32, device=weights.device)
+        k, k_stride = self._rows(kept, "kept", "int32", len(seqs))
+        if k_stride != kept.shape[1]:
+            raise ValueError("kept must be contiguous")
+        _check(_lib.pe_evict_batch(self._h, len(seqs), _i32_array(seqs), _i32_array(keep), int(sinks), int(recent), w,
+                                   w_stride, k, k_stride, self._s(stream)))
+        return kept
 
     def replay_rounds(self, seqs, take, cu_tok, K=None, V=None, Q=None, out=None, softmax_scale=None,
                       num_q_heads=None, stream=None):

@@ -114,7 +114,11 @@ struct pe_cache {
     // device state
     int device = 0;
     int num_sms = 148;
-    void *k_pool = nullptr, *v_pool = nullptr;
+    void *k_pool = nullptr, *v_pool = nullptr;  // bf16, what the attention kernels read.  8-bit cache: one layer only,
+                                                // the called layer's pages unpacked at their page ids
+    bool q8 = false;              // K and V held in 8 bits (q8.cuh)
+    void *k8 = nullptr, *v8 = nullptr;  // codes [L][num_pages][Hkv][ps][d]
+    int8_t *exps = nullptr;       // scale exponents [L][num_pages][Hkv][2]
     bool own_pools = false;
     int32_t *d_table = nullptr;
     int64_t *d_len = nullptr;
@@ -123,7 +127,7 @@ struct pe_cache {
     int64_t ws_bytes = 0;
     int32_t *d_tickets = nullptr;  // merge counters: decode (per sequence and kv-head, then the scheduler's
                                    // two), then the persistent attention's (per slot, q-tile and warp)
-    int64_t pool_rows = 0;  // L * num_pages * Hkv * ps
+    int64_t pool_rows = 0;  // rows of k_pool: L (8-bit cache: 1) * num_pages * Hkv * ps
     CUtensorMap tm_k{}, tm_v{};    // tensor-core kernel: 64 x ps boxes
     CUtensorMap tm_kd{}, tm_vd{};  // decode kernel: 64 x min(ps, 64) boxes
     // options
@@ -327,18 +331,31 @@ void free_device(pe_cache *c)
         if (c->k_pool) cudaFree(c->k_pool);
         if (c->v_pool) cudaFree(c->v_pool);
     }
+    if (c->k8) cudaFree(c->k8);
+    if (c->v8) cudaFree(c->v8);
+    if (c->exps) cudaFree(c->exps);
     if (c->d_table) cudaFree(c->d_table);
     if (c->d_len) cudaFree(c->d_len);
     if (c->d_status) cudaFree(c->d_status);
     if (c->d_ws) cudaFree(c->d_ws);
     if (c->d_tickets) cudaFree(c->d_tickets);
-    c->k_pool = c->v_pool = nullptr;
+    c->k_pool = c->v_pool = c->k8 = c->v8 = nullptr;
+    c->exps = nullptr;
     c->d_tickets = nullptr;
     c->d_table = nullptr;
     c->d_len = nullptr;
     c->d_status = nullptr;
     c->d_ws = nullptr;
 }
+
+// ---- where K and V are held
+// The finite poison written by the debug crop: bf16 2^100, or the largest e4m3 code.
+constexpr uint32_t kPoisonPair = 0x71807180u, kPoisonCodes = 0x7e7e7e7eu;
+
+void *stored_k(const pe_cache *c) { return c->q8 ? c->k8 : c->k_pool; }
+void *stored_v(const pe_cache *c) { return c->q8 ? c->v8 : c->v_pool; }
+// 16-byte chunks of a stored row of K or V
+int32_t row_chunks(const pe_cache *c) { return c->cfg.head_dim / (c->q8 ? 16 : 8); }
 
 // ---- crop bookkeeping shared by pe_crop, pe_crop_batch, pe_restore and pe_seq_release
 struct CropPlan {
@@ -385,13 +402,14 @@ pe_status launch_crops(pe_cache *c, const std::vector<CropPlan> &plans, cudaStre
     std::memset(static_cast<void *>(&p), 0, offsetof(CropParams, segs));
     p.page_table = c->d_table;
     p.seq_len = c->d_len;
-    p.k_pool = static_cast<uint4 *>(c->k_pool);
-    p.v_pool = static_cast<uint4 *>(c->v_pool);
+    p.k_pool = static_cast<uint4 *>(stored_k(c));
+    p.v_pool = static_cast<uint4 *>(stored_v(c));
     p.poison = c->debug_poison;
+    p.poison_word = c->q8 ? kPoisonCodes : kPoisonPair;
     p.L = c->cfg.num_layers;
     p.hkv = c->cfg.num_kv_heads;
     p.ps = c->cfg.page_size;
-    p.dvec = c->cfg.head_dim / 8;
+    p.dvec = row_chunks(c);
     p.num_pages = c->cfg.num_pages;
     size_t i = 0;
     while (i < plans.size()) {
@@ -498,13 +516,14 @@ struct CowList {
     pe_status flush(pe_cache *c, cudaStream_t st)
     {
         if (p.n == 0) return PE_OK;
-        p.k_pool = static_cast<uint4 *>(c->k_pool);
-        p.v_pool = static_cast<uint4 *>(c->v_pool);
+        p.k_pool = static_cast<uint4 *>(stored_k(c));
+        p.v_pool = static_cast<uint4 *>(stored_v(c));
+        p.exps = c->exps;
         p.page_table = c->d_table;
         p.L = c->cfg.num_layers;
         p.hkv = c->cfg.num_kv_heads;
         p.ps = c->cfg.page_size;
-        p.dvec = c->cfg.head_dim / 8;
+        p.dvec = row_chunks(c);
         p.num_pages = c->cfg.num_pages;
         cudaError_t e = launch_cow_copy(p, st);
         p.n = 0;
@@ -557,8 +576,9 @@ pe_status apply_appends(pe_cache *c, const std::vector<AppendPlan> &plans, const
     {
         p->K = static_cast<const uint4 *>(K);
         p->V = static_cast<const uint4 *>(V);
-        p->k_pool = static_cast<uint4 *>(c->k_pool);
-        p->v_pool = static_cast<uint4 *>(c->v_pool);
+        p->k_pool = static_cast<uint4 *>(stored_k(c));
+        p->v_pool = static_cast<uint4 *>(stored_v(c));
+        p->exps = c->exps;
         p->page_table = c->d_table;
         p->seq_len = c->d_len;
         p->L = c->cfg.num_layers;
@@ -578,10 +598,18 @@ pe_status apply_appends(pe_cache *c, const std::vector<AppendPlan> &plans, const
         if (cs != PE_OK) return cs;
         p->n_new = pages_in_launch;
         p->seg_tokens = p->segs[p->n_segs - 1].cum0 + p->segs[p->n_segs - 1].n_tokens;
+        if (c->q8) {  // (that kernel works page by page)
+            p->seg_tokens = 0;
+            for (int i = 0; i < p->n_segs; ++i) {
+                AppendSeg &sg = p->segs[i];
+                sg.cum0 = p->seg_tokens;
+                p->seg_tokens += static_cast<int32_t>(ceil_div(static_cast<int64_t>(sg.len0) + sg.n_tokens, ps)) - sg.len0 / ps;
+            }
+        }
         const int64_t chunks = static_cast<int64_t>(p->L) * p->seg_tokens * p->hkv * p->dvec;
         if (injected_failure(c)) return launch_fault("append kernel");
         if (!c->host_only) {
-            cudaError_t e = launch_append(*p, chunks, st);
+            cudaError_t e = c->q8 ? launch_append_q8(c->cfg.head_dim, *p, st) : launch_append(*p, chunks, st);
             if (e != cudaSuccess) return cuda_fail(e, "append kernel launch");
             c->launches++;
         }
@@ -1609,6 +1637,121 @@ pe_status run_attention(pe_cache *c, const std::vector<AttnItem> &items, int32_t
 }
 
 // Pointers are only checked when the call has queries (an empty tensor may be null).
+// 8-bit cache: unpacks `layer` of the sequences' pages, so that the bf16 kernels can attend them as layer 0.
+pe_status unpack_layer(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer, cudaStream_t st)
+{
+    UnpackParams p;
+    std::memset(static_cast<void *>(&p), 0, offsetof(UnpackParams, segs));
+    p.page_table = c->d_table;
+    p.k8 = static_cast<const uint4 *>(c->k8);
+    p.v8 = static_cast<const uint4 *>(c->v8);
+    p.exps = c->exps;
+    p.k = static_cast<uint4 *>(c->k_pool);
+    p.v = static_cast<uint4 *>(c->v_pool);
+    p.layer = layer;
+    p.hkv = c->cfg.num_kv_heads;
+    p.ps = c->cfg.page_size;
+    p.d = c->cfg.head_dim;
+    p.num_pages = c->cfg.num_pages;
+    int32_t pages = 0;
+    auto flush = [&]() -> pe_status {
+        if (p.n == 0) return PE_OK;
+        if (injected_failure(c)) return launch_fault("unpack kernel");
+        cudaError_t e = launch_unpack_q8(p, pages, st);
+        if (e != cudaSuccess) return cuda_fail(e, "unpack kernel launch");
+        c->launches++;
+        p.n = pages = 0;
+        return PE_OK;
+    };
+    for (const AttnItem &it : items) {
+        if (it.n_q <= 0) continue;
+        if (p.n == kMaxSegs)
+            if (pe_status s = flush()) return s;
+        p.segs[p.n++] = UnpackSeg{it.seq * c->cfg.max_pages_per_seq, pages};
+        pages += static_cast<int32_t>(c->table[it.seq].size());
+    }
+    return flush();
+}
+
+// The attention of every call: 8-bit caches by way of the unpacked layer.
+pe_status attend(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer, const void *Q, int64_t q_rows, void *out,
+                 int32_t hq, float scale, cudaStream_t st)
+{
+    if (!c->q8) return run_attention(c, items, layer, Q, q_rows, out, hq, scale, st);
+    if (pe_status s = unpack_layer(c, items, layer, st)) return s;
+    return run_attention(c, items, 0, Q, q_rows, out, hq, scale, st);
+}
+
+// Adds the items' softmax weights to `weights` (row i: item i), after the attention of the same call, whose layer is
+// still unpacked.  The workspace holds the query rows' log-sum-exp.
+pe_status add_weights(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer, const void *Q, int32_t hq, float scale,
+                      float *weights, int64_t stride, cudaStream_t st)
+{
+    const pe_cache_config &cf = c->cfg;
+    WeightParams p;
+    std::memset(static_cast<void *>(&p), 0, offsetof(WeightParams, segs));
+    p.page_table = c->d_table;
+    p.q = static_cast<const __nv_bfloat16 *>(Q);
+    p.k = static_cast<const __nv_bfloat16 *>(c->k_pool) +
+          (c->q8 ? 0 : static_cast<int64_t>(layer) * cf.num_pages * cf.num_kv_heads * cf.page_size * cf.head_dim);
+    p.lse = c->d_ws;
+    p.weights = weights;
+    p.weights_stride = stride;
+    p.hq = hq;
+    p.hkv = cf.num_kv_heads;
+    p.group = hq / cf.num_kv_heads;
+    p.ps = cf.page_size;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    int64_t rows = 0;
+    int32_t max_keys = 0;
+    auto flush = [&]() -> pe_status {
+        if (p.n == 0) return PE_OK;
+        if (injected_failure(c)) return launch_fault("weights kernels");
+        cudaError_t e = launch_weights(cf.head_dim, p, rows, max_keys, st);
+        if (e != cudaSuccess) return cuda_fail(e, "weights kernel launch");
+        c->launches += 2;
+        c->ends_in_merge = false;
+        p.n = max_keys = 0;
+        rows = 0;
+        return PE_OK;
+    };
+    for (size_t i = 0; i < items.size(); ++i) {
+        const AttnItem &it = items[i];
+        if (it.n_q <= 0) continue;
+        if (p.n == kMaxSegs)
+            if (pe_status s = flush()) return s;
+        p.segs[p.n++] = WeightSeg{static_cast<int32_t>(i), it.seq * cf.max_pages_per_seq, it.q_row0, it.n_q,
+                                  static_cast<int32_t>(c->len[it.seq])};
+        rows += it.n_q;
+        max_keys = std::max(max_keys, static_cast<int32_t>(c->len[it.seq]));
+    }
+    return flush();
+}
+
+// The arguments of a batched attention call, as items.
+pe_status batch_items(pe_cache *c, int32_t n, const int32_t *seqs, const int32_t *cu_q, std::vector<AttnItem> &items)
+{
+    if (cu_q[0] != 0) return fail(PE_ERR_INVALID, "cu_q[0] must be 0");
+    items.resize(n);
+    for (int32_t i = 0; i < n; ++i) {
+        if (pe_status s = check_seq(c, seqs[i])) return s;
+        const int32_t nq = cu_q[i + 1] - cu_q[i];
+        if (nq < 0) return fail(PE_ERR_INVALID, "cu_q must be non-decreasing");
+        if (nq > c->len[seqs[i]])
+            return fail(PE_ERR_RANGE, "sequence %d: n_q = %d exceeds its length %lld", seqs[i], nq,
+                        static_cast<long long>(c->len[seqs[i]]));
+        items[i] = AttnItem{seqs[i], cu_q[i], nq};
+    }
+    return PE_OK;
+}
+
+// ---- eviction
+struct EvictPlan {
+    int32_t row, seq;
+    int32_t len, keep;
+    int32_t first, n_new, old_n;   // logical index of the first replaced page, pages popped, pages before
+};
+
 pe_status check_attn_args(const pe_cache *c, int32_t layer, const void *Q, const void *out, int32_t hq, float scale,
                           bool has_rows = true)
 {
@@ -1633,12 +1776,13 @@ extern "C" {
 const char *pe_last_error(void) { return g_err.c_str(); }
 const char *pe_version(void) { return "pe 0.1 (sm_103a)"; }
 
-pe_status pe_cache_create(const pe_cache_config *cfg, pe_cache **out)
+static pe_status create_cache(const pe_cache_config *cfg, bool q8, pe_cache **out)
 {
     g_err.clear();
     if (!cfg || !out) return fail(PE_ERR_INVALID, "null argument");
     *out = nullptr;
     const pe_cache_config &c = *cfg;
+    if (q8 && (c.k_pool || c.v_pool)) return fail(PE_ERR_INVALID, "an 8-bit cache allocates its own pools");
     if (c.num_layers < 1 || c.num_kv_heads < 1 || c.num_pages < 1 || c.max_seqs < 1 || c.max_pages_per_seq < 1)
         return fail(PE_ERR_INVALID, "all counts must be positive");
     if (c.head_dim != 64 && c.head_dim != 128) return fail(PE_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
@@ -1677,7 +1821,8 @@ pe_status pe_cache_create(const pe_cache_config *cfg, pe_cache **out)
     cc->alive.assign(c.max_seqs, 0);
     cc->refs.assign(c.num_pages, 0);
     cc->ckpt.resize(c.max_seqs);
-    cc->pool_rows = pool_rows;
+    cc->q8 = q8;
+    cc->pool_rows = q8 ? pool_rows / c.num_layers : pool_rows;
     cc->ws_bytes = c.workspace_bytes > 0 ? c.workspace_bytes : (256ll << 20);  // (also sizes host-only plans)
     if (cc->host_only) {
         *out = cc;
@@ -1697,7 +1842,8 @@ pe_status pe_cache_create(const pe_cache_config *cfg, pe_cache **out)
         delete cc;
         return fail(PE_ERR_UNSUPPORTED, "kernels are built for sm_103a; device is sm_%d%d", major, minor);
     }
-    const size_t pool_bytes = static_cast<size_t>(pool_rows) * c.head_dim * 2;
+    const size_t pool_bytes = static_cast<size_t>(cc->pool_rows) * c.head_dim * 2;
+    const size_t code_bytes = static_cast<size_t>(pool_rows) * c.head_dim, exp_bytes = static_cast<size_t>(pool_rows / ps) * 2;
     const size_t table_bytes = static_cast<size_t>(c.max_seqs) * c.max_pages_per_seq * sizeof(int32_t);
     pe_status st = PE_OK;
     do {
@@ -1712,6 +1858,15 @@ pe_status pe_cache_create(const pe_cache_config *cfg, pe_cache **out)
             if ((e = cudaMemset(cc->k_pool, 0, pool_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
             if ((e = cudaMemset(cc->v_pool, 0, pool_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
         }
+        if (q8) {
+            if ((e = cudaMalloc(&cc->k8, code_bytes)) != cudaSuccess) { st = cuda_fail(e, "cudaMalloc K codes"); break; }
+            if ((e = cudaMalloc(&cc->v8, code_bytes)) != cudaSuccess) { st = cuda_fail(e, "cudaMalloc V codes"); break; }
+            if ((e = cudaMalloc(&cc->exps, exp_bytes)) != cudaSuccess) { st = cuda_fail(e, "cudaMalloc exponents"); break; }
+            // (no slot may hold a NaN V code, written or not: q8.cuh)
+            if ((e = cudaMemset(cc->k8, 0, code_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
+            if ((e = cudaMemset(cc->v8, 0, code_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
+            if ((e = cudaMemset(cc->exps, 0, exp_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
+        }
         if ((e = cudaMalloc(&cc->d_table, table_bytes)) != cudaSuccess) { st = cuda_fail(e, "cudaMalloc page table"); break; }
         if ((e = cudaMemset(cc->d_table, 0xFF, table_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
         if ((e = cudaMalloc(&cc->d_len, sizeof(int64_t) * c.max_seqs)) != cudaSuccess) { st = cuda_fail(e, "cudaMalloc"); break; }
@@ -1724,11 +1879,11 @@ pe_status pe_cache_create(const pe_cache_config *cfg, pe_cache **out)
         const size_t tickets = sizeof(int32_t) * ticket_count(c.num_kv_heads);
         if ((e = cudaMalloc(&cc->d_tickets, tickets)) != cudaSuccess) { st = cuda_fail(e, "cudaMalloc"); break; }
         if ((e = cudaMemset(cc->d_tickets, 0, tickets)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
-        if ((st = encode_2d(&cc->tm_k, cc->k_pool, c.head_dim, pool_rows, 64, ps)) != PE_OK) break;
-        if ((st = encode_2d(&cc->tm_v, cc->v_pool, c.head_dim, pool_rows, 64, ps)) != PE_OK) break;
+        if ((st = encode_2d(&cc->tm_k, cc->k_pool, c.head_dim, cc->pool_rows, 64, ps)) != PE_OK) break;
+        if ((st = encode_2d(&cc->tm_v, cc->v_pool, c.head_dim, cc->pool_rows, 64, ps)) != PE_OK) break;
         const uint32_t dec_rows = ps < kDecKeys ? ps : kDecKeys;
-        if ((st = encode_2d(&cc->tm_kd, cc->k_pool, c.head_dim, pool_rows, 64, dec_rows)) != PE_OK) break;
-        if ((st = encode_2d(&cc->tm_vd, cc->v_pool, c.head_dim, pool_rows, 64, dec_rows)) != PE_OK) break;
+        if ((st = encode_2d(&cc->tm_kd, cc->k_pool, c.head_dim, cc->pool_rows, 64, dec_rows)) != PE_OK) break;
+        if ((st = encode_2d(&cc->tm_vd, cc->v_pool, c.head_dim, cc->pool_rows, 64, dec_rows)) != PE_OK) break;
         if ((e = cudaDeviceSynchronize()) != cudaSuccess) { st = cuda_fail(e, "create sync"); break; }
     } while (false);
     if (st != PE_OK) {
@@ -1739,6 +1894,9 @@ pe_status pe_cache_create(const pe_cache_config *cfg, pe_cache **out)
     *out = cc;
     return PE_OK;
 }
+
+pe_status pe_cache_create(const pe_cache_config *cfg, pe_cache **out) { return create_cache(cfg, false, out); }
+pe_status pe_cache_create_q8(const pe_cache_config *cfg, pe_cache **out) { return create_cache(cfg, true, out); }
 
 pe_status pe_cache_destroy(pe_cache *cache)
 {
@@ -1969,7 +2127,7 @@ pe_status pe_replay_attn(pe_cache *c, int32_t seq, int32_t layer, const void *Q,
     if (n_q > c->len[seq])
         return fail(PE_ERR_RANGE, "n_q = %d exceeds the sequence length %lld", n_q, static_cast<long long>(c->len[seq]));
     if (n_q == 0) return PE_OK;
-    return run_attention(c, {AttnItem{seq, 0, n_q}}, layer, Q, n_q, out, num_q_heads, softmax_scale,
+    return attend(c, {AttnItem{seq, 0, n_q}}, layer, Q, n_q, out, num_q_heads, softmax_scale,
                          static_cast<cudaStream_t>(stream));
 }
 
@@ -1981,20 +2139,45 @@ pe_status pe_replay_attn_batch(pe_cache *c, int32_t n, const int32_t *seqs, int3
     if (n == 0) return PE_OK;
     pe_status s = check_attn_args(c, layer, Q_packed, out, num_q_heads, softmax_scale, cu_q[n] > 0);
     if (s != PE_OK) return s;
-    if (cu_q[0] != 0) return fail(PE_ERR_INVALID, "cu_q[0] must be 0");
-    std::vector<AttnItem> items(n);
-    for (int32_t i = 0; i < n; ++i) {
-        if ((s = check_seq(c, seqs[i])) != PE_OK) return s;
-        const int32_t nq = cu_q[i + 1] - cu_q[i];
-        if (nq < 0) return fail(PE_ERR_INVALID, "cu_q must be non-decreasing");
-        if (nq > c->len[seqs[i]])
-            return fail(PE_ERR_RANGE, "sequence %d: n_q = %d exceeds its length %lld", seqs[i], nq,
-                        static_cast<long long>(c->len[seqs[i]]));
-        items[i] = AttnItem{seqs[i], cu_q[i], nq};
-    }
+    std::vector<AttnItem> items;
+    if ((s = batch_items(c, n, seqs, cu_q, items)) != PE_OK) return s;
     if (cu_q[n] == 0) return PE_OK;
-    return run_attention(c, items, layer, Q_packed, cu_q[n], out, num_q_heads, softmax_scale,
-                         static_cast<cudaStream_t>(stream));
+    return attend(c, items, layer, Q_packed, cu_q[n], out, num_q_heads, softmax_scale, static_cast<cudaStream_t>(stream));
+}
+
+static pe_status attn_weights_batch(pe_cache *c, int32_t n, const int32_t *seqs, int32_t layer, const void *Q_packed,
+                                       const int32_t *cu_q, void *out, int32_t num_q_heads, float softmax_scale,
+                                       float *weights, int64_t weights_stride, void *stream)
+{
+    if (!c) return fail(PE_ERR_INVALID, "null cache");
+    if (n < 0 || (n > 0 && (!seqs || !cu_q))) return fail(PE_ERR_INVALID, "bad batch arguments");
+    if (n == 0) return PE_OK;
+    pe_status s = check_attn_args(c, layer, Q_packed, out, num_q_heads, softmax_scale, cu_q[n] > 0);
+    if (s != PE_OK) return s;
+    std::vector<AttnItem> items;
+    if ((s = batch_items(c, n, seqs, cu_q, items)) != PE_OK) return s;
+    if (cu_q[n] == 0) return PE_OK;
+    if (!weights || (reinterpret_cast<uintptr_t>(weights) & 3u)) return fail(PE_ERR_INVALID, "weights: null or misaligned pointer");
+    for (const AttnItem &it : items)
+        if (it.n_q > 0 && c->len[it.seq] > weights_stride)
+            return fail(PE_ERR_RANGE, "sequence %d: its length %lld exceeds weights_stride %lld", it.seq,
+                        static_cast<long long>(c->len[it.seq]), static_cast<long long>(weights_stride));
+    if (static_cast<int64_t>(cu_q[n]) * num_q_heads * 4 > c->ws_bytes)
+        return fail(PE_ERR_RANGE, "the query rows' log-sum-exp exceed the workspace");
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if ((s = attend(c, items, layer, Q_packed, cu_q[n], out, num_q_heads, softmax_scale, st)) != PE_OK) return s;
+    return add_weights(c, items, layer, Q_packed, num_q_heads, softmax_scale, weights, weights_stride, st);
+}
+
+pe_status pe_replay_attn_weights_batch(pe_cache *c, int32_t n, const int32_t *seqs, int32_t layer, const void *Q_packed,
+                                       const int32_t *cu_q, void *out, int32_t num_q_heads, float softmax_scale,
+                                       float *weights, int64_t weights_stride, void *stream)
+{
+    try {
+        return attn_weights_batch(c, n, seqs, layer, Q_packed, cu_q, out, num_q_heads, softmax_scale, weights, weights_stride, stream);
+    } catch (const std::bad_alloc &) {
+        return fail(PE_ERR_OOM, "host allocation failed");
+    }
 }
 
 pe_status pe_replay_rounds(pe_cache *c, int32_t n, const int32_t *seqs, int32_t n_rounds, const int32_t *take,
@@ -2079,8 +2262,8 @@ pe_status pe_replay_rounds(pe_cache *c, int32_t n, const int32_t *seqs, int32_t 
         if (c->host_only) continue;
         for (int32_t layer = 0; layer < c->cfg.num_layers; ++layer) {
             const int64_t off = static_cast<int64_t>(layer) * N * row_bytes;
-            s = run_attention(c, items, layer, static_cast<const char *>(Q) + off, N, static_cast<char *>(out) + off,
-                              num_q_heads, softmax_scale, st);
+            s = attend(c, items, layer, static_cast<const char *>(Q) + off, N, static_cast<char *>(out) + off, num_q_heads,
+                       softmax_scale, st);
             if (s != PE_OK) return tx.end(s);
         }
         after_merge = c->ends_in_merge;
@@ -2156,6 +2339,10 @@ pe_status pe_replay_attn_static_scratch(pe_cache *c, int32_t seq, int32_t layer,
     p.part_o = scratch;
     p.part_lse = scratch + prow * d;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (c->q8) {
+        p.layer = 0;
+        if ((s = unpack_layer(c, {AttnItem{seq, 0, n_q}}, layer, st)) != PE_OK) return s;
+    }
     if (injected_failure(c)) return launch_fault("replay attention");
     e = launch_replay_attn(d, true, tm_q, c->tm_k, c->tm_v, tm_q, p, st);
     if (e != cudaSuccess) return cuda_fail(e, "replay attention launch");
@@ -2220,9 +2407,223 @@ pe_status pe_seq_device_page_table(pe_cache *c, int32_t seq, int32_t *out, int32
 pe_status pe_cache_pools(const pe_cache *c, void **k_pool, void **v_pool)
 {
     if (!c) return fail(PE_ERR_INVALID, "null cache");
-    if (k_pool) *k_pool = c->k_pool;
-    if (v_pool) *v_pool = c->v_pool;
+    if (k_pool) *k_pool = stored_k(c);
+    if (v_pool) *v_pool = stored_v(c);
     return PE_OK;
+}
+
+pe_status pe_cache_scales(const pe_cache *c, void **exponents)
+{
+    if (!c || !exponents) return fail(PE_ERR_INVALID, "null argument");
+    if (!c->q8) return fail(PE_ERR_UNSUPPORTED, "a bf16 cache has no scales");
+    *exponents = c->exps;
+    return PE_OK;
+}
+
+pe_status pe_read_kv_batch(pe_cache *c, int32_t n, const int32_t *seqs, const int64_t *begins, const int32_t *cu_tokens,
+                           void *K_out, void *V_out, void *stream)
+{
+    if (pe_status s = check_device(c)) return s;
+    if (n < 0 || (n > 0 && (!seqs || !begins || !cu_tokens))) return fail(PE_ERR_INVALID, "bad batch arguments");
+    if (n > 0 && cu_tokens[0] != 0) return fail(PE_ERR_INVALID, "cu_tokens[0] must be 0");
+    for (int32_t i = 0; i < n; ++i) {
+        if (pe_status s = check_seq(c, seqs[i])) return s;
+        if (cu_tokens[i + 1] < cu_tokens[i]) return fail(PE_ERR_INVALID, "cu_tokens must be non-decreasing");
+        const int64_t cnt = cu_tokens[i + 1] - cu_tokens[i];
+        if (begins[i] < 0 || begins[i] > c->len[seqs[i]] || cnt > c->len[seqs[i]] - begins[i])
+            return fail(PE_ERR_RANGE, "sequence %d: tokens %lld + %lld exceed its length %lld", seqs[i],
+                        static_cast<long long>(begins[i]), static_cast<long long>(cnt), static_cast<long long>(c->len[seqs[i]]));
+    }
+    if (n == 0 || cu_tokens[n] == 0) return PE_OK;
+    if (c->host_only) return fail(PE_ERR_UNSUPPORTED, "a host-only cache holds no K and V");
+    if (!K_out || !V_out) return fail(PE_ERR_INVALID, "null K_out or V_out");
+    if (!aligned16(K_out) || !aligned16(V_out)) return fail(PE_ERR_INVALID, "K_out and V_out must be 16-byte aligned");
+    ReadParams p;
+    std::memset(static_cast<void *>(&p), 0, offsetof(ReadParams, segs));
+    p.page_table = c->d_table;
+    p.k_pool = stored_k(c);
+    p.v_pool = stored_v(c);
+    p.exps = c->exps;
+    p.K = static_cast<uint4 *>(K_out);
+    p.V = static_cast<uint4 *>(V_out);
+    p.L = c->cfg.num_layers;
+    p.hkv = c->cfg.num_kv_heads;
+    p.ps = c->cfg.page_size;
+    p.d = c->cfg.head_dim;
+    p.num_pages = c->cfg.num_pages;
+    p.n_total = cu_tokens[n];
+    for (int32_t i = 0; i < n;) {
+        for (p.n = p.seg_tokens = 0; i < n && p.n < kMaxSegs; ++i) {
+            const int32_t cnt = cu_tokens[i + 1] - cu_tokens[i];
+            if (cnt == 0) continue;
+            p.segs[p.n++] = ReadSeg{seqs[i] * c->cfg.max_pages_per_seq, static_cast<int32_t>(begins[i]), p.seg_tokens, cu_tokens[i]};
+            p.seg_tokens += cnt;
+        }
+        if (p.n == 0) continue;
+        if (injected_failure(c)) return launch_fault("read kernel");
+        cudaError_t e = launch_read_kv(c->q8, p, c->num_sms, static_cast<cudaStream_t>(stream));
+        if (e != cudaSuccess) return cuda_fail(e, "read kernel launch");
+        c->launches++;
+    }
+    return PE_OK;
+}
+
+static pe_status evict_batch(pe_cache *c, int32_t n, const int32_t *seqs, const int32_t *keep, int32_t sinks, int32_t recent,
+                             float *weights, int64_t weights_stride, int32_t *kept, int64_t kept_stride, void *stream)
+{
+    if (pe_status s = check_device(c)) return s;
+    if (n < 0 || (n > 0 && (!seqs || !keep))) return fail(PE_ERR_INVALID, "bad batch arguments");
+    if (sinks < 0 || recent < 0) return fail(PE_ERR_INVALID, "sinks and recent must not be negative");
+    if (!c->host_only && n > 0) {
+        if (weights_stride < 0 || kept_stride < 0 || kept_stride > INT32_MAX) return fail(PE_ERR_RANGE, "bad weights_stride or kept_stride");
+        if ((weights_stride > 0 && !weights) || (kept_stride > 0 && !kept) || (reinterpret_cast<uintptr_t>(weights) & 3u) ||
+            (reinterpret_cast<uintptr_t>(kept) & 3u))
+            return fail(PE_ERR_INVALID, "weights and kept: null or misaligned pointer");
+    }
+    const int ps = c->cfg.page_size;
+    std::vector<EvictPlan> plans;
+    std::vector<uint8_t> seen(c->cfg.max_seqs, 0);
+    int64_t need = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        if (pe_status s = check_seq(c, seqs[i])) return s;
+        if (seen[seqs[i]]) return fail(PE_ERR_INVALID, "sequence %d appears twice in the batch", seqs[i]);
+        seen[seqs[i]] = 1;
+        if (keep[i] < 0) return fail(PE_ERR_INVALID, "negative keep");
+        EvictPlan pl{};
+        pl.row = i;
+        pl.seq = seqs[i];
+        pl.len = static_cast<int32_t>(c->len[seqs[i]]);
+        pl.keep = std::min(keep[i], pl.len);
+        pl.old_n = static_cast<int32_t>(c->table[seqs[i]].size());
+        if (pl.keep < pl.len && static_cast<int64_t>(sinks) + recent > pl.keep)
+            return fail(PE_ERR_INVALID, "sequence %d: sinks + recent = %lld exceed keep = %d", pl.seq,
+                        static_cast<long long>(sinks) + recent, pl.keep);
+        if (!c->host_only) {
+            if (weights_stride < pl.len || kept_stride < pl.keep)
+                return fail(PE_ERR_RANGE, "sequence %d: weights_stride or kept_stride is below its %d or %d entries", pl.seq, pl.len, pl.keep);
+        }
+        if (pl.keep < pl.len) {
+            pl.first = std::min(sinks, pl.keep) / ps;  // pages wholly of sinks stay
+            pl.n_new = static_cast<int32_t>(ceil_div(pl.keep, ps)) - pl.first;
+            need += pl.n_new;
+        }
+        plans.push_back(pl);
+    }
+    if (need > static_cast<int64_t>(c->free_stack.size()))
+        return fail(PE_ERR_OOM, "eviction needs %lld pages, %zu free", static_cast<long long>(need), c->free_stack.size());
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    CallTxn tx(c, st);
+    // bookkeeping: every new page is popped before any old one is given back, since the copies read the old ones
+    // (nothing is allocated after the first change: a table only gets shorter, the free list holds every page)
+    std::vector<std::vector<int32_t>> fresh(plans.size());
+    c->jr.popped.reserve(static_cast<size_t>(need));
+    for (size_t i = 0; i < plans.size(); ++i) {
+        if (plans[i].keep >= plans[i].len) continue;
+        j_seq(c, plans[i].seq, plans[i].first);
+        fresh[i].reserve(plans[i].n_new);
+    }
+    for (size_t i = 0; i < plans.size(); ++i) {
+        if (plans[i].keep >= plans[i].len) continue;
+        for (int32_t k = 0; k < plans[i].n_new; ++k) {
+            fresh[i].push_back(free_pop(c));
+            set_ref(c, fresh[i].back(), 1);
+        }
+    }
+    for (size_t i = 0; i < plans.size(); ++i) {
+        const EvictPlan &pl = plans[i];
+        if (pl.keep >= pl.len) continue;
+        std::vector<int32_t> &t = c->table[pl.seq];
+        for (int32_t e = pl.old_n - 1; e >= pl.first; --e) {
+            set_ref(c, t[e], c->refs[t[e]] - 1);
+            if (c->refs[t[e]] == 0) free_push(c, t[e]);
+        }
+        t.resize(pl.first);
+        t.insert(t.end(), fresh[i].begin(), fresh[i].end());
+        c->len[pl.seq] = pl.keep;
+        std::vector<int64_t> &ck = c->ckpt[pl.seq];
+        while (!ck.empty() && ck.back() > std::min(sinks, pl.keep)) ck.pop_back();
+    }
+    EvictParams p;
+    std::memset(static_cast<void *>(&p), 0, offsetof(EvictParams, segs));
+    p.page_table = c->d_table;
+    p.seq_len = c->d_len;
+    p.k_pool = stored_k(c);
+    p.v_pool = stored_v(c);
+    p.exps = c->exps;
+    p.weights = weights;
+    p.kept = kept;
+    p.weights_stride = weights_stride;
+    p.kept_stride = kept_stride;
+    p.L = c->cfg.num_layers;
+    p.hkv = c->cfg.num_kv_heads;
+    p.ps = ps;
+    p.num_pages = c->cfg.num_pages;
+    p.kept_cols = static_cast<int32_t>(kept_stride);
+    auto seg_of = [&](const EvictPlan &pl) {
+        EvictSeg sg{};
+        sg.row = pl.row;
+        sg.seq = pl.seq;
+        sg.table_row = pl.seq * c->cfg.max_pages_per_seq;
+        sg.len = pl.len;
+        sg.keep = pl.keep;
+        sg.sinks = sinks;
+        sg.recent = recent;
+        sg.old_n = pl.old_n;
+        return sg;
+    };
+    auto step = [&](const char *what, auto launch) -> pe_status {
+        if (injected_failure(c)) return launch_fault(what);
+        if (c->host_only) return PE_OK;
+        cudaError_t e = launch();
+        if (e != cudaSuccess) return cuda_fail(e, what);
+        c->launches++;
+        return PE_OK;
+    };
+    pe_status s = PE_OK;
+    for (size_t i = 0; i < plans.size(); i += kMaxSegs) {
+        for (p.n = 0; p.n < kMaxSegs && i + p.n < plans.size(); ++p.n) p.segs[p.n] = seg_of(plans[i + p.n]);
+        if ((s = step("evict select", [&] { return launch_evict_select(p, st); })) != PE_OK) return tx.end(s);
+    }
+    // The copies, and after each group of new pages their table entries: a row moves from a position no lower than its
+    // own, so the entries replaced so far are none that a later group's copies read through.
+    p.n = p.n_new = 0;
+    auto flush = [&]() -> pe_status {
+        if (p.n_new == 0) return PE_OK;
+        pe_status r = step("evict copy", [&] { return launch_evict_copy(c->q8, c->cfg.head_dim, p, st); });
+        if (r == PE_OK) r = step("evict table", [&] { return launch_evict_table(p, st); });
+        p.n = p.n_new = 0;
+        return r;
+    };
+    for (size_t i = 0; i < plans.size(); ++i) {
+        for (int32_t done = 0; done < plans[i].n_new;) {
+            if (p.n == kMaxSegs || p.n_new == kAppendMaxPages)
+                if ((s = flush()) != PE_OK) return tx.end(s);
+            EvictSeg sg = seg_of(plans[i]);
+            sg.first_lp = plans[i].first + done;
+            sg.new0 = p.n_new;
+            sg.n_new = std::min(plans[i].n_new - done, kAppendMaxPages - p.n_new);
+            std::copy_n(fresh[i].begin() + done, sg.n_new, p.new_pages + p.n_new);
+            p.n_new += sg.n_new;
+            done += sg.n_new;
+            p.segs[p.n++] = sg;
+        }
+    }
+    if ((s = flush()) != PE_OK) return tx.end(s);
+    for (size_t i = 0; i < plans.size(); i += kMaxSegs) {
+        for (p.n = 0; p.n < kMaxSegs && i + p.n < plans.size(); ++p.n) p.segs[p.n] = seg_of(plans[i + p.n]);
+        if ((s = step("evict finish", [&] { return launch_evict_finish(p, st); })) != PE_OK) return tx.end(s);
+    }
+    return tx.end(PE_OK);
+}
+
+pe_status pe_evict_batch(pe_cache *c, int32_t n, const int32_t *seqs, const int32_t *keep, int32_t sinks, int32_t recent,
+                         float *weights, int64_t weights_stride, int32_t *kept, int64_t kept_stride, void *stream)
+{
+    try {
+        return evict_batch(c, n, seqs, keep, sinks, recent, weights, weights_stride, kept, kept_stride, stream);
+    } catch (const std::bad_alloc &) {
+        return fail(PE_ERR_OOM, "host allocation failed");
+    }
 }
 
 pe_status pe_set_option(pe_cache *c, const char *key, int64_t value)

@@ -5,6 +5,7 @@
 #include <atomic>
 #include <cstdint>
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 namespace pe {
@@ -44,6 +45,7 @@ struct AppendParamsT {
     int32_t L, hkv, dvec, ps, num_pages, n_total, n_segs, seg_tokens;
     int32_t n_new;         // page ids carried
     int32_t beside;        // 1: runs beside the decode merge launched just before (append_kv_kernel)
+    int8_t *exps;          // 8-bit cache: scale exponents [L][num_pages][Hkv][2] (K, V); the pools hold codes
     AppendSeg segs[SEGS];
     int32_t new_pages[PAGES];
 };
@@ -59,9 +61,85 @@ struct CowCopy {
 struct CowParams {
     uint4 *k_pool;
     uint4 *v_pool;
+    int8_t *exps;          // 8-bit cache: scale exponents, copied too (else null)
     int32_t *page_table;
     int32_t n, L, hkv, ps, dvec, num_pages;
     CowCopy copies[kMaxSegs];
+};
+
+// ---------------------------------------------------------------- 8-bit cache
+struct UnpackSeg {
+    int32_t table_row;     // seq * max_pages_per_seq
+    int32_t page0;         // first block of this sequence (a block per page)
+};
+
+// One layer's codes of the listed sequences' pages as bf16, at the same page ids.
+struct UnpackParams {
+    const int32_t *page_table;
+    const uint4 *k8, *v8;  // codes [L][num_pages][Hkv][ps][d]
+    const int8_t *exps;    // [L][num_pages][Hkv][2]
+    uint4 *k, *v;          // bf16 [num_pages][Hkv][ps][d]
+    int32_t n, layer, hkv, ps, d, num_pages;
+    UnpackSeg segs[kMaxSegs];
+};
+
+struct ReadSeg {
+    int32_t table_row;
+    int32_t begin;         // first token read
+    int32_t cum0;          // prefix of tokens inside this launch
+    int32_t tok0;          // first row of K / V
+};
+
+struct ReadParams {
+    const int32_t *page_table;
+    const void *k_pool, *v_pool;
+    const int8_t *exps;    // 8-bit cache only
+    uint4 *K, *V;          // bf16 [L][n_total][Hkv][d]
+    int32_t n, L, hkv, ps, d, num_pages, n_total, seg_tokens;
+    ReadSeg segs[kMaxSegs];
+};
+
+// ---------------------------------------------------------------- eviction
+struct EvictSeg {
+    int32_t row;           // of weights and kept
+    int32_t seq, table_row;
+    int32_t len, keep;     // tokens before and after
+    int32_t sinks, recent;
+    int32_t old_n;         // pages before
+    int32_t first_lp;      // logical index of the first new page in this launch
+    int32_t new0, n_new;   // this launch's new pages of the sequence, in new_pages
+};
+
+struct EvictParams {
+    int32_t *page_table;
+    int64_t *seq_len;
+    void *k_pool, *v_pool;
+    int8_t *exps;          // 8-bit cache only
+    float *weights;        // [rows][weights_stride]
+    int32_t *kept;         // [rows][kept_stride]
+    int64_t weights_stride, kept_stride;
+    int32_t n, L, hkv, ps, num_pages, n_new, kept_cols;
+    EvictSeg segs[kMaxSegs];
+    int32_t new_pages[kAppendMaxPages];
+};
+
+// ---------------------------------------------------------------- accumulated weights
+struct WeightSeg {
+    int32_t row;           // of weights
+    int32_t table_row;
+    int32_t q_row0, n_q, n_keys;
+};
+
+struct WeightParams {
+    const int32_t *page_table;
+    const __nv_bfloat16 *q;  // bf16 [rows][Hq][d]
+    const __nv_bfloat16 *k;  // bf16 [num_pages][Hkv][ps][d], one layer
+    float *lse;            // workspace [rows][Hq], log2 units
+    float *weights;        // [rows][weights_stride]
+    int64_t weights_stride;
+    int32_t n, hq, hkv, group, ps;
+    float scale_log2;
+    WeightSeg segs[kMaxSegs];
 };
 
 // ---------------------------------------------------------------- crop
@@ -86,6 +164,7 @@ struct CropParamsT {
     uint4 *k_pool;
     uint4 *v_pool;
     int32_t n, poison, L, hkv, ps, dvec, num_pages;
+    uint32_t poison_word;  // debug poison: what a word of a freed slot becomes
     CropSeg segs[SEGS];
     int32_t freed[FREED];
 };
@@ -229,6 +308,17 @@ cudaError_t launch_replay_attn_sk(int head_dim, const CUtensorMap &tm_q, const C
 // counts 128-key tiles); otherwise CUDA cores, 64-key tiles.
 cudaError_t launch_decode_attn(int head_dim, int rows_cap, bool tensor_core, const CUtensorMap &tm_k,
                                const CUtensorMap &tm_v, const DecodeParams &p, cudaStream_t st);
+// 8-bit cache: p's pools hold codes, p.exps their scales, p.segs[].cum0 and p.seg_tokens count touched pages.
+cudaError_t launch_append_q8(int head_dim, const AppendParams &p, cudaStream_t st);
+cudaError_t launch_unpack_q8(const UnpackParams &p, int pages, cudaStream_t st);
+cudaError_t launch_read_kv(bool q8, const ReadParams &p, int num_sms, cudaStream_t st);
+// Eviction, in this order on one stream; copy and table once for each group of new pages.
+cudaError_t launch_evict_select(const EvictParams &p, cudaStream_t st);
+cudaError_t launch_evict_copy(bool q8, int head_dim, const EvictParams &p, cudaStream_t st);
+cudaError_t launch_evict_table(const EvictParams &p, cudaStream_t st);
+cudaError_t launch_evict_finish(const EvictParams &p, cudaStream_t st);
+// q_rows: query rows of the launch's sequences (consecutive from segs[0].q_row0).
+cudaError_t launch_weights(int head_dim, const WeightParams &p, int64_t q_rows, int max_keys, cudaStream_t st);
 cudaError_t launch_bounded_wait_selftest(int32_t *status, uint64_t limit_ns, cudaStream_t st);
 
 // Raises `kernel`'s dynamic shared-memory limit to `bytes` on the current

@@ -14,9 +14,6 @@
 
 namespace pe {
 
-// The finite poison written by the debug crop: bf16 2^100 (0x7180) in every lane.
-constexpr uint32_t kPoisonPair = 0x71807180u;
-
 __device__ __forceinline__ uint4 ld_stream(const uint4 *p)
 {
     uint4 v;
@@ -139,7 +136,7 @@ __global__ void __launch_bounds__(256) crop_kernel(const __grid_constant__ Param
     const CropSeg &sg = p.segs[blockIdx.x];
     int32_t *row = p.page_table + sg.table_row;
     if (p.poison) {
-        const uint4 poison = make_uint4(kPoisonPair, kPoisonPair, kPoisonPair, kPoisonPair);
+        const uint4 poison = make_uint4(p.poison_word, p.poison_word, p.poison_word, p.poison_word);
         const int slot_chunks = p.dvec;                          // chunks per (page, head, slot)
         const int page_chunks = p.hkv * p.ps * slot_chunks;      // per (layer, page)
         for (int e = 0; e < sg.n_freed; ++e) {
@@ -236,6 +233,9 @@ __global__ void __launch_bounds__(128) cow_copy_kernel(const __grid_constant__ C
         p.k_pool[d_base + i] = p.k_pool[s_base + i];
         p.v_pool[d_base + i] = p.v_pool[s_base + i];
     }
+    if (p.exps && threadIdx.x == 0)
+        reinterpret_cast<char2 *>(p.exps)[(static_cast<int64_t>(l) * p.num_pages + c.dst) * p.hkv + h] =
+            reinterpret_cast<const char2 *>(p.exps)[(static_cast<int64_t>(l) * p.num_pages + c.src) * p.hkv + h];
     if (blockIdx.x == 0 && threadIdx.x == 0) p.page_table[c.entry] = c.dst;
 }
 
