@@ -195,7 +195,7 @@ pe_status pe_replay_attn_batch(pe_cache *cache, int32_t n, const int32_t *seqs, 
  * of weights_stride >= the sequence's length entries; entries past the length
  * and rows of sequences without queries are not touched.  Held and summed in
  * 32 bits, in an order that does not depend on timing.  `out` as in
- * pe_replay_attn_batch (the same values).  weights must not overlap Q or out.
+ * pe_replay_attn_batch.  weights must not overlap Q or out.
  * Errors: those of pe_replay_attn_batch; INVALID (weights null or not 4-byte
  * aligned), RANGE (weights_stride below a length; n_q x num_q_heads x 4 bytes
  * above the cache's workspace). */
@@ -444,8 +444,9 @@ pe_status pe_attn_plan_persistent(pe_cache *cache, int32_t n, const int32_t *seq
  * partial row part_row0 + ((q-tile x Hkv + kv-head) x n_splits + split) x 128
  * + r for row r, and its combine merges, for each of its combine rows
  * comb0 + (q-tile x Hkv + kv-head) x 128 + r, the n_splits rows from there.
- * Errors: INVALID, RANGE (cap below *n_words, n_q > len), UNSUPPORTED.  The
- * paper has no counterpart: this plans the build's own kernels. */
+ * Errors: INVALID, RANGE (cap below *n_words, n_q > len), UNSUPPORTED (among
+ * others an 8-bit cache).  The paper has no counterpart: this plans the
+ * build's own kernels. */
 pe_status pe_attn_plan_launches(pe_cache *cache, int32_t n, const int32_t *seqs, const int32_t *cu_q,
                                 int32_t num_q_heads, int32_t num_sms, int64_t *words, int64_t cap,
                                 int64_t *n_words);

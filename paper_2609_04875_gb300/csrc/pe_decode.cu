@@ -42,7 +42,6 @@ constexpr int kConsumers = 32 * kDecWarps;
 constexpr int kDecThreads = kConsumers + 32;       // + producer warp
 constexpr int kDecStages = 3;
 constexpr int kBarConsumers = 1;                   // named barrier of the consumer warps
-constexpr int kStatusBadPage = 2;                  // device status: page id outside the pool
 
 // Every split of a (sequence, kv-head) has written its partial (O, m, l) for
 // the RB rows: O unnormalised [RB][HD], m the running max (log2 units), l the

@@ -130,6 +130,8 @@ struct pe_cache {
     int64_t pool_rows = 0;  // rows of k_pool: L (8-bit cache: 1) * num_pages * Hkv * ps
     CUtensorMap tm_k{}, tm_v{};    // tensor-core kernel: 64 x ps boxes
     CUtensorMap tm_kd{}, tm_vd{};  // decode kernel: 64 x min(ps, 64) boxes
+    CUtensorMap tm_k8{}, tm_v8{};  // 8-bit cache: d x ps boxes of codes
+    int64_t code_rows = 0;         // rows of k8: L * num_pages * Hkv * ps
     // options
     int splitkv = -1, num_splits = 0, debug_poison = 0, decode_kernel = 1;
     int dec_chunks_per_sm = 0;    // decode chunks per SM (0 = the length with the earliest estimated finish)
@@ -306,6 +308,22 @@ pe_status encode_2d(CUtensorMap *m, void *base, uint64_t cols, uint64_t rows, ui
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(PE_ERR_CUDA, "cuTensorMapEncodeTiled (2d) failed: %d", static_cast<int>(r));
+    return PE_OK;
+}
+
+// The codes as [rows][d]: a box is one page of one kv-head.
+pe_status encode_codes(CUtensorMap *m, void *base, int d, uint64_t rows, uint32_t box_rows)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return fail(PE_ERR_CUDA, "cuTensorMapEncodeTiled unavailable");
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(d), rows};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(d)};
+    cuuint32_t box[2] = {static_cast<cuuint32_t>(d), box_rows};
+    cuuint32_t es[2] = {1, 1};
+    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(PE_ERR_CUDA, "cuTensorMapEncodeTiled (codes) failed: %d", static_cast<int>(r));
     return PE_OK;
 }
 
@@ -685,32 +703,35 @@ struct AttnItem {
 // chunk length that gives every SM one or two equal chunks (94 tiles x 8 kv-heads: 152 chunks of at most
 // 5 tiles, not 376 of 2: 20.8 -> 17.4 us a layer with its merge); one of many tiles (more than 12 per SM)
 // takes 8, where a chunk's cost is least and the estimates hardly differ (16 agents, 5200 tiles: 67.4 us
-// with 7 or 8, 4.6 % more with 6).
+// with 7 or 8, 4.6 % more with 6).  tiles_of(i): sequence i's tiles, items_of(i): its items, each all those tiles;
+// tiles: of all items; longest: the longest chunk, taken from `many` tiles per SM on.
 constexpr double kDecChunkCost = 0.35;
-int64_t decode_chunk_tiles(const pe_cache *c, const std::vector<AttnItem> &items, size_t lo, size_t hi, int64_t tiles)
+template <typename Tiles, typename Items>
+int64_t chunk_tiles(const pe_cache *c, size_t lo, size_t hi, const Tiles &tiles_of, const Items &items_of, int64_t tiles,
+                    int64_t longest, int64_t many, double chunk_cost)
 {
-    const int64_t hkv = c->cfg.num_kv_heads, N = c->num_sms;
-    if (tiles > 12 * N) return 8;  // many tiles per SM: the longest chunks
-    int64_t best = 8;
+    const int64_t N = c->num_sms;
+    if (tiles > many * N) return longest;  // many tiles per SM: the longest chunks
+    int64_t best = longest;
     double best_t = 1e30;
-    for (int64_t ct = 8; ct >= 1; --ct) {
+    for (int64_t ct = longest; ct >= 1; --ct) {
         int64_t F = 0, R = 0, rem_tiles = 0, rem_max = 0, cpi = 1;
         for (size_t i = lo; i < hi; ++i) {
-            const int64_t nt = ceil_div(c->len[items[i].seq], 128), rem = nt % ct;
+            const int64_t nt = tiles_of(i), rem = nt % ct, hkv = items_of(i);
             F += nt / ct * hkv;
             R += rem ? hkv : 0;
             rem_tiles += rem * hkv;
             rem_max = std::max(rem_max, rem);
             cpi = std::max(cpi, ceil_div(nt, ct));
         }
-        const double U = static_cast<double>(ct) + kDecChunkCost;
+        const double U = static_cast<double>(ct) + chunk_cost;
         const int64_t rounds = ceil_div(F, N), idle = rounds * N - F;
-        const double rem_cost = static_cast<double>(rem_tiles) + static_cast<double>(R) * kDecChunkCost;
+        const double rem_cost = static_cast<double>(rem_tiles) + static_cast<double>(R) * chunk_cost;
         double t = static_cast<double>(rounds) * U;
         // remainders beyond what the idle SMs of the last round hold (each at least one)
         const double room = static_cast<double>(idle) * U;
         if (R > 0 && (idle == 0 || rem_cost > room))
-            t += std::max((rem_cost - room) / static_cast<double>(N), static_cast<double>(rem_max) + kDecChunkCost - (idle > 0 ? U : 0.0));
+            t += std::max((rem_cost - room) / static_cast<double>(N), static_cast<double>(rem_max) + chunk_cost - (idle > 0 ? U : 0.0));
         t += 0.1 * static_cast<double>(ceil_div(cpi, 32));  // the merge's round trips
         if (t < best_t - 1e-9) {
             best_t = t;
@@ -718,6 +739,13 @@ int64_t decode_chunk_tiles(const pe_cache *c, const std::vector<AttnItem> &items
         }
     }
     return best;
+}
+
+int64_t decode_chunk_tiles(const pe_cache *c, const std::vector<AttnItem> &items, size_t lo, size_t hi, int64_t tiles)
+{
+    return chunk_tiles(
+        c, lo, hi, [&](size_t i) { return ceil_div(c->len[items[i].seq], 128); },
+        [&](size_t) { return static_cast<int64_t>(c->cfg.num_kv_heads); }, tiles, 8, 12, kDecChunkCost);
 }
 
 // Decode kernel launches (groups of kMaxSegs sequences).  Key splits: about two
@@ -1673,18 +1701,207 @@ pe_status unpack_layer(pe_cache *c, const std::vector<AttnItem> &items, int32_t 
     return flush();
 }
 
-// The attention of every call: 8-bit caches by way of the unpacked layer.
+// ---- 8-bit cache: attention of few rows on the codes
+// Queries [q_row0, q_row0 + n_q) of Q, the last of which sees n_keys keys.
+struct Q8Item {
+    int32_t seq;
+    int32_t q_row0, n_q, n_keys;
+    int32_t row;  // of weights
+};
+
+// A chunk's cost besides its tiles, in tiles (kDecChunkCost).
+constexpr double kQ8ChunkCost = 0.7;
+
+// Rows (n_q x group) up to which the codes are attended as they are.  Beyond, a sequence's keys are read once per
+// block of 16 rows, and unpacking them once costs less.
+constexpr int64_t kQ8MaxRows = 16;
+
+bool q8_takes(const pe_cache *c, int64_t n_q, int g)
+{
+    return c->decode_kernel == 1 && c->splitkv != 0 && n_q * g <= kQ8MaxRows;
+}
+
+// One launch over items [lo, hi), at most kMaxSegs: fills p.  ws: floats of workspace for partials and, with `scores`,
+// the rows' scores, which then begin at *scores_at.  False when they do not fit.
+bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, size_t hi, int g, bool scores, int64_t ws,
+             Q8AttnParams &p, int &rb, int64_t *scores_at)
+{
+    const pe_cache_config &cf = c->cfg;
+    const int hkv = cf.num_kv_heads, d = cf.head_dim;
+    int64_t max_rows = 1, tiles = 0;
+    for (size_t i = lo; i < hi; ++i) max_rows = std::max<int64_t>(max_rows, static_cast<int64_t>(items[i].n_q) * g);
+    rb = max_rows <= 4 ? 4 : (max_rows <= 8 ? 8 : 16);
+    auto tiles_of = [&](size_t i) { return ceil_div(items[i].n_keys, 128); };
+    auto items_of = [&](size_t i) { return ceil_div(static_cast<int64_t>(items[i].n_q) * g, rb) * hkv; };
+    for (size_t i = lo; i < hi; ++i) tiles += tiles_of(i) * items_of(i);
+    int64_t longest_item = 1;
+    for (size_t i = lo; i < hi; ++i) longest_item = std::max(longest_item, tiles_of(i));
+    int64_t ct = c->dec_chunks_per_sm > 0
+                     ? std::min<int64_t>(kQ8MaxChunk, std::max<int64_t>(1, ceil_div(tiles, c->dec_chunks_per_sm * static_cast<int64_t>(c->num_sms))))
+                     : chunk_tiles(c, lo, hi, tiles_of, items_of, tiles, kQ8MaxChunk, 24, kQ8ChunkCost);
+    if (c->splitkv == 1 && c->num_splits > 0) ct = std::min<int64_t>(kQ8MaxChunk, ceil_div(longest_item, c->num_splits));
+    std::memset(static_cast<void *>(&p), 0, offsetof(Q8AttnParams, seqs));
+    for (;; ct = kQ8MaxChunk) {
+        int64_t chunks = 0, n_items = 0, score = 0;
+        p.n_seqs = p.n_rem = p.any_split = 0;
+        for (size_t i = lo; i < hi; ++i) {
+            const Q8Item &it = items[i];
+            const int64_t nt = tiles_of(i), per = items_of(i);
+            Q8Seq &q = p.seqs[p.n_seqs];
+            q = Q8Seq{};
+            q.table_row = it.seq * cf.max_pages_per_seq;
+            q.q_row0 = it.q_row0;
+            q.n_q = it.n_q;
+            q.n_keys = it.n_keys;
+            q.n_blocks = static_cast<int32_t>(per / hkv);
+            q.ct = static_cast<int32_t>(ct);
+            q.full0 = static_cast<int32_t>(std::min<int64_t>(chunks, INT32_MAX));
+            q.rem0 = -1;
+            q.item0 = static_cast<int32_t>(std::min<int64_t>(n_items, INT32_MAX));
+            q.score_stride = static_cast<int32_t>(nt * 128);
+            q.score0 = score;
+            if (scores) score += static_cast<int64_t>(hkv) * it.n_q * g * nt * 128;
+            if (nt > ct) p.any_split = 1;
+            chunks += nt / ct * per;
+            n_items += per;
+            if (nt % ct) {  // insertion by decreasing remainder, stable
+                int j = p.n_rem++;
+                for (; j > 0 && tiles_of(lo + p.rem_seq[j - 1]) % ct < nt % ct; --j) p.rem_seq[j] = p.rem_seq[j - 1];
+                p.rem_seq[j] = p.n_seqs;
+            }
+            p.n_seqs++;
+        }
+        p.full_chunks = static_cast<int32_t>(std::min<int64_t>(chunks, INT32_MAX));
+        for (int j = 0; j < p.n_rem; ++j) {
+            p.seqs[p.rem_seq[j]].rem0 = static_cast<int32_t>(std::min<int64_t>(chunks, INT32_MAX));
+            chunks += items_of(lo + p.rem_seq[j]);
+        }
+        const int64_t part = p.any_split ? ceil_div(chunks * rb * (d + 2), 64) * 64 : 0;
+        if (part + score <= ws && chunks <= INT32_MAX / 64 && n_items <= INT32_MAX / 64) {
+            *scores_at = part;
+            p.total_chunks = static_cast<int32_t>(chunks);
+            p.total_items = static_cast<int32_t>(n_items);
+            break;
+        }
+        if (ct == kQ8MaxChunk) return false;
+    }
+    p.total_ctas = std::min<int32_t>(p.total_chunks, c->num_sms);
+    p.page_table = c->d_table;
+    p.exps = c->exps;
+    p.sched = c->d_tickets + kMaxSegs * hkv;
+    p.status = c->d_status;
+    p.hkv = hkv;
+    p.hq = hkv * g;
+    p.group = g;
+    p.num_pages = cf.num_pages;
+    p.ps = cf.page_size;
+    p.oob_row = static_cast<int32_t>(c->code_rows);
+    return true;
+}
+
+// Attends the items on the codes, in as few launches as the parameter block and the workspace allow; what does not fit
+// (a single sequence's partials, or one query's scores) goes to `left`.  weights: also adds the softmax weights
+// (out may then be null).
+pe_status run_q8(pe_cache *c, std::vector<Q8Item> items, int32_t layer, const void *Q, int64_t q_rows, void *out, int32_t hq,
+                 float scale, float *weights, int64_t stride, std::vector<Q8Item> *left, cudaStream_t st)
+{
+    const int g = hq / c->cfg.num_kv_heads;
+    const int64_t lse = weights ? ceil_div(q_rows * hq, 64) * 64 : 0;  // floats, before the partials
+    const int64_t ws = c->ws_bytes / 4 - lse;
+    Q8AttnParams p;
+    for (size_t lo = 0; lo < items.size();) {
+        size_t hi = std::min(items.size(), lo + kMaxSegs);
+        int rb = 0;
+        int64_t scores_at = 0;
+        while (!plan_q8(c, items, lo, hi, g, weights != nullptr, ws, p, rb, &scores_at)) {
+            if (hi - lo > 1) {
+                hi = lo + (hi - lo) / 2;
+                continue;
+            }
+            Q8Item &it = items[lo];
+            if (!weights || it.n_q == 1) {
+                left->push_back(it);
+                hi = lo;
+                break;
+            }
+            // the first half of its queries now, the others next
+            Q8Item rest = it;
+            const int32_t half = it.n_q / 2;
+            it.n_keys -= it.n_q - half;
+            it.n_q = half;
+            rest.q_row0 += half;
+            rest.n_q -= half;
+            items.insert(items.begin() + lo + 1, rest);
+        }
+        if (hi == lo) {
+            ++lo;
+            continue;
+        }
+        p.layer = layer;
+        p.q = static_cast<const __nv_bfloat16 *>(Q);
+        p.out = static_cast<__nv_bfloat16 *>(out);
+        p.scale_log2 = scale * 1.4426950408889634f;
+        p.part = c->d_ws + lse;
+        p.lse = weights ? c->d_ws : nullptr;
+        p.scores = weights ? p.part + scores_at : nullptr;
+        c->last_split = p.any_split;
+        c->last_splits = static_cast<int32_t>(ceil_div(ceil_div(p.seqs[0].n_keys, 128), p.seqs[0].ct));
+        c->last_ctas = p.total_ctas;
+        if (injected_failure(c)) return launch_fault("8-bit attention");
+        cudaError_t e = launch_attn_q8(c->cfg.head_dim, rb, c->tm_k8, c->tm_v8, p, st);
+        if (e != cudaSuccess) return cuda_fail(e, "8-bit attention launch");
+        c->launches += p.any_split ? 2 : 1;
+        c->ends_in_merge = false;
+        if (weights) {
+            WeightParams w;
+            std::memset(static_cast<void *>(&w), 0, offsetof(WeightParams, segs));
+            w.lse = p.lse;
+            w.scores = p.scores;
+            w.weights = weights;
+            w.weights_stride = stride;
+            w.hq = hq;
+            w.hkv = c->cfg.num_kv_heads;
+            w.group = g;
+            int32_t max_keys = 0;
+            for (size_t i = lo; i < hi; ++i) {
+                const Q8Seq &q = p.seqs[i - lo];
+                w.segs[w.n++] = WeightSeg{items[i].row, q.table_row, q.q_row0, q.n_q, q.n_keys, q.score_stride, q.score0};
+                max_keys = std::max(max_keys, q.n_keys);
+            }
+            if (injected_failure(c)) return launch_fault("weights kernel");
+            if ((e = launch_weights_kept(w, max_keys, st)) != cudaSuccess) return cuda_fail(e, "weights kernel launch");
+            c->launches++;
+        }
+        lo = hi;
+    }
+    return PE_OK;
+}
+
+// The attention of every call.  8-bit caches: few rows on the codes, the others by way of the unpacked layer.
 pe_status attend(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer, const void *Q, int64_t q_rows, void *out,
                  int32_t hq, float scale, cudaStream_t st)
 {
     if (!c->q8) return run_attention(c, items, layer, Q, q_rows, out, hq, scale, st);
-    if (pe_status s = unpack_layer(c, items, layer, st)) return s;
-    return run_attention(c, items, 0, Q, q_rows, out, hq, scale, st);
+    const int g = hq / c->cfg.num_kv_heads;
+    std::vector<Q8Item> few, left;
+    std::vector<AttnItem> many;
+    for (const AttnItem &it : items) {
+        if (it.n_q <= 0) continue;
+        if (q8_takes(c, it.n_q, g)) few.push_back(Q8Item{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq]), 0});
+        else many.push_back(it);
+    }
+    if (!few.empty()) {
+        if (pe_status s = run_q8(c, std::move(few), layer, Q, q_rows, out, hq, scale, nullptr, 0, &left, st)) return s;
+        for (const Q8Item &it : left) many.push_back(AttnItem{it.seq, it.q_row0, it.n_q});
+    }
+    if (many.empty()) return PE_OK;
+    if (pe_status s = unpack_layer(c, many, layer, st)) return s;
+    return run_attention(c, many, 0, Q, q_rows, out, hq, scale, st);
 }
 
-// Adds the items' softmax weights to `weights` (row i: item i), after the attention of the same call, whose layer is
-// still unpacked.  The workspace holds the query rows' log-sum-exp.
-pe_status add_weights(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer, const void *Q, int32_t hq, float scale,
+// Adds the items' softmax weights to `weights` from K in bf16: the bf16 cache's, or the unpacked layer.  The workspace
+// holds the query rows' log-sum-exp.
+pe_status add_weights(pe_cache *c, const std::vector<Q8Item> &items, int32_t layer, const void *Q, int32_t hq, float scale,
                       float *weights, int64_t stride, cudaStream_t st)
 {
     const pe_cache_config &cf = c->cfg;
@@ -1715,17 +1932,45 @@ pe_status add_weights(pe_cache *c, const std::vector<AttnItem> &items, int32_t l
         rows = 0;
         return PE_OK;
     };
+    for (const Q8Item &it : items) {
+        // (a launch's query rows are consecutive: not so where an item between two was attended otherwise)
+        if (p.n == kMaxSegs || (p.n > 0 && p.segs[p.n - 1].q_row0 + p.segs[p.n - 1].n_q != it.q_row0))
+            if (pe_status s = flush()) return s;
+        p.segs[p.n++] = WeightSeg{it.row, it.seq * cf.max_pages_per_seq, it.q_row0, it.n_q, it.n_keys, 0, 0};
+        rows += it.n_q;
+        max_keys = std::max(max_keys, it.n_keys);
+    }
+    return flush();
+}
+
+// Attention and weights of one call.  8-bit cache: sequences of few rows keep their scores as they are attended; the
+// others are attended as ever, then their scores are computed again in pieces that fit the workspace.
+pe_status attend_with_weights(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer, const void *Q, int64_t q_rows,
+                              void *out, int32_t hq, float scale, float *weights, int64_t stride, cudaStream_t st)
+{
+    const int g = hq / c->cfg.num_kv_heads;
+    std::vector<Q8Item> few, more, left;
+    std::vector<AttnItem> many;
     for (size_t i = 0; i < items.size(); ++i) {
         const AttnItem &it = items[i];
         if (it.n_q <= 0) continue;
-        if (p.n == kMaxSegs)
-            if (pe_status s = flush()) return s;
-        p.segs[p.n++] = WeightSeg{static_cast<int32_t>(i), it.seq * cf.max_pages_per_seq, it.q_row0, it.n_q,
-                                  static_cast<int32_t>(c->len[it.seq])};
-        rows += it.n_q;
-        max_keys = std::max(max_keys, static_cast<int32_t>(c->len[it.seq]));
+        const bool takes = c->q8 && q8_takes(c, it.n_q, g);
+        (takes ? few : more).push_back(Q8Item{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq]), static_cast<int32_t>(i)});
+        if (!takes) many.push_back(it);
     }
-    return flush();
+    pe_status s = PE_OK;
+    if (!few.empty() && (s = run_q8(c, few, layer, Q, q_rows, out, hq, scale, weights, stride, &left, st)) != PE_OK) return s;
+    // (a sequence of which a query's scores do not fit is attended again as a whole)
+    for (size_t i = 0; i < left.size(); ++i)
+        if (i == 0 || left[i].row != left[i - 1].row) many.push_back(items[left[i].row]);
+    if (!many.empty() && (s = attend(c, many, layer, Q, q_rows, out, hq, scale, st)) != PE_OK) return s;
+    if (!c->q8) return add_weights(c, more, layer, Q, hq, scale, weights, stride, st);
+    if (!more.empty() && (s = run_q8(c, more, layer, Q, q_rows, nullptr, hq, scale, weights, stride, &left, st)) != PE_OK) return s;
+    if (left.empty()) return PE_OK;
+    std::vector<AttnItem> whole;
+    for (const Q8Item &it : left) whole.push_back(AttnItem{it.seq, it.q_row0, it.n_q});
+    if ((s = unpack_layer(c, whole, layer, st)) != PE_OK) return s;
+    return add_weights(c, left, 0, Q, hq, scale, weights, stride, st);
 }
 
 // The arguments of a batched attention call, as items.
@@ -1866,6 +2111,9 @@ static pe_status create_cache(const pe_cache_config *cfg, bool q8, pe_cache **ou
             if ((e = cudaMemset(cc->k8, 0, code_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
             if ((e = cudaMemset(cc->v8, 0, code_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
             if ((e = cudaMemset(cc->exps, 0, exp_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
+            cc->code_rows = pool_rows;
+            if ((st = encode_codes(&cc->tm_k8, cc->k8, c.head_dim, pool_rows, ps)) != PE_OK) break;
+            if ((st = encode_codes(&cc->tm_v8, cc->v8, c.head_dim, pool_rows, ps)) != PE_OK) break;
         }
         if ((e = cudaMalloc(&cc->d_table, table_bytes)) != cudaSuccess) { st = cuda_fail(e, "cudaMalloc page table"); break; }
         if ((e = cudaMemset(cc->d_table, 0xFF, table_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
@@ -2165,8 +2413,7 @@ static pe_status attn_weights_batch(pe_cache *c, int32_t n, const int32_t *seqs,
     if (static_cast<int64_t>(cu_q[n]) * num_q_heads * 4 > c->ws_bytes)
         return fail(PE_ERR_RANGE, "the query rows' log-sum-exp exceed the workspace");
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if ((s = attend(c, items, layer, Q_packed, cu_q[n], out, num_q_heads, softmax_scale, st)) != PE_OK) return s;
-    return add_weights(c, items, layer, Q_packed, num_q_heads, softmax_scale, weights, weights_stride, st);
+    return attend_with_weights(c, items, layer, Q_packed, cu_q[n], out, num_q_heads, softmax_scale, weights, weights_stride, st);
 }
 
 pe_status pe_replay_attn_weights_batch(pe_cache *c, int32_t n, const int32_t *seqs, int32_t layer, const void *Q_packed,
@@ -2751,6 +2998,7 @@ pe_status pe_attn_plan_launches(pe_cache *c, int32_t n, const int32_t *seqs, con
                                 int32_t num_sms, int64_t *words, int64_t cap, int64_t *n_words)
 {
     if (!c) return fail(PE_ERR_INVALID, "null cache");
+    if (c->q8) return fail(PE_ERR_UNSUPPORTED, "launches of an 8-bit cache are not listed");
     if (n < 1 || !seqs || !cu_q || !n_words) return fail(PE_ERR_INVALID, "bad plan arguments");
     if (cu_q[0] != 0) return fail(PE_ERR_INVALID, "cu_q[0] must be 0");
     const int32_t hkv = c->cfg.num_kv_heads;

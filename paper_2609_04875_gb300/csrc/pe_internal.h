@@ -18,6 +18,7 @@ constexpr int kAppendMaxPages = 3072;  // new page ids carried by one append lau
 
 // Device status word codes (pe_device_status).
 constexpr int kStatusWaitTimeout = 1;
+constexpr int kStatusBadPage = 2;      // page id outside the pool
 constexpr int kStatusBadPlan = 3;      // the persistent kernel met a partial slot outside its workspace (skipped)
 
 // ---------------------------------------------------------------- append
@@ -99,6 +100,40 @@ struct ReadParams {
     ReadSeg segs[kMaxSegs];
 };
 
+// Attention of few rows on the codes (pe_q8_attn.cu): items are (sequence, kv-head, block of query rows).
+constexpr int kQ8MaxChunk = 16;        // key tiles (128 keys) of a chunk
+
+struct Q8Seq {
+    int32_t table_row;     // seq * max_pages_per_seq
+    int32_t q_row0, n_q;   // rows of Q / out
+    int32_t n_keys;        // the last query sees all of them
+    int32_t n_blocks;      // of n_q x group rows
+    int32_t ct;            // tiles per full chunk
+    int32_t full0;         // first full chunk id: full0 + (kv-head * nfull + k) * n_blocks + block
+    int32_t rem0;          // first remainder chunk id (rem0 + kv-head * n_blocks + block), -1: none
+    int32_t item0;         // first item (merge): item0 + kv-head * n_blocks + block
+    int32_t score_stride;  // scores: of a row, a multiple of 128
+    int64_t score0;        // scores: first row (kv-head * n_q x group + row)
+};
+
+struct Q8AttnParams {
+    const int32_t *page_table;
+    const __nv_bfloat16 *q;  // bf16 [rows][Hq][d]
+    __nv_bfloat16 *out;      // the same, or null
+    const int8_t *exps;      // [L][num_pages][Hkv][2]
+    float *part;             // partials: O [chunks][RB][d], then m [chunks][RB], then l [chunks][RB]
+    float *lse;              // null, or log2-sum-exp [rows][Hq]
+    float *scores;           // null, or every row's scores in log2 units (-inf: not seen)
+    int32_t *sched;          // [0] next chunk, [1] CTAs that stopped taking; zero between launches
+    int32_t *status;
+    int32_t n_seqs, hq, hkv, group, layer, num_pages, ps;
+    int32_t oob_row;         // a pool row past the end: boxes there read zeros
+    int32_t full_chunks, total_chunks, total_items, total_ctas, any_split, n_rem;
+    float scale_log2;        // softmax_scale * log2(e)
+    Q8Seq seqs[kMaxSegs];
+    int32_t rem_seq[kMaxSegs];  // sequences with remainder chunks, longest remainder first
+};
+
 // ---------------------------------------------------------------- eviction
 struct EvictSeg {
     int32_t row;           // of weights and kept
@@ -128,6 +163,8 @@ struct WeightSeg {
     int32_t row;           // of weights
     int32_t table_row;
     int32_t q_row0, n_q, n_keys;
+    int32_t score_stride;  // scores kept by the attention (Q8Seq)
+    int64_t score0;
 };
 
 struct WeightParams {
@@ -135,6 +172,7 @@ struct WeightParams {
     const __nv_bfloat16 *q;  // bf16 [rows][Hq][d]
     const __nv_bfloat16 *k;  // bf16 [num_pages][Hkv][ps][d], one layer
     float *lse;            // workspace [rows][Hq], log2 units
+    const float *scores;   // kept by the attention, or null
     float *weights;        // [rows][weights_stride]
     int64_t weights_stride;
     int32_t n, hq, hkv, group, ps;
@@ -319,6 +357,12 @@ cudaError_t launch_evict_table(const EvictParams &p, cudaStream_t st);
 cudaError_t launch_evict_finish(const EvictParams &p, cudaStream_t st);
 // q_rows: query rows of the launch's sequences (consecutive from segs[0].q_row0).
 cudaError_t launch_weights(int head_dim, const WeightParams &p, int64_t q_rows, int max_keys, cudaStream_t st);
+// The same from scores and lse that launch_attn_q8 left.
+cudaError_t launch_weights_kept(const WeightParams &p, int max_keys, cudaStream_t st);
+// rows_cap: 4, 8 or 16 rows a block.  tm_k / tm_v: the codes as 2-D maps {d, L*num_pages*Hkv*ps} with d x ps boxes,
+// swizzled over d bytes.
+cudaError_t launch_attn_q8(int head_dim, int rows_cap, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
+                           const Q8AttnParams &p, cudaStream_t st);
 cudaError_t launch_bounded_wait_selftest(int32_t *status, uint64_t limit_ns, cudaStream_t st);
 
 // Raises `kernel`'s dynamic shared-memory limit to `bytes` on the current

@@ -1,0 +1,917 @@
+// Attention of few query rows over the 8-bit cache, on its codes: tcgen05
+// kind::f8f6f4 with keys on the M side, so that K and V go from HBM to the
+// tensor cores as they are stored.
+//
+//     S^T [128 keys x NQ] = K8 [128 x d] . Q8^T     (A = K codes, K-major)
+//     O^T [d x NP]       += V8^T [d x 128] . P8^T   (A = V codes, MN-major)
+//
+// Both factors must be e4m3, so q and the softmax weights are split into parts
+// of four significant bits, each a row of the B operand:
+//   q   = 2^eq (q_hi + 2^-4 q_lo): bf16 has eight bits, so two parts are exact
+//         for elements down to 2^-14 of the row's largest (the rest err by at
+//         most 2^-22 of it); S = 2^(eq + ek) (S_hi + 2^-4 S_lo).
+//   p   = 2^-6 (p_hi + 2^-4 p_mid + 2^-8 p_lo): twelve bits of every weight, and
+//         an absolute floor of 2^-24 of the largest.
+// The products are exact and accumulate in fp32 (measured: within 2^-22 of the
+// sum of magnitudes), so what is rounded is the output alone, to bf16.
+//
+// A key's V scale goes into its weight: with ev its page's exponent and evm the
+// largest of the chunk, y = x + ev - evm (x the score in log2 units) gets the
+// weight pv = 2^(y - m), the sum of weights adds pv 2^(evm - ev) = 2^(x - m),
+// and O = 2^evm sum pv code.  The reference m is taken on y, so that pages of
+// any scale use the codes' range.  (ev - evm is held at -100 or more.)
+//
+// A sequence's query rows R = query * g + head-in-group of a kv-head are cut
+// into blocks of RB; the blocks of one chunk of keys are neighbours in the
+// order of work, so that the second finds the chunk in L2.
+//
+// Bound by HBM: 2 d bytes a key and kv-head.  One CTA a SM takes chunks of up to
+// kQ8MaxChunk tiles from a counter, longest first; partials (O, m, l) of items
+// held in several chunks are merged by a second launch.
+//
+// Roles (384 threads): warps 0-3 softmax (thread = key of the tile), warp 4 K
+// producer, 5 MMA, 6 V producer, 7-10 epilogue (thread = d-column), 11 scheduler:
+// takes chunk ids, reads page ids and scales, splits the chunk's q rows.
+#include <algorithm>
+
+#include "dev_common.cuh"
+#include "q8.cuh"
+
+namespace pe {
+
+namespace {
+
+constexpr int kQ8Keys = 128;
+constexpr int kQ8Stages = 5;                 // K ring, and V ring
+constexpr int kQ8Threads = 384;
+constexpr int kQ8Ring = 4;                   // chunks between the scheduler and the softmax
+constexpr int kQ8Desc = 2;                   // chunk descriptors of the producers
+constexpr int kQ8DescInts = 8 + 16 * kQ8MaxChunk;
+constexpr int kQ8BarSoftmax = 2;             // named barrier
+constexpr float kQ8WeightLimit = 256.f;      // of 2^6 pv: e4m3 holds up to 448
+constexpr float kQ8Unpart = 1.f / 16.f;
+
+// kind::f8f6f4: e4m3 A and B (format 0), fp32 D; the fields are those of kind::f16
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, bool a_mn_major)
+{
+    return (1u << 4) | ((a_mn_major ? 1u : 0u) << 15) | (static_cast<uint32_t>(N >> 3) << 17) |
+           (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+__device__ __forceinline__ void mma_e4m3_warp(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                              uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// smem_desc_sw128, or the same for 64-byte rows (64-byte swizzle) where HD = 64
+template <int HD>
+__device__ __forceinline__ uint64_t row_desc(uint32_t addr, uint32_t lbo_bytes)
+{
+    const uint64_t d = ptx::smem_desc_sw128(addr, lbo_bytes, 8 * HD);
+    return HD == 128 ? d : (d & ~(7ull << 61)) | (4ull << 61);
+}
+
+// byte offset of 16-byte chunk c of row r in a tile of HD-byte rows
+template <int HD>
+__device__ __forceinline__ int row_chunk(int r, int c)
+{
+    return HD == 128 ? r * 128 + ((c ^ (r & 7)) << 4) : r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
+}
+
+template <int HD, int RB>
+struct Q8Cfg {
+    static constexpr int kTile = kQ8Keys * HD;                   // a K or V stage
+    static constexpr int kOffV = kQ8Stages * kTile;
+    static constexpr int kOffZero = 2 * kQ8Stages * kTile;       // d = 64: O^T rows 64..127 read zeros here
+    static constexpr int kZero = HD == 64 ? kTile : 0;
+    static constexpr int kNQ = RB > 8 ? 32 : 16;                 // columns of S^T: high parts, then low parts
+    static constexpr int kQLo = kNQ / 2;
+    static constexpr int kParts = 3;                             // of a weight, RB columns of O^T each
+    static constexpr int kNP = (kParts * RB + 15) / 16 * 16;
+    static constexpr int kOffQ = kOffZero + kZero;
+    static constexpr int kQBytes = kNQ * HD;                     // per ring entry
+    static constexpr int kOffP = kOffQ + kQ8Ring * kQBytes;
+    static constexpr int kPBytes = kNP * 128;
+    static constexpr int kOffRed = kOffP + 2 * kPBytes;          // float [4 warps][16]
+    static constexpr int kOffBar = kOffRed + 4 * 16 * 4;
+    // k_full, k_empty, v_full, v_empty [stages]; s_full, p_full, o_done [2]; drain; ch_full, ch_empty [ring];
+    // o_item, o_free, stats [2]; desc_full, desc_empty [2]
+    static constexpr int kNumBars = 4 * kQ8Stages + 7 + 2 * kQ8Ring + 6 + 2 * kQ8Desc;
+    static constexpr int kOffMisc = kOffBar + kNumBars * 8;      // tmem slot, abort, K / V tiles issued
+    static constexpr int kStatsFloats = 2 + 2 * RB;              // id, 2^(evm - 6), m[RB], l[RB]
+    static constexpr int kOffStats = kOffMisc + 16;
+    // per ring entry: id, evm, -, -, 2^eq [16], then (ek, ev) of page slot j of tile k as int8 pairs [k][16]
+    static constexpr int kEntryBytes = 16 + 64 + kQ8MaxChunk * 32;
+    static constexpr int kOffEntry = (kOffStats + 2 * kStatsFloats * 4 + 15) / 16 * 16;
+    static constexpr int kOffDesc = kOffEntry + kQ8Ring * kEntryBytes;
+    static constexpr int kOffSeqs = kOffDesc + kQ8Desc * kQ8DescInts * 4;
+    static constexpr int kSmem = kOffSeqs + kMaxSegs * static_cast<int>(sizeof(Q8Seq) + 8);
+    static constexpr int kDynSmem = kSmem + 1024;
+    static constexpr int kTmemO = 2 * kNQ;                       // O^T buffers after the S^T buffers
+    static constexpr uint32_t kTmemCols = 2 * kNQ + 2 * kNP <= 64 ? 64 : (2 * kNQ + 2 * kNP <= 128 ? 128 : 256);
+    static_assert(kOffP % 1024 == 0 && kPBytes % 1024 == 0 && kQBytes % 1024 == 0, "operand alignment");
+    static_assert(kDynSmem <= 232448, "shared memory budget");
+    static_assert(sizeof(Q8Seq) % 4 == 0, "copied by words");
+};
+
+// A chunk: tiles [t0, t1) of an item (sequence si, kv-head, row block).  The item's full chunks have ids first + k
+// stride, k < nfull, and its shorter remainder, if any, id rem.
+struct Q8Chunk {
+    int si, kvh, blk, t0, t1;
+};
+
+__device__ __forceinline__ int q8_tiles(const Q8Seq &sq) { return (sq.n_keys + kQ8Keys - 1) / kQ8Keys; }
+
+// seqs, rem: shared-memory copies; rem[j]: (first id, sequence) of the j-th sequence with remainder chunks
+__device__ __forceinline__ Q8Chunk q8_chunk(const Q8AttnParams &p, const Q8Seq *seqs, const int2 *rem, int c)
+{
+    Q8Chunk ci;
+    int lo = 0;
+    if (c < p.full_chunks) {
+        int hi = p.n_seqs;
+        while (hi - lo > 1) {  // the last sequence whose first full chunk is at most c
+            const int mid = (lo + hi) >> 1;
+            if (seqs[mid].full0 <= c) lo = mid; else hi = mid;
+        }
+        const Q8Seq &sq = seqs[lo];
+        const int nfull = q8_tiles(sq) / sq.ct;
+        int off = c - sq.full0;
+        ci.si = lo;
+        ci.blk = off % sq.n_blocks;
+        off /= sq.n_blocks;
+        ci.kvh = off / nfull;
+        ci.t0 = (off - ci.kvh * nfull) * sq.ct;
+        ci.t1 = ci.t0 + sq.ct;
+    } else {
+        int hi = p.n_rem;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (rem[mid].x <= c) lo = mid; else hi = mid;
+        }
+        ci.si = rem[lo].y;
+        const Q8Seq &sq = seqs[ci.si];
+        const int off = c - rem[lo].x;
+        ci.blk = off % sq.n_blocks;
+        ci.kvh = off / sq.n_blocks;
+        ci.t1 = q8_tiles(sq);
+        ci.t0 = ci.t1 / sq.ct * sq.ct;
+    }
+    return ci;
+}
+
+template <int HD, int RB>
+__global__ void __launch_bounds__(kQ8Threads, 1)
+    attn_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                   const __grid_constant__ Q8AttnParams p)
+{
+    using C = Q8Cfg<HD, RB>;
+    constexpr int R = kQ8Ring;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const int g = p.group;
+
+    const uint32_t sbase = ptx::smem_addr(smem);
+    float *s_red = reinterpret_cast<float *>(smem + C::kOffRed);
+    const uint32_t bar0 = sbase + C::kOffBar;
+    auto k_full = [&](int s) { return bar0 + 8u * s; };
+    auto k_empty = [&](int s) { return bar0 + 8u * (kQ8Stages + s); };
+    auto v_full = [&](int s) { return bar0 + 8u * (2 * kQ8Stages + s); };
+    auto v_empty = [&](int s) { return bar0 + 8u * (3 * kQ8Stages + s); };
+    const uint32_t b_s_full = bar0 + 8u * 4 * kQ8Stages;      // [2]
+    const uint32_t b_p_full = b_s_full + 16;                  // [2]
+    const uint32_t b_o_done = b_p_full + 16;                  // [2]
+    const uint32_t b_drain = b_o_done + 16;
+    const uint32_t b_ch_full = b_drain + 8;                   // [R] a chunk's id, scales and q parts are in its entry
+    const uint32_t b_ch_empty = b_ch_full + 8 * R;            // [R] the softmax is done with the chunk
+    const uint32_t b_o_item = b_ch_empty + 8 * R;             // [2] a chunk's O^T is complete
+    const uint32_t b_o_free = b_o_item + 16;                  // [2] the epilogue has read that O^T buffer
+    const uint32_t b_stats = b_o_free + 16;                   // [2] a chunk's statistics are in s_stats
+    const uint32_t b_desc_full = b_stats + 16;                // [2] a chunk's TMA rows are in s_desc
+    const uint32_t b_desc_empty = b_desc_full + 8 * kQ8Desc;  // [2] both producers have issued that chunk
+    float *s_stats = reinterpret_cast<float *>(smem + C::kOffStats);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::kOffMisc);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::kOffMisc + 4);
+    volatile int *s_issued = reinterpret_cast<volatile int *>(smem + C::kOffMisc + 8);  // [2]: K, V
+    Q8Seq *s_seqs = reinterpret_cast<Q8Seq *>(smem + C::kOffSeqs);
+    int2 *s_rem = reinterpret_cast<int2 *>(smem + C::kOffSeqs + kMaxSegs * sizeof(Q8Seq));
+    int *s_desc = reinterpret_cast<int *>(smem + C::kOffDesc);
+    auto entry = [&](int n) { return smem + C::kOffEntry + (n % R) * C::kEntryBytes; };
+    const WaitCtx wctx{abort_flag, p.status};
+
+    if (threadIdx.x == 128) {
+        for (int s = 0; s < kQ8Stages; ++s) {
+            ptx::mbar_init(k_full(s), 1);
+            ptx::mbar_init(k_empty(s), 1);
+            ptx::mbar_init(v_full(s), 1);
+            ptx::mbar_init(v_empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            ptx::mbar_init(b_s_full + 8 * b, 1);
+            ptx::mbar_init(b_p_full + 8 * b, 128);
+            ptx::mbar_init(b_o_done + 8 * b, 1);
+            ptx::mbar_init(b_o_item + 8 * b, 1);
+            ptx::mbar_init(b_o_free + 8 * b, 128);
+            ptx::mbar_init(b_stats + 8 * b, 1);
+        }
+        ptx::mbar_init(b_drain, 1);
+        for (int r = 0; r < R; ++r) {
+            ptx::mbar_init(b_ch_full + 8 * r, 1);
+            ptx::mbar_init(b_ch_empty + 8 * r, 1 + 128);  // MMA, softmax threads
+        }
+        for (int d = 0; d < kQ8Desc; ++d) {
+            ptx::mbar_init(b_desc_full + 8 * d, 1);
+            ptx::mbar_init(b_desc_empty + 8 * d, 2);      // K and V producers
+        }
+        *abort_flag = 0;
+        s_issued[0] = 0;
+        s_issued[1] = 0;
+        ptx::fence_barrier_init();
+        ptx::prefetch_tensormap(&tm_k);
+        ptx::prefetch_tensormap(&tm_v);
+    }
+    if (warp == 5) {
+        ptx::tmem_alloc(ptx::smem_addr(tmem_slot), C::kTmemCols);
+        ptx::tmem_relinquish();
+    }
+    if (warp < 4) {
+        // columns that hold no part of a weight or of q stay zero
+        for (int e = threadIdx.x; e < (R * C::kQBytes + 2 * C::kPBytes) / 16; e += 128)
+            reinterpret_cast<uint4 *>(smem + C::kOffQ)[e] = make_uint4(0u, 0u, 0u, 0u);
+        for (int e = threadIdx.x; e < C::kZero / 16; e += 128)
+            reinterpret_cast<uint4 *>(smem + C::kOffZero)[e] = make_uint4(0u, 0u, 0u, 0u);
+        ptx::fence_proxy_async_smem();
+    } else if (warp >= 7) {
+        const int n_words = p.n_seqs * static_cast<int>(sizeof(Q8Seq) / 4);
+        const int32_t *src = reinterpret_cast<const int32_t *>(p.seqs);
+        for (int e = threadIdx.x - 224; e < n_words; e += kQ8Threads - 224) reinterpret_cast<int32_t *>(s_seqs)[e] = src[e];
+        for (int e = threadIdx.x - 224; e < p.n_rem; e += kQ8Threads - 224)
+            s_rem[e] = make_int2(p.seqs[p.rem_seq[e]].rem0, p.rem_seq[e]);
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    // Launched with programmatic serialization: nothing written by earlier kernels is read before this point.
+    ptx::griddep_wait();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 4 || warp == 6) {
+        // ============================================================ producers (warp 4: K, warp 6: V)
+        const bool is_v = warp == 6;
+        const CUtensorMap *map = is_v ? &tm_v : &tm_k;
+        const int n_boxes = kQ8Keys / p.ps;  // a page a box
+        int i = 0;                           // tile ordinal in this CTA
+        for (int n = 0;; ++n) {
+            const int d = n % kQ8Desc;
+            if (!wait_bar_warp(b_desc_full + 8 * d, (n / kQ8Desc) & 1, wctx)) break;
+            const int *desc = s_desc + d * kQ8DescInts;
+            if (desc[0] < 0) break;  // no more chunks
+            const int nt = desc[1];
+            bool ok = true;
+            for (int k = 0; k < nt; ++k) {
+                const int s = i % kQ8Stages;
+                const uint32_t b_empty = is_v ? v_empty(s) : k_empty(s);
+                const uint32_t b_full = is_v ? v_full(s) : k_full(s);
+                if (i >= kQ8Stages && !wait_bar_warp(b_empty, ((i / kQ8Stages) - 1) & 1, wctx)) {
+                    ok = false;
+                    break;
+                }
+                if (lane == 0) ptx::mbar_arrive_expect_tx(b_full, C::kTile);
+                __syncwarp();
+                if (lane < n_boxes)
+                    ptx::tma_load_2d(sbase + (is_v ? C::kOffV : 0) + s * C::kTile + lane * p.ps * HD, map, 0,
+                                     desc[8 + 16 * k + lane], b_full);
+                __syncwarp();
+                ++i;
+                if (lane == 0) s_issued[is_v ? 1 : 0] = i;
+            }
+            if (!ok) break;
+            if (lane == 0) ptx::mbar_arrive(b_desc_empty + 8 * d);
+        }
+    } else if (warp == 11) {
+        // ============================================================ scheduler
+        const int n_slots = kQ8Keys / p.ps;  // <= 16
+        for (int n = 0;; ++n) {
+            const int d = n % kQ8Desc;
+            const bool ok = n < kQ8Desc || wait_bar_warp(b_desc_empty + 8 * d, ((n / kQ8Desc) - 1) & 1, wctx);
+            int c = -1;
+            if (ok && lane == 0) {
+                c = n < 2 ? n * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x)
+                          : 2 * static_cast<int>(gridDim.x) + atomicAdd(p.sched, 1);
+                if (c >= p.total_chunks) c = -1;
+            }
+            c = __shfl_sync(0xffffffffu, c, 0);
+            int *desc = s_desc + d * kQ8DescInts;
+            Q8Chunk ci{};
+            constexpr int kPer = kQ8MaxChunk / 2;
+            int ex[kPer];  // (ek, ev) of entry e = 32 u + lane: tile e / 16, page slot e % 16
+            int evm = -126;
+            if (c >= 0) {
+                ci = q8_chunk(p, s_seqs, s_rem, c);
+                const Q8Seq &sq = s_seqs[ci.si];
+                int pg[kPer];
+                bool in[kPer];
+#pragma unroll
+                for (int u = 0; u < kPer; ++u) {
+                    const int e = 32 * u + lane;
+                    const int key0 = (ci.t0 + (e >> 4)) * kQ8Keys + (e & 15) * p.ps;
+                    in[u] = ci.t0 + (e >> 4) < ci.t1 && (e & 15) < n_slots && key0 < sq.n_keys;
+                    pg[u] = in[u] ? p.page_table[sq.table_row + key0 / p.ps] : -1;
+                }
+#pragma unroll
+                for (int u = 0; u < kPer; ++u) {
+                    const bool ok_page = pg[u] >= 0 && pg[u] < p.num_pages;
+                    if (!ok_page && in[u]) atomicCAS(p.status, 0, kStatusBadPage);
+                    const int head = (p.layer * p.num_pages + pg[u]) * p.hkv + ci.kvh;
+                    desc[8 + 32 * u + lane] = ok_page ? head * p.ps : p.oob_row;  // past the sequence (or a bad id): zeros
+                    ex[u] = ok_page ? reinterpret_cast<const uint16_t *>(p.exps)[head] : 0x8282;  // -126, -126
+                }
+#pragma unroll
+                for (int u = 0; u < kPer; ++u) evm = max(evm, static_cast<int>(static_cast<int8_t>(ex[u] >> 8)));
+                evm = __reduce_max_sync(0xffffffffu, evm);
+                if (lane == 0) {
+                    desc[0] = c;
+                    desc[1] = ci.t1 - ci.t0;
+                }
+            } else if (lane == 0) {
+                desc[0] = -1;
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(b_desc_full + 8 * d);  // release: the producers read the rows
+
+            // q of the chunk's rows (bf16), while the ring entry's previous chunk is finished
+            constexpr int kPieces = HD / 8;       // eight columns each; lane e: row e / kPieces, piece e % kPieces
+            constexpr int kRowsAt = 32 / kPieces;
+            constexpr int kPasses = RB / kRowsAt;
+            const int pc = lane % kPieces;
+            uint4 qv[kPasses];
+#pragma unroll
+            for (int j = 0; j < kPasses; ++j) {
+                qv[j] = make_uint4(0u, 0u, 0u, 0u);
+                if (c < 0) continue;
+                const Q8Seq &sq = s_seqs[ci.si];
+                const int row = ci.blk * RB + j * kRowsAt + lane / kPieces;
+                if (row < sq.n_q * g)
+                    qv[j] = *reinterpret_cast<const uint4 *>(
+                        p.q + (static_cast<int64_t>(sq.q_row0 + row / g) * p.hq + ci.kvh * g + row % g) * HD + pc * 8);
+            }
+            if (n >= R && !wait_bar_warp(b_ch_empty + 8 * (n % R), ((n / R) - 1) & 1, wctx)) break;
+            uint8_t *en = entry(n);
+            if (c >= 0) {
+#pragma unroll
+                for (int u = 0; u < kPer; ++u)
+                    reinterpret_cast<uint16_t *>(en + 80)[32 * u + lane] = static_cast<uint16_t>(ex[u]);
+                uint8_t *qb = smem + C::kOffQ + (n % R) * C::kQBytes;
+#pragma unroll
+                for (int j = 0; j < kPasses; ++j) {
+                    const int r = j * kRowsAt + lane / kPieces;
+                    uint32_t a = bf16x8_absmax(qv[j]);
+#pragma unroll
+                    for (int off = kPieces / 2; off >= 1; off >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, off));
+                    const bool bad = a >= 0x7f80u;  // an infinity or NaN in the row: the row becomes NaN
+                    const int eq = bad ? 0 : q8_exponent(a);
+                    const float s = pow2i(-eq);
+                    const uint32_t w[4] = {qv[j].x, qv[j].y, qv[j].z, qv[j].w};
+                    uint32_t hi[4], low[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const float2 f = make_float2(__uint_as_float(w[x] << 16) * s, __uint_as_float(w[x] & 0xffff0000u) * s);
+                        hi[x] = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
+                        const float2 h = e4m3x2_to_float2(hi[x]);
+                        low[x] = __nv_cvt_float2_to_fp8x2(make_float2((f.x - h.x) * 16.f, (f.y - h.y) * 16.f), __NV_SATFINITE, __NV_E4M3);
+                    }
+                    uint2 vh = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+                    uint2 vl = make_uint2(low[0] | low[1] << 16, low[2] | low[3] << 16);
+                    if (bad) vh = make_uint2(kQ8NanWord, kQ8NanWord);
+                    *reinterpret_cast<uint2 *>(qb + row_chunk<HD>(r, pc >> 1) + (pc & 1) * 8) = vh;
+                    *reinterpret_cast<uint2 *>(qb + row_chunk<HD>(C::kQLo + r, pc >> 1) + (pc & 1) * 8) = vl;
+                    if (pc == 0) reinterpret_cast<float *>(en + 16)[r] = pow2i(eq);
+                }
+                ptx::fence_proxy_async_smem();
+            }
+            if (lane == 0) {
+                reinterpret_cast<int *>(en)[0] = c;
+                reinterpret_cast<int *>(en)[1] = evm;
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(b_ch_full + 8 * (n % R));  // release: MMA and softmax read the entry
+            if (c < 0) break;
+        }
+        // the last scheduler to stop resets the counter for the next launch
+        if (lane == 0) {
+            __threadfence();
+            if (atomicAdd(p.sched + 1, 1) == static_cast<int>(gridDim.x) - 1) {
+                p.sched[0] = 0;
+                p.sched[1] = 0;
+                __threadfence();
+            }
+        }
+    } else if (warp == 5) {
+        // ============================================================ MMA issuer (the whole warp, converged)
+        constexpr uint32_t kIdS = idesc_e4m3_f32(128, C::kNQ, false);
+        constexpr uint32_t kIdPV = idesc_e4m3_f32(128, C::kNP, true);
+        constexpr uint32_t kAll = 0xffffffffu;
+        const uint32_t tm = __shfl_sync(kAll, tmem, 0);
+        const uint64_t k_desc = row_desc<HD>(sbase, 16);
+        const uint64_t q_desc = row_desc<HD>(sbase + C::kOffQ, 16);
+        const uint64_t p_desc = ptx::smem_desc_sw128(sbase + C::kOffP, 16, 1024);
+        auto ready = [&](uint32_t bar, int parity) -> bool {
+            return __all_sync(kAll, ptx::mbar_test_wait(bar, parity));
+        };
+        auto next_tiles = [&](int n) -> int {  // chunk ordinal n's tiles (0: no more chunks)
+            int nt = 0;
+            if (wait_bar_warp(b_ch_full + 8 * (n % R), (n / R) & 1, wctx)) {
+                const int c = reinterpret_cast<volatile int *>(entry(n))[0];
+                if (c >= 0) {
+                    const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
+                    nt = ci.t1 - ci.t0;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(b_ch_empty + 8 * (n % R));
+            return __shfl_sync(kAll, nt, 0);
+        };
+        int ns = 0, np = 0;                    // next S^T tile, next P V tile (ordinals in this CTA)
+        int ns_chunk = 0;
+        int s_left = next_tiles(0);            // tiles of chunk ns_chunk not yet given an S^T
+        uint32_t pv_tiles = s_left;            // tile counts of the chunks the S^T cursor has read: byte n & 3
+        int np_chunk = 0, p_done = 0;
+        bool more = s_left > 0;
+        auto tiles_of = [&](int n) -> int { return (pv_tiles >> (8 * (n & 3))) & 0xffu; };
+        uint64_t t_last = ptx::globaltimer();
+        while (s_left > 0 || np < ns) {
+            bool progress = false;
+            // S^T(ns): K landed, S buffer free (P V(ns - 2) issued)
+            if (s_left > 0 && ns <= np + 1 && ready(k_full(ns % kQ8Stages), (ns / kQ8Stages) & 1)) {
+                const int s = ns % kQ8Stages;
+                ptx::tc_fence_after();
+                const uint64_t kd = k_desc + s * (C::kTile >> 4);
+                const uint64_t qd = q_desc + (ns_chunk % R) * (C::kQBytes >> 4);
+#pragma unroll
+                for (int kk = 0; kk < HD / 32; ++kk)
+                    mma_e4m3_warp(tm + C::kNQ * (ns & 1), kd + (kk * 32 >> 4), qd + (kk * 32 >> 4), kIdS, kk > 0 ? 1u : 0u);
+                mma_commit_warp(b_s_full + 8 * (ns & 1));
+                mma_commit_warp(k_empty(s));
+                ++ns;
+                if (--s_left == 0 && more) {
+                    const int nt = next_tiles(ns_chunk + 1);
+                    if (nt > 0) {
+                        ++ns_chunk;
+                        s_left = nt;
+                        const int sh = 8 * (ns_chunk & 3);
+                        pv_tiles = (pv_tiles & ~(0xffu << sh)) | (static_cast<uint32_t>(nt) << sh);
+                    } else {
+                        more = false;
+                    }
+                }
+                progress = true;
+            }
+            // O^T += V^T P^T(np): V landed, P^T(np) written, at a chunk's first tile the O^T buffer read
+            if (np < ns && ready(v_full(np % kQ8Stages), (np / kQ8Stages) & 1) &&
+                ready(b_p_full + 8 * (np & 1), (np >> 1) & 1) &&
+                (p_done > 0 || np_chunk < 2 || ready(b_o_free + 8 * (np_chunk & 1), ((np_chunk - 2) >> 1) & 1))) {
+                ptx::tc_fence_after();
+                const int s = np % kQ8Stages;
+                const uint32_t va = sbase + C::kOffV + s * C::kTile;
+                const uint64_t vd = row_desc<HD>(va, HD == 64 ? sbase + C::kOffZero - va : 16);
+                const uint64_t pd = p_desc + (np & 1) * (C::kPBytes >> 4);
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)  // 32 keys each
+                    mma_e4m3_warp(tm + C::kTmemO + C::kNP * (np_chunk & 1), vd + (kk * 32 * HD >> 4), pd + (kk * 32 >> 4), kIdPV,
+                                  (p_done > 0 || kk > 0) ? 1u : 0u);
+                mma_commit_warp(v_empty(s));
+                mma_commit_warp(b_o_done + 8 * (np & 1));
+                ++np;
+                if (++p_done == tiles_of(np_chunk)) {
+                    mma_commit_warp(b_o_item + 8 * (np_chunk & 1));
+                    ++np_chunk;
+                    p_done = 0;
+                }
+                progress = true;
+            }
+            if (progress) {
+                t_last = ptx::globaltimer();
+            } else {
+                if (__any_sync(kAll, *abort_flag != 0)) break;
+                if (__any_sync(kAll, ptx::globaltimer() - t_last > kWaitNs)) {
+                    if (lane == 0) {
+                        *abort_flag = 1;
+                        atomicCAS(p.status, 0, kStatusWaitTimeout);
+                    }
+                    break;
+                }
+            }
+        }
+        mma_commit_warp(b_drain);
+        if (lane == 0) {
+            const uint64_t start = ptx::globaltimer();
+            while (!ptx::mbar_try_wait(b_drain, 0) && ptx::globaltimer() - start < 4000000ull) {
+            }
+        }
+        __syncwarp();
+    } else if (warp < 4) {
+        // ============================================================ softmax (thread = key of the tile)
+        const int t = threadIdx.x;
+        const uint32_t lane_off = static_cast<uint32_t>(warp * 32) << 16;
+        const int slot = t / p.ps;
+        float mref[RB], lpart[RB], qs[RB];
+        auto tile_max = [&](const float (&x)[RB], float (&m)[RB]) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                float v = x[r];
+#pragma unroll
+                for (int off = 16; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+                if (lane == 0) s_red[warp * 16 + r] = v;
+            }
+            ptx::bar_sync(kQ8BarSoftmax, 128);
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+                m[r] = fmaxf(fmaxf(s_red[r], s_red[16 + r]), fmaxf(s_red[32 + r], s_red[48 + r]));
+            ptx::bar_sync(kQ8BarSoftmax, 128);  // s_red is reused
+        };
+        int n = 0;   // chunk ordinal
+        int i = 0;   // tile ordinal in this CTA
+        bool stopped = false;
+        for (;; ++n) {
+            const bool got = wait_bar_warp(b_ch_full + 8 * (n % R), (n / R) & 1, wctx);
+            const uint8_t *en = entry(n);
+            const int c = got ? reinterpret_cast<const volatile int *>(en)[0] : -1;
+            if (ptx::bar_sync_or(kQ8BarSoftmax, 128, !got)) stopped = true;
+            if (stopped || c < 0) break;
+            const int evm = reinterpret_cast<const volatile int *>(en)[1];
+            const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
+            const Q8Seq &sq = s_seqs[ci.si];
+            const int row0 = ci.blk * RB;
+            const int n_rows = min(RB, sq.n_q * g - row0);
+            const int qpos0 = sq.n_keys - sq.n_q;
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                mref[r] = -INFINITY;
+                lpart[r] = 0.f;
+                qs[r] = reinterpret_cast<const float *>(en + 16)[r];
+            }
+            float *sc = p.scores ? p.scores + sq.score0 + (static_cast<int64_t>(ci.kvh) * sq.n_q * g + row0) * sq.score_stride : nullptr;
+            for (int lt = ci.t0; lt < ci.t1; ++lt, ++i) {
+                const int j = lt - ci.t0;
+                const char2 ex = reinterpret_cast<const char2 *>(en + 80)[16 * j + slot];
+                const bool ok = wait_bar_warp(b_s_full + 8 * (i & 1), (i >> 1) & 1, wctx);
+                if (ptx::bar_sync_or(kQ8BarSoftmax, 128, !ok || *abort_flag)) {
+                    stopped = true;
+                    break;
+                }
+                ptx::tc_fence_after();
+                float x[RB], low[RB];
+                ptx::tmem_ld_n<RB>(tmem + C::kNQ * (i & 1) + lane_off, x);
+                ptx::tmem_ld_n<RB>(tmem + C::kNQ * (i & 1) + C::kQLo + lane_off, low);
+                ptx::tmem_wait_ld();
+                const int key = lt * kQ8Keys + t;
+                const float ks = pow2i(static_cast<int8_t>(ex.x)) * p.scale_log2;
+                const int dv = max(static_cast<int8_t>(ex.y) - evm, -100);
+                const float fdv = static_cast<float>(dv), unv = pow2i(-dv);
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const int qpos = qpos0 + (row0 + r) / g;  // (rows past n_rows hold zeros and are not written)
+                    x[r] = key < sq.n_keys && key <= qpos ? fmaf(low[r], kQ8Unpart, x[r]) * (ks * qs[r]) : -INFINITY;
+                }
+                if (sc) {
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+                        if (r < n_rows) sc[r * sq.score_stride + key] = x[r];
+                }
+#pragma unroll
+                for (int r = 0; r < RB; ++r) x[r] += fdv;  // y
+                if (j == 0) tile_max(x, mref);
+                float pr[RB];
+                bool big = false;
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    pr[r] = mref[r] == -INFINITY ? (x[r] == -INFINITY ? 0.f : INFINITY) : ex2(x[r] - mref[r] + 6.f);
+                    big = big || !(pr[r] <= kQ8WeightLimit);
+                }
+                if (ptx::bar_sync_or(kQ8BarSoftmax, 128, big)) {
+                    // rare: move the reference to the running max, rescale O^T and the partial sums
+                    float tm[RB], f[RB];
+                    tile_max(x, tm);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        const float mn = fmaxf(mref[r], tm[r]);
+                        f[r] = mn == -INFINITY ? 1.f : ex2(mref[r] - mn);
+                        mref[r] = mn;
+                        lpart[r] *= f[r];
+                        pr[r] = mn == -INFINITY ? (x[r] == -INFINITY ? 0.f : x[r]) : ex2(x[r] - mn + 6.f);
+                    }
+                    if (j > 0) {  // every earlier O^T update of this chunk has landed
+                        const bool done = wait_bar_warp(b_o_done + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, wctx);
+                        if (done) {
+                            ptx::tc_fence_after();
+#pragma unroll
+                            for (int part = 0; part < C::kParts; ++part) {
+                                const uint32_t to = tmem + C::kTmemO + C::kNP * (n & 1) + part * RB + lane_off;
+                                float o[RB];
+                                ptx::tmem_ld_n<RB>(to, o);
+                                ptx::tmem_wait_ld();
+#pragma unroll
+                                for (int r = 0; r < RB; ++r) o[r] *= f[r];
+                                ptx::tmem_st_n<RB>(to, o);
+                            }
+                            ptx::tmem_wait_st();
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < RB; ++r) lpart[r] = fmaf(pr[r], unv, lpart[r]);
+                // P^T(i) into buffer i & 1 once O^T += V^T P^T(i - 2) has read it
+                if (i >= 2) (void)wait_bar_warp(b_o_done + 8 * (i & 1), ((i - 2) >> 1) & 1, wctx);
+                uint8_t *pt = smem + C::kOffP + (i & 1) * C::kPBytes;
+#pragma unroll
+                for (int r = 0; r < RB; r += 2) {
+                    float2 w = make_float2(pr[r], pr[r + 1]);
+#pragma unroll
+                    for (int part = 0; part < C::kParts; ++part) {
+                        const uint32_t q = __nv_cvt_float2_to_fp8x2(w, __NV_SATFINITE, __NV_E4M3);
+                        const int r0 = part * RB + r, r1 = r0 + 1;
+                        pt[row_chunk<128>(r0, t >> 4) + (t & 15)] = static_cast<uint8_t>(q);
+                        pt[row_chunk<128>(r1, t >> 4) + (t & 15)] = static_cast<uint8_t>(q >> 8);
+                        if (part + 1 < C::kParts) {
+                            const float2 h = e4m3x2_to_float2(q);
+                            w = make_float2((w.x - h.x) * 16.f, (w.y - h.y) * 16.f);
+                        }
+                    }
+                }
+                ptx::fence_proxy_async_smem();
+                ptx::tc_fence_before();
+                ptx::mbar_arrive(b_p_full + 8 * (i & 1));
+            }
+            if (stopped) break;
+
+            // ---------------------------------------------------- row statistics for the epilogue warps
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                float v = lpart[r];
+#pragma unroll
+                for (int off = 16; off >= 1; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+                if (lane == 0) s_red[warp * 16 + r] = v;
+            }
+            ptx::bar_sync(kQ8BarSoftmax, 128);
+            if (t == 0) {
+                // the stats slot of chunk n - 2 must have been read
+                if (n >= 2) (void)wait_bar(b_o_free + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx);
+                float *st = s_stats + (n & 1) * C::kStatsFloats;
+                st[0] = __int_as_float(c);
+                st[1] = ldexpf(1.f, evm - 6);  // (subnormal where the chunk's V is)
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    st[2 + r] = mref[r];
+                    st[2 + RB + r] = ((s_red[r] + s_red[16 + r]) + (s_red[32 + r] + s_red[48 + r])) * (1.f / 64.f);
+                }
+                ptx::mbar_arrive(b_stats + 8 * (n & 1));  // release: the epilogue reads the slot
+            }
+            ptx::bar_sync(kQ8BarSoftmax, 128);  // s_red is reused
+            ptx::mbar_arrive(b_ch_empty + 8 * (n % R));
+        }
+        if (t == 0) {  // no more chunks: the epilogue warps stop at ordinal n
+            if (n >= 2) (void)wait_bar(b_o_free + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx);
+            s_stats[(n & 1) * C::kStatsFloats] = __int_as_float(-1);
+            ptx::mbar_arrive(b_stats + 8 * (n & 1));
+        }
+    } else if (warp >= 7 && warp < 11) {
+        // ============================================================ epilogue (thread = d-column = TMEM lane)
+        const int q4 = warp & 3;                       // TMEM lane quarter this warp may access
+        const int t = q4 * 32 + lane;                  // d-column
+        const int et = (warp - 7) * 32 + lane;         // thread index within the epilogue group
+        const uint32_t lane_off = static_cast<uint32_t>(q4 * 32) << 16;
+        for (int n = 0;; ++n) {
+            if (!wait_bar_warp(b_stats + 8 * (n & 1), (n >> 1) & 1, wctx)) break;
+            const float *st = s_stats + (n & 1) * C::kStatsFloats;
+            const int c = __float_as_int(st[0]);
+            if (c < 0) break;
+            const float scale = st[1], my_m = st[2 + et % RB], my_l = st[2 + RB + et % RB];
+            float o[RB], mref[RB], lsum[RB];
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                mref[r] = st[2 + r];
+                lsum[r] = st[2 + RB + r];
+                o[r] = 0.f;
+            }
+            if (wait_bar_warp(b_o_item + 8 * (n & 1), (n >> 1) & 1, wctx)) {
+                ptx::tc_fence_after();
+                const uint32_t to = tmem + C::kTmemO + C::kNP * (n & 1) + lane_off;
+                float part[C::kParts][RB];
+#pragma unroll
+                for (int k = 0; k < C::kParts; ++k) ptx::tmem_ld_n<RB>(to + k * RB, part[k]);
+                ptx::tmem_wait_ld();
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    float v = part[C::kParts - 1][r];
+#pragma unroll
+                    for (int k = C::kParts - 2; k >= 0; --k) v = fmaf(v, kQ8Unpart, part[k][r]);
+                    o[r] = v * scale;
+                }
+            }
+            ptx::tc_fence_before();
+            ptx::mbar_arrive(b_o_free + 8 * (n & 1));  // O^T buffer and stats slot may be reused
+            const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
+            const Q8Seq &sq = s_seqs[ci.si];
+            const int row0 = ci.blk * RB;
+            const int n_rows = min(RB, sq.n_q * g - row0);
+            if (q8_tiles(sq) <= sq.ct) {
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    if (r >= n_rows) continue;
+                    const int row = row0 + r;
+                    const int64_t at = static_cast<int64_t>(sq.q_row0 + row / g) * p.hq + ci.kvh * g + row % g;
+                    if (t < HD && p.out) p.out[at * HD + t] = __float2bfloat16_rn(o[r] * (lsum[r] > 0.f ? 1.0f / lsum[r] : 0.f));
+                    if (p.lse && et == r) p.lse[at] = mref[r] + log2f(lsum[r]);
+                }
+                continue;
+            }
+            float *po = p.part + static_cast<int64_t>(c) * RB * HD;
+            float *pm = p.part + static_cast<int64_t>(p.total_chunks) * RB * HD;
+            float *pl = pm + static_cast<int64_t>(p.total_chunks) * RB;
+            if (t < HD) {
+#pragma unroll
+                for (int r = 0; r < RB; ++r) po[r * HD + t] = o[r];
+            }
+            if (et < RB) {
+                pm[static_cast<int64_t>(c) * RB + et] = my_m;
+                pl[static_cast<int64_t>(c) * RB + et] = my_l;
+            }
+        }
+    }
+
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) {
+        // after an abort, copies may still be in flight: bounded wait for the last ones issued
+        const uint64_t start = ptx::globaltimer();
+        for (int ring = 0; ring < 2; ++ring) {
+            const int issued = s_issued[ring];
+            for (int i = max(0, issued - kQ8Stages); i < issued; ++i) {
+                const uint32_t b = ring ? v_full(i % kQ8Stages) : k_full(i % kQ8Stages);
+                while (!ptx::mbar_try_wait(b, (i / kQ8Stages) & 1) && ptx::globaltimer() - start < 4000000ull) {
+                }
+            }
+        }
+    }
+    if (warp == 5) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, C::kTmemCols);
+    }
+}
+
+// Merge of the items held in several chunks: M = max_k m_k, O = sum_k 2^(m_k - M) O_k / sum_k 2^(m_k - M) l_k, in
+// the item's chunk order.  A block per item and row; its groups of HD / 4 threads take every kGroups-th chunk.
+constexpr int kQ8CombThreads = 128;
+template <int HD, int RB>
+__global__ void __launch_bounds__(kQ8CombThreads) attn_q8_combine_kernel(const __grid_constant__ Q8AttnParams p)
+{
+    constexpr int kLanes = HD / 4;
+    constexpr int kGroups = kQ8CombThreads / kLanes;
+    constexpr int kOB = 8;
+    __shared__ float4 s_acc[kGroups][kLanes];
+    __shared__ float s_m[kGroups], s_l[kGroups];
+    const int item = static_cast<int>(blockIdx.x), r = static_cast<int>(blockIdx.y);
+    int lo = 0, hi = p.n_seqs;
+    while (hi - lo > 1) {  // the last sequence whose first item is at most this one
+        const int mid = (lo + hi) >> 1;
+        if (p.seqs[mid].item0 <= item) lo = mid; else hi = mid;
+    }
+    const Q8Seq &sq = p.seqs[lo];
+    const int blk = (item - sq.item0) % sq.n_blocks, kvh = (item - sq.item0) / sq.n_blocks;
+    const int nt = q8_tiles(sq), nfull = nt / sq.ct;
+    const int cpi = nfull + (nt % sq.ct ? 1 : 0);
+    const int first = sq.full0 + kvh * nfull * sq.n_blocks + blk;
+    const int rem = sq.rem0 + kvh * sq.n_blocks + blk;
+    const int row = blk * RB + r;
+    const int grp = static_cast<int>(threadIdx.x) / kLanes;
+    const int t = static_cast<int>(threadIdx.x) % kLanes;
+    const float *pm = p.part + static_cast<int64_t>(p.total_chunks) * RB * HD;
+    const float *pl = pm + static_cast<int64_t>(p.total_chunks) * RB;
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    if (cpi <= 1 || row >= sq.n_q * p.group) return;
+    float mx = -INFINITY, den = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = grp; k0 < cpi; k0 += kGroups * kOB) {
+        float mv[kOB], lv[kOB];
+        float4 ov[kOB];
+#pragma unroll
+        for (int u = 0; u < kOB; ++u) {
+            const int k = k0 + u * kGroups;
+            const bool in = k < cpi;
+            const int64_t c = k < nfull ? first + static_cast<int64_t>(k) * sq.n_blocks : (in ? rem : (nfull ? first : rem));
+            mv[u] = in ? __ldcg(pm + c * RB + r) : -INFINITY;
+            lv[u] = in ? __ldcg(pl + c * RB + r) : 0.f;
+            ov[u] = in ? __ldcg(reinterpret_cast<const float4 *>(p.part + (c * RB + r) * HD) + t)
+                       : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float bmx = mx;
+#pragma unroll
+        for (int u = 0; u < kOB; ++u) bmx = fmaxf(bmx, mv[u]);
+        if (bmx == -INFINITY) {  // no visible key so far, or NaN keys only
+#pragma unroll
+            for (int u = 0; u < kOB; ++u) den += lv[u];
+            continue;
+        }
+        const float f = mx == -INFINITY ? 0.f : ex2(mx - bmx);
+        den *= f;
+        acc.x *= f;
+        acc.y *= f;
+        acc.z *= f;
+        acc.w *= f;
+        mx = bmx;
+#pragma unroll
+        for (int u = 0; u < kOB; ++u) {
+            if (mv[u] == -INFINITY && lv[u] == 0.f) continue;  // O_k and l_k hold nothing
+            const float w = ex2(mv[u] - bmx);
+            den += w * lv[u];
+            acc.x += w * ov[u].x;
+            acc.y += w * ov[u].y;
+            acc.z += w * ov[u].z;
+            acc.w += w * ov[u].w;
+        }
+    }
+    s_acc[grp][t] = acc;
+    if (t == 0) {
+        s_m[grp] = mx;
+        s_l[grp] = den;
+    }
+    __syncthreads();
+    if (grp != 0) return;
+    float M = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < kGroups; ++q) M = fmaxf(M, s_m[q]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll
+    for (int q = 0; q < kGroups; ++q) {
+        if (s_m[q] == -INFINITY) {
+            l += s_l[q];  // 0 or NaN
+            continue;
+        }
+        const float w = ex2(s_m[q] - M);
+        const float4 x = s_acc[q][t];
+        l += w * s_l[q];
+        o.x += w * x.x;
+        o.y += w * x.y;
+        o.z += w * x.z;
+        o.w += w * x.w;
+    }
+    const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : NAN);
+    const int64_t at = static_cast<int64_t>(sq.q_row0 + row / p.group) * p.hq + kvh * p.group + row % p.group;
+    if (p.out) reinterpret_cast<uint2 *>(p.out + at * HD)[t] = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    if (p.lse && t == 0) p.lse[at] = M + log2f(l);
+}
+
+template <int HD, int RB>
+cudaError_t launch_q8_t(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const Q8AttnParams &p, cudaStream_t st)
+{
+    using C = Q8Cfg<HD, RB>;
+    static std::atomic<uint64_t> configured{0};
+    cudaError_t e = set_dyn_smem_once(attn_q8_kernel<HD, RB>, C::kDynSmem, configured);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.total_ctas));
+    cfg.blockDim = dim3(kQ8Threads);
+    cfg.dynamicSmemBytes = C::kDynSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, attn_q8_kernel<HD, RB>, tm_k, tm_v, p);
+    if (e != cudaSuccess || !p.any_split) return e;
+    cfg.gridDim = dim3(static_cast<unsigned>(p.total_items), RB);
+    cfg.blockDim = dim3(kQ8CombThreads);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, attn_q8_combine_kernel<HD, RB>, p);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_q8(int head_dim, int rows_cap, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
+                           const Q8AttnParams &p, cudaStream_t st)
+{
+    if (p.total_ctas <= 0) return cudaSuccess;
+    if (head_dim == 128) {
+        if (rows_cap == 4) return launch_q8_t<128, 4>(tm_k, tm_v, p, st);
+        if (rows_cap == 8) return launch_q8_t<128, 8>(tm_k, tm_v, p, st);
+        if (rows_cap == 16) return launch_q8_t<128, 16>(tm_k, tm_v, p, st);
+    } else if (head_dim == 64) {
+        if (rows_cap == 4) return launch_q8_t<64, 4>(tm_k, tm_v, p, st);
+        if (rows_cap == 8) return launch_q8_t<64, 8>(tm_k, tm_v, p, st);
+        if (rows_cap == 16) return launch_q8_t<64, 16>(tm_k, tm_v, p, st);
+    }
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace pe

@@ -126,7 +126,31 @@ __global__ void __launch_bounds__(kWtKeys) weights_sum_kernel(const __grid_const
     }
 }
 
+// The same sum from kept scores: rows of a kv-head one after another, 128 keys a block.
+__global__ void __launch_bounds__(kWtKeys) weights_kept_kernel(const __grid_constant__ WeightParams p)
+{
+    const WeightSeg &sg = p.segs[blockIdx.y];
+    const int key = static_cast<int>(blockIdx.x) * kWtKeys + static_cast<int>(threadIdx.x);
+    if (key >= sg.n_keys) return;
+    const int rows = sg.n_q * p.group;
+    const float *s = p.scores + sg.score0 + key;
+    float sum = 0.f;
+    for (int h = 0; h < p.hkv; ++h) {
+        for (int r = 0; r < rows; ++r, s += sg.score_stride)
+            sum += ex2(*s - p.lse[static_cast<int64_t>(sg.q_row0 + r / p.group) * p.hq + h * p.group + r % p.group]);
+    }
+    float *a = p.weights + static_cast<int64_t>(sg.row) * p.weights_stride + key;
+    *a += sum;
+}
+
 }  // namespace
+
+cudaError_t launch_weights_kept(const WeightParams &p, int max_keys, cudaStream_t st)
+{
+    const dim3 tiles(static_cast<unsigned>((max_keys + kWtKeys - 1) / kWtKeys), static_cast<unsigned>(p.n));
+    weights_kept_kernel<<<tiles, kWtKeys, 0, st>>>(p);
+    return cudaGetLastError();
+}
 
 cudaError_t launch_weights(int head_dim, const WeightParams &p, int64_t q_rows, int max_keys, cudaStream_t st)
 {

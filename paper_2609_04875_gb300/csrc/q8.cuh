@@ -36,12 +36,18 @@ __device__ __forceinline__ int q8_exponent(uint32_t a)
     return e < -126 ? -126 : (e > 119 ? 119 : e);
 }
 
-// two codes (low byte first) times s, as a bf16 pair
-__device__ __forceinline__ uint32_t q8_pair_to_bf16(uint32_t codes, float s)
+// two codes, low byte first
+__device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t codes)
 {
     const __half2_raw hr =
         __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes & 0xffffu), __NV_E4M3);
-    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&hr));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&hr));
+}
+
+// two codes times s, as a bf16 pair
+__device__ __forceinline__ uint32_t q8_pair_to_bf16(uint32_t codes, float s)
+{
+    const float2 f = e4m3x2_to_float2(codes);
     const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * s, f.y * s);
     return *reinterpret_cast<const uint32_t *>(&b);
 }

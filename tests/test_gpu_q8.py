@@ -3,7 +3,8 @@ leave in the cache (bit for bit), attention over it, the keys' accumulated weigh
 
 Attention's bound, element by element: against the values held, the kernels differ from the exact result by the output's
 rounding to bf16 (2^-8 |o|), the softmax weights' rounding (to bf16 or finer: 2^-8 of each, so 2^-8 sum_j w_j |v_j|) and
-the scores' error as below, times the same sum; a twentieth is added for the products of these.  The weights are fp32
+the scores' error as below, times the same sum; a twentieth is added for the products of these.  Weights held in e4m3
+parts have an absolute floor too: n keys each off by 2^-24 of the largest, times the largest |v|.  The weights are fp32
 sums of terms 2^(x - lse): an error dx of a score (a dot product of d exact products, each addition within 2^-24 of
 the sum of magnitudes) moves a term by a factor 2^dx, lse's own error no further, the exponential and logarithm add
 2^-20, and each of the sum's additions 2^-24."""
@@ -33,9 +34,10 @@ def score_error(K, Q, scale):
 def assert_attention(out, m, Q, scale, layer=0, what=""):
     """out against the model's attention of sequence m's last rows Q (64 bits); returns the keys' weights."""
     ref, w, size = q8_model.attend(m.K[layer], m.V[layer], Q, scale)
+    floor = len(m) * 2.0 ** -24 * np.abs(np.nan_to_num(m.V[layer])).max()
     got = to64(out)
     assert np.array_equal(np.isnan(got), np.isnan(ref)), f"{what}: NaN rows"
-    bound = 1.05 * (2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + score_error(m.K[layer], Q, scale)) * size) + 1e-30
+    bound = 1.05 * (2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + score_error(m.K[layer], Q, scale)) * size + floor)
     over = np.nan_to_num(np.abs(got - ref) / bound)
     assert over.max() <= 1, f"{what}: error {over.max():.3g} times the bound"
     return w
