@@ -1734,14 +1734,15 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
     auto tiles_of = [&](size_t i) { return ceil_div(items[i].n_keys, 128); };
     auto items_of = [&](size_t i) { return ceil_div(static_cast<int64_t>(items[i].n_q) * g, rb) * hkv; };
     for (size_t i = lo; i < hi; ++i) tiles += tiles_of(i) * items_of(i);
+    const int64_t longest = q8_max_chunk(rb);
     int64_t longest_item = 1;
     for (size_t i = lo; i < hi; ++i) longest_item = std::max(longest_item, tiles_of(i));
     int64_t ct = c->dec_chunks_per_sm > 0
-                     ? std::min<int64_t>(kQ8MaxChunk, std::max<int64_t>(1, ceil_div(tiles, c->dec_chunks_per_sm * static_cast<int64_t>(c->num_sms))))
-                     : chunk_tiles(c, lo, hi, tiles_of, items_of, tiles, kQ8MaxChunk, 24, kQ8ChunkCost);
-    if (c->splitkv == 1 && c->num_splits > 0) ct = std::min<int64_t>(kQ8MaxChunk, ceil_div(longest_item, c->num_splits));
+                     ? std::min<int64_t>(longest, std::max<int64_t>(1, ceil_div(tiles, c->dec_chunks_per_sm * static_cast<int64_t>(c->num_sms))))
+                     : chunk_tiles(c, lo, hi, tiles_of, items_of, tiles, longest, 24, kQ8ChunkCost);
+    if (c->splitkv == 1 && c->num_splits > 0) ct = std::min<int64_t>(longest, ceil_div(longest_item, c->num_splits));
     std::memset(static_cast<void *>(&p), 0, offsetof(Q8AttnParams, seqs));
-    for (;; ct = kQ8MaxChunk) {
+    for (;; ct = longest) {
         int64_t chunks = 0, n_items = 0, score = 0;
         p.n_seqs = p.n_rem = p.any_split = 0;
         for (size_t i = lo; i < hi; ++i) {
@@ -1783,7 +1784,7 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
             p.total_items = static_cast<int32_t>(n_items);
             break;
         }
-        if (ct == kQ8MaxChunk) return false;
+        if (ct == longest) return false;
     }
     p.total_ctas = std::min<int32_t>(p.total_chunks, c->num_sms);
     p.page_table = c->d_table;
@@ -1793,6 +1794,7 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
     p.hkv = hkv;
     p.hq = hkv * g;
     p.group = g;
+    while ((1 << p.log_group) < g) p.log_group++;
     p.num_pages = cf.num_pages;
     p.ps = cf.page_size;
     p.oob_row = static_cast<int32_t>(c->code_rows);

@@ -10,16 +10,24 @@
 //   q   = 2^eq (q_hi + 2^-4 q_lo): bf16 has eight bits, so two parts are exact
 //         for elements down to 2^-14 of the row's largest (the rest err by at
 //         most 2^-22 of it); S = 2^(eq + ek) (S_hi + 2^-4 S_lo).
-//   p   = 2^-6 (p_hi + 2^-4 p_mid + 2^-8 p_lo): twelve bits of every weight, and
-//         an absolute floor of 2^-24 of the largest.
+//   p   = 2^-8 (p_hi + 2^-4 p_mid + 2^-8 p_lo): twelve bits of every weight, and
+//         an absolute floor of 2^-26 of the largest.
 // The products are exact and accumulate in fp32 (measured: within 2^-22 of the
 // sum of magnitudes), so what is rounded is the output alone, to bf16.
 //
 // A key's V scale goes into its weight: with ev its page's exponent and evm the
 // largest of the chunk, y = x + ev - evm (x the score in log2 units) gets the
 // weight pv = 2^(y - m), the sum of weights adds pv 2^(evm - ev) = 2^(x - m),
-// and O = 2^evm sum pv code.  The reference m is taken on y, so that pages of
-// any scale use the codes' range.  (ev - evm is held at -100 or more.)
+// and O = 2^evm sum pv code.  The reference m is the largest y of the chunk's
+// row, so that pages of any scale use the codes' range.  (ev - evm is held at
+// -100 or more.)
+//
+// The scores of a whole chunk stay in TMEM: one group of warps takes their
+// maximum as the tiles arrive, another, a chunk behind, reads them again for the
+// weights.  So nothing is ever rescaled and no tile waits at a barrier of the
+// group.  With a running maximum, moved when a tile passed it and O^T rescaled
+// then, the chain from a tile's scores to its weights took 1200 cycles with 4
+// rows and 4500 with 16 (a tile's share of HBM is 1390).
 //
 // A sequence's query rows R = query * g + head-in-group of a kv-head are cut
 // into blocks of RB; the blocks of one chunk of keys are neighbours in the
@@ -29,9 +37,9 @@
 // kQ8MaxChunk tiles from a counter, longest first; partials (O, m, l) of items
 // held in several chunks are merged by a second launch.
 //
-// Roles (384 threads): warps 0-3 softmax (thread = key of the tile), warp 4 K
-// producer, 5 MMA, 6 V producer, 7-10 epilogue (thread = d-column), 11 scheduler:
-// takes chunk ids, reads page ids and scales, splits the chunk's q rows.
+// Roles (512 threads): warps 0-3 maxima and 4-7 weights (thread = key of the
+// tile), 8-11 epilogue (thread = d-column), 12 K producer, 13 MMA, 14 V producer,
+// 15 scheduler: takes chunk ids, reads page ids and scales, splits the q rows.
 #include <algorithm>
 
 #include "dev_common.cuh"
@@ -43,12 +51,11 @@ namespace {
 
 constexpr int kQ8Keys = 128;
 constexpr int kQ8Stages = 5;                 // K ring, and V ring
-constexpr int kQ8Threads = 384;
-constexpr int kQ8Ring = 4;                   // chunks between the scheduler and the softmax
+constexpr int kQ8Threads = 512;
+constexpr int kQ8Ring = 4;                   // chunks between the scheduler and the weights
 constexpr int kQ8Desc = 2;                   // chunk descriptors of the producers
 constexpr int kQ8DescInts = 8 + 16 * kQ8MaxChunk;
-constexpr int kQ8BarSoftmax = 2;             // named barrier
-constexpr float kQ8WeightLimit = 256.f;      // of 2^6 pv: e4m3 holds up to 448
+constexpr int kQ8BarMax = 1, kQ8BarWeights = 2;  // named barriers of the two groups
 constexpr float kQ8Unpart = 1.f / 16.f;
 
 // kind::f8f6f4: e4m3 A and B (format 0), fp32 D; the fields are those of kind::f16
@@ -99,13 +106,14 @@ struct Q8Cfg {
     static constexpr int kQBytes = kNQ * HD;                     // per ring entry
     static constexpr int kOffP = kOffQ + kQ8Ring * kQBytes;
     static constexpr int kPBytes = kNP * 128;
-    static constexpr int kOffRed = kOffP + 2 * kPBytes;          // float [4 warps][16]
-    static constexpr int kOffBar = kOffRed + 4 * 16 * 4;
-    // k_full, k_empty, v_full, v_empty [stages]; s_full, p_full, o_done [2]; drain; ch_full, ch_empty [ring];
-    // o_item, o_free, stats [2]; desc_full, desc_empty [2]
-    static constexpr int kNumBars = 4 * kQ8Stages + 7 + 2 * kQ8Ring + 6 + 2 * kQ8Desc;
+    static constexpr int kCT = q8_max_chunk(RB);                 // tiles of a chunk whose scores TMEM holds, twice
+    static constexpr int kOffRed = kOffP + 2 * kPBytes;          // float [2 groups][4 warps][16], then the maxima [2][16]
+    static constexpr int kOffBar = kOffRed + (8 + 2) * 16 * 4;
+    // k_full, k_empty, v_full, v_empty [stages]; s_full [2][kCT]; s_free, m_full, p_full, o_done [2]; drain;
+    // ch_full, ch_empty [ring]; o_item, o_free, stats [2]; desc_full, desc_empty [2]
+    static constexpr int kNumBars = 4 * kQ8Stages + 2 * kCT + 9 + 2 * kQ8Ring + 6 + 2 * kQ8Desc;
     static constexpr int kOffMisc = kOffBar + kNumBars * 8;      // tmem slot, abort, K / V tiles issued
-    static constexpr int kStatsFloats = 2 + 2 * RB;              // id, 2^(evm - 6), m[RB], l[RB]
+    static constexpr int kStatsFloats = 2 + 2 * RB;              // id, 2^(evm - 8), m[RB], l[RB]
     static constexpr int kOffStats = kOffMisc + 16;
     // per ring entry: id, evm, -, -, 2^eq [16], then (ek, ev) of page slot j of tile k as int8 pairs [k][16]
     static constexpr int kEntryBytes = 16 + 64 + kQ8MaxChunk * 32;
@@ -114,8 +122,10 @@ struct Q8Cfg {
     static constexpr int kOffSeqs = kOffDesc + kQ8Desc * kQ8DescInts * 4;
     static constexpr int kSmem = kOffSeqs + kMaxSegs * static_cast<int>(sizeof(Q8Seq) + 8);
     static constexpr int kDynSmem = kSmem + 1024;
-    static constexpr int kTmemO = 2 * kNQ;                       // O^T buffers after the S^T buffers
-    static constexpr uint32_t kTmemCols = 2 * kNQ + 2 * kNP <= 64 ? 64 : (2 * kNQ + 2 * kNP <= 128 ? 128 : 256);
+    static constexpr int kTmemO = 2 * kCT * kNQ;                 // two O^T buffers after the scores of two chunks
+    static constexpr uint32_t kTmemCols = 512;
+    static_assert(kTmemO + 2 * kNP <= static_cast<int>(kTmemCols), "tensor memory");
+    static_assert(kCT <= kQ8MaxChunk, "chunk length");
     static_assert(kOffP % 1024 == 0 && kPBytes % 1024 == 0 && kQBytes % 1024 == 0, "operand alignment");
     static_assert(kDynSmem <= 232448, "shared memory budget");
     static_assert(sizeof(Q8Seq) % 4 == 0, "copied by words");
@@ -186,12 +196,14 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
     auto k_empty = [&](int s) { return bar0 + 8u * (kQ8Stages + s); };
     auto v_full = [&](int s) { return bar0 + 8u * (2 * kQ8Stages + s); };
     auto v_empty = [&](int s) { return bar0 + 8u * (3 * kQ8Stages + s); };
-    const uint32_t b_s_full = bar0 + 8u * 4 * kQ8Stages;      // [2]
-    const uint32_t b_p_full = b_s_full + 16;                  // [2]
+    const uint32_t b_s_full = bar0 + 8u * 4 * kQ8Stages;      // [2][kCT] a tile's scores, by chunk parity
+    const uint32_t b_s_free = b_s_full + 8 * 2 * C::kCT;      // [2] a chunk's scores have been read
+    const uint32_t b_m_full = b_s_free + 16;                  // [2] a chunk's maxima are in s_max
+    const uint32_t b_p_full = b_m_full + 16;                  // [2]
     const uint32_t b_o_done = b_p_full + 16;                  // [2]
     const uint32_t b_drain = b_o_done + 16;
     const uint32_t b_ch_full = b_drain + 8;                   // [R] a chunk's id, scales and q parts are in its entry
-    const uint32_t b_ch_empty = b_ch_full + 8 * R;            // [R] the softmax is done with the chunk
+    const uint32_t b_ch_empty = b_ch_full + 8 * R;            // [R] the weights are done with the chunk
     const uint32_t b_o_item = b_ch_empty + 8 * R;             // [2] a chunk's O^T is complete
     const uint32_t b_o_free = b_o_item + 16;                  // [2] the epilogue has read that O^T buffer
     const uint32_t b_stats = b_o_free + 16;                   // [2] a chunk's statistics are in s_stats
@@ -207,15 +219,17 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
     auto entry = [&](int n) { return smem + C::kOffEntry + (n % R) * C::kEntryBytes; };
     const WaitCtx wctx{abort_flag, p.status};
 
-    if (threadIdx.x == 128) {
+    if (threadIdx.x == 384) {
         for (int s = 0; s < kQ8Stages; ++s) {
             ptx::mbar_init(k_full(s), 1);
             ptx::mbar_init(k_empty(s), 1);
             ptx::mbar_init(v_full(s), 1);
             ptx::mbar_init(v_empty(s), 1);
         }
+        for (int b = 0; b < 2 * C::kCT; ++b) ptx::mbar_init(b_s_full + 8 * b, 1);
         for (int b = 0; b < 2; ++b) {
-            ptx::mbar_init(b_s_full + 8 * b, 1);
+            ptx::mbar_init(b_s_free + 8 * b, 128);
+            ptx::mbar_init(b_m_full + 8 * b, 1);
             ptx::mbar_init(b_p_full + 8 * b, 128);
             ptx::mbar_init(b_o_done + 8 * b, 1);
             ptx::mbar_init(b_o_item + 8 * b, 1);
@@ -225,7 +239,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         ptx::mbar_init(b_drain, 1);
         for (int r = 0; r < R; ++r) {
             ptx::mbar_init(b_ch_full + 8 * r, 1);
-            ptx::mbar_init(b_ch_empty + 8 * r, 1 + 128);  // MMA, softmax threads
+            ptx::mbar_init(b_ch_empty + 8 * r, 1 + 128);  // MMA, weight threads
         }
         for (int d = 0; d < kQ8Desc; ++d) {
             ptx::mbar_init(b_desc_full + 8 * d, 1);
@@ -238,7 +252,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         ptx::prefetch_tensormap(&tm_k);
         ptx::prefetch_tensormap(&tm_v);
     }
-    if (warp == 5) {
+    if (warp == 13) {
         ptx::tmem_alloc(ptx::smem_addr(tmem_slot), C::kTmemCols);
         ptx::tmem_relinquish();
     }
@@ -249,11 +263,11 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         for (int e = threadIdx.x; e < C::kZero / 16; e += 128)
             reinterpret_cast<uint4 *>(smem + C::kOffZero)[e] = make_uint4(0u, 0u, 0u, 0u);
         ptx::fence_proxy_async_smem();
-    } else if (warp >= 7) {
+    } else if (warp >= 4 && warp < 12) {
         const int n_words = p.n_seqs * static_cast<int>(sizeof(Q8Seq) / 4);
         const int32_t *src = reinterpret_cast<const int32_t *>(p.seqs);
-        for (int e = threadIdx.x - 224; e < n_words; e += kQ8Threads - 224) reinterpret_cast<int32_t *>(s_seqs)[e] = src[e];
-        for (int e = threadIdx.x - 224; e < p.n_rem; e += kQ8Threads - 224)
+        for (int e = threadIdx.x - 128; e < n_words; e += 256) reinterpret_cast<int32_t *>(s_seqs)[e] = src[e];
+        for (int e = threadIdx.x - 128; e < p.n_rem; e += 256)
             s_rem[e] = make_int2(p.seqs[p.rem_seq[e]].rem0, p.rem_seq[e]);
     }
     ptx::tc_fence_before();
@@ -263,9 +277,9 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
     ptx::griddep_wait();
     const uint32_t tmem = *tmem_slot;
 
-    if (warp == 4 || warp == 6) {
-        // ============================================================ producers (warp 4: K, warp 6: V)
-        const bool is_v = warp == 6;
+    if (warp == 12 || warp == 14) {
+        // ============================================================ producers (warp 12: K, warp 14: V)
+        const bool is_v = warp == 14;
         const CUtensorMap *map = is_v ? &tm_v : &tm_k;
         const int n_boxes = kQ8Keys / p.ps;  // a page a box
         int i = 0;                           // tile ordinal in this CTA
@@ -296,7 +310,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             if (!ok) break;
             if (lane == 0) ptx::mbar_arrive(b_desc_empty + 8 * d);
         }
-    } else if (warp == 11) {
+    } else if (warp == 15) {
         // ============================================================ scheduler
         const int n_slots = kQ8Keys / p.ps;  // <= 16
         for (int n = 0;; ++n) {
@@ -402,7 +416,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                 reinterpret_cast<int *>(en)[1] = evm;
             }
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(b_ch_full + 8 * (n % R));  // release: MMA and softmax read the entry
+            if (lane == 0) ptx::mbar_arrive(b_ch_full + 8 * (n % R));  // release: the other roles read the entry
             if (c < 0) break;
         }
         // the last scheduler to stop resets the counter for the next launch
@@ -414,7 +428,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                 __threadfence();
             }
         }
-    } else if (warp == 5) {
+    } else if (warp == 13) {
         // ============================================================ MMA issuer (the whole warp, converged)
         constexpr uint32_t kIdS = idesc_e4m3_f32(128, C::kNQ, false);
         constexpr uint32_t kIdPV = idesc_e4m3_f32(128, C::kNP, true);
@@ -426,55 +440,52 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         auto ready = [&](uint32_t bar, int parity) -> bool {
             return __all_sync(kAll, ptx::mbar_test_wait(bar, parity));
         };
-        auto next_tiles = [&](int n) -> int {  // chunk ordinal n's tiles (0: no more chunks)
-            int nt = 0;
-            if (wait_bar_warp(b_ch_full + 8 * (n % R), (n / R) & 1, wctx)) {
-                const int c = reinterpret_cast<volatile int *>(entry(n))[0];
+        // the S^T cursor: chunk ordinal ns_chunk, its tiles (-1: not read yet, 0: no more chunks), the next one
+        int ns = 0, ns_chunk = 0, s_tiles = -1, s_tile = 0;
+        // the P V cursor; pv_tiles: the tiles of the chunks the S^T cursor has read, byte n & 7 (it is at most
+        // four chunks ahead)
+        int np = 0, np_chunk = 0, p_done = 0;
+        uint64_t pv_tiles = 0;
+        auto tiles_of = [&](int n) -> int { return static_cast<int>(pv_tiles >> (8 * (n & 7))) & 0xff; };
+        uint64_t t_last = ptx::globaltimer();
+        while (s_tiles != 0 || np_chunk < ns_chunk) {
+            bool progress = false;
+            if (s_tiles < 0 && ready(b_ch_full + 8 * (ns_chunk % R), (ns_chunk / R) & 1)) {
+                const int c = reinterpret_cast<volatile int *>(entry(ns_chunk))[0];
+                int nt = 0;
                 if (c >= 0) {
                     const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
                     nt = ci.t1 - ci.t0;
                 }
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(b_ch_empty + 8 * (ns_chunk % R));
+                s_tiles = __shfl_sync(kAll, nt, 0);
+                s_tile = 0;
+                const int sh = 8 * (ns_chunk & 7);
+                pv_tiles = (pv_tiles & ~(0xffull << sh)) | (static_cast<uint64_t>(s_tiles) << sh);
+                progress = true;
             }
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(b_ch_empty + 8 * (n % R));
-            return __shfl_sync(kAll, nt, 0);
-        };
-        int ns = 0, np = 0;                    // next S^T tile, next P V tile (ordinals in this CTA)
-        int ns_chunk = 0;
-        int s_left = next_tiles(0);            // tiles of chunk ns_chunk not yet given an S^T
-        uint32_t pv_tiles = s_left;            // tile counts of the chunks the S^T cursor has read: byte n & 3
-        int np_chunk = 0, p_done = 0;
-        bool more = s_left > 0;
-        auto tiles_of = [&](int n) -> int { return (pv_tiles >> (8 * (n & 3))) & 0xffu; };
-        uint64_t t_last = ptx::globaltimer();
-        while (s_left > 0 || np < ns) {
-            bool progress = false;
-            // S^T(ns): K landed, S buffer free (P V(ns - 2) issued)
-            if (s_left > 0 && ns <= np + 1 && ready(k_full(ns % kQ8Stages), (ns / kQ8Stages) & 1)) {
-                const int s = ns % kQ8Stages;
+            // S^T: K landed; at a chunk's first tile, the scores of the chunk before the last read
+            if (s_tiles > 0 && ready(k_full(ns % kQ8Stages), (ns / kQ8Stages) & 1) &&
+                (s_tile > 0 || ns_chunk < 2 || ready(b_s_free + 8 * (ns_chunk & 1), ((ns_chunk - 2) >> 1) & 1))) {
+                const int s = ns % kQ8Stages, at = (ns_chunk & 1) * C::kCT + s_tile;
                 ptx::tc_fence_after();
                 const uint64_t kd = k_desc + s * (C::kTile >> 4);
                 const uint64_t qd = q_desc + (ns_chunk % R) * (C::kQBytes >> 4);
 #pragma unroll
                 for (int kk = 0; kk < HD / 32; ++kk)
-                    mma_e4m3_warp(tm + C::kNQ * (ns & 1), kd + (kk * 32 >> 4), qd + (kk * 32 >> 4), kIdS, kk > 0 ? 1u : 0u);
-                mma_commit_warp(b_s_full + 8 * (ns & 1));
+                    mma_e4m3_warp(tm + C::kNQ * at, kd + (kk * 32 >> 4), qd + (kk * 32 >> 4), kIdS, kk > 0 ? 1u : 0u);
+                mma_commit_warp(b_s_full + 8 * at);
                 mma_commit_warp(k_empty(s));
                 ++ns;
-                if (--s_left == 0 && more) {
-                    const int nt = next_tiles(ns_chunk + 1);
-                    if (nt > 0) {
-                        ++ns_chunk;
-                        s_left = nt;
-                        const int sh = 8 * (ns_chunk & 3);
-                        pv_tiles = (pv_tiles & ~(0xffu << sh)) | (static_cast<uint32_t>(nt) << sh);
-                    } else {
-                        more = false;
-                    }
+                if (++s_tile == s_tiles) {
+                    ++ns_chunk;
+                    s_tiles = -1;
                 }
                 progress = true;
             }
-            // O^T += V^T P^T(np): V landed, P^T(np) written, at a chunk's first tile the O^T buffer read
+            // O^T += V^T P^T(np): V landed, P^T(np) written (so its scores are complete), at a chunk's first tile the
+            // O^T buffer read
             if (np < ns && ready(v_full(np % kQ8Stages), (np / kQ8Stages) & 1) &&
                 ready(b_p_full + 8 * (np & 1), (np >> 1) & 1) &&
                 (p_done > 0 || np_chunk < 2 || ready(b_o_free + 8 * (np_chunk & 1), ((np_chunk - 2) >> 1) & 1))) {
@@ -517,119 +528,138 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             }
         }
         __syncwarp();
-    } else if (warp < 4) {
-        // ============================================================ softmax (thread = key of the tile)
-        const int t = threadIdx.x;
-        const uint32_t lane_off = static_cast<uint32_t>(warp * 32) << 16;
+    } else if (warp < 8) {
+        // ============================================================ maxima (warps 0-3), weights (4-7): thread = key
+        const bool is_max = warp < 4;
+        const int t = threadIdx.x & 127;
+        const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const int slot = t / p.ps;
-        float mref[RB], lpart[RB], qs[RB];
-        auto tile_max = [&](const float (&x)[RB], float (&m)[RB]) {
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                float v = x[r];
-#pragma unroll
-                for (int off = 16; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
-                if (lane == 0) s_red[warp * 16 + r] = v;
-            }
-            ptx::bar_sync(kQ8BarSoftmax, 128);
-#pragma unroll
-            for (int r = 0; r < RB; ++r)
-                m[r] = fmaxf(fmaxf(s_red[r], s_red[16 + r]), fmaxf(s_red[32 + r], s_red[48 + r]));
-            ptx::bar_sync(kQ8BarSoftmax, 128);  // s_red is reused
-        };
+        float *red = s_red + (is_max ? 0 : 4 * 16);
+        float *s_max = s_red + 8 * 16;  // [2][16]
+        const int lg = p.log_group;
         int n = 0;   // chunk ordinal
         int i = 0;   // tile ordinal in this CTA
         bool stopped = false;
-        for (;; ++n) {
+        for (; !stopped; ++n) {
+            // (a wait that gave up is voted on, so that a group leaves together)
             const bool got = wait_bar_warp(b_ch_full + 8 * (n % R), (n / R) & 1, wctx);
+            if (ptx::bar_sync_or(is_max ? kQ8BarMax : kQ8BarWeights, 128, !got)) {
+                stopped = true;
+                break;
+            }
             const uint8_t *en = entry(n);
-            const int c = got ? reinterpret_cast<const volatile int *>(en)[0] : -1;
-            if (ptx::bar_sync_or(kQ8BarSoftmax, 128, !got)) stopped = true;
-            if (stopped || c < 0) break;
+            const int c = reinterpret_cast<const volatile int *>(en)[0];
+            if (c < 0) break;
             const int evm = reinterpret_cast<const volatile int *>(en)[1];
             const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
             const Q8Seq &sq = s_seqs[ci.si];
             const int row0 = ci.blk * RB;
-            const int n_rows = min(RB, sq.n_q * g - row0);
             const int qpos0 = sq.n_keys - sq.n_q;
+            // tiles from this one on hold keys that the block's first row does not see
+            const int masked_from = (qpos0 + (row0 >> lg) + 1) / kQ8Keys;
+            float qs[RB];
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                mref[r] = -INFINITY;
-                lpart[r] = 0.f;
-                qs[r] = reinterpret_cast<const float *>(en + 16)[r];
-            }
-            float *sc = p.scores ? p.scores + sq.score0 + (static_cast<int64_t>(ci.kvh) * sq.n_q * g + row0) * sq.score_stride : nullptr;
-            for (int lt = ci.t0; lt < ci.t1; ++lt, ++i) {
-                const int j = lt - ci.t0;
+            for (int r = 0; r < RB; ++r) qs[r] = reinterpret_cast<const float *>(en + 16)[r];
+            // s = scores without their scales, of tile ordinal j of the chunk; ks, dv: the key's K scale times
+            // scale_log2, and its V scale against the chunk's largest
+            float s[RB], ks;
+            int dv;
+            auto load_scores = [&](int j) -> bool {
                 const char2 ex = reinterpret_cast<const char2 *>(en + 80)[16 * j + slot];
-                const bool ok = wait_bar_warp(b_s_full + 8 * (i & 1), (i >> 1) & 1, wctx);
-                if (ptx::bar_sync_or(kQ8BarSoftmax, 128, !ok || *abort_flag)) {
+                ks = pow2i(static_cast<int8_t>(ex.x)) * p.scale_log2;
+                dv = max(static_cast<int8_t>(ex.y) - evm, -100);
+                const int at = (n & 1) * C::kCT + j;
+                if (is_max) {  // (the weights come after the maxima of the whole chunk)
+                    if (!wait_bar_warp(b_s_full + 8 * at, (n >> 1) & 1, wctx)) return false;
+                    ptx::tc_fence_after();
+                }
+                float low[RB];
+                ptx::tmem_ld_n<RB>(tmem + C::kNQ * at + lane_off, s);
+                ptx::tmem_ld_n<RB>(tmem + C::kNQ * at + C::kQLo + lane_off, low);
+                ptx::tmem_wait_ld();
+#pragma unroll
+                for (int r = 0; r < RB; ++r) s[r] = fmaf(low[r], kQ8Unpart, s[r]);
+                return true;
+            };
+            auto sees = [&](int key, int r) { return key <= qpos0 + ((row0 + r) >> lg); };  // (< n_keys for every row held)
+            if (is_max) {
+                const int n_rows = min(RB, (sq.n_q << lg) - row0);
+                float *sc = p.scores ? p.scores + sq.score0 + (static_cast<int64_t>(ci.kvh) * (sq.n_q << lg) + row0) * sq.score_stride : nullptr;
+                float m[RB];
+#pragma unroll
+                for (int r = 0; r < RB; ++r) m[r] = -INFINITY;
+                for (int lt = ci.t0; lt < ci.t1; ++lt) {
+                    if (!load_scores(lt - ci.t0)) {
+                        stopped = true;
+                        break;
+                    }
+                    const int key = lt * kQ8Keys + t;
+                    const float fdv = static_cast<float>(dv);
+                    if (lt >= masked_from) {
+#pragma unroll
+                        for (int r = 0; r < RB; ++r) s[r] = sees(key, r) && key < sq.n_keys ? s[r] * (ks * qs[r]) : -INFINITY;
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < RB; ++r) s[r] *= ks * qs[r];
+                    }
+                    if (sc) {
+#pragma unroll
+                        for (int r = 0; r < RB; ++r)
+                            if (r < n_rows) sc[r * sq.score_stride + key] = s[r];
+                    }
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) m[r] = fmaxf(m[r], s[r] + fdv);  // (a NaN is not taken)
+                }
+                ptx::tc_fence_before();
+                if (ptx::bar_sync_or(kQ8BarMax, 128, stopped)) {
                     stopped = true;
                     break;
                 }
-                ptx::tc_fence_after();
-                float x[RB], low[RB];
-                ptx::tmem_ld_n<RB>(tmem + C::kNQ * (i & 1) + lane_off, x);
-                ptx::tmem_ld_n<RB>(tmem + C::kNQ * (i & 1) + C::kQLo + lane_off, low);
-                ptx::tmem_wait_ld();
-                const int key = lt * kQ8Keys + t;
-                const float ks = pow2i(static_cast<int8_t>(ex.x)) * p.scale_log2;
-                const int dv = max(static_cast<int8_t>(ex.y) - evm, -100);
-                const float fdv = static_cast<float>(dv), unv = pow2i(-dv);
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
-                    const int qpos = qpos0 + (row0 + r) / g;  // (rows past n_rows hold zeros and are not written)
-                    x[r] = key < sq.n_keys && key <= qpos ? fmaf(low[r], kQ8Unpart, x[r]) * (ks * qs[r]) : -INFINITY;
+                    const int b = __float_as_int(m[r]);  // integers in the order of the numbers
+                    const int k = __reduce_max_sync(0xffffffffu, b ^ ((b >> 31) & 0x7fffffff));
+                    if (lane == r) red[(warp & 3) * 16 + r] = __int_as_float(k ^ ((k >> 31) & 0x7fffffff));
                 }
-                if (sc) {
+                ptx::bar_sync(kQ8BarMax, 128);
+                // (the slot's chunk n - 2 has been read: its scores were freed before this chunk's were computed)
+                if (t < RB) s_max[(n & 1) * 16 + t] = fmaxf(fmaxf(red[t], red[16 + t]), fmaxf(red[32 + t], red[48 + t]));
+                if (warp == 0) {
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(b_m_full + 8 * (n & 1));  // release: the weights read them
+                }
+                continue;
+            }
+            // ------------------------------------------------ weights
+            stopped = !wait_bar_warp(b_m_full + 8 * (n & 1), (n >> 1) & 1, wctx);
+            ptx::tc_fence_after();
+            const float my_max = s_max[(n & 1) * 16 + lane % RB];
+            float m8[RB], lpart[RB];  // 8 - m: the largest weight is 2^8
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const float m = s_max[(n & 1) * 16 + r];
+                m8[r] = m == -INFINITY ? 0.f : 8.f - m;
+                lpart[r] = 0.f;
+            }
+            for (int lt = ci.t0; lt < ci.t1 && !stopped; ++lt, ++i) {
+                (void)load_scores(lt - ci.t0);
+                const int key = lt * kQ8Keys + t;
+                const float fdv = static_cast<float>(dv), unv = pow2i(-dv);
+                float pr[RB];
+#pragma unroll
+                for (int r = 0; r < RB; ++r) pr[r] = ex2(fmaf(s[r], ks * qs[r], m8[r] + fdv));
+                if (lt >= masked_from) {
 #pragma unroll
                     for (int r = 0; r < RB; ++r)
-                        if (r < n_rows) sc[r * sq.score_stride + key] = x[r];
-                }
-#pragma unroll
-                for (int r = 0; r < RB; ++r) x[r] += fdv;  // y
-                if (j == 0) tile_max(x, mref);
-                float pr[RB];
-                bool big = false;
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    pr[r] = mref[r] == -INFINITY ? (x[r] == -INFINITY ? 0.f : INFINITY) : ex2(x[r] - mref[r] + 6.f);
-                    big = big || !(pr[r] <= kQ8WeightLimit);
-                }
-                if (ptx::bar_sync_or(kQ8BarSoftmax, 128, big)) {
-                    // rare: move the reference to the running max, rescale O^T and the partial sums
-                    float tm[RB], f[RB];
-                    tile_max(x, tm);
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) {
-                        const float mn = fmaxf(mref[r], tm[r]);
-                        f[r] = mn == -INFINITY ? 1.f : ex2(mref[r] - mn);
-                        mref[r] = mn;
-                        lpart[r] *= f[r];
-                        pr[r] = mn == -INFINITY ? (x[r] == -INFINITY ? 0.f : x[r]) : ex2(x[r] - mn + 6.f);
-                    }
-                    if (j > 0) {  // every earlier O^T update of this chunk has landed
-                        const bool done = wait_bar_warp(b_o_done + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, wctx);
-                        if (done) {
-                            ptx::tc_fence_after();
-#pragma unroll
-                            for (int part = 0; part < C::kParts; ++part) {
-                                const uint32_t to = tmem + C::kTmemO + C::kNP * (n & 1) + part * RB + lane_off;
-                                float o[RB];
-                                ptx::tmem_ld_n<RB>(to, o);
-                                ptx::tmem_wait_ld();
-#pragma unroll
-                                for (int r = 0; r < RB; ++r) o[r] *= f[r];
-                                ptx::tmem_st_n<RB>(to, o);
-                            }
-                            ptx::tmem_wait_st();
-                        }
-                    }
+                        if (!(sees(key, r) && key < sq.n_keys)) pr[r] = 0.f;
                 }
 #pragma unroll
                 for (int r = 0; r < RB; ++r) lpart[r] = fmaf(pr[r], unv, lpart[r]);
                 // P^T(i) into buffer i & 1 once O^T += V^T P^T(i - 2) has read it
-                if (i >= 2) (void)wait_bar_warp(b_o_done + 8 * (i & 1), ((i - 2) >> 1) & 1, wctx);
+                if (i >= 2 && !wait_bar_warp(b_o_done + 8 * (i & 1), ((i - 2) >> 1) & 1, wctx)) {
+                    stopped = true;
+                    break;
+                }
                 uint8_t *pt = smem + C::kOffP + (i & 1) * C::kPBytes;
 #pragma unroll
                 for (int r = 0; r < RB; r += 2) {
@@ -650,7 +680,11 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                 ptx::tc_fence_before();
                 ptx::mbar_arrive(b_p_full + 8 * (i & 1));
             }
-            if (stopped) break;
+            if (ptx::bar_sync_or(kQ8BarWeights, 128, stopped)) {
+                stopped = true;
+                break;
+            }
+            ptx::mbar_arrive(b_s_free + 8 * (n & 1));
 
             // ---------------------------------------------------- row statistics for the epilogue warps
 #pragma unroll
@@ -658,42 +692,42 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                 float v = lpart[r];
 #pragma unroll
                 for (int off = 16; off >= 1; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-                if (lane == 0) s_red[warp * 16 + r] = v;
+                if (lane == 0) red[(warp & 3) * 16 + r] = v;
             }
-            ptx::bar_sync(kQ8BarSoftmax, 128);
-            if (t == 0) {
+            ptx::bar_sync(kQ8BarWeights, 128);
+            if (warp == 4) {
                 // the stats slot of chunk n - 2 must have been read
-                if (n >= 2) (void)wait_bar(b_o_free + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx);
+                if (n >= 2) (void)wait_bar_warp(b_o_free + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx);
                 float *st = s_stats + (n & 1) * C::kStatsFloats;
-                st[0] = __int_as_float(c);
-                st[1] = ldexpf(1.f, evm - 6);  // (subnormal where the chunk's V is)
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    st[2 + r] = mref[r];
-                    st[2 + RB + r] = ((s_red[r] + s_red[16 + r]) + (s_red[32 + r] + s_red[48 + r])) * (1.f / 64.f);
+                if (lane == 31) {
+                    st[0] = __int_as_float(c);
+                    st[1] = ldexpf(1.f, evm - 8);  // (subnormal where the chunk's V is)
                 }
-                ptx::mbar_arrive(b_stats + 8 * (n & 1));  // release: the epilogue reads the slot
+                if (lane < RB) {
+                    st[2 + lane] = my_max;
+                    st[2 + RB + lane] = ((red[lane] + red[16 + lane]) + (red[32 + lane] + red[48 + lane])) * (1.f / 256.f);
+                }
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(b_stats + 8 * (n & 1));  // release: the epilogue reads the slot
             }
-            ptx::bar_sync(kQ8BarSoftmax, 128);  // s_red is reused
             ptx::mbar_arrive(b_ch_empty + 8 * (n % R));
         }
-        if (t == 0) {  // no more chunks: the epilogue warps stop at ordinal n
+        if (threadIdx.x == 128) {  // no more chunks: the epilogue warps stop at ordinal n
             if (n >= 2) (void)wait_bar(b_o_free + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx);
             s_stats[(n & 1) * C::kStatsFloats] = __int_as_float(-1);
             ptx::mbar_arrive(b_stats + 8 * (n & 1));
         }
-    } else if (warp >= 7 && warp < 11) {
+    } else {
         // ============================================================ epilogue (thread = d-column = TMEM lane)
         const int q4 = warp & 3;                       // TMEM lane quarter this warp may access
         const int t = q4 * 32 + lane;                  // d-column
-        const int et = (warp - 7) * 32 + lane;         // thread index within the epilogue group
         const uint32_t lane_off = static_cast<uint32_t>(q4 * 32) << 16;
         for (int n = 0;; ++n) {
             if (!wait_bar_warp(b_stats + 8 * (n & 1), (n >> 1) & 1, wctx)) break;
             const float *st = s_stats + (n & 1) * C::kStatsFloats;
             const int c = __float_as_int(st[0]);
             if (c < 0) break;
-            const float scale = st[1], my_m = st[2 + et % RB], my_l = st[2 + RB + et % RB];
+            const float scale = st[1], my_m = st[2 + t % RB], my_l = st[2 + RB + t % RB];
             float o[RB], mref[RB], lsum[RB];
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
@@ -729,7 +763,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                     const int row = row0 + r;
                     const int64_t at = static_cast<int64_t>(sq.q_row0 + row / g) * p.hq + ci.kvh * g + row % g;
                     if (t < HD && p.out) p.out[at * HD + t] = __float2bfloat16_rn(o[r] * (lsum[r] > 0.f ? 1.0f / lsum[r] : 0.f));
-                    if (p.lse && et == r) p.lse[at] = mref[r] + log2f(lsum[r]);
+                    if (p.lse && t == r) p.lse[at] = mref[r] + log2f(lsum[r]);
                 }
                 continue;
             }
@@ -740,9 +774,9 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
 #pragma unroll
                 for (int r = 0; r < RB; ++r) po[r * HD + t] = o[r];
             }
-            if (et < RB) {
-                pm[static_cast<int64_t>(c) * RB + et] = my_m;
-                pl[static_cast<int64_t>(c) * RB + et] = my_l;
+            if (t < RB) {
+                pm[static_cast<int64_t>(c) * RB + t] = my_m;
+                pl[static_cast<int64_t>(c) * RB + t] = my_l;
             }
         }
     }
@@ -761,7 +795,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             }
         }
     }
-    if (warp == 5) {
+    if (warp == 13) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, C::kTmemCols);
     }
