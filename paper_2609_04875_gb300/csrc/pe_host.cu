@@ -1714,7 +1714,7 @@ constexpr double kQ8ChunkCost = 0.7;
 
 // Rows (n_q x group) up to which the codes are attended as they are.  Beyond, a sequence's keys are read once per
 // block of 16 rows, and unpacking them once costs less.
-constexpr int64_t kQ8MaxRows = 16;
+constexpr int64_t kQ8MaxRows = 64;
 
 bool q8_takes(const pe_cache *c, int64_t n_q, int g)
 {
@@ -1797,6 +1797,7 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
     while ((1 << p.log_group) < g) p.log_group++;
     p.num_pages = cf.num_pages;
     p.ps = cf.page_size;
+    while ((1 << p.log_ps) < p.ps) p.log_ps++;
     p.oob_row = static_cast<int32_t>(c->code_rows);
     return true;
 }

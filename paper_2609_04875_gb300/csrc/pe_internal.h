@@ -102,7 +102,7 @@ struct ReadParams {
 
 // Attention of few rows on the codes (pe_q8_attn.cu): items are (sequence, kv-head, block of query rows).
 constexpr int kQ8MaxChunk = 14;        // key tiles (128 keys) of a chunk, and with blocks of rb rows:
-__host__ __device__ constexpr int q8_max_chunk(int rb) { return rb <= 4 ? 14 : (rb <= 8 ? 14 : 6); }
+__host__ __device__ constexpr int q8_max_chunk(int rb) { return rb <= 8 ? 14 : 12; }
 
 struct Q8Seq {
     int32_t table_row;     // seq * max_pages_per_seq
@@ -127,7 +127,7 @@ struct Q8AttnParams {
     float *scores;           // null, or every row's scores in log2 units (-inf: not seen)
     int32_t *sched;          // [0] next chunk, [1] CTAs that stopped taking; zero between launches
     int32_t *status;
-    int32_t n_seqs, hq, hkv, group, log_group, layer, num_pages, ps;
+    int32_t n_seqs, hq, hkv, group, log_group, layer, num_pages, ps, log_ps;
     int32_t oob_row;         // a pool row past the end: boxes there read zeros
     int32_t full_chunks, total_chunks, total_items, total_ctas, any_split, n_rem;
     float scale_log2;        // softmax_scale * log2(e)

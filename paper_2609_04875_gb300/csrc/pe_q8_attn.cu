@@ -2,14 +2,17 @@
 // kind::f8f6f4 with keys on the M side, so that K and V go from HBM to the
 // tensor cores as they are stored.
 //
-//     S^T [128 keys x NQ] = K8 [128 x d] . Q8^T     (A = K codes, K-major)
-//     O^T [d x NP]       += V8^T [d x 128] . P8^T   (A = V codes, MN-major)
+//     S^T [128 keys x 16] = K8 [128 x d] . Q8^T     (A = K codes, K-major)
+//     O^T [d x NP]       += V8^T [d x 128] . P8^T   (A = V codes, MN-major; B too)
 //
 // Both factors must be e4m3, so q and the softmax weights are split into parts
-// of four significant bits, each a row of the B operand:
+// of four significant bits:
 //   q   = 2^eq (q_hi + 2^-4 q_lo): bf16 has eight bits, so two parts are exact
-//         for elements down to 2^-14 of the row's largest (the rest err by at
-//         most 2^-22 of it); S = 2^(eq + ek) (S_hi + 2^-4 S_lo).
+//         for elements down to 2^-14 of the row's largest; S = S_hi + 2^-4 S_lo
+//         in columns of their own.  With 16 rows q_lo is not scaled and both add
+//         up in the same columns, or TMEM would hold chunks of half the length:
+//         exact down to 2^-10 (smaller elements err by at most 2^-18 of the
+//         largest).
 //   p   = 2^-8 (p_hi + 2^-4 p_mid + 2^-8 p_lo): twelve bits of every weight, and
 //         an absolute floor of 2^-26 of the largest.
 // The products are exact and accumulate in fp32 (measured: within 2^-22 of the
@@ -37,9 +40,13 @@
 // kQ8MaxChunk tiles from a counter, longest first; partials (O, m, l) of items
 // held in several chunks are merged by a second launch.
 //
-// Roles (512 threads): warps 0-3 maxima and 4-7 weights (thread = key of the
-// tile), 8-11 epilogue (thread = d-column), 12 K producer, 13 MMA, 14 V producer,
-// 15 scheduler: takes chunk ids, reads page ids and scales, splits the q rows.
+// Roles (544 threads): warps 0-3 maxima (thread = key of the tile) and, two chunks
+// behind, the epilogue (thread = d-column), 4-7 and 8-11 weights of every other
+// tile (thread = key), 12 K producer, 13 S^T MMAs, 14 V producer, 15 scheduler
+// (takes chunk ids, reads page ids and scales, splits the q rows), 16 O^T MMAs.
+// A commit takes its warp 80 cycles and an MMA 45, a probe of a barrier as long:
+// one warp for both products spent 1500 cycles a tile, more than a tile's share
+// of HBM, so each product has its warp, and each MMA group one commit.
 #include <algorithm>
 
 #include "dev_common.cuh"
@@ -51,18 +58,41 @@ namespace {
 
 constexpr int kQ8Keys = 128;
 constexpr int kQ8Stages = 5;                 // K ring, and V ring
-constexpr int kQ8Threads = 512;
+constexpr int kQ8Threads = 544;
 constexpr int kQ8Ring = 4;                   // chunks between the scheduler and the weights
-constexpr int kQ8Desc = 2;                   // chunk descriptors of the producers
+constexpr int kQ8Desc = 3;                   // chunk descriptors of the producers (V is one behind K)
 constexpr int kQ8DescInts = 8 + 16 * kQ8MaxChunk;
 constexpr int kQ8BarMax = 1, kQ8BarWeights = 2;  // named barriers of the two groups
 constexpr float kQ8Unpart = 1.f / 16.f;
+constexpr int kNQ = 16;                      // columns of a tile's scores
 
 // kind::f8f6f4: e4m3 A and B (format 0), fp32 D; the fields are those of kind::f16
-__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, bool a_mn_major)
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, bool mn_major)
 {
-    return (1u << 4) | ((a_mn_major ? 1u : 0u) << 15) | (static_cast<uint32_t>(N >> 3) << 17) |
+    return (1u << 4) | ((mn_major ? 3u : 0u) << 15) | (static_cast<uint32_t>(N >> 3) << 17) |
            (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// wait_bar_warp (dev_common.cuh) that looks at the clock and the abort flag once in kQ8Spins tries: reading the
+// clock takes longer than a try, and these waits are many and short.
+constexpr uint32_t kQ8Spins = 64;
+__device__ __forceinline__ bool wait_spin(uint32_t bar, uint32_t parity, const WaitCtx &w)
+{
+    bool ok = ptx::mbar_try_wait(bar, parity);
+    uint64_t t0 = 0;
+    for (uint32_t n = 1; !ok; ++n) {
+        ok = ptx::mbar_try_wait(bar, parity);
+        if (ok || (n & (kQ8Spins - 1))) continue;
+        if (*w.abort) break;
+        const uint64_t now = ptx::globaltimer();
+        if (n == kQ8Spins) t0 = now;
+        if (now - t0 > kWaitNs) {
+            *w.abort = 1;
+            atomicCAS(w.status, 0, kStatusWaitTimeout);
+            break;
+        }
+    }
+    return __all_sync(0xffffffffu, ok);
 }
 
 __device__ __forceinline__ void mma_e4m3_warp(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
@@ -85,6 +115,14 @@ __device__ __forceinline__ uint64_t row_desc(uint32_t addr, uint32_t lbo_bytes)
     return HD == 128 ? d : (d & ~(7ull << 61)) | (4ull << 61);
 }
 
+// P^T as the B operand, MN-major without swizzle: 16 columns of a key are 16 bytes, keys 16 bytes apart, groups of 16
+// columns 2 KB apart.  So a thread, which holds one key, stores a key's parts 16 bytes at a time; K-major, a byte for
+// each row and part (48 for 16 rows), a tile's weights took twice as long.
+__device__ __forceinline__ uint64_t weights_desc(uint32_t addr)
+{
+    return ptx::smem_desc_sw128(addr, 8 * 16, 2048) & ~(7ull << 61);
+}
+
 // byte offset of 16-byte chunk c of row r in a tile of HD-byte rows
 template <int HD>
 __device__ __forceinline__ int row_chunk(int r, int c)
@@ -98,20 +136,20 @@ struct Q8Cfg {
     static constexpr int kOffV = kQ8Stages * kTile;
     static constexpr int kOffZero = 2 * kQ8Stages * kTile;       // d = 64: O^T rows 64..127 read zeros here
     static constexpr int kZero = HD == 64 ? kTile : 0;
-    static constexpr int kNQ = RB > 8 ? 32 : 16;                 // columns of S^T: high parts, then low parts
-    static constexpr int kQLo = kNQ / 2;
     static constexpr int kParts = 3;                             // of a weight, RB columns of O^T each
     static constexpr int kNP = (kParts * RB + 15) / 16 * 16;
     static constexpr int kOffQ = kOffZero + kZero;
-    static constexpr int kQBytes = kNQ * HD;                     // per ring entry
+    static constexpr bool kQSum = RB > 8;                        // both parts of q in the same columns
+    static constexpr int kQPart = kNQ * HD;                      // .. from two operands; else rows 0.. and 8.. of one
+    static constexpr int kQBytes = (kQSum ? 2 : 1) * kQPart;     // per ring entry
     static constexpr int kOffP = kOffQ + kQ8Ring * kQBytes;
     static constexpr int kPBytes = kNP * 128;
     static constexpr int kCT = q8_max_chunk(RB);                 // tiles of a chunk whose scores TMEM holds, twice
-    static constexpr int kOffRed = kOffP + 2 * kPBytes;          // float [2 groups][4 warps][16], then the maxima [2][16]
-    static constexpr int kOffBar = kOffRed + (8 + 2) * 16 * 4;
-    // k_full, k_empty, v_full, v_empty [stages]; s_full [2][kCT]; s_free, m_full, p_full, o_done [2]; drain;
-    // ch_full, ch_empty [ring]; o_item, o_free, stats [2]; desc_full, desc_empty [2]
-    static constexpr int kNumBars = 4 * kQ8Stages + 2 * kCT + 9 + 2 * kQ8Ring + 6 + 2 * kQ8Desc;
+    static constexpr int kOffRed = kOffP + 2 * kPBytes;          // float [12 warps][16], then the maxima [2][16]
+    static constexpr int kOffBar = kOffRed + (12 + 2) * 16 * 4;
+    // k_full, v_full, v_empty [stages]; s_full [2][kCT]; s_free, m_full, p_full, drain [2];
+    // ch_full, ch_empty [ring]; o_item, o_free, stats [2]; desc_full, desc_empty [kQ8Desc]
+    static constexpr int kNumBars = 3 * kQ8Stages + 2 * kCT + 8 + 2 * kQ8Ring + 6 + 2 * kQ8Desc;
     static constexpr int kOffMisc = kOffBar + kNumBars * 8;      // tmem slot, abort, K / V tiles issued
     static constexpr int kStatsFloats = 2 + 2 * RB;              // id, 2^(evm - 8), m[RB], l[RB]
     static constexpr int kOffStats = kOffMisc + 16;
@@ -176,6 +214,31 @@ __device__ __forceinline__ Q8Chunk q8_chunk(const Q8AttnParams &p, const Q8Seq *
     return ci;
 }
 
+// Reduces v[r] over the warp's lanes for every r < N (4, 8 or 16), always in the same order: each step halves the rows
+// that a lane still holds.  The lane keeps v[0], of row reduced_row<N>().
+template <int N, typename Op>
+__device__ __forceinline__ void reduce_rows(float (&v)[N], const Op &op)
+{
+    const int lane = threadIdx.x & 31;
+    int m = 16;
+#pragma unroll
+    for (int c = N / 2; c >= 1; c >>= 1, m >>= 1) {
+        const bool up = lane & m;
+#pragma unroll
+        for (int i = 0; i < c; ++i) {
+            const float got = __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + c], m);
+            v[i] = op(up ? v[i + c] : v[i], got);
+        }
+    }
+    for (; m >= 1; m >>= 1) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], m));
+}
+template <int N>
+__device__ __forceinline__ int reduced_row()
+{
+    constexpr int kBits = N == 16 ? 4 : (N == 8 ? 3 : 2);
+    return (threadIdx.x & 31) >> (5 - kBits);  // lane bit 4 chose the upper half of the rows, bit 3 of those, ..
+}
+
 template <int HD, int RB>
 __global__ void __launch_bounds__(kQ8Threads, 1)
     attn_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -187,28 +250,26 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
-    const int g = p.group;
 
     const uint32_t sbase = ptx::smem_addr(smem);
     float *s_red = reinterpret_cast<float *>(smem + C::kOffRed);
     const uint32_t bar0 = sbase + C::kOffBar;
     auto k_full = [&](int s) { return bar0 + 8u * s; };
-    auto k_empty = [&](int s) { return bar0 + 8u * (kQ8Stages + s); };
-    auto v_full = [&](int s) { return bar0 + 8u * (2 * kQ8Stages + s); };
-    auto v_empty = [&](int s) { return bar0 + 8u * (3 * kQ8Stages + s); };
-    const uint32_t b_s_full = bar0 + 8u * 4 * kQ8Stages;      // [2][kCT] a tile's scores, by chunk parity
+    auto v_full = [&](int s) { return bar0 + 8u * (kQ8Stages + s); };
+    auto v_empty = [&](int s) { return bar0 + 8u * (2 * kQ8Stages + s); };  // P V done: also frees the tile's P^T
+    // [2][kCT] a tile's scores, by chunk parity; also frees its K stage
+    const uint32_t b_s_full = bar0 + 8u * 3 * kQ8Stages;
     const uint32_t b_s_free = b_s_full + 8 * 2 * C::kCT;      // [2] a chunk's scores have been read
     const uint32_t b_m_full = b_s_free + 16;                  // [2] a chunk's maxima are in s_max
     const uint32_t b_p_full = b_m_full + 16;                  // [2]
-    const uint32_t b_o_done = b_p_full + 16;                  // [2]
-    const uint32_t b_drain = b_o_done + 16;
-    const uint32_t b_ch_full = b_drain + 8;                   // [R] a chunk's id, scales and q parts are in its entry
+    const uint32_t b_drain = b_p_full + 16;                   // [2] S^T, O^T
+    const uint32_t b_ch_full = b_drain + 16;                  // [R] a chunk's id, scales and q parts are in its entry
     const uint32_t b_ch_empty = b_ch_full + 8 * R;            // [R] the weights are done with the chunk
     const uint32_t b_o_item = b_ch_empty + 8 * R;             // [2] a chunk's O^T is complete
     const uint32_t b_o_free = b_o_item + 16;                  // [2] the epilogue has read that O^T buffer
     const uint32_t b_stats = b_o_free + 16;                   // [2] a chunk's statistics are in s_stats
-    const uint32_t b_desc_full = b_stats + 16;                // [2] a chunk's TMA rows are in s_desc
-    const uint32_t b_desc_empty = b_desc_full + 8 * kQ8Desc;  // [2] both producers have issued that chunk
+    const uint32_t b_desc_full = b_stats + 16;                // [kQ8Desc] a chunk's TMA rows are in s_desc
+    const uint32_t b_desc_empty = b_desc_full + 8 * kQ8Desc;  // [kQ8Desc] both producers have issued that chunk
     float *s_stats = reinterpret_cast<float *>(smem + C::kOffStats);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::kOffMisc + 4);
@@ -222,24 +283,22 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
     if (threadIdx.x == 384) {
         for (int s = 0; s < kQ8Stages; ++s) {
             ptx::mbar_init(k_full(s), 1);
-            ptx::mbar_init(k_empty(s), 1);
             ptx::mbar_init(v_full(s), 1);
             ptx::mbar_init(v_empty(s), 1);
         }
         for (int b = 0; b < 2 * C::kCT; ++b) ptx::mbar_init(b_s_full + 8 * b, 1);
         for (int b = 0; b < 2; ++b) {
-            ptx::mbar_init(b_s_free + 8 * b, 128);
+            ptx::mbar_init(b_s_free + 8 * b, 256);
             ptx::mbar_init(b_m_full + 8 * b, 1);
             ptx::mbar_init(b_p_full + 8 * b, 128);
-            ptx::mbar_init(b_o_done + 8 * b, 1);
+            ptx::mbar_init(b_drain + 8 * b, 1);
             ptx::mbar_init(b_o_item + 8 * b, 1);
             ptx::mbar_init(b_o_free + 8 * b, 128);
             ptx::mbar_init(b_stats + 8 * b, 1);
         }
-        ptx::mbar_init(b_drain, 1);
         for (int r = 0; r < R; ++r) {
             ptx::mbar_init(b_ch_full + 8 * r, 1);
-            ptx::mbar_init(b_ch_empty + 8 * r, 1 + 128);  // MMA, weight threads
+            ptx::mbar_init(b_ch_empty + 8 * r, 2 + 256);  // MMA warps, weight threads
         }
         for (int d = 0; d < kQ8Desc; ++d) {
             ptx::mbar_init(b_desc_full + 8 * d, 1);
@@ -283,21 +342,27 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         const CUtensorMap *map = is_v ? &tm_v : &tm_k;
         const int n_boxes = kQ8Keys / p.ps;  // a page a box
         int i = 0;                           // tile ordinal in this CTA
+        uint32_t used[kQ8Stages] = {};       // K: the score barrier (and its parity << 8) of the last tiles, newest first
         for (int n = 0;; ++n) {
             const int d = n % kQ8Desc;
-            if (!wait_bar_warp(b_desc_full + 8 * d, (n / kQ8Desc) & 1, wctx)) break;
+            if (!wait_spin(b_desc_full + 8 * d, (n / kQ8Desc) & 1, wctx)) break;
             const int *desc = s_desc + d * kQ8DescInts;
             if (desc[0] < 0) break;  // no more chunks
             const int nt = desc[1];
             bool ok = true;
             for (int k = 0; k < nt; ++k) {
                 const int s = i % kQ8Stages;
-                const uint32_t b_empty = is_v ? v_empty(s) : k_empty(s);
                 const uint32_t b_full = is_v ? v_full(s) : k_full(s);
-                if (i >= kQ8Stages && !wait_bar_warp(b_empty, ((i / kQ8Stages) - 1) & 1, wctx)) {
-                    ok = false;
-                    break;
+                if (i >= kQ8Stages) {
+                    const uint32_t u = used[kQ8Stages - 1];
+                    if (!(is_v ? wait_spin(v_empty(s), ((i / kQ8Stages) - 1) & 1, wctx) : wait_spin(b_s_full + 8 * (u & 255u), u >> 8, wctx))) {
+                        ok = false;
+                        break;
+                    }
                 }
+#pragma unroll
+                for (int x = kQ8Stages - 1; x > 0; --x) used[x] = used[x - 1];
+                used[0] = (n & 1) * C::kCT + k + (((n >> 1) & 1) << 8);
                 if (lane == 0) ptx::mbar_arrive_expect_tx(b_full, C::kTile);
                 __syncwarp();
                 if (lane < n_boxes)
@@ -312,86 +377,108 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         }
     } else if (warp == 15) {
         // ============================================================ scheduler
-        const int n_slots = kQ8Keys / p.ps;  // <= 16
-        for (int n = 0;; ++n) {
-            const int d = n % kQ8Desc;
-            const bool ok = n < kQ8Desc || wait_bar_warp(b_desc_empty + 8 * d, ((n / kQ8Desc) - 1) & 1, wctx);
+        const int lg = p.log_group, lps = p.log_ps;
+        const int n_slots = kQ8Keys >> lps;  // <= 16
+        constexpr int kPer = kQ8MaxChunk / 2;
+        constexpr int kPieces = HD / 8;       // of a q row, eight columns each; lane e: row e / kPieces, piece e % kPieces
+        constexpr int kRowsAt = 32 / kPieces;
+        constexpr int kPasses = RB / kRowsAt;
+        const int pc = lane % kPieces;
+        auto claim = [&](int n) -> int {  // lane 0's is the id of chunk ordinal n (-1: no more)
             int c = -1;
-            if (ok && lane == 0) {
+            if (lane == 0) {
                 c = n < 2 ? n * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x)
                           : 2 * static_cast<int>(gridDim.x) + atomicAdd(p.sched, 1);
                 if (c >= p.total_chunks) c = -1;
             }
-            c = __shfl_sync(0xffffffffu, c, 0);
-            int *desc = s_desc + d * kQ8DescInts;
-            Q8Chunk ci{};
-            constexpr int kPer = kQ8MaxChunk / 2;
-            int ex[kPer];  // (ek, ev) of entry e = 32 u + lane: tile e / 16, page slot e % 16
-            int evm = -126;
-            if (c >= 0) {
-                ci = q8_chunk(p, s_seqs, s_rem, c);
-                const Q8Seq &sq = s_seqs[ci.si];
-                int pg[kPer];
-                bool in[kPer];
+            return c;
+        };
+        // page ids of a chunk: entry e = 32 u + lane is tile e / 16, page slot e % 16
+        auto load_pages = [&](const Q8Chunk &ci, int (&pg)[kPer]) {
+            const Q8Seq &sq = s_seqs[ci.si];
 #pragma unroll
-                for (int u = 0; u < kPer; ++u) {
-                    const int e = 32 * u + lane;
-                    const int key0 = (ci.t0 + (e >> 4)) * kQ8Keys + (e & 15) * p.ps;
-                    in[u] = ci.t0 + (e >> 4) < ci.t1 && (e & 15) < n_slots && key0 < sq.n_keys;
-                    pg[u] = in[u] ? p.page_table[sq.table_row + key0 / p.ps] : -1;
-                }
+            for (int u = 0; u < kPer; ++u) {
+                const int e = 32 * u + lane;
+                const int key0 = (ci.t0 + (e >> 4)) * kQ8Keys + ((e & 15) << lps);
+                const bool in = ci.t0 + (e >> 4) < ci.t1 && (e & 15) < n_slots && key0 < sq.n_keys;
+                pg[u] = in ? p.page_table[sq.table_row + (key0 >> lps)] : INT32_MIN;
+            }
+        };
+        // Loads under load take 2000 cycles, so the next chunk's are in flight while this one's are used.
+        int c = __shfl_sync(0xffffffffu, claim(0), 0);
+        Q8Chunk ci{};
+        int pg[kPer];
+        if (c >= 0) {
+            ci = q8_chunk(p, s_seqs, s_rem, c);
+            load_pages(ci, pg);
+        }
+        for (int n = 0;; ++n) {
+            const int d = n % kQ8Desc;
+            const int claimed = c >= 0 ? claim(n + 1) : -1;
+            if (n >= kQ8Desc && !wait_spin(b_desc_empty + 8 * d, ((n / kQ8Desc) - 1) & 1, wctx)) c = -1;
+            int *desc = s_desc + d * kQ8DescInts;
+            int ex[kPer];  // (ek, ev)
+            uint4 qv[kPasses];
+            if (c >= 0) {
+                const Q8Seq &sq = s_seqs[ci.si];
 #pragma unroll
                 for (int u = 0; u < kPer; ++u) {
                     const bool ok_page = pg[u] >= 0 && pg[u] < p.num_pages;
-                    if (!ok_page && in[u]) atomicCAS(p.status, 0, kStatusBadPage);
-                    const int head = (p.layer * p.num_pages + pg[u]) * p.hkv + ci.kvh;
-                    desc[8 + 32 * u + lane] = ok_page ? head * p.ps : p.oob_row;  // past the sequence (or a bad id): zeros
-                    ex[u] = ok_page ? reinterpret_cast<const uint16_t *>(p.exps)[head] : 0x8282;  // -126, -126
+                    if (!ok_page && pg[u] != INT32_MIN) atomicCAS(p.status, 0, kStatusBadPage);
+                    pg[u] = ok_page ? (p.layer * p.num_pages + pg[u]) * p.hkv + ci.kvh : -1;
+                    desc[8 + 32 * u + lane] = pg[u] >= 0 ? pg[u] << lps : p.oob_row;  // past the sequence (or a bad id): zeros
                 }
-#pragma unroll
-                for (int u = 0; u < kPer; ++u) evm = max(evm, static_cast<int>(static_cast<int8_t>(ex[u] >> 8)));
-                evm = __reduce_max_sync(0xffffffffu, evm);
                 if (lane == 0) {
                     desc[0] = c;
                     desc[1] = ci.t1 - ci.t0;
                 }
-            } else if (lane == 0) {
-                desc[0] = -1;
-            }
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(b_desc_full + 8 * d);  // release: the producers read the rows
-
-            // q of the chunk's rows (bf16), while the ring entry's previous chunk is finished
-            constexpr int kPieces = HD / 8;       // eight columns each; lane e: row e / kPieces, piece e % kPieces
-            constexpr int kRowsAt = 32 / kPieces;
-            constexpr int kPasses = RB / kRowsAt;
-            const int pc = lane % kPieces;
-            uint4 qv[kPasses];
-#pragma unroll
-            for (int j = 0; j < kPasses; ++j) {
-                qv[j] = make_uint4(0u, 0u, 0u, 0u);
-                if (c < 0) continue;
-                const Q8Seq &sq = s_seqs[ci.si];
-                const int row = ci.blk * RB + j * kRowsAt + lane / kPieces;
-                if (row < sq.n_q * g)
-                    qv[j] = *reinterpret_cast<const uint4 *>(
-                        p.q + (static_cast<int64_t>(sq.q_row0 + row / g) * p.hq + ci.kvh * g + row % g) * HD + pc * 8);
-            }
-            if (n >= R && !wait_bar_warp(b_ch_empty + 8 * (n % R), ((n / R) - 1) & 1, wctx)) break;
-            uint8_t *en = entry(n);
-            if (c >= 0) {
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(b_desc_full + 8 * d);  // release: the producers read the rows
 #pragma unroll
                 for (int u = 0; u < kPer; ++u)
+                    ex[u] = pg[u] >= 0 ? reinterpret_cast<const uint16_t *>(p.exps)[pg[u]] : 0x8282;  // -126, -126
+#pragma unroll
+                for (int j = 0; j < kPasses; ++j) {
+                    qv[j] = make_uint4(0u, 0u, 0u, 0u);
+                    const int row = ci.blk * RB + j * kRowsAt + lane / kPieces;
+                    if (row < sq.n_q << lg)
+                        qv[j] = *reinterpret_cast<const uint4 *>(
+                            p.q + (static_cast<int64_t>(sq.q_row0 + (row >> lg)) * p.hq + (ci.kvh << lg) + (row & ((1 << lg) - 1))) * HD + pc * 8);
+                }
+            } else if (lane == 0) {
+                desc[0] = -1;
+                ptx::mbar_arrive(b_desc_full + 8 * d);
+            }
+            const int c_next = __shfl_sync(0xffffffffu, claimed, 0);
+            Q8Chunk ci_next{};
+            if (c_next >= 0) {
+                ci_next = q8_chunk(p, s_seqs, s_rem, c_next);
+                load_pages(ci_next, pg);
+            }
+            if (n >= R && !wait_spin(b_ch_empty + 8 * (n % R), ((n / R) - 1) & 1, wctx)) break;
+            uint8_t *en = entry(n);
+            if (c >= 0) {
+                int evm = -126;
+#pragma unroll
+                for (int u = 0; u < kPer; ++u) {
+                    evm = max(evm, static_cast<int>(static_cast<int8_t>(ex[u] >> 8)));
                     reinterpret_cast<uint16_t *>(en + 80)[32 * u + lane] = static_cast<uint16_t>(ex[u]);
+                }
+                evm = __reduce_max_sync(0xffffffffu, evm);
+                if (lane == 0) reinterpret_cast<int *>(en)[1] = evm;
                 uint8_t *qb = smem + C::kOffQ + (n % R) * C::kQBytes;
+                uint32_t amax[kPasses];
+#pragma unroll
+                for (int j = 0; j < kPasses; ++j) amax[j] = bf16x8_absmax(qv[j]);
+#pragma unroll
+                for (int off = kPieces / 2; off >= 1; off >>= 1)
+#pragma unroll
+                    for (int j = 0; j < kPasses; ++j) amax[j] = max(amax[j], __shfl_xor_sync(0xffffffffu, amax[j], off));
 #pragma unroll
                 for (int j = 0; j < kPasses; ++j) {
                     const int r = j * kRowsAt + lane / kPieces;
-                    uint32_t a = bf16x8_absmax(qv[j]);
-#pragma unroll
-                    for (int off = kPieces / 2; off >= 1; off >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, off));
-                    const bool bad = a >= 0x7f80u;  // an infinity or NaN in the row: the row becomes NaN
-                    const int eq = bad ? 0 : q8_exponent(a);
+                    const bool bad = amax[j] >= 0x7f80u;  // an infinity or NaN in the row: the row becomes NaN
+                    const int eq = bad ? 0 : q8_exponent(amax[j]);
                     const float s = pow2i(-eq);
                     const uint32_t w[4] = {qv[j].x, qv[j].y, qv[j].z, qv[j].w};
                     uint32_t hi[4], low[4];
@@ -400,25 +487,27 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                         const float2 f = make_float2(__uint_as_float(w[x] << 16) * s, __uint_as_float(w[x] & 0xffff0000u) * s);
                         hi[x] = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
                         const float2 h = e4m3x2_to_float2(hi[x]);
-                        low[x] = __nv_cvt_float2_to_fp8x2(make_float2((f.x - h.x) * 16.f, (f.y - h.y) * 16.f), __NV_SATFINITE, __NV_E4M3);
+                        constexpr float kUp = C::kQSum ? 1.f : 16.f;
+                        low[x] = __nv_cvt_float2_to_fp8x2(make_float2((f.x - h.x) * kUp, (f.y - h.y) * kUp), __NV_SATFINITE, __NV_E4M3);
                     }
                     uint2 vh = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-                    uint2 vl = make_uint2(low[0] | low[1] << 16, low[2] | low[3] << 16);
+                    const uint2 vl = make_uint2(low[0] | low[1] << 16, low[2] | low[3] << 16);
                     if (bad) vh = make_uint2(kQ8NanWord, kQ8NanWord);
                     *reinterpret_cast<uint2 *>(qb + row_chunk<HD>(r, pc >> 1) + (pc & 1) * 8) = vh;
-                    *reinterpret_cast<uint2 *>(qb + row_chunk<HD>(C::kQLo + r, pc >> 1) + (pc & 1) * 8) = vl;
+                    *reinterpret_cast<uint2 *>(qb + (C::kQSum ? C::kQPart + row_chunk<HD>(r, pc >> 1) : row_chunk<HD>(kNQ / 2 + r, pc >> 1)) +
+                                                (pc & 1) * 8) = vl;
                     if (pc == 0) reinterpret_cast<float *>(en + 16)[r] = pow2i(eq);
                 }
                 ptx::fence_proxy_async_smem();
             }
-            if (lane == 0) {
-                reinterpret_cast<int *>(en)[0] = c;
-                reinterpret_cast<int *>(en)[1] = evm;
-            }
+            if (lane == 0) reinterpret_cast<int *>(en)[0] = c;
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(b_ch_full + 8 * (n % R));  // release: the other roles read the entry
             if (c < 0) break;
+            c = c_next;
+            ci = ci_next;
         }
+        ptx::griddep_launch_dependents();  // the merge's blocks come as CTAs end
         // the last scheduler to stop resets the counter for the next launch
         if (lane == 0) {
             __threadfence();
@@ -428,122 +517,133 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                 __threadfence();
             }
         }
-    } else if (warp == 13) {
-        // ============================================================ MMA issuer (the whole warp, converged)
-        constexpr uint32_t kIdS = idesc_e4m3_f32(128, C::kNQ, false);
+    } else if (warp == 13 || warp == 16) {
+        // ============================================================ MMA issuers (converged warps; one lane issues)
+        const bool is_s = warp == 13;
+        constexpr uint32_t kIdS = idesc_e4m3_f32(128, kNQ, false);
         constexpr uint32_t kIdPV = idesc_e4m3_f32(128, C::kNP, true);
-        constexpr uint32_t kAll = 0xffffffffu;
-        const uint32_t tm = __shfl_sync(kAll, tmem, 0);
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
         const uint64_t k_desc = row_desc<HD>(sbase, 16);
         const uint64_t q_desc = row_desc<HD>(sbase + C::kOffQ, 16);
-        const uint64_t p_desc = ptx::smem_desc_sw128(sbase + C::kOffP, 16, 1024);
-        auto ready = [&](uint32_t bar, int parity) -> bool {
-            return __all_sync(kAll, ptx::mbar_test_wait(bar, parity));
-        };
-        // the S^T cursor: chunk ordinal ns_chunk, its tiles (-1: not read yet, 0: no more chunks), the next one
-        int ns = 0, ns_chunk = 0, s_tiles = -1, s_tile = 0;
-        // the P V cursor; pv_tiles: the tiles of the chunks the S^T cursor has read, byte n & 7 (it is at most
-        // four chunks ahead)
-        int np = 0, np_chunk = 0, p_done = 0;
-        uint64_t pv_tiles = 0;
-        auto tiles_of = [&](int n) -> int { return static_cast<int>(pv_tiles >> (8 * (n & 7))) & 0xff; };
-        uint64_t t_last = ptx::globaltimer();
-        while (s_tiles != 0 || np_chunk < ns_chunk) {
-            bool progress = false;
-            if (s_tiles < 0 && ready(b_ch_full + 8 * (ns_chunk % R), (ns_chunk / R) & 1)) {
-                const int c = reinterpret_cast<volatile int *>(entry(ns_chunk))[0];
-                int nt = 0;
-                if (c >= 0) {
-                    const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
-                    nt = ci.t1 - ci.t0;
-                }
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(b_ch_empty + 8 * (ns_chunk % R));
-                s_tiles = __shfl_sync(kAll, nt, 0);
-                s_tile = 0;
-                const int sh = 8 * (ns_chunk & 7);
-                pv_tiles = (pv_tiles & ~(0xffull << sh)) | (static_cast<uint64_t>(s_tiles) << sh);
-                progress = true;
-            }
-            // S^T: K landed; at a chunk's first tile, the scores of the chunk before the last read
-            if (s_tiles > 0 && ready(k_full(ns % kQ8Stages), (ns / kQ8Stages) & 1) &&
-                (s_tile > 0 || ns_chunk < 2 || ready(b_s_free + 8 * (ns_chunk & 1), ((ns_chunk - 2) >> 1) & 1))) {
-                const int s = ns % kQ8Stages, at = (ns_chunk & 1) * C::kCT + s_tile;
-                ptx::tc_fence_after();
-                const uint64_t kd = k_desc + s * (C::kTile >> 4);
-                const uint64_t qd = q_desc + (ns_chunk % R) * (C::kQBytes >> 4);
+        const uint64_t p_desc = weights_desc(sbase + C::kOffP);
+        int i = 0;  // tile ordinal in this CTA
+        bool ok = true;
+        for (int n = 0; ok; ++n) {
+            if (!wait_spin(b_ch_full + 8 * (n % R), (n / R) & 1, wctx)) break;
+            const int c = reinterpret_cast<volatile int *>(entry(n))[0];
+            if (c < 0) break;
+            const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
+            const int nt = __shfl_sync(0xffffffffu, ci.t1 - ci.t0, 0);
+            if (lane == 0) ptx::mbar_arrive(b_ch_empty + 8 * (n % R));
+            // the scores, or the O^T, of the chunk before the last have been read
+            if (n >= 2 && !wait_spin((is_s ? b_s_free : b_o_free) + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx)) break;
+            for (int j = 0; j < nt; ++j, ++i) {
+                const int s = i % kQ8Stages;
+                if (is_s) {
+                    if (!(ok = wait_spin(k_full(s), (i / kQ8Stages) & 1, wctx))) break;
+                    ptx::tc_fence_after();
+                    const int at = (n & 1) * C::kCT + j;
+                    const uint64_t kd = k_desc + s * (C::kTile >> 4);
+                    const uint64_t qd = q_desc + (n % R) * (C::kQBytes >> 4);
 #pragma unroll
-                for (int kk = 0; kk < HD / 32; ++kk)
-                    mma_e4m3_warp(tm + C::kNQ * at, kd + (kk * 32 >> 4), qd + (kk * 32 >> 4), kIdS, kk > 0 ? 1u : 0u);
-                mma_commit_warp(b_s_full + 8 * at);
-                mma_commit_warp(k_empty(s));
-                ++ns;
-                if (++s_tile == s_tiles) {
-                    ++ns_chunk;
-                    s_tiles = -1;
-                }
-                progress = true;
-            }
-            // O^T += V^T P^T(np): V landed, P^T(np) written (so its scores are complete), at a chunk's first tile the
-            // O^T buffer read
-            if (np < ns && ready(v_full(np % kQ8Stages), (np / kQ8Stages) & 1) &&
-                ready(b_p_full + 8 * (np & 1), (np >> 1) & 1) &&
-                (p_done > 0 || np_chunk < 2 || ready(b_o_free + 8 * (np_chunk & 1), ((np_chunk - 2) >> 1) & 1))) {
-                ptx::tc_fence_after();
-                const int s = np % kQ8Stages;
-                const uint32_t va = sbase + C::kOffV + s * C::kTile;
-                const uint64_t vd = row_desc<HD>(va, HD == 64 ? sbase + C::kOffZero - va : 16);
-                const uint64_t pd = p_desc + (np & 1) * (C::kPBytes >> 4);
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)  // 32 keys each
-                    mma_e4m3_warp(tm + C::kTmemO + C::kNP * (np_chunk & 1), vd + (kk * 32 * HD >> 4), pd + (kk * 32 >> 4), kIdPV,
-                                  (p_done > 0 || kk > 0) ? 1u : 0u);
-                mma_commit_warp(v_empty(s));
-                mma_commit_warp(b_o_done + 8 * (np & 1));
-                ++np;
-                if (++p_done == tiles_of(np_chunk)) {
-                    mma_commit_warp(b_o_item + 8 * (np_chunk & 1));
-                    ++np_chunk;
-                    p_done = 0;
-                }
-                progress = true;
-            }
-            if (progress) {
-                t_last = ptx::globaltimer();
-            } else {
-                if (__any_sync(kAll, *abort_flag != 0)) break;
-                if (__any_sync(kAll, ptx::globaltimer() - t_last > kWaitNs)) {
-                    if (lane == 0) {
-                        *abort_flag = 1;
-                        atomicCAS(p.status, 0, kStatusWaitTimeout);
+                    for (int kk = 0; kk < (C::kQSum ? 2 : 1) * (HD / 32); ++kk) {
+                        const int col = kk % (HD / 32) * 32, part = kk / (HD / 32);
+                        mma_e4m3_warp(tm + kNQ * at, kd + (col >> 4), qd + ((part * C::kQPart + col) >> 4), kIdS, kk > 0 ? 1u : 0u);
                     }
-                    break;
+                    mma_commit_warp(b_s_full + 8 * at);
+                } else {
+                    // (the weights are written once the scores are complete, so P^T(i) stands for S^T(i) too)
+                    if (!(ok = wait_spin(v_full(s), (i / kQ8Stages) & 1, wctx) && wait_spin(b_p_full + 8 * (i & 1), (i >> 1) & 1, wctx))) break;
+                    ptx::tc_fence_after();
+                    const uint32_t va = sbase + C::kOffV + s * C::kTile;
+                    const uint64_t vd = row_desc<HD>(va, HD == 64 ? sbase + C::kOffZero - va : 16);
+                    const uint64_t pd = p_desc + (i & 1) * (C::kPBytes >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)  // 32 keys each
+                        mma_e4m3_warp(tm + C::kTmemO + C::kNP * (n & 1), vd + (kk * 32 * HD >> 4), pd + (kk * 32 * 16 >> 4), kIdPV,
+                                      (j > 0 || kk > 0) ? 1u : 0u);
+                    mma_commit_warp(v_empty(s));
+                    if (j == nt - 1) mma_commit_warp(b_o_item + 8 * (n & 1));
                 }
             }
         }
-        mma_commit_warp(b_drain);
+        // every tcgen05 op of this warp completes before TMEM is released
+        const uint32_t b_mine = b_drain + (is_s ? 0 : 8);
+        mma_commit_warp(b_mine);
         if (lane == 0) {
             const uint64_t start = ptx::globaltimer();
-            while (!ptx::mbar_try_wait(b_drain, 0) && ptx::globaltimer() - start < 4000000ull) {
+            while (!ptx::mbar_try_wait(b_mine, 0) && ptx::globaltimer() - start < 4000000ull) {
             }
         }
         __syncwarp();
-    } else if (warp < 8) {
-        // ============================================================ maxima (warps 0-3), weights (4-7): thread = key
+    } else {
+        // ============================================================ maxima and epilogue (warps 0-3), weights (4-11)
         const bool is_max = warp < 4;
-        const int t = threadIdx.x & 127;
-        const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const int slot = t / p.ps;
-        float *red = s_red + (is_max ? 0 : 4 * 16);
-        float *s_max = s_red + 8 * 16;  // [2][16]
+        const int t = threadIdx.x & 127;      // key of the tile, or d-column
+        const int grp = (warp >> 2) - 1;      // weights: the tiles of ordinal grp mod 2
+        const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;  // the TMEM lanes this warp may access
+        const int slot = t >> p.log_ps;
+        float *s_max = s_red + 12 * 16;       // [2][16]
         const int lg = p.log_group;
+        // the output, or the partial, of chunk ordinal n
+        auto epilogue = [&](int n) -> bool {
+            if (!wait_spin(b_stats + 8 * (n & 1), (n >> 1) & 1, wctx)) return false;
+            const float *st = s_stats + (n & 1) * C::kStatsFloats;
+            const int c = __float_as_int(st[0]);
+            const float scale = st[1], my_m = st[2 + t % RB], my_l = st[2 + RB + t % RB];
+            float o[RB], lsum[RB];
+#pragma unroll
+            for (int r = 0; r < RB; ++r) lsum[r] = st[2 + RB + r];
+            if (!wait_spin(b_o_item + 8 * (n & 1), (n >> 1) & 1, wctx)) return false;
+            ptx::tc_fence_after();
+            const uint32_t to = tmem + C::kTmemO + C::kNP * (n & 1) + lane_off;
+            ptx::tmem_ld_n<RB>(to + (C::kParts - 1) * RB, o);
+#pragma unroll
+            for (int k = C::kParts - 2; k >= 0; --k) {
+                float part[RB];
+                ptx::tmem_ld_n<RB>(to + k * RB, part);
+                ptx::tmem_wait_ld();
+#pragma unroll
+                for (int r = 0; r < RB; ++r) o[r] = fmaf(o[r], kQ8Unpart, part[r]);
+            }
+            ptx::tc_fence_before();
+            ptx::mbar_arrive(b_o_free + 8 * (n & 1));  // O^T buffer and stats slot may be reused
+            const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
+            const Q8Seq &sq = s_seqs[ci.si];
+            const int row0 = ci.blk * RB;
+            const int n_rows = min(RB, (sq.n_q << lg) - row0);
+            if (q8_tiles(sq) <= sq.ct) {
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    if (r >= n_rows) continue;
+                    const int row = row0 + r;
+                    const int64_t at = static_cast<int64_t>(sq.q_row0 + (row >> lg)) * p.hq + (ci.kvh << lg) + (row & ((1 << lg) - 1));
+                    // (a sum that is NaN: the row sees a NaN)
+                    if (t < HD && p.out) p.out[at * HD + t] = __float2bfloat16_rn(o[r] * scale * (lsum[r] > 0.f ? 1.0f / lsum[r] : lsum[r]));
+                    if (p.lse && t == r) p.lse[at] = my_m + log2f(my_l);
+                }
+                return true;
+            }
+            float *po = p.part + static_cast<int64_t>(c) * RB * HD;
+            float *pm = p.part + static_cast<int64_t>(p.total_chunks) * RB * HD;
+            float *pl = pm + static_cast<int64_t>(p.total_chunks) * RB;
+            if (t < HD) {
+#pragma unroll
+                for (int r = 0; r < RB; ++r) po[r * HD + t] = o[r] * scale;
+            }
+            if (t < RB) {
+                pm[static_cast<int64_t>(c) * RB + t] = my_m;
+                pl[static_cast<int64_t>(c) * RB + t] = my_l;
+            }
+            return true;
+        };
         int n = 0;   // chunk ordinal
         int i = 0;   // tile ordinal in this CTA
         bool stopped = false;
-        for (; !stopped; ++n) {
-            // (a wait that gave up is voted on, so that a group leaves together)
-            const bool got = wait_bar_warp(b_ch_full + 8 * (n % R), (n / R) & 1, wctx);
-            if (ptx::bar_sync_or(is_max ? kQ8BarMax : kQ8BarWeights, 128, !got)) {
+        for (;; ++n) {
+            // (a wait that gave up is voted on, here and after a chunk's tiles, so that a group leaves together)
+            if (!wait_spin(b_ch_full + 8 * (n % R), (n / R) & 1, wctx)) stopped = true;
+            if (ptx::bar_sync_or(is_max ? kQ8BarMax : kQ8BarWeights, is_max ? 128 : 256, stopped)) {
                 stopped = true;
                 break;
             }
@@ -560,8 +660,8 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             float qs[RB];
 #pragma unroll
             for (int r = 0; r < RB; ++r) qs[r] = reinterpret_cast<const float *>(en + 16)[r];
-            // s = scores without their scales, of tile ordinal j of the chunk; ks, dv: the key's K scale times
-            // scale_log2, and its V scale against the chunk's largest
+            // s = scores without their scales, of tile j of the chunk; ks, dv: the key's K scale times scale_log2, and
+            // its V scale against the chunk's largest
             float s[RB], ks;
             int dv;
             auto load_scores = [&](int j) -> bool {
@@ -570,18 +670,22 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                 dv = max(static_cast<int8_t>(ex.y) - evm, -100);
                 const int at = (n & 1) * C::kCT + j;
                 if (is_max) {  // (the weights come after the maxima of the whole chunk)
-                    if (!wait_bar_warp(b_s_full + 8 * at, (n >> 1) & 1, wctx)) return false;
+                    if (!wait_spin(b_s_full + 8 * at, (n >> 1) & 1, wctx)) return false;
                     ptx::tc_fence_after();
                 }
-                float low[RB];
-                ptx::tmem_ld_n<RB>(tmem + C::kNQ * at + lane_off, s);
-                ptx::tmem_ld_n<RB>(tmem + C::kNQ * at + C::kQLo + lane_off, low);
-                ptx::tmem_wait_ld();
+                ptx::tmem_ld_n<RB>(tmem + kNQ * at + lane_off, s);
+                if constexpr (!C::kQSum) {
+                    float low[RB];
+                    ptx::tmem_ld_n<RB>(tmem + kNQ * at + kNQ / 2 + lane_off, low);
+                    ptx::tmem_wait_ld();
 #pragma unroll
-                for (int r = 0; r < RB; ++r) s[r] = fmaf(low[r], kQ8Unpart, s[r]);
+                    for (int r = 0; r < RB; ++r) s[r] = fmaf(low[r], kQ8Unpart, s[r]);
+                } else {
+                    ptx::tmem_wait_ld();
+                }
                 return true;
             };
-            auto sees = [&](int key, int r) { return key <= qpos0 + ((row0 + r) >> lg); };  // (< n_keys for every row held)
+            auto sees = [&](int key, int r) { return key <= qpos0 + ((row0 + r) >> lg); };
             if (is_max) {
                 const int n_rows = min(RB, (sq.n_q << lg) - row0);
                 float *sc = p.scores ? p.scores + sq.score0 + (static_cast<int64_t>(ci.kvh) * (sq.n_q << lg) + row0) * sq.score_stride : nullptr;
@@ -615,23 +719,21 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                     stopped = true;
                     break;
                 }
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    const int b = __float_as_int(m[r]);  // integers in the order of the numbers
-                    const int k = __reduce_max_sync(0xffffffffu, b ^ ((b >> 31) & 0x7fffffff));
-                    if (lane == r) red[(warp & 3) * 16 + r] = __int_as_float(k ^ ((k >> 31) & 0x7fffffff));
-                }
+                reduce_rows<RB>(m, [](float x, float y) { return fmaxf(x, y); });
+                if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = m[0];
                 ptx::bar_sync(kQ8BarMax, 128);
                 // (the slot's chunk n - 2 has been read: its scores were freed before this chunk's were computed)
-                if (t < RB) s_max[(n & 1) * 16 + t] = fmaxf(fmaxf(red[t], red[16 + t]), fmaxf(red[32 + t], red[48 + t]));
+                if (t < RB) s_max[(n & 1) * 16 + t] = fmaxf(fmaxf(s_red[t], s_red[16 + t]), fmaxf(s_red[32 + t], s_red[48 + t]));
                 if (warp == 0) {
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(b_m_full + 8 * (n & 1));  // release: the weights read them
                 }
+                // the weights of chunk n - 2 are complete (its scores are free), its O^T is or will be soon
+                if (n >= 2) stopped = !epilogue(n - 2);
                 continue;
             }
             // ------------------------------------------------ weights
-            stopped = !wait_bar_warp(b_m_full + 8 * (n & 1), (n >> 1) & 1, wctx);
+            stopped = !wait_spin(b_m_full + 8 * (n & 1), (n >> 1) & 1, wctx);
             ptx::tc_fence_after();
             const float my_max = s_max[(n & 1) * 16 + lane % RB];
             float m8[RB], lpart[RB];  // 8 - m: the largest weight is 2^8
@@ -642,6 +744,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                 lpart[r] = 0.f;
             }
             for (int lt = ci.t0; lt < ci.t1 && !stopped; ++lt, ++i) {
+                if ((i & 1) != grp) continue;
                 (void)load_scores(lt - ci.t0);
                 const int key = lt * kQ8Keys + t;
                 const float fdv = static_cast<float>(dv), unv = pow2i(-dv);
@@ -656,128 +759,66 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
 #pragma unroll
                 for (int r = 0; r < RB; ++r) lpart[r] = fmaf(pr[r], unv, lpart[r]);
                 // P^T(i) into buffer i & 1 once O^T += V^T P^T(i - 2) has read it
-                if (i >= 2 && !wait_bar_warp(b_o_done + 8 * (i & 1), ((i - 2) >> 1) & 1, wctx)) {
+                if (i >= 2 && !wait_spin(v_empty((i - 2) % kQ8Stages), ((i - 2) / kQ8Stages) & 1, wctx)) {
                     stopped = true;
                     break;
                 }
-                uint8_t *pt = smem + C::kOffP + (i & 1) * C::kPBytes;
+                uint32_t pw[C::kNP / 4];  // column part * RB + r of O^T, a byte each
 #pragma unroll
-                for (int r = 0; r < RB; r += 2) {
-                    float2 w = make_float2(pr[r], pr[r + 1]);
+                for (int x = C::kParts * RB / 4; x < C::kNP / 4; ++x) pw[x] = 0u;
+#pragma unroll
+                for (int r = 0; r < RB; r += 4) {
+                    float2 w0 = make_float2(pr[r], pr[r + 1]), w1 = make_float2(pr[r + 2], pr[r + 3]);
 #pragma unroll
                     for (int part = 0; part < C::kParts; ++part) {
-                        const uint32_t q = __nv_cvt_float2_to_fp8x2(w, __NV_SATFINITE, __NV_E4M3);
-                        const int r0 = part * RB + r, r1 = r0 + 1;
-                        pt[row_chunk<128>(r0, t >> 4) + (t & 15)] = static_cast<uint8_t>(q);
-                        pt[row_chunk<128>(r1, t >> 4) + (t & 15)] = static_cast<uint8_t>(q >> 8);
+                        const uint32_t q0 = __nv_cvt_float2_to_fp8x2(w0, __NV_SATFINITE, __NV_E4M3);
+                        const uint32_t q1 = __nv_cvt_float2_to_fp8x2(w1, __NV_SATFINITE, __NV_E4M3);
+                        pw[(part * RB + r) / 4] = q0 | q1 << 16;
                         if (part + 1 < C::kParts) {
-                            const float2 h = e4m3x2_to_float2(q);
-                            w = make_float2((w.x - h.x) * 16.f, (w.y - h.y) * 16.f);
+                            const float2 h0 = e4m3x2_to_float2(q0), h1 = e4m3x2_to_float2(q1);
+                            w0 = make_float2((w0.x - h0.x) * 16.f, (w0.y - h0.y) * 16.f);
+                            w1 = make_float2((w1.x - h1.x) * 16.f, (w1.y - h1.y) * 16.f);
                         }
                     }
                 }
+                uint4 *pt = reinterpret_cast<uint4 *>(smem + C::kOffP + grp * C::kPBytes) + t;
+#pragma unroll
+                for (int x = 0; x < C::kNP / 16; ++x) pt[x * 128] = make_uint4(pw[4 * x], pw[4 * x + 1], pw[4 * x + 2], pw[4 * x + 3]);
                 ptx::fence_proxy_async_smem();
                 ptx::tc_fence_before();
-                ptx::mbar_arrive(b_p_full + 8 * (i & 1));
+                ptx::mbar_arrive(b_p_full + 8 * grp);
             }
-            if (ptx::bar_sync_or(kQ8BarWeights, 128, stopped)) {
+            // ---------------------------------------------------- row statistics for the epilogue
+            reduce_rows<RB>(lpart, [](float x, float y) { return x + y; });
+            if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = lpart[0];
+            if (ptx::bar_sync_or(kQ8BarWeights, 256, stopped)) {
                 stopped = true;
                 break;
             }
             ptx::mbar_arrive(b_s_free + 8 * (n & 1));
-
-            // ---------------------------------------------------- row statistics for the epilogue warps
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                float v = lpart[r];
-#pragma unroll
-                for (int off = 16; off >= 1; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-                if (lane == 0) red[(warp & 3) * 16 + r] = v;
-            }
-            ptx::bar_sync(kQ8BarWeights, 128);
             if (warp == 4) {
                 // the stats slot of chunk n - 2 must have been read
-                if (n >= 2) (void)wait_bar_warp(b_o_free + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx);
+                if (n >= 2) (void)wait_spin(b_o_free + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx);
                 float *st = s_stats + (n & 1) * C::kStatsFloats;
                 if (lane == 31) {
                     st[0] = __int_as_float(c);
                     st[1] = ldexpf(1.f, evm - 8);  // (subnormal where the chunk's V is)
                 }
                 if (lane < RB) {
+                    float l = 0.f;
+#pragma unroll
+                    for (int w = 4; w < 12; ++w) l += s_red[w * 16 + lane];
                     st[2 + lane] = my_max;
-                    st[2 + RB + lane] = ((red[lane] + red[16 + lane]) + (red[32 + lane] + red[48 + lane])) * (1.f / 256.f);
+                    st[2 + RB + lane] = l * (1.f / 256.f);
                 }
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(b_stats + 8 * (n & 1));  // release: the epilogue reads the slot
             }
-            ptx::mbar_arrive(b_ch_empty + 8 * (n % R));
+            ptx::mbar_arrive(b_ch_empty + 8 * (n % R));  // (warp 4 last: s_red is read)
         }
-        if (threadIdx.x == 128) {  // no more chunks: the epilogue warps stop at ordinal n
-            if (n >= 2) (void)wait_bar(b_o_free + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx);
-            s_stats[(n & 1) * C::kStatsFloats] = __int_as_float(-1);
-            ptx::mbar_arrive(b_stats + 8 * (n & 1));
-        }
-    } else {
-        // ============================================================ epilogue (thread = d-column = TMEM lane)
-        const int q4 = warp & 3;                       // TMEM lane quarter this warp may access
-        const int t = q4 * 32 + lane;                  // d-column
-        const uint32_t lane_off = static_cast<uint32_t>(q4 * 32) << 16;
-        for (int n = 0;; ++n) {
-            if (!wait_bar_warp(b_stats + 8 * (n & 1), (n >> 1) & 1, wctx)) break;
-            const float *st = s_stats + (n & 1) * C::kStatsFloats;
-            const int c = __float_as_int(st[0]);
-            if (c < 0) break;
-            const float scale = st[1], my_m = st[2 + t % RB], my_l = st[2 + RB + t % RB];
-            float o[RB], mref[RB], lsum[RB];
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                mref[r] = st[2 + r];
-                lsum[r] = st[2 + RB + r];
-                o[r] = 0.f;
-            }
-            if (wait_bar_warp(b_o_item + 8 * (n & 1), (n >> 1) & 1, wctx)) {
-                ptx::tc_fence_after();
-                const uint32_t to = tmem + C::kTmemO + C::kNP * (n & 1) + lane_off;
-                float part[C::kParts][RB];
-#pragma unroll
-                for (int k = 0; k < C::kParts; ++k) ptx::tmem_ld_n<RB>(to + k * RB, part[k]);
-                ptx::tmem_wait_ld();
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    float v = part[C::kParts - 1][r];
-#pragma unroll
-                    for (int k = C::kParts - 2; k >= 0; --k) v = fmaf(v, kQ8Unpart, part[k][r]);
-                    o[r] = v * scale;
-                }
-            }
-            ptx::tc_fence_before();
-            ptx::mbar_arrive(b_o_free + 8 * (n & 1));  // O^T buffer and stats slot may be reused
-            const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
-            const Q8Seq &sq = s_seqs[ci.si];
-            const int row0 = ci.blk * RB;
-            const int n_rows = min(RB, sq.n_q * g - row0);
-            if (q8_tiles(sq) <= sq.ct) {
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    if (r >= n_rows) continue;
-                    const int row = row0 + r;
-                    const int64_t at = static_cast<int64_t>(sq.q_row0 + row / g) * p.hq + ci.kvh * g + row % g;
-                    if (t < HD && p.out) p.out[at * HD + t] = __float2bfloat16_rn(o[r] * (lsum[r] > 0.f ? 1.0f / lsum[r] : 0.f));
-                    if (p.lse && t == r) p.lse[at] = mref[r] + log2f(lsum[r]);
-                }
-                continue;
-            }
-            float *po = p.part + static_cast<int64_t>(c) * RB * HD;
-            float *pm = p.part + static_cast<int64_t>(p.total_chunks) * RB * HD;
-            float *pl = pm + static_cast<int64_t>(p.total_chunks) * RB;
-            if (t < HD) {
-#pragma unroll
-                for (int r = 0; r < RB; ++r) po[r * HD + t] = o[r];
-            }
-            if (t < RB) {
-                pm[static_cast<int64_t>(c) * RB + t] = my_m;
-                pl[static_cast<int64_t>(c) * RB + t] = my_l;
-            }
+        if (is_max && !stopped) {  // the epilogues that are left
+            bool ok = true;
+            for (int k = max(0, n - 2); k < n && ok; ++k) ok = epilogue(k);
         }
     }
 

@@ -126,29 +126,46 @@ __global__ void __launch_bounds__(kWtKeys) weights_sum_kernel(const __grid_const
     }
 }
 
-// The same sum from kept scores: rows of a kv-head one after another, 128 keys a block.
-__global__ void __launch_bounds__(kWtKeys) weights_kept_kernel(const __grid_constant__ WeightParams p)
+// The same sum from kept scores.  A block per 32 keys: warp w takes the rows w, w + 8, .. of every kv-head (a key per
+// lane, eight rows in flight), and the warps' sums are added in order.  Bound by the scores' latency and bytes (L2).
+constexpr int kKeptWarps = 8, kKeptRows = 8;
+__global__ void __launch_bounds__(32 * kKeptWarps) weights_kept_kernel(const __grid_constant__ WeightParams p)
 {
+    __shared__ float s_sum[kKeptWarps][32];
     const WeightSeg &sg = p.segs[blockIdx.y];
-    const int key = static_cast<int>(blockIdx.x) * kWtKeys + static_cast<int>(threadIdx.x);
-    if (key >= sg.n_keys) return;
-    const int rows = sg.n_q * p.group;
-    const float *s = p.scores + sg.score0 + key;
+    const int key0 = static_cast<int>(blockIdx.x) * 32;
+    if (key0 >= sg.n_keys) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int per_head = sg.n_q * p.group, rows = per_head * p.hkv;  // row R: kv-head R / per_head
+    const float *s = p.scores + sg.score0 + key0 + lane;
     float sum = 0.f;
-    for (int h = 0; h < p.hkv; ++h) {
-        for (int r = 0; r < rows; ++r, s += sg.score_stride)
-            sum += ex2(*s - p.lse[static_cast<int64_t>(sg.q_row0 + r / p.group) * p.hq + h * p.group + r % p.group]);
+    for (int r0 = warp; r0 < rows; r0 += kKeptWarps * kKeptRows) {
+        float x[kKeptRows], l[kKeptRows];
+#pragma unroll
+        for (int u = 0; u < kKeptRows; ++u) {
+            const int R = r0 + u * kKeptWarps;
+            const int h = R / per_head, r = R - h * per_head;
+            x[u] = R < rows ? s[static_cast<int64_t>(R) * sg.score_stride] : -INFINITY;
+            l[u] = R < rows ? p.lse[static_cast<int64_t>(sg.q_row0 + r / p.group) * p.hq + h * p.group + r % p.group] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < kKeptRows; ++u) sum += ex2(x[u] - l[u]);
     }
-    float *a = p.weights + static_cast<int64_t>(sg.row) * p.weights_stride + key;
-    *a += sum;
+    s_sum[warp][lane] = sum;
+    __syncthreads();
+    if (warp != 0 || key0 + lane >= sg.n_keys) return;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kKeptWarps; ++w) sum += s_sum[w][lane];
+    p.weights[static_cast<int64_t>(sg.row) * p.weights_stride + key0 + lane] += sum;
 }
 
 }  // namespace
 
 cudaError_t launch_weights_kept(const WeightParams &p, int max_keys, cudaStream_t st)
 {
-    const dim3 tiles(static_cast<unsigned>((max_keys + kWtKeys - 1) / kWtKeys), static_cast<unsigned>(p.n));
-    weights_kept_kernel<<<tiles, kWtKeys, 0, st>>>(p);
+    const dim3 blocks(static_cast<unsigned>((max_keys + 31) / 32), static_cast<unsigned>(p.n));
+    weights_kept_kernel<<<blocks, 32 * kKeptWarps, 0, st>>>(p);
     return cudaGetLastError();
 }
 
