@@ -73,26 +73,31 @@ __host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, bool mn_majo
            (static_cast<uint32_t>(M >> 4) << 24);
 }
 
-// wait_bar_warp (dev_common.cuh) that looks at the clock and the abort flag once in kQ8Spins tries: reading the
-// clock takes longer than a try, and these waits are many and short.
+// wait_bar_warp (dev_common.cuh) that looks at the clock and the abort flag once in kQ8Spins tries (reading the clock
+// takes longer than a try), out of line but for its first try: the kernel's code has to stay in the instruction cache.
 constexpr uint32_t kQ8Spins = 64;
-__device__ __forceinline__ bool wait_spin(uint32_t bar, uint32_t parity, const WaitCtx &w)
+__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int *abort, int32_t *status)
 {
-    bool ok = ptx::mbar_try_wait(bar, parity);
+    bool ok = false;
     uint64_t t0 = 0;
     for (uint32_t n = 1; !ok; ++n) {
         ok = ptx::mbar_try_wait(bar, parity);
         if (ok || (n & (kQ8Spins - 1))) continue;
-        if (*w.abort) break;
+        if (*abort) break;
         const uint64_t now = ptx::globaltimer();
         if (n == kQ8Spins) t0 = now;
         if (now - t0 > kWaitNs) {
-            *w.abort = 1;
-            atomicCAS(w.status, 0, kStatusWaitTimeout);
+            *abort = 1;
+            atomicCAS(status, 0, kStatusWaitTimeout);
             break;
         }
     }
     return __all_sync(0xffffffffu, ok);
+}
+__device__ __forceinline__ bool wait_spin(uint32_t bar, uint32_t parity, const WaitCtx &w)
+{
+    if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
+    return wait_slow(bar, parity, w.abort, w.status);
 }
 
 __device__ __forceinline__ void mma_e4m3_warp(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
@@ -151,10 +156,11 @@ struct Q8Cfg {
     // ch_full, ch_empty [ring]; o_item, o_free, stats [2]; desc_full, desc_empty [kQ8Desc]
     static constexpr int kNumBars = 3 * kQ8Stages + 2 * kCT + 8 + 2 * kQ8Ring + 6 + 2 * kQ8Desc;
     static constexpr int kOffMisc = kOffBar + kNumBars * 8;      // tmem slot, abort, K / V tiles issued
-    static constexpr int kStatsFloats = 2 + 2 * RB;              // id, 2^(evm - 8), m[RB], l[RB]
+    static constexpr int kStatsFloats = 8 + 2 * RB;              // id, 2^(evm - 8), Q8Chunk, -, m[RB], l[RB]
     static constexpr int kOffStats = kOffMisc + 16;
-    // per ring entry: id, evm, -, -, 2^eq [16], then (ek, ev) of page slot j of tile k as int8 pairs [k][16]
-    static constexpr int kEntryBytes = 16 + 64 + kQ8MaxChunk * 32;
+    // per ring entry: id, evm, Q8Chunk, -, 2^eq [16], then (ek, ev) of page slot j of tile k as int8 pairs [k][16]
+    static constexpr int kEntryEq = 32, kEntryEx = 96;
+    static constexpr int kEntryBytes = kEntryEx + kQ8MaxChunk * 32;
     static constexpr int kOffEntry = (kOffStats + 2 * kStatsFloats * 4 + 15) / 16 * 16;
     static constexpr int kOffDesc = kOffEntry + kQ8Ring * kEntryBytes;
     static constexpr int kOffSeqs = kOffDesc + kQ8Desc * kQ8DescInts * 4;
@@ -172,7 +178,7 @@ struct Q8Cfg {
 // A chunk: tiles [t0, t1) of an item (sequence si, kv-head, row block).  The item's full chunks have ids first + k
 // stride, k < nfull, and its shorter remainder, if any, id rem.
 struct Q8Chunk {
-    int si, kvh, blk, t0, t1;
+    int32_t si, kvh, blk, t0, t1;
 };
 
 __device__ __forceinline__ int q8_tiles(const Q8Seq &sq) { return (sq.n_keys + kQ8Keys - 1) / kQ8Keys; }
@@ -462,10 +468,13 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
 #pragma unroll
                 for (int u = 0; u < kPer; ++u) {
                     evm = max(evm, static_cast<int>(static_cast<int8_t>(ex[u] >> 8)));
-                    reinterpret_cast<uint16_t *>(en + 80)[32 * u + lane] = static_cast<uint16_t>(ex[u]);
+                    reinterpret_cast<uint16_t *>(en + C::kEntryEx)[32 * u + lane] = static_cast<uint16_t>(ex[u]);
                 }
                 evm = __reduce_max_sync(0xffffffffu, evm);
-                if (lane == 0) reinterpret_cast<int *>(en)[1] = evm;
+                if (lane == 0) {
+                    reinterpret_cast<int *>(en)[1] = evm;
+                    *reinterpret_cast<Q8Chunk *>(en + 8) = ci;
+                }
                 uint8_t *qb = smem + C::kOffQ + (n % R) * C::kQBytes;
                 uint32_t amax[kPasses];
 #pragma unroll
@@ -496,7 +505,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                     *reinterpret_cast<uint2 *>(qb + row_chunk<HD>(r, pc >> 1) + (pc & 1) * 8) = vh;
                     *reinterpret_cast<uint2 *>(qb + (C::kQSum ? C::kQPart + row_chunk<HD>(r, pc >> 1) : row_chunk<HD>(kNQ / 2 + r, pc >> 1)) +
                                                 (pc & 1) * 8) = vl;
-                    if (pc == 0) reinterpret_cast<float *>(en + 16)[r] = pow2i(eq);
+                    if (pc == 0) reinterpret_cast<float *>(en + C::kEntryEq)[r] = pow2i(eq);
                 }
                 ptx::fence_proxy_async_smem();
             }
@@ -532,8 +541,8 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             if (!wait_spin(b_ch_full + 8 * (n % R), (n / R) & 1, wctx)) break;
             const int c = reinterpret_cast<volatile int *>(entry(n))[0];
             if (c < 0) break;
-            const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
-            const int nt = __shfl_sync(0xffffffffu, ci.t1 - ci.t0, 0);
+            const Q8Chunk *ci = reinterpret_cast<const Q8Chunk *>(entry(n) + 8);
+            const int nt = __shfl_sync(0xffffffffu, ci->t1 - ci->t0, 0);
             if (lane == 0) ptx::mbar_arrive(b_ch_empty + 8 * (n % R));
             // the scores, or the O^T, of the chunk before the last have been read
             if (n >= 2 && !wait_spin((is_s ? b_s_free : b_o_free) + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx)) break;
@@ -585,56 +594,52 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         const int slot = t >> p.log_ps;
         float *s_max = s_red + 12 * 16;       // [2][16]
         const int lg = p.log_group;
-        // the output, or the partial, of chunk ordinal n
+        // the output, or the partial, of chunk ordinal n, four rows at a time
         auto epilogue = [&](int n) -> bool {
             if (!wait_spin(b_stats + 8 * (n & 1), (n >> 1) & 1, wctx)) return false;
             const float *st = s_stats + (n & 1) * C::kStatsFloats;
             const int c = __float_as_int(st[0]);
-            const float scale = st[1], my_m = st[2 + t % RB], my_l = st[2 + RB + t % RB];
-            float o[RB], lsum[RB];
-#pragma unroll
-            for (int r = 0; r < RB; ++r) lsum[r] = st[2 + RB + r];
+            const float scale = st[1];
+            const Q8Chunk ci = *reinterpret_cast<const Q8Chunk *>(st + 2);
             if (!wait_spin(b_o_item + 8 * (n & 1), (n >> 1) & 1, wctx)) return false;
             ptx::tc_fence_after();
-            const uint32_t to = tmem + C::kTmemO + C::kNP * (n & 1) + lane_off;
-            ptx::tmem_ld_n<RB>(to + (C::kParts - 1) * RB, o);
-#pragma unroll
-            for (int k = C::kParts - 2; k >= 0; --k) {
-                float part[RB];
-                ptx::tmem_ld_n<RB>(to + k * RB, part);
-                ptx::tmem_wait_ld();
-#pragma unroll
-                for (int r = 0; r < RB; ++r) o[r] = fmaf(o[r], kQ8Unpart, part[r]);
-            }
-            ptx::tc_fence_before();
-            ptx::mbar_arrive(b_o_free + 8 * (n & 1));  // O^T buffer and stats slot may be reused
-            const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
             const Q8Seq &sq = s_seqs[ci.si];
             const int row0 = ci.blk * RB;
             const int n_rows = min(RB, (sq.n_q << lg) - row0);
-            if (q8_tiles(sq) <= sq.ct) {
+            const bool whole = q8_tiles(sq) <= sq.ct;
+            float *po = p.part + static_cast<int64_t>(c) * RB * HD + t;
+#pragma unroll 1
+            for (int r0 = 0; r0 < RB; r0 += 4) {
+                const uint32_t to = tmem + C::kTmemO + C::kNP * (n & 1) + r0 + lane_off;
+                float o[C::kParts][4];
 #pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    if (r >= n_rows) continue;
-                    const int row = row0 + r;
-                    const int64_t at = static_cast<int64_t>(sq.q_row0 + (row >> lg)) * p.hq + (ci.kvh << lg) + (row & ((1 << lg) - 1));
-                    // (a sum that is NaN: the row sees a NaN)
-                    if (t < HD && p.out) p.out[at * HD + t] = __float2bfloat16_rn(o[r] * scale * (lsum[r] > 0.f ? 1.0f / lsum[r] : lsum[r]));
-                    if (p.lse && t == r) p.lse[at] = my_m + log2f(my_l);
+                for (int k = 0; k < C::kParts; ++k) ptx::tmem_ld_n<4>(to + k * RB, o[k]);
+                ptx::tmem_wait_ld();
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int r = r0 + x;
+                    float v = o[C::kParts - 1][x];
+#pragma unroll
+                    for (int k = C::kParts - 2; k >= 0; --k) v = fmaf(v, kQ8Unpart, o[k][x]);
+                    v *= scale;
+                    if (!whole) {
+                        if (t < HD) po[r * HD] = v;
+                    } else if (r < n_rows) {
+                        const int row = row0 + r;
+                        const int64_t at = static_cast<int64_t>(sq.q_row0 + (row >> lg)) * p.hq + (ci.kvh << lg) + (row & ((1 << lg) - 1));
+                        const float l = st[8 + RB + r];  // (NaN: the row sees a NaN)
+                        if (t < HD && p.out) p.out[at * HD + t] = __float2bfloat16_rn(v * (l > 0.f ? 1.0f / l : l));
+                        if (p.lse && t == r) p.lse[at] = st[8 + r] + log2f(l);
+                    }
                 }
-                return true;
             }
-            float *po = p.part + static_cast<int64_t>(c) * RB * HD;
-            float *pm = p.part + static_cast<int64_t>(p.total_chunks) * RB * HD;
-            float *pl = pm + static_cast<int64_t>(p.total_chunks) * RB;
-            if (t < HD) {
-#pragma unroll
-                for (int r = 0; r < RB; ++r) po[r * HD + t] = o[r] * scale;
+            if (!whole && t < RB) {
+                float *pm = p.part + static_cast<int64_t>(p.total_chunks) * RB * HD + static_cast<int64_t>(c) * RB + t;
+                pm[0] = st[8 + t];
+                pm[static_cast<int64_t>(p.total_chunks) * RB] = st[8 + RB + t];
             }
-            if (t < RB) {
-                pm[static_cast<int64_t>(c) * RB + t] = my_m;
-                pl[static_cast<int64_t>(c) * RB + t] = my_l;
-            }
+            ptx::tc_fence_before();
+            ptx::mbar_arrive(b_o_free + 8 * (n & 1));  // O^T buffer and stats slot may be reused
             return true;
         };
         int n = 0;   // chunk ordinal
@@ -643,15 +648,12 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         for (;; ++n) {
             // (a wait that gave up is voted on, here and after a chunk's tiles, so that a group leaves together)
             if (!wait_spin(b_ch_full + 8 * (n % R), (n / R) & 1, wctx)) stopped = true;
-            if (ptx::bar_sync_or(is_max ? kQ8BarMax : kQ8BarWeights, is_max ? 128 : 256, stopped)) {
-                stopped = true;
-                break;
-            }
+            if (ptx::bar_sync_or(is_max ? kQ8BarMax : kQ8BarWeights, is_max ? 128 : 256, stopped)) break;
             const uint8_t *en = entry(n);
             const int c = reinterpret_cast<const volatile int *>(en)[0];
-            if (c < 0) break;
+            if (c < 0 && !is_max) break;
             const int evm = reinterpret_cast<const volatile int *>(en)[1];
-            const Q8Chunk ci = q8_chunk(p, s_seqs, s_rem, c);
+            const Q8Chunk ci = c >= 0 ? *reinterpret_cast<const Q8Chunk *>(en + 8) : Q8Chunk{};
             const Q8Seq &sq = s_seqs[ci.si];
             const int row0 = ci.blk * RB;
             const int qpos0 = sq.n_keys - sq.n_q;
@@ -659,13 +661,13 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             const int masked_from = (qpos0 + (row0 >> lg) + 1) / kQ8Keys;
             float qs[RB];
 #pragma unroll
-            for (int r = 0; r < RB; ++r) qs[r] = reinterpret_cast<const float *>(en + 16)[r];
+            for (int r = 0; r < RB; ++r) qs[r] = reinterpret_cast<const float *>(en + C::kEntryEq)[r];
             // s = scores without their scales, of tile j of the chunk; ks, dv: the key's K scale times scale_log2, and
             // its V scale against the chunk's largest
             float s[RB], ks;
             int dv;
             auto load_scores = [&](int j) -> bool {
-                const char2 ex = reinterpret_cast<const char2 *>(en + 80)[16 * j + slot];
+                const char2 ex = reinterpret_cast<const char2 *>(en + C::kEntryEx)[16 * j + slot];
                 ks = pow2i(static_cast<int8_t>(ex.x)) * p.scale_log2;
                 dv = max(static_cast<int8_t>(ex.y) - evm, -100);
                 const int at = (n & 1) * C::kCT + j;
@@ -687,49 +689,51 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             };
             auto sees = [&](int key, int r) { return key <= qpos0 + ((row0 + r) >> lg); };
             if (is_max) {
-                const int n_rows = min(RB, (sq.n_q << lg) - row0);
-                float *sc = p.scores ? p.scores + sq.score0 + (static_cast<int64_t>(ci.kvh) * (sq.n_q << lg) + row0) * sq.score_stride : nullptr;
-                float m[RB];
+                if (c >= 0) {
+                    const int n_rows = min(RB, (sq.n_q << lg) - row0);
+                    float *sc = p.scores ? p.scores + sq.score0 + (static_cast<int64_t>(ci.kvh) * (sq.n_q << lg) + row0) * sq.score_stride : nullptr;
+                    float m[RB];
 #pragma unroll
-                for (int r = 0; r < RB; ++r) m[r] = -INFINITY;
-                for (int lt = ci.t0; lt < ci.t1; ++lt) {
-                    if (!load_scores(lt - ci.t0)) {
-                        stopped = true;
-                        break;
+                    for (int r = 0; r < RB; ++r) m[r] = -INFINITY;
+                    for (int lt = ci.t0; lt < ci.t1; ++lt) {
+                        if (!load_scores(lt - ci.t0)) {
+                            stopped = true;
+                            break;
+                        }
+                        const int key = lt * kQ8Keys + t;
+                        const float fdv = static_cast<float>(dv);
+                        if (lt >= masked_from) {
+#pragma unroll
+                            for (int r = 0; r < RB; ++r) s[r] = sees(key, r) && key < sq.n_keys ? s[r] * (ks * qs[r]) : -INFINITY;
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < RB; ++r) s[r] *= ks * qs[r];
+                        }
+                        if (sc) {
+#pragma unroll
+                            for (int r = 0; r < RB; ++r)
+                                if (r < n_rows) sc[r * sq.score_stride + key] = s[r];
+                        }
+#pragma unroll
+                        for (int r = 0; r < RB; ++r) m[r] = fmaxf(m[r], s[r] + fdv);  // (a NaN is not taken)
                     }
-                    const int key = lt * kQ8Keys + t;
-                    const float fdv = static_cast<float>(dv);
-                    if (lt >= masked_from) {
-#pragma unroll
-                        for (int r = 0; r < RB; ++r) s[r] = sees(key, r) && key < sq.n_keys ? s[r] * (ks * qs[r]) : -INFINITY;
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < RB; ++r) s[r] *= ks * qs[r];
+                    ptx::tc_fence_before();
+                    if (ptx::bar_sync_or(kQ8BarMax, 128, stopped)) break;
+                    reduce_rows<RB>(m, [](float x, float y) { return fmaxf(x, y); });
+                    if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = m[0];
+                    ptx::bar_sync(kQ8BarMax, 128);
+                    // (the slot's chunk n - 2 has been read: its scores were freed before this chunk's were computed)
+                    if (t < RB) s_max[(n & 1) * 16 + t] = fmaxf(fmaxf(s_red[t], s_red[16 + t]), fmaxf(s_red[32 + t], s_red[48 + t]));
+                    if (warp == 0) {
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(b_m_full + 8 * (n & 1));  // release: the weights read them
                     }
-                    if (sc) {
-#pragma unroll
-                        for (int r = 0; r < RB; ++r)
-                            if (r < n_rows) sc[r * sq.score_stride + key] = s[r];
-                    }
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) m[r] = fmaxf(m[r], s[r] + fdv);  // (a NaN is not taken)
                 }
-                ptx::tc_fence_before();
-                if (ptx::bar_sync_or(kQ8BarMax, 128, stopped)) {
-                    stopped = true;
-                    break;
-                }
-                reduce_rows<RB>(m, [](float x, float y) { return fmaxf(x, y); });
-                if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = m[0];
-                ptx::bar_sync(kQ8BarMax, 128);
-                // (the slot's chunk n - 2 has been read: its scores were freed before this chunk's were computed)
-                if (t < RB) s_max[(n & 1) * 16 + t] = fmaxf(fmaxf(s_red[t], s_red[16 + t]), fmaxf(s_red[32 + t], s_red[48 + t]));
-                if (warp == 0) {
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(b_m_full + 8 * (n & 1));  // release: the weights read them
-                }
-                // the weights of chunk n - 2 are complete (its scores are free), its O^T is or will be soon
-                if (n >= 2) stopped = !epilogue(n - 2);
+                // the weights of chunk n - 2 are complete (its scores are free), its O^T is or will be soon; after the
+                // last chunk, the two that are left
+#pragma unroll 1
+                for (int k = max(0, n - 2); k < (c >= 0 ? n - 1 : n) && !stopped; ++k) stopped = !epilogue(k);
+                if (c < 0) break;
                 continue;
             }
             // ------------------------------------------------ weights
@@ -791,10 +795,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             // ---------------------------------------------------- row statistics for the epilogue
             reduce_rows<RB>(lpart, [](float x, float y) { return x + y; });
             if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = lpart[0];
-            if (ptx::bar_sync_or(kQ8BarWeights, 256, stopped)) {
-                stopped = true;
-                break;
-            }
+            if (ptx::bar_sync_or(kQ8BarWeights, 256, stopped)) break;
             ptx::mbar_arrive(b_s_free + 8 * (n & 1));
             if (warp == 4) {
                 // the stats slot of chunk n - 2 must have been read
@@ -802,23 +803,21 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                 float *st = s_stats + (n & 1) * C::kStatsFloats;
                 if (lane == 31) {
                     st[0] = __int_as_float(c);
-                    st[1] = ldexpf(1.f, evm - 8);  // (subnormal where the chunk's V is)
+                    // 2^(evm - 8), subnormal where the chunk's V is
+                    st[1] = evm - 8 >= -126 ? pow2i(evm - 8) : pow2i(evm + 56) * 0x1p-64f;
+                    *reinterpret_cast<Q8Chunk *>(st + 2) = ci;
                 }
                 if (lane < RB) {
                     float l = 0.f;
 #pragma unroll
                     for (int w = 4; w < 12; ++w) l += s_red[w * 16 + lane];
-                    st[2 + lane] = my_max;
-                    st[2 + RB + lane] = l * (1.f / 256.f);
+                    st[8 + lane] = my_max;
+                    st[8 + RB + lane] = l * (1.f / 256.f);
                 }
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(b_stats + 8 * (n & 1));  // release: the epilogue reads the slot
             }
             ptx::mbar_arrive(b_ch_empty + 8 * (n % R));  // (warp 4 last: s_red is read)
-        }
-        if (is_max && !stopped) {  // the epilogues that are left
-            bool ok = true;
-            for (int k = max(0, n - 2); k < n && ok; ++k) ok = epilogue(k);
         }
     }
 
