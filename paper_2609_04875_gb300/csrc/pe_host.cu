@@ -704,11 +704,12 @@ struct AttnItem {
 // 5 tiles, not 376 of 2: 20.8 -> 17.4 us a layer with its merge); one of many tiles (more than 12 per SM)
 // takes 8, where a chunk's cost is least and the estimates hardly differ (16 agents, 5200 tiles: 67.4 us
 // with 7 or 8, 4.6 % more with 6).  tiles_of(i): sequence i's tiles, items_of(i): its items, each all those tiles;
-// tiles: of all items; longest: the longest chunk, taken from `many` tiles per SM on.
+// tiles: of all items; longest: the longest chunk, taken from `many` tiles per SM on; drain: what the last chunk's tiles
+// cost once more.
 constexpr double kDecChunkCost = 0.35;
 template <typename Tiles, typename Items>
 int64_t chunk_tiles(const pe_cache *c, size_t lo, size_t hi, const Tiles &tiles_of, const Items &items_of, int64_t tiles,
-                    int64_t longest, int64_t many, double chunk_cost)
+                    int64_t longest, int64_t many, double chunk_cost, double drain)
 {
     const int64_t N = c->num_sms;
     if (tiles > many * N) return longest;  // many tiles per SM: the longest chunks
@@ -732,7 +733,7 @@ int64_t chunk_tiles(const pe_cache *c, size_t lo, size_t hi, const Tiles &tiles_
         const double room = static_cast<double>(idle) * U;
         if (R > 0 && (idle == 0 || rem_cost > room))
             t += std::max((rem_cost - room) / static_cast<double>(N), static_cast<double>(rem_max) + chunk_cost - (idle > 0 ? U : 0.0));
-        t += 0.1 * static_cast<double>(ceil_div(cpi, 32));  // the merge's round trips
+        t += 0.1 * static_cast<double>(ceil_div(cpi, 32)) + drain * static_cast<double>(ct);  // the merge's round trips
         if (t < best_t - 1e-9) {
             best_t = t;
             best = ct;
@@ -745,7 +746,7 @@ int64_t decode_chunk_tiles(const pe_cache *c, const std::vector<AttnItem> &items
 {
     return chunk_tiles(
         c, lo, hi, [&](size_t i) { return ceil_div(c->len[items[i].seq], 128); },
-        [&](size_t) { return static_cast<int64_t>(c->cfg.num_kv_heads); }, tiles, 8, 12, kDecChunkCost);
+        [&](size_t) { return static_cast<int64_t>(c->cfg.num_kv_heads); }, tiles, 8, 12, kDecChunkCost, 0.0);
 }
 
 // Decode kernel launches (groups of kMaxSegs sequences).  Key splits: about two
@@ -1709,8 +1710,9 @@ struct Q8Item {
     int32_t row;  // of weights
 };
 
-// A chunk's cost besides its tiles, in tiles (kDecChunkCost).
-constexpr double kQ8ChunkCost = 0.7;
+// A chunk's cost besides its tiles, in tiles (kDecChunkCost), and the drain: V is loaded a chunk behind K.  16 agents:
+// chunks of 14 tiles 37.1 us, of 8 34.9, of 5 35.5; one of 120k keys (8 rows): 14 51.6, 10 49.8, 9 52.9.
+constexpr double kQ8ChunkCost = 0.7, kQ8Drain = 0.3;
 
 // Rows (n_q x group) up to which the codes are attended as they are.  Beyond, a sequence's keys are read once per
 // block of 16 rows, and unpacking them once costs less.
@@ -1739,7 +1741,7 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
     for (size_t i = lo; i < hi; ++i) longest_item = std::max(longest_item, tiles_of(i));
     int64_t ct = c->dec_chunks_per_sm > 0
                      ? std::min<int64_t>(longest, std::max<int64_t>(1, ceil_div(tiles, c->dec_chunks_per_sm * static_cast<int64_t>(c->num_sms))))
-                     : chunk_tiles(c, lo, hi, tiles_of, items_of, tiles, longest, 24, kQ8ChunkCost);
+                     : chunk_tiles(c, lo, hi, tiles_of, items_of, tiles, longest, 64, kQ8ChunkCost, kQ8Drain);
     if (c->splitkv == 1 && c->num_splits > 0) ct = std::min<int64_t>(longest, ceil_div(longest_item, c->num_splits));
     std::memset(static_cast<void *>(&p), 0, offsetof(Q8AttnParams, seqs));
     for (;; ct = longest) {

@@ -13,8 +13,9 @@
 //         up in the same columns, or TMEM would hold chunks of half the length:
 //         exact down to 2^-10 (smaller elements err by at most 2^-18 of the
 //         largest).
-//   p   = 2^-8 (p_hi + 2^-4 p_mid + 2^-8 p_lo): twelve bits of every weight, and
-//         an absolute floor of 2^-26 of the largest.
+//   p   = 2^-8 (p_hi + 2^-4 p_mid + 2^-8 p_lo): the eleven bits of the weight in
+//         fp16, in which the parts are taken two at a time, and an absolute floor
+//         of 2^-26 of the largest.
 // The products are exact and accumulate in fp32 (measured: within 2^-22 of the
 // sum of magnitudes), so what is rounded is the output alone, to bf16.
 //
@@ -120,6 +121,26 @@ __device__ __forceinline__ uint64_t row_desc(uint32_t addr, uint32_t lbo_bytes)
     return HD == 128 ? d : (d & ~(7ull << 61)) | (4ull << 61);
 }
 
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t ra, rb, rd;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(ra) : "f"(a.x), "f"(a.y));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(rb) : "f"(b.x), "f"(b.y));
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(rd) : "l"(ra), "l"(rb));
+    float2 d;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(rd));
+    return d;
+}
+
+__device__ __forceinline__ uint32_t half2_to_e4m3(__half2 w)
+{
+    return __nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(w), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ __half2 e4m3_to_half2(uint32_t codes)
+{
+    return __half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes), __NV_E4M3));
+}
+
 // P^T as the B operand, MN-major without swizzle: 16 columns of a key are 16 bytes, keys 16 bytes apart, groups of 16
 // columns 2 KB apart.  So a thread, which holds one key, stores a key's parts 16 bytes at a time; K-major, a byte for
 // each row and part (48 for 16 rows), a tile's weights took twice as long.
@@ -150,8 +171,8 @@ struct Q8Cfg {
     static constexpr int kOffP = kOffQ + kQ8Ring * kQBytes;
     static constexpr int kPBytes = kNP * 128;
     static constexpr int kCT = q8_max_chunk(RB);                 // tiles of a chunk whose scores TMEM holds, twice
-    static constexpr int kOffRed = kOffP + 2 * kPBytes;          // float [12 warps][16], then the maxima [2][16]
-    static constexpr int kOffBar = kOffRed + (12 + 2) * 16 * 4;
+    static constexpr int kOffRed = kOffP + 2 * kPBytes;          // float [12 warps][16], then the maxima [2][16], 8 - them
+    static constexpr int kOffBar = kOffRed + (12 + 4) * 16 * 4;
     // k_full, v_full, v_empty [stages]; s_full [2][kCT]; s_free, m_full, p_full, drain [2];
     // ch_full, ch_empty [ring]; o_item, o_free, stats [2]; desc_full, desc_empty [kQ8Desc]
     static constexpr int kNumBars = 3 * kQ8Stages + 2 * kCT + 8 + 2 * kQ8Ring + 6 + 2 * kQ8Desc;
@@ -592,7 +613,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         const int grp = (warp >> 2) - 1;      // weights: the tiles of ordinal grp mod 2
         const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;  // the TMEM lanes this warp may access
         const int slot = t >> p.log_ps;
-        float *s_max = s_red + 12 * 16;       // [2][16]
+        float *s_max = s_red + 12 * 16;       // [2][16], then 8 - them: the largest weight is 2^8
         const int lg = p.log_group;
         // the output, or the partial, of chunk ordinal n, four rows at a time
         auto epilogue = [&](int n) -> bool {
@@ -659,9 +680,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             const int qpos0 = sq.n_keys - sq.n_q;
             // tiles from this one on hold keys that the block's first row does not see
             const int masked_from = (qpos0 + (row0 >> lg) + 1) / kQ8Keys;
-            float qs[RB];
-#pragma unroll
-            for (int r = 0; r < RB; ++r) qs[r] = reinterpret_cast<const float *>(en + C::kEntryEq)[r];
+            const float4 *qs = reinterpret_cast<const float4 *>(en + C::kEntryEq);  // four rows' 2^eq
             // s = scores without their scales, of tile j of the chunk; ks, dv: the key's K scale times scale_log2, and
             // its V scale against the chunk's largest
             float s[RB], ks;
@@ -701,13 +720,20 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                             break;
                         }
                         const int key = lt * kQ8Keys + t;
-                        const float fdv = static_cast<float>(dv);
+                        const float2 fdv = make_float2(static_cast<float>(dv), static_cast<float>(dv)), ks2 = make_float2(ks, ks);
+#pragma unroll
+                        for (int r = 0; r < RB; r += 4) {
+                            const float4 q = qs[r / 4];
+                            const float2 x = mul2(make_float2(s[r], s[r + 1]), mul2(ks2, make_float2(q.x, q.y)));
+                            const float2 y = mul2(make_float2(s[r + 2], s[r + 3]), mul2(ks2, make_float2(q.z, q.w)));
+                            s[r] = x.x;
+                            s[r + 1] = x.y;
+                            s[r + 2] = y.x;
+                            s[r + 3] = y.y;
+                        }
                         if (lt >= masked_from) {
 #pragma unroll
-                            for (int r = 0; r < RB; ++r) s[r] = sees(key, r) && key < sq.n_keys ? s[r] * (ks * qs[r]) : -INFINITY;
-                        } else {
-#pragma unroll
-                            for (int r = 0; r < RB; ++r) s[r] *= ks * qs[r];
+                            for (int r = 0; r < RB; ++r) s[r] = sees(key, r) && key < sq.n_keys ? s[r] : -INFINITY;
                         }
                         if (sc) {
 #pragma unroll
@@ -715,7 +741,11 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                                 if (r < n_rows) sc[r * sq.score_stride + key] = s[r];
                         }
 #pragma unroll
-                        for (int r = 0; r < RB; ++r) m[r] = fmaxf(m[r], s[r] + fdv);  // (a NaN is not taken)
+                        for (int r = 0; r < RB; r += 2) {
+                            const float2 y = add2(make_float2(s[r], s[r + 1]), fdv);
+                            m[r] = fmaxf(m[r], y.x);  // (a NaN is not taken)
+                            m[r + 1] = fmaxf(m[r + 1], y.y);
+                        }
                     }
                     ptx::tc_fence_before();
                     if (ptx::bar_sync_or(kQ8BarMax, 128, stopped)) break;
@@ -723,7 +753,11 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                     if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = m[0];
                     ptx::bar_sync(kQ8BarMax, 128);
                     // (the slot's chunk n - 2 has been read: its scores were freed before this chunk's were computed)
-                    if (t < RB) s_max[(n & 1) * 16 + t] = fmaxf(fmaxf(s_red[t], s_red[16 + t]), fmaxf(s_red[32 + t], s_red[48 + t]));
+                    if (t < RB) {
+                        const float x = fmaxf(fmaxf(s_red[t], s_red[16 + t]), fmaxf(s_red[32 + t], s_red[48 + t]));
+                        s_max[(n & 1) * 16 + t] = x;
+                        s_max[(2 + (n & 1)) * 16 + t] = x == -INFINITY ? 0.f : 8.f - x;
+                    }
                     if (warp == 0) {
                         __syncwarp();
                         if (lane == 0) ptx::mbar_arrive(b_m_full + 8 * (n & 1));  // release: the weights read them
@@ -740,28 +774,33 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             stopped = !wait_spin(b_m_full + 8 * (n & 1), (n >> 1) & 1, wctx);
             ptx::tc_fence_after();
             const float my_max = s_max[(n & 1) * 16 + lane % RB];
-            float m8[RB], lpart[RB];  // 8 - m: the largest weight is 2^8
+            const float4 *m8 = reinterpret_cast<const float4 *>(s_max + (2 + (n & 1)) * 16);
+            float2 lpart[RB / 2];
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const float m = s_max[(n & 1) * 16 + r];
-                m8[r] = m == -INFINITY ? 0.f : 8.f - m;
-                lpart[r] = 0.f;
-            }
+            for (int r = 0; r < RB / 2; ++r) lpart[r] = make_float2(0.f, 0.f);
             for (int lt = ci.t0; lt < ci.t1 && !stopped; ++lt, ++i) {
                 if ((i & 1) != grp) continue;
                 (void)load_scores(lt - ci.t0);
                 const int key = lt * kQ8Keys + t;
-                const float fdv = static_cast<float>(dv), unv = pow2i(-dv);
-                float pr[RB];
+                const float2 fdv = make_float2(static_cast<float>(dv), static_cast<float>(dv)), ks2 = make_float2(ks, ks);
+                const float2 unv = make_float2(pow2i(-dv), pow2i(-dv));
 #pragma unroll
-                for (int r = 0; r < RB; ++r) pr[r] = ex2(fmaf(s[r], ks * qs[r], m8[r] + fdv));
+                for (int r = 0; r < RB; r += 4) {
+                    const float4 q = qs[r / 4], m = m8[r / 4];
+                    const float2 x = fma2(make_float2(s[r], s[r + 1]), mul2(ks2, make_float2(q.x, q.y)), add2(make_float2(m.x, m.y), fdv));
+                    const float2 y = fma2(make_float2(s[r + 2], s[r + 3]), mul2(ks2, make_float2(q.z, q.w)), add2(make_float2(m.z, m.w), fdv));
+                    s[r] = ex2(x.x);
+                    s[r + 1] = ex2(x.y);
+                    s[r + 2] = ex2(y.x);
+                    s[r + 3] = ex2(y.y);
+                }
                 if (lt >= masked_from) {
 #pragma unroll
                     for (int r = 0; r < RB; ++r)
-                        if (!(sees(key, r) && key < sq.n_keys)) pr[r] = 0.f;
+                        if (!(sees(key, r) && key < sq.n_keys)) s[r] = 0.f;
                 }
 #pragma unroll
-                for (int r = 0; r < RB; ++r) lpart[r] = fmaf(pr[r], unv, lpart[r]);
+                for (int r = 0; r < RB; r += 2) lpart[r / 2] = fma2(make_float2(s[r], s[r + 1]), unv, lpart[r / 2]);
                 // P^T(i) into buffer i & 1 once O^T += V^T P^T(i - 2) has read it
                 if (i >= 2 && !wait_spin(v_empty((i - 2) % kQ8Stages), ((i - 2) / kQ8Stages) & 1, wctx)) {
                     stopped = true;
@@ -772,16 +811,15 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                 for (int x = C::kParts * RB / 4; x < C::kNP / 4; ++x) pw[x] = 0u;
 #pragma unroll
                 for (int r = 0; r < RB; r += 4) {
-                    float2 w0 = make_float2(pr[r], pr[r + 1]), w1 = make_float2(pr[r + 2], pr[r + 3]);
+                    __half2 w0 = __floats2half2_rn(s[r], s[r + 1]), w1 = __floats2half2_rn(s[r + 2], s[r + 3]);
 #pragma unroll
                     for (int part = 0; part < C::kParts; ++part) {
-                        const uint32_t q0 = __nv_cvt_float2_to_fp8x2(w0, __NV_SATFINITE, __NV_E4M3);
-                        const uint32_t q1 = __nv_cvt_float2_to_fp8x2(w1, __NV_SATFINITE, __NV_E4M3);
+                        const uint32_t q0 = half2_to_e4m3(w0), q1 = half2_to_e4m3(w1);
                         pw[(part * RB + r) / 4] = q0 | q1 << 16;
-                        if (part + 1 < C::kParts) {
-                            const float2 h0 = e4m3x2_to_float2(q0), h1 = e4m3x2_to_float2(q1);
-                            w0 = make_float2((w0.x - h0.x) * 16.f, (w0.y - h0.y) * 16.f);
-                            w1 = make_float2((w1.x - h1.x) * 16.f, (w1.y - h1.y) * 16.f);
+                        if (part + 1 < C::kParts) {  // 16 (w - part), exact
+                            const __half2 up = __float2half2_rn(16.f), down = __float2half2_rn(-16.f);
+                            w0 = __hfma2(e4m3_to_half2(q0), down, __hmul2(w0, up));
+                            w1 = __hfma2(e4m3_to_half2(q1), down, __hmul2(w1, up));
                         }
                     }
                 }
@@ -793,8 +831,14 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                 ptx::mbar_arrive(b_p_full + 8 * grp);
             }
             // ---------------------------------------------------- row statistics for the epilogue
-            reduce_rows<RB>(lpart, [](float x, float y) { return x + y; });
-            if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = lpart[0];
+            float lsum[RB];
+#pragma unroll
+            for (int r = 0; r < RB; r += 2) {
+                lsum[r] = lpart[r / 2].x;
+                lsum[r + 1] = lpart[r / 2].y;
+            }
+            reduce_rows<RB>(lsum, [](float x, float y) { return x + y; });
+            if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = lsum[0];
             if (ptx::bar_sync_or(kQ8BarWeights, 256, stopped)) break;
             ptx::mbar_arrive(b_s_free + 8 * (n & 1));
             if (warp == 4) {

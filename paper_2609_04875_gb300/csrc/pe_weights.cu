@@ -135,6 +135,8 @@ __global__ void __launch_bounds__(32 * kKeptWarps) weights_kept_kernel(const __g
     const WeightSeg &sg = p.segs[blockIdx.y];
     const int key0 = static_cast<int>(blockIdx.x) * 32;
     if (key0 >= sg.n_keys) return;
+    ptx::griddep_wait();  // launched with programmatic serialization
+    ptx::griddep_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per_head = sg.n_q * p.group, rows = per_head * p.hkv;  // row R: kv-head R / per_head
     const float *s = p.scores + sg.score0 + key0 + lane;
@@ -164,9 +166,16 @@ __global__ void __launch_bounds__(32 * kKeptWarps) weights_kept_kernel(const __g
 
 cudaError_t launch_weights_kept(const WeightParams &p, int max_keys, cudaStream_t st)
 {
-    const dim3 blocks(static_cast<unsigned>((max_keys + 31) / 32), static_cast<unsigned>(p.n));
-    weights_kept_kernel<<<blocks, 32 * kKeptWarps, 0, st>>>(p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>((max_keys + 31) / 32), static_cast<unsigned>(p.n));
+    cfg.blockDim = dim3(32 * kKeptWarps);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, weights_kept_kernel, p);
 }
 
 cudaError_t launch_weights(int head_dim, const WeightParams &p, int64_t q_rows, int max_keys, cudaStream_t st)
