@@ -8,6 +8,7 @@ module fails.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import math
 import os
@@ -134,17 +135,30 @@ def _check(rc: int):
 _i32_types, _i64_types = {}, {}  # array types by length (a program's calls use few lengths)
 
 
+_ARRAY_CODES = {ctypes.c_int32: "i", ctypes.c_int64: "q"}
+
+
+def _array_type(n, ctype, types):
+    arr = types.get(n)
+    if arr is None:
+        arr = ctype * n
+        if len(types) < 256:
+            types[n] = arr
+    return arr
+
+
 def _int_array(vals, ctype, types):
     if isinstance(vals, ctypes.Array) and vals._type_ is ctype:
         return vals
     if type(vals) is not list:
         vals = list(vals)
     n = max(1, len(vals))
-    arr = types.get(n)
-    if arr is None:
-        arr = ctype * n
-        if len(types) < 256:
-            types[n] = arr
+    if n >= 8:  # (in one step; what array refuses takes the way below)
+        try:
+            return _array_type(n, ctype, types).from_buffer(array.array(_ARRAY_CODES[ctype], vals))
+        except (TypeError, OverflowError):
+            pass
+    arr = _array_type(n, ctype, types)
     try:
         return arr(*vals)
     except TypeError:  # entries that only int() converts

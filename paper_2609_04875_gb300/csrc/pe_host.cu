@@ -1805,13 +1805,14 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
 }
 
 // Attends the items on the codes, in as few launches as the parameter block and the workspace allow; what does not fit
-// (a single sequence's partials, or one query's scores) goes to `left`.  weights: also adds the softmax weights
-// (out may then be null).
-pe_status run_q8(pe_cache *c, std::vector<Q8Item> items, int32_t layer, const void *Q, int64_t q_rows, void *out, int32_t hq,
+// (a single sequence's partials, or one query's scores) goes to `left`.  lse_rows > 0: also leaves the rows' log-sum-exp
+// (of lse_rows rows of Q) at the workspace's start.  weights: keeps the scores and adds the softmax weights to it.
+// out may be null.
+pe_status run_q8(pe_cache *c, std::vector<Q8Item> items, int32_t layer, const void *Q, int64_t lse_rows, void *out, int32_t hq,
                  float scale, float *weights, int64_t stride, std::vector<Q8Item> *left, cudaStream_t st)
 {
     const int g = hq / c->cfg.num_kv_heads;
-    const int64_t lse = weights ? ceil_div(q_rows * hq, 64) * 64 : 0;  // floats, before the partials
+    const int64_t lse = ceil_div(lse_rows * hq, 64) * 64;  // floats, before the partials
     const int64_t ws = c->ws_bytes / 4 - lse;
     Q8AttnParams p;
     for (size_t lo = 0; lo < items.size();) {
@@ -1824,7 +1825,7 @@ pe_status run_q8(pe_cache *c, std::vector<Q8Item> items, int32_t layer, const vo
                 continue;
             }
             Q8Item &it = items[lo];
-            if (!weights || it.n_q == 1) {
+            if (lse_rows == 0 || it.n_q == 1) {
                 left->push_back(it);
                 hi = lo;
                 break;
@@ -1847,7 +1848,7 @@ pe_status run_q8(pe_cache *c, std::vector<Q8Item> items, int32_t layer, const vo
         p.out = static_cast<__nv_bfloat16 *>(out);
         p.scale_log2 = scale * 1.4426950408889634f;
         p.part = c->d_ws + lse;
-        p.lse = weights ? c->d_ws : nullptr;
+        p.lse = lse_rows > 0 ? c->d_ws : nullptr;
         p.scores = weights ? p.part + scores_at : nullptr;
         c->last_split = p.any_split;
         c->last_splits = static_cast<int32_t>(ceil_div(ceil_div(p.seqs[0].n_keys, 128), p.seqs[0].ct));
@@ -1896,12 +1897,22 @@ pe_status attend(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer,
         else many.push_back(it);
     }
     if (!few.empty()) {
-        if (pe_status s = run_q8(c, std::move(few), layer, Q, q_rows, out, hq, scale, nullptr, 0, &left, st)) return s;
+        if (pe_status s = run_q8(c, std::move(few), layer, Q, 0, out, hq, scale, nullptr, 0, &left, st)) return s;
         for (const Q8Item &it : left) many.push_back(AttnItem{it.seq, it.q_row0, it.n_q});
     }
     if (many.empty()) return PE_OK;
     if (pe_status s = unpack_layer(c, many, layer, st)) return s;
     return run_attention(c, many, 0, Q, q_rows, out, hq, scale, st);
+}
+
+// Whether a launch's block already has a sequence that adds to this row of weights: two pieces of a sequence's queries
+// in one launch would race.
+template <typename Params>
+bool adds_to(const Params &p, int32_t row)
+{
+    for (int i = 0; i < p.n; ++i)
+        if (p.segs[i].row == row) return true;
+    return false;
 }
 
 // Adds the items' softmax weights to `weights` from K in bf16: the bf16 cache's, or the unpacked layer.  The workspace
@@ -1938,8 +1949,9 @@ pe_status add_weights(pe_cache *c, const std::vector<Q8Item> &items, int32_t lay
         return PE_OK;
     };
     for (const Q8Item &it : items) {
-        // (a launch's query rows are consecutive: not so where an item between two was attended otherwise)
-        if (p.n == kMaxSegs || (p.n > 0 && p.segs[p.n - 1].q_row0 + p.segs[p.n - 1].n_q != it.q_row0))
+        // (a launch's query rows are consecutive: not so where an item between two was attended otherwise; and a launch adds
+        // to a row of weights once)
+        if (p.n == kMaxSegs || adds_to(p, it.row) || (p.n > 0 && p.segs[p.n - 1].q_row0 + p.segs[p.n - 1].n_q != it.q_row0))
             if (pe_status s = flush()) return s;
         p.segs[p.n++] = WeightSeg{it.row, it.seq * cf.max_pages_per_seq, it.q_row0, it.n_q, it.n_keys, 0, 0};
         rows += it.n_q;
@@ -1948,34 +1960,115 @@ pe_status add_weights(pe_cache *c, const std::vector<Q8Item> &items, int32_t lay
     return flush();
 }
 
-// Attention and weights of one call.  8-bit cache: sequences of few rows keep their scores as they are attended; the
-// others are attended as ever, then their scores are computed again in pieces that fit the workspace.
+// Adds the items' softmax weights from the codes and their rows' log-sum-exp at the workspace's start (of lse_rows rows
+// of Q); the row groups lie behind.  What does not fit goes to `left`.
+pe_status add_weights_q8(pe_cache *c, std::vector<Q8Item> items, int32_t layer, const void *Q, int64_t lse_rows, int32_t hq, float scale,
+                         float *weights, int64_t stride, std::vector<Q8Item> *left, cudaStream_t st)
+{
+    const pe_cache_config &cf = c->cfg;
+    const int hkv = cf.num_kv_heads, g = hq / hkv;
+    const int64_t lse = ceil_div(lse_rows * hq, 256) * 256;  // floats; the groups need 16-byte alignment
+    const int64_t room = (c->ws_bytes - lse * 4) / q8_row_group_bytes(cf.head_dim);
+    WeightQ8Params p;
+    std::memset(static_cast<void *>(&p), 0, offsetof(WeightQ8Params, segs));
+    p.page_table = c->d_table;
+    p.q = static_cast<const __nv_bfloat16 *>(Q);
+    p.exps = c->exps;
+    p.lse = c->d_ws;
+    p.groups = reinterpret_cast<uint8_t *>(c->d_ws + lse);
+    p.weights = weights;
+    p.weights_stride = stride;
+    p.status = c->d_status;
+    p.hq = hq;
+    p.hkv = hkv;
+    while ((1 << p.log_group) < g) p.log_group++;
+    p.layer = layer;
+    p.num_pages = cf.num_pages;
+    p.ps = cf.page_size;
+    while ((1 << p.log_ps) < p.ps) p.log_ps++;
+    p.oob_row = static_cast<int32_t>(c->code_rows);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    int64_t groups = 0, tiles = 0;
+    auto flush = [&]() -> pe_status {
+        if (p.n == 0) return PE_OK;
+        if (injected_failure(c)) return launch_fault("weights kernels");
+        cudaError_t e = launch_weights_q8(cf.head_dim, c->tm_k8, p, static_cast<int>(groups), static_cast<int>(tiles), st);
+        if (e != cudaSuccess) return cuda_fail(e, "weights kernel launch");
+        c->launches += 2;
+        p.n = 0;
+        groups = tiles = 0;
+        return PE_OK;
+    };
+    for (size_t i = 0; i < items.size(); ++i) {
+        const Q8Item it = items[i];
+        const int64_t n_groups = ceil_div(static_cast<int64_t>(it.n_q) * g, 128);
+        if (n_groups * hkv > room) {
+            if (it.n_q == 1) {
+                left->push_back(it);
+                continue;
+            }
+            Q8Item a = it, b = it;  // the two halves of its queries
+            a.n_q = it.n_q / 2;
+            a.n_keys -= it.n_q - a.n_q;
+            b.q_row0 += a.n_q;
+            b.n_q -= a.n_q;
+            items.push_back(a);
+            items.push_back(b);
+            continue;
+        }
+        if (p.n == kMaxSegs || adds_to(p, it.row) || (groups + n_groups * hkv) > room)
+            if (pe_status s = flush()) return s;
+        p.segs[p.n++] = WeightQ8Seg{it.row, it.seq * cf.max_pages_per_seq, it.q_row0, it.n_q, it.n_keys, static_cast<int32_t>(tiles),
+                                    static_cast<int32_t>(n_groups), static_cast<int32_t>(groups)};
+        groups += n_groups * hkv;
+        tiles += ceil_div(it.n_keys, 128);
+    }
+    return flush();
+}
+
+// Attention and weights of one call.  8-bit cache: sequences of few rows keep their scores as they are attended; of others
+// the scores are computed again, with the log-sum-exp of an attention on the codes (which is also the output's, unless
+// there are so many rows that the unpacked layer's attention is faster).
+constexpr int64_t kQ8KeptRows = 16, kQ8OutRows = 512;
 pe_status attend_with_weights(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer, const void *Q, int64_t q_rows,
                               void *out, int32_t hq, float scale, float *weights, int64_t stride, cudaStream_t st)
 {
     const int g = hq / c->cfg.num_kv_heads;
-    std::vector<Q8Item> few, more, left;
+    const bool codes = c->q8 && c->decode_kernel == 1 && c->splitkv != 0;
+    std::vector<Q8Item> few, some, most, left;
     std::vector<AttnItem> many;
+    std::vector<uint8_t> again(items.size(), 0);
     for (size_t i = 0; i < items.size(); ++i) {
         const AttnItem &it = items[i];
         if (it.n_q <= 0) continue;
-        const bool takes = c->q8 && q8_takes(c, it.n_q, g);
-        (takes ? few : more).push_back(Q8Item{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq]), static_cast<int32_t>(i)});
-        if (!takes) many.push_back(it);
+        const int64_t rows = static_cast<int64_t>(it.n_q) * g;
+        std::vector<Q8Item> &to = codes && rows <= kQ8KeptRows ? few : (codes && rows <= kQ8OutRows ? some : most);
+        to.push_back(Q8Item{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq]), static_cast<int32_t>(i)});
+        if (&to == &most) many.push_back(it);
     }
     pe_status s = PE_OK;
-    if (!few.empty() && (s = run_q8(c, few, layer, Q, q_rows, out, hq, scale, weights, stride, &left, st)) != PE_OK) return s;
-    // (a sequence of which a query's scores do not fit is attended again as a whole)
-    for (size_t i = 0; i < left.size(); ++i)
-        if (i == 0 || left[i].row != left[i - 1].row) many.push_back(items[left[i].row]);
     if (!many.empty() && (s = attend(c, many, layer, Q, q_rows, out, hq, scale, st)) != PE_OK) return s;
-    if (!c->q8) return add_weights(c, more, layer, Q, hq, scale, weights, stride, st);
-    if (!more.empty() && (s = run_q8(c, more, layer, Q, q_rows, nullptr, hq, scale, weights, stride, &left, st)) != PE_OK) return s;
-    if (left.empty()) return PE_OK;
-    std::vector<AttnItem> whole;
-    for (const Q8Item &it : left) whole.push_back(AttnItem{it.seq, it.q_row0, it.n_q});
-    if ((s = unpack_layer(c, whole, layer, st)) != PE_OK) return s;
-    return add_weights(c, left, 0, Q, hq, scale, weights, stride, st);
+    if (!c->q8) return add_weights(c, most, layer, Q, hq, scale, weights, stride, st);
+    if (!few.empty() && (s = run_q8(c, few, layer, Q, q_rows, out, hq, scale, weights, stride, &left, st)) != PE_OK) return s;
+    const size_t n_few = left.size();
+    if (!some.empty() && (s = run_q8(c, some, layer, Q, q_rows, out, hq, scale, nullptr, 0, &left, st)) != PE_OK) return s;
+    if (!most.empty() && (s = run_q8(c, most, layer, Q, q_rows, nullptr, hq, scale, nullptr, 0, &left, st)) != PE_OK) return s;
+    // A sequence of which some query did not fit the workspace is attended again as a whole, and takes the unpacked
+    // layer for its weights (a few of `few`'s queries may have been added: those go by query).
+    for (size_t i = 0; i < left.size(); ++i) again[left[i].row] = 1;
+    some.insert(some.end(), most.begin(), most.end());
+    std::vector<Q8Item> whole(left.begin(), left.begin() + n_few), sums;
+    for (const Q8Item &it : some) (again[it.row] ? whole : sums).push_back(it);
+    if (!sums.empty() && (s = add_weights_q8(c, sums, layer, Q, q_rows, hq, scale, weights, stride, &whole, st)) != PE_OK) return s;
+    if (whole.empty()) return PE_OK;
+    many.clear();
+    for (size_t i = 0; i < items.size(); ++i)
+        if (again[i]) many.push_back(items[i]);
+    if (!many.empty() && (s = attend(c, many, layer, Q, q_rows, out, hq, scale, st)) != PE_OK) return s;
+    many.clear();
+    for (const Q8Item &it : whole) many.push_back(AttnItem{it.seq, it.q_row0, it.n_q});
+    if ((s = unpack_layer(c, many, layer, st)) != PE_OK) return s;
+    return add_weights(c, whole, 0, Q, hq, scale, weights, stride, st);
 }
 
 // The arguments of a batched attention call, as items.
@@ -2701,19 +2794,20 @@ pe_status pe_read_kv_batch(pe_cache *c, int32_t n, const int32_t *seqs, const in
     p.L = c->cfg.num_layers;
     p.hkv = c->cfg.num_kv_heads;
     p.ps = c->cfg.page_size;
+    while ((1 << p.log_ps) < p.ps) p.log_ps++;
     p.d = c->cfg.head_dim;
     p.num_pages = c->cfg.num_pages;
     p.n_total = cu_tokens[n];
     for (int32_t i = 0; i < n;) {
-        for (p.n = p.seg_tokens = 0; i < n && p.n < kMaxSegs; ++i) {
-            const int32_t cnt = cu_tokens[i + 1] - cu_tokens[i];
+        for (p.n = p.pages = 0; i < n && p.n < kMaxSegs; ++i) {
+            const int32_t cnt = cu_tokens[i + 1] - cu_tokens[i], begin = static_cast<int32_t>(begins[i]);
             if (cnt == 0) continue;
-            p.segs[p.n++] = ReadSeg{seqs[i] * c->cfg.max_pages_per_seq, static_cast<int32_t>(begins[i]), p.seg_tokens, cu_tokens[i]};
-            p.seg_tokens += cnt;
+            p.segs[p.n++] = ReadSeg{seqs[i] * c->cfg.max_pages_per_seq, begin, begin + cnt, p.pages, cu_tokens[i]};
+            p.pages += (begin + cnt - 1) / p.ps - begin / p.ps + 1;
         }
         if (p.n == 0) continue;
         if (injected_failure(c)) return launch_fault("read kernel");
-        cudaError_t e = launch_read_kv(c->q8, p, c->num_sms, static_cast<cudaStream_t>(stream));
+        cudaError_t e = launch_read_kv(c->q8, p, static_cast<cudaStream_t>(stream));
         if (e != cudaSuccess) return cuda_fail(e, "read kernel launch");
         c->launches++;
     }
@@ -2809,6 +2903,7 @@ static pe_status evict_batch(pe_cache *c, int32_t n, const int32_t *seqs, const 
     p.L = c->cfg.num_layers;
     p.hkv = c->cfg.num_kv_heads;
     p.ps = ps;
+    while ((1 << p.log_ps) < ps) p.log_ps++;
     p.num_pages = c->cfg.num_pages;
     p.kept_cols = static_cast<int32_t>(kept_stride);
     auto seg_of = [&](const EvictPlan &pl) {
@@ -2834,20 +2929,26 @@ static pe_status evict_batch(pe_cache *c, int32_t n, const int32_t *seqs, const 
     pe_status s = PE_OK;
     for (size_t i = 0; i < plans.size(); i += kMaxSegs) {
         for (p.n = 0; p.n < kMaxSegs && i + p.n < plans.size(); ++p.n) p.segs[p.n] = seg_of(plans[i + p.n]);
-        if ((s = step("evict select", [&] { return launch_evict_select(p, st); })) != PE_OK) return tx.end(s);
+        int32_t max_len = 0;
+        for (int32_t k = 0; k < p.n; ++k) max_len = std::max(max_len, p.segs[k].len);
+        if ((s = step("evict select", [&] { return launch_evict_select(p, max_len, st); })) != PE_OK) return tx.end(s);
     }
     // The copies, and after each group of new pages their table entries: a row moves from a position no lower than its
-    // own, so the entries replaced so far are none that a later group's copies read through.
+    // own, so the entries replaced so far are none that a later group's copies read through.  One group is the rule: it
+    // lists every sequence, and its entries come with the finish.
+    const bool one_group = need <= kAppendMaxPages && plans.size() <= static_cast<size_t>(kMaxSegs);
     p.n = p.n_new = 0;
     auto flush = [&]() -> pe_status {
-        if (p.n_new == 0) return PE_OK;
         pe_status r = step("evict copy", [&] { return launch_evict_copy(c->q8, c->cfg.head_dim, p, st); });
-        if (r == PE_OK) r = step("evict table", [&] { return launch_evict_table(p, st); });
-        p.n = p.n_new = 0;
+        if (r == PE_OK && !one_group) {
+            r = step("evict table", [&] { return launch_evict_table(p, st); });
+            p.n = p.n_new = 0;
+        }
         return r;
     };
     for (size_t i = 0; i < plans.size(); ++i) {
-        for (int32_t done = 0; done < plans[i].n_new;) {
+        int32_t done = 0;
+        while (done < plans[i].n_new || (one_group && done == 0)) {
             if (p.n == kMaxSegs || p.n_new == kAppendMaxPages)
                 if ((s = flush()) != PE_OK) return tx.end(s);
             EvictSeg sg = seg_of(plans[i]);
@@ -2858,9 +2959,15 @@ static pe_status evict_batch(pe_cache *c, int32_t n, const int32_t *seqs, const 
             p.n_new += sg.n_new;
             done += sg.n_new;
             p.segs[p.n++] = sg;
+            if (sg.n_new == 0) break;
         }
     }
-    if ((s = flush()) != PE_OK) return tx.end(s);
+    if (p.n_new > 0 && (s = flush()) != PE_OK) return tx.end(s);
+    if (one_group) {
+        if (p.n > 0 && (s = step("evict finish", [&] { return launch_evict_finish(p, st); })) != PE_OK) return tx.end(s);
+        return tx.end(PE_OK);
+    }
+    p.n_new = 0;
     for (size_t i = 0; i < plans.size(); i += kMaxSegs) {
         for (p.n = 0; p.n < kMaxSegs && i + p.n < plans.size(); ++p.n) p.segs[p.n] = seg_of(plans[i + p.n]);
         if ((s = step("evict finish", [&] { return launch_evict_finish(p, st); })) != PE_OK) return tx.end(s);

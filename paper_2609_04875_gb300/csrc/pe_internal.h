@@ -71,7 +71,7 @@ struct CowParams {
 // ---------------------------------------------------------------- 8-bit cache
 struct UnpackSeg {
     int32_t table_row;     // seq * max_pages_per_seq
-    int32_t page0;         // first block of this sequence (a block per page)
+    int32_t page0;         // prefix of pages inside this launch
 };
 
 // One layer's codes of the listed sequences' pages as bf16, at the same page ids.
@@ -86,8 +86,8 @@ struct UnpackParams {
 
 struct ReadSeg {
     int32_t table_row;
-    int32_t begin;         // first token read
-    int32_t cum0;          // prefix of tokens inside this launch
+    int32_t begin, end;    // tokens read
+    int32_t page0;         // prefix of touched pages inside this launch
     int32_t tok0;          // first row of K / V
 };
 
@@ -96,7 +96,7 @@ struct ReadParams {
     const void *k_pool, *v_pool;
     const int8_t *exps;    // 8-bit cache only
     uint4 *K, *V;          // bf16 [L][n_total][Hkv][d]
-    int32_t n, L, hkv, ps, d, num_pages, n_total, seg_tokens;
+    int32_t n, L, hkv, ps, log_ps, d, num_pages, n_total, pages;
     ReadSeg segs[kMaxSegs];
 };
 
@@ -146,7 +146,8 @@ struct EvictSeg {
     int32_t new0, n_new;   // this launch's new pages of the sequence, in new_pages
 };
 
-struct EvictParams {
+template <int SEGS, int PAGES>
+struct EvictParamsT {
     int32_t *page_table;
     int64_t *seq_len;
     void *k_pool, *v_pool;
@@ -154,10 +155,11 @@ struct EvictParams {
     float *weights;        // [rows][weights_stride]
     int32_t *kept;         // [rows][kept_stride]
     int64_t weights_stride, kept_stride;
-    int32_t n, L, hkv, ps, num_pages, n_new, kept_cols;
-    EvictSeg segs[kMaxSegs];
-    int32_t new_pages[kAppendMaxPages];
+    int32_t n, L, hkv, ps, log_ps, num_pages, n_new, kept_cols;
+    EvictSeg segs[SEGS];
+    int32_t new_pages[PAGES];
 };
+using EvictParams = EvictParamsT<kMaxSegs, kAppendMaxPages>;
 
 // ---------------------------------------------------------------- accumulated weights
 struct WeightSeg {
@@ -321,6 +323,32 @@ struct DecodeParams {
                                 // full_chunks + j hkv .., one per kv-head), blocks longest first
 };
 
+// Weights of many rows from the codes: rows R = query * group + head-in-group of a kv-head in groups of 128.
+__host__ __device__ constexpr int q8_row_group_bytes(int head_dim) { return 2 * 128 * head_dim + 1024; }
+
+struct WeightQ8Seg {
+    int32_t row;           // of weights
+    int32_t table_row;
+    int32_t q_row0, n_q, n_keys;
+    int32_t tile0;         // first tile of 128 keys (a block each)
+    int32_t n_groups;      // groups of 128 rows of a kv-head
+    int32_t group0;        // first group: group0 + kv-head * n_groups + i
+};
+
+struct WeightQ8Params {
+    const int32_t *page_table;
+    const __nv_bfloat16 *q;
+    const int8_t *exps;
+    const float *lse;      // [rows][Hq], log2 units
+    uint8_t *groups;       // workspace, q8_row_group_bytes each
+    float *weights;
+    int64_t weights_stride;
+    int32_t *status;
+    int32_t n, hq, hkv, log_group, layer, num_pages, ps, log_ps, oob_row;
+    float scale_log2;
+    WeightQ8Seg segs[kMaxSegs];
+};
+
 // Records `msg` as this thread's last error (pe_last_error) and returns code.
 int32_t report_error(int32_t code, const char *msg);
 
@@ -350,9 +378,10 @@ cudaError_t launch_decode_attn(int head_dim, int rows_cap, bool tensor_core, con
 // 8-bit cache: p's pools hold codes, p.exps their scales, p.segs[].cum0 and p.seg_tokens count touched pages.
 cudaError_t launch_append_q8(int head_dim, const AppendParams &p, cudaStream_t st);
 cudaError_t launch_unpack_q8(const UnpackParams &p, int pages, cudaStream_t st);
-cudaError_t launch_read_kv(bool q8, const ReadParams &p, int num_sms, cudaStream_t st);
-// Eviction, in this order on one stream; copy and table once for each group of new pages.
-cudaError_t launch_evict_select(const EvictParams &p, cudaStream_t st);
+cudaError_t launch_read_kv(bool q8, const ReadParams &p, cudaStream_t st);
+// Eviction, in this order on one stream: select, then copy for each group of new pages, a table after each but the last,
+// whose pages finish enters.
+cudaError_t launch_evict_select(const EvictParams &p, int max_len, cudaStream_t st);
 cudaError_t launch_evict_copy(bool q8, int head_dim, const EvictParams &p, cudaStream_t st);
 cudaError_t launch_evict_table(const EvictParams &p, cudaStream_t st);
 cudaError_t launch_evict_finish(const EvictParams &p, cudaStream_t st);
@@ -360,6 +389,8 @@ cudaError_t launch_evict_finish(const EvictParams &p, cudaStream_t st);
 cudaError_t launch_weights(int head_dim, const WeightParams &p, int64_t q_rows, int max_keys, cudaStream_t st);
 // The same from scores and lse that launch_attn_q8 left.
 cudaError_t launch_weights_kept(const WeightParams &p, int max_keys, cudaStream_t st);
+cudaError_t launch_weights_q8(int head_dim, const CUtensorMap &tm_k, const WeightQ8Params &p, int groups, int tiles,
+                              cudaStream_t st);
 // rows_cap: 4, 8 or 16 rows a block.  tm_k / tm_v: the codes as 2-D maps {d, L*num_pages*Hkv*ps} with d x ps boxes,
 // swizzled over d bytes.
 cudaError_t launch_attn_q8(int head_dim, int rows_cap, const CUtensorMap &tm_k, const CUtensorMap &tm_v,

@@ -89,7 +89,8 @@ cudaError_t launch_append_t(const cudaLaunchConfig_t &cfg, int head_dim, int nc,
     return cudaLaunchKernelEx(&cfg, append_q8_kernel<Params, 8, 2>, p, threads);
 }
 
-// One block per (sequence, page): the page of one layer is Hkv x ps x d contiguous codes.
+// A page of one layer is Hkv x ps x d contiguous codes: a thread takes 16 of K and of V, a block 256 such chunks of one
+// page (blockIdx.y of them make a page).
 __global__ void __launch_bounds__(256) unpack_q8_kernel(const __grid_constant__ UnpackParams p)
 {
     ptx::griddep_launch_dependents();
@@ -100,65 +101,64 @@ __global__ void __launch_bounds__(256) unpack_q8_kernel(const __grid_constant__ 
         const int mid = (lo + hi + 1) >> 1;
         if (p.segs[mid].page0 <= b) lo = mid; else hi = mid - 1;
     }
+    const int per_head = p.ps * p.d / 16;
+    const int c = static_cast<int>(blockIdx.y) * 256 + static_cast<int>(threadIdx.x);
+    if (c >= p.hkv * per_head) return;
     const int page = p.page_table[p.segs[lo].table_row + (b - p.segs[lo].page0)];
     if (page < 0 || page >= p.num_pages) return;
-    const int per_head = p.ps * p.d / 16;  // 16-code chunks
-    const int64_t src = static_cast<int64_t>(p.layer) * p.num_pages + page;
-    const uint4 *k8 = p.k8 + src * p.hkv * per_head, *v8 = p.v8 + src * p.hkv * per_head;
-    uint4 *k = p.k + static_cast<int64_t>(page) * p.hkv * per_head * 2;
-    uint4 *v = p.v + static_cast<int64_t>(page) * p.hkv * per_head * 2;
-    const int8_t *ex = p.exps + src * p.hkv * 2;
-    for (int c = threadIdx.x; c < p.hkv * per_head; c += 256) {
-        const int h = c / per_head;
-        const float ks = pow2i(ex[2 * h]), vs = pow2i(ex[2 * h + 1]);
-        const uint4 a = k8[c], w = v8[c];
-        k[2 * c] = q8_to_bf16(make_uint2(a.x, a.y), ks);
-        k[2 * c + 1] = q8_to_bf16(make_uint2(a.z, a.w), ks);
-        v[2 * c] = q8_to_bf16(make_uint2(w.x, w.y), vs);
-        v[2 * c + 1] = q8_to_bf16(make_uint2(w.z, w.w), vs);
-    }
+    const int64_t src = (static_cast<int64_t>(p.layer) * p.num_pages + page) * p.hkv, dst = static_cast<int64_t>(page) * p.hkv * per_head + c;
+    const uint4 a = p.k8[src * per_head + c], w = p.v8[src * per_head + c];
+    const char2 e = reinterpret_cast<const char2 *>(p.exps)[src + c / per_head];
+    const float ks = pow2i(static_cast<int8_t>(e.x)), vs = pow2i(static_cast<int8_t>(e.y));
+    p.k[2 * dst] = q8_to_bf16(make_uint2(a.x, a.y), ks);
+    p.k[2 * dst + 1] = q8_to_bf16(make_uint2(a.z, a.w), ks);
+    p.v[2 * dst] = q8_to_bf16(make_uint2(w.x, w.y), vs);
+    p.v[2 * dst + 1] = q8_to_bf16(make_uint2(w.z, w.w), vs);
 }
 
-// A thread moves eight values of K and of V.  Tokens [begin_i, begin_i + n_i) of each sequence, every layer.
+// One block per touched page and layer: its tokens' rows, kv-heads and 16-byte chunks fastest, so that a warp writes
+// contiguous memory and reads whole rows.
 template <bool Q8>
-__global__ void __launch_bounds__(256) read_kv_kernel(const __grid_constant__ ReadParams p, int64_t chunks)
+__global__ void __launch_bounds__(256) read_kv_kernel(const __grid_constant__ ReadParams p)
 {
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    const int cpr = p.d / 8;
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * blockDim.x;
-    for (int64_t c = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; c < chunks; c += stride) {
-        const int col8 = static_cast<int>(c % cpr);
-        int64_t r = c / cpr;
-        const int h = static_cast<int>(r % p.hkv);
-        r /= p.hkv;
-        const int t = static_cast<int>(r % p.seg_tokens);
-        const int64_t l = r / p.seg_tokens;
-        int lo = 0, hi = p.n - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (p.segs[mid].cum0 <= t) lo = mid; else hi = mid - 1;
-        }
-        const ReadSeg &sg = p.segs[lo];
-        const int pos = sg.begin + (t - sg.cum0);
-        const int page = p.page_table[sg.table_row + pos / p.ps];
-        const int64_t head = (l * p.num_pages + page) * p.hkv + h;
-        const int64_t src = (head * p.ps + pos % p.ps) * cpr + col8;
-        uint4 k, v;
-        if (page < 0 || page >= p.num_pages) {
-            k = v = make_uint4(kBf16NanPair, kBf16NanPair, kBf16NanPair, kBf16NanPair);
-        } else if constexpr (Q8) {
-            const uint2 kc = static_cast<const uint2 *>(p.k_pool)[src], vc = static_cast<const uint2 *>(p.v_pool)[src];
-            k = q8_to_bf16(kc, pow2i(p.exps[2 * head]));
-            v = q8_to_bf16(vc, pow2i(p.exps[2 * head + 1]));
-            if (kc.x == kQ8NanWord) v = k;  // a token held as NaN
+    const int pg = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.pages));
+    const int64_t l = blockIdx.x / static_cast<unsigned>(p.pages);
+    int lo = 0, hi = p.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.segs[mid].page0 <= pg) lo = mid; else hi = mid - 1;
+    }
+    const ReadSeg &sg = p.segs[lo];
+    const int lp = (sg.begin >> p.log_ps) + (pg - sg.page0);
+    const int first = max(sg.begin, lp << p.log_ps), rows = min(sg.end, (lp + 1) << p.log_ps) - first;
+    const int page = p.page_table[sg.table_row + lp];
+    if (page < 0 || page >= p.num_pages) return;  // (no valid token lies there)
+    const int cpr = p.d / (Q8 ? 16 : 8);  // 16-byte chunks of a stored row
+    const int64_t head0 = (l * p.num_pages + page) * p.hkv;
+    const int64_t out0 = (l * p.n_total + sg.tok0 + (first - sg.begin)) * p.hkv;
+    const uint4 *kp = static_cast<const uint4 *>(p.k_pool), *vp = static_cast<const uint4 *>(p.v_pool);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < rows * p.hkv * cpr; i += 256) {
+        const int col = i % cpr, r = i / cpr;  // (cpr: a power of two)
+        const int row = r / p.hkv, h = r - row * p.hkv;
+        const int64_t src = (((head0 + h) << p.log_ps) + (first & (p.ps - 1)) + row) * cpr + col;
+        const int64_t dst = (out0 + r) * cpr + col;
+        const uint4 k = kp[src], v = vp[src];
+        if constexpr (Q8) {
+            const char2 e = reinterpret_cast<const char2 *>(p.exps)[head0 + h];
+            const float ks = pow2i(static_cast<int8_t>(e.x)), vs = pow2i(static_cast<int8_t>(e.y));
+            const uint4 k0 = q8_to_bf16(make_uint2(k.x, k.y), ks), k1 = q8_to_bf16(make_uint2(k.z, k.w), ks);
+            const bool nan = k.x == kQ8NanWord;  // a token held as NaN
+            __stcs(p.K + 2 * dst, k0);
+            __stcs(p.K + 2 * dst + 1, k1);
+            __stcs(p.V + 2 * dst, nan ? k0 : q8_to_bf16(make_uint2(v.x, v.y), vs));
+            __stcs(p.V + 2 * dst + 1, nan ? k1 : q8_to_bf16(make_uint2(v.z, v.w), vs));
         } else {
-            k = static_cast<const uint4 *>(p.k_pool)[src];
-            v = static_cast<const uint4 *>(p.v_pool)[src];
+            __stcs(p.K + dst, k);
+            __stcs(p.V + dst, v);
         }
-        const int64_t dst = ((l * p.n_total + sg.tok0 + (t - sg.cum0)) * p.hkv + h) * cpr + col8;
-        __stcs(p.K + dst, k);
-        __stcs(p.V + dst, v);
     }
 }
 
@@ -201,18 +201,19 @@ cudaError_t launch_unpack_q8(const UnpackParams &p, int pages, cudaStream_t st)
 {
     if (pages <= 0) return cudaSuccess;
     cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = serial_config(static_cast<unsigned>(pages), 256, st, &attr);
+    cudaLaunchConfig_t cfg = serial_config(static_cast<unsigned>(pages), 256, st, &attr);
+    cfg.gridDim.y = static_cast<unsigned>((p.hkv * p.ps * p.d / 16 + 255) / 256);
     return cudaLaunchKernelEx(&cfg, unpack_q8_kernel, p);
 }
 
-cudaError_t launch_read_kv(bool q8, const ReadParams &p, int num_sms, cudaStream_t st)
+cudaError_t launch_read_kv(bool q8, const ReadParams &p, cudaStream_t st)
 {
-    const int64_t chunks = static_cast<int64_t>(p.L) * p.seg_tokens * p.hkv * (p.d / 8);
-    if (chunks <= 0) return cudaSuccess;
-    const int64_t blocks = std::min<int64_t>((chunks + 255) / 256, static_cast<int64_t>(num_sms) * 16);
+    const int64_t blocks = static_cast<int64_t>(p.L) * p.pages;
+    if (blocks <= 0) return cudaSuccess;
+    if (blocks > INT32_MAX) return cudaErrorInvalidValue;
     cudaLaunchAttribute attr;
     const cudaLaunchConfig_t cfg = serial_config(static_cast<unsigned>(blocks), 256, st, &attr);
-    return q8 ? cudaLaunchKernelEx(&cfg, read_kv_kernel<true>, p, chunks) : cudaLaunchKernelEx(&cfg, read_kv_kernel<false>, p, chunks);
+    return q8 ? cudaLaunchKernelEx(&cfg, read_kv_kernel<true>, p) : cudaLaunchKernelEx(&cfg, read_kv_kernel<false>, p);
 }
 
 }  // namespace pe

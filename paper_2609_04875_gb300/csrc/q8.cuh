@@ -72,6 +72,30 @@ __device__ __forceinline__ uint2 q8_from_bf16(uint4 v, float s)
                       q8_pair_from_bf16(v.z, s) | (q8_pair_from_bf16(v.w, s) << 16));
 }
 
+// the largest of sixteen codes' magnitudes, as a code
+__device__ __forceinline__ uint32_t codes_absmax(uint4 c)
+{
+    constexpr uint32_t kAbs = 0x7f7f7f7fu;
+    uint32_t m = __vmaxu4(__vmaxu4(c.x & kAbs, c.y & kAbs), __vmaxu4(c.z & kAbs, c.w & kAbs));
+    m = __vmaxu4(m, m >> 16);
+    return max(m & 0xffu, m >> 8 & 0xffu);
+}
+
+// sixteen codes times 2^k, rounded (every one that is not zero stays within 448)
+__device__ __forceinline__ uint4 rescale_codes(uint4 c, int k)
+{
+    const float s = pow2i(max(-100, min(100, k)));
+    uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const float2 a = e4m3x2_to_float2(w[x]), b = e4m3x2_to_float2(w[x] >> 16);
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a.x * s, a.y * s), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(b.x * s, b.y * s), __NV_SATFINITE, __NV_E4M3);
+        w[x] = lo | hi << 16;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // the largest magnitude of eight bf16, as bits; an infinity or NaN gives 0x7f80 or more
 __device__ __forceinline__ uint32_t bf16x8_absmax(uint4 v)
 {
