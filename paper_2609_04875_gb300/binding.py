@@ -262,10 +262,12 @@ class PagedKVCache:
                 raise ValueError("init_free_order must list every page")
             cfg.init_free_order = ctypes.cast(self._order, _I32P)
         self._device = None
-        self._raw_stream = self._cur_dev = self._bf16 = None
+        self._raw_stream = self._cur_dev = self._bf16 = self._torch = None
         if not host_only:
             import torch
+            self._torch = torch  # (looked up once: an import statement costs a call 1 us)
             self._device = torch.cuda.current_device()
+            self._torch_device = torch.device("cuda", self._device)
             self._bf16 = torch.bfloat16
             self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
             self._cur_dev = getattr(torch._C, "_cuda_getDevice", None)
@@ -433,8 +435,7 @@ class PagedKVCache:
             raise ValueError("Q must be [cu_q[-1]][Hq][d]")
         _same_shape(out, Q)
         if out is None:
-            import torch
-            out = torch.empty_like(Q)
+            out = self._torch.empty_like(Q)
         scale = self._default_scale if softmax_scale is None else float(softmax_scale)
         _check(_lib.pe_replay_attn_batch(self._h, len(seqs), _i32_array(seqs), layer, self._ptr(Q, "Q"),
                                          _i32_array(cu_q), self._ptr(out, "out"), shape[1], scale,
@@ -450,8 +451,7 @@ class PagedKVCache:
             raise ValueError("Q must be [cu_q[-1]][Hq][d]")
         _same_shape(out, Q)
         if out is None:
-            import torch
-            out = torch.empty_like(Q)
+            out = self._torch.empty_like(Q)
         scale = self._default_scale if softmax_scale is None else float(softmax_scale)
         ptr, stride = self._weights(weights, seqs)
         _check(_lib.pe_replay_attn_weights_batch(self._h, len(seqs), _i32_array(seqs), layer, self._ptr(Q, "Q"),
@@ -461,23 +461,23 @@ class PagedKVCache:
 
     def _rows(self, t, name, dtype, n):
         """(address, row stride) of a CUDA tensor of n rows with contiguous columns."""
-        import torch
-        if t.dtype is not getattr(torch, dtype):
+        if t.dtype is not dtype:
             raise TypeError(f"{name} must be {dtype}")
-        if not t.is_cuda:
-            raise TypeError(f"{name} must be a CUDA tensor")
         if t.get_device() != self._device:
+            if not t.is_cuda:
+                raise TypeError(f"{name} must be a CUDA tensor")
             raise ValueError(f"{name} is on cuda:{t.get_device()}, the cache on cuda:{self._device}")
-        if t.dim() != 2 or t.shape[0] != n or (t.shape[1] > 1 and t.stride(1) != 1):
+        shape, stride = t.shape, t.stride()
+        if len(shape) != 2 or shape[0] != n or (shape[1] > 1 and stride[1] != 1):
             raise ValueError(f"{name} must be [{n}][columns], columns contiguous")
-        if n > 1 and t.stride(0) < t.shape[1]:
+        if n > 1 and stride[0] < shape[1]:
             raise ValueError(f"{name}: rows overlap")
-        return t.data_ptr(), t.stride(0) if n > 1 else t.shape[1]
+        return t.data_ptr(), stride[0] if n > 1 else shape[1]
 
     def _weights(self, t, seqs):
         """The same for weights: the library checks the sequences' lengths against the row stride, which is the
         number of columns unless the rows are parts of longer ones."""
-        ptr, stride = self._rows(t, "weights", "float32", len(seqs))
+        ptr, stride = self._rows(t, "weights", self._torch.float32, len(seqs))
         if stride != t.shape[1] and max(self.seq_info(s)[0] for s in seqs) > t.shape[1]:
             raise ValueError("weights: a sequence is longer than a row")
         return ptr, stride
@@ -486,14 +486,13 @@ class PagedKVCache:
     def read_kv_batch(self, seqs, begins, cu_tokens, stream=None):
         """(K, V): bf16 [L][cu_tokens[-1]][Hkv][d], rows cu_tokens[i]:cu_tokens[i+1] the values the cache holds for
         seqs[i]'s tokens from begins[i] on."""
-        import torch
         if len(begins) != len(seqs) or len(cu_tokens) != len(seqs) + 1:
             raise ValueError("begins and cu_tokens must match seqs")
         if self.host_only:
             raise ValueError("a host-only cache holds no K and V")
-        K = torch.empty((self.num_layers, cu_tokens[-1], self.num_kv_heads, self.head_dim), dtype=torch.bfloat16,
-                        device=f"cuda:{self._device}")
-        V = torch.empty_like(K)
+        K = self._torch.empty((self.num_layers, cu_tokens[-1], self.num_kv_heads, self.head_dim), dtype=self._bf16,
+                              device=self._torch_device)
+        V = self._torch.empty_like(K)
         _check(_lib.pe_read_kv_batch(self._h, len(seqs), _i32_array(seqs), _i64_array(begins), _i32_array(cu_tokens),
                                      K.data_ptr(), V.data_ptr(), self._s(stream)))
         return K, V
@@ -514,11 +513,11 @@ class PagedKVCache:
             _check(_lib.pe_evict_batch(self._h, len(seqs), _i32_array(seqs), _i32_array(keep), int(sinks), int(recent),
                                        None, 0, None, 0, self._s(stream)))
             return None
-        import torch
+        int32 = self._torch.int32
         w, w_stride = self._weights(weights, seqs)
         if kept is None:
-            kept = torch.empty((len(seqs), max(0, *keep) if len(keep) else 0), dtype=torch.int32, device=weights.device)
-        k, k_stride = self._rows(kept, "kept", "int32", len(seqs))
+            kept = self._torch.empty((len(seqs), max(0, *keep) if len(keep) else 0), dtype=int32, device=self._torch_device)
+        k, k_stride = self._rows(kept, "kept", int32, len(seqs))
         if k_stride != kept.shape[1]:
             raise ValueError("kept must be contiguous")
         _check(_lib.pe_evict_batch(self._h, len(seqs), _i32_array(seqs), _i32_array(keep), int(sinks), int(recent), w,
