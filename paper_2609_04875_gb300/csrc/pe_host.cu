@@ -1746,7 +1746,7 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
     std::memset(static_cast<void *>(&p), 0, offsetof(Q8AttnParams, seqs));
     for (;; ct = longest) {
         int64_t chunks = 0, n_items = 0, score = 0;
-        p.n_seqs = p.n_rem = p.any_split = 0;
+        p.n_seqs = p.n_rem = p.any_split = p.max_chunks = 0;
         for (size_t i = lo; i < hi; ++i) {
             const Q8Item &it = items[i];
             const int64_t nt = tiles_of(i), per = items_of(i);
@@ -1765,6 +1765,7 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
             q.score0 = score;
             if (scores) score += static_cast<int64_t>(hkv) * it.n_q * g * nt * 128;
             if (nt > ct) p.any_split = 1;
+            p.max_chunks = std::max(p.max_chunks, static_cast<int32_t>(ceil_div(nt, ct)));
             chunks += nt / ct * per;
             n_items += per;
             if (nt % ct) {  // insertion by decreasing remainder, stable

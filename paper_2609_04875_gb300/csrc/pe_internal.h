@@ -130,6 +130,7 @@ struct Q8AttnParams {
     int32_t n_seqs, hq, hkv, group, log_group, layer, num_pages, ps, log_ps;
     int32_t oob_row;         // a pool row past the end: boxes there read zeros
     int32_t full_chunks, total_chunks, total_items, total_ctas, any_split, n_rem;
+    int32_t max_chunks;      // of an item
     float scale_log2;        // softmax_scale * log2(e)
     Q8Seq seqs[kMaxSegs];
     int32_t rem_seq[kMaxSegs];  // sequences with remainder chunks, longest remainder first

@@ -89,8 +89,9 @@ cudaError_t launch_append_t(const cudaLaunchConfig_t &cfg, int head_dim, int nc,
     return cudaLaunchKernelEx(&cfg, append_q8_kernel<Params, 8, 2>, p, threads);
 }
 
-// A page of one layer is Hkv x ps x d contiguous codes: a thread takes 16 of K and of V, a block 256 such chunks of one
-// page (blockIdx.y of them make a page).
+// A page of one layer is Hkv x ps x d contiguous codes: a block takes 1024 chunks of eight of K and of V of one page
+// (blockIdx.y), a thread four of each, so that a warp's loads and stores are contiguous.
+constexpr int kUnpackChunks = 4;
 __global__ void __launch_bounds__(256) unpack_q8_kernel(const __grid_constant__ UnpackParams p)
 {
     ptx::griddep_launch_dependents();
@@ -101,23 +102,35 @@ __global__ void __launch_bounds__(256) unpack_q8_kernel(const __grid_constant__ 
         const int mid = (lo + hi + 1) >> 1;
         if (p.segs[mid].page0 <= b) lo = mid; else hi = mid - 1;
     }
-    const int per_head = p.ps * p.d / 16;
-    const int c = static_cast<int>(blockIdx.y) * 256 + static_cast<int>(threadIdx.x);
-    if (c >= p.hkv * per_head) return;
     const int page = p.page_table[p.segs[lo].table_row + (b - p.segs[lo].page0)];
     if (page < 0 || page >= p.num_pages) return;
-    const int64_t src = (static_cast<int64_t>(p.layer) * p.num_pages + page) * p.hkv, dst = static_cast<int64_t>(page) * p.hkv * per_head + c;
-    const uint4 a = p.k8[src * per_head + c], w = p.v8[src * per_head + c];
-    const char2 e = reinterpret_cast<const char2 *>(p.exps)[src + c / per_head];
-    const float ks = pow2i(static_cast<int8_t>(e.x)), vs = pow2i(static_cast<int8_t>(e.y));
-    p.k[2 * dst] = q8_to_bf16(make_uint2(a.x, a.y), ks);
-    p.k[2 * dst + 1] = q8_to_bf16(make_uint2(a.z, a.w), ks);
-    p.v[2 * dst] = q8_to_bf16(make_uint2(w.x, w.y), vs);
-    p.v[2 * dst + 1] = q8_to_bf16(make_uint2(w.z, w.w), vs);
+    const int per_head = p.ps * p.d / 8, n = p.hkv * per_head;
+    const int c0 = static_cast<int>(blockIdx.y) * 256 * kUnpackChunks + static_cast<int>(threadIdx.x);
+    const int64_t src = (static_cast<int64_t>(p.layer) * p.num_pages + page) * p.hkv;
+    const uint2 *k8 = reinterpret_cast<const uint2 *>(p.k8) + src * per_head, *v8 = reinterpret_cast<const uint2 *>(p.v8) + src * per_head;
+    const char2 *ex = reinterpret_cast<const char2 *>(p.exps) + src;
+    uint4 *k = p.k + static_cast<int64_t>(page) * n, *v = p.v + static_cast<int64_t>(page) * n;
+    uint2 a[kUnpackChunks], w[kUnpackChunks];
+    char2 e[kUnpackChunks];
+#pragma unroll
+    for (int u = 0; u < kUnpackChunks; ++u) {
+        const int c = c0 + u * 256;
+        if (c >= n) continue;
+        a[u] = k8[c];
+        w[u] = v8[c];
+        e[u] = ex[c / per_head];
+    }
+#pragma unroll
+    for (int u = 0; u < kUnpackChunks; ++u) {
+        const int c = c0 + u * 256;
+        if (c >= n) continue;
+        k[c] = q8_to_bf16(a[u], pow2i(static_cast<int8_t>(e[u].x)));
+        v[c] = q8_to_bf16(w[u], pow2i(static_cast<int8_t>(e[u].y)));
+    }
 }
 
-// One block per touched page and layer: its tokens' rows, kv-heads and 16-byte chunks fastest, so that a warp writes
-// contiguous memory and reads whole rows.
+// One block per touched page and layer: its tokens' rows, kv-heads and chunks fastest, so that a warp writes contiguous
+// memory and reads whole rows.  (Eight codes a load, and so contiguous 16-byte stores, took 12 % more.)
 template <bool Q8>
 __global__ void __launch_bounds__(256) read_kv_kernel(const __grid_constant__ ReadParams p)
 {
@@ -202,7 +215,7 @@ cudaError_t launch_unpack_q8(const UnpackParams &p, int pages, cudaStream_t st)
     if (pages <= 0) return cudaSuccess;
     cudaLaunchAttribute attr;
     cudaLaunchConfig_t cfg = serial_config(static_cast<unsigned>(pages), 256, st, &attr);
-    cfg.gridDim.y = static_cast<unsigned>((p.hkv * p.ps * p.d / 16 + 255) / 256);
+    cfg.gridDim.y = static_cast<unsigned>((p.hkv * p.ps * p.d / 8 + 256 * kUnpackChunks - 1) / (256 * kUnpackChunks));
     return cudaLaunchKernelEx(&cfg, unpack_q8_kernel, p);
 }
 

@@ -803,13 +803,14 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
 }
 
 // Merge of the items held in several chunks: M = max_k m_k, O = sum_k 2^(m_k - M) O_k / sum_k 2^(m_k - M) l_k, in
-// the item's chunk order.  A block per item and row; its groups of HD / 4 threads take every kGroups-th chunk.
-constexpr int kQ8CombThreads = 128;
-template <int HD, int RB>
-__global__ void __launch_bounds__(kQ8CombThreads) attn_q8_combine_kernel(const __grid_constant__ Q8AttnParams p)
+// the item's chunk order.  A block per item and row; its groups of HD / 4 threads take every kGroups-th chunk, eight of
+// them a round trip to L2.  Items of many chunks take the form with 512 threads: 94 chunks (8 rows on 120k keys) in one
+// round trip, not three.
+template <int HD, int RB, int THREADS>
+__global__ void __launch_bounds__(THREADS) attn_q8_combine_kernel(const __grid_constant__ Q8AttnParams p)
 {
     constexpr int kLanes = HD / 4;
-    constexpr int kGroups = kQ8CombThreads / kLanes;
+    constexpr int kGroups = THREADS / kLanes;
     constexpr int kOB = 8;
     __shared__ float4 s_acc[kGroups][kLanes];
     __shared__ float s_m[kGroups], s_l[kGroups];
@@ -926,9 +927,13 @@ cudaError_t launch_q8_t(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const 
     e = cudaLaunchKernelEx(&cfg, attn_q8_kernel<HD, RB>, tm_k, tm_v, p);
     if (e != cudaSuccess || !p.any_split) return e;
     cfg.gridDim = dim3(static_cast<unsigned>(p.total_items), RB);
-    cfg.blockDim = dim3(kQ8CombThreads);
     cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, attn_q8_combine_kernel<HD, RB>, p);
+    if (p.max_chunks > 8 * 128 / (HD / 4)) {
+        cfg.blockDim = dim3(512);
+        return cudaLaunchKernelEx(&cfg, attn_q8_combine_kernel<HD, RB, 512>, p);
+    }
+    cfg.blockDim = dim3(128);
+    return cudaLaunchKernelEx(&cfg, attn_q8_combine_kernel<HD, RB, 128>, p);
 }
 
 }  // namespace
