@@ -1714,13 +1714,17 @@ struct Q8Item {
 // chunks of 14 tiles 37.1 us, of 8 34.9, of 5 35.5; one of 120k keys (8 rows): 14 51.6, 10 49.8, 9 52.9.
 constexpr double kQ8ChunkCost = 0.7, kQ8Drain = 0.3;
 
-// Rows (n_q x group) up to which the codes are attended as they are.  Beyond, a sequence's keys are read once per
-// block of 16 rows, and unpacking them once costs less.
-constexpr int64_t kQ8MaxRows = 64;
-
-bool q8_takes(const pe_cache *c, int64_t n_q, int g)
+// Whether a sequence's rows (n_q x group a kv-head) are attended on the codes, or by way of the unpacked layer.  On the
+// codes every block of 16 rows goes through the keys again (in L2); unpacking costs once 5 bytes a code and then HBM's
+// time for bf16.  GPU time in us, codes / unpacked, 8 kv-heads, d = 128: 32 rows on 600 keys 11.4 / 10.4, on 4000 14.7 /
+// 15.0 (8 sequences 36.6 / 57.0), on 32k 29.5 / 57.8; 64 rows on 4000 18.8 / 15.3 (8: 58.6 / 59.1), on 32k 46.9 / 58.7
+// (8: 281 / 407); 128 rows on 32k 79.9 / 59.1.  d = 64, half the bytes for the same products: 32 rows on 4000 13.5 / 13.8,
+// on 32k 28.2 / 33.0; 64 rows on 32k 45.6 / 33.8.
+bool q8_takes(const pe_cache *c, const AttnItem &it, int g)
 {
-    return c->decode_kernel == 1 && c->splitkv != 0 && n_q * g <= kQ8MaxRows;
+    if (c->decode_kernel != 1 || c->splitkv == 0) return false;
+    const int64_t rows = static_cast<int64_t>(it.n_q) * g, keys = c->len[it.seq];
+    return rows <= 16 || (rows <= 32 && keys >= 4096) || (rows <= 64 && keys >= 8192 && c->cfg.head_dim == 128);
 }
 
 // One launch over items [lo, hi), at most kMaxSegs: fills p.  ws: floats of workspace for partials and, with `scores`,
@@ -1758,6 +1762,9 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
             q.n_keys = it.n_keys;
             q.n_blocks = static_cast<int32_t>(per / hkv);
             q.ct = static_cast<int32_t>(ct);
+            q.n_full = static_cast<int32_t>(nt / ct);
+            q.blocks_inv = static_cast<uint32_t>(ceil_div(1ll << 32, std::max(q.n_blocks, 2)));
+            q.full_inv = static_cast<uint32_t>(ceil_div(1ll << 32, std::max(q.n_full, 2)));
             q.full0 = static_cast<int32_t>(std::min<int64_t>(chunks, INT32_MAX));
             q.rem0 = -1;
             q.item0 = static_cast<int32_t>(std::min<int64_t>(n_items, INT32_MAX));
@@ -1781,7 +1788,7 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
             chunks += items_of(lo + p.rem_seq[j]);
         }
         const int64_t part = p.any_split ? ceil_div(chunks * rb * (d + 2), 64) * 64 : 0;
-        if (part + score <= ws && chunks <= INT32_MAX / 64 && n_items <= INT32_MAX / 64) {
+        if (part + score <= ws && chunks < (1 << 26) && n_items < (1 << 26)) {
             *scores_at = part;
             p.total_chunks = static_cast<int32_t>(chunks);
             p.total_items = static_cast<int32_t>(n_items);
@@ -1894,7 +1901,7 @@ pe_status attend(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer,
     std::vector<AttnItem> many;
     for (const AttnItem &it : items) {
         if (it.n_q <= 0) continue;
-        if (q8_takes(c, it.n_q, g)) few.push_back(Q8Item{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq]), 0});
+        if (q8_takes(c, it, g)) few.push_back(Q8Item{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq]), 0});
         else many.push_back(it);
     }
     if (!few.empty()) {

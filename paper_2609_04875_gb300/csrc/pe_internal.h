@@ -110,10 +110,13 @@ struct Q8Seq {
     int32_t n_keys;        // the last query sees all of them
     int32_t n_blocks;      // of n_q x group rows
     int32_t ct;            // tiles per full chunk
+    int32_t n_full;        // full chunks
+    uint32_t blocks_inv, full_inv;  // ceil(2^32 / n_blocks), ceil(2^32 / n_full) (for more than one)
     int32_t full0;         // first full chunk id: full0 + (kv-head * nfull + k) * n_blocks + block
     int32_t rem0;          // first remainder chunk id (rem0 + kv-head * n_blocks + block), -1: none
     int32_t item0;         // first item (merge): item0 + kv-head * n_blocks + block
     int32_t score_stride;  // scores: of a row, a multiple of 128
+    int32_t pad_;
     int64_t score0;        // scores: first row (kv-head * n_q x group + row)
 };
 

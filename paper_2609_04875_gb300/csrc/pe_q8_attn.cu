@@ -41,9 +41,9 @@
 // kQ8MaxChunk tiles from a counter, longest first; partials (O, m, l) of items
 // held in several chunks are merged by a second launch.
 //
-// Roles (544 threads): warps 0-3 maxima (thread = key of the tile) and, two chunks
-// behind, the epilogue (thread = d-column), 4-7 and 8-11 weights of every other
-// tile (thread = key), 12 K producer, 13 S^T MMAs, 14 V producer, 15 scheduler
+// Roles (544 threads): warps 0-3 maxima (thread = key of the tile), 4-7 and 8-11
+// weights of every other tile (thread = key) and, a chunk behind, the epilogue of
+// every other chunk (thread = d-column), 12 K producer, 13 S^T MMAs, 14 V producer, 15 scheduler
 // (takes chunk ids, reads page ids and scales, splits the q rows), 16 O^T MMAs.
 // A commit takes its warp 80 cycles and an MMA 45, a probe of a barrier as long:
 // one warp for both products spent 1500 cycles a tile, more than a tile's share
@@ -131,6 +131,14 @@ struct Q8Chunk {
 
 __device__ __forceinline__ int q8_tiles(const Q8Seq &sq) { return (sq.n_keys + kQ8Keys - 1) / kQ8Keys; }
 
+// a / d with inv = ceil(2^32 / d), for a below 2^26: the product is at most one too high (no call of the compiler's
+// division: the kernel's code has to stay in the instruction cache)
+__device__ __forceinline__ int div_by(int a, int d, uint32_t inv)
+{
+    const int q = d == 1 ? a : static_cast<int>(__umulhi(static_cast<uint32_t>(a), inv));
+    return q * d > a ? q - 1 : q;
+}
+
 // seqs, rem: shared-memory copies; rem[j]: (first id, sequence) of the j-th sequence with remainder chunks
 __device__ __forceinline__ Q8Chunk q8_chunk(const Q8AttnParams &p, const Q8Seq *seqs, const int2 *rem, int c)
 {
@@ -143,13 +151,11 @@ __device__ __forceinline__ Q8Chunk q8_chunk(const Q8AttnParams &p, const Q8Seq *
             if (seqs[mid].full0 <= c) lo = mid; else hi = mid;
         }
         const Q8Seq &sq = seqs[lo];
-        const int nfull = q8_tiles(sq) / sq.ct;
-        int off = c - sq.full0;
+        const int off = c - sq.full0, u = div_by(off, sq.n_blocks, sq.blocks_inv);
         ci.si = lo;
-        ci.blk = off % sq.n_blocks;
-        off /= sq.n_blocks;
-        ci.kvh = off / nfull;
-        ci.t0 = (off - ci.kvh * nfull) * sq.ct;
+        ci.blk = off - u * sq.n_blocks;
+        ci.kvh = div_by(u, sq.n_full, sq.full_inv);
+        ci.t0 = (u - ci.kvh * sq.n_full) * sq.ct;
         ci.t1 = ci.t0 + sq.ct;
     } else {
         int hi = p.n_rem;
@@ -160,10 +166,10 @@ __device__ __forceinline__ Q8Chunk q8_chunk(const Q8AttnParams &p, const Q8Seq *
         ci.si = rem[lo].y;
         const Q8Seq &sq = seqs[ci.si];
         const int off = c - rem[lo].x;
-        ci.blk = off % sq.n_blocks;
-        ci.kvh = off / sq.n_blocks;
+        ci.kvh = div_by(off, sq.n_blocks, sq.blocks_inv);
+        ci.blk = off - ci.kvh * sq.n_blocks;
+        ci.t0 = sq.n_full * sq.ct;
         ci.t1 = q8_tiles(sq);
-        ci.t0 = ci.t1 / sq.ct * sq.ct;
     }
     return ci;
 }
@@ -336,8 +342,19 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         constexpr int kPer = kQ8MaxChunk / 2;
         constexpr int kPieces = HD / 8;       // of a q row, eight columns each; lane e: row e / kPieces, piece e % kPieces
         constexpr int kRowsAt = 32 / kPieces;
-        constexpr int kPasses = RB / kRowsAt;
+        constexpr int kPasses = RB / kRowsAt, kAt = kPasses < 4 ? kPasses : 4;  // passes over the rows, at a time
         const int pc = lane % kPieces;
+        auto load_q = [&](const Q8Chunk &ci, int j0, uint4 (&qv)[kAt]) {
+            const Q8Seq &sq = s_seqs[ci.si];
+#pragma unroll
+            for (int j = 0; j < kAt; ++j) {
+                qv[j] = make_uint4(0u, 0u, 0u, 0u);
+                const int row = ci.blk * RB + (j0 + j) * kRowsAt + lane / kPieces;
+                if (row < sq.n_q << lg)
+                    qv[j] = *reinterpret_cast<const uint4 *>(
+                        p.q + (static_cast<int64_t>(sq.q_row0 + (row >> lg)) * p.hq + (ci.kvh << lg) + (row & ((1 << lg) - 1))) * HD + pc * 8);
+            }
+        };
         auto claim = [&](int n) -> int {  // lane 0's is the id of chunk ordinal n (-1: no more)
             int c = -1;
             if (lane == 0) {
@@ -359,22 +376,18 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             }
         };
         // Loads under load take 2000 cycles, so the next chunk's are in flight while this one's are used.
-        int c = __shfl_sync(0xffffffffu, claim(0), 0);
+        int c = 0;  // (round -1 only takes the first)
         Q8Chunk ci{};
         int pg[kPer];
-        if (c >= 0) {
-            ci = q8_chunk(p, s_seqs, s_rem, c);
-            load_pages(ci, pg);
-        }
-        for (int n = 0;; ++n) {
+        for (int n = -1;; ++n) {
             const int d = n % kQ8Desc;
             const int claimed = c >= 0 ? claim(n + 1) : -1;
             if (n >= kQ8Desc && !wait_spin(b_desc_empty + 8 * d, ((n / kQ8Desc) - 1) & 1, wctx)) c = -1;
             int *desc = s_desc + d * kQ8DescInts;
             int ex[kPer];  // (ek, ev)
-            uint4 qv[kPasses];
-            if (c >= 0) {
-                const Q8Seq &sq = s_seqs[ci.si];
+            uint4 qv[kAt];
+            if (n < 0) {
+            } else if (c >= 0) {
 #pragma unroll
                 for (int u = 0; u < kPer; ++u) {
                     const bool ok_page = pg[u] >= 0 && pg[u] < p.num_pages;
@@ -391,14 +404,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
 #pragma unroll
                 for (int u = 0; u < kPer; ++u)
                     ex[u] = pg[u] >= 0 ? reinterpret_cast<const uint16_t *>(p.exps)[pg[u]] : 0x8282;  // -126, -126
-#pragma unroll
-                for (int j = 0; j < kPasses; ++j) {
-                    qv[j] = make_uint4(0u, 0u, 0u, 0u);
-                    const int row = ci.blk * RB + j * kRowsAt + lane / kPieces;
-                    if (row < sq.n_q << lg)
-                        qv[j] = *reinterpret_cast<const uint4 *>(
-                            p.q + (static_cast<int64_t>(sq.q_row0 + (row >> lg)) * p.hq + (ci.kvh << lg) + (row & ((1 << lg) - 1))) * HD + pc * 8);
-                }
+                load_q(ci, 0, qv);
             } else if (lane == 0) {
                 desc[0] = -1;
                 ptx::mbar_arrive(b_desc_full + 8 * d);
@@ -408,6 +414,11 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             if (c_next >= 0) {
                 ci_next = q8_chunk(p, s_seqs, s_rem, c_next);
                 load_pages(ci_next, pg);
+            }
+            if (n < 0) {
+                c = c_next;
+                ci = ci_next;
+                continue;
             }
             if (n >= R && !wait_spin(b_ch_empty + 8 * (n % R), ((n / R) - 1) & 1, wctx)) break;
             uint8_t *en = entry(n);
@@ -424,26 +435,30 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                     *reinterpret_cast<Q8Chunk *>(en + 8) = ci;
                 }
                 uint8_t *qb = smem + C::kOffQ + (n % R) * C::kQBytes;
-                uint32_t amax[kPasses];
+#pragma unroll 1
+                for (int j0 = 0;;) {
+                    uint32_t amax[kAt];
 #pragma unroll
-                for (int j = 0; j < kPasses; ++j) amax[j] = bf16x8_absmax(qv[j]);
+                    for (int j = 0; j < kAt; ++j) amax[j] = bf16x8_absmax(qv[j]);
 #pragma unroll
-                for (int off = kPieces / 2; off >= 1; off >>= 1)
+                    for (int off = kPieces / 2; off >= 1; off >>= 1)
 #pragma unroll
-                    for (int j = 0; j < kPasses; ++j) amax[j] = max(amax[j], __shfl_xor_sync(0xffffffffu, amax[j], off));
+                        for (int j = 0; j < kAt; ++j) amax[j] = max(amax[j], __shfl_xor_sync(0xffffffffu, amax[j], off));
 #pragma unroll
-                for (int j = 0; j < kPasses; ++j) {
-                    const int r = j * kRowsAt + lane / kPieces;
-                    const bool bad = amax[j] >= 0x7f80u;  // an infinity or NaN in the row: the row becomes NaN
-                    const int eq = bad ? 0 : q8_exponent(amax[j]);
-                    const float s = pow2i(-eq);
-                    uint2 vh, vl;
-                    q8_split(qv[j], s, C::kQSum ? 1.f : 16.f, vh, vl);
-                    if (bad) vh = make_uint2(kQ8NanWord, kQ8NanWord);
-                    *reinterpret_cast<uint2 *>(qb + row_chunk<HD>(r, pc >> 1) + (pc & 1) * 8) = vh;
-                    *reinterpret_cast<uint2 *>(qb + (C::kQSum ? C::kQPart + row_chunk<HD>(r, pc >> 1) : row_chunk<HD>(kNQ / 2 + r, pc >> 1)) +
-                                                (pc & 1) * 8) = vl;
-                    if (pc == 0) reinterpret_cast<float *>(en + C::kEntryEq)[r] = pow2i(eq);
+                    for (int j = 0; j < kAt; ++j) {
+                        const int r = (j0 + j) * kRowsAt + lane / kPieces;
+                        const bool bad = amax[j] >= 0x7f80u;  // an infinity or NaN in the row: the row becomes NaN
+                        const int eq = bad ? 0 : q8_exponent(amax[j]);
+                        uint2 vh, vl;
+                        q8_split(qv[j], pow2i(-eq), C::kQSum ? 1.f : 16.f, vh, vl);
+                        if (bad) vh = make_uint2(kQ8NanWord, kQ8NanWord);
+                        *reinterpret_cast<uint2 *>(qb + row_chunk<HD>(r, pc >> 1) + (pc & 1) * 8) = vh;
+                        *reinterpret_cast<uint2 *>(qb + (C::kQSum ? C::kQPart + row_chunk<HD>(r, pc >> 1) : row_chunk<HD>(kNQ / 2 + r, pc >> 1)) +
+                                                   (pc & 1) * 8) = vl;
+                        if (pc == 0) reinterpret_cast<float *>(en + C::kEntryEq)[r] = pow2i(eq);
+                    }
+                    if ((j0 += kAt) >= kPasses) break;
+                    load_q(ci, j0, qv);
                 }
                 ptx::fence_proxy_async_smem();
             }
@@ -493,10 +508,10 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                     const uint64_t kd = k_desc + s * (C::kTile >> 4);
                     const uint64_t qd = q_desc + (n % R) * (C::kQBytes >> 4);
 #pragma unroll
-                    for (int kk = 0; kk < (C::kQSum ? 2 : 1) * (HD / 32); ++kk) {
-                        const int col = kk % (HD / 32) * 32, part = kk / (HD / 32);
-                        mma_e4m3_warp(tm + kNQ * at, kd + (col >> 4), qd + ((part * C::kQPart + col) >> 4), kIdS, kk > 0 ? 1u : 0u);
-                    }
+                    for (int part = 0; part < (C::kQSum ? 2 : 1); ++part)
+#pragma unroll
+                        for (int col = 0; col < HD; col += 32)
+                            mma_e4m3_warp(tm + kNQ * at, kd + (col >> 4), qd + ((part * C::kQPart + col) >> 4), kIdS, part + col > 0 ? 1u : 0u);
                     mma_commit_warp(b_s_full + 8 * at);
                 } else {
                     // (the weights are written once the scores are complete, so P^T(i) stands for S^T(i) too)
@@ -524,7 +539,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
         }
         __syncwarp();
     } else {
-        // ============================================================ maxima and epilogue (warps 0-3), weights (4-11)
+        // ============================================================ maxima (warps 0-3), weights and epilogue (4-11)
         const bool is_max = warp < 4;
         const int t = threadIdx.x & 127;      // key of the tile, or d-column
         const int grp = (warp >> 2) - 1;      // weights: the tiles of ordinal grp mod 2
@@ -544,7 +559,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             const Q8Seq &sq = s_seqs[ci.si];
             const int row0 = ci.blk * RB;
             const int n_rows = min(RB, (sq.n_q << lg) - row0);
-            const bool whole = q8_tiles(sq) <= sq.ct;
+            const bool whole = sq.n_full + (sq.rem0 >= 0 ? 1 : 0) == 1;
             float *po = p.part + static_cast<int64_t>(c) * RB * HD + t;
 #pragma unroll 1
             for (int r0 = 0; r0 < RB; r0 += 4) {
@@ -566,8 +581,8 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
                         const int row = row0 + r;
                         const int64_t at = static_cast<int64_t>(sq.q_row0 + (row >> lg)) * p.hq + (ci.kvh << lg) + (row & ((1 << lg) - 1));
                         const float l = st[8 + RB + r];  // (NaN: the row sees a NaN)
-                        if (t < HD && p.out) p.out[at * HD + t] = __float2bfloat16_rn(v * (l > 0.f ? 1.0f / l : l));
-                        if (p.lse && t == r) p.lse[at] = st[8 + r] + log2f(l);
+                        if (t < HD && p.out) p.out[at * HD + t] = __float2bfloat16_rn(v * (l > 0.f ? __fdividef(1.0f, l) : l));
+                        if (p.lse && t == r) p.lse[at] = st[8 + r] + __log2f(l);
                     }
                 }
             }
@@ -589,7 +604,7 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             if (ptx::bar_sync_or(is_max ? kQ8BarMax : kQ8BarWeights, is_max ? 128 : 256, stopped)) break;
             const uint8_t *en = entry(n);
             const int c = reinterpret_cast<const volatile int *>(en)[0];
-            if (c < 0 && !is_max) break;
+            if (c < 0 && is_max) break;
             const int evm = reinterpret_cast<const volatile int *>(en)[1];
             const Q8Chunk ci = c >= 0 ? *reinterpret_cast<const Q8Chunk *>(en + 8) : Q8Chunk{};
             const Q8Seq &sq = s_seqs[ci.si];
@@ -625,160 +640,158 @@ __global__ void __launch_bounds__(kQ8Threads, 1)
             };
             auto sees = [&](int key, int r) { return key <= qpos0 + ((row0 + r) >> lg); };
             if (is_max) {
-                if (c >= 0) {
-                    const int n_rows = min(RB, (sq.n_q << lg) - row0);
-                    float *sc = p.scores ? p.scores + sq.score0 + (static_cast<int64_t>(ci.kvh) * (sq.n_q << lg) + row0) * sq.score_stride : nullptr;
-                    float m[RB];
+                const int n_rows = min(RB, (sq.n_q << lg) - row0);
+                float *sc = p.scores ? p.scores + sq.score0 + (static_cast<int64_t>(ci.kvh) * (sq.n_q << lg) + row0) * sq.score_stride : nullptr;
+                float m[RB];
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) m[r] = -INFINITY;
-                    for (int lt = ci.t0; lt < ci.t1; ++lt) {
-                        if (!load_scores(lt - ci.t0)) {
-                            stopped = true;
-                            break;
-                        }
-                        const int key = lt * kQ8Keys + t;
-                        const float2 fdv = make_float2(static_cast<float>(dv), static_cast<float>(dv)), ks2 = make_float2(ks, ks);
-#pragma unroll
-                        for (int r = 0; r < RB; r += 4) {
-                            const float4 q = qs[r / 4];
-                            const float2 x = mul2(make_float2(s[r], s[r + 1]), mul2(ks2, make_float2(q.x, q.y)));
-                            const float2 y = mul2(make_float2(s[r + 2], s[r + 3]), mul2(ks2, make_float2(q.z, q.w)));
-                            s[r] = x.x;
-                            s[r + 1] = x.y;
-                            s[r + 2] = y.x;
-                            s[r + 3] = y.y;
-                        }
-                        if (lt >= masked_from) {
-#pragma unroll
-                            for (int r = 0; r < RB; ++r) s[r] = sees(key, r) && key < sq.n_keys ? s[r] : -INFINITY;
-                        }
-                        if (sc) {
-#pragma unroll
-                            for (int r = 0; r < RB; ++r)
-                                if (r < n_rows) sc[r * sq.score_stride + key] = s[r];
-                        }
-#pragma unroll
-                        for (int r = 0; r < RB; r += 2) {
-                            const float2 y = add2(make_float2(s[r], s[r + 1]), fdv);
-                            m[r] = fmaxf(m[r], y.x);  // (a NaN is not taken)
-                            m[r + 1] = fmaxf(m[r + 1], y.y);
-                        }
+                for (int r = 0; r < RB; ++r) m[r] = -INFINITY;
+                for (int lt = ci.t0; lt < ci.t1; ++lt) {
+                    if (!load_scores(lt - ci.t0)) {
+                        stopped = true;
+                        break;
                     }
-                    ptx::tc_fence_before();
-                    if (ptx::bar_sync_or(kQ8BarMax, 128, stopped)) break;
-                    reduce_rows<RB>(m, [](float x, float y) { return fmaxf(x, y); });
-                    if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = m[0];
-                    ptx::bar_sync(kQ8BarMax, 128);
-                    // (the slot's chunk n - 2 has been read: its scores were freed before this chunk's were computed)
-                    if (t < RB) {
-                        const float x = fmaxf(fmaxf(s_red[t], s_red[16 + t]), fmaxf(s_red[32 + t], s_red[48 + t]));
-                        s_max[(n & 1) * 16 + t] = x;
-                        s_max[(2 + (n & 1)) * 16 + t] = x == -INFINITY ? 0.f : 8.f - x;
+                    const int key = lt * kQ8Keys + t;
+                    const float2 fdv = make_float2(static_cast<float>(dv), static_cast<float>(dv)), ks2 = make_float2(ks, ks);
+#pragma unroll
+                    for (int r = 0; r < RB; r += 4) {
+                        const float4 q = qs[r / 4];
+                        const float2 x = mul2(make_float2(s[r], s[r + 1]), mul2(ks2, make_float2(q.x, q.y)));
+                        const float2 y = mul2(make_float2(s[r + 2], s[r + 3]), mul2(ks2, make_float2(q.z, q.w)));
+                        s[r] = x.x;
+                        s[r + 1] = x.y;
+                        s[r + 2] = y.x;
+                        s[r + 3] = y.y;
                     }
-                    if (warp == 0) {
-                        __syncwarp();
-                        if (lane == 0) ptx::mbar_arrive(b_m_full + 8 * (n & 1));  // release: the weights read them
+                    if (lt >= masked_from) {
+#pragma unroll
+                        for (int r = 0; r < RB; ++r) s[r] = sees(key, r) && key < sq.n_keys ? s[r] : -INFINITY;
+                    }
+                    if (sc) {
+#pragma unroll
+                        for (int r = 0; r < RB; ++r)
+                            if (r < n_rows) sc[r * sq.score_stride + key] = s[r];
+                    }
+#pragma unroll
+                    for (int r = 0; r < RB; r += 2) {
+                        const float2 y = add2(make_float2(s[r], s[r + 1]), fdv);
+                        m[r] = fmaxf(m[r], y.x);  // (a NaN is not taken)
+                        m[r + 1] = fmaxf(m[r + 1], y.y);
                     }
                 }
-                // the weights of chunk n - 2 are complete (its scores are free), its O^T is or will be soon; after the
-                // last chunk, the two that are left
-#pragma unroll 1
-                for (int k = max(0, n - 2); k < (c >= 0 ? n - 1 : n) && !stopped; ++k) stopped = !epilogue(k);
-                if (c < 0) break;
+                ptx::tc_fence_before();
+                if (ptx::bar_sync_or(kQ8BarMax, 128, stopped)) break;
+                reduce_rows<RB>(m, [](float x, float y) { return fmaxf(x, y); });
+                if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = m[0];
+                ptx::bar_sync(kQ8BarMax, 128);
+                // (the slot's chunk n - 2 has been read: its scores were freed before this chunk's were computed)
+                if (t < RB) {
+                    const float x = fmaxf(fmaxf(s_red[t], s_red[16 + t]), fmaxf(s_red[32 + t], s_red[48 + t]));
+                    s_max[(n & 1) * 16 + t] = x;
+                    s_max[(2 + (n & 1)) * 16 + t] = x == -INFINITY ? 0.f : 8.f - x;
+                }
+                if (warp == 0) {
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(b_m_full + 8 * (n & 1));  // release: the weights read them
+                }
                 continue;
             }
             // ------------------------------------------------ weights
-            stopped = !wait_spin(b_m_full + 8 * (n & 1), (n >> 1) & 1, wctx);
-            ptx::tc_fence_after();
-            const float my_max = s_max[(n & 1) * 16 + lane % RB];
-            const float4 *m8 = reinterpret_cast<const float4 *>(s_max + (2 + (n & 1)) * 16);
-            float2 lpart[RB / 2];
+            if (c >= 0) {
+                stopped = !wait_spin(b_m_full + 8 * (n & 1), (n >> 1) & 1, wctx);
+                ptx::tc_fence_after();
+                const float my_max = s_max[(n & 1) * 16 + lane % RB];
+                const float4 *m8 = reinterpret_cast<const float4 *>(s_max + (2 + (n & 1)) * 16);
+                float2 lpart[RB / 2];
 #pragma unroll
-            for (int r = 0; r < RB / 2; ++r) lpart[r] = make_float2(0.f, 0.f);
-            for (int lt = ci.t0; lt < ci.t1 && !stopped; ++lt, ++i) {
-                if ((i & 1) != grp) continue;
-                (void)load_scores(lt - ci.t0);
-                const int key = lt * kQ8Keys + t;
-                const float2 fdv = make_float2(static_cast<float>(dv), static_cast<float>(dv)), ks2 = make_float2(ks, ks);
-                const float2 unv = make_float2(pow2i(-dv), pow2i(-dv));
+                for (int r = 0; r < RB / 2; ++r) lpart[r] = make_float2(0.f, 0.f);
+                for (int lt = ci.t0; lt < ci.t1 && !stopped; ++lt, ++i) {
+                    if ((i & 1) != grp) continue;
+                    (void)load_scores(lt - ci.t0);
+                    const int key = lt * kQ8Keys + t;
+                    const float2 fdv = make_float2(static_cast<float>(dv), static_cast<float>(dv)), ks2 = make_float2(ks, ks);
+                    const float2 unv = make_float2(pow2i(-dv), pow2i(-dv));
 #pragma unroll
-                for (int r = 0; r < RB; r += 4) {
-                    const float4 q = qs[r / 4], m = m8[r / 4];
-                    const float2 x = fma2(make_float2(s[r], s[r + 1]), mul2(ks2, make_float2(q.x, q.y)), add2(make_float2(m.x, m.y), fdv));
-                    const float2 y = fma2(make_float2(s[r + 2], s[r + 3]), mul2(ks2, make_float2(q.z, q.w)), add2(make_float2(m.z, m.w), fdv));
-                    s[r] = ex2(x.x);
-                    s[r + 1] = ex2(x.y);
-                    s[r + 2] = ex2(y.x);
-                    s[r + 3] = ex2(y.y);
-                }
-                if (lt >= masked_from) {
+                    for (int r = 0; r < RB; r += 4) {
+                        const float4 q = qs[r / 4], m = m8[r / 4];
+                        const float2 x = fma2(make_float2(s[r], s[r + 1]), mul2(ks2, make_float2(q.x, q.y)), add2(make_float2(m.x, m.y), fdv));
+                        const float2 y = fma2(make_float2(s[r + 2], s[r + 3]), mul2(ks2, make_float2(q.z, q.w)), add2(make_float2(m.z, m.w), fdv));
+                        s[r] = ex2(x.x);
+                        s[r + 1] = ex2(x.y);
+                        s[r + 2] = ex2(y.x);
+                        s[r + 3] = ex2(y.y);
+                    }
+                    if (lt >= masked_from) {
 #pragma unroll
-                    for (int r = 0; r < RB; ++r)
-                        if (!(sees(key, r) && key < sq.n_keys)) s[r] = 0.f;
-                }
+                        for (int r = 0; r < RB; ++r)
+                            if (!(sees(key, r) && key < sq.n_keys)) s[r] = 0.f;
+                    }
 #pragma unroll
-                for (int r = 0; r < RB; r += 2) lpart[r / 2] = fma2(make_float2(s[r], s[r + 1]), unv, lpart[r / 2]);
-                // P^T(i) into buffer i & 1 once O^T += V^T P^T(i - 2) has read it
-                if (i >= 2 && !wait_spin(v_empty((i - 2) % kQ8Stages), ((i - 2) / kQ8Stages) & 1, wctx)) {
-                    stopped = true;
-                    break;
-                }
-                uint32_t pw[C::kNP / 4];  // column part * RB + r of O^T, a byte each
+                    for (int r = 0; r < RB; r += 2) lpart[r / 2] = fma2(make_float2(s[r], s[r + 1]), unv, lpart[r / 2]);
+                    // P^T(i) into buffer i & 1 once O^T += V^T P^T(i - 2) has read it
+                    if (i >= 2 && !wait_spin(v_empty((i - 2) % kQ8Stages), ((i - 2) / kQ8Stages) & 1, wctx)) {
+                        stopped = true;
+                        break;
+                    }
+                    uint32_t pw[C::kNP / 4];  // column part * RB + r of O^T, a byte each
 #pragma unroll
-                for (int x = C::kParts * RB / 4; x < C::kNP / 4; ++x) pw[x] = 0u;
+                    for (int x = C::kParts * RB / 4; x < C::kNP / 4; ++x) pw[x] = 0u;
 #pragma unroll
-                for (int r = 0; r < RB; r += 4) {
-                    __half2 w0 = __floats2half2_rn(s[r], s[r + 1]), w1 = __floats2half2_rn(s[r + 2], s[r + 3]);
+                    for (int r = 0; r < RB; r += 4) {
+                        __half2 w0 = __floats2half2_rn(s[r], s[r + 1]), w1 = __floats2half2_rn(s[r + 2], s[r + 3]);
 #pragma unroll
-                    for (int part = 0; part < C::kParts; ++part) {
-                        const uint32_t q0 = half2_to_e4m3(w0), q1 = half2_to_e4m3(w1);
-                        pw[(part * RB + r) / 4] = q0 | q1 << 16;
-                        if (part + 1 < C::kParts) {  // 16 (w - part), exact
-                            const __half2 up = __float2half2_rn(16.f), down = __float2half2_rn(-16.f);
-                            w0 = __hfma2(e4m3_to_half2(q0), down, __hmul2(w0, up));
-                            w1 = __hfma2(e4m3_to_half2(q1), down, __hmul2(w1, up));
+                        for (int part = 0; part < C::kParts; ++part) {
+                            const uint32_t q0 = half2_to_e4m3(w0), q1 = half2_to_e4m3(w1);
+                            pw[(part * RB + r) / 4] = q0 | q1 << 16;
+                            if (part + 1 < C::kParts) {  // 16 (w - part), exact
+                                const __half2 up = __float2half2_rn(16.f), down = __float2half2_rn(-16.f);
+                                w0 = __hfma2(e4m3_to_half2(q0), down, __hmul2(w0, up));
+                                w1 = __hfma2(e4m3_to_half2(q1), down, __hmul2(w1, up));
+                            }
                         }
                     }
-                }
-                uint4 *pt = reinterpret_cast<uint4 *>(smem + C::kOffP + grp * C::kPBytes) + t;
+                    uint4 *pt = reinterpret_cast<uint4 *>(smem + C::kOffP + grp * C::kPBytes) + t;
 #pragma unroll
-                for (int x = 0; x < C::kNP / 16; ++x) pt[x * 128] = make_uint4(pw[4 * x], pw[4 * x + 1], pw[4 * x + 2], pw[4 * x + 3]);
-                ptx::fence_proxy_async_smem();
-                ptx::tc_fence_before();
-                ptx::mbar_arrive(b_p_full + 8 * grp);
-            }
-            // ---------------------------------------------------- row statistics for the epilogue
-            float lsum[RB];
-#pragma unroll
-            for (int r = 0; r < RB; r += 2) {
-                lsum[r] = lpart[r / 2].x;
-                lsum[r + 1] = lpart[r / 2].y;
-            }
-            reduce_rows<RB>(lsum, [](float x, float y) { return x + y; });
-            if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = lsum[0];
-            if (ptx::bar_sync_or(kQ8BarWeights, 256, stopped)) break;
-            ptx::mbar_arrive(b_s_free + 8 * (n & 1));
-            if (warp == 4) {
-                // the stats slot of chunk n - 2 must have been read
-                if (n >= 2) (void)wait_spin(b_o_free + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx);
-                float *st = s_stats + (n & 1) * C::kStatsFloats;
-                if (lane == 31) {
-                    st[0] = __int_as_float(c);
-                    // 2^(evm - 8), subnormal where the chunk's V is
-                    st[1] = evm - 8 >= -126 ? pow2i(evm - 8) : pow2i(evm + 56) * 0x1p-64f;
-                    *reinterpret_cast<Q8Chunk *>(st + 2) = ci;
+                    for (int x = 0; x < C::kNP / 16; ++x) pt[x * 128] = make_uint4(pw[4 * x], pw[4 * x + 1], pw[4 * x + 2], pw[4 * x + 3]);
+                    ptx::fence_proxy_async_smem();
+                    ptx::tc_fence_before();
+                    ptx::mbar_arrive(b_p_full + 8 * grp);
                 }
-                if (lane < RB) {
-                    float l = 0.f;
+                // ---------------------------------------------------- row statistics for the epilogue
+                float lsum[RB];
 #pragma unroll
-                    for (int w = 4; w < 12; ++w) l += s_red[w * 16 + lane];
-                    st[8 + lane] = my_max;
-                    st[8 + RB + lane] = l * (1.f / 256.f);
+                for (int r = 0; r < RB; r += 2) {
+                    lsum[r] = lpart[r / 2].x;
+                    lsum[r + 1] = lpart[r / 2].y;
                 }
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(b_stats + 8 * (n & 1));  // release: the epilogue reads the slot
+                reduce_rows<RB>(lsum, [](float x, float y) { return x + y; });
+                if (lane % (32 / RB) == 0) s_red[warp * 16 + reduced_row<RB>()] = lsum[0];
+                if (ptx::bar_sync_or(kQ8BarWeights, 256, stopped)) break;
+                ptx::mbar_arrive(b_s_free + 8 * (n & 1));
+                if (warp == 4) {
+                    // the stats slot of chunk n - 2 must have been read
+                    if (n >= 2) (void)wait_spin(b_o_free + 8 * (n & 1), ((n - 2) >> 1) & 1, wctx);
+                    float *st = s_stats + (n & 1) * C::kStatsFloats;
+                    if (lane == 31) {
+                        st[0] = __int_as_float(c);
+                        // 2^(evm - 8), subnormal where the chunk's V is
+                        st[1] = evm - 8 >= -126 ? pow2i(evm - 8) : pow2i(evm + 56) * 0x1p-64f;
+                        *reinterpret_cast<Q8Chunk *>(st + 2) = ci;
+                    }
+                    if (lane < RB) {
+                        float l = 0.f;
+#pragma unroll
+                        for (int w = 4; w < 12; ++w) l += s_red[w * 16 + lane];
+                        st[8 + lane] = my_max;
+                        st[8 + RB + lane] = l * (1.f / 256.f);
+                    }
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(b_stats + 8 * (n & 1));  // release: the epilogue reads the slot
+                }
+                ptx::mbar_arrive(b_ch_empty + 8 * (n % R));  // (warp 4 last: s_red is read)
             }
-            ptx::mbar_arrive(b_ch_empty + 8 * (n % R));  // (warp 4 last: s_red is read)
+            // the chunk before, whose O^T is complete by now (or, after the last chunk, will be soon), by the two groups in turn
+            if (n >= 1 && ((n - 1) & 1) == grp) stopped = !epilogue(n - 1);
+            if (c < 0) break;
         }
     }
 
@@ -822,8 +835,7 @@ __global__ void __launch_bounds__(THREADS) attn_q8_combine_kernel(const __grid_c
     }
     const Q8Seq &sq = p.seqs[lo];
     const int blk = (item - sq.item0) % sq.n_blocks, kvh = (item - sq.item0) / sq.n_blocks;
-    const int nt = q8_tiles(sq), nfull = nt / sq.ct;
-    const int cpi = nfull + (nt % sq.ct ? 1 : 0);
+    const int nfull = sq.n_full, cpi = nfull + (sq.rem0 >= 0 ? 1 : 0);
     const int first = sq.full0 + kvh * nfull * sq.n_blocks + blk;
     const int rem = sq.rem0 + kvh * sq.n_blocks + blk;
     const int row = blk * RB + r;
@@ -904,7 +916,7 @@ __global__ void __launch_bounds__(THREADS) attn_q8_combine_kernel(const __grid_c
     const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : NAN);
     const int64_t at = static_cast<int64_t>(sq.q_row0 + row / p.group) * p.hq + kvh * p.group + row % p.group;
     if (p.out) reinterpret_cast<uint2 *>(p.out + at * HD)[t] = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-    if (p.lse && t == 0) p.lse[at] = M + log2f(l);
+    if (p.lse && t == 0) p.lse[at] = M + __log2f(l);
 }
 
 template <int HD, int RB>

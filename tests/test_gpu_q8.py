@@ -270,6 +270,7 @@ def test_long_sessions_and_many_sequences():
     b.append([long_], [20011], spread=0.5)
     run_attention(b, [long_], [1], 8)
     run_attention(b, [long_], [3], 16)
+    run_attention(b, [long_], [8], 16)
     many = [b.new() for _ in range(70)]
     b.append(many, [1 + (i * 37) % 200 for i in range(70)])
     run_attention(b, many, [1] * 70, 4)
