@@ -56,15 +56,16 @@ __global__ void __launch_bounds__(kQ8Block) append_q8_kernel(const __grid_consta
     uint8_t *kp = reinterpret_cast<uint8_t *>(p.k_pool) + head * p.ps * HD;
     uint8_t *vp = reinterpret_cast<uint8_t *>(p.v_pool) + head * p.ps * HD;
     int8_t *ex = p.exps + head * 2;
-    float kes = 0.f, ves = 0.f;
+    int ke0 = 0, ve0 = 0;
     if (on && old > 0) {
-        kes = pow2i(ex[0]);
-        ves = pow2i(ex[1]);
+        ke0 = ex[0];
+        ve0 = ex[1];
     }
+    const float kes = pow2i(ke0), ves = pow2i(ve0);
     const int64_t src0 = ((l * p.n_total + sg.tok0 + (pos0 - sg.len0)) * p.hkv + h) * CPR;  // of the page's row 0
     if (threads <= 32) __syncwarp();
     else __syncthreads();  // the old exponents are read before they are written
-    q8_write_page<CPR, NC>(on, threadIdx.x % threads, threads, rows, kp, vp, ex, s_max,
+    q8_write_page<CPR, NC>(on, threadIdx.x % threads, threads, rows, old, ke0, ve0, kp, vp, ex, s_max,
                            [&](int row, int col8, uint4 &k, uint4 &v) {
                                if (row < old) {
                                    k = q8_to_bf16(*reinterpret_cast<const uint2 *>(kp + row * HD + col8 * 8), kes);

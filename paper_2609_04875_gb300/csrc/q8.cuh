@@ -115,11 +115,12 @@ __host__ __device__ constexpr int q8_unit_chunks(int page_elems) { return page_e
 constexpr int kQ8Block = 256;
 
 // Quantises one page of one kv-head.  Thread t of `threads` holds chunks c = i * threads + t (row c / CPR, eight
-// columns from 8 (c % CPR)): rows [0, n_rows) are valid; load(row, col8, k, v) gives their bf16 values.  Every
+// columns from 8 (c % CPR)): rows [0, n_rows) are valid; load(row, col8, k, v) gives their bf16 values.  Rows below
+// `old` are the page's own, held with exponents (ke0, ve0): where an exponent stays, so do their codes.  Every
 // thread of the block calls this (pages wider than a warp meet at the block's barrier), `on` or not.
 template <int CPR, int NC, typename Load>
-__device__ __forceinline__ void q8_write_page(bool on, int t, int threads, int n_rows, uint8_t *k_dst, uint8_t *v_dst,
-                                              int8_t *exps, uint32_t *s_max, const Load &load)
+__device__ __forceinline__ void q8_write_page(bool on, int t, int threads, int n_rows, int old, int ke0, int ve0,
+                                              uint8_t *k_dst, uint8_t *v_dst, int8_t *exps, uint32_t *s_max, const Load &load)
 {
     uint4 k[NC], v[NC];
     uint32_t bad = 0, km = 0, vm = 0;
@@ -168,8 +169,8 @@ __device__ __forceinline__ void q8_write_page(bool on, int t, int threads, int n
             kc = make_uint2(kQ8NanWord, kQ8NanWord);
             vc = make_uint2(0u, 0u);
         }
-        reinterpret_cast<uint2 *>(k_dst)[c] = kc;
-        reinterpret_cast<uint2 *>(v_dst)[c] = vc;
+        if (c / CPR >= old || ke != ke0) reinterpret_cast<uint2 *>(k_dst)[c] = kc;
+        if (c / CPR >= old || ve != ve0) reinterpret_cast<uint2 *>(v_dst)[c] = vc;
     }
     if (t == 0) *reinterpret_cast<char2 *>(exps) = make_char2(static_cast<char>(ke), static_cast<char>(ve));
 }

@@ -513,6 +513,27 @@ def test_a_failed_eviction_changes_nothing():
     evict(b, [s, t], [40, 50], w0.cpu().numpy(), sinks=1, recent=2)
 
 
+def test_offsets_past_32_bits():
+    """Pages at the end of pools of 4.5 GB of codes: append, read-back, attention on the codes and unpacked, weights,
+    eviction, copy-on-write."""
+    import paper_2609_04875_gb300 as pe
+    pages = 34000
+    b = Both(1, 8, 128, 128, pages=8, max_pages=16)
+    b.cache = pe.PagedKVCache(1, 8, 128, 128, pages, 8, 16, init_free_order=list(range(pages))[::-1], kv_bits=8)
+    s = b.new()
+    b.append([s], [300])
+    assert min(b.cache.page_table(s)) * 8 * 128 * 128 > 2 ** 32
+    for n in (1, 5, 140):
+        run_attention(b, [s], [n], 16)
+    f = b.fork(s)
+    b.append([f], [9])
+    evict(b, [f], [200], b.g.exponential(size=(1, 309)).astype(np.float32), sinks=3)
+    for q in (s, f):
+        k, v = b.cache.read_kv(q)
+        np.testing.assert_array_equal(to64(k), b.seqs[q].K)
+        np.testing.assert_array_equal(to64(v), b.seqs[q].V)
+
+
 # ---------------------------------------------------------------- refusals
 def refused(kind, call, *args, **kw):
     from paper_2609_04875_gb300 import binding
