@@ -1711,20 +1711,30 @@ struct Q8Item {
 };
 
 // A chunk's cost besides its tiles, in tiles (kDecChunkCost), and the drain: V is loaded a chunk behind K.  16 agents:
-// chunks of 14 tiles 37.1 us, of 8 34.9, of 5 35.5; one of 120k keys (8 rows): 14 51.6, 10 49.8, 9 52.9.
+// chunks of 14 tiles 37.1 us, of 8 34.9, of 5 35.5; one of 120k keys (8 rows): 14 51.6, 10 49.8, 9 52.9.  Blocks of more
+// than 16 rows have no drain to speak of: one of 32k keys (64 rows) in chunks of 14 26.3, of 7 34.7.
 constexpr double kQ8ChunkCost = 0.7, kQ8Drain = 0.3;
 
+// Rows of a block: up to 16 with keys on the M side, more with rows there.
+int q8_block(int64_t rows)
+{
+    int rb = 4;
+    while (rb < 128 && rb < rows) rb *= 2;
+    return rb;
+}
+
 // Whether a sequence's rows (n_q x group a kv-head) are attended on the codes, or by way of the unpacked layer.  On the
-// codes every block of 16 rows goes through the keys again (in L2); unpacking costs once 5 bytes a code and then HBM's
-// time for bf16.  GPU time in us, codes / unpacked, 8 kv-heads, d = 128: 32 rows on 600 keys 11.4 / 10.4, on 4000 14.7 /
-// 15.0 (8 sequences 36.6 / 57.0), on 32k 29.5 / 57.8; 64 rows on 4000 18.8 / 15.3 (8: 58.6 / 59.1), on 32k 46.9 / 58.7
-// (8: 281 / 407); 128 rows on 32k 79.9 / 59.1.  d = 64, half the bytes for the same products: 32 rows on 4000 13.5 / 13.8,
-// on 32k 28.2 / 33.0; 64 rows on 32k 45.6 / 33.8.
+// codes every block of up to 128 rows goes through the keys again (in L2); unpacking costs once 5 bytes a code and then
+// HBM's time for bf16.  GPU time in us, codes / unpacked, 8 kv-heads, d = 128: 32 rows on 600 keys 9.4 / 9.9, on 32k 26.6 /
+// 59.0; 64 rows on 600 11.4 / 10.3, on 2000 12.3 / 11.7, on 4000 13.6 / 14.8 (8 sequences 40.3 / 58.6), on 32k 34.2 / 59.5
+// (8: 148 / 416); 128 rows on 4000 17.3 / 15.0, on 8192 20.5 / 18.8 (8: 81 / 119), on 32k 52.0 / 60.4 (8: 220 / 421); 256
+// on 32k 83 / 66.  d = 64, half the bytes for the same scores: 32 rows on 600 8.2 / 9.6, 64 on 4000 11.1 / 13.5, 128 on 8192
+// 17.3 / 16.4, on 32k 33.6 / 33.9.
 bool q8_takes(const pe_cache *c, const AttnItem &it, int g)
 {
     if (c->decode_kernel != 1 || c->splitkv == 0) return false;
     const int64_t rows = static_cast<int64_t>(it.n_q) * g, keys = c->len[it.seq];
-    return rows <= 16 || (rows <= 32 && keys >= 4096) || (rows <= 64 && keys >= 8192 && c->cfg.head_dim == 128);
+    return rows <= 32 || (rows <= 64 && keys >= 2048) || (rows <= 128 && keys >= 8192 && c->cfg.head_dim == 128);
 }
 
 // One launch over items [lo, hi), at most kMaxSegs: fills p.  ws: floats of workspace for partials and, with `scores`,
@@ -1736,7 +1746,7 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
     const int hkv = cf.num_kv_heads, d = cf.head_dim;
     int64_t max_rows = 1, tiles = 0;
     for (size_t i = lo; i < hi; ++i) max_rows = std::max<int64_t>(max_rows, static_cast<int64_t>(items[i].n_q) * g);
-    rb = max_rows <= 4 ? 4 : (max_rows <= 8 ? 8 : 16);
+    rb = q8_block(max_rows);
     auto tiles_of = [&](size_t i) { return ceil_div(items[i].n_keys, 128); };
     auto items_of = [&](size_t i) { return ceil_div(static_cast<int64_t>(items[i].n_q) * g, rb) * hkv; };
     for (size_t i = lo; i < hi; ++i) tiles += tiles_of(i) * items_of(i);
@@ -1745,7 +1755,7 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
     for (size_t i = lo; i < hi; ++i) longest_item = std::max(longest_item, tiles_of(i));
     int64_t ct = c->dec_chunks_per_sm > 0
                      ? std::min<int64_t>(longest, std::max<int64_t>(1, ceil_div(tiles, c->dec_chunks_per_sm * static_cast<int64_t>(c->num_sms))))
-                     : chunk_tiles(c, lo, hi, tiles_of, items_of, tiles, longest, 64, kQ8ChunkCost, kQ8Drain);
+                     : chunk_tiles(c, lo, hi, tiles_of, items_of, tiles, longest, 64, kQ8ChunkCost, rb <= 16 ? kQ8Drain : 0.0);
     if (c->splitkv == 1 && c->num_splits > 0) ct = std::min<int64_t>(longest, ceil_div(longest_item, c->num_splits));
     std::memset(static_cast<void *>(&p), 0, offsetof(Q8AttnParams, seqs));
     for (;; ct = longest) {
@@ -1822,9 +1832,12 @@ pe_status run_q8(pe_cache *c, std::vector<Q8Item> items, int32_t layer, const vo
     const int g = hq / c->cfg.num_kv_heads;
     const int64_t lse = ceil_div(lse_rows * hq, 64) * 64;  // floats, before the partials
     const int64_t ws = c->ws_bytes / 4 - lse;
+    auto narrow = [&](const Q8Item &it) { return static_cast<int64_t>(it.n_q) * g <= 16; };  // (launches of one kernel)
+    std::stable_partition(items.begin(), items.end(), narrow);
     Q8AttnParams p;
     for (size_t lo = 0; lo < items.size();) {
-        size_t hi = std::min(items.size(), lo + kMaxSegs);
+        size_t hi = lo + 1;
+        while (hi < items.size() && hi - lo < kMaxSegs && narrow(items[hi]) == narrow(items[lo])) ++hi;
         int rb = 0;
         int64_t scores_at = 0;
         while (!plan_q8(c, items, lo, hi, g, weights != nullptr, ws, p, rb, &scores_at)) {
@@ -1862,7 +1875,7 @@ pe_status run_q8(pe_cache *c, std::vector<Q8Item> items, int32_t layer, const vo
         c->last_splits = static_cast<int32_t>(ceil_div(ceil_div(p.seqs[0].n_keys, 128), p.seqs[0].ct));
         c->last_ctas = p.total_ctas;
         if (injected_failure(c)) return launch_fault("8-bit attention");
-        cudaError_t e = launch_attn_q8(c->cfg.head_dim, rb, c->tm_k8, c->tm_v8, p, st);
+        cudaError_t e = (rb <= 16 ? launch_attn_q8 : launch_attn_q8_rows)(c->cfg.head_dim, rb, c->tm_k8, c->tm_v8, p, st);
         if (e != cudaSuccess) return cuda_fail(e, "8-bit attention launch");
         c->launches += p.any_split ? 2 : 1;
         c->ends_in_merge = false;

@@ -100,9 +100,9 @@ struct ReadParams {
     ReadSeg segs[kMaxSegs];
 };
 
-// Attention of few rows on the codes (pe_q8_attn.cu): items are (sequence, kv-head, block of query rows).
+// Attention of few rows on the codes (pe_q8_attn.cu, pe_q8_rows.cu): items are (sequence, kv-head, block of query rows).
 constexpr int kQ8MaxChunk = 14;        // key tiles (128 keys) of a chunk, and with blocks of rb rows:
-__host__ __device__ constexpr int q8_max_chunk(int rb) { return rb <= 8 ? 14 : 12; }
+__host__ __device__ constexpr int q8_max_chunk(int rb) { return rb == 16 ? 12 : 14; }
 
 struct Q8Seq {
     int32_t table_row;     // seq * max_pages_per_seq
@@ -399,6 +399,8 @@ cudaError_t launch_weights_q8(int head_dim, const CUtensorMap &tm_k, const Weigh
 // swizzled over d bytes.
 cudaError_t launch_attn_q8(int head_dim, int rows_cap, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
                            const Q8AttnParams &p, cudaStream_t st);
+cudaError_t launch_attn_q8_rows(int head_dim, int rows_cap, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
+                                const Q8AttnParams &p, cudaStream_t st);
 cudaError_t launch_bounded_wait_selftest(int32_t *status, uint64_t limit_ns, cudaStream_t st);
 
 // Raises `kernel`'s dynamic shared-memory limit to `bytes` on the current

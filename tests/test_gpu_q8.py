@@ -359,6 +359,63 @@ def test_nan_tokens_reach_only_the_rows_that_see_them():
     run_attention(b, [f], [1], 8)
 
 
+@pytest.mark.parametrize("hq,hkv,n,d,ps", [(4, 2, 9, 128, 16), (8, 2, 13, 64, 8), (32, 1, 1, 128, 64), (16, 1, 4, 64, 128), (1, 1, 50, 128, 8),
+                                           (8, 1, 16, 128, 32), (2, 1, 64, 128, 128), (16, 2, 9, 128, 16)])
+def test_blocks_of_many_rows(hq, hkv, n, d, ps):
+    """Blocks of 32, 64 and 128 rows, whole and not, with tiles that only some rows see; one launch also of few rows."""
+    b = Both(1, hkv, d, ps, pages=26000 // ps + 20)
+    lens = [8192 + n // 2, 2049, 12000, 1793, 130]
+    seqs = [b.new() for _ in lens]
+    b.append(seqs, lens, spread=0.5)
+    run_attention(b, seqs, [n, n, n, 1, n], hq)
+
+
+@pytest.mark.parametrize("rows", [32, 64, 128])
+@pytest.mark.parametrize("d", [64, 128])
+def test_references_that_move_row_by_row(rows, d):
+    """Scores that rise for some rows and fall for others, in steps below and above the slack of a block's references; a
+    few tokens that outweigh all others, in different tiles for different rows."""
+    b = Both(1, 1, d, 16, pages=540)
+    s = b.new()
+    n, g = 8300, 16
+    k, v = b.draw(n, 0.0) * 0.1, b.draw(n, 0.0)
+    k[0, :, 0, 0] = np.linspace(-80, 80, n)
+    k[0, ::37, 0, 1] = 40 * b.g.standard_normal(len(range(0, n, 37)))
+    b.append([s], [n], k, v)
+    q = b.g.standard_normal((rows // g, g, d)).astype(np.float32) * 0.1
+    q[..., 0] = np.linspace(-1.5, 1.5, rows).reshape(rows // g, g)
+    q[..., 1] = np.where(np.arange(rows).reshape(rows // g, g) % 3 == 0, 3.0, 0.0)
+    q, q64 = bf16(q)
+    out = b.cache.replay_attn(s, 0, q, softmax_scale=1.0)
+    assert b.cache.device_status() == 0
+    assert_attention(out, b.seqs[s], q64, 1.0)
+
+
+def test_many_rows_with_nan_tokens_and_scales_apart():
+    """NaN tokens reach the rows that see them; V scales 2^30 apart; a row of q that is infinite or NaN stays alone."""
+    b = Both(1, 2, 128, 16, pages=540)
+    s = b.new()
+    n = 8300
+    k, v = b.draw(n, 0.3), b.draw(n, 0.3)
+    v[0, 4000:4016] *= 2.0 ** 30
+    k[0, 4000:4016] *= -4.0
+    k[0, n - 9, 0, 5] = np.nan
+    v[0, n - 20, 1, 0] = np.inf
+    b.append([s], [n], k, v)
+    q, q64 = bf16(b.g.standard_normal((31, 4, 128)).astype(np.float32))
+    q[3, 1, 7] = float("inf")
+    q[4, 2, 0] = float("nan")
+    q64[3, 1], q64[4, 2] = np.nan, np.nan
+    out = b.cache.replay_attn(s, 0, q)
+    assert b.cache.device_status() == 0
+    ref, w, size = q8_model.attend(b.seqs[s].K[0], b.seqs[s].V[0], q64, 1 / math.sqrt(128))
+    got = to64(out)
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    bound = 1.05 * (2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + score_error(np.nan_to_num(b.seqs[s].K[0]), np.nan_to_num(q64), 1 / math.sqrt(128))) * size
+                    + n * 2.0 ** -24 * np.abs(np.nan_to_num(b.seqs[s].V[0])).max())
+    assert (np.nan_to_num(np.abs(got - ref) / bound) <= 1).all()
+
+
 def test_stale_and_freed_slots_are_never_seen():
     b = Both(1, 2, 64, 16)
     b.cache.set_option("debug_poison", 1)
