@@ -220,24 +220,24 @@ __global__ void __launch_bounds__(256) weights_rows_kernel(const __grid_constant
     uint8_t *dst = p.groups + static_cast<int64_t>(grp) * C::kGroup;
     float *coef = reinterpret_cast<float *>(dst + 2 * C::kPart);
     constexpr int kPieces = HD / 8;
-    for (int e = threadIdx.x; e < kWqRows * kPieces; e += 256) {  // (whole warps: rows do not straddle them)
-        const int r = e / kPieces, pc = e % kPieces, row = row0 + r;
-        const int64_t at = static_cast<int64_t>(sg.q_row0 + (row >> p.log_group)) * p.hq + (kvh << p.log_group) + (row & ((1 << p.log_group) - 1));
-        const uint4 v = row < rows ? *reinterpret_cast<const uint4 *>(p.q + at * HD + pc * 8) : make_uint4(0u, 0u, 0u, 0u);
-        uint32_t a = bf16x8_absmax(v);
+    // a piece of eight columns a thread (rows do not straddle warps)
+    const int e = static_cast<int>(blockIdx.y) * 256 + static_cast<int>(threadIdx.x);
+    const int r = e / kPieces, pc = e % kPieces, row = row0 + r;
+    const int64_t at = static_cast<int64_t>(sg.q_row0 + (row >> p.log_group)) * p.hq + (kvh << p.log_group) + (row & ((1 << p.log_group) - 1));
+    const uint4 v = row < rows ? *reinterpret_cast<const uint4 *>(p.q + at * HD + pc * 8) : make_uint4(0u, 0u, 0u, 0u);
+    uint32_t a = bf16x8_absmax(v);
 #pragma unroll
-        for (int off = kPieces / 2; off >= 1; off >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, off));
-        const bool bad = a >= 0x7f80u;
-        const int eq = bad ? 0 : q8_exponent(a);
-        uint2 vh, vl;
-        q8_split(v, pow2i(-eq), 1.f, vh, vl);
-        if (bad) vh = make_uint2(kQ8NanWord, kQ8NanWord);
-        *reinterpret_cast<uint2 *>(dst + row_chunk<HD>(r, pc >> 1) + (pc & 1) * 8) = vh;
-        *reinterpret_cast<uint2 *>(dst + C::kPart + row_chunk<HD>(r, pc >> 1) + (pc & 1) * 8) = vl;
-        if (pc == 0) {  // a row past the last adds 2^-inf
-            coef[r] = row < rows ? pow2i(eq) * p.scale_log2 : 0.f;
-            coef[kWqRows + r] = row < rows ? -p.lse[at] : -INFINITY;
-        }
+    for (int off = kPieces / 2; off >= 1; off >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, off));
+    const bool bad = a >= 0x7f80u;
+    const int eq = bad ? 0 : q8_exponent(a);
+    uint2 vh, vl;
+    q8_split(v, pow2i(-eq), 1.f, vh, vl);
+    if (bad) vh = make_uint2(kQ8NanWord, kQ8NanWord);
+    *reinterpret_cast<uint2 *>(dst + row_chunk<HD>(r, pc >> 1) + (pc & 1) * 8) = vh;
+    *reinterpret_cast<uint2 *>(dst + C::kPart + row_chunk<HD>(r, pc >> 1) + (pc & 1) * 8) = vl;
+    if (pc == 0) {  // a row past the last adds 2^-inf
+        coef[r] = row < rows ? pow2i(eq) * p.scale_log2 : 0.f;
+        coef[kWqRows + r] = row < rows ? -p.lse[at] : -INFINITY;
     }
 }
 
@@ -436,7 +436,7 @@ cudaError_t launch_weights_q8_t(const CUtensorMap &tm_k, const WeightQ8Params &p
     cudaError_t e = set_dyn_smem_once(weights_q8_kernel<HD>, WqCfg<HD>::kDynSmem, configured);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(groups));
+    cfg.gridDim = dim3(static_cast<unsigned>(groups), kWqRows * (HD / 8) / 256);
     cfg.blockDim = dim3(256);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
