@@ -146,20 +146,22 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
 //
 // 8 bits: codes stay codes.  The page's largest magnitude is the largest of its rows' largest codes, each with its old
 // page's scale; a row whose scale stays moves as it is, another's codes are scaled by the difference.  (Through
-// bf16 values in registers, eight codes a load, 8 sequences x 8 layers down to 4k tokens took 545 us.)
-// Bound by the rows' scattered reads: 128 bytes each at d = 128.
+// bf16 values in registers, eight codes a load, 8 sequences x 8 layers down to 4k tokens took 545 us; with divisions and
+// rows in 64 bits, 94 registers a thread, 272.)  Bound by the rows' scattered reads, 128 bytes each at d = 128, at the end
+// of a chain of three loads: 214 us, 5.0 TB/s of reads and writes.
 template <typename Params, bool Q8, int CPR, int NC>
 __global__ void __launch_bounds__(kQ8Block) evict_copy_kernel(const __grid_constant__ Params p, int threads)
 {
     __shared__ uint2 s_max[kQ8Block / 32];
     ptx::griddep_wait();  // launched with programmatic serialization
     ptx::griddep_launch_dependents();
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kQ8Block / threads) + threadIdx.x / threads;
-    const bool on = unit < static_cast<int64_t>(p.L) * p.n_new * p.hkv;
-    const int64_t u = on ? unit : 0;
-    const int h = static_cast<int>(u % p.hkv);
-    const int pg = static_cast<int>(u / p.hkv % p.n_new);
-    const int64_t l = u / p.hkv / p.n_new;
+    const int log_threads = 31 - __clz(threads);
+    const uint32_t unit = (blockIdx.x << (kLogQ8Block - log_threads)) + (threadIdx.x >> log_threads);  // (below 2^31: the pools' pages)
+    const bool on = unit < static_cast<uint32_t>(p.L * p.n_new * p.hkv);
+    const uint32_t u = on ? unit : 0, page = u / p.hkv;
+    const int h = static_cast<int>(u - page * p.hkv);
+    const int pg = static_cast<int>(page % p.n_new);
+    const int l = static_cast<int>(page / p.n_new);
     int lo = 0, hi = p.n - 1;
     while (lo < hi) {  // last segment with new0 <= pg
         const int mid = (lo + hi + 1) >> 1;
@@ -170,9 +172,9 @@ __global__ void __launch_bounds__(kQ8Block) evict_copy_kernel(const __grid_const
     const int32_t *kept = p.kept + static_cast<int64_t>(sg.row) * p.kept_stride + (lp << lps);
     const int32_t *table = p.page_table + sg.table_row;
     const int rows = on ? min(p.ps, sg.keep - (lp << lps)) : 0;
-    const int64_t head = (l * p.num_pages + p.new_pages[pg]) * p.hkv + h;
+    const int head = (l * p.num_pages + p.new_pages[pg]) * p.hkv + h;
     const uint4 *kp = static_cast<const uint4 *>(p.k_pool), *vp = static_cast<const uint4 *>(p.v_pool);
-    int64_t from[NC];  // the source row, of all layers' rows
+    int from[NC];  // the source row, of all layers' rows (a cache's rows are below 2^31)
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
         const int row = (i * threads + t) / CPR;
@@ -189,7 +191,7 @@ __global__ void __launch_bounds__(kQ8Block) evict_copy_kernel(const __grid_const
         k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
         ke[i] = ve[i] = -126;
         if (from[i] < 0) continue;
-        const int64_t c = from[i] * CPR + (i * threads + t) % CPR;
+        const int64_t c = static_cast<int64_t>(from[i]) * CPR + (i * threads + t) % CPR;
         k[i] = kp[c];
         v[i] = vp[c];
         if constexpr (Q8) {
@@ -227,7 +229,8 @@ __global__ void __launch_bounds__(kQ8Block) evict_copy_kernel(const __grid_const
         }
         if (on && t == 0) reinterpret_cast<char2 *>(p.exps)[head] = make_char2(static_cast<char>(kn), static_cast<char>(vn));
     }
-    uint4 *kd = static_cast<uint4 *>(p.k_pool) + (head << lps) * CPR, *vd = static_cast<uint4 *>(p.v_pool) + (head << lps) * CPR;
+    const int64_t to = (static_cast<int64_t>(head) << lps) * CPR;
+    uint4 *kd = static_cast<uint4 *>(p.k_pool) + to, *vd = static_cast<uint4 *>(p.v_pool) + to;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
         if (from[i] < 0) continue;

@@ -112,7 +112,7 @@ __host__ __device__ constexpr int q8_unit_threads(int page_elems)
 }
 __host__ __device__ constexpr int q8_unit_chunks(int page_elems) { return page_elems / 8 / q8_unit_threads(page_elems); }
 
-constexpr int kQ8Block = 256;
+constexpr int kLogQ8Block = 8, kQ8Block = 1 << kLogQ8Block;
 
 // Quantises one page of one kv-head.  Thread t of `threads` holds chunks c = i * threads + t (row c / CPR, eight
 // columns from 8 (c % CPR)): rows [0, n_rows) are valid; load(row, col8, k, v) gives their bf16 values.  Rows below
