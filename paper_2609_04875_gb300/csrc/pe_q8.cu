@@ -149,14 +149,14 @@ __global__ void __launch_bounds__(256) read_kv_kernel(const __grid_constant__ Re
     const int first = max(sg.begin, lp << p.log_ps), rows = min(sg.end, (lp + 1) << p.log_ps) - first;
     const int page = p.page_table[sg.table_row + lp];
     if (page < 0 || page >= p.num_pages) return;  // (no valid token lies there)
-    const int cpr = p.d / (Q8 ? 16 : 8);  // 16-byte chunks of a stored row
+    const int log_cpr = 31 - __clz(p.d / (Q8 ? 16 : 8)), cpr = 1 << log_cpr;  // 16-byte chunks of a stored row
     const int64_t head0 = (l * p.num_pages + page) * p.hkv;
     const int64_t out0 = (l * p.n_total + sg.tok0 + (first - sg.begin)) * p.hkv;
     const uint4 *kp = static_cast<const uint4 *>(p.k_pool), *vp = static_cast<const uint4 *>(p.v_pool);
 #pragma unroll 4
     for (int i = threadIdx.x; i < rows * p.hkv * cpr; i += 256) {
-        const int col = i % cpr, r = i / cpr;  // (cpr: a power of two)
-        const int row = r / p.hkv, h = r - row * p.hkv;
+        const int col = i & (cpr - 1), r = i >> log_cpr;
+        const int row = static_cast<int>(static_cast<unsigned>(r) / static_cast<unsigned>(p.hkv)), h = r - row * p.hkv;
         const int64_t src = (((head0 + h) << p.log_ps) + (first & (p.ps - 1)) + row) * cpr + col;
         const int64_t dst = (out0 + r) * cpr + col;
         const uint4 k = kp[src], v = vp[src];
