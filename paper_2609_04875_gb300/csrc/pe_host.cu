@@ -2009,15 +2009,18 @@ pe_status add_weights_q8(pe_cache *c, std::vector<Q8Item> items, int32_t layer, 
     while ((1 << p.log_ps) < p.ps) p.log_ps++;
     p.oob_row = static_cast<int32_t>(c->code_rows);
     p.scale_log2 = scale * 1.4426950408889634f;
-    int64_t groups = 0, tiles = 0;
+    int64_t groups = 0, tiles = 0, units = 0;  // units: of a tile, at most
     auto flush = [&]() -> pe_status {
         if (p.n == 0) return PE_OK;
         if (injected_failure(c)) return launch_fault("weights kernels");
-        cudaError_t e = launch_weights_q8(cf.head_dim, c->tm_k8, p, static_cast<int>(groups), static_cast<int>(tiles), st);
+        // few tiles of keys: the kv-heads and groups of each are split over a cluster
+        int split = 1;
+        while (split < 8 && tiles * split <= c->num_sms && split < units) split *= 2;
+        cudaError_t e = launch_weights_q8(cf.head_dim, c->tm_k8, p, static_cast<int>(groups), static_cast<int>(tiles), split, st);
         if (e != cudaSuccess) return cuda_fail(e, "weights kernel launch");
         c->launches += 2;
         p.n = 0;
-        groups = tiles = 0;
+        groups = tiles = units = 0;
         return PE_OK;
     };
     for (size_t i = 0; i < items.size(); ++i) {
@@ -2042,6 +2045,7 @@ pe_status add_weights_q8(pe_cache *c, std::vector<Q8Item> items, int32_t layer, 
         p.segs[p.n++] = WeightQ8Seg{it.row, it.seq * cf.max_pages_per_seq, it.q_row0, it.n_q, it.n_keys, static_cast<int32_t>(tiles),
                                     static_cast<int32_t>(n_groups), static_cast<int32_t>(groups)};
         groups += n_groups * hkv;
+        units = std::max(units, n_groups * hkv);
         tiles += ceil_div(it.n_keys, 128);
     }
     return flush();

@@ -393,7 +393,7 @@ cudaError_t launch_evict_finish(const EvictParams &p, cudaStream_t st);
 cudaError_t launch_weights(int head_dim, const WeightParams &p, int64_t q_rows, int max_keys, cudaStream_t st);
 // The same from scores and lse that launch_attn_q8 left.
 cudaError_t launch_weights_kept(const WeightParams &p, int max_keys, cudaStream_t st);
-cudaError_t launch_weights_q8(int head_dim, const CUtensorMap &tm_k, const WeightQ8Params &p, int groups, int tiles,
+cudaError_t launch_weights_q8(int head_dim, const CUtensorMap &tm_k, const WeightQ8Params &p, int groups, int tiles, int split,
                               cudaStream_t st);
 // rows_cap: 4, 8 or 16 rows a block.  tm_k / tm_v: the codes as 2-D maps {d, L*num_pages*Hkv*ps} with d x ps boxes,
 // swizzled over d bytes.

@@ -456,6 +456,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             const Q8Seq &sq = s_seqs[ci.si];
             const int row0 = ci.blk * RB;
             const int n_rows = min(RB, (sq.n_q << lg) - row0);
+            const int out_rows = p.out ? n_rows : 0;  // (no output: the log-sum-exp alone is asked for)
             const bool whole = sq.n_full + (sq.rem0 >= 0 ? 1 : 0) == 1;
             auto out_row = [&](int r) {  // of row r of the block
                 const int row = row0 + r;
@@ -499,7 +500,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                         make_float4(o[k] * scale, o[k + 1] * scale, o[k + 2] * scale, o[k + 3] * scale);
                 ptx::bar_sync(kRowsBarEpi, 128);
 #pragma unroll 4
-                for (int r = t / 8; r < n_rows; r += 16) {
+                for (int r = t / 8; r < out_rows; r += 16) {
                     const int col = t % 8 * 4;
                     float4 v = *reinterpret_cast<const float4 *>(stage + r * C::kStageRow + col);
 #pragma unroll
@@ -509,7 +510,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                     }
                     if (!whole) {
                         *reinterpret_cast<float4 *>(p.part + (static_cast<int64_t>(c) * RB + r) * HD + x + col) = v;
-                    } else if (p.out) {
+                    } else {
                         const float inv = s_inv[r];
                         *reinterpret_cast<uint2 *>(p.out + out_row(r) * HD + x + col) =
                             make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));

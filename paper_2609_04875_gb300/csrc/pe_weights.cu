@@ -181,10 +181,13 @@ __global__ void __launch_bounds__(32 * kKeptWarps) weights_kept_kernel(const __g
 //     S^T [128 keys x 128 rows] = K8 [128 x d] . Q8^T, q in two e4m3 parts added up in the same columns (q8_mma.cuh),
 //     acc[key] += sum over rows of 2^(S 2^(ek + eq) scale_log2 - lse)
 // A CTA takes 128 keys of a sequence and goes through all kv-heads and groups of 128 rows (a unit each), so that a key
-// has one writer; a thread owns a key and adds up its rows in order.  Bound by the exponentials: rows x keys of them.
+// has one writer; a thread owns a key and adds up its rows in order.  Where the tiles of keys are fewer than the SMs, a
+// cluster of up to 8 CTAs shares a tile's units (1.6 us each, one after another) and its first CTA adds up the others'
+// sums in order: 128 queries of 32 q-heads on 1000 keys 80 -> 37 us, all launches.  Bound by the exponentials: rows x keys
+// of them.
 // q's parts, 2^eq scale_log2 and -lse of each group are laid out once (weights_rows_kernel) as the kernel's shared
 // memory holds them, so a group is one bulk copy.  For 2 x 32 queries of 32 q-heads on 9k and 16k keys the scores kept by
-// the attention, 8 bytes a row and key, took 99 us to add up; this takes 33, its layout of q included.
+// the attention, 8 bytes a row and key, took 99 us to add up; this takes 28, its layout of q included.
 //
 // Roles (320 threads): warps 0-3 and 4-7 the sums of every other unit, warp 8 copies, warp 9 MMAs.
 constexpr int kWqThreads = 320, kWqStages = 2, kWqRows = 128;
@@ -243,7 +246,7 @@ __global__ void __launch_bounds__(256) weights_rows_kernel(const __grid_constant
 
 template <int HD>
 __global__ void __launch_bounds__(kWqThreads, 2)
-    weights_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ WeightQ8Params p)
+    weights_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ WeightQ8Params p, int split)
 {
     using C = WqCfg<HD>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -280,14 +283,18 @@ __global__ void __launch_bounds__(kWqThreads, 2)
     ptx::griddep_wait();  // launched with programmatic serialization: the row groups
     ptx::griddep_launch_dependents();
     const uint32_t tmem = *tmem_slot;
-    const int b = static_cast<int>(blockIdx.x);
+    const int b = static_cast<int>(blockIdx.x) / split, rank = static_cast<int>(blockIdx.x) % split;
     int lo = 0, hi = p.n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (p.segs[mid].tile0 <= b) lo = mid; else hi = mid;
     }
     const WeightQ8Seg &sg = p.segs[lo];
-    const int key0 = (b - sg.tile0) * 128, units = p.hkv * sg.n_groups;
+    const int key0 = (b - sg.tile0) * 128, all_units = p.hkv * sg.n_groups;
+    // the CTA's units (kv-head u / n_groups, group u % n_groups): unit0 + [0, units), of kv-heads head0 + ..
+    const int unit0 = static_cast<int>(static_cast<int64_t>(all_units) * rank / split);
+    const int units = static_cast<int>(static_cast<int64_t>(all_units) * (rank + 1) / split) - unit0;
+    const int head0 = unit0 / sg.n_groups, group0 = unit0 - head0 * sg.n_groups;
     int issued = 0;  // copies: stages filled (K in the low half, groups in the high)
 
     if (warp == 8) {
@@ -304,20 +311,20 @@ __global__ void __launch_bounds__(kWqThreads, 2)
             }
         }
         bool ok = true;
-        for (int u = 0, h = 0, g = 0; u < units && ok; ++u) {
-            if (g == 0) {
+        for (int u = 0, h = 0, g = group0; u < units && ok; ++u) {
+            if (u == 0 || g == 0) {
                 if (h >= kWqStages && !(ok = wait_spin(bar(kKEmpty, h), ((h / kWqStages) - 1) & 1, wctx))) break;
                 if (lane == 0) ptx::mbar_arrive_expect_tx(bar(kKFull, h), C::kTile);
                 __syncwarp();
                 if (lane < (128 >> p.log_ps))
-                    ptx::tma_load_2d(sbase + C::kOffK + (h & 1) * C::kTile + (lane << p.log_ps) * HD, &tm_k, 0, row0 + h * step, bar(kKFull, h));
+                    ptx::tma_load_2d(sbase + C::kOffK + (h & 1) * C::kTile + (lane << p.log_ps) * HD, &tm_k, 0, row0 + (head0 + h) * step, bar(kKFull, h));
                 __syncwarp();
                 issued += 1;
             }
             if (u >= kWqStages && !(ok = wait_spin(bar(kQEmpty, u), ((u / kWqStages) - 1) & 1, wctx))) break;
             if (lane == 0) {
                 ptx::mbar_arrive_expect_tx(bar(kQFull, u), C::kGroup);
-                ptx::bulk_load(sbase + (u & 1) * C::kGroup, p.groups + static_cast<int64_t>(sg.group0 + u) * C::kGroup, C::kGroup, bar(kQFull, u));
+                ptx::bulk_load(sbase + (u & 1) * C::kGroup, p.groups + static_cast<int64_t>(sg.group0 + unit0 + u) * C::kGroup, C::kGroup, bar(kQFull, u));
             }
             __syncwarp();
             issued += 1 << 16;
@@ -342,8 +349,8 @@ __global__ void __launch_bounds__(kWqThreads, 2)
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
         const uint64_t k_desc = row_desc<HD>(sbase + C::kOffK, 16), q_desc = row_desc<HD>(sbase, 16);
         bool ok = true;
-        for (int u = 0, h = 0, g = 0; u < units; ++u) {
-            if (g == 0 && !(ok = wait_spin(bar(kKFull, h), (h / kWqStages) & 1, wctx))) break;
+        for (int u = 0, h = 0, g = group0; u < units; ++u) {
+            if ((u == 0 || g == 0) && !(ok = wait_spin(bar(kKFull, h), (h / kWqStages) & 1, wctx))) break;
             if (!(ok = wait_spin(bar(kQFull, u), (u / kWqStages) & 1, wctx))) break;
             if (u >= 2 && !(ok = wait_spin(bar(kSEmpty, u), ((u / 2) - 1) & 1, wctx))) break;
             ptx::tc_fence_after();
@@ -380,7 +387,7 @@ __global__ void __launch_bounds__(kWqThreads, 2)
         float sum = 0.f;
         bool ok = true;
         for (int u = side; u < units && ok; u += 2) {
-            const int h = u / sg.n_groups, row0 = (u - h * sg.n_groups) * kWqRows;
+            const int h = (unit0 + u) / sg.n_groups, row0 = (unit0 + u - h * sg.n_groups) * kWqRows;
             const float ks = head >= 0 ? pow2i(p.exps[2 * (head + h)]) : 0.f;
             const float2 ks2 = make_float2(ks, ks);
             const float *coef = reinterpret_cast<const float *>(smem + side * C::kGroup + 2 * C::kPart);
@@ -419,10 +426,18 @@ __global__ void __launch_bounds__(kWqThreads, 2)
         }
         if (side == 1) s_sum[t] = sum;
         ptx::bar_sync(1, 256);
-        if (side == 0 && key < sg.n_keys) p.weights[static_cast<int64_t>(sg.row) * p.weights_stride + key] += sum + s_sum[t];
+        if (side == 0) s_sum[t] += sum;
     }
     ptx::tc_fence_before();
     __syncthreads();
+    if (split > 1) ptx::cluster_sync();  // every CTA's sums are in its shared memory
+    if (rank == 0 && threadIdx.x < 128) {
+        const int t = static_cast<int>(threadIdx.x);
+        float sum = s_sum[t];
+        for (int r = 1; r < split; ++r) sum += ptx::ld_cluster_f32(ptx::smem_addr(s_sum + t), r);
+        if (key0 + t < sg.n_keys) p.weights[static_cast<int64_t>(sg.row) * p.weights_stride + key0 + t] += sum;
+    }
+    if (split > 1) ptx::cluster_sync();  // .. and has been read
     if (warp == 9) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, C::kTmemCols);
@@ -430,7 +445,7 @@ __global__ void __launch_bounds__(kWqThreads, 2)
 }
 
 template <int HD>
-cudaError_t launch_weights_q8_t(const CUtensorMap &tm_k, const WeightQ8Params &p, int groups, int tiles, cudaStream_t st)
+cudaError_t launch_weights_q8_t(const CUtensorMap &tm_k, const WeightQ8Params &p, int groups, int tiles, int split, cudaStream_t st)
 {
     static std::atomic<uint64_t> configured{0};
     cudaError_t e = set_dyn_smem_once(weights_q8_kernel<HD>, WqCfg<HD>::kDynSmem, configured);
@@ -445,17 +460,23 @@ cudaError_t launch_weights_q8_t(const CUtensorMap &tm_k, const WeightQ8Params &p
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if ((e = cudaLaunchKernelEx(&cfg, weights_rows_kernel<HD>, p)) != cudaSuccess) return e;
-    cfg.gridDim = dim3(static_cast<unsigned>(tiles));
+    cudaLaunchAttribute both[2] = {attr[0], {}};
+    both[1].id = cudaLaunchAttributeClusterDimension;
+    both[1].val.clusterDim.x = static_cast<unsigned>(split);
+    both[1].val.clusterDim.y = both[1].val.clusterDim.z = 1;
+    cfg.attrs = both;
+    cfg.numAttrs = split > 1 ? 2 : 1;
+    cfg.gridDim = dim3(static_cast<unsigned>(tiles * split));
     cfg.blockDim = dim3(kWqThreads);
     cfg.dynamicSmemBytes = WqCfg<HD>::kDynSmem;
-    return cudaLaunchKernelEx(&cfg, weights_q8_kernel<HD>, tm_k, p);
+    return cudaLaunchKernelEx(&cfg, weights_q8_kernel<HD>, tm_k, p, split);
 }
 
 }  // namespace
 
-cudaError_t launch_weights_q8(int head_dim, const CUtensorMap &tm_k, const WeightQ8Params &p, int groups, int tiles, cudaStream_t st)
+cudaError_t launch_weights_q8(int head_dim, const CUtensorMap &tm_k, const WeightQ8Params &p, int groups, int tiles, int split, cudaStream_t st)
 {
-    return head_dim == 128 ? launch_weights_q8_t<128>(tm_k, p, groups, tiles, st) : launch_weights_q8_t<64>(tm_k, p, groups, tiles, st);
+    return head_dim == 128 ? launch_weights_q8_t<128>(tm_k, p, groups, tiles, split, st) : launch_weights_q8_t<64>(tm_k, p, groups, tiles, split, st);
 }
 
 cudaError_t launch_weights_kept(const WeightParams &p, int max_keys, cudaStream_t st)

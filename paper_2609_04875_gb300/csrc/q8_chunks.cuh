@@ -103,8 +103,8 @@ __global__ void __launch_bounds__(THREADS) attn_q8_combine_kernel(const __grid_c
             const int64_t c = k < nfull ? first + static_cast<int64_t>(k) * sq.n_blocks : (in ? rem : (nfull ? first : rem));
             mv[u] = in ? __ldcg(pm + c * RB + r) : -INFINITY;
             lv[u] = in ? __ldcg(pl + c * RB + r) : 0.f;
-            ov[u] = in ? __ldcg(reinterpret_cast<const float4 *>(p.part + (c * RB + r) * HD) + t)
-                       : make_float4(0.f, 0.f, 0.f, 0.f);
+            ov[u] = in && p.out ? __ldcg(reinterpret_cast<const float4 *>(p.part + (c * RB + r) * HD) + t)
+                                : make_float4(0.f, 0.f, 0.f, 0.f);
         }
         float bmx = mx;
 #pragma unroll
