@@ -705,11 +705,12 @@ struct AttnItem {
 // takes 8, where a chunk's cost is least and the estimates hardly differ (16 agents, 5200 tiles: 67.4 us
 // with 7 or 8, 4.6 % more with 6).  tiles_of(i): sequence i's tiles, items_of(i): its items, each all those tiles;
 // tiles: of all items; longest: the longest chunk, taken from `many` tiles per SM on; drain: what the last chunk's tiles
-// cost once more.
+// cost once more; whole: what is left is whole remainders, one after another on an SM (2 sequences of 128 tiles x 8
+// kv-heads: chunks of 14, not of 13 that leave 16 remainders of 11 for 8 idle SMs, 43 us for 55).
 constexpr double kDecChunkCost = 0.35;
 template <typename Tiles, typename Items>
 int64_t chunk_tiles(const pe_cache *c, size_t lo, size_t hi, const Tiles &tiles_of, const Items &items_of, int64_t tiles,
-                    int64_t longest, int64_t many, double chunk_cost, double drain)
+                    int64_t longest, int64_t many, double chunk_cost, double drain, bool whole = false)
 {
     const int64_t N = c->num_sms;
     if (tiles > many * N) return longest;  // many tiles per SM: the longest chunks
@@ -731,7 +732,11 @@ int64_t chunk_tiles(const pe_cache *c, size_t lo, size_t hi, const Tiles &tiles_
         double t = static_cast<double>(rounds) * U;
         // remainders beyond what the idle SMs of the last round hold (each at least one)
         const double room = static_cast<double>(idle) * U;
-        if (R > 0 && (idle == 0 || rem_cost > room))
+        if (whole && R > 0) {  // .. whole ones
+            const double each = rem_cost / static_cast<double>(R);
+            const int64_t later = R - idle * static_cast<int64_t>(U / each);
+            if (later > 0) t += static_cast<double>(ceil_div(later, N)) * each;
+        } else if (R > 0 && (idle == 0 || rem_cost > room))
             t += std::max((rem_cost - room) / static_cast<double>(N), static_cast<double>(rem_max) + chunk_cost - (idle > 0 ? U : 0.0));
         t += 0.1 * static_cast<double>(ceil_div(cpi, 32)) + drain * static_cast<double>(ct);  // the merge's round trips
         if (t < best_t - 1e-9) {
@@ -1755,7 +1760,7 @@ bool plan_q8(const pe_cache *c, const std::vector<Q8Item> &items, size_t lo, siz
     for (size_t i = lo; i < hi; ++i) longest_item = std::max(longest_item, tiles_of(i));
     int64_t ct = c->dec_chunks_per_sm > 0
                      ? std::min<int64_t>(longest, std::max<int64_t>(1, ceil_div(tiles, c->dec_chunks_per_sm * static_cast<int64_t>(c->num_sms))))
-                     : chunk_tiles(c, lo, hi, tiles_of, items_of, tiles, longest, 64, kQ8ChunkCost, rb <= 16 ? kQ8Drain : 0.0);
+                     : chunk_tiles(c, lo, hi, tiles_of, items_of, tiles, longest, 64, kQ8ChunkCost, rb <= 16 ? kQ8Drain : 0.0, rb > 16);
     if (c->splitkv == 1 && c->num_splits > 0) ct = std::min<int64_t>(longest, ceil_div(longest_item, c->num_splits));
     std::memset(static_cast<void *>(&p), 0, offsetof(Q8AttnParams, seqs));
     for (;; ct = longest) {

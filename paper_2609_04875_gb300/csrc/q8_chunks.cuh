@@ -63,8 +63,10 @@ __device__ __forceinline__ Q8Chunk q8_chunk(const Q8AttnParams &p, const Q8Seq *
 // Merge of the items held in several chunks: M = max_k m_k, O = sum_k 2^(m_k - M) O_k / sum_k 2^(m_k - M) l_k, in
 // the item's chunk order.  A block per item and row; its groups of HD / 4 threads take every kGroups-th chunk, eight of
 // them a round trip to L2.  Items of many chunks take the form with 512 threads: 94 chunks (8 rows on 120k keys) in one
-// round trip, not three.
-template <int HD, int RB, int THREADS>
+// round trip, not three.  ROWS, for blocks of many rows held in few chunks: a group has a row to itself, and a block
+// several (8 sequences of 4000 keys, 64 rows, with the attention: 39.2 -> 33.1 us; of 32k, 128 rows: 221 -> 217; but one
+// of 32k, 19 chunks, 36.8 -> 39.1).
+template <int HD, int RB, int THREADS, bool ROWS>
 __global__ void __launch_bounds__(THREADS) attn_q8_combine_kernel(const __grid_constant__ Q8AttnParams p)
 {
     constexpr int kLanes = HD / 4;
@@ -72,7 +74,7 @@ __global__ void __launch_bounds__(THREADS) attn_q8_combine_kernel(const __grid_c
     constexpr int kOB = 8;
     __shared__ float4 s_acc[kGroups][kLanes];
     __shared__ float s_m[kGroups], s_l[kGroups];
-    const int item = static_cast<int>(blockIdx.x), r = static_cast<int>(blockIdx.y);
+    const int item = static_cast<int>(blockIdx.x), r0 = static_cast<int>(blockIdx.y) * (ROWS ? kGroups : 1);
     int lo = 0, hi = p.n_seqs;
     while (hi - lo > 1) {  // the last sequence whose first item is at most this one
         const int mid = (lo + hi) >> 1;
@@ -83,8 +85,8 @@ __global__ void __launch_bounds__(THREADS) attn_q8_combine_kernel(const __grid_c
     const int nfull = sq.n_full, cpi = nfull + (sq.rem0 >= 0 ? 1 : 0);
     const int first = sq.full0 + kvh * nfull * sq.n_blocks + blk;
     const int rem = sq.rem0 + kvh * sq.n_blocks + blk;
-    const int row = blk * RB + r;
     const int grp = static_cast<int>(threadIdx.x) / kLanes;
+    const int r = ROWS ? r0 + grp : r0, row = blk * RB + r;
     const int t = static_cast<int>(threadIdx.x) % kLanes;
     const float *pm = p.part + static_cast<int64_t>(p.total_chunks) * RB * HD;
     const float *pl = pm + static_cast<int64_t>(p.total_chunks) * RB;
@@ -93,12 +95,13 @@ __global__ void __launch_bounds__(THREADS) attn_q8_combine_kernel(const __grid_c
     if (cpi <= 1 || row >= sq.n_q * p.group) return;
     float mx = -INFINITY, den = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = grp; k0 < cpi; k0 += kGroups * kOB) {
+    constexpr int kStep = ROWS ? 1 : kGroups;  // from one of the group's chunks to the next
+    for (int k0 = ROWS ? 0 : grp; k0 < cpi; k0 += kStep * kOB) {
         float mv[kOB], lv[kOB];
         float4 ov[kOB];
 #pragma unroll
         for (int u = 0; u < kOB; ++u) {
-            const int k = k0 + u * kGroups;
+            const int k = k0 + u * kStep;
             const bool in = k < cpi;
             const int64_t c = k < nfull ? first + static_cast<int64_t>(k) * sq.n_blocks : (in ? rem : (nfull ? first : rem));
             mv[u] = in ? __ldcg(pm + c * RB + r) : -INFINITY;
@@ -132,20 +135,23 @@ __global__ void __launch_bounds__(THREADS) attn_q8_combine_kernel(const __grid_c
             acc.w += w * ov[u].w;
         }
     }
-    s_acc[grp][t] = acc;
-    if (t == 0) {
-        s_m[grp] = mx;
-        s_l[grp] = den;
+    float M = mx, l = den;
+    float4 o = acc;
+    if constexpr (!ROWS) {
+        s_acc[grp][t] = acc;
+        if (t == 0) {
+            s_m[grp] = mx;
+            s_l[grp] = den;
+        }
+        __syncthreads();
+        if (grp != 0) return;
+#pragma unroll
+        for (int q = 0; q < kGroups; ++q) M = fmaxf(M, s_m[q]);
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+        l = 0.f;
     }
-    __syncthreads();
-    if (grp != 0) return;
-    float M = -INFINITY;
 #pragma unroll
-    for (int q = 0; q < kGroups; ++q) M = fmaxf(M, s_m[q]);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-#pragma unroll
-    for (int q = 0; q < kGroups; ++q) {
+    for (int q = 0; q < (ROWS ? 0 : kGroups); ++q) {
         if (s_m[q] == -INFINITY) {
             l += s_l[q];  // 0 or NaN
             continue;
@@ -168,16 +174,20 @@ template <int HD, int RB>
 cudaError_t launch_q8_merge(const Q8AttnParams &p, cudaStream_t st)
 {
     const bool many = p.max_chunks > 8 * 128 / (HD / 4);
+    constexpr int kRows = 128 / (HD / 4);
+    const bool rows = RB >= 32 && (p.max_chunks <= 8 || p.total_items * RB >= 4096);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.total_items), RB);
-    cfg.blockDim = dim3(many ? 512 : 128);
+    cfg.gridDim = dim3(static_cast<unsigned>(p.total_items), rows ? RB / kRows : RB);
+    cfg.blockDim = dim3(many && !rows ? 512 : 128);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, many ? attn_q8_combine_kernel<HD, RB, 512> : attn_q8_combine_kernel<HD, RB, 128>, p);
+    if constexpr (RB >= 32)
+        if (rows) return cudaLaunchKernelEx(&cfg, attn_q8_combine_kernel<HD, RB, 128, true>, p);
+    return cudaLaunchKernelEx(&cfg, many ? attn_q8_combine_kernel<HD, RB, 512, false> : attn_q8_combine_kernel<HD, RB, 128, false>, p);
 }
 
 }  // namespace
