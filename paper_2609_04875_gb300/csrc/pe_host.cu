@@ -1728,18 +1728,22 @@ int q8_block(int64_t rows)
     return rb;
 }
 
-// Whether a sequence's rows (n_q x group a kv-head) are attended on the codes, or by way of the unpacked layer.  On the
-// codes every block of up to 128 rows goes through the keys again (in L2); unpacking costs once 5 bytes a code and then
-// HBM's time for bf16.  GPU time in us, codes / unpacked, 8 kv-heads, d = 128: 32 rows on 600 keys 9.4 / 9.9, on 32k 26.6 /
-// 59.0; 64 rows on 600 11.4 / 10.3, on 2000 12.3 / 11.7, on 4000 13.6 / 14.8 (8 sequences 40.3 / 58.6), on 32k 34.2 / 59.5
-// (8: 148 / 416); 128 rows on 4000 17.3 / 15.0, on 8192 20.5 / 18.8 (8: 81 / 119), on 32k 52.0 / 60.4 (8: 220 / 421); 256
-// on 32k 83 / 66.  d = 64, half the bytes for the same scores: 32 rows on 600 8.2 / 9.6, 64 on 4000 11.1 / 13.5, 128 on 8192
-// 17.3 / 16.4, on 32k 33.6 / 33.9.
-bool q8_takes(const pe_cache *c, const AttnItem &it, int g)
+int64_t q8_rows(const AttnItem &it, int g) { return static_cast<int64_t>(it.n_q) * g; }
+
+// Whether a sequence's rows (n_q x group a kv-head) are attended on the codes, or by way of the unpacked layer; keys: of all
+// of the call's sequences of 33 to 128 rows.  On the codes every block of up to 128 rows goes through the keys again (in
+// L2); unpacking costs once 5 bytes a code and then HBM's time for bf16.  GPU time in us, codes / unpacked, 8 kv-heads, d =
+// 128: 32 rows on 600 keys 9.1 / 10.0, on 32k 23 / 59; 64 rows on 600 10.7 / 10.2, on 2000 12.5 / 11.6, on 4000 13.5 / 14.8
+// (8 sequences 32 / 58), on 32k 26 / 60 (8: 145 / 415); 128 rows on 4000 17.5 / 15.0 (8: 47 / 60), on 8192 20.9 / 18.9 (8: 69 /
+// 117), on 32k 37 / 61; 256 on 8192 30.6 / 22.8 (8: 122 / 131), on 32k 71 / 66.  d = 64, half the bytes for the same scores:
+// 64 rows on 600 8.4 / 9.6, on 32k 23 / 33; 128 on 8192 17.4 / 16.5 (8: 56 / 63), on 32k 32.2 / 34.3, 8 sequences of 4000
+// 38.9 / 34.3.
+bool q8_takes(const pe_cache *c, const AttnItem &it, int g, int64_t keys)
 {
     if (c->decode_kernel != 1 || c->splitkv == 0) return false;
-    const int64_t rows = static_cast<int64_t>(it.n_q) * g, keys = c->len[it.seq];
-    return rows <= 32 || (rows <= 64 && keys >= 2048) || (rows <= 128 && keys >= 8192 && c->cfg.head_dim == 128);
+    const int64_t rows = q8_rows(it, g);
+    if (c->cfg.head_dim == 64) return rows <= 64 || (rows <= 128 && keys >= 65536);
+    return rows <= 32 || (rows <= 64 && keys >= 4096) || (rows <= 128 && keys >= 16384);
 }
 
 // One launch over items [lo, hi), at most kMaxSegs: fills p.  ws: floats of workspace for partials and, with `scores`,
@@ -1917,9 +1921,12 @@ pe_status attend(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer,
     const int g = hq / c->cfg.num_kv_heads;
     std::vector<Q8Item> few, left;
     std::vector<AttnItem> many;
+    int64_t keys = 0;
+    for (const AttnItem &it : items)
+        if (q8_rows(it, g) > 32 && q8_rows(it, g) <= 128) keys += c->len[it.seq];
     for (const AttnItem &it : items) {
         if (it.n_q <= 0) continue;
-        if (q8_takes(c, it, g)) few.push_back(Q8Item{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq]), 0});
+        if (q8_takes(c, it, g, keys)) few.push_back(Q8Item{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq]), 0});
         else many.push_back(it);
     }
     if (!few.empty()) {
