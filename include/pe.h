@@ -337,7 +337,11 @@ pe_status pe_cache_scales(const pe_cache *cache, void **exponents);
  * decode kernel (the prefill kernel serves every call);
  * "decode_chunks_per_sm" = 0 (auto, default) or 1..64: how many chunks of
  * 1..8 key tiles per SM the tcgen05 decode kernel cuts a launch's keys into --
- * auto takes the chunk length with the earliest estimated finish;
+ * auto takes the chunk length with the earliest estimated finish; on an 8-bit
+ * cache the kernels on the codes cut theirs likewise, into chunks of 1..14.
+ * There "decode_kernel" = 1 attends sequences of up to 128 query rows (of more
+ * than 32 where the keys are many) on the codes, any other value, or "splitkv"
+ * = 0, all of them by way of the unpacked layer;
  * "attn_kernel" = 1
  * (default) / 2 / 0: the prefill kernel -- 1: the one-item kernel or the
  * persistent stream-K kernel, whichever plan's estimated time is smaller (the

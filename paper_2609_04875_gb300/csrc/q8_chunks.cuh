@@ -175,7 +175,7 @@ cudaError_t launch_q8_merge(const Q8AttnParams &p, cudaStream_t st)
 {
     const bool many = p.max_chunks > 8 * 128 / (HD / 4);
     constexpr int kRows = 128 / (HD / 4);
-    const bool rows = RB >= 32 && (p.max_chunks <= 8 || p.total_items * RB >= 4096);
+    const bool rows = RB >= 32 && (p.max_chunks <= 8 || p.total_items * RB >= 2048);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.total_items), rows ? RB / kRows : RB);
     cfg.blockDim = dim3(many && !rows ? 512 : 128);
