@@ -635,15 +635,17 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
                 for (int part = 0; part < 3; ++part)
                     ptx::tmem_st_n<C::kEPT / 4>(tmem + C::kTmemP + 96 * (i & 1) + 32 * part + key0 / 4 + lane_off, word[part]);
                 if (scaled) {
-#pragma unroll 1
-                    for (int x = 0; x < HD / 2; x += 32) {  // half of O each of the lane's two threads
-                        const uint32_t at = tmem + C::kTmemO + (t >> 7) * (HD / 2) + x + lane_off;
-                        float o[32];
-                        ptx::tmem_ld32(at, o);
-                        ptx::tmem_wait_ld();
+                    constexpr int kN = HD / 64;  // half of O each of the lane's two threads
+                    const uint32_t at = tmem + C::kTmemO + (t >> 7) * (HD / 2) + lane_off;
+                    float o[kN][32];
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] *= f;
-                        ptx::tmem_st32(at, o);
+                    for (int x = 0; x < kN; ++x) ptx::tmem_ld32(at + 32 * x, o[x]);
+                    ptx::tmem_wait_ld();
+#pragma unroll
+                    for (int x = 0; x < kN; ++x) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[x][k] *= f;
+                        ptx::tmem_st32(at + 32 * x, o[x]);
                     }
                 }
                 ptx::tmem_wait_st();
