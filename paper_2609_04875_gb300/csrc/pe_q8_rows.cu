@@ -28,10 +28,11 @@
 // through them once for every 16 and for each reads 58 KB of shared memory a tile besides what its warps exchange.  HBM's
 // share of a tile is 1390 cycles, its 20 MMAs of 64 cycles are 1280; what bounds is the chain of a tile's steps (scores
 // read, maxima exchanged, weights, parts, O scaled): 2200 cycles with 64 rows, of which leaving out any one of the
-// loads, MMAs, exponentials, parts and scaling saves 2 to 8 %.  8 sequences of 32k keys and 8 kv-heads, d = 128: 32 rows 126
-// us, 64 rows 148 (the swap-AB kernel 286), 128 rows 220; HBM's time for the codes is 79.  Not kept: four threads a lane (64
-// rows 161 us), the next tile's scores read before the parts are stored (153; 128 rows spill, 357), weights as three e4m3
-// parts, which need two accumulators (166).
+// loads, MMAs, exponentials, parts and scaling saves 2 to 8 %.  8 sequences of 32k keys and 8 kv-heads, d = 128, with the
+// merge: 32 rows 123 us, 64 rows 144 (the swap-AB kernel 286), 128 rows 214; HBM's time for the codes is 79.  Not kept, 64 rows:
+// four threads a lane 161; groups that take every other tile and pass the references on 148; the next tile's scores read
+// before the parts are stored 153 (128 rows spill, 357); q as an operand in TMEM and six stages 147 (128 rows 211); chunks of
+// 28 tiles 149; weights as three e4m3 parts, which need two accumulators, 166.
 //
 // Roles (512 threads): warps 0-3 and 4-7 weights (lane = thread % 128, the first and second half of its keys), 8-11 q's
 // parts and the epilogue, 12 producer, 13 S, 14 P V, 15 scheduler.
