@@ -168,6 +168,20 @@ __device__ __forceinline__ float4 *part_chunk(float *part_o, int64_t row, int k)
     return reinterpret_cast<float4 *>(part_o + (row & ~static_cast<int64_t>(31)) * HD) + k * 32 + (row & 31);
 }
 
+__device__ __forceinline__ float2 unpack_bf16(uint32_t w)
+{
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
+// a pair of bf16 added to two floats
+__device__ __forceinline__ float2 add_bf16(float2 a, uint32_t w)
+{
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tadd.rn.f32.bf16 %0, lo, %0;\n\tadd.rn.f32.bf16 %1, hi, %1;\n\t}"
+        : "+f"(a.x), "+f"(a.y)
+        : "r"(w));
+    return a;
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
     __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);

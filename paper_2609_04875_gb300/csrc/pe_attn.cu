@@ -104,7 +104,13 @@ struct TileGeo {
 // tiles alternate between the two S buffers, so that S(j+1) runs during the softmax of tile j and the chain of
 // a tile is its softmax alone (at d = 64 S(j+1) overlaps it anyway).  16 agents of 30 tokens on 4k: 55.8 -> 52.1
 // us a layer; 64 MHA agents of 60 tokens on 1.5k: 100.6 -> 93.8.
-template <int HD, bool SPLIT, bool VAPART, bool ONE>
+// RSUM (8-bit caches): the row's sum is that of its weights as P V sees them, rounded to bf16.  A reference moves rarely, so
+// the largest weight is seldom exactly 1; where a few keys carry a row, its rounding then cancels in O / l.  1638 queries on
+// 16k keys with 1 % outlier tokens: 1.6e-3 off 64 bits in the 2-norm against 2.2e-3 (fp32 rounded at the output: 1.5e-3), for
+// 264 us against 252; 8000 queries 334 against 308.  How the rounded pair is added (unpacked, or by mixed adds, one pair in
+// four here) is what was fastest: unpacked 357, mixed 357; stream-K, d = 128: unpacked 274, mixed 264; d = 64 211 and 226 (192
+// without).
+template <int HD, bool SPLIT, bool VAPART, bool ONE, bool RSUM>
 __global__ void __launch_bounds__(kPrefillThreads, 1)
     replay_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                        const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
@@ -567,8 +573,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1)
                         const int c = ch * 32 + 2 * k;
                         const float2 x = fma2(make_float2(s[c], s[c + 1]), sl2x2, nref);
                         const float2 e = make_float2(ex2(x.x), ex2(x.y));
-                        acc[k & 3] = add2(acc[k & 3], e);
                         pk[k] = pack_bf16(e.x, e.y);
+                        acc[k & 3] = !RSUM ? add2(acc[k & 3], e) : (HD == 128 && k % 4 == 3 ? add_bf16(acc[k & 3], pk[k]) : add2(acc[k & 3], unpack_bf16(pk[k])));
                     }
                     if (C::kSepP && ch == 0 && j > 0) {
                         // P_t(j) goes to P_t's own columns once P V_t(j-1) has read P_t(j-1)
@@ -867,13 +873,13 @@ cudaError_t static_scratch(float **ptr)
     return cudaSuccess;
 }
 
-template <int HD, bool SPLIT, bool VAPART, bool ONE>
-static cudaError_t launch_attn_t(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v,
+template <int HD, bool SPLIT, bool VAPART, bool ONE, bool RSUM>
+static cudaError_t launch_attn_r(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v,
                                  const CUtensorMap &o, const AttnParams &p, cudaStream_t st)
 {
     using C = AttnCfg<HD>;
     static std::atomic<uint64_t> configured{0};
-    cudaError_t e = set_dyn_smem_once(replay_attn_kernel<HD, SPLIT, VAPART, ONE>, C::kDynSmem, configured);
+    cudaError_t e = set_dyn_smem_once(replay_attn_kernel<HD, SPLIT, VAPART, ONE, RSUM>, C::kDynSmem, configured);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.total_items));
@@ -885,7 +891,15 @@ static cudaError_t launch_attn_t(const CUtensorMap &q, const CUtensorMap &k, con
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, replay_attn_kernel<HD, SPLIT, VAPART, ONE>, q, k, v, o, p);
+    return cudaLaunchKernelEx(&cfg, replay_attn_kernel<HD, SPLIT, VAPART, ONE, RSUM>, q, k, v, o, p);
+}
+
+template <int HD, bool SPLIT, bool VAPART, bool ONE>
+static cudaError_t launch_attn_t(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v,
+                                 const CUtensorMap &o, const AttnParams &p, cudaStream_t st)
+{
+    return p.rounded_sums ? launch_attn_r<HD, SPLIT, VAPART, ONE, true>(q, k, v, o, p, st)
+                          : launch_attn_r<HD, SPLIT, VAPART, ONE, false>(q, k, v, o, p, st);
 }
 
 cudaError_t launch_replay_attn(int head_dim, bool split, const CUtensorMap &tm_q, const CUtensorMap &tm_k,

@@ -296,8 +296,8 @@ __device__ __noinline__ void merge_own_row(const SkParams &P, int slot, int t, i
 // ONE: every unit of the launch is one q-tile (suffixes of at most 128 rows per kv-head): its key tiles
 // alternate between the two S buffers, so that S(j+1) runs during the softmax of tile j.  A kernel of its
 // own, because both forms in one cost the two-q-tile launches 1 % (d = 64: 7 %).  Short suffix (8 x 16 tokens
-// on 32k, HBM-bound) 181 -> 175 us, at d = 64 133 -> 104 us.
-template <int HD, bool ONE>
+// on 32k, HBM-bound) 181 -> 175 us, at d = 64 133 -> 104 us.  RSUM: see replay_attn_kernel.
+template <int HD, bool ONE, bool RSUM>
 __global__ void __launch_bounds__(kPrefillThreads, 1)
     replay_attn_sk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                           const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ SkParams P)
@@ -709,8 +709,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1)
                             const int c = ch * 32 + 2 * q;
                             const float2 x = fma2(make_float2(s[c], s[c + 1]), sl2x2, nref);
                             const float2 e = make_float2(ex2(x.x), ex2(x.y));
-                            acc[q & 3] = add2(acc[q & 3], e);
                             pk[q] = pack_bf16(e.x, e.y);
+                            acc[q & 3] = !RSUM ? add2(acc[q & 3], e) : (HD == 128 ? add_bf16(acc[q & 3], pk[q]) : add2(acc[q & 3], unpack_bf16(pk[q])));
                         }
                         if (C::kSepP && ch == 0 && j > 0) {
                             // P_t(j) goes to P_t's own columns once P V_t(j-1) has read P_t(j-1)
@@ -884,13 +884,13 @@ __global__ void __launch_bounds__(kPrefillThreads, 1)
     }
 }
 
-template <int HD, bool ONE>
-cudaError_t launch_sk_t(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const SkParams &p,
+template <int HD, bool ONE, bool RSUM>
+cudaError_t launch_sk_r(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const SkParams &p,
                         cudaStream_t st)
 {
     using C = SkCfg<HD, ONE>;
     static std::atomic<uint64_t> configured{0};
-    cudaError_t e = set_dyn_smem_once(replay_attn_sk_kernel<HD, ONE>, C::kDynSmem, configured);
+    cudaError_t e = set_dyn_smem_once(replay_attn_sk_kernel<HD, ONE, RSUM>, C::kDynSmem, configured);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.n_ctas));
@@ -902,7 +902,14 @@ cudaError_t launch_sk_t(const CUtensorMap &q, const CUtensorMap &k, const CUtens
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, replay_attn_sk_kernel<HD, ONE>, q, k, v, p);
+    return cudaLaunchKernelEx(&cfg, replay_attn_sk_kernel<HD, ONE, RSUM>, q, k, v, p);
+}
+
+template <int HD, bool ONE>
+cudaError_t launch_sk_t(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const SkParams &p,
+                        cudaStream_t st)
+{
+    return p.a.rounded_sums ? launch_sk_r<HD, ONE, true>(q, k, v, p, st) : launch_sk_r<HD, ONE, false>(q, k, v, p, st);
 }
 
 }  // namespace

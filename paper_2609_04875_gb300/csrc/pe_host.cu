@@ -995,6 +995,7 @@ pe_status plan_sk(pe_cache *c, const std::vector<AttnItem> &order, size_t lo, si
     p.ps = cf.page_size;
     p.oob_row = static_cast<int32_t>(c->pool_rows);
     p.scale_log2 = scale * 1.4426950408889634f;
+    p.rounded_sums = c->q8;
     std::vector<int32_t> n_all;   // key tiles per unit
     std::vector<double> wt;        // cost of one of its key tiles
     std::vector<double> cum{0.0};  // cost before each unit
@@ -1464,6 +1465,7 @@ pe_status run_attention(pe_cache *c, const std::vector<AttnItem> &items, int32_t
         p.ps = cf.page_size;
         p.oob_row = static_cast<int32_t>(c->pool_rows);
         p.scale_log2 = scale * 1.4426950408889634f;
+        p.rounded_sums = c->q8;
         p.next_stride = c->num_sms;  // one CTA per SM: CTA b's successor on its SM is about b + SMs
         for (;;) {
             int32_t item = 0, comb = 0;
@@ -2706,6 +2708,7 @@ pe_status pe_replay_attn_static_scratch(pe_cache *c, int32_t seq, int32_t layer,
     p.oob_row = static_cast<int32_t>(c->pool_rows);
     p.split_tiles = split_tiles;
     p.scale_log2 = softmax_scale * 1.4426950408889634f;
+    p.rounded_sums = c->q8;
     AttnSeq &q = p.seqs[0];
     q.table_row = seq * cf.max_pages_per_seq;
     q.n_pages = static_cast<int32_t>(c->table[seq].size());

@@ -370,6 +370,16 @@ def test_blocks_of_many_rows(hq, hkv, n, d, ps):
     run_attention(b, seqs, [n, n, n, 1, n], hq)
 
 
+@pytest.mark.parametrize("hq,hkv,n,d,lens", [(128, 1, 1, 128, [17000, 300, 5]), (128, 1, 3, 64, [2000, 700]), (64, 1, 2, 128, [9000, 9000]),
+                                             (32, 8, 16, 128, [1500] * 12), (4, 2, 13, 128, [100 + 3 * i for i in range(70)])])
+def test_wide_groups_and_many_sequences(hq, hkv, n, d, lens):
+    """A query of one sequence fills a block, or several; more sequences than a launch carries."""
+    b = Both(1, hkv, d, 16, pages=sum(x // 16 + 1 for x in lens) + 40, seqs=80)
+    seqs = [b.new() for _ in lens]
+    b.append(seqs, lens, spread=0.5)
+    run_attention(b, seqs, [min(n, x) for x in lens], hq)
+
+
 @pytest.mark.parametrize("rows", [32, 64, 128])
 @pytest.mark.parametrize("d", [64, 128])
 def test_references_that_move_row_by_row(rows, d):
