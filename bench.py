@@ -308,18 +308,18 @@ def oracle_tokens_per_s(units, budget_s, seed=7):
 # DRAM traffic per attention launch from one ncu capture (profiles/), valid only
 # while the kernel source is the one that was captured.
 NCU_TRAFFIC = {
-    "tiny": {"bytes": 1.510912e6, "profile": "profiles/traffic_attention_configs.md", "kernels": ["prefill"],
-             "src_sha256": {"prefill": "2d832440c6589db32d3d476157626a9c118b9d57f1b94e78b8ac82a81e71eacb"}},
-    "agent_batch": {"bytes": 684.892928e6 + 315.216384e6, "profile": "profiles/traffic_attention_configs.md",
-                    "kernels": ["prefill"], "src_sha256": {"prefill": "2d832440c6589db32d3d476157626a9c118b9d57f1b94e78b8ac82a81e71eacb"}},
-    "short_suffix": {"bytes": 1.088975872e9 + 5.404672e6, "profile": "profiles/traffic_attention_configs.md",
-                     "kernels": ["prefill_sk"], "src_sha256": {"prefill_sk": "ce48ccbfdcf5cddb3c29b0c9a2f3fcb1eb298e33bbd25aeab9da20abd269e752"}},
-    "long_suffix": {"bytes": 1.4108928e9 + 1.0369536e9, "profile": "profiles/traffic_attention_configs.md",
-                    "kernels": ["prefill"], "src_sha256": {"prefill": "2d832440c6589db32d3d476157626a9c118b9d57f1b94e78b8ac82a81e71eacb"}},
+    "tiny": {"bytes": 1.510656e6, "profile": "profiles/traffic_attention_configs.md", "kernels": ["prefill"],
+             "src_sha256": {"prefill": "e6f34b019872f72f7a48c0b1ffebbc8b361493f0b106c37ad34c941b6428f8d8"}},
+    "agent_batch": {"bytes": 684.932096e6 + 314.89408e6, "profile": "profiles/traffic_attention_configs.md",
+                    "kernels": ["prefill"], "src_sha256": {"prefill": "e6f34b019872f72f7a48c0b1ffebbc8b361493f0b106c37ad34c941b6428f8d8"}},
+    "short_suffix": {"bytes": 1.087851776e9 + 5.2544e6, "profile": "profiles/traffic_attention_configs.md",
+                     "kernels": ["prefill_sk"], "src_sha256": {"prefill_sk": "24099f079a7ce0ff071dd0f06d6c77bf9d2b506d9629ddaadc32566875e2b416"}},
+    "long_suffix": {"bytes": 1.41099008e9 + 1.036792064e9, "profile": "profiles/traffic_attention_configs.md",
+                    "kernels": ["prefill"], "src_sha256": {"prefill": "e6f34b019872f72f7a48c0b1ffebbc8b361493f0b106c37ad34c941b6428f8d8"}},
     # one sweep step's 192 attention launches (5 forget requests x 32 layers, two launches per layer where a
     # tail launch runs), per layer: bytes / 160
-    "tau_sweep": {"bytes": (47444.38e6 + 8073.877e6) / 160, "profile": "profiles/traffic_attention_configs.md",
-                  "kernels": ["prefill", "prefill_sk"], "src_sha256": {"prefill": "2d832440c6589db32d3d476157626a9c118b9d57f1b94e78b8ac82a81e71eacb", "prefill_sk": "ce48ccbfdcf5cddb3c29b0c9a2f3fcb1eb298e33bbd25aeab9da20abd269e752"}},
+    "tau_sweep": {"bytes": (48420.718e6 + 8106.271e6) / 160, "profile": "profiles/traffic_attention_configs.md",
+                  "kernels": ["prefill", "prefill_sk"], "src_sha256": {"prefill": "e6f34b019872f72f7a48c0b1ffebbc8b361493f0b106c37ad34c941b6428f8d8", "prefill_sk": "24099f079a7ce0ff071dd0f06d6c77bf9d2b506d9629ddaadc32566875e2b416"}},
     "decode_batch": {"bytes": 341.534464e6 + 3.933184e6, "profile": "profiles/decode_tc_decode_batch.md",
                      "kernels": ["decode"],
                      "src_sha256": {"decode": "9afb7597d4a46f6bacd82afca7ce98c9e9b576a6d049d4a91e8ff87a7d73ef63"}},
@@ -327,8 +327,8 @@ NCU_TRAFFIC = {
 CSRC = os.path.join(ROOT, "paper_2609_04875_gb300", "csrc")
 # (file, first line of the kernel's source, the text that follows it): the span that is hashed
 KERNEL_SRC = {
-    "prefill": ("pe_attn.cu", "template <int HD, bool SPLIT, bool VAPART, bool ONE>\n__global__", "// Exercises the bounded wait on its own"),
-    "prefill_sk": ("pe_attn_sk.cu", "// Merge of one row of a cut unit's q-tile", "template <int HD, bool ONE>\ncudaError_t launch_sk_t("),
+    "prefill": ("pe_attn.cu", "template <int HD, bool SPLIT, bool VAPART, bool ONE, bool RSUM>\n__global__", "// Exercises the bounded wait on its own"),
+    "prefill_sk": ("pe_attn_sk.cu", "// Merge of one row of a cut unit's q-tile", "template <int HD, bool ONE, bool RSUM>\ncudaError_t launch_sk_r("),
     "decode": ("pe_decode.cu", "template <int HD, int RB, bool TWO>\n__global__ void __launch_bounds__(kTcThreads, 1)",
                "template <int HD, int RB, bool TWO>\ncudaError_t launch_tc_t("),
 }
