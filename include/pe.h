@@ -34,7 +34,8 @@
  *     device page-table rows and lengths of the sequences it touched from the
  *     host, on `stream`, before returning PE_ERR_CUDA.  Pool slots the failed
  *     call already wrote belong to pages or positions outside every
- *     sequence's valid range afterwards, so no later result reads them
+ *     sequence's valid range afterwards, so no later result reads them; pages
+ *     of an 8-bit cache that it quantised again are put back from a copy
  *     (exception: with "debug_poison" on, a batched crop that fails after its
  *     first launch may leave poisoned slots in pages it had already freed).
  *     A cache is not thread-safe: calls on one cache must not run
@@ -106,7 +107,10 @@ pe_status pe_cache_create(const pe_cache_config *cfg, pe_cache **out);
  * k_pool and v_pool must be NULL (INVALID otherwise).  Device memory: half of
  * a bf16 cache's pools, 2 bytes a page, kv-head and layer for the scales, and
  * one layer's pools in bf16, into which calls that attend many queries unpack
- * the layer they need.  Errors as pe_cache_create. */
+ * the layer they need; and, from the first append of several launches or
+ * pe_replay_rounds on a partly filled page on, room for a copy of the pages that
+ * such a call quantises again (a page a sequence at most).  Errors as
+ * pe_cache_create. */
 pe_status pe_cache_create_q8(const pe_cache_config *cfg, pe_cache **out);
 pe_status pe_cache_destroy(pe_cache *cache);
 

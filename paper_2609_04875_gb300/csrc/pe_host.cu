@@ -99,6 +99,7 @@ struct Journal {
     std::vector<int32_t> popped;       // entries of the start free list popped below `low`, in pop order
     std::vector<SeqSave> seqs;         // one per touched sequence
     std::vector<int32_t> seq_index;    // sequence -> index in seqs, -1 when untouched
+    std::vector<int32_t> saved;        // 8-bit cache: pages whose contents were copied out (save_tails), in slot order
 };
 
 struct pe_cache {
@@ -119,6 +120,8 @@ struct pe_cache {
     bool q8 = false;              // K and V held in 8 bits (q8.cuh)
     void *k8 = nullptr, *v8 = nullptr;  // codes [L][num_pages][Hkv][ps][d]
     int8_t *exps = nullptr;       // scale exponents [L][num_pages][Hkv][2]
+    uint8_t *d_saved = nullptr;   // contents of pages that the call in progress quantises again (save_tails)
+    int64_t saved_slots = 0;      // pages that d_saved holds
     bool own_pools = false;
     int32_t *d_table = nullptr;
     int64_t *d_len = nullptr;
@@ -173,6 +176,13 @@ pe_status check_device(const pe_cache *c)
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// A saved page's slot: its codes and scale exponents of all layers.
+int64_t saved_page_bytes(const pe_cache *c)
+{
+    const int64_t heads = static_cast<int64_t>(c->cfg.num_layers) * c->cfg.num_kv_heads;
+    return heads * c->cfg.page_size * c->cfg.head_dim * 2 + ceil_div(heads * 2, 16) * 16;
+}
+
 // ---- journal: every bookkeeping change of a call, undone if the call fails
 // Saves sequence `seq`'s state before the call changes its table entries at
 // index >= from (or its length, counter, checkpoints, liveness).
@@ -225,15 +235,44 @@ void journal_clear(pe_cache *c)
     for (const SeqSave &sv : j.seqs) j.seq_index[sv.seq] = -1;
     j.seqs.clear();
     j.popped.clear();
+    j.saved.clear();
     j.low = c->free_stack.size();
 }
 
-// Undoes the call's changes and rewrites the device mirror
+// Copies the contents of the journal's saved pages out, or back.
+cudaError_t copy_saved(pe_cache *c, bool back, cudaStream_t st)
+{
+    const pe_cache_config &cf = c->cfg;
+    SaveParams p;
+    std::memset(static_cast<void *>(&p), 0, offsetof(SaveParams, pages));
+    p.k8 = static_cast<uint4 *>(c->k8);
+    p.v8 = static_cast<uint4 *>(c->v8);
+    p.exps = c->exps;
+    p.slot_bytes = saved_page_bytes(c);
+    p.L = cf.num_layers;
+    p.hkv = cf.num_kv_heads;
+    p.ps = cf.page_size;
+    p.d = cf.head_dim;
+    p.num_pages = cf.num_pages;
+    p.back = back ? 1 : 0;
+    const std::vector<int32_t> &pages = c->jr.saved;
+    for (size_t i = 0; i < pages.size(); i += kMaxSavedPages) {
+        p.n = static_cast<int32_t>(std::min<size_t>(kMaxSavedPages, pages.size() - i));
+        p.slots = c->d_saved + static_cast<int64_t>(i) * p.slot_bytes;
+        std::copy_n(pages.begin() + static_cast<int64_t>(i), p.n, p.pages);
+        if (cudaError_t e = launch_save_pages(p, st); e != cudaSuccess) return e;
+        c->launches++;
+    }
+    return cudaSuccess;
+}
+
+// Undoes the call's changes, puts saved pages back and rewrites the device mirror
 // (table row and length) of every touched live sequence on `st`, after any
 // device work the call already enqueued.
 void rollback(pe_cache *c, cudaStream_t st)
 {
     Journal &j = c->jr;
+    (void)copy_saved(c, true, st);
     // the free list: back to its start entries below `low`, then the popped ones in reverse pop order
     c->free_stack.resize(j.low);
     for (auto it = j.popped.rbegin(); it != j.popped.rend(); ++it) c->free_stack.push_back(*it);
@@ -352,6 +391,7 @@ void free_device(pe_cache *c)
     if (c->k8) cudaFree(c->k8);
     if (c->v8) cudaFree(c->v8);
     if (c->exps) cudaFree(c->exps);
+    if (c->d_saved) cudaFree(c->d_saved);
     if (c->d_table) cudaFree(c->d_table);
     if (c->d_len) cudaFree(c->d_len);
     if (c->d_status) cudaFree(c->d_status);
@@ -359,6 +399,7 @@ void free_device(pe_cache *c)
     if (c->d_tickets) cudaFree(c->d_tickets);
     c->k_pool = c->v_pool = c->k8 = c->v8 = nullptr;
     c->exps = nullptr;
+    c->d_saved = nullptr;
     c->d_tickets = nullptr;
     c->d_table = nullptr;
     c->d_len = nullptr;
@@ -525,6 +566,52 @@ void settle_batch_cow(const pe_cache *c, std::vector<AppendPlan> &plans)
         if (it == dropped.end()) dropped.emplace_back(pg, 1);
         else it->second += 1;
     }
+}
+
+// Whether apply_appends takes one launch for the plans.
+bool one_append_launch(const std::vector<AppendPlan> &plans)
+{
+    int64_t segs = 0, pages = 0;
+    for (const AppendPlan &pl : plans) {
+        segs += pl.n > 0 ? 1 : 0;
+        pages += pl.need - (pl.cow ? 1 : 0);
+    }
+    return segs <= kMaxSegs && pages <= kAppendMaxPages;
+}
+
+// Appending onto a partly filled page of an 8-bit cache quantises the page's kept tokens again in place, which a change of
+// lengths and tables does not undo.  So a call with device steps after its first append launch copies the pages that its
+// plans' sequences may so change out first; rollback puts them back.  (A page of which every plan but one makes a copy is
+// among them; which plan that is, rounds decide as they come.)
+pe_status save_tails(pe_cache *c, const std::vector<AppendPlan> &plans, cudaStream_t st)
+{
+    if (!c->q8) return PE_OK;
+    std::vector<int32_t> pages;
+    for (const AppendPlan &pl : plans)
+        if (pl.n > 0 && c->len[pl.seq] % c->cfg.page_size != 0) pages.push_back(c->table[pl.seq].back());
+    std::sort(pages.begin(), pages.end());
+    pages.erase(std::unique(pages.begin(), pages.end()), pages.end());
+    if (pages.empty()) return PE_OK;
+    if (injected_failure(c)) return launch_fault("page save");
+    if (c->host_only) return PE_OK;
+    const int64_t n = static_cast<int64_t>(pages.size());
+    if (n > c->saved_slots) {  // at most a page a sequence; kept for the next call
+        const int64_t slots = std::max(n, std::min<int64_t>(2 * c->saved_slots, c->cfg.max_seqs));
+        uint8_t *fresh = nullptr;
+        const cudaError_t e = cudaMalloc(&fresh, static_cast<size_t>(slots * saved_page_bytes(c)));
+        if (e != cudaSuccess) {
+            (void)cudaGetLastError();  // (no later launch is to find it)
+            return cuda_fail(e, "cudaMalloc saved pages");
+        }
+        if (c->d_saved) cudaFree(c->d_saved);
+        c->d_saved = fresh;
+        c->saved_slots = slots;
+    }
+    c->jr.saved = std::move(pages);
+    const cudaError_t e = copy_saved(c, false, st);
+    if (e == cudaSuccess) return PE_OK;
+    c->jr.saved.clear();  // nothing has changed yet
+    return cuda_fail(e, "page save launch");
 }
 
 // The copies-on-write of one append call that await their launch.
@@ -2468,6 +2555,7 @@ pe_status pe_append_kv(pe_cache *c, int32_t seq, const void *K, const void *V, i
         return fail(PE_ERR_OOM, "append needs %d pages, %zu free", pl.need, c->free_stack.size());
     pl.tok0 = 0;
     CallTxn tx(c, static_cast<cudaStream_t>(stream));
+    if (c->q8 && !one_append_launch({pl}) && (s = save_tails(c, {pl}, static_cast<cudaStream_t>(stream))) != PE_OK) return tx.end(s);
     return tx.end(apply_appends(c, {pl}, K, V, n_tokens, static_cast<cudaStream_t>(stream)));
 }
 
@@ -2499,6 +2587,8 @@ pe_status pe_append_kv_batch(pe_cache *c, int32_t n, const int32_t *seqs, const 
         return fail(PE_ERR_OOM, "batch append needs %lld pages, %zu free", static_cast<long long>(need),
                     c->free_stack.size());
     CallTxn tx(c, static_cast<cudaStream_t>(stream));
+    if (c->q8 && !one_append_launch(plans))
+        if (pe_status s = save_tails(c, plans, static_cast<cudaStream_t>(stream))) return tx.end(s);
     return tx.end(apply_appends(c, plans, K, V, total, static_cast<cudaStream_t>(stream)));
 }
 
@@ -2615,6 +2705,7 @@ pe_status pe_replay_rounds(pe_cache *c, int32_t n, const int32_t *seqs, int32_t 
 
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     CallTxn tx(c, st);
+    if ((s = save_tails(c, whole, st)) != PE_OK) return tx.end(s);
     const int64_t row_bytes = static_cast<int64_t>(num_q_heads) * c->cfg.head_dim * 2;  // one bf16 [Hq][d] row
     // A round's append may run beside the merge of the round before, which writes `out`.
     auto apart = [](const void *a, int64_t na, const void *b, int64_t nb) {

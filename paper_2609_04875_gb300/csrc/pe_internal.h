@@ -100,6 +100,18 @@ struct ReadParams {
     ReadSeg segs[kMaxSegs];
 };
 
+// Stored pages, codes and scales of all layers, copied out or back: a slot a page.
+constexpr int kMaxSavedPages = 512;    // of one launch
+struct SaveParams {
+    uint4 *k8, *v8;
+    int8_t *exps;
+    uint8_t *slots;        // page i: K codes [L][Hkv][ps][d], V codes, exponents [L][Hkv][2], from i * slot_bytes on
+    int64_t slot_bytes;
+    int32_t n, L, hkv, ps, d, num_pages;
+    int32_t back;          // 1: from the slots into the pages
+    int32_t pages[kMaxSavedPages];
+};
+
 // Attention of few rows on the codes (pe_q8_attn.cu, pe_q8_rows.cu): items are (sequence, kv-head, block of query rows).
 constexpr int kQ8MaxChunk = 14;        // key tiles (128 keys) of a chunk, and with blocks of rb rows:
 __host__ __device__ constexpr int q8_max_chunk(int rb) { return rb == 16 ? 12 : 14; }
@@ -383,6 +395,7 @@ cudaError_t launch_decode_attn(int head_dim, int rows_cap, bool tensor_core, con
 // 8-bit cache: p's pools hold codes, p.exps their scales, p.segs[].cum0 and p.seg_tokens count touched pages.
 cudaError_t launch_append_q8(int head_dim, const AppendParams &p, cudaStream_t st);
 cudaError_t launch_unpack_q8(const UnpackParams &p, int pages, cudaStream_t st);
+cudaError_t launch_save_pages(const SaveParams &p, cudaStream_t st);
 cudaError_t launch_read_kv(bool q8, const ReadParams &p, cudaStream_t st);
 // Eviction, in this order on one stream: select, then copy for each group of new pages, a table after each but the last,
 // whose pages finish enters.

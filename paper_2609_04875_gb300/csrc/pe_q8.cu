@@ -130,6 +130,33 @@ __global__ void __launch_bounds__(256) unpack_q8_kernel(const __grid_constant__ 
     }
 }
 
+// A block per page and layer.
+__global__ void __launch_bounds__(256) save_pages_kernel(const __grid_constant__ SaveParams p)
+{
+    ptx::griddep_wait();  // launched with programmatic serialization
+    ptx::griddep_launch_dependents();
+    const int l = static_cast<int>(blockIdx.y), n = p.hkv * p.ps * p.d / 16;
+    const int64_t head = (static_cast<int64_t>(l) * p.num_pages + p.pages[blockIdx.x]) * p.hkv;
+    uint4 *k = p.k8 + head * (p.ps * p.d / 16), *v = p.v8 + head * (p.ps * p.d / 16);
+    char2 *e = reinterpret_cast<char2 *>(p.exps) + head;
+    uint8_t *slot = p.slots + static_cast<int64_t>(blockIdx.x) * p.slot_bytes;
+    uint4 *sk = reinterpret_cast<uint4 *>(slot) + static_cast<int64_t>(l) * n, *sv = sk + static_cast<int64_t>(p.L) * n;
+    char2 *se = reinterpret_cast<char2 *>(slot + static_cast<int64_t>(p.L) * n * 32) + static_cast<int64_t>(l) * p.hkv;
+    for (int i = threadIdx.x; i < n; i += 256) {
+        if (p.back) {
+            k[i] = sk[i];
+            v[i] = sv[i];
+        } else {
+            sk[i] = k[i];
+            sv[i] = v[i];
+        }
+    }
+    for (int h = threadIdx.x; h < p.hkv; h += 256) {
+        if (p.back) e[h] = se[h];
+        else se[h] = e[h];
+    }
+}
+
 // One block per touched page and layer: its tokens' rows, kv-heads and chunks fastest, so that a warp writes contiguous
 // memory and reads whole rows.  (Eight codes a load, and so contiguous 16-byte stores, took 12 % more.)
 template <bool Q8>
@@ -218,6 +245,15 @@ cudaError_t launch_unpack_q8(const UnpackParams &p, int pages, cudaStream_t st)
     cudaLaunchConfig_t cfg = serial_config(static_cast<unsigned>(pages), 256, st, &attr);
     cfg.gridDim.y = static_cast<unsigned>((p.hkv * p.ps * p.d / 8 + 256 * kUnpackChunks - 1) / (256 * kUnpackChunks));
     return cudaLaunchKernelEx(&cfg, unpack_q8_kernel, p);
+}
+
+cudaError_t launch_save_pages(const SaveParams &p, cudaStream_t st)
+{
+    if (p.n <= 0) return cudaSuccess;
+    cudaLaunchAttribute attr;
+    cudaLaunchConfig_t cfg = serial_config(static_cast<unsigned>(p.n), 256, st, &attr);
+    cfg.gridDim.y = static_cast<unsigned>(p.L);
+    return cudaLaunchKernelEx(&cfg, save_pages_kernel, p);
 }
 
 cudaError_t launch_read_kv(bool q8, const ReadParams &p, cudaStream_t st)
