@@ -50,6 +50,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
     const float *w = p.weights + static_cast<int64_t>(sg.row) * p.weights_stride;
     int32_t *kept = p.kept + static_cast<int64_t>(sg.row) * p.kept_stride;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (p.done && threadIdx.x == 0) p.done[sg.row] = EvictDone{sg.seq, sg.len, sg.keep, 0};
     for (int j = sg.keep + static_cast<int>(threadIdx.x); j < p.kept_cols; j += kSelThreads) kept[j] = -1;
     if (sg.keep >= sg.len) {
         for (int j = threadIdx.x; j < sg.len; j += kSelThreads) kept[j] = j;
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(kQ8Block) evict_copy_kernel(const __grid_const
     }
 }
 
-// The table entries of a group of new pages, when more groups follow (their copies read the table, so they wait).
+// The table entries of a group of new pages, where there are several (their copies read the table, so they wait).
 __global__ void __launch_bounds__(256) evict_table_kernel(const __grid_constant__ EvictParams p)
 {
     ptx::griddep_wait();
@@ -248,8 +249,34 @@ __global__ void __launch_bounds__(256) evict_table_kernel(const __grid_constant_
     for (int i = threadIdx.x; i < sg.n_new; i += 256) p.page_table[sg.table_row + sg.first_lp + i] = p.new_pages[sg.new0 + i];
 }
 
-// One block per sequence, last of all: the table (with the entries of the last group), the length, and the weights:
-// kept[j] >= j, so taken some positions at a time in ascending order they move down in place.
+// A sequence's weights, the end of its table row and its length, last of all.  kept[j] >= j, so taken some positions at
+// a time in ascending order the weights move down in place.  (One block; all of its threads.)
+__device__ __forceinline__ void finish_sequence(float *w, const int32_t *kept, int32_t *table, int64_t *len_out, int len, int keep, int ps,
+                                                int log_ps)
+{
+    constexpr int kAt = 4;  // positions of a thread in flight
+    for (int j0 = 0; j0 < keep; j0 += kAt * kSelThreads) {
+        float x[kAt];
+#pragma unroll
+        for (int u = 0; u < kAt; ++u) {
+            const int j = j0 + u * kSelThreads + static_cast<int>(threadIdx.x);
+            x[u] = j < keep ? w[kept[j]] : 0.f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kAt; ++u) {
+            const int j = j0 + u * kSelThreads + static_cast<int>(threadIdx.x);
+            if (j < keep) w[j] = x[u];
+        }
+    }
+    __syncthreads();
+    for (int j = keep + static_cast<int>(threadIdx.x); j < len; j += kSelThreads) w[j] = 0.f;
+    const int now = (keep + ps - 1) >> log_ps, before = (len + ps - 1) >> log_ps;
+    for (int e = now + static_cast<int>(threadIdx.x); e < before; e += kSelThreads) table[e] = -1;
+    if (threadIdx.x == 0) *len_out = keep;
+}
+
+// One block per sequence of the only group, whose new pages it enters.
 template <typename Params>
 __global__ void __launch_bounds__(kSelThreads) evict_finish_kernel(const __grid_constant__ Params p)
 {
@@ -257,29 +284,22 @@ __global__ void __launch_bounds__(kSelThreads) evict_finish_kernel(const __grid_
     ptx::griddep_launch_dependents();
     const EvictSeg &sg = p.segs[blockIdx.x];
     if (sg.keep >= sg.len) return;
-    float *w = p.weights + static_cast<int64_t>(sg.row) * p.weights_stride;
-    const int32_t *kept = p.kept + static_cast<int64_t>(sg.row) * p.kept_stride;
     for (int i = threadIdx.x; i < sg.n_new; i += kSelThreads) p.page_table[sg.table_row + sg.first_lp + i] = p.new_pages[sg.new0 + i];
-    constexpr int kAt = 4;  // positions of a thread in flight
-    for (int j0 = 0; j0 < sg.keep; j0 += kAt * kSelThreads) {
-        float x[kAt];
-#pragma unroll
-        for (int u = 0; u < kAt; ++u) {
-            const int j = j0 + u * kSelThreads + static_cast<int>(threadIdx.x);
-            x[u] = j < sg.keep ? w[kept[j]] : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kAt; ++u) {
-            const int j = j0 + u * kSelThreads + static_cast<int>(threadIdx.x);
-            if (j < sg.keep) w[j] = x[u];
-        }
-    }
-    __syncthreads();
-    for (int j = sg.keep + static_cast<int>(threadIdx.x); j < sg.len; j += kSelThreads) w[j] = 0.f;
-    const int now = (sg.keep + p.ps - 1) >> p.log_ps;
-    for (int e = now + static_cast<int>(threadIdx.x); e < sg.old_n; e += kSelThreads) p.page_table[sg.table_row + e] = -1;
-    if (threadIdx.x == 0) p.seq_len[sg.seq] = sg.keep;
+    finish_sequence(p.weights + static_cast<int64_t>(sg.row) * p.weights_stride, p.kept + static_cast<int64_t>(sg.row) * p.kept_stride,
+                    p.page_table + sg.table_row, p.seq_len + sg.seq, sg.len, sg.keep, p.ps, p.log_ps);
+}
+
+// One block per sequence of the call, from the records that the selections left: a single launch, however many groups
+// there were, so that no sequence's weights move unless all do.
+__global__ void __launch_bounds__(kSelThreads) evict_finish_all_kernel(const __grid_constant__ EvictFinishParams p)
+{
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    const int row = static_cast<int>(blockIdx.x);
+    const EvictDone s = p.done[row];
+    if (s.keep >= s.len) return;
+    finish_sequence(p.weights + static_cast<int64_t>(row) * p.weights_stride, p.kept + static_cast<int64_t>(row) * p.kept_stride,
+                    p.page_table + static_cast<int64_t>(s.seq) * p.max_pages, p.seq_len + s.seq, s.len, s.keep, p.ps, p.log_ps);
 }
 
 cudaLaunchConfig_t serial_config(unsigned blocks, unsigned threads, size_t smem, cudaStream_t st, cudaLaunchAttribute *attr)
@@ -376,6 +396,13 @@ cudaError_t launch_evict_finish(const EvictParams &p, cudaStream_t st)
     const cudaLaunchConfig_t cfg = serial_config(static_cast<unsigned>(p.n), kSelThreads, 0, st, &attr);
     if (fits_small(p, true)) return cudaLaunchKernelEx(&cfg, evict_finish_kernel<Small>, small_of(p, true));
     return cudaLaunchKernelEx(&cfg, evict_finish_kernel<EvictParams>, p);
+}
+
+cudaError_t launch_evict_finish_all(const EvictFinishParams &p, cudaStream_t st)
+{
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = serial_config(static_cast<unsigned>(p.n), kSelThreads, 0, st, &attr);
+    return cudaLaunchKernelEx(&cfg, evict_finish_all_kernel, p);
 }
 
 }  // namespace pe

@@ -122,6 +122,7 @@ struct pe_cache {
     int8_t *exps = nullptr;       // scale exponents [L][num_pages][Hkv][2]
     uint8_t *d_saved = nullptr;   // contents of pages that the call in progress quantises again (save_tails)
     int64_t saved_slots = 0;      // pages that d_saved holds
+    EvictDone *d_evicted = nullptr;  // [max_seqs]: an eviction's records, by its rows
     bool own_pools = false;
     int32_t *d_table = nullptr;
     int64_t *d_len = nullptr;
@@ -392,6 +393,7 @@ void free_device(pe_cache *c)
     if (c->v8) cudaFree(c->v8);
     if (c->exps) cudaFree(c->exps);
     if (c->d_saved) cudaFree(c->d_saved);
+    if (c->d_evicted) cudaFree(c->d_evicted);
     if (c->d_table) cudaFree(c->d_table);
     if (c->d_len) cudaFree(c->d_len);
     if (c->d_status) cudaFree(c->d_status);
@@ -400,6 +402,7 @@ void free_device(pe_cache *c)
     c->k_pool = c->v_pool = c->k8 = c->v8 = nullptr;
     c->exps = nullptr;
     c->d_saved = nullptr;
+    c->d_evicted = nullptr;
     c->d_tickets = nullptr;
     c->d_table = nullptr;
     c->d_len = nullptr;
@@ -2339,6 +2342,7 @@ static pe_status create_cache(const pe_cache_config *cfg, bool q8, pe_cache **ou
             if ((st = encode_codes(&cc->tm_k8, cc->k8, c.head_dim, pool_rows, ps)) != PE_OK) break;
             if ((st = encode_codes(&cc->tm_v8, cc->v8, c.head_dim, pool_rows, ps)) != PE_OK) break;
         }
+        if ((e = cudaMalloc(&cc->d_evicted, sizeof(EvictDone) * c.max_seqs)) != cudaSuccess) { st = cuda_fail(e, "cudaMalloc"); break; }
         if ((e = cudaMalloc(&cc->d_table, table_bytes)) != cudaSuccess) { st = cuda_fail(e, "cudaMalloc page table"); break; }
         if ((e = cudaMemset(cc->d_table, 0xFF, table_bytes)) != cudaSuccess) { st = cuda_fail(e, "memset"); break; }
         if ((e = cudaMalloc(&cc->d_len, sizeof(int64_t) * c.max_seqs)) != cudaSuccess) { st = cuda_fail(e, "cudaMalloc"); break; }
@@ -3046,7 +3050,6 @@ static pe_status evict_batch(pe_cache *c, int32_t n, const int32_t *seqs, const 
         sg.keep = pl.keep;
         sg.sinks = sinks;
         sg.recent = recent;
-        sg.old_n = pl.old_n;
         return sg;
     };
     auto step = [&](const char *what, auto launch) -> pe_status {
@@ -3058,6 +3061,9 @@ static pe_status evict_batch(pe_cache *c, int32_t n, const int32_t *seqs, const 
         return PE_OK;
     };
     pe_status s = PE_OK;
+    // one group of sequences and new pages is the rule: it lists every sequence, and its entries come with the finish
+    const bool one_group = need <= kAppendMaxPages && plans.size() <= static_cast<size_t>(kMaxSegs);
+    p.done = one_group ? nullptr : c->d_evicted;
     for (size_t i = 0; i < plans.size(); i += kMaxSegs) {
         for (p.n = 0; p.n < kMaxSegs && i + p.n < plans.size(); ++p.n) p.segs[p.n] = seg_of(plans[i + p.n]);
         int32_t max_len = 0;
@@ -3065,9 +3071,7 @@ static pe_status evict_batch(pe_cache *c, int32_t n, const int32_t *seqs, const 
         if ((s = step("evict select", [&] { return launch_evict_select(p, max_len, st); })) != PE_OK) return tx.end(s);
     }
     // The copies, and after each group of new pages their table entries: a row moves from a position no lower than its
-    // own, so the entries replaced so far are none that a later group's copies read through.  One group is the rule: it
-    // lists every sequence, and its entries come with the finish.
-    const bool one_group = need <= kAppendMaxPages && plans.size() <= static_cast<size_t>(kMaxSegs);
+    // own, so the entries replaced so far are none that a later group's copies read through.
     p.n = p.n_new = 0;
     auto flush = [&]() -> pe_status {
         pe_status r = step("evict copy", [&] { return launch_evict_copy(c->q8, c->cfg.head_dim, p, st); });
@@ -3098,12 +3102,10 @@ static pe_status evict_batch(pe_cache *c, int32_t n, const int32_t *seqs, const 
         if (p.n > 0 && (s = step("evict finish", [&] { return launch_evict_finish(p, st); })) != PE_OK) return tx.end(s);
         return tx.end(PE_OK);
     }
-    p.n_new = 0;
-    for (size_t i = 0; i < plans.size(); i += kMaxSegs) {
-        for (p.n = 0; p.n < kMaxSegs && i + p.n < plans.size(); ++p.n) p.segs[p.n] = seg_of(plans[i + p.n]);
-        if ((s = step("evict finish", [&] { return launch_evict_finish(p, st); })) != PE_OK) return tx.end(s);
-    }
-    return tx.end(PE_OK);
+    // (a single step, the last: weights that moved for some sequences could not be put back if another's step failed)
+    const EvictFinishParams f{p.page_table, p.seq_len, weights, kept, c->d_evicted, weights_stride, kept_stride,
+                              static_cast<int32_t>(plans.size()), ps, p.log_ps, c->cfg.max_pages_per_seq};
+    return tx.end(step("evict finish", [&] { return launch_evict_finish_all(f, st); }));
 }
 
 pe_status pe_evict_batch(pe_cache *c, int32_t n, const int32_t *seqs, const int32_t *keep, int32_t sinks, int32_t recent,

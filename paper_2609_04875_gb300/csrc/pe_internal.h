@@ -157,9 +157,13 @@ struct EvictSeg {
     int32_t seq, table_row;
     int32_t len, keep;     // tokens before and after
     int32_t sinks, recent;
-    int32_t old_n;         // pages before
     int32_t first_lp;      // logical index of the first new page in this launch
     int32_t new0, n_new;   // this launch's new pages of the sequence, in new_pages
+};
+
+// What the finish of an eviction of several groups needs of a sequence: device memory, one a row of weights and kept.
+struct EvictDone {
+    int32_t seq, len, keep, pad_;
 };
 
 template <int SEGS, int PAGES>
@@ -170,12 +174,23 @@ struct EvictParamsT {
     int8_t *exps;          // 8-bit cache only
     float *weights;        // [rows][weights_stride]
     int32_t *kept;         // [rows][kept_stride]
+    EvictDone *done;       // null, or the rows' records (the selection writes them)
     int64_t weights_stride, kept_stride;
     int32_t n, L, hkv, ps, log_ps, num_pages, n_new, kept_cols;
     EvictSeg segs[SEGS];
     int32_t new_pages[PAGES];
 };
 using EvictParams = EvictParamsT<kMaxSegs, kAppendMaxPages>;
+
+struct EvictFinishParams {
+    int32_t *page_table;
+    int64_t *seq_len;
+    float *weights;
+    const int32_t *kept;
+    const EvictDone *done;
+    int64_t weights_stride, kept_stride;
+    int32_t n, ps, log_ps, max_pages;
+};
 
 // ---------------------------------------------------------------- accumulated weights
 struct WeightSeg {
@@ -397,12 +412,14 @@ cudaError_t launch_append_q8(int head_dim, const AppendParams &p, cudaStream_t s
 cudaError_t launch_unpack_q8(const UnpackParams &p, int pages, cudaStream_t st);
 cudaError_t launch_save_pages(const SaveParams &p, cudaStream_t st);
 cudaError_t launch_read_kv(bool q8, const ReadParams &p, cudaStream_t st);
-// Eviction, in this order on one stream: select, then copy for each group of new pages, a table after each but the last,
-// whose pages finish enters.
+// Eviction, in this order on one stream: select for each group of sequences, then copy for each group of new pages.  One
+// group: finish, which enters its pages; else a table after each copy and finish_all over all sequences, the only step
+// that changes their weights.
 cudaError_t launch_evict_select(const EvictParams &p, int max_len, cudaStream_t st);
 cudaError_t launch_evict_copy(bool q8, int head_dim, const EvictParams &p, cudaStream_t st);
 cudaError_t launch_evict_table(const EvictParams &p, cudaStream_t st);
 cudaError_t launch_evict_finish(const EvictParams &p, cudaStream_t st);
+cudaError_t launch_evict_finish_all(const EvictFinishParams &p, cudaStream_t st);
 // q_rows: query rows of the launch's sequences (consecutive from segs[0].q_row0).
 cudaError_t launch_weights(int head_dim, const WeightParams &p, int64_t q_rows, int max_keys, cudaStream_t st);
 // The same from scores and lse that launch_attn_q8 left.
