@@ -62,6 +62,7 @@ __global__ void __launch_bounds__(kLseThreads) weights_lse_kernel(const __grid_c
     float m = -INFINITY, l = 0.f;
     for (int key = threadIdx.x; key < n_keys; key += kLseThreads) {
         const float x = p.scale_log2 * dot_row<HD>(s_q, reinterpret_cast<const uint4 *>(p.k + key_row(p, sg, hq / p.group, key) * HD));
+        if (x == -INFINITY) continue;  // adds nothing (and -inf - -inf, before a thread's first other key, would be NaN)
         const float mn = x > m || x != x ? x : m;
         l = l * (m == -INFINITY ? 0.f : exp2f(m - mn)) + exp2f(x - mn);
         m = mn;
