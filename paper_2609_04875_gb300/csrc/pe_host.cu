@@ -1762,9 +1762,9 @@ pe_status run_attention(pe_cache *c, const std::vector<AttnItem> &items, int32_t
     return PE_OK;
 }
 
-// Pointers are only checked when the call has queries (an empty tensor may be null).
-// 8-bit cache: unpacks `layer` of the sequences' pages, so that the bf16 kernels can attend them as layer 0.
-pe_status unpack_layer(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer, cudaStream_t st)
+// 8-bit cache: unpacks `layer` of the n items' sequences' pages, so that the bf16 kernels can attend them as layer 0.
+// (Allocates nothing: the static-scratch call comes here.)
+pe_status unpack_layer(pe_cache *c, const AttnItem *items, size_t n, int32_t layer, cudaStream_t st)
 {
     UnpackParams p;
     std::memset(static_cast<void *>(&p), 0, offsetof(UnpackParams, segs));
@@ -1789,7 +1789,8 @@ pe_status unpack_layer(pe_cache *c, const std::vector<AttnItem> &items, int32_t 
         p.n = pages = 0;
         return PE_OK;
     };
-    for (const AttnItem &it : items) {
+    for (size_t i = 0; i < n; ++i) {
+        const AttnItem &it = items[i];
         if (it.n_q <= 0) continue;
         if (p.n == kMaxSegs)
             if (pe_status s = flush()) return s;
@@ -2026,7 +2027,7 @@ pe_status attend(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer,
         for (const Q8Item &it : left) many.push_back(AttnItem{it.seq, it.q_row0, it.n_q});
     }
     if (many.empty()) return PE_OK;
-    if (pe_status s = unpack_layer(c, many, layer, st)) return s;
+    if (pe_status s = unpack_layer(c, many.data(), many.size(), layer, st)) return s;
     return run_attention(c, many, 0, Q, q_rows, out, hq, scale, st);
 }
 
@@ -2196,7 +2197,7 @@ pe_status attend_with_weights(pe_cache *c, const std::vector<AttnItem> &items, i
     if (!many.empty() && (s = attend(c, many, layer, Q, q_rows, out, hq, scale, st)) != PE_OK) return s;
     many.clear();
     for (const Q8Item &it : whole) many.push_back(AttnItem{it.seq, it.q_row0, it.n_q});
-    if ((s = unpack_layer(c, many, layer, st)) != PE_OK) return s;
+    if ((s = unpack_layer(c, many.data(), many.size(), layer, st)) != PE_OK) return s;
     return add_weights(c, whole, 0, Q, hq, scale, weights, stride, st);
 }
 
@@ -2224,6 +2225,7 @@ struct EvictPlan {
     int32_t first, n_new, old_n;   // logical index of the first replaced page, pages popped, pages before
 };
 
+// Pointers are only checked when the call has queries (an empty tensor may be null).
 pe_status check_attn_args(const pe_cache *c, int32_t layer, const void *Q, const void *out, int32_t hq, float scale,
                           bool has_rows = true)
 {
@@ -2821,7 +2823,8 @@ pe_status pe_replay_attn_static_scratch(pe_cache *c, int32_t seq, int32_t layer,
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (c->q8) {
         p.layer = 0;
-        if ((s = unpack_layer(c, {AttnItem{seq, 0, n_q}}, layer, st)) != PE_OK) return s;
+        const AttnItem item{seq, 0, n_q};
+        if ((s = unpack_layer(c, &item, 1, layer, st)) != PE_OK) return s;
     }
     if (injected_failure(c)) return launch_fault("replay attention");
     e = launch_replay_attn(d, true, tm_q, c->tm_k, c->tm_v, tm_q, p, st);
