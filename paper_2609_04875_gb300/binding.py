@@ -228,6 +228,16 @@ def _dev_ptr(t, name, device=None):
     return ctypes.c_void_p(t.data_ptr())
 
 
+def _covers(seqs, vals, name, more=1):
+    """The library reads len(seqs) + more entries of a host array; the last of them, of offsets, bounds the rows it reads
+    (the tensors have vals[-1])."""
+    n = len(seqs)
+    if n and len(vals) < n + more:
+        raise ValueError(f"{name} has {len(vals)} entries, {n} sequences need {n + more}")
+    if n and more and vals[n] > vals[-1]:
+        raise ValueError(f"{name}[{n}] is past the last offset")
+
+
 def _same_shape(out, Q):
     if out is not None and out.shape != Q.shape and tuple(out.shape) != tuple(Q.shape):
         raise ValueError(f"out has shape {tuple(out.shape)}, Q {tuple(Q.shape)}: they must match")
@@ -380,6 +390,7 @@ class PagedKVCache:
         return list(buf[: n.value])
 
     def crop_batch(self, seqs, taus, stream=None):
+        _covers(seqs, taus, "taus", 0)
         _check(_lib.pe_crop_batch(self._h, len(seqs), _i32_array(seqs), _i64_array(taus), self._s(stream)))
 
     # -- append (prefill write) ------------------------------------------------
@@ -395,6 +406,7 @@ class PagedKVCache:
 
     def append_kv_batch(self, seqs, K=None, V=None, cu_tokens=None, stream=None):
         """K, V: CUDA bf16 [L][cu_tokens[-1]][Hkv][d]; sequence i gets tokens cu_tokens[i]:cu_tokens[i+1]."""
+        _covers(seqs, cu_tokens, "cu_tokens")
         cu = _i32_array(cu_tokens)
         if K is None:
             if not self.host_only:
@@ -430,6 +442,7 @@ class PagedKVCache:
 
     def replay_attn_batch(self, seqs, layer, Q, cu_q, out=None, softmax_scale=None, stream=None):
         """Q, out: CUDA bf16 [cu_q[-1]][Hq][d]; rows cu_q[i]:cu_q[i+1] are the last positions of seqs[i]."""
+        _covers(seqs, cu_q, "cu_q")
         shape = Q.shape
         if len(shape) != 3 or shape[2] != self.head_dim or shape[0] != cu_q[-1]:
             raise ValueError("Q must be [cu_q[-1]][Hq][d]")
@@ -446,6 +459,8 @@ class PagedKVCache:
         """replay_attn_batch, and each key's softmax weight, summed over the
         sequence's queries and q-heads, added to ``weights``: CUDA float32
         [len(seqs)][>= the longest length], columns contiguous."""
+        if len(cu_q) != len(seqs) + 1:
+            raise ValueError("cu_q must have an entry more than seqs")
         shape = Q.shape
         if len(shape) != 3 or shape[2] != self.head_dim or shape[0] != cu_q[-1]:
             raise ValueError("Q must be [cu_q[-1]][Hq][d]")
@@ -536,6 +551,7 @@ class PagedKVCache:
         n_rounds = int(take.shape[0]) if take.ndim == 2 else 0
         if take.size and take.shape[1] != len(seqs):
             raise ValueError("take must be [rounds][len(seqs)]")
+        _covers(seqs, cu_tok, "cu_tok")
         take_p = take.ctypes.data_as(_I32P) if take.size else None
         scale = 1.0 / math.sqrt(self.head_dim) if softmax_scale is None else float(softmax_scale)
         if self.host_only:
@@ -564,6 +580,7 @@ class PagedKVCache:
     # kept alive by the returned function; their contents may change between
     # calls, their storage may not.
     def prepare_crop_batch(self, seqs, taus, stream=None):
+        _covers(seqs, taus, "taus", 0)
         args = (self._h, len(seqs), _i32_array(seqs), _i64_array(taus), self._s(stream))
         fn = _lib.pe_crop_batch
 
@@ -574,6 +591,7 @@ class PagedKVCache:
         return call
 
     def prepare_append_kv_batch(self, seqs, K, V, cu_tokens, stream=None):
+        _covers(seqs, cu_tokens, "cu_tokens")
         self._check_kv(K, V)
         if K.shape[1] != cu_tokens[-1]:
             raise ValueError("K token count does not match cu_tokens")
@@ -590,6 +608,7 @@ class PagedKVCache:
         return call
 
     def prepare_replay_attn_batch(self, seqs, layer, Q, cu_q, out, softmax_scale=None, stream=None):
+        _covers(seqs, cu_q, "cu_q")
         if Q.dim() != 3 or Q.shape[2] != self.head_dim or Q.shape[0] != cu_q[-1] or out.shape != Q.shape:
             raise ValueError("Q and out must be [cu_q[-1]][Hq][d]")
         scale = 1.0 / math.sqrt(self.head_dim) if softmax_scale is None else float(softmax_scale)
