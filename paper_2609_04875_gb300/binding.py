@@ -335,6 +335,12 @@ class PagedKVCache:
             pass
         return _dev_ptr(t, name, self._device)
 
+    def _empty_like(self, t):
+        torch = self._torch
+        if torch is None:  # a host-only cache: the call is about to be refused for its tensors
+            import torch
+        return torch.empty_like(t)
+
     # -- sequences -----------------------------------------------------------
     def seq_create(self) -> int:
         s = ctypes.c_int32()
@@ -448,7 +454,7 @@ class PagedKVCache:
             raise ValueError("Q must be [cu_q[-1]][Hq][d]")
         _same_shape(out, Q)
         if out is None:
-            out = self._torch.empty_like(Q)
+            out = self._empty_like(Q)
         scale = self._default_scale if softmax_scale is None else float(softmax_scale)
         _check(_lib.pe_replay_attn_batch(self._h, len(seqs), _i32_array(seqs), layer, self._ptr(Q, "Q"),
                                          _i32_array(cu_q), self._ptr(out, "out"), shape[1], scale,
@@ -461,12 +467,14 @@ class PagedKVCache:
         [len(seqs)][>= the longest length], columns contiguous."""
         if len(cu_q) != len(seqs) + 1:
             raise ValueError("cu_q must have an entry more than seqs")
+        if self.host_only:
+            raise ValueError("attention on a host-only cache")
         shape = Q.shape
         if len(shape) != 3 or shape[2] != self.head_dim or shape[0] != cu_q[-1]:
             raise ValueError("Q must be [cu_q[-1]][Hq][d]")
         _same_shape(out, Q)
         if out is None:
-            out = self._torch.empty_like(Q)
+            out = self._empty_like(Q)
         scale = self._default_scale if softmax_scale is None else float(softmax_scale)
         ptr, stride = self._weights(weights, seqs)
         _check(_lib.pe_replay_attn_weights_batch(self._h, len(seqs), _i32_array(seqs), layer, self._ptr(Q, "Q"),
