@@ -335,11 +335,27 @@ class PagedKVCache:
             pass
         return _dev_ptr(t, name, self._device)
 
-    def _empty_like(self, t):
+    def _output(self, make, stream):
+        """make(): the tensor that a call writes on ``stream``.  Not the current stream's memory then: the allocator may
+        give out a block whose last use there is still to come.  And not reused before what the current stream has been
+        given to do with it by the time it is freed."""
+        if stream is None or self.host_only:
+            return make()
+        torch = self._torch
+        if not isinstance(stream, torch.cuda.Stream):
+            handle = int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
+            stream = (torch.cuda.ExternalStream(handle, device=self._torch_device) if handle
+                      else torch.cuda.default_stream(self._torch_device))
+        with torch.cuda.stream(stream):
+            t = make()
+        t.record_stream(torch.cuda.current_stream(self._torch_device))
+        return t
+
+    def _output_like(self, t, stream):
         torch = self._torch
         if torch is None:  # a host-only cache: the call is about to be refused for its tensors
             import torch
-        return torch.empty_like(t)
+        return self._output(lambda: torch.empty_like(t), stream)
 
     # -- sequences -----------------------------------------------------------
     def seq_create(self) -> int:
@@ -435,12 +451,11 @@ class PagedKVCache:
     # -- replay attention ------------------------------------------------------
     def replay_attn(self, seq, layer, Q, out=None, softmax_scale=None, stream=None):
         """Attention of the last Q.shape[0] positions of ``seq``; Q, out: CUDA bf16 [n_q][Hq][d]."""
-        import torch
         if Q.dim() != 3 or Q.shape[2] != self.head_dim:
             raise ValueError("Q must be [n_q][Hq][d]")
         _same_shape(out, Q)
         if out is None:
-            out = torch.empty_like(Q)
+            out = self._output_like(Q, stream)
         scale = 1.0 / math.sqrt(self.head_dim) if softmax_scale is None else float(softmax_scale)
         _check(_lib.pe_replay_attn(self._h, seq, layer, self._ptr(Q, "Q"), self._ptr(out, "out"), Q.shape[0],
                                    Q.shape[1], scale, self._s(stream)))
@@ -454,7 +469,7 @@ class PagedKVCache:
             raise ValueError("Q must be [cu_q[-1]][Hq][d]")
         _same_shape(out, Q)
         if out is None:
-            out = self._empty_like(Q)
+            out = self._output_like(Q, stream)
         scale = self._default_scale if softmax_scale is None else float(softmax_scale)
         _check(_lib.pe_replay_attn_batch(self._h, len(seqs), _i32_array(seqs), layer, self._ptr(Q, "Q"),
                                          _i32_array(cu_q), self._ptr(out, "out"), shape[1], scale,
@@ -474,7 +489,7 @@ class PagedKVCache:
             raise ValueError("Q must be [cu_q[-1]][Hq][d]")
         _same_shape(out, Q)
         if out is None:
-            out = self._empty_like(Q)
+            out = self._output_like(Q, stream)
         scale = self._default_scale if softmax_scale is None else float(softmax_scale)
         ptr, stride = self._weights(weights, seqs)
         _check(_lib.pe_replay_attn_weights_batch(self._h, len(seqs), _i32_array(seqs), layer, self._ptr(Q, "Q"),
@@ -513,9 +528,9 @@ class PagedKVCache:
             raise ValueError("begins and cu_tokens must match seqs")
         if self.host_only:
             raise ValueError("a host-only cache holds no K and V")
-        K = self._torch.empty((self.num_layers, cu_tokens[-1], self.num_kv_heads, self.head_dim), dtype=self._bf16,
-                              device=self._torch_device)
-        V = self._torch.empty_like(K)
+        shape = (self.num_layers, cu_tokens[-1], self.num_kv_heads, self.head_dim)
+        K, V = [self._output(lambda: self._torch.empty(shape, dtype=self._bf16, device=self._torch_device), stream)
+                for _ in range(2)]
         _check(_lib.pe_read_kv_batch(self._h, len(seqs), _i32_array(seqs), _i64_array(begins), _i32_array(cu_tokens),
                                      K.data_ptr(), V.data_ptr(), self._s(stream)))
         return K, V
@@ -539,7 +554,8 @@ class PagedKVCache:
         int32 = self._torch.int32
         w, w_stride = self._weights(weights, seqs)
         if kept is None:
-            kept = self._torch.empty((len(seqs), max(0, *keep) if len(keep) else 0), dtype=int32, device=self._torch_device)
+            shape = (len(seqs), max(0, *keep) if len(keep) else 0)
+            kept = self._output(lambda: self._torch.empty(shape, dtype=int32, device=self._torch_device), stream)
         k, k_stride = self._rows(kept, "kept", int32, len(seqs))
         if k_stride != kept.shape[1]:
             raise ValueError("kept must be contiguous")
@@ -554,7 +570,6 @@ class PagedKVCache:
         [L][N][Hq][d]; agent i owns rows cu_tok[i]:cu_tok[i+1].  Host-only
         caches take no tensors (bookkeeping only)."""
         import numpy as np
-        import torch
         take = np.ascontiguousarray(take, dtype=np.int32)
         n_rounds = int(take.shape[0]) if take.ndim == 2 else 0
         if take.size and take.shape[1] != len(seqs):
@@ -574,7 +589,7 @@ class PagedKVCache:
             raise ValueError("K row count does not match cu_tok")
         _same_shape(out, Q)
         if out is None:
-            out = torch.empty_like(Q)
+            out = self._output_like(Q, stream)
         _check(_lib.pe_replay_rounds(self._h, len(seqs), _i32_array(seqs), n_rounds, take_p, _i32_array(cu_tok),
                                      self._ptr(K, "K"), self._ptr(V, "V"), self._ptr(Q, "Q"), self._ptr(out, "out"),
                                      Q.shape[2], scale, self._s(stream)))
@@ -635,12 +650,11 @@ class PagedKVCache:
     def replay_attn_static_scratch(self, seq, layer, Q, out=None, softmax_scale=None, stream=None):
         """pe_replay_attn_static_scratch: split-KV replay attention whose partials
         live in the library's fixed device array (the call allocates nothing)."""
-        import torch
         if Q.dim() != 3 or Q.shape[2] != self.head_dim:
             raise ValueError("Q must be [n_q][Hq][d]")
         _same_shape(out, Q)
         if out is None:
-            out = torch.empty_like(Q)
+            out = self._output_like(Q, stream)
         scale = 1.0 / math.sqrt(self.head_dim) if softmax_scale is None else float(softmax_scale)
         _check(_lib.pe_replay_attn_static_scratch(self._h, seq, layer, self._ptr(Q, "Q"), self._ptr(out, "out"),
                                                   Q.shape[0], Q.shape[1], scale, self._s(stream)))
