@@ -199,9 +199,9 @@ pe_status pe_replay_attn_batch(pe_cache *cache, int32_t n, const int32_t *seqs, 
  * of weights_stride >= the sequence's length entries; entries past the length
  * and rows of sequences without queries are not touched.  Held and summed in
  * 32 bits, in an order that does not depend on timing.  `out` as in
- * pe_replay_attn_batch.  weights must not overlap Q or out.
+ * pe_replay_attn_batch.  Q, out and the rows of weights must not overlap.
  * Errors: those of pe_replay_attn_batch; INVALID (weights null or not 4-byte
- * aligned), RANGE (weights_stride below a length; n_q x num_q_heads x 4 bytes
+ * aligned, overlapping tensors), RANGE (weights_stride below a length; n_q x num_q_heads x 4 bytes
  * above the cache's workspace). */
 pe_status pe_replay_attn_weights_batch(pe_cache *cache, int32_t n, const int32_t *seqs, int32_t layer,
                                        const void *Q_packed, const int32_t *cu_q, void *out, int32_t num_q_heads,

@@ -177,6 +177,13 @@ pe_status check_device(const pe_cache *c)
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Whether na bytes from a and nb from b have none in common.
+bool apart(const void *a, int64_t na, const void *b, int64_t nb)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x + static_cast<uint64_t>(na) <= y || y + static_cast<uint64_t>(nb) <= x;
+}
+
 // A saved page's slot: its codes and scale exponents of all layers.
 int64_t saved_page_bytes(const pe_cache *c)
 {
@@ -2643,6 +2650,15 @@ static pe_status attn_weights_batch(pe_cache *c, int32_t n, const int32_t *seqs,
         if (it.n_q > 0 && c->len[it.seq] > weights_stride)
             return fail(PE_ERR_RANGE, "sequence %d: its length %lld exceeds weights_stride %lld", it.seq,
                         static_cast<long long>(c->len[it.seq]), static_cast<long long>(weights_stride));
+    // Q is read again, for the weights, after out is written; and the weights of a sequence grow in several steps
+    const int64_t q_bytes = static_cast<int64_t>(cu_q[n]) * num_q_heads * c->cfg.head_dim * 2;
+    if (!apart(Q_packed, q_bytes, out, q_bytes)) return fail(PE_ERR_INVALID, "out overlaps Q");
+    for (int32_t i = 0; i < n; ++i) {
+        const float *row = weights + i * weights_stride;
+        const int64_t bytes = c->len[seqs[i]] * 4;
+        if (items[i].n_q > 0 && !(apart(row, bytes, Q_packed, q_bytes) && apart(row, bytes, out, q_bytes)))
+            return fail(PE_ERR_INVALID, "weights overlap Q or out");
+    }
     if (static_cast<int64_t>(cu_q[n]) * num_q_heads * 4 > c->ws_bytes)
         return fail(PE_ERR_RANGE, "the query rows' log-sum-exp exceed the workspace");
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -2714,10 +2730,6 @@ pe_status pe_replay_rounds(pe_cache *c, int32_t n, const int32_t *seqs, int32_t 
     if ((s = save_tails(c, whole, st)) != PE_OK) return tx.end(s);
     const int64_t row_bytes = static_cast<int64_t>(num_q_heads) * c->cfg.head_dim * 2;  // one bf16 [Hq][d] row
     // A round's append may run beside the merge of the round before, which writes `out`.
-    auto apart = [](const void *a, int64_t na, const void *b, int64_t nb) {
-        const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-        return x + static_cast<uint64_t>(na) <= y || y + static_cast<uint64_t>(nb) <= x;
-    };
     const int64_t out_bytes = c->cfg.num_layers * N * row_bytes;
     const int64_t kv_bytes = static_cast<int64_t>(c->cfg.num_layers) * N * c->cfg.num_kv_heads * c->cfg.head_dim * 2;
     const bool out_apart = apart(out, out_bytes, K, kv_bytes) && apart(out, out_bytes, V, kv_bytes);
