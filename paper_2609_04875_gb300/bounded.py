@@ -1,5 +1,5 @@
 """Agents with bounded sessions: K and V in 8 bits, an account of every key's softmax weight, and eviction when a session
-passes its budget.  Forget requests still work: the driver keeps each held token's original position.
+passes its budget.  A forget request names a position of the whole session: the driver keeps each held token's.
 
     python -m paper_2609_04875_gb300.bounded        # a short synthetic run, one GPU
 
@@ -7,6 +7,11 @@ One step of every agent is: append its token to all layers, attend it layer by l
 to the agent's account), and, once a session is longer than ``budget + slack``, come down to ``budget`` tokens: the
 first ``sinks``, the last ``recent`` and the ones that drew the most weight.  So the cache of an agent never holds more
 than ``budget + slack + 1`` tokens, whatever its session's length.
+
+A forget request leaves no held token, no later position and nothing in the account of the forgotten turns, so what is
+evicted from then on does not depend on them.  Two traces stay.  Tokens that were evicted while the forgotten turns were
+there, for want of the weight that those drew to others, do not come back.  And kept tokens that share the last page with
+forgotten ones stay rounded to a scale that those may have set; a request on a page's end has no such tokens.
 """
 from __future__ import annotations
 
@@ -70,16 +75,26 @@ class BoundedAgents:
 
     def forget(self, agent, tau):
         """Crops the agent to the held tokens that stood before position tau (1-based) of its whole session; returns how
-        many those are.  Their K and V may be replayed from there."""
+        many those are.  Their K and V may be replayed from there.  The account starts anew, since the forgotten turns'
+        queries are in every key's sum (recount fills it from the kept ones)."""
         if not 1 <= tau <= self.seen[agent] + 1:
             raise ValueError("tau outside the session")
         held = self.lengths()[agent]
         keep = int((self.origin[agent, :held] < tau - 1).sum())  # (positions ascend: eviction keeps the order)
         self.cache.crop(self.seqs[agent], keep + 1)
-        self.weights[agent, keep:] = 0
+        self.weights[agent] = 0
         self.origin[agent, keep:] = -1
         self.seen[agent] = tau - 1
         return keep
+
+    def recount(self, agent, Q):
+        """The agent's account from its held tokens' queries alone, Q bf16 [L][held][Hq][d]."""
+        held = self.lengths()[agent]
+        if tuple(Q.shape) != (self.layers, held, self.hq, self.cache.head_dim):
+            raise ValueError(f"Q must be [{self.layers}][{held}][{self.hq}][{self.cache.head_dim}]")
+        self.weights[agent] = 0
+        for layer in range(self.layers if held else 0):
+            self.cache.replay_attn_weights_batch([self.seqs[agent]], layer, Q[layer], [0, held], self.weights[agent: agent + 1])
 
 
 def main():
@@ -105,6 +120,7 @@ def main():
     print("after 300 steps:", b.lengths(), f"{start.elapsed_time(end) / 300 * 1e3:.0f} us a step of {agents} agents x {layers} layers")
     kept = b.forget(2, 2900)
     print("agent 2 forgets from position 2900 on:", kept, "tokens held before it")
+    b.recount(2, tokens([kept])[2])  # (a program has the kept tokens' queries from their replay)
     b.append(*tokens([1] * agents))
     assert b.cache.device_status() == 0
 
