@@ -101,7 +101,11 @@ pe_status pe_cache_create(const pe_cache_config *cfg, pe_cache **out);
  * code * 2^e, code = x * 2^-e rounded to e4m3, nearest, ties to even.
  * Every call takes and gives bf16 as before and keeps its meaning on the values
  * held.  Appending to a partly filled page quantises that page again from its
- * kept values and the new tokens.  e4m3 has no infinity: a token whose K or V
+ * kept values and the new tokens.  So what is held depends on what shared a
+ * page: tokens that a crop inside a page keeps stay rounded to a scale that the
+ * removed tokens may have set, and differ then from a session that never held
+ * those.  A crop to a page's end leaves no such trace; for one inside a page,
+ * crop to the page's start and append its kept tokens again.  e4m3 has no infinity: a token whose K or V
  * holds an infinity or NaN for a kv-head is held as NaN there, and every query
  * row that sees it gets NaN; rows that do not see it are not affected.
  * k_pool and v_pool must be NULL (INVALID otherwise).  Device memory: half of
@@ -125,6 +129,8 @@ pe_status pe_seq_release(pe_cache *cache, int32_t seq, void *stream);
  * last reference goes is pushed on the free list.  The device table entries
  * are set to -1 by a kernel on `stream`.  Resets the recomputation counter to
  * 0 and drops checkpoints past the new length.  tau = len+1 keeps every token.
+ * On an 8-bit cache the kept tokens of a page cut inside keep the rounding that
+ * the page had (pe_cache_create_q8).
  * freed_out (host, nullable) receives the pages returned to the free list in
  * ascending logical order; n_freed (nullable) their number.
  * Errors: INVALID (tau < 1, unknown seq), RANGE (tau-1 > len, freed_cap too small). */
