@@ -204,10 +204,14 @@ pe_status pe_replay_attn_batch(pe_cache *cache, int32_t n, const int32_t *seqs, 
  * weight (0 for a query that does not see the key).  weights: device fp32, rows
  * of weights_stride >= the sequence's length entries; entries past the length
  * and rows of sequences without queries are not touched.  Held and summed in
- * 32 bits, in an order that does not depend on timing.  `out` as in
- * pe_replay_attn_batch.  Q, out and the rows of weights must not overlap.
- * Errors: those of pe_replay_attn_batch; INVALID (weights null or not 4-byte
- * aligned, overlapping tensors), RANGE (weights_stride below a length; n_q x num_q_heads x 4 bytes
+ * 32 bits, in an order that does not depend on timing.  `out` has the meaning
+ * that it has in pe_replay_attn_batch, though not always the same bits: an
+ * 8-bit cache may attend on the codes in one call and by way of the unpacked
+ * layer in the other, which round differently.  Q, out and the rows of weights
+ * must not overlap.
+ * Errors: those of pe_replay_attn_batch (after CUDA the weights may hold a part
+ * of the call's sums); INVALID (weights null or not 4-byte aligned, overlapping
+ * tensors), RANGE (weights_stride below a length; n_q x num_q_heads x 4 bytes
  * above the cache's workspace). */
 pe_status pe_replay_attn_weights_batch(pe_cache *cache, int32_t n, const int32_t *seqs, int32_t layer,
                                        const void *Q_packed, const int32_t *cu_q, void *out, int32_t num_q_heads,
@@ -241,8 +245,8 @@ pe_status pe_read_kv_batch(pe_cache *cache, int32_t n, const int32_t *seqs, cons
  * an 8-bit cache quantises each new page from the values it receives.
  * Checkpoints past the sinks are dropped; the recomputation counter stays.
  * Everything runs on `stream`, without a wait for the device.  All-or-nothing,
- * a sequence may appear once.  On a host-only cache only the bookkeeping runs
- * (weights and kept unused).
+ * a sequence may appear once; weights and kept must not overlap.  On a
+ * host-only cache only the bookkeeping runs (weights and kept unused).
  * Errors: INVALID (unknown or repeated sequence, negative keep / sinks / recent,
  * sinks + recent above a keep[i] < T, null or misaligned weights or kept), RANGE
  * (a stride too small), OOM, CUDA (the weights are then as before, kept is

@@ -1832,8 +1832,8 @@ int64_t q8_rows(const AttnItem &it, int g) { return static_cast<int64_t>(it.n_q)
 
 // Whether a sequence's rows (n_q x group a kv-head) are attended on the codes, or by way of the unpacked layer; keys: of all
 // of the call's sequences of 33 to 128 rows.  On the codes every block of up to 128 rows goes through the keys again (in
-// L2); unpacking costs once 5 bytes a code and then HBM's time for bf16.  GPU time in us, codes / unpacked, 8 kv-heads, d =
-// 128: 32 rows on 600 keys 9.1 / 10.0, on 32k 23 / 59; 64 rows on 600 10.7 / 10.2, on 2000 12.5 / 11.6, on 4000 13.5 / 14.8
+// L2); unpacking costs once 5 bytes a code and then HBM's time for bf16.  How many kv-heads there are, and so how many
+// chunks, is not weighed.  GPU time in us, codes / unpacked, 8 kv-heads, d = 128: 32 rows on 600 keys 9.1 / 10.0, on 32k 23 / 59; 64 rows on 600 10.7 / 10.2, on 2000 12.5 / 11.6, on 4000 13.5 / 14.8
 // (8 sequences 32 / 58), on 32k 26 / 60 (8: 145 / 415); 128 rows on 4000 17.5 / 15.0 (8: 47 / 60), on 8192 20.9 / 18.9 (8: 69 /
 // 117), on 32k 37 / 61; 256 on 8192 30.6 / 22.8 (8: 122 / 131), on 32k 71 / 66.  d = 64, half the bytes for the same scores:
 // 64 rows on 600 8.4 / 9.6, on 32k 23 / 33; 128 on 8192 17.4 / 16.5 (8: 56 / 63), on 32k 32.2 / 34.3, 8 sequences of 4000

@@ -130,7 +130,8 @@ __global__ void __launch_bounds__(256) unpack_q8_kernel(const __grid_constant__ 
     }
 }
 
-// A block per page and layer.
+// A block per page and layer.  Bound by memory: 32 pages of 32 layers and 8 kv-heads of 16 x 128, 34 MB read and written, add
+// 8 us to a call of rounds.
 __global__ void __launch_bounds__(256) save_pages_kernel(const __grid_constant__ SaveParams p)
 {
     ptx::griddep_wait();  // launched with programmatic serialization

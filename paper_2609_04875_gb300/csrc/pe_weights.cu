@@ -2,8 +2,9 @@
 // queries i of w_ij^h, w = softmax(scale q_i^h K^T)_j, for the queries of one
 // attention call.  Two passes over K (bf16): the log-sum-exp of every query row,
 // then, one thread per key, the sum of its weights over the rows in a fixed
-// order (nothing is added atomically).  That is the form for bf16 caches; 8-bit
-// caches take it only for what does not fit their workspace:
+// order (nothing is added atomically).  That is the form for bf16 caches, and on
+// an 8-bit cache for what does not fit its workspace or is kept off the codes by
+// an option.  Otherwise 8-bit caches take one of two others:
 //   - few rows: the attention keeps its scores, which are summed here;
 //   - more rows: the scores are computed again on the tensor cores
 //     (weights_q8_kernel), from the codes and the attention's log-sum-exp.
