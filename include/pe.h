@@ -180,6 +180,51 @@ pe_status pe_append_kv(pe_cache *cache, int32_t seq, const void *K, const void *
 pe_status pe_append_kv_batch(pe_cache *cache, int32_t n, const int32_t *seqs, const void *K_packed,
                              const void *V_packed, const int32_t *cu_tokens, void *stream);
 
+/* A position rotation (rotary embedding).  Pair i of a head's columns, (i, i +
+ * n_pairs) or, interleaved, (2i, 2i + 1), turns by the angle freq[i] * position:
+ *   a' = scale (a cos - b sin),  b' = scale (b cos + a sin)
+ * in 32 bits, rounded once.  Columns from 2 n_pairs on stay as they are.  The
+ * position is the token's on axis axis[i] (time, height, width, ...).  Angles
+ * are taken modulo a full turn in 64-bit integers, so far positions lose no
+ * precision.  Kept by the caller; read inside the call only. */
+typedef struct {
+    int32_t n_pairs;            /* 1 .. head_dim / 2 */
+    int32_t interleaved;        /* 0: pairs (i, i + n_pairs); 1: neighbours */
+    int32_t n_axes;             /* 1 .. 8 */
+    float scale;                /* 1: a rotation alone */
+    const double *freq;         /* host [n_pairs]: radians per position, finite */
+    const int32_t *axis;        /* host [n_pairs], nullable: every pair on axis 0 */
+} pe_rope;
+
+/* pe_append_kv_batch from projections that are not rotated yet: K is rotated on
+ * its way into the pages, V goes in as it is, and Q (nullable; device bf16
+ * [L][cu_tokens[n]][num_q_heads][d], the same tokens' queries, any number of
+ * heads) is rotated into Q_out (the same shape; may be Q).  A bf16 cache holds K
+ * rotated and rounded once; an 8-bit cache quantises the value that the rotation
+ * gives in 32 bits.  (A K so large that its rotation leaves fp32's range is an
+ * infinity there.)  positions: device int32 [n_axes][cu_tokens[n]], any values,
+ * or NULL: the positions that the tokens get in their sequences, on every axis.
+ * What the cache holds does not turn again: a sequence whose positions change
+ * (eviction, crops of middle parts) goes on with positions of the caller's.
+ * On a host-only cache only the bookkeeping runs (tensors unused).
+ * Errors: those of pe_append_kv_batch; INVALID (a bad rotation, null or
+ * misaligned Q_out or positions, Q_out that overlaps K, V or a part of Q). */
+pe_status pe_append_kv_rope_batch(pe_cache *cache, int32_t n, const int32_t *seqs, const void *K_packed,
+                                  const void *V_packed, const int32_t *cu_tokens, const pe_rope *rope,
+                                  const int32_t *positions, const void *Q_packed, void *Q_out, int32_t num_q_heads,
+                                  void *stream);
+
+/* The same rotation of one tensor alone: rows [cu_tokens[i], cu_tokens[i+1]) of
+ * X, device bf16 [num_layers][cu_tokens[n]][num_heads][d] (any number of layers
+ * and heads; d of the cache), into out (the same shape; may be X).  positions as
+ * above; NULL: the rows of sequence i are its last positions, as in
+ * pe_replay_attn_batch.  A sequence may appear more than once.  The cache is
+ * not changed.  Errors: INVALID, RANGE (without positions: more rows than the
+ * sequence has), UNSUPPORTED (host-only cache), CUDA. */
+pe_status pe_rotate_batch(pe_cache *cache, int32_t n, const int32_t *seqs, const void *X_packed, const int32_t *cu_tokens,
+                          void *out, int32_t num_layers, int32_t num_heads, const pe_rope *rope,
+                          const int32_t *positions, void *stream);
+
 /* Replay attention (Alg. 1 replay loop; Sec. 3.2 prefill on the cropped cache).
  * The n_q queries are the LAST n_q positions of `seq`: query i sits at
  * position len-n_q+i and attends keys 0..len-n_q+i of `layer` (causal,
@@ -216,6 +261,30 @@ pe_status pe_replay_attn_batch(pe_cache *cache, int32_t n, const int32_t *seqs, 
 pe_status pe_replay_attn_weights_batch(pe_cache *cache, int32_t n, const int32_t *seqs, int32_t layer,
                                        const void *Q_packed, const int32_t *cu_q, void *out, int32_t num_q_heads,
                                        float softmax_scale, float *weights, int64_t weights_stride, void *stream);
+
+/* Differential attention of the last positions of n sequences (rows, lengths and
+ * causal alignment as in pe_replay_attn_batch).  Heads 2i and 2i + 1 of Q are
+ * the two maps of head i, and kv-heads 2j and 2j + 1, j = i / (Hq/Hkv), hold
+ * their keys and, side by side, the values [V_2j | V_2j+1] of width 2d that
+ * both maps weigh:
+ *   A_m = softmax(softmax_scale * q_{2i+m} K_{2j+m}^T),  O = (A_0 - lambda[i] A_1) V
+ *   out = gain O / sqrt(mean(O^2) + eps) over the head's 2d columns
+ * lambda: device fp32 [Hq / 2].  gain: device fp32 [2d] (what the model
+ * multiplies the norm by, 1 - lambda_init included), or NULL: out = O.  eps >= 0.
+ * Q: device bf16 [cu_q[n]][Hq][d]; out: device bf16 [cu_q[n]][Hq / 2][2d], which
+ * must not overlap Q, lambda or gain.  Sums, maxima and the norm in 32 bits, in
+ * an order that does not depend on timing; weights rounded to bf16, as in
+ * pe_replay_attn_batch.  A map none of whose scores is above -infinity counts as
+ * zero.  Keys that a row does not see do not reach it, whatever they hold; an
+ * infinity or NaN among those it sees makes outputs infinite or NaN.
+ * 8-bit caches attend by way of the unpacked layer.
+ * Errors: those of pe_replay_attn_batch; UNSUPPORTED (an odd number of
+ * kv-heads), INVALID (null or misaligned lambda, misaligned gain, eps negative
+ * or not finite, overlapping tensors), RANGE (a workspace too small for the
+ * smallest launch's partials). */
+pe_status pe_diff_attn_batch(pe_cache *cache, int32_t n, const int32_t *seqs, int32_t layer, const void *Q_packed,
+                             const int32_t *cu_q, void *out, int32_t num_q_heads, float softmax_scale,
+                             const float *lambda, const float *gain, float eps, void *stream);
 
 /* The values the cache holds: tokens [begins[i], begins[i] + cu_tokens[i+1] -
  * cu_tokens[i]) of sequence i into rows [cu_tokens[i], cu_tokens[i+1]) of

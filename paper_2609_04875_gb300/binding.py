@@ -34,6 +34,7 @@ EXPORTED = [
     "pe_prov_locate_source", "pe_prov_taint_closure", "pe_prov_first_entry", "pe_replay_schedule",
     "pe_replay_rounds", "pe_attn_plan_persistent", "pe_attn_plan_launches", "pe_last_error", "pe_version",
     "pe_cache_create_q8", "pe_cache_scales", "pe_read_kv_batch", "pe_replay_attn_weights_batch", "pe_evict_batch",
+    "pe_append_kv_rope_batch", "pe_rotate_batch", "pe_diff_attn_batch",
 ]
 
 # Turn kinds and replay policies of pe_replay_schedule (pe.h).
@@ -55,6 +56,13 @@ class _Config(ctypes.Structure):
         ("max_pages_per_seq", ctypes.c_int32), ("host_only", ctypes.c_int32),
         ("init_free_order", ctypes.POINTER(ctypes.c_int32)), ("k_pool", ctypes.c_void_p),
         ("v_pool", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [
+        ("n_pairs", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("freq", ctypes.POINTER(ctypes.c_double)), ("axis", ctypes.POINTER(ctypes.c_int32)),
     ]
 
 
@@ -107,6 +115,9 @@ _sigs = {
     "pe_read_kv_batch": [_P, _I32, _I32P, _I64P, _I32P, _P, _P, _P],
     "pe_replay_attn_weights_batch": [_P, _I32, _I32P, _I32, _P, _I32P, _P, _I32, ctypes.c_float, _P, _I64, _P],
     "pe_evict_batch": [_P, _I32, _I32P, _I32P, _I32, _I32, _P, _I64, _P, _I64, _P],
+    "pe_append_kv_rope_batch": [_P, _I32, _I32P, _P, _P, _I32P, ctypes.POINTER(_Rope), _P, _P, _P, _I32, _P],
+    "pe_rotate_batch": [_P, _I32, _I32P, _P, _I32P, _P, _I32, _I32, ctypes.POINTER(_Rope), _P, _P],
+    "pe_diff_attn_batch": [_P, _I32, _I32P, _I32, _P, _I32P, _P, _I32, ctypes.c_float, _P, _P, ctypes.c_float, _P],
     "pe_attn_plan_launches": [_P, _I32, _I32P, _I32P, _I32, _I32, _I64P, _I64, _I64P],
 }
 for _name, _args in _sigs.items():
@@ -238,9 +249,27 @@ def _covers(seqs, vals, name, more=1):
         raise ValueError(f"{name}[{n}] is past the last offset")
 
 
-def _same_shape(out, Q):
+def _same_shape(out, Q, name="out", like="Q"):
     if out is not None and out.shape != Q.shape and tuple(out.shape) != tuple(Q.shape):
-        raise ValueError(f"out has shape {tuple(out.shape)}, Q {tuple(Q.shape)}: they must match")
+        raise ValueError(f"{name} has shape {tuple(out.shape)}, {like} {tuple(Q.shape)}: they must match")
+
+
+class Rope:
+    """A position rotation (pe_rope): ``freq[i]``, in radians per position, turns pair i of a head's columns, (i, i +
+    len(freq)) or, ``interleaved``, (2i, 2i + 1).  ``axis[i]``: the axis of positions that pair i follows (time,
+    height, width, ...; all 0 by default).  ``scale`` multiplies the rotated columns.  Columns past the pairs stay."""
+
+    def __init__(self, freq, axis=None, interleaved=False, scale=1.0):
+        freq = [float(f) for f in freq]
+        if axis is not None and len(axis) != len(freq):
+            raise ValueError("axis must name one axis for each frequency")
+        self.n_pairs = len(freq)
+        self.n_axes = 1 if axis is None or not len(axis) else int(max(axis)) + 1
+        self._freq = (ctypes.c_double * max(1, len(freq)))(*freq)
+        self._axis = None if axis is None else i32_array(axis)
+        self._c = _Rope(self.n_pairs, 1 if interleaved else 0, self.n_axes, float(scale), self._freq,
+                        None if axis is None else ctypes.cast(self._axis, _I32P))
+        self._ref = ctypes.byref(self._c)
 
 
 class PagedKVCache:
@@ -448,6 +477,86 @@ class PagedKVCache:
         if shape[0] != self.num_layers or shape[2] != self.num_kv_heads or shape[3] != self.head_dim:
             raise ValueError(f"K shape {tuple(shape)} does not match the cache")
 
+    # -- position rotation -----------------------------------------------------
+    def append_kv_rope_batch(self, seqs, K=None, V=None, cu_tokens=None, rope=None, Q=None, positions=None, Q_out=None,
+                             stream=None):
+        """append_kv_batch from projections that are not rotated yet: K turns by ``rope`` on its way into the pages, V
+        goes in as it is, and Q (CUDA bf16 [L][cu_tokens[-1]][Hq][d], the same tokens' queries) is returned rotated
+        (``Q_out``: the tensor to write, Q itself among them).  ``positions``: CUDA int32 [axes][cu_tokens[-1]] (or
+        [cu_tokens[-1]] for one axis); by default those that the tokens get in their sequences."""
+        _covers(seqs, cu_tokens, "cu_tokens")
+        cu = _i32_array(cu_tokens)
+        if not isinstance(rope, Rope):
+            raise TypeError("rope must be a Rope")
+        if K is None:
+            if not self.host_only:
+                raise ValueError("K and V are required")
+            _check(_lib.pe_append_kv_rope_batch(self._h, len(seqs), _i32_array(seqs), None, None, cu, rope._ref, None, None,
+                                                None, 0, self._s(stream)))
+            return None
+        self._check_kv(K, V)
+        total = K.shape[1]
+        if total != cu_tokens[-1]:
+            raise ValueError("K token count does not match cu_tokens")
+        q = q_out = None
+        heads = 0
+        if Q is not None:
+            shape = Q.shape
+            if len(shape) != 4 or shape[0] != self.num_layers or shape[1] != total or shape[3] != self.head_dim:
+                raise ValueError("Q must be [L][cu_tokens[-1]][Hq][d]")
+            _same_shape(Q_out, Q, "Q_out")
+            if Q_out is None:
+                Q_out = self._output_like(Q, stream)
+            q, q_out, heads = self._ptr(Q, "Q"), self._ptr(Q_out, "Q_out"), shape[2]
+        elif Q_out is not None:
+            raise ValueError("Q_out without Q")
+        _check(_lib.pe_append_kv_rope_batch(self._h, len(seqs), _i32_array(seqs), self._ptr(K, "K"), self._ptr(V, "V"), cu,
+                                            rope._ref, self._positions(positions, rope, total), q, q_out, heads,
+                                            self._s(stream)))
+        return Q_out
+
+    def append_kv_rope(self, seq, K, V, rope, Q=None, positions=None, Q_out=None, stream=None):
+        """append_kv_rope_batch of one sequence's tokens."""
+        return self.append_kv_rope_batch([seq], K, V, [0, K.shape[1]], rope, Q, positions, Q_out, stream)
+
+    def rotate_batch(self, seqs, X, cu_tokens, rope, positions=None, out=None, stream=None):
+        """X, CUDA bf16 [cu_tokens[-1]][H][d] or [layers][cu_tokens[-1]][H][d], rotated (``out``: the tensor to write, X
+        itself among them).  ``positions`` as in append_kv_rope_batch; by default rows cu_tokens[i]:cu_tokens[i+1] are
+        the last positions of seqs[i]."""
+        _covers(seqs, cu_tokens, "cu_tokens")
+        if not isinstance(rope, Rope):
+            raise TypeError("rope must be a Rope")
+        shape = X.shape
+        if len(shape) not in (3, 4) or shape[-1] != self.head_dim or shape[-3] != cu_tokens[-1]:
+            raise ValueError("X must be [layers][cu_tokens[-1]][H][d]")
+        _same_shape(out, X, "out", "X")
+        if out is None:
+            out = self._output_like(X, stream)
+        _check(_lib.pe_rotate_batch(self._h, len(seqs), _i32_array(seqs), self._ptr(X, "X"), _i32_array(cu_tokens),
+                                    self._ptr(out, "out"), shape[0] if len(shape) == 4 else 1, shape[-2], rope._ref,
+                                    self._positions(positions, rope, shape[-3]), self._s(stream)))
+        return out
+
+    def rotate(self, seq, X, rope, positions=None, out=None, stream=None):
+        """rotate_batch of one sequence's last positions."""
+        return self.rotate_batch([seq], X, [0, X.shape[-3]], rope, positions, out, stream)
+
+    def _positions(self, t, rope, tokens):
+        if t is None:
+            return None
+        if t.dtype is not self._torch.int32:
+            raise TypeError("positions must be int32")
+        if t.get_device() != self._device:
+            if not t.is_cuda:
+                raise TypeError("positions must be a CUDA tensor")
+            raise ValueError(f"positions is on cuda:{t.get_device()}, the cache on cuda:{self._device}")
+        shape = tuple(t.shape)
+        if shape != (rope.n_axes, tokens) and not (rope.n_axes == 1 and shape == (tokens,)):
+            raise ValueError(f"positions must be [{rope.n_axes}][{tokens}]")
+        if not t.is_contiguous():
+            raise ValueError("positions must be contiguous")
+        return t.data_ptr()
+
     # -- replay attention ------------------------------------------------------
     def replay_attn(self, seq, layer, Q, out=None, softmax_scale=None, stream=None):
         """Attention of the last Q.shape[0] positions of ``seq``; Q, out: CUDA bf16 [n_q][Hq][d]."""
@@ -496,6 +605,49 @@ class PagedKVCache:
                                                  _i32_array(cu_q), self._ptr(out, "out"), shape[1], scale, ptr, stride,
                                                  self._s(stream)))
         return out
+
+    # -- differential attention ------------------------------------------------
+    def diff_attn_batch(self, seqs, layer, Q, cu_q, lam, gain=None, eps=1e-5, out=None, softmax_scale=None, stream=None):
+        """Differential attention (pe_diff_attn_batch).  Q: CUDA bf16 [cu_q[-1]][Hq][d], rows cu_q[i]:cu_q[i+1] the last
+        positions of seqs[i]; heads 2i and 2i + 1 are the maps of head i.  ``lam``: CUDA float32 [Hq / 2], what the
+        second map counts.  ``gain``: CUDA float32 [2d] of the norm over a head's 2d columns (None: no norm).  Returns
+        bf16 [cu_q[-1]][Hq / 2][2d]."""
+        _covers(seqs, cu_q, "cu_q")
+        if self.host_only:
+            raise ValueError("attention on a host-only cache")
+        shape = Q.shape
+        if len(shape) != 3 or shape[2] != self.head_dim or shape[0] != cu_q[-1]:
+            raise ValueError("Q must be [cu_q[-1]][Hq][d]")
+        if shape[1] % 2:
+            raise ValueError("Q must have pairs of heads")
+        want = (shape[0], shape[1] // 2, 2 * shape[2])
+        if out is None:
+            out = self._output(lambda: self._torch.empty(want, dtype=self._bf16, device=self._torch_device), stream)
+        elif tuple(out.shape) != want:
+            raise ValueError(f"out has shape {tuple(out.shape)}, it must be {want}")
+        scale = self._default_scale if softmax_scale is None else float(softmax_scale)
+        _check(_lib.pe_diff_attn_batch(self._h, len(seqs), _i32_array(seqs), layer, self._ptr(Q, "Q"), _i32_array(cu_q),
+                                       self._ptr(out, "out"), shape[1], scale, self._vec(lam, "lam", shape[1] // 2),
+                                       None if gain is None else self._vec(gain, "gain", 2 * shape[2]), float(eps),
+                                       self._s(stream)))
+        return out
+
+    def diff_attn(self, seq, layer, Q, lam, gain=None, eps=1e-5, out=None, softmax_scale=None, stream=None):
+        """diff_attn_batch of one sequence's last positions."""
+        return self.diff_attn_batch([seq], layer, Q, [0, Q.shape[0]], lam, gain, eps, out, softmax_scale, stream)
+
+    def _vec(self, t, name, n):
+        if t.dtype is not self._torch.float32:
+            raise TypeError(f"{name} must be float32")
+        if t.get_device() != self._device:
+            if not t.is_cuda:
+                raise TypeError(f"{name} must be a CUDA tensor")
+            raise ValueError(f"{name} is on cuda:{t.get_device()}, the cache on cuda:{self._device}")
+        if tuple(t.shape) != (n,):
+            raise ValueError(f"{name} must be [{n}]")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        return t.data_ptr()
 
     def _rows(self, t, name, dtype, n):
         """(address, row stride) of a CUDA tensor of n rows with contiguous columns."""

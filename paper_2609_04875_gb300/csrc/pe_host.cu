@@ -681,8 +681,9 @@ pe_status apply_cow(pe_cache *c, int32_t seq, CowList &cow, cudaStream_t st)
 // kMaxSegs segments and kAppendMaxPages new page ids.
 // `beside`: the stream's last launch is a decode merge of the same call, and the
 // first append launch may run beside it (not one that follows copies-on-write).
+// `rope`: K turns on the way, and the queries beside it.
 pe_status apply_appends(pe_cache *c, const std::vector<AppendPlan> &plans, const void *K, const void *V,
-                        int64_t n_total, cudaStream_t st, bool beside = false)
+                        int64_t n_total, cudaStream_t st, bool beside = false, const RopeCall *rope = nullptr)
 {
     const int ps = c->cfg.page_size;
     AppendParams pbuf;  // (only the header, the segments and the page ids in use are written: 15 KB otherwise)
@@ -724,7 +725,9 @@ pe_status apply_appends(pe_cache *c, const std::vector<AppendPlan> &plans, const
         const int64_t chunks = static_cast<int64_t>(p->L) * p->seg_tokens * p->hkv * p->dvec;
         if (injected_failure(c)) return launch_fault("append kernel");
         if (!c->host_only) {
-            cudaError_t e = c->q8 ? launch_append_q8(c->cfg.head_dim, *p, st) : launch_append(*p, chunks, st);
+            cudaError_t e = rope    ? launch_append_rope(c->q8, c->cfg.head_dim, *p, *rope, st)
+                            : c->q8 ? launch_append_q8(c->cfg.head_dim, *p, st)
+                                    : launch_append(*p, chunks, st);
             if (e != cudaSuccess) return cuda_fail(e, "append kernel launch");
             c->launches++;
         }
@@ -2250,6 +2253,76 @@ pe_status check_attn_args(const pe_cache *c, int32_t layer, const void *Q, const
     return PE_OK;
 }
 
+// ---- position rotation
+// A rotation's description for the kernels.  axes: rows of `positions`, which has `tokens` columns.
+pe_status rope_params(const pe_cache *c, const pe_rope *rope, const int32_t *positions, int64_t tokens, RopeParams *r)
+{
+    if (!rope || !rope->freq) return fail(PE_ERR_INVALID, "null rotation");
+    if (rope->n_pairs < 1 || rope->n_pairs > c->cfg.head_dim / 2)
+        return fail(PE_ERR_INVALID, "%d pairs: a head of %d columns has 1 to %d", rope->n_pairs, c->cfg.head_dim, c->cfg.head_dim / 2);
+    if (rope->n_axes < 1 || rope->n_axes > kRopeMaxAxes)
+        return fail(PE_ERR_INVALID, "%d axes: there are 1 to %d", rope->n_axes, kRopeMaxAxes);
+    if (!std::isfinite(rope->scale)) return fail(PE_ERR_INVALID, "the rotation's scale is not finite");
+    std::memset(r, 0, sizeof *r);
+    for (int32_t i = 0; i < rope->n_pairs; ++i) {
+        const double f = rope->freq[i];
+        if (!std::isfinite(f)) return fail(PE_ERR_INVALID, "frequency %d is not finite", i);
+        const int32_t axis = rope->axis ? rope->axis[i] : 0;
+        if (axis < 0 || axis >= rope->n_axes) return fail(PE_ERR_INVALID, "pair %d: axis %d of %d", i, axis, rope->n_axes);
+        // turns a position, their whole part dropped, in units of 2^-64 turn
+        double t = std::fabs(f) / 6.283185307179586476925;
+        t -= std::floor(t);
+        const uint64_t u = static_cast<uint64_t>(std::ldexp(t, 64));
+        r->turn[i] = f < 0 ? 0 - u : u;
+        r->axis[i] = static_cast<uint8_t>(axis);
+    }
+    if (reinterpret_cast<uintptr_t>(positions) & 3u) return fail(PE_ERR_INVALID, "positions: misaligned pointer");
+    r->positions = positions;
+    r->positions_stride = tokens;
+    r->n_pairs = rope->n_pairs;
+    r->interleaved = rope->interleaved ? 1 : 0;
+    r->scale = rope->scale;
+    return PE_OK;
+}
+
+// ---- differential attention
+pe_status run_diff(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer, const void *Q, void *out, int32_t hq, float scale,
+                   const float *lambda, const float *gain, float eps, cudaStream_t st)
+{
+    DiffParams p;
+    std::memset(static_cast<void *>(&p), 0, offsetof(DiffParams, seqs));
+    p.page_table = c->d_table;
+    p.q = static_cast<const __nv_bfloat16 *>(Q);
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.k_pool = static_cast<const __nv_bfloat16 *>(c->k_pool);
+    p.v_pool = static_cast<const __nv_bfloat16 *>(c->v_pool);
+    p.lambda = lambda;
+    p.gain = gain;
+    p.hq = hq;
+    p.hkv = c->cfg.num_kv_heads;
+    p.group = hq / p.hkv;
+    p.layer = layer;
+    p.num_pages = c->cfg.num_pages;
+    p.ps = c->cfg.page_size;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.eps = eps;
+    for (size_t i = 0; i < items.size();) {
+        int64_t rows = 0;
+        for (p.n_seqs = 0; i < items.size() && p.n_seqs < kMaxSegs; ++i) {
+            const AttnItem &it = items[i];
+            if (it.n_q <= 0) continue;
+            p.seqs[p.n_seqs++] = DiffSeq{it.seq * c->cfg.max_pages_per_seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq])};
+            rows += it.n_q;
+        }
+        if (p.n_seqs == 0) continue;
+        if (injected_failure(c)) return launch_fault("differential attention");
+        cudaError_t e = launch_diff_attn(c->cfg.head_dim, p, rows, st);
+        if (e != cudaSuccess) return cuda_fail(e, "differential attention launch");
+        c->launches++;
+    }
+    return PE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -2572,8 +2645,17 @@ pe_status pe_append_kv(pe_cache *c, int32_t seq, const void *K, const void *V, i
     return tx.end(apply_appends(c, {pl}, K, V, n_tokens, static_cast<cudaStream_t>(stream)));
 }
 
-pe_status pe_append_kv_batch(pe_cache *c, int32_t n, const int32_t *seqs, const void *K, const void *V,
-                             const int32_t *cu_tokens, void *stream)
+// What an append that rotates is given besides K and V.
+struct RopeArgs {
+    const pe_rope *rope;
+    const int32_t *positions;
+    const void *Q;
+    void *Q_out;
+    int32_t hq;
+};
+
+static pe_status append_batch(pe_cache *c, int32_t n, const int32_t *seqs, const void *K, const void *V, const int32_t *cu_tokens,
+                              const RopeArgs *ra, void *stream)
 {
     if (pe_status s = check_device(c)) return s;
     if (n < 0 || (n > 0 && (!seqs || !cu_tokens))) return fail(PE_ERR_INVALID, "bad batch arguments");
@@ -2599,10 +2681,134 @@ pe_status pe_append_kv_batch(pe_cache *c, int32_t n, const int32_t *seqs, const 
     if (need > static_cast<int64_t>(c->free_stack.size()))
         return fail(PE_ERR_OOM, "batch append needs %lld pages, %zu free", static_cast<long long>(need),
                     c->free_stack.size());
+    RopeCall rc;
+    if (ra) {
+        if (pe_status s = rope_params(c, ra->rope, ra->positions, total, &rc.r)) return s;
+        rc.Q = static_cast<const uint4 *>(ra->Q);
+        rc.Q_out = static_cast<uint4 *>(ra->Q_out);
+        rc.hq = ra->hq;
+        if (ra->Q && !c->host_only && total > 0) {
+            if (!ra->Q_out) return fail(PE_ERR_INVALID, "null Q_out");
+            if (!aligned16(ra->Q) || !aligned16(ra->Q_out)) return fail(PE_ERR_INVALID, "Q and Q_out must be 16-byte aligned");
+            if (ra->hq <= 0) return fail(PE_ERR_INVALID, "num_q_heads must be positive");
+            const int64_t row = static_cast<int64_t>(c->cfg.num_layers) * total * c->cfg.head_dim * 2;
+            const int64_t kv_bytes = row * c->cfg.num_kv_heads, q_bytes = row * ra->hq;
+            if (ra->Q != ra->Q_out && !apart(ra->Q, q_bytes, ra->Q_out, q_bytes)) return fail(PE_ERR_INVALID, "Q_out overlaps Q");
+            if (!apart(ra->Q_out, q_bytes, K, kv_bytes) || !apart(ra->Q_out, q_bytes, V, kv_bytes))
+                return fail(PE_ERR_INVALID, "Q_out overlaps K or V");
+        }
+    }
     CallTxn tx(c, static_cast<cudaStream_t>(stream));
     if (c->q8 && !one_append_launch(plans))
         if (pe_status s = save_tails(c, plans, static_cast<cudaStream_t>(stream))) return tx.end(s);
-    return tx.end(apply_appends(c, plans, K, V, total, static_cast<cudaStream_t>(stream)));
+    return tx.end(apply_appends(c, plans, K, V, total, static_cast<cudaStream_t>(stream), false, ra ? &rc : nullptr));
+}
+
+pe_status pe_append_kv_batch(pe_cache *c, int32_t n, const int32_t *seqs, const void *K, const void *V,
+                             const int32_t *cu_tokens, void *stream)
+{
+    return append_batch(c, n, seqs, K, V, cu_tokens, nullptr, stream);
+}
+
+pe_status pe_append_kv_rope_batch(pe_cache *c, int32_t n, const int32_t *seqs, const void *K, const void *V,
+                                  const int32_t *cu_tokens, const pe_rope *rope, const int32_t *positions, const void *Q,
+                                  void *Q_out, int32_t num_q_heads, void *stream)
+{
+    try {
+        const RopeArgs ra{rope, positions, Q, Q_out, num_q_heads};
+        return append_batch(c, n, seqs, K, V, cu_tokens, &ra, stream);
+    } catch (const std::bad_alloc &) {
+        return fail(PE_ERR_OOM, "host allocation failed");
+    }
+}
+
+pe_status pe_rotate_batch(pe_cache *c, int32_t n, const int32_t *seqs, const void *X, const int32_t *cu_tokens, void *out,
+                          int32_t num_layers, int32_t num_heads, const pe_rope *rope, const int32_t *positions, void *stream)
+{
+    if (pe_status s = check_device(c)) return s;
+    if (n < 0 || (n > 0 && (!seqs || !cu_tokens))) return fail(PE_ERR_INVALID, "bad batch arguments");
+    if (n > 0 && cu_tokens[0] != 0) return fail(PE_ERR_INVALID, "cu_tokens[0] must be 0");
+    if (num_layers < 0 || num_heads < 1) return fail(PE_ERR_INVALID, "%d layers of %d heads", num_layers, num_heads);
+    for (int32_t i = 0; i < n; ++i) {
+        if (pe_status s = check_seq(c, seqs[i])) return s;
+        const int32_t cnt = cu_tokens[i + 1] - cu_tokens[i];
+        if (cu_tokens[i + 1] < cu_tokens[i]) return fail(PE_ERR_INVALID, "cu_tokens must be non-decreasing");
+        if (!positions && cnt > c->len[seqs[i]])
+            return fail(PE_ERR_RANGE, "sequence %d: %d tokens exceed its length %lld", seqs[i], cnt, static_cast<long long>(c->len[seqs[i]]));
+    }
+    const int64_t total = n > 0 ? cu_tokens[n] : 0;
+    RotateParams p;
+    std::memset(static_cast<void *>(&p), 0, offsetof(RotateParams, segs));
+    if (pe_status s = rope_params(c, rope, positions, total, &p.r)) return s;
+    if (total == 0 || num_layers == 0) return PE_OK;
+    if (c->host_only) return fail(PE_ERR_UNSUPPORTED, "rotation on a host-only cache");
+    if (!X || !out) return fail(PE_ERR_INVALID, "null X or out");
+    if (!aligned16(X) || !aligned16(out)) return fail(PE_ERR_INVALID, "X and out must be 16-byte aligned");
+    const int64_t bytes = static_cast<int64_t>(num_layers) * total * num_heads * c->cfg.head_dim * 2;
+    if (X != out && !apart(X, bytes, out, bytes)) return fail(PE_ERR_INVALID, "out overlaps X");
+    p.X = static_cast<const uint4 *>(X);
+    p.out = static_cast<uint4 *>(out);
+    p.layers = num_layers;
+    p.heads = num_heads;
+    p.n_total = static_cast<int32_t>(total);
+    for (int32_t i = 0; i < n;) {
+        p.n_segs = 0;
+        p.tok0 = cu_tokens[i];
+        if (positions) {
+            p.segs[p.n_segs++] = RotateSeg{0, 0};
+            i = n;
+        }
+        for (; i < n && p.n_segs < kMaxSegs; ++i) {
+            const int32_t cnt = cu_tokens[i + 1] - cu_tokens[i];
+            if (cnt > 0) p.segs[p.n_segs++] = RotateSeg{cu_tokens[i], static_cast<int32_t>(c->len[seqs[i]]) - cnt};
+        }
+        p.n_tokens = cu_tokens[i] - p.tok0;
+        if (p.n_tokens == 0) continue;
+        if (injected_failure(c)) return launch_fault("rotation kernel");
+        cudaError_t e = launch_rotate(c->cfg.head_dim, p, static_cast<cudaStream_t>(stream));
+        if (e != cudaSuccess) return cuda_fail(e, "rotation kernel launch");
+        c->launches++;
+    }
+    return PE_OK;
+}
+
+static pe_status diff_attn_batch(pe_cache *c, int32_t n, const int32_t *seqs, int32_t layer, const void *Q, const int32_t *cu_q,
+                                 void *out, int32_t hq, float scale, const float *lambda, const float *gain, float eps, cudaStream_t st)
+{
+    if (!c) return fail(PE_ERR_INVALID, "null cache");
+    if (n < 0 || (n > 0 && (!seqs || !cu_q))) return fail(PE_ERR_INVALID, "bad batch arguments");
+    if (n == 0) return PE_OK;
+    pe_status s = check_attn_args(c, layer, Q, out, hq, scale, cu_q[n] > 0);
+    if (s != PE_OK) return s;
+    if (c->cfg.num_kv_heads % 2 != 0)
+        return fail(PE_ERR_UNSUPPORTED, "differential attention needs pairs of kv-heads, the cache has %d", c->cfg.num_kv_heads);
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(PE_ERR_INVALID, "eps must be finite and not negative");
+    std::vector<AttnItem> items;
+    if ((s = batch_items(c, n, seqs, cu_q, items)) != PE_OK) return s;
+    if (cu_q[n] == 0) return PE_OK;
+    if (!lambda || (reinterpret_cast<uintptr_t>(lambda) & 3u)) return fail(PE_ERR_INVALID, "lambda: null or misaligned pointer");
+    if (reinterpret_cast<uintptr_t>(gain) & 3u) return fail(PE_ERR_INVALID, "gain: misaligned pointer");
+    const int64_t q_bytes = static_cast<int64_t>(cu_q[n]) * hq * c->cfg.head_dim * 2;
+    if (!apart(Q, q_bytes, out, q_bytes)) return fail(PE_ERR_INVALID, "out overlaps Q");
+    if (!apart(lambda, 2 * static_cast<int64_t>(hq), out, q_bytes) || (gain && !apart(gain, 8 * static_cast<int64_t>(c->cfg.head_dim), out, q_bytes)))
+        return fail(PE_ERR_INVALID, "out overlaps lambda or gain");
+    if (c->q8) {
+        if ((s = unpack_layer(c, items.data(), items.size(), layer, st)) != PE_OK) return s;
+        layer = 0;
+    }
+    return run_diff(c, items, layer, Q, out, hq, scale, lambda, gain, eps, st);
+}
+
+pe_status pe_diff_attn_batch(pe_cache *c, int32_t n, const int32_t *seqs, int32_t layer, const void *Q_packed,
+                             const int32_t *cu_q, void *out, int32_t num_q_heads, float softmax_scale, const float *lambda,
+                             const float *gain, float eps, void *stream)
+{
+    try {
+        return diff_attn_batch(c, n, seqs, layer, Q_packed, cu_q, out, num_q_heads, softmax_scale, lambda, gain, eps,
+                               static_cast<cudaStream_t>(stream));
+    } catch (const std::bad_alloc &) {
+        return fail(PE_ERR_OOM, "host allocation failed");
+    }
 }
 
 pe_status pe_replay_attn(pe_cache *c, int32_t seq, int32_t layer, const void *Q, void *out, int32_t n_q,

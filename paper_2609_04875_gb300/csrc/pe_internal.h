@@ -52,6 +52,70 @@ struct AppendParamsT {
 };
 using AppendParams = AppendParamsT<kMaxSegs, kAppendMaxPages>;
 
+// ---------------------------------------------------------------- position rotation
+constexpr int kRopeMaxPairs = 64;      // head_dim / 2
+constexpr int kRopeMaxAxes = 8;
+
+// Pair i of a head's columns turns by turn[i] 2^-64 of a full turn a position.  The product with a position, modulo 2^64,
+// is the angle modulo a full turn, exactly: however far the position, the angle errs by no more than turn[i]'s own rounding.
+struct RopeParams {
+    uint64_t turn[kRopeMaxPairs];
+    uint8_t axis[kRopeMaxPairs];
+    const int32_t *positions;  // [n_axes][positions_stride], or null: the tokens' positions in their sequences
+    int64_t positions_stride;
+    int32_t n_pairs, interleaved;
+    float scale;               // of the rotated columns
+};
+
+// What an append that rotates has besides: the queries of the same tokens.
+struct RopeCall {
+    RopeParams r;
+    const uint4 *Q;            // [L][n_total][Hq][d], or null
+    uint4 *Q_out;
+    int32_t hq;
+};
+
+template <int SEGS, int PAGES>
+struct AppendRopeParamsT {
+    RopeCall c;
+    AppendParamsT<SEGS, PAGES> a;
+};
+
+// Rows of one tensor [layers][n_total][heads][d].
+struct RotateSeg {
+    int32_t tok0;          // first token inside the tensor
+    int32_t pos0;          // its position in its sequence
+};
+
+struct RotateParams {
+    RopeParams r;
+    const uint4 *X;
+    uint4 *out;
+    int32_t layers, n_total, heads, n_segs;
+    int32_t tok0, n_tokens;  // of this launch
+    RotateSeg segs[kMaxSegs];
+};
+
+// ---------------------------------------------------------------- differential attention
+struct DiffSeq {
+    int32_t table_row;     // seq * max_pages_per_seq
+    int32_t q_row0, n_q;   // rows of Q / out
+    int32_t n_keys;        // the last query sees all of them
+};
+
+struct DiffParams {
+    const int32_t *page_table;
+    const __nv_bfloat16 *q;      // bf16 [rows][Hq][d]
+    __nv_bfloat16 *out;          // bf16 [rows][Hq / 2][2 d]
+    const __nv_bfloat16 *k_pool, *v_pool;
+    const float *lambda;         // [Hq / 2]
+    const float *gain;           // [2 d], or null: no norm
+    int32_t n_seqs, hq, hkv, group, layer, num_pages, ps;
+    float scale_log2;            // softmax_scale * log2(e)
+    float eps;
+    DiffSeq seqs[kMaxSegs];
+};
+
 // ---------------------------------------------------------------- copy-on-write
 struct CowCopy {
     int32_t src, dst;      // pages
@@ -409,6 +473,10 @@ cudaError_t launch_decode_attn(int head_dim, int rows_cap, bool tensor_core, con
                                const CUtensorMap &tm_v, const DecodeParams &p, cudaStream_t st);
 // 8-bit cache: p's pools hold codes, p.exps their scales, p.segs[].cum0 and p.seg_tokens count touched pages.
 cudaError_t launch_append_q8(int head_dim, const AppendParams &p, cudaStream_t st);
+// Append with the rotation on the way (a block of append parameters as above, and the rotation's).
+cudaError_t launch_append_rope(bool q8, int head_dim, const AppendParams &p, const RopeCall &rope, cudaStream_t st);
+cudaError_t launch_rotate(int head_dim, const RotateParams &p, cudaStream_t st);
+cudaError_t launch_diff_attn(int head_dim, const DiffParams &p, int64_t rows, cudaStream_t st);
 cudaError_t launch_unpack_q8(const UnpackParams &p, int pages, cudaStream_t st);
 cudaError_t launch_save_pages(const SaveParams &p, cudaStream_t st);
 cudaError_t launch_read_kv(bool q8, const ReadParams &p, cudaStream_t st);

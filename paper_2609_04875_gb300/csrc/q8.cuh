@@ -36,6 +36,14 @@ __device__ __forceinline__ int q8_exponent(uint32_t a)
     return e < -126 ? -126 : (e > 119 ? 119 : e);
 }
 
+// The same from a magnitude in 32 bits.
+__device__ __forceinline__ int q8_exponent_f32(float a)
+{
+    const uint32_t w = __float_as_uint(a);
+    const int e = static_cast<int>(w >> 23) - 135 + ((w & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return e < -126 ? -126 : (e > 119 ? 119 : e);
+}
+
 // two codes, low byte first
 __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t codes)
 {
@@ -57,6 +65,28 @@ __device__ __forceinline__ uint4 q8_to_bf16(uint2 c, float s)
 {
     return make_uint4(q8_pair_to_bf16(c.x, s), q8_pair_to_bf16(c.x >> 16, s), q8_pair_to_bf16(c.y, s),
                       q8_pair_to_bf16(c.y >> 16, s));
+}
+
+// eight codes times s in 32 bits
+__device__ __forceinline__ void q8_to_float(uint2 c, float s, float (&y)[8])
+{
+    const uint32_t w[4] = {c.x, c.x >> 16, c.y, c.y >> 16};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = e4m3x2_to_float2(w[i]);
+        y[2 * i] = f.x * s;
+        y[2 * i + 1] = f.y * s;
+    }
+}
+
+// eight floats times s, rounded to codes
+__device__ __forceinline__ uint2 q8_from_float(const float (&y)[8], float s)
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(y[2 * i] * s, y[2 * i + 1] * s), __NV_SATFINITE, __NV_E4M3));
+    return make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
 }
 
 // a bf16 pair times s, rounded to two codes
@@ -165,6 +195,72 @@ __device__ __forceinline__ void q8_write_page(bool on, int t, int threads, int n
         const int c = i * threads + t;
         if (c / CPR >= n_rows) continue;
         uint2 kc = q8_from_bf16(k[i], ks), vc = q8_from_bf16(v[i], vs);
+        if (bad >> i & 1u) {
+            kc = make_uint2(kQ8NanWord, kQ8NanWord);
+            vc = make_uint2(0u, 0u);
+        }
+        if (c / CPR >= old || ke != ke0) reinterpret_cast<uint2 *>(k_dst)[c] = kc;
+        if (c / CPR >= old || ve != ve0) reinterpret_cast<uint2 *>(v_dst)[c] = vc;
+    }
+    if (t == 0) *reinterpret_cast<char2 *>(exps) = make_char2(static_cast<char>(ke), static_cast<char>(ve));
+}
+
+// The same with K in 32 bits: load(row, col8, float (&k)[8], uint4 &v).
+template <int CPR, int NC, typename Load>
+__device__ __forceinline__ void q8_write_page_f32(bool on, int t, int threads, int n_rows, int old, int ke0, int ve0,
+                                                  uint8_t *k_dst, uint8_t *v_dst, int8_t *exps, uint32_t *s_max, const Load &load)
+{
+    float k[NC][8];
+    uint4 v[NC];
+    uint32_t bad = 0, vm = 0;
+    float kmax = 0.f;
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = i * threads + t;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) k[i][x] = 0.f;
+        v[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (on && c / CPR < n_rows) load(c / CPR, c % CPR, k[i], v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        // (as bits: an infinity or NaN is 0x7f800000 or more)
+        uint32_t ka = 0;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) ka = max(ka, __float_as_uint(k[i][x]) & 0x7fffffffu);
+        const uint32_t va = bf16x8_absmax(v[i]);
+        const uint32_t any = __ballot_sync(0xffffffffu, ka >= 0x7f800000u || va >= 0x7f80u);
+        if ((any >> (lane / CPR * CPR)) & ((1u << CPR) - 1)) {
+            bad |= 1u << i;
+        } else {
+            kmax = fmaxf(kmax, __uint_as_float(ka));
+            vm = max(vm, va);
+        }
+    }
+    // An exponent is monotone in the magnitude: the page's is the largest of the threads' (biased, a byte each).
+    const uint32_t ke_t = static_cast<uint32_t>(q8_exponent_f32(kmax) + 127), ve_t = static_cast<uint32_t>(q8_exponent(vm) + 127);
+    uint32_t km = __reduce_max_sync(0xffffffffu, ke_t);
+    vm = __reduce_max_sync(0xffffffffu, ve_t);
+    if (threads > 32) {  // uniform over the block
+        const int warp = threadIdx.x >> 5;
+        __syncthreads();
+        if (lane == 0) s_max[warp] = (km << 16) | vm;
+        __syncthreads();
+        const int w0 = (threadIdx.x / threads) * (threads >> 5);
+        for (int w = w0; w < w0 + (threads >> 5); ++w) {
+            km = max(km, s_max[w] >> 16);
+            vm = max(vm, s_max[w] & 0xffffu);
+        }
+    }
+    if (!on) return;
+    const int ke = static_cast<int>(km) - 127, ve = static_cast<int>(vm) - 127;
+    const float ks = pow2i(-ke), vs = pow2i(-ve);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = i * threads + t;
+        if (c / CPR >= n_rows) continue;
+        uint2 kc = q8_from_float(k[i], ks), vc = q8_from_bf16(v[i], vs);
         if (bad >> i & 1u) {
             kc = make_uint2(kQ8NanWord, kQ8NanWord);
             vc = make_uint2(0u, 0u);
