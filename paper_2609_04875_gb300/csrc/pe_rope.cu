@@ -19,39 +19,190 @@ namespace {
 // (cos, sin) times the scale of pair i for token tok (of the whole tensor), whose position in its sequence is pos.
 __device__ __forceinline__ float2 rope_turn(const RopeParams &r, int i, int64_t tok, int pos)
 {
-    const int at = r.positions ? r.positions[r.axis[i] * r.positions_stride + tok] : pos;
+    const int at = r.positions ? __ldg(r.positions + r.axis[i] * r.positions_stride + tok) : pos;
     const uint64_t phase = static_cast<uint64_t>(static_cast<int64_t>(at)) * r.turn[i];
     float s, c;
     sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 4.656612873077393e-10f, &s, &c);  // 2^-31 half turns
     return make_float2(c * r.scale, s * r.scale);
 }
 
-__device__ __forceinline__ float bf16_at(const uint4 *row, int col)
+__device__ __forceinline__ void unpack8(uint4 v, float (&y)[8])
 {
-    return __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(row)[col]);
-}
-
-// Columns 8 chunk .. + 7 of a row, rotated.
-__device__ __forceinline__ void rope_chunk(const RopeParams &r, const uint4 *row, int chunk, int64_t tok, int pos, float (&y)[8])
-{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int col = chunk * 8 + k;
-        const float x = bf16_at(row, col);
-        y[k] = x;
-        if (col >= 2 * r.n_pairs) continue;
-        const bool second = r.interleaved ? col & 1 : col >= r.n_pairs;
-        const int i = r.interleaved ? col >> 1 : (second ? col - r.n_pairs : col);
-        const int other = r.interleaved ? col ^ 1 : (second ? i : col + r.n_pairs);
-        const float2 t = rope_turn(r, i, tok, pos);
-        const float z = bf16_at(row, other);
-        y[k] = second ? x * t.x + z * t.y : x * t.x - z * t.y;
+    for (int k = 0; k < 4; ++k) {
+        const float2 f = unpack_bf16(w[k]);
+        y[2 * k] = f.x;
+        y[2 * k + 1] = f.y;
     }
 }
 
 __device__ __forceinline__ uint4 pack8(const float (&y)[8])
 {
     return make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+}
+
+// Columns 8 chunk .. + 7 of a row, rotated, one by one: for any number of pairs.
+__device__ __forceinline__ void rope_chunk(const RopeParams &r, const uint4 *row, int chunk, int64_t tok, int pos, float (&y)[8])
+{
+    const __nv_bfloat16 *x = reinterpret_cast<const __nv_bfloat16 *>(row);
+#pragma unroll 1
+    for (int k = 0; k < 8; ++k) {
+        const int col = chunk * 8 + k;
+        float v = __bfloat162float(x[col]);
+        if (col < 2 * r.n_pairs) {
+            const bool second = r.interleaved ? col & 1 : col >= r.n_pairs;
+            const int i = r.interleaved ? col >> 1 : (second ? col - r.n_pairs : col);
+            const float2 t = rope_turn(r, i, tok, pos);
+            const float z = __bfloat162float(x[r.interleaved ? col ^ 1 : (second ? i : col + r.n_pairs)]);
+            v = second ? v * t.x + z * t.y : v * t.x - z * t.y;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (u == k) y[u] = v;
+    }
+}
+
+// The same where n_pairs is a multiple of 8: the other half of each of the chunk's pairs is one chunk, or this one.
+__device__ __forceinline__ void rope_chunk_whole(const RopeParams &r, const uint4 *row, int chunk, int64_t tok, int pos, float (&y)[8])
+{
+    const int whole = r.n_pairs / 8;
+    unpack8(__ldg(row + chunk), y);
+    if (chunk >= 2 * whole) return;
+    if (r.interleaved) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 t = rope_turn(r, 4 * chunk + k, tok, pos);
+            const float p = y[2 * k], q = y[2 * k + 1];
+            y[2 * k] = p * t.x - q * t.y;
+            y[2 * k + 1] = q * t.x + p * t.y;
+        }
+        return;
+    }
+    const bool second = chunk >= whole;
+    float z[8];
+    unpack8(__ldg(row + (second ? chunk - whole : chunk + whole)), z);
+    const float sign = second ? 1.f : -1.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float2 t = rope_turn(r, 8 * (second ? chunk - whole : chunk) + k, tok, pos);
+        y[k] = y[k] * t.x + z[k] * (sign * t.y);
+    }
+}
+
+// A thread's share of every row of a token: two chunks of eight columns, a and b, which are either copied or eight whole
+// pairs, whose angles it keeps.  In halves those are chunks c and c + n_pairs / 8, of neighbours 2c and 2c + 1.
+template <int CPR>
+struct PairOfChunks {
+    int a, b;
+    bool turns, interleaved;
+    float2 t[8];
+    __device__ __forceinline__ PairOfChunks(const RopeParams &r, int c, int64_t tok, int pos)
+    {
+        const int whole = r.n_pairs / 8;
+        turns = c < whole;
+        interleaved = r.interleaved;
+        a = turns && !interleaved ? c : 2 * c;
+        b = turns && !interleaved ? c + whole : 2 * c + 1;
+        if (turns)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t[k] = rope_turn(r, 8 * c + k, tok, pos);
+    }
+    __device__ __forceinline__ void turn(uint4 &va, uint4 &vb) const
+    {
+        if (!turns) return;
+        float x[8], y[8];
+        unpack8(va, x);
+        unpack8(vb, y);
+        if (interleaved) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float p = x[2 * k], q = x[2 * k + 1], u = y[2 * k], w = y[2 * k + 1];
+                x[2 * k] = p * t[k].x - q * t[k].y;
+                x[2 * k + 1] = q * t[k].x + p * t[k].y;
+                y[2 * k] = u * t[4 + k].x - w * t[4 + k].y;
+                y[2 * k + 1] = w * t[4 + k].x + u * t[4 + k].y;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float p = x[k], q = y[k];
+                x[k] = p * t[k].x - q * t[k].y;
+                y[k] = q * t[k].x + p * t[k].y;
+            }
+        }
+        va = pack8(x);
+        vb = pack8(y);
+    }
+};
+
+// (reads and writes of a row are one thread's, or come one after the other within a warp: out may be the input)
+__device__ __forceinline__ uint4 ld_once(const uint4 *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p));
+    return v;
+}
+
+// Rows [0, n) of one token, a warp: row h from src + h * CPR to dst + h * dst_stride.
+template <int CPR, bool WHOLE>
+__device__ __forceinline__ void rotate_rows(const RopeParams &r, const uint4 *src, uint4 *dst, int64_t dst_stride, int n, int64_t tok, int pos)
+{
+    constexpr int CP = CPR / 2, RPW = 32 / CP, U = 4;
+    const int lane = threadIdx.x & 31, c = lane % CP;
+    if constexpr (WHOLE) {
+        const PairOfChunks<CPR> pc(r, c, tok, pos);
+        for (int h0 = lane / CP; h0 < n; h0 += U * RPW) {
+            uint4 a[U], b[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (h0 + u * RPW < n) {
+                    const uint4 *row = src + static_cast<int64_t>(h0 + u * RPW) * CPR;
+                    a[u] = ld_once(row + pc.a);
+                    b[u] = ld_once(row + pc.b);
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (h0 + u * RPW < n) {
+                    pc.turn(a[u], b[u]);
+                    uint4 *row = dst + (h0 + u * RPW) * dst_stride;
+                    row[pc.a] = a[u];
+                    row[pc.b] = b[u];
+                }
+        }
+    } else {
+        for (int h0 = 0; h0 < n; h0 += RPW) {
+            const int h = h0 + lane / CP;
+            float x[8], y[8];
+            if (h < n) {
+                rope_chunk(r, src + static_cast<int64_t>(h) * CPR, 2 * c, tok, pos, x);
+                rope_chunk(r, src + static_cast<int64_t>(h) * CPR, 2 * c + 1, tok, pos, y);
+            }
+            __syncwarp();
+            if (h < n) {
+                dst[h * dst_stride + 2 * c] = pack8(x);
+                dst[h * dst_stride + 2 * c + 1] = pack8(y);
+            }
+        }
+    }
+}
+
+template <int CPR>
+__device__ __forceinline__ void copy_rows(const uint4 *src, uint4 *dst, int64_t dst_stride, int n)
+{
+    constexpr int RPW = 32 / CPR, U = 4;
+    const int lane = threadIdx.x & 31;
+    for (int h0 = lane / CPR; h0 < n; h0 += U * RPW) {
+        uint4 a[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (h0 + u * RPW < n) a[u] = ld_once(src + static_cast<int64_t>(h0 + u * RPW) * CPR + lane % CPR);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (h0 + u * RPW < n) dst[(h0 + u * RPW) * dst_stride + lane % CPR] = a[u];
+    }
 }
 
 template <typename Segs>
@@ -65,73 +216,70 @@ __device__ __forceinline__ int find_seg(const Segs &segs, int n, int t)
     return lo;
 }
 
-// A thread per 16-byte chunk, whole rows within a warp: reads come before writes there, so out may be X.
-template <int CPR>
-__global__ void __launch_bounds__(256) rotate_kernel(const __grid_constant__ RotateParams p, int64_t chunks)
+constexpr int kRowThreads = 128;  // of a block of rows: 4 tasks, a warp each
+
+// A warp per token, layer and block of head_block heads.
+template <int CPR, bool WHOLE>
+__global__ void __launch_bounds__(kRowThreads) rotate_kernel(const __grid_constant__ RotateParams p, int head_blocks, int head_block)
 {
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const bool on = c < chunks;
-    const int64_t r = on ? c / CPR : 0;
-    const int h = static_cast<int>(r % p.heads);
-    const int64_t t = r / p.heads;
-    const int tok = p.tok0 + static_cast<int>(t % p.n_tokens);
-    const int64_t row = ((t / p.n_tokens) * p.n_total + tok) * p.heads + h;
+    int64_t r = static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5);
+    const int h0 = static_cast<int>(r % head_blocks) * head_block;
+    r /= head_blocks;
+    const int tok = p.tok0 + static_cast<int>(r % p.n_tokens);
+    const int64_t l = r / p.n_tokens;
+    if (l >= p.layers) return;
     int lo = 0, hi = p.n_segs - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (p.segs[mid].tok0 <= tok) lo = mid; else hi = mid - 1;
     }
-    const int pos = p.segs[lo].pos0 + tok - p.segs[lo].tok0;
-    float y[8];
-    if (on) rope_chunk(p.r, p.X + row * CPR, static_cast<int>(c % CPR), tok, pos, y);
-    __syncwarp();
-    if (on) p.out[row * CPR + c % CPR] = pack8(y);
+    const int64_t row = (l * p.n_total + tok) * p.heads + h0;
+    rotate_rows<CPR, WHOLE>(p.r, p.X + row * CPR, p.out + row * CPR, CPR, min(head_block, p.heads - h0), tok,
+                            p.segs[lo].pos0 + tok - p.segs[lo].tok0);
 }
 
-// K's rows rotated and V's copied into their slots, and Q's rows rotated: `rows` of each token, Hkv and then Hq.
-template <typename Params, int CPR>
-__global__ void __launch_bounds__(256) append_rope_kernel(const __grid_constant__ Params p, int64_t chunks)
+template <typename Block>
+__device__ __forceinline__ void enter_pages(const Block &a)
+{
+    for (int s = 0; s < a.n_segs; ++s) {
+        const AppendSeg &sg = a.segs[s];
+        for (int i = threadIdx.x; i < sg.n_new; i += blockDim.x)
+            a.page_table[sg.table_row + sg.first_new_lp + i] = a.new_pages[sg.new0 + i];
+        if (threadIdx.x == 0) a.seq_len[sg.seq] = static_cast<int64_t>(sg.len0) + sg.n_tokens;
+    }
+}
+
+// A warp per token, layer and one of: K's rows and V's, into their slots, or head_block of Q's.
+template <typename Params, int CPR, bool WHOLE>
+__global__ void __launch_bounds__(kRowThreads) append_rope_kernel(const __grid_constant__ Params p, int head_blocks, int head_block)
 {
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     const auto &a = p.a;
-    if (blockIdx.x == 0) {
-        for (int s = 0; s < a.n_segs; ++s) {
-            const AppendSeg &sg = a.segs[s];
-            for (int i = threadIdx.x; i < sg.n_new; i += 256)
-                a.page_table[sg.table_row + sg.first_new_lp + i] = a.new_pages[sg.new0 + i];
-            if (threadIdx.x == 0) a.seq_len[sg.seq] = static_cast<int64_t>(sg.len0) + sg.n_tokens;
-        }
-    }
-    const int heads = a.hkv + (p.c.Q ? p.c.hq : 0);
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const bool on = c < chunks;
-    const int64_t r = on ? c / CPR : 0;
-    const int chunk = static_cast<int>(c % CPR);
-    const int h = static_cast<int>(r % heads);
-    const int64_t lt = r / heads;
-    const int t = static_cast<int>(lt % a.seg_tokens);
-    const int64_t l = lt / a.seg_tokens;
+    if (blockIdx.x == 0) enter_pages(a);
+    int64_t r = static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5);
+    const int part = static_cast<int>(r % (1 + head_blocks));
+    r /= 1 + head_blocks;
+    const int t = static_cast<int>(r % a.seg_tokens);
+    const int64_t l = r / a.seg_tokens;
+    if (l >= a.L) return;
     const AppendSeg &sg = a.segs[find_seg(a.segs, a.n_segs, t)];
     const int local = t - sg.cum0, pos = sg.len0 + local;
-    const int64_t tok = sg.tok0 + local;
-    const bool is_q = h >= a.hkv;
-    const int64_t src = is_q ? ((l * a.n_total + tok) * p.c.hq + (h - a.hkv)) * CPR : ((l * a.n_total + tok) * a.hkv + h) * CPR;
-    float y[8];
-    if (on) rope_chunk(p.c.r, (is_q ? p.c.Q : a.K) + src, chunk, tok, pos, y);
-    __syncwarp();
-    if (!on) return;
-    if (is_q) {
-        p.c.Q_out[src + chunk] = pack8(y);
+    const int64_t tok = sg.tok0 + local, lt = l * a.n_total + tok;
+    if (part > 0) {
+        const int h0 = (part - 1) * head_block;
+        const int64_t at = (lt * p.c.hq + h0) * CPR;
+        rotate_rows<CPR, WHOLE>(p.c.r, p.c.Q + at, p.c.Q_out + at, CPR, min(head_block, p.c.hq - h0), tok, pos);
         return;
     }
     const int lp = pos / a.ps;
     const int page = lp < sg.first_new_lp ? sg.last_page : a.new_pages[sg.new0 + (lp - sg.first_new_lp)];
-    const int64_t dst = (((l * a.num_pages + page) * a.hkv + h) * a.ps + (pos - lp * a.ps)) * CPR + chunk;
-    a.k_pool[dst] = pack8(y);
-    a.v_pool[dst] = a.V[src + chunk];
+    const int64_t src = lt * a.hkv * CPR, stride = static_cast<int64_t>(a.ps) * CPR;  // between a slot's heads
+    const int64_t dst = ((l * a.num_pages + page) * a.hkv * a.ps + (pos - lp * a.ps)) * CPR;
+    copy_rows<CPR>(a.V + src, a.v_pool + dst, stride, a.hkv);
+    rotate_rows<CPR, WHOLE>(p.c.r, a.K + src, a.k_pool + dst, stride, a.hkv, tok, pos);
 }
 
 cudaLaunchConfig_t serial_config(int64_t blocks, unsigned threads, cudaStream_t st, cudaLaunchAttribute *attr)
@@ -148,40 +296,28 @@ cudaLaunchConfig_t serial_config(int64_t blocks, unsigned threads, cudaStream_t 
 }
 
 // Page by page (append_q8_kernel): the new rows of K rotated in 32 bits, so that a value is rounded once, to its code.
-template <typename Params, int CPR, int NC>
-__global__ void __launch_bounds__(kQ8Block) append_rope_q8_kernel(const __grid_constant__ Params p, int threads, int page_blocks)
+template <typename Params, int CPR, int NC, bool WHOLE>
+__global__ void __launch_bounds__(kQ8Block) append_rope_q8_kernel(const __grid_constant__ Params p, int threads, int page_blocks, int tokens,
+                                                                  int head_blocks, int head_block)
 {
     __shared__ uint32_t s_max[kQ8Block / 32];
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     const auto &a = p.a;
     constexpr int HD = CPR * 8;
-    if (static_cast<int>(blockIdx.x) >= page_blocks) {  // Q's rows
-        const int64_t c = static_cast<int64_t>(blockIdx.x - page_blocks) * kQ8Block + threadIdx.x;
-        int n_tok = 0;
-        for (int s = 0; s < a.n_segs; ++s) n_tok += a.segs[s].n_tokens;
-        const bool on = c < static_cast<int64_t>(a.L) * n_tok * p.c.hq * CPR;
-        const int64_t r = on ? c / CPR : 0;
-        const int h = static_cast<int>(r % p.c.hq);
-        const int64_t lt = r / p.c.hq;
-        int t = static_cast<int>(lt % n_tok), s = 0;
+    if (static_cast<int>(blockIdx.x) >= page_blocks) {  // Q's rows, a warp per token, layer and block of heads
+        int64_t r = static_cast<int64_t>(blockIdx.x - page_blocks) * (kQ8Block / 32) + (threadIdx.x >> 5);
+        const int h0 = static_cast<int>(r % head_blocks) * head_block;
+        r /= head_blocks;
+        int t = static_cast<int>(r % tokens), s = 0;
+        const int64_t l = r / tokens;
+        if (l >= a.L) return;
         for (; t >= a.segs[s].n_tokens; ++s) t -= a.segs[s].n_tokens;
-        const int64_t tok = a.segs[s].tok0 + t;
-        const int64_t src = (((lt / n_tok) * a.n_total + tok) * p.c.hq + h) * CPR;
-        float y[8];
-        if (on) rope_chunk(p.c.r, p.c.Q + src, static_cast<int>(c % CPR), tok, a.segs[s].len0 + t, y);
-        __syncwarp();
-        if (on) p.c.Q_out[src + c % CPR] = pack8(y);
+        const int64_t tok = a.segs[s].tok0 + t, at = ((l * a.n_total + tok) * p.c.hq + h0) * CPR;
+        rotate_rows<CPR, WHOLE>(p.c.r, p.c.Q + at, p.c.Q_out + at, CPR, min(head_block, p.c.hq - h0), tok, a.segs[s].len0 + t);
         return;
     }
-    if (blockIdx.x == 0) {
-        for (int s = 0; s < a.n_segs; ++s) {
-            const AppendSeg &sg = a.segs[s];
-            for (int i = threadIdx.x; i < sg.n_new; i += kQ8Block)
-                a.page_table[sg.table_row + sg.first_new_lp + i] = a.new_pages[sg.new0 + i];
-            if (threadIdx.x == 0) a.seq_len[sg.seq] = static_cast<int64_t>(sg.len0) + sg.n_tokens;
-        }
-    }
+    if (blockIdx.x == 0) enter_pages(a);
     const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kQ8Block / threads) + threadIdx.x / threads;
     const bool on = unit < static_cast<int64_t>(a.L) * a.seg_tokens * a.hkv;
     const int64_t u = on ? unit : 0;
@@ -216,7 +352,8 @@ __global__ void __launch_bounds__(kQ8Block) append_rope_q8_kernel(const __grid_c
                                    } else {
                                        const int64_t tok = tok0 + row;
                                        const int64_t s = ((l * a.n_total + tok) * a.hkv + h) * CPR;
-                                       rope_chunk(p.c.r, a.K + s, col8, tok, pos0 + row, k);
+                                       if constexpr (WHOLE) rope_chunk_whole(p.c.r, a.K + s, col8, tok, pos0 + row, k);
+                                       else rope_chunk(p.c.r, a.K + s, col8, tok, pos0 + row, k);
                                        v = a.V[s + col8];
                                    }
                                });
@@ -224,32 +361,40 @@ __global__ void __launch_bounds__(kQ8Block) append_rope_q8_kernel(const __grid_c
 
 constexpr int kSmallSegs = 16, kSmallPages = 128;  // the small parameter block (as in pe_kv.cu)
 
-template <typename Params>
-cudaError_t launch_append_rope_t(bool q8, int head_dim, const Params &p, cudaStream_t st)
+// Heads of a block of rows: all, or fewer (a multiple of what a warp reads at once) until the warps are 16 an SM.
+int block_of_heads(int64_t token_layers, int heads, int cpr)
+{
+    const int least = 64 / cpr;  // rows of a warp
+    int hb = (heads + least - 1) / least * least;
+    while (hb > least && token_layers * ((heads + hb - 1) / hb) < 152 * 16) hb = (hb / 2 + least - 1) / least * least;
+    return hb;
+}
+
+template <typename Params, int CPR, bool WHOLE>
+cudaError_t launch_append_rope_t(bool q8, const Params &p, cudaStream_t st)
 {
     cudaLaunchAttribute attr;
-    if (!q8) {
-        const int64_t chunks = static_cast<int64_t>(p.a.L) * p.a.seg_tokens * (p.a.hkv + (p.c.Q ? p.c.hq : 0)) * (head_dim / 8);
-        const cudaLaunchConfig_t cfg = serial_config((chunks + 255) / 256, 256, st, &attr);
-        return head_dim == 128 ? cudaLaunchKernelEx(&cfg, append_rope_kernel<Params, 16>, p, chunks)
-                               : cudaLaunchKernelEx(&cfg, append_rope_kernel<Params, 8>, p, chunks);
-    }
-    const int elems = p.a.ps * head_dim, threads = q8_unit_threads(elems), nc = q8_unit_chunks(elems);
-    const int64_t units = static_cast<int64_t>(p.a.L) * p.a.seg_tokens * p.a.hkv;
-    const int64_t page_blocks = (units * threads + kQ8Block - 1) / kQ8Block;
     int64_t tokens = 0;
     for (int i = 0; i < p.a.n_segs; ++i) tokens += p.a.segs[i].n_tokens;
-    const int64_t q_blocks = p.c.Q ? (p.a.L * tokens * p.c.hq * (head_dim / 8) + kQ8Block - 1) / kQ8Block : 0;
-    if (page_blocks + q_blocks > INT32_MAX) return cudaErrorInvalidValue;
-    const cudaLaunchConfig_t cfg = serial_config(page_blocks + q_blocks, kQ8Block, st, &attr);
-    const int pb = static_cast<int>(page_blocks);
-    if (head_dim == 128) {
-        if (nc == 8) return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, 16, 8>, p, threads, pb);
-        return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, 16, 4>, p, threads, pb);
+    const int64_t lt = p.a.L * tokens;
+    const int hb = p.c.Q ? block_of_heads(lt, p.c.hq, CPR) : 1, nb = p.c.Q ? (p.c.hq + hb - 1) / hb : 0;
+    if (!q8) {
+        const int64_t blocks = (lt * (1 + nb) + kRowThreads / 32 - 1) / (kRowThreads / 32);
+        if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+        const cudaLaunchConfig_t cfg = serial_config(blocks, kRowThreads, st, &attr);
+        return cudaLaunchKernelEx(&cfg, append_rope_kernel<Params, CPR, WHOLE>, p, nb, hb);
     }
-    if (nc == 8) return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, 8, 8>, p, threads, pb);
-    if (nc == 4) return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, 8, 4>, p, threads, pb);
-    return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, 8, 2>, p, threads, pb);
+    const int elems = p.a.ps * CPR * 8, threads = q8_unit_threads(elems), nc = q8_unit_chunks(elems);
+    const int64_t units = static_cast<int64_t>(p.a.L) * p.a.seg_tokens * p.a.hkv;
+    const int64_t page_blocks = (units * threads + kQ8Block - 1) / kQ8Block;
+    const int64_t blocks = page_blocks + (lt * nb + kQ8Block / 32 - 1) / (kQ8Block / 32);
+    if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+    const cudaLaunchConfig_t cfg = serial_config(blocks, kQ8Block, st, &attr);
+    const int pb = static_cast<int>(page_blocks), n = static_cast<int>(tokens);
+    if (nc == 8) return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, CPR, 8, WHOLE>, p, threads, pb, n, std::max(1, nb), hb);
+    if (CPR == 16 || nc == 4)
+        return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, CPR, 4, WHOLE>, p, threads, pb, n, std::max(1, nb), hb);
+    return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, CPR, 2, WHOLE>, p, threads, pb, n, std::max(1, nb), hb);
 }
 
 template <int SEGS, int PAGES>
@@ -262,7 +407,10 @@ cudaError_t launch_sized(bool q8, int head_dim, const AppendParams &a, const Rop
     std::memcpy(static_cast<void *>(&p.a), static_cast<const void *>(&a), offsetof(AppendParams, segs));
     std::copy(a.segs, a.segs + a.n_segs, p.a.segs);
     std::copy(a.new_pages, a.new_pages + a.n_new, p.a.new_pages);
-    return launch_append_rope_t(q8, head_dim, p, st);
+    const bool whole = rope.r.n_pairs % 8 == 0;
+    using P = AppendRopeParamsT<SEGS, PAGES>;
+    if (head_dim == 128) return whole ? launch_append_rope_t<P, 16, true>(q8, p, st) : launch_append_rope_t<P, 16, false>(q8, p, st);
+    return whole ? launch_append_rope_t<P, 8, true>(q8, p, st) : launch_append_rope_t<P, 8, false>(q8, p, st);
 }
 
 }  // namespace
@@ -273,13 +421,23 @@ cudaError_t launch_append_rope(bool q8, int head_dim, const AppendParams &a, con
     return launch_sized<kMaxSegs, kAppendMaxPages>(q8, head_dim, a, rope, st);
 }
 
+template <int CPR>
+static cudaError_t launch_rotate_t(const RotateParams &p, cudaStream_t st)
+{
+    const int64_t lt = static_cast<int64_t>(p.layers) * p.n_tokens;
+    if (lt <= 0) return cudaSuccess;
+    const int hb = block_of_heads(lt, p.heads, CPR), nb = (p.heads + hb - 1) / hb;
+    const int64_t blocks = (lt * nb + kRowThreads / 32 - 1) / (kRowThreads / 32);
+    if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = serial_config(blocks, kRowThreads, st, &attr);
+    return p.r.n_pairs % 8 == 0 ? cudaLaunchKernelEx(&cfg, rotate_kernel<CPR, true>, p, nb, hb)
+                                : cudaLaunchKernelEx(&cfg, rotate_kernel<CPR, false>, p, nb, hb);
+}
+
 cudaError_t launch_rotate(int head_dim, const RotateParams &p, cudaStream_t st)
 {
-    const int64_t chunks = static_cast<int64_t>(p.layers) * p.n_tokens * p.heads * (head_dim / 8);
-    if (chunks <= 0) return cudaSuccess;
-    cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = serial_config((chunks + 255) / 256, 256, st, &attr);
-    return head_dim == 128 ? cudaLaunchKernelEx(&cfg, rotate_kernel<16>, p, chunks) : cudaLaunchKernelEx(&cfg, rotate_kernel<8>, p, chunks);
+    return head_dim == 128 ? launch_rotate_t<16>(p, st) : launch_rotate_t<8>(p, st);
 }
 
 }  // namespace pe
