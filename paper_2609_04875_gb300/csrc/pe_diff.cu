@@ -2,99 +2,544 @@
 // 2j and 2j + 1 (j = i / group): their keys, one head a map, and side by side their values, of width 2d.
 //     A_m = softmax(scale q_m K_{2j+m}^T),  O = (A_0 - lambda_i A_1) [V_2j | V_2j+1],
 //     out = gain O / sqrt(mean(O^2) + eps)   (or O, without a gain)
+//
+// One pass over keys and values for both maps: the M side of the products holds 64 rows of each map, the maps of the same
+// queries.  Per tile of 64 keys
+//     S [128 x 128]  = Q [128 x d] . [K_2j ; K_2j+1]^T        (a row uses the 64 columns of its own map)
+//     O [128 x 2d]  += P [128 x 64] . [V_2j | V_2j+1]         (A = P from TMEM)
+// so half of S is not used, and where there are few rows most of M is not; both cost less than the keys' way from memory
+// (64 keys, d = 128: 64 KB, 2800 cycles of an SM's share of HBM; its MMAs 1024).
+//
+// Work is cut into equal stretches of tiles, a CTA each (pe_internal.h); every piece writes O / l and its log-sum-exp, and
+// the merge joins a row's pieces of both maps, subtracts and norms.
+#include <algorithm>
+
 #include "dev_common.cuh"
+#include "q8.cuh"
 
 namespace pe {
 
 namespace {
 
-// A block per query row and head: each warp takes every eighth key, with sums of its own; the block's first warp joins them.
+constexpr float kTileSumLimit = 1.8446744e19f;  // 2^64: larger tile sums move the reference (pe_attn.cu)
+constexpr int kDiffThreads = 288;               // warps 0-3 softmax, 4-7 producers, 8 MMA
+
 template <int HD>
-__global__ void __launch_bounds__(256) diff_attn_kernel(const __grid_constant__ DiffParams p)
-{
-    constexpr int E = HD / 32, W = 2 * HD / 32;  // columns of q and of O that a lane holds
-    __shared__ float s_m[2][8], s_l[2][8], s_o[2][8][2 * HD];
-    ptx::griddep_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int i = static_cast<int>(blockIdx.y), j = i / p.group;
-    int row = static_cast<int>(blockIdx.x), si = 0;
-    while (row >= p.seqs[si].n_q) row -= p.seqs[si++].n_q;
-    const DiffSeq &sq = p.seqs[si];
-    const int keys = sq.n_keys - sq.n_q + row + 1;
-    const int64_t q_row = sq.q_row0 + row;
-    float q[2][E], o[2][W], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    for (int x = 0; x < 2; ++x) {
-        for (int e = 0; e < E; ++e) q[x][e] = __bfloat162float(p.q[(q_row * p.hq + 2 * i + x) * HD + e * 32 + lane]);
-        for (int w = 0; w < W; ++w) o[x][w] = 0.f;
+struct DiffCfg {
+    static constexpr int kRegions = HD / 64;                  // 128-byte swizzle atoms along d
+    static constexpr int kStages = HD == 128 ? 3 : 6;
+    static constexpr int kQBytes = 128 * HD * 2;
+    static constexpr int kKBytes = 2 * kDiffKeys * HD * 2;    // both maps' keys of a tile
+    static constexpr int kKRegion = 2 * kDiffKeys * 128;
+    static constexpr int kVBytes = kDiffKeys * 2 * HD * 2;
+    static constexpr int kVRegion = kDiffKeys * 128;
+    static constexpr int kOffK = kQBytes;
+    static constexpr int kOffV = kOffK + kStages * kKBytes;
+    static constexpr int kOffBar = kOffV + kStages * kVBytes;
+    // k_full, k_empty, v_full, v_empty [stages]; q_full, edge; s_full, p_full, o_done [2]
+    static constexpr int kNumBars = 4 * kStages + 2 + 6;
+    static constexpr int kOffMisc = kOffBar + kNumBars * 8;   // tmem slot, abort flag, keys not finite [2]
+    static constexpr int kDynSmem = kOffMisc + 16 + 1024;
+    static constexpr int kTmemO = 256;                        // S at 0 and 128, P over S
+    static constexpr uint32_t kTmemCols = 512;
+    static_assert(kDynSmem <= 232448, "shared memory budget");
+};
+
+// A CTA's pieces, one after another: every role walks them alike.
+struct DiffWalk {
+    const DiffParams &p;
+    int u, t, u1, t1;  // next piece, end of the stretch
+    int si, pair, block, t0, n, slot;
+    __device__ __forceinline__ DiffWalk(const DiffParams &p_, int cta) : p(p_)
+    {
+        u = p.start[cta].u;
+        t = p.start[cta].t;
+        u1 = p.start[cta + 1].u;
+        t1 = p.start[cta + 1].t;
     }
-    for (int k = warp; k < keys; k += 8) {
-        const int page = p.page_table[sq.table_row + k / p.ps];
-        if (page < 0 || page >= p.num_pages) continue;
-        const int64_t at = (((static_cast<int64_t>(p.layer) * p.num_pages + page) * p.hkv + 2 * j) * p.ps + k % p.ps) * HD;
-        const int64_t next = static_cast<int64_t>(p.ps) * HD;  // the same token of kv-head 2j + 1
-        float v[W];
-        for (int w = 0; w < W; ++w) v[w] = __bfloat162float(p.v_pool[at + (w * 32 / HD) * next + (w * 32 % HD) + lane]);
-        for (int x = 0; x < 2; ++x) {
-            float s = 0.f;
-            for (int e = 0; e < E; ++e) s += q[x][e] * __bfloat162float(p.k_pool[at + x * next + e * 32 + lane]);
-            for (int w = 16; w; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
-            s *= p.scale_log2;
-            const float m_new = fmaxf(m[x], s);
-            if (m_new == -INFINITY && s == -INFINITY) continue;  // (a NaN goes on)
-            const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - m_new), pw = ex2(s - m_new);
-            l[x] = l[x] * f + pw;
-            for (int w = 0; w < W; ++w) o[x][w] = o[x][w] * f + pw * v[w];
-            m[x] = m_new;
+    // The next piece with tiles [t0, t0 + n), or false.
+    __device__ __forceinline__ bool next(int cta)
+    {
+        while (u < u1 || (u == u1 && t < t1)) {
+            int lo = 0, hi = p.n_seqs - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (p.seqs[mid].unit0 <= u) lo = mid; else hi = mid - 1;
+            }
+            si = lo;
+            const int local = u - p.seqs[si].unit0;
+            block = local % p.seqs[si].n_blocks;
+            pair = local / p.seqs[si].n_blocks;
+            slot = u + cta;
+            t0 = t;
+            n = (u == u1 ? t1 : diff_tiles(p.seqs[si], p.group, block)) - t;
+            ++u;
+            t = 0;
+            if (n > 0) return true;
+        }
+        return false;
+    }
+};
+
+template <int HD>
+__global__ void __launch_bounds__(kDiffThreads, 1)
+    diff_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                     const __grid_constant__ DiffParams p)
+{
+    using C = DiffCfg<HD>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = ptx::smem_addr(smem_raw);
+    const uint32_t sbase = (raw + 1023u) & ~1023u;
+    uint8_t *smem = smem_raw + (sbase - raw);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cta = static_cast<int>(blockIdx.x);
+
+    const uint32_t b_k_full = sbase + C::kOffBar;
+    const uint32_t b_k_empty = b_k_full + 8 * C::kStages;
+    const uint32_t b_v_full = b_k_empty + 8 * C::kStages;
+    const uint32_t b_v_empty = b_v_full + 8 * C::kStages;
+    const uint32_t b_q_full = b_v_empty + 8 * C::kStages;
+    const uint32_t b_edge = b_q_full + 8;      // the softmax threads among themselves
+    const uint32_t b_s_full = b_edge + 8;      // [2]
+    const uint32_t b_p_full = b_s_full + 16;   // [2]
+    const uint32_t b_o_done = b_p_full + 16;   // [2]
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::kOffMisc);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::kOffMisc + 4);
+    uint32_t *odd_keys = reinterpret_cast<uint32_t *>(smem + C::kOffMisc + 8);  // [2]
+    const WaitCtx wctx{abort_flag, p.status};
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::kStages; ++s) {
+            ptx::mbar_init(b_k_full + 8 * s, 2);
+            ptx::mbar_init(b_k_empty + 8 * s, 1);
+            ptx::mbar_init(b_v_full + 8 * s, 2);
+            ptx::mbar_init(b_v_empty + 8 * s, 1);
+        }
+        ptx::mbar_init(b_q_full, 128);
+        ptx::mbar_init(b_edge, 128);
+        for (int s = 0; s < 2; ++s) {
+            ptx::mbar_init(b_s_full + 8 * s, 1);
+            ptx::mbar_init(b_p_full + 8 * s, 128);
+            ptx::mbar_init(b_o_done + 8 * s, 1);
+        }
+        *abort_flag = 0;
+        odd_keys[0] = odd_keys[1] = 0;
+        ptx::fence_barrier_init();
+        ptx::fence_proxy_async_smem();
+        ptx::prefetch_tensormap(&tm_k);
+        ptx::prefetch_tensormap(&tm_v);
+    }
+    if (warp == 8) {
+        ptx::tmem_alloc(ptx::smem_addr(tmem_slot), C::kTmemCols);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    // everything before this overlapped the kernel before; the merge's blocks may come in from here on
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
+
+    DiffWalk w(p, cta);
+    int i = 0;  // tiles of the pieces before
+    if (warp >= 4 && warp < 8) {
+        // =================================================== producers: K of a map, or V of a kv-head
+        const bool is_v = warp >= 6;
+        const int head = warp & 1;
+        const CUtensorMap *map = is_v ? &tm_v : &tm_k;
+        const uint32_t b_full = is_v ? b_v_full : b_k_full, b_empty = is_v ? b_v_empty : b_k_empty;
+        const int rows = min(p.ps, kDiffKeys);                 // of a box
+        const int n_ops = kDiffKeys / rows * C::kRegions;      // <= 16
+        const int op_page = lane / C::kRegions, op_reg = lane % C::kRegions;
+        const bool on = lane < n_ops;
+        const uint32_t base = sbase + (is_v ? C::kOffV + (head * C::kRegions + op_reg) * C::kVRegion
+                                            : C::kOffK + op_reg * C::kKRegion + head * kDiffKeys * 128) + op_page * rows * 128;
+        bool ok = true;
+        while (ok && w.next(cta)) {
+            const DiffSeq &sq = p.seqs[w.si];
+            const int kvh = 2 * w.pair + head;
+            auto row_of = [&](int k) -> int {  // of the pool, of this lane's box of tile k
+                const int key = (w.t0 + k) * kDiffKeys + op_page * rows, lp = key >> p.log_ps;
+                const int page = on && lp < sq.n_pages ? p.page_table[sq.table_row + lp] : -1;
+                return page >= 0 && page < p.num_pages ? (((p.layer * p.num_pages + page) * p.hkv + kvh) << p.log_ps) + (key & (p.ps - 1))
+                                                       : p.oob_row;
+            };
+            int y = row_of(0);
+            for (int k = 0; k < w.n; ++k, ++i) {
+                const int next = k + 1 < w.n ? row_of(k + 1) : 0, s = i % C::kStages;
+                if (i >= C::kStages && !wait_bar_warp(b_empty + 8 * s, ((i / C::kStages) - 1) & 1, wctx)) { ok = false; break; }
+                if (lane == 0) ptx::mbar_arrive_expect_tx(b_full + 8 * s, kDiffKeys * HD * 2);
+                __syncwarp();
+                if (on) ptx::tma_load_2d(base + s * (is_v ? C::kVBytes : C::kKBytes), map, op_reg * 64, y, b_full + 8 * s);
+                y = next;
+            }
+        }
+        __syncwarp();
+        if (*abort_flag && lane == 0) {  // a bounded chance for copies in flight to land
+            const uint64_t g0 = ptx::globaltimer();
+            for (int k = max(0, i - C::kStages); k < i; ++k)
+                while (!ptx::mbar_try_wait(b_full + 8 * (k % C::kStages), (k / C::kStages) & 1) && ptx::globaltimer() - g0 < 4000000ull) {}
+        }
+    } else if (warp == 8) {
+        // =================================================== MMA (the converged warp; one elected lane issues)
+        constexpr uint32_t kIdescS = ptx::idesc_bf16_f32(128, 2 * kDiffKeys, false);
+        constexpr uint32_t kIdescO = ptx::idesc_bf16_f32(128, 2 * HD, true);
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint64_t q_desc = ptx::smem_desc_sw128(sbase, 16, 1024);
+        const uint64_t k_desc = ptx::smem_desc_sw128(sbase + C::kOffK, 16, 1024);
+        const uint64_t v_desc = ptx::smem_desc_sw128(sbase + C::kOffV, C::kVRegion, 1024);
+        auto full = [&](uint32_t bar, int j) { return wait_bar_warp(bar + 8 * (j % C::kStages), (j / C::kStages) & 1, wctx); };
+        auto issue_s = [&](int j) {
+            if (!full(b_k_full, j)) return false;
+            ptx::tc_fence_after();
+            const uint64_t kd = k_desc + (j % C::kStages) * (C::kKBytes >> 4);
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk)
+                mma_bf16_warp(tm + 128 * (j & 1), q_desc + (((kk >> 2) * (128 * 128) + (kk & 3) * 32) >> 4),
+                              kd + (((kk >> 2) * C::kKRegion + (kk & 3) * 32) >> 4), kIdescS, kk > 0 ? 1u : 0u);
+            mma_commit_warp(b_s_full + 8 * (j & 1));
+            mma_commit_warp(b_k_empty + 8 * (j % C::kStages));
+            return true;
+        };
+        bool ok = true;
+        for (int piece = 0; ok && w.next(cta); ++piece) {
+            const int n = __shfl_sync(0xffffffffu, w.n, 0);
+            if (!wait_bar_warp(b_q_full, piece & 1, wctx)) break;
+            ok = issue_s(i) && (n < 2 || issue_s(i + 1));
+            for (int k = 0; ok && k < n; ++k, ++i) {
+                if (!full(b_v_full, i) || !wait_bar_warp(b_p_full + 8 * (i & 1), (i >> 1) & 1, wctx)) { ok = false; break; }
+                ptx::tc_fence_after();
+                const uint64_t vd = v_desc + (i % C::kStages) * (C::kVBytes >> 4);
+#pragma unroll
+                for (int kk = 0; kk < kDiffKeys / 16; ++kk)
+                    mma_bf16_ts_warp(tm + C::kTmemO, tm + 128 * (i & 1) + kk * 8, vd + (kk * 16 * 128 >> 4), kIdescO,
+                                     (k > 0 || kk > 0) ? 1u : 0u);
+                mma_commit_warp(b_o_done + 8 * (i & 1));
+                mma_commit_warp(b_v_empty + 8 * (i % C::kStages));
+                if (k + 2 < n) ok = issue_s(i + 2);  // (P(i), over S(i), is read by then)
+            }
+        }
+    } else {
+        // =================================================== softmax: thread r owns row r (TMEM lane r)
+        const int row = threadIdx.x, m = row / kDiffRows;
+        const uint32_t lane_off = static_cast<uint32_t>(warp * 32) << 16;
+        const float2 sl2 = make_float2(p.scale_log2, p.scale_log2);
+        bool ok = true;
+        int met = 0;
+        auto meet = [&]() {  // of all softmax threads; bounded, as every wait
+            ptx::mbar_arrive(b_edge);
+            return wait_bar_warp(b_edge, met++ & 1, wctx);
+        };
+        while (ok && w.next(cta)) {
+            const DiffSeq &sq = p.seqs[w.si];
+            const int r = w.block * kDiffRows + (row & (kDiffRows - 1));  // packed row of its map
+            const int qi = r / p.group, head = 2 * (w.pair * p.group + r - qi * p.group) + m;
+            const bool valid = qi < sq.n_q, any = __any_sync(0xffffffffu, valid);
+            const int pos = sq.n_keys - sq.n_q + qi;
+            const int pos_first = sq.n_keys - sq.n_q + w.block * kDiffRows / p.group;
+            // Q's row into shared memory (the S products of the piece before are done), 16-byte chunks swizzled by row & 7
+            if (valid) {
+                const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (static_cast<int64_t>(sq.q_row0 + qi) * p.hq + head) * HD);
+#pragma unroll
+                for (int c = 0; c < HD / 8; ++c) {
+                    const uint4 v = __ldg(src + c);
+                    *reinterpret_cast<uint4 *>(smem + (c >> 3) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+                }
+            }
+            ptx::fence_proxy_async_smem();
+            ptx::mbar_arrive(b_q_full);
+            float m_ref = -INFINITY, l = 0.f;
+            for (int k = 0; k < w.n; ++k, ++i) {
+                const int kbase = (w.t0 + k) * kDiffKeys;
+                const uint32_t tS = tmem + 128 * (i & 1) + lane_off;
+                const bool edge = kbase + kDiffKeys - 1 > pos_first;  // a row of the block does not see some key of the tile
+                if (edge) {
+                    // V of keys that some row does not see: 0 times an infinity or NaN would reach that row.  Such keys' V
+                    // become 0, and rows that see them NaN.
+                    if (!wait_bar_warp(b_v_full + 8 * (i % C::kStages), (i / C::kStages) & 1, wctx)) { ok = false; break; }
+                    const int key = row & 63;
+                    uint8_t *v = smem + C::kOffV + (i % C::kStages) * C::kVBytes + (row >> 6) * C::kRegions * C::kVRegion + key * 128;
+                    uint32_t odd = 0;
+#pragma unroll
+                    for (int c = 0; c < HD / 8; ++c)
+                        odd = max(odd, bf16x8_absmax(*reinterpret_cast<const uint4 *>(v + (c >> 3) * C::kVRegion + (((c & 7) ^ (key & 7)) << 4))));
+                    const bool is_odd = odd >= 0x7f80u;
+                    if (is_odd) atomicOr(&odd_keys[key >> 5], 1u << (key & 31));
+                    if (!meet()) { ok = false; break; }
+                    const uint64_t odd_mask = odd_keys[0] | static_cast<uint64_t>(odd_keys[1]) << 32;
+                    if (odd_mask) {
+                        if (is_odd)
+                            for (int c = 0; c < HD / 8; ++c)
+                                *reinterpret_cast<uint4 *>(v + (c >> 3) * C::kVRegion + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        ptx::fence_proxy_async_smem();
+                        const int sees = pos - kbase + 1;  // keys of the tile
+                        if (sees > 0 && (odd_mask & (sees >= 64 ? ~0ull : (1ull << sees) - 1))) l = NAN;
+                        if (!meet()) { ok = false; break; }  // the mask is read
+                        if (row < 2) odd_keys[row] = 0;
+                        if (!meet()) { ok = false; break; }  // and cleared
+                    }
+                }
+                if (!wait_bar_warp(b_s_full + 8 * (i & 1), (i >> 1) & 1, wctx)) { ok = false; break; }
+                ptx::tc_fence_after();
+                if (any) {
+                    float s[kDiffKeys];
+                    {
+                        float (&s0)[32] = *reinterpret_cast<float (*)[32]>(&s[0]);
+                        float (&s1)[32] = *reinterpret_cast<float (*)[32]>(&s[32]);
+                        ptx::tmem_ld32(tS + 64 * m, s0);
+                        ptx::tmem_ld32(tS + 64 * m + 32, s1);
+                        ptx::tmem_wait_ld();
+                    }
+                    if (edge) {
+#pragma unroll
+                        for (int c = 0; c < kDiffKeys; ++c)
+                            if (kbase + c > pos) s[c] = -INFINITY;
+                    }
+                    // weights against the row's reference, which moves only when a tile's sum passes 2^64 (pe_attn.cu); the
+                    // row is divided by the sum of its weights as rounded
+                    auto exp_tile = [&](float ref) -> float {
+                        const float2 nref = make_float2(-ref, -ref);
+                        float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+                        for (int ch = 0; ch < kDiffKeys / 32; ++ch) {
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int x = 0; x < 16; ++x) {
+                                const int c = ch * 32 + 2 * x;
+                                const float2 y = fma2(make_float2(s[c], s[c + 1]), sl2, nref);
+                                pk[x] = pack_bf16(ex2(y.x), ex2(y.y));
+                                acc[x & 3] = add2(acc[x & 3], unpack_bf16(pk[x]));
+                            }
+                            tmem_st16(tS + ch * 16, pk);
+                        }
+                        const float2 a = add2(add2(acc[0], acc[1]), add2(acc[2], acc[3]));
+                        return a.x + a.y;
+                    };
+                    float rs = 0.f;
+                    bool need = valid && m_ref == -INFINITY;
+                    if (!__all_sync(0xffffffffu, need)) {
+                        rs = exp_tile(m_ref == -INFINITY ? 0.f : m_ref);
+                        need = need || (valid && !(rs <= kTileSumLimit));
+                    }
+                    if (__any_sync(0xffffffffu, need)) {
+                        float mx[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) mx[x] = max3(s[x], s[4 + x], s[8 + x]);
+#pragma unroll
+                        for (int c = 12; c < 60; c += 8)
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], s[c + x], s[c + 4 + x]);
+                        const float mt = fmaxf(max3(mx[0], mx[1], mx[2]), max3(mx[3], fmaxf(s[60], s[61]), fmaxf(s[62], s[63])));
+                        const float m_new = fmaxf(m_ref, mt * sl2.x);
+                        if (k > 0 && __any_sync(0xffffffffu, need && m_ref != -INFINITY)) {
+                            // O holds P V of the tiles before once the last of them is done
+                            if (!wait_bar_warp(b_o_done + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, wctx)) { ok = false; break; }
+                            ptx::tc_fence_after();
+                            const float alpha = need && m_ref != -INFINITY ? ex2(m_ref - m_new) : 1.f;
+#pragma unroll 1
+                            for (int ch = 0; ch < 2 * HD / 16; ++ch) {
+                                uint32_t o[16];
+                                tmem_ld16(tmem + C::kTmemO + lane_off + ch * 16, o);
+                                ptx::tmem_wait_ld();
+#pragma unroll
+                                for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * alpha);
+                                tmem_st16(tmem + C::kTmemO + lane_off + ch * 16, o);
+                            }
+                            if (need) l *= alpha;
+                        }
+                        if (need) m_ref = m_new;
+                        ptx::tmem_wait_st();
+                        rs = exp_tile(m_ref == -INFINITY ? 0.f : m_ref);
+                    }
+                    l += rs;
+                    ptx::tmem_wait_st();
+                }
+                ptx::tc_fence_before();
+                ptx::mbar_arrive(b_p_full + 8 * (i & 1));
+            }
+            if (!ok || !wait_bar_warp(b_o_done + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, wctx)) break;
+            ptx::tc_fence_after();
+            if (any) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
+                const int64_t at = static_cast<int64_t>(w.slot) * 128 + row;
+                float4 *dst = reinterpret_cast<float4 *>(p.part + at * 2 * HD);
+#pragma unroll 1
+                for (int ch = 0; ch < 2 * HD / 32; ++ch) {
+                    float o[32];
+                    ptx::tmem_ld32(tmem + C::kTmemO + lane_off + ch * 32, o);
+                    ptx::tmem_wait_ld();
+                    if (valid && l != 0.f)
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            dst[ch * 8 + x] = make_float4(o[4 * x] * inv, o[4 * x + 1] * inv, o[4 * x + 2] * inv, o[4 * x + 3] * inv);
+                }
+                if (valid) p.part_lse[at] = l == 0.f ? -INFINITY : m_ref + __log2f(l);
+            }
+            ptx::tc_fence_before();
         }
     }
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, C::kTmemCols);
+    }
+}
+
+constexpr int kMergeWarps = 4;
+
+// A block per output row and head: warp x joins pieces x, x + 4, ... of both maps, lane t the columns 4t .. + 3 of every 128;
+// then the first warp the four.  A row's pieces are those of CTAs whose stretches meet its unit.
+template <int HD>
+__global__ void __launch_bounds__(32 * kMergeWarps) diff_combine_kernel(const __grid_constant__ DiffParams p)
+{
+    constexpr int V4 = 2 * HD / 128;  // float4 a lane
+    __shared__ float s_m[2][kMergeWarps], s_l[2][kMergeWarps];
+    __shared__ float4 s_o[2][kMergeWarps][2 * HD / 4];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int lo = 0, hi = p.n_seqs - 1;
+    const int id = static_cast<int>(blockIdx.x);
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.seqs[mid].out0 <= id) lo = mid; else hi = mid - 1;
+    }
+    const DiffSeq &sq = p.seqs[lo];
+    const int heads = p.hq / 2, local = id - sq.out0, qi = local / heads, head = local - qi * heads;
+    const int pair = head / p.group, r = qi * p.group + head - pair * p.group;
+    const int u = sq.unit0 + pair * sq.n_blocks + r / kDiffRows, row = r % kDiffRows;
+    lo = 0;
+    hi = p.n_ctas - 1;
+    while (lo < hi) {  // the last CTA whose stretch begins at or before the unit's first tile
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.start[mid].u < u || (p.start[mid].u == u && p.start[mid].t == 0)) lo = mid; else hi = mid - 1;
+    }
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float4 o[2][V4];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int v = 0; v < V4; ++v) o[x][v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = lo + warp; c < p.n_ctas && (c == lo || p.start[c].u == u); c += kMergeWarps) {
+        if (p.start[c].u == p.start[c + 1].u && p.start[c].t == p.start[c + 1].t) continue;  // nothing of the CTA's
+        const int64_t at = static_cast<int64_t>(u + c) * 128 + row;
+        float lse[2];
+        float4 y[2][V4];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            lse[x] = __ldcg(p.part_lse + at + x * kDiffRows);
+            const float4 *src = reinterpret_cast<const float4 *>(p.part + (at + x * kDiffRows) * 2 * HD);
+#pragma unroll
+            for (int v = 0; v < V4; ++v) y[x][v] = __ldcg(src + v * 32 + lane);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            if (lse[x] == -INFINITY) continue;  // (its row may hold anything)
+            const float mn = fmaxf(m[x], lse[x]);
+            const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - mn), g = ex2(lse[x] - mn);  // (NaN where lse is)
+            m[x] = mn;
+            l[x] = l[x] * f + g;
+#pragma unroll
+            for (int v = 0; v < V4; ++v)
+                o[x][v] = make_float4(o[x][v].x * f + y[x][v].x * g, o[x][v].y * f + y[x][v].y * g, o[x][v].z * f + y[x][v].z * g,
+                                      o[x][v].w * f + y[x][v].w * g);
+        }
+    }
+#pragma unroll
     for (int x = 0; x < 2; ++x) {
         if (lane == 0) {
             s_m[x][warp] = m[x];
             s_l[x][warp] = l[x];
         }
-        for (int w = 0; w < W; ++w) s_o[x][warp][w * 32 + lane] = o[x][w];
+#pragma unroll
+        for (int v = 0; v < V4; ++v) s_o[x][warp][v * 32 + lane] = o[x][v];
     }
     __syncthreads();
     if (warp > 0) return;
-    float r[W], sum = 0.f;
-    for (int w = 0; w < W; ++w) r[w] = 0.f;
+    float4 y[V4];
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < V4; ++v) y[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
     for (int x = 0; x < 2; ++x) {
-        float mx = -INFINITY, den = 0.f, acc[W];
-        for (int u = 0; u < 8; ++u) mx = fmaxf(mx, s_m[x][u]);
-        for (int w = 0; w < W; ++w) acc[w] = 0.f;
-        for (int u = 0; u < 8; ++u) {
-            const float f = s_m[x][u] == -INFINITY ? (s_l[x][u] == 0.f ? 0.f : s_l[x][u]) : ex2(s_m[x][u] - mx);
-            den += f * s_l[x][u];
-            if (f != 0.f)
-                for (int w = 0; w < W; ++w) acc[w] += f * s_o[x][u][w * 32 + lane];
+        float mx = -INFINITY, den = 0.f, f[kMergeWarps];
+#pragma unroll
+        for (int k = 0; k < kMergeWarps; ++k) mx = fmaxf(mx, s_m[x][k]);
+#pragma unroll
+        for (int k = 0; k < kMergeWarps; ++k) {
+            f[k] = s_l[x][k] == 0.f ? 0.f : ex2(s_m[x][k] - mx);
+            den += f[k] * s_l[x][k];
         }
-        const float inv = den == 0.f ? 0.f : 1.f / den, part = x ? -p.lambda[i] : 1.f;
-        for (int w = 0; w < W; ++w) r[w] += part * acc[w] * inv;
+        const float part = (x ? -p.lambda[head] : 1.f) * (den == 0.f ? 0.f : 1.f / den);
+#pragma unroll
+        for (int k = 0; k < kMergeWarps; ++k) {
+            const float g = f[k] * part;
+            if (f[k] == 0.f) continue;
+#pragma unroll
+            for (int v = 0; v < V4; ++v) {
+                const float4 z = s_o[x][k][v * 32 + lane];
+                y[v] = make_float4(y[v].x + g * z.x, y[v].y + g * z.y, y[v].z + g * z.z, y[v].w + g * z.w);
+            }
+        }
     }
     if (p.gain) {
-        for (int w = 0; w < W; ++w) sum += r[w] * r[w];
-        for (int w = 16; w; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+#pragma unroll
+        for (int v = 0; v < V4; ++v) sum += y[v].x * y[v].x + y[v].y * y[v].y + y[v].z * y[v].z + y[v].w * y[v].w;
+#pragma unroll
+        for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
         const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
-        for (int w = 0; w < W; ++w) r[w] *= f * p.gain[w * 32 + lane];
+#pragma unroll
+        for (int v = 0; v < V4; ++v) {
+            const float4 g = __ldg(reinterpret_cast<const float4 *>(p.gain) + v * 32 + lane);
+            y[v] = make_float4(y[v].x * f * g.x, y[v].y * f * g.y, y[v].z * f * g.z, y[v].w * f * g.w);
+        }
     }
-    for (int w = 0; w < W; ++w) p.out[(q_row * (p.hq / 2) + i) * 2 * HD + w * 32 + lane] = __float2bfloat16(r[w]);
+    uint2 *dst = reinterpret_cast<uint2 *>(p.out + (static_cast<int64_t>(sq.q_row0 + qi) * heads + head) * 2 * HD);
+#pragma unroll
+    for (int v = 0; v < V4; ++v) dst[v * 32 + lane] = make_uint2(pack_bf16(y[v].x, y[v].y), pack_bf16(y[v].z, y[v].w));
+}
+
+cudaLaunchConfig_t diff_config(int blocks, int threads, int smem, cudaStream_t st, cudaLaunchAttribute *attr)
+{
+    attr->id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr->val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cfg;
+}
+
+template <int HD>
+cudaError_t launch_diff_t(const CUtensorMap &k, const CUtensorMap &v, const DiffParams &p, cudaStream_t st)
+{
+    static std::atomic<uint64_t> configured{0};
+    cudaError_t e = set_dyn_smem_once(diff_attn_kernel<HD>, DiffCfg<HD>::kDynSmem, configured);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = diff_config(p.n_ctas, kDiffThreads, DiffCfg<HD>::kDynSmem, st, &attr);
+    return cudaLaunchKernelEx(&cfg, diff_attn_kernel<HD>, k, v, p);
 }
 
 }  // namespace
 
-cudaError_t launch_diff_attn(int head_dim, const DiffParams &p, int64_t rows, cudaStream_t st)
+cudaError_t launch_diff_attn(int head_dim, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const DiffParams &p, cudaStream_t st)
 {
-    if (rows <= 0) return cudaSuccess;
+    if (p.n_ctas <= 0) return cudaSuccess;
+    return head_dim == 128 ? launch_diff_t<128>(tm_k, tm_v, p, st) : launch_diff_t<64>(tm_k, tm_v, p, st);
+}
+
+cudaError_t launch_diff_combine(int head_dim, const DiffParams &p, cudaStream_t st)
+{
+    if (p.n_out <= 0) return cudaSuccess;
     cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(rows), static_cast<unsigned>(p.hq / 2));
-    cfg.blockDim = dim3(256);
-    cfg.stream = st;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_attn_kernel<128>, p) : cudaLaunchKernelEx(&cfg, diff_attn_kernel<64>, p);
+    const cudaLaunchConfig_t cfg = diff_config(p.n_out, 32 * kMergeWarps, 0, st, &attr);
+    return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_combine_kernel<128>, p) : cudaLaunchKernelEx(&cfg, diff_combine_kernel<64>, p);
 }
 
 }  // namespace pe

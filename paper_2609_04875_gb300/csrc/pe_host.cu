@@ -2286,7 +2286,63 @@ pe_status rope_params(const pe_cache *c, const pe_rope *rope, const int32_t *pos
 }
 
 // ---- differential attention
-pe_status run_diff(pe_cache *c, const std::vector<AttnItem> &items, int32_t layer, const void *Q, void *out, int32_t hq, float scale,
+// Queries [q_row0, q_row0 + n_q) of Q, the last of which sees n_keys keys.
+struct DiffItem {
+    int32_t seq;
+    int32_t q_row0, n_q, n_keys;
+};
+
+int64_t diff_slot_bytes(const pe_cache *c) { return 128 * (2 * static_cast<int64_t>(c->cfg.head_dim) + 1) * 4; }
+
+// A unit's cost besides its tiles, in tiles.
+constexpr int64_t kDiffUnitCost = 1;
+
+// One launch over the items, at most kMaxSegs: fills p's sequences and stretches.
+void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t max_ctas, DiffParams &p)
+{
+    p.n_seqs = p.n_out = 0;
+    int64_t work = 0, tiles = 0;
+    int32_t units = 0;
+    const int pairs = p.hkv / 2;
+    for (const DiffItem &it : items) {
+        DiffSeq &q = p.seqs[p.n_seqs++];
+        q.table_row = it.seq * c->cfg.max_pages_per_seq;
+        q.n_pages = static_cast<int32_t>(c->table[it.seq].size());
+        q.q_row0 = it.q_row0;
+        q.n_q = it.n_q;
+        q.n_keys = it.n_keys;
+        q.n_blocks = static_cast<int32_t>(ceil_div(static_cast<int64_t>(it.n_q) * p.group, kDiffRows));
+        q.unit0 = units;
+        q.out0 = p.n_out;
+        units += q.n_blocks * pairs;
+        p.n_out += it.n_q * (p.hq / 2);
+        int64_t one = 0;
+        for (int b = 0; b < q.n_blocks; ++b) one += diff_tiles(q, p.group, b);
+        tiles += one * pairs;
+        work += (one + q.n_blocks * kDiffUnitCost) * pairs;
+    }
+    // equal stretches of work; CTA c's begins at work * c / n
+    const int64_t n = std::min(tiles, max_ctas);
+    p.n_ctas = static_cast<int32_t>(n);
+    int64_t at = 0;  // work before the unit
+    int32_t u = 0, s = 0;
+    int64_t next = 0;  // the next CTA
+    for (s = 0; s < p.n_seqs; ++s) {
+        const DiffSeq &q = p.seqs[s];
+        for (int j = 0; j < pairs; ++j)
+            for (int b = 0; b < q.n_blocks; ++b, ++u) {
+                const int64_t w = diff_tiles(q, p.group, b) + kDiffUnitCost;
+                for (; next < n && work * next / n < at + w; ++next) {
+                    const int64_t t = work * next / n - at - kDiffUnitCost;
+                    p.start[next] = DiffStart{u, static_cast<int32_t>(std::max<int64_t>(0, t))};
+                }
+                at += w;
+            }
+    }
+    for (; next <= n; ++next) p.start[next] = DiffStart{u, 0};
+}
+
+pe_status run_diff(pe_cache *c, const std::vector<AttnItem> &all, int32_t layer, const void *Q, void *out, int32_t hq, float scale,
                    const float *lambda, const float *gain, float eps, cudaStream_t st)
 {
     DiffParams p;
@@ -2294,33 +2350,60 @@ pe_status run_diff(pe_cache *c, const std::vector<AttnItem> &items, int32_t laye
     p.page_table = c->d_table;
     p.q = static_cast<const __nv_bfloat16 *>(Q);
     p.out = static_cast<__nv_bfloat16 *>(out);
-    p.k_pool = static_cast<const __nv_bfloat16 *>(c->k_pool);
-    p.v_pool = static_cast<const __nv_bfloat16 *>(c->v_pool);
     p.lambda = lambda;
     p.gain = gain;
+    p.status = c->d_status;
     p.hq = hq;
     p.hkv = c->cfg.num_kv_heads;
     p.group = hq / p.hkv;
     p.layer = layer;
     p.num_pages = c->cfg.num_pages;
     p.ps = c->cfg.page_size;
+    while ((1 << p.log_ps) < p.ps) p.log_ps++;
+    p.oob_row = static_cast<int32_t>(c->pool_rows);
     p.scale_log2 = scale * 1.4426950408889634f;
     p.eps = eps;
-    for (size_t i = 0; i < items.size();) {
-        int64_t rows = 0;
-        for (p.n_seqs = 0; i < items.size() && p.n_seqs < kMaxSegs; ++i) {
-            const AttnItem &it = items[i];
-            if (it.n_q <= 0) continue;
-            p.seqs[p.n_seqs++] = DiffSeq{it.seq * c->cfg.max_pages_per_seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq])};
-            rows += it.n_q;
-        }
-        if (p.n_seqs == 0) continue;
+    // units that a launch's partials have room for, besides a slot a CTA
+    const int64_t slots = c->ws_bytes / diff_slot_bytes(c), pairs = p.hkv / 2;
+    const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>({c->num_sms, kMaxSkCtas, slots / 2}));
+    const int64_t room = (slots - ctas) / pairs;  // blocks
+    if (room < 1) return fail(PE_ERR_RANGE, "the workspace has no room for a launch's partials");
+    std::vector<DiffItem> items;
+    int64_t used = 0;
+    auto flush = [&]() -> pe_status {
+        if (items.empty()) return PE_OK;
+        plan_diff(c, items, ctas, p);
+        p.part = c->d_ws;
+        p.part_lse = c->d_ws + slots * 128 * 2 * c->cfg.head_dim;
         if (injected_failure(c)) return launch_fault("differential attention");
-        cudaError_t e = launch_diff_attn(c->cfg.head_dim, p, rows, st);
+        cudaError_t e = launch_diff_attn(c->cfg.head_dim, c->tm_kd, c->tm_vd, p, st);
         if (e != cudaSuccess) return cuda_fail(e, "differential attention launch");
         c->launches++;
+        if (injected_failure(c)) return launch_fault("differential attention's merge");
+        e = launch_diff_combine(c->cfg.head_dim, p, st);
+        if (e != cudaSuccess) return cuda_fail(e, "differential attention's merge launch");
+        c->launches++;
+        items.clear();
+        used = 0;
+        return PE_OK;
+    };
+    for (const AttnItem &it : all) {
+        const int32_t before = static_cast<int32_t>(c->len[it.seq]) - it.n_q;  // keys that the first query's see besides its own
+        for (int32_t done = 0; done < it.n_q;) {
+            // (whole queries; a block of them may be shared with none of the next piece's)
+            const int64_t fit = (room - used) * kDiffRows / p.group;
+            if (fit < 1 || items.size() == kMaxSegs) {
+                if (items.empty()) return fail(PE_ERR_RANGE, "the workspace has no room for a launch's partials");
+                if (pe_status s = flush()) return s;
+                continue;
+            }
+            const int32_t take = static_cast<int32_t>(std::min<int64_t>(fit, it.n_q - done));
+            items.push_back(DiffItem{it.seq, it.q_row0 + done, take, before + done + take});
+            used += ceil_div(static_cast<int64_t>(take) * p.group, kDiffRows);
+            done += take;
+        }
     }
-    return PE_OK;
+    return flush();
 }
 
 }  // namespace

@@ -14,6 +14,7 @@ constexpr int kBM = 128;               // query rows (GQA-packed) per attention 
 constexpr int kBN = 128;               // keys per attention tile
 constexpr int kMaxSegs = 64;           // sequences per append / attention launch
 constexpr int kMaxCropSegs = 256;      // sequences per crop launch
+constexpr int kMaxSkCtas = 160;        // >= SMs of the GPU: CTAs of the kernels that run one per SM
 constexpr int kAppendMaxPages = 3072;  // new page ids carried by one append launch
 
 // Device status word codes (pe_device_status).
@@ -97,24 +98,51 @@ struct RotateParams {
 };
 
 // ---------------------------------------------------------------- differential attention
+// Work units are (sequence, pair of kv-heads, block of kDiffRows query rows), numbered sequence by sequence, blocks fastest;
+// a unit's tiles are of kDiffKeys keys, up to what its last query sees.  CTA c takes the stretch from tile start[c].t of unit
+// start[c].u up to start[c + 1]; the piece of unit u that it computes is slot u + c of the partials (of two pieces in the
+// order of the stretches, the later one has the larger unit, the larger CTA, or both, so no two share a slot).
+constexpr int kDiffRows = 64;          // of each map; query * group + head-in-group
+constexpr int kDiffKeys = 64;
+
 struct DiffSeq {
     int32_t table_row;     // seq * max_pages_per_seq
+    int32_t n_pages;
     int32_t q_row0, n_q;   // rows of Q / out
     int32_t n_keys;        // the last query sees all of them
+    int32_t n_blocks;
+    int32_t unit0;
+    int32_t out0;          // first output of the launch: out0 + query * Hq / 2 + head
+};
+
+struct DiffStart {
+    int32_t u, t;
 };
 
 struct DiffParams {
     const int32_t *page_table;
     const __nv_bfloat16 *q;      // bf16 [rows][Hq][d]
     __nv_bfloat16 *out;          // bf16 [rows][Hq / 2][2 d]
-    const __nv_bfloat16 *k_pool, *v_pool;
     const float *lambda;         // [Hq / 2]
     const float *gain;           // [2 d], or null: no norm
-    int32_t n_seqs, hq, hkv, group, layer, num_pages, ps;
+    float *part;                 // partials: O / l fp32 [slots][128][2 d] (a map's kDiffRows rows, then the other's)
+    float *part_lse;             // [slots][128], log2 units
+    int32_t *status;
+    int32_t n_seqs, hq, hkv, group, layer, num_pages, ps, log_ps;
+    int32_t oob_row;             // a pool row past the end: boxes there read zeros
+    int32_t n_ctas, n_out;
     float scale_log2;            // softmax_scale * log2(e)
     float eps;
     DiffSeq seqs[kMaxSegs];
+    DiffStart start[kMaxSkCtas + 1];
 };
+
+// Key tiles of a block's unit.
+__host__ __device__ inline int diff_tiles(const DiffSeq &q, int group, int block)
+{
+    const int rows = q.n_q * group, last = (block + 1) * kDiffRows < rows ? (block + 1) * kDiffRows - 1 : rows - 1;
+    return (q.n_keys - q.n_q + last / group + kDiffKeys) / kDiffKeys;
+}
 
 // ---------------------------------------------------------------- copy-on-write
 struct CowCopy {
@@ -348,7 +376,6 @@ struct AttnParams {
 // units cut by a stretch boundary write fp32 partials (O / l and log2-sum-exp)
 // into slot `slot`, part `part`, and the warp that writes a slot's last part
 // (counted on its ticket) merges the slot's parts.
-constexpr int kMaxSkCtas = 160;        // >= SMs of the GPU
 constexpr int kSkTicketsPerSlot = 8;   // one per (q-tile, warp of 32 rows)
 
 struct SkCta {
@@ -476,7 +503,9 @@ cudaError_t launch_append_q8(int head_dim, const AppendParams &p, cudaStream_t s
 // Append with the rotation on the way (a block of append parameters as above, and the rotation's).
 cudaError_t launch_append_rope(bool q8, int head_dim, const AppendParams &p, const RopeCall &rope, cudaStream_t st);
 cudaError_t launch_rotate(int head_dim, const RotateParams &p, cudaStream_t st);
-cudaError_t launch_diff_attn(int head_dim, const DiffParams &p, int64_t rows, cudaStream_t st);
+// tm_k / tm_v: the pools as 2-D maps with 64 x min(ps, 64) boxes, 128-byte swizzle.
+cudaError_t launch_diff_attn(int head_dim, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const DiffParams &p, cudaStream_t st);
+cudaError_t launch_diff_combine(int head_dim, const DiffParams &p, cudaStream_t st);
 cudaError_t launch_unpack_q8(const UnpackParams &p, int pages, cudaStream_t st);
 cudaError_t launch_save_pages(const SaveParams &p, cudaStream_t st);
 cudaError_t launch_read_kv(bool q8, const ReadParams &p, cudaStream_t st);
