@@ -15,7 +15,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpe.so")
 SOURCES = ["pe_host.cu", "pe_kv.cu", "pe_attn.cu", "pe_attn_sk.cu", "pe_decode.cu", "pe_q8.cu", "pe_q8_attn.cu", "pe_q8_rows.cu", "pe_evict.cu", "pe_weights.cu",
-           "pe_rope.cu", "pe_diff.cu",
+           "pe_rope.cu", "pe_diff.cu", "pe_diff_many.cu",
            "pe_prov.cpp", "pe_sched.cpp"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",

@@ -15,13 +15,13 @@
 #include <algorithm>
 
 #include "dev_common.cuh"
+#include "diff.cuh"
 #include "q8.cuh"
 
 namespace pe {
 
 namespace {
 
-constexpr float kTileSumLimit = 1.8446744e19f;  // 2^64: larger tile sums move the reference (pe_attn.cu)
 constexpr int kDiffThreads = 288;               // warps 0-3 softmax, 4-7 producers, 8 MMA
 
 template <int HD>
@@ -29,10 +29,10 @@ struct DiffCfg {
     static constexpr int kRegions = HD / 64;                  // 128-byte swizzle atoms along d
     static constexpr int kStages = HD == 128 ? 3 : 6;
     static constexpr int kQBytes = 128 * HD * 2;
-    static constexpr int kKBytes = 2 * kDiffKeys * HD * 2;    // both maps' keys of a tile
-    static constexpr int kKRegion = 2 * kDiffKeys * 128;
-    static constexpr int kVBytes = kDiffKeys * 2 * HD * 2;
-    static constexpr int kVRegion = kDiffKeys * 128;
+    static constexpr int kKBytes = 2 * DiffFew::kKeys * HD * 2;    // both maps' keys of a tile
+    static constexpr int kKRegion = 2 * DiffFew::kKeys * 128;
+    static constexpr int kVBytes = DiffFew::kKeys * 2 * HD * 2;
+    static constexpr int kVRegion = DiffFew::kKeys * 128;
     static constexpr int kOffK = kQBytes;
     static constexpr int kOffV = kOffK + kStages * kKBytes;
     static constexpr int kOffBar = kOffV + kStages * kVBytes;
@@ -43,42 +43,6 @@ struct DiffCfg {
     static constexpr int kTmemO = 256;                        // S at 0 and 128, P over S
     static constexpr uint32_t kTmemCols = 512;
     static_assert(kDynSmem <= 232448, "shared memory budget");
-};
-
-// A CTA's pieces, one after another: every role walks them alike.
-struct DiffWalk {
-    const DiffParams &p;
-    int u, t, u1, t1;  // next piece, end of the stretch
-    int si, pair, block, t0, n, slot;
-    __device__ __forceinline__ DiffWalk(const DiffParams &p_, int cta) : p(p_)
-    {
-        u = p.start[cta].u;
-        t = p.start[cta].t;
-        u1 = p.start[cta + 1].u;
-        t1 = p.start[cta + 1].t;
-    }
-    // The next piece with tiles [t0, t0 + n), or false.
-    __device__ __forceinline__ bool next(int cta)
-    {
-        while (u < u1 || (u == u1 && t < t1)) {
-            int lo = 0, hi = p.n_seqs - 1;
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (p.seqs[mid].unit0 <= u) lo = mid; else hi = mid - 1;
-            }
-            si = lo;
-            const int local = u - p.seqs[si].unit0;
-            block = local % p.seqs[si].n_blocks;
-            pair = local / p.seqs[si].n_blocks;
-            slot = u + cta;
-            t0 = t;
-            n = (u == u1 ? t1 : diff_tiles(p.seqs[si], p.group, block)) - t;
-            ++u;
-            t = 0;
-            if (n > 0) return true;
-        }
-        return false;
-    }
 };
 
 template <int HD>
@@ -141,7 +105,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
 
-    DiffWalk w(p, cta);
+    DiffWalk<DiffFew> w(p, cta);
     int i = 0;  // tiles of the pieces before
     if (warp >= 4 && warp < 8) {
         // =================================================== producers: K of a map, or V of a kv-head
@@ -149,18 +113,18 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
         const int head = warp & 1;
         const CUtensorMap *map = is_v ? &tm_v : &tm_k;
         const uint32_t b_full = is_v ? b_v_full : b_k_full, b_empty = is_v ? b_v_empty : b_k_empty;
-        const int rows = min(p.ps, kDiffKeys);                 // of a box
-        const int n_ops = kDiffKeys / rows * C::kRegions;      // <= 16
+        const int rows = min(p.ps, DiffFew::kKeys);                 // of a box
+        const int n_ops = DiffFew::kKeys / rows * C::kRegions;      // <= 16
         const int op_page = lane / C::kRegions, op_reg = lane % C::kRegions;
         const bool on = lane < n_ops;
         const uint32_t base = sbase + (is_v ? C::kOffV + (head * C::kRegions + op_reg) * C::kVRegion
-                                            : C::kOffK + op_reg * C::kKRegion + head * kDiffKeys * 128) + op_page * rows * 128;
+                                            : C::kOffK + op_reg * C::kKRegion + head * DiffFew::kKeys * 128) + op_page * rows * 128;
         bool ok = true;
-        while (ok && w.next(cta)) {
+        while (ok && w.next()) {
             const DiffSeq &sq = p.seqs[w.si];
             const int kvh = 2 * w.pair + head;
             auto row_of = [&](int k) -> int {  // of the pool, of this lane's box of tile k
-                const int key = (w.t0 + k) * kDiffKeys + op_page * rows, lp = key >> p.log_ps;
+                const int key = (w.t0 + k) * DiffFew::kKeys + op_page * rows, lp = key >> p.log_ps;
                 const int page = on && lp < sq.n_pages ? p.page_table[sq.table_row + lp] : -1;
                 return page >= 0 && page < p.num_pages ? (((p.layer * p.num_pages + page) * p.hkv + kvh) << p.log_ps) + (key & (p.ps - 1))
                                                        : p.oob_row;
@@ -169,7 +133,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
             for (int k = 0; k < w.n; ++k, ++i) {
                 const int next = k + 1 < w.n ? row_of(k + 1) : 0, s = i % C::kStages;
                 if (i >= C::kStages && !wait_bar_warp(b_empty + 8 * s, ((i / C::kStages) - 1) & 1, wctx)) { ok = false; break; }
-                if (lane == 0) ptx::mbar_arrive_expect_tx(b_full + 8 * s, kDiffKeys * HD * 2);
+                if (lane == 0) ptx::mbar_arrive_expect_tx(b_full + 8 * s, DiffFew::kKeys * HD * 2);
                 __syncwarp();
                 if (on) ptx::tma_load_2d(base + s * (is_v ? C::kVBytes : C::kKBytes), map, op_reg * 64, y, b_full + 8 * s);
                 y = next;
@@ -183,7 +147,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
         }
     } else if (warp == 8) {
         // =================================================== MMA (the converged warp; one elected lane issues)
-        constexpr uint32_t kIdescS = ptx::idesc_bf16_f32(128, 2 * kDiffKeys, false);
+        constexpr uint32_t kIdescS = ptx::idesc_bf16_f32(128, 2 * DiffFew::kKeys, false);
         constexpr uint32_t kIdescO = ptx::idesc_bf16_f32(128, 2 * HD, true);
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
         const uint64_t q_desc = ptx::smem_desc_sw128(sbase, 16, 1024);
@@ -203,7 +167,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
             return true;
         };
         bool ok = true;
-        for (int piece = 0; ok && w.next(cta); ++piece) {
+        for (int piece = 0; ok && w.next(); ++piece) {
             const int n = __shfl_sync(0xffffffffu, w.n, 0);
             if (!wait_bar_warp(b_q_full, piece & 1, wctx)) break;
             ok = issue_s(i) && (n < 2 || issue_s(i + 1));
@@ -212,7 +176,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                 ptx::tc_fence_after();
                 const uint64_t vd = v_desc + (i % C::kStages) * (C::kVBytes >> 4);
 #pragma unroll
-                for (int kk = 0; kk < kDiffKeys / 16; ++kk)
+                for (int kk = 0; kk < DiffFew::kKeys / 16; ++kk)
                     mma_bf16_ts_warp(tm + C::kTmemO, tm + 128 * (i & 1) + kk * 8, vd + (kk * 16 * 128 >> 4), kIdescO,
                                      (k > 0 || kk > 0) ? 1u : 0u);
                 mma_commit_warp(b_o_done + 8 * (i & 1));
@@ -222,7 +186,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
         }
     } else {
         // =================================================== softmax: thread r owns row r (TMEM lane r)
-        const int row = threadIdx.x, m = row / kDiffRows;
+        const int row = threadIdx.x, m = row / DiffFew::kRows;
         const uint32_t lane_off = static_cast<uint32_t>(warp * 32) << 16;
         const float2 sl2 = make_float2(p.scale_log2, p.scale_log2);
         bool ok = true;
@@ -231,13 +195,13 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
             ptx::mbar_arrive(b_edge);
             return wait_bar_warp(b_edge, met++ & 1, wctx);
         };
-        while (ok && w.next(cta)) {
+        while (ok && w.next()) {
             const DiffSeq &sq = p.seqs[w.si];
-            const int r = w.block * kDiffRows + (row & (kDiffRows - 1));  // packed row of its map
+            const int r = w.block * DiffFew::kRows + (row & (DiffFew::kRows - 1));  // packed row of its map
             const int qi = r / p.group, head = 2 * (w.pair * p.group + r - qi * p.group) + m;
             const bool valid = qi < sq.n_q, any = __any_sync(0xffffffffu, valid);
             const int pos = sq.n_keys - sq.n_q + qi;
-            const int pos_first = sq.n_keys - sq.n_q + w.block * kDiffRows / p.group;
+            const int pos_first = sq.n_keys - sq.n_q + w.block * DiffFew::kRows / p.group;
             // Q's row into shared memory (the S products of the piece before are done), 16-byte chunks swizzled by row & 7
             if (valid) {
                 const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (static_cast<int64_t>(sq.q_row0 + qi) * p.hq + head) * HD);
@@ -251,9 +215,9 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
             ptx::mbar_arrive(b_q_full);
             float m_ref = -INFINITY, l = 0.f;
             for (int k = 0; k < w.n; ++k, ++i) {
-                const int kbase = (w.t0 + k) * kDiffKeys;
+                const int kbase = (w.t0 + k) * DiffFew::kKeys;
                 const uint32_t tS = tmem + 128 * (i & 1) + lane_off;
-                const bool edge = kbase + kDiffKeys - 1 > pos_first;  // a row of the block does not see some key of the tile
+                const bool edge = kbase + DiffFew::kKeys - 1 > pos_first;  // a row of the block does not see some key of the tile
                 if (edge) {
                     // V of keys that some row does not see: 0 times an infinity or NaN would reach that row.  Such keys' V
                     // become 0, and rows that see them NaN.
@@ -283,7 +247,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                 if (!wait_bar_warp(b_s_full + 8 * (i & 1), (i >> 1) & 1, wctx)) { ok = false; break; }
                 ptx::tc_fence_after();
                 if (any) {
-                    float s[kDiffKeys];
+                    float s[DiffFew::kKeys];
                     {
                         float (&s0)[32] = *reinterpret_cast<float (*)[32]>(&s[0]);
                         float (&s1)[32] = *reinterpret_cast<float (*)[32]>(&s[32]);
@@ -293,7 +257,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                     }
                     if (edge) {
 #pragma unroll
-                        for (int c = 0; c < kDiffKeys; ++c)
+                        for (int c = 0; c < DiffFew::kKeys; ++c)
                             if (kbase + c > pos) s[c] = -INFINITY;
                     }
                     // weights against the row's reference, which moves only when a tile's sum passes 2^64 (pe_attn.cu); the
@@ -302,7 +266,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                         const float2 nref = make_float2(-ref, -ref);
                         float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-                        for (int ch = 0; ch < kDiffKeys / 32; ++ch) {
+                        for (int ch = 0; ch < DiffFew::kKeys / 32; ++ch) {
                             uint32_t pk[16];
 #pragma unroll
                             for (int x = 0; x < 16; ++x) {
@@ -320,7 +284,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                     bool need = valid && m_ref == -INFINITY;
                     if (!__all_sync(0xffffffffu, need)) {
                         rs = exp_tile(m_ref == -INFINITY ? 0.f : m_ref);
-                        need = need || (valid && !(rs <= kTileSumLimit));
+                        need = need || (valid && !(rs <= kDiffSumLimit));
                     }
                     if (__any_sync(0xffffffffu, need)) {
                         float mx[4];
@@ -390,7 +354,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
 constexpr int kMergeWarps = 4;
 
 // A block per output row and head: warp x joins pieces x, x + 4, ... of both maps, lane t the columns 4t .. + 3 of every 128;
-// then the first warp the four.  A row's pieces are those of CTAs whose stretches meet its unit.
+// then the first warp the four.
 template <int HD>
 __global__ void __launch_bounds__(32 * kMergeWarps) diff_combine_kernel(const __grid_constant__ DiffParams p)
 {
@@ -407,59 +371,36 @@ __global__ void __launch_bounds__(32 * kMergeWarps) diff_combine_kernel(const __
     const DiffSeq &sq = p.seqs[lo];
     const int heads = p.hq / 2, local = id - sq.out0, qi = local / heads, head = local - qi * heads;
     const int pair = head / p.group, r = qi * p.group + head - pair * p.group;
-    const int u = sq.unit0 + pair * sq.n_blocks + r / kDiffRows, row = r % kDiffRows;
-    lo = 0;
-    hi = p.n_ctas - 1;
-    while (lo < hi) {  // the last CTA whose stretch begins at or before the unit's first tile
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.start[mid].u < u || (p.start[mid].u == u && p.start[mid].t == 0)) lo = mid; else hi = mid - 1;
-    }
+    const int u = sq.unit0 + pair * sq.n_blocks + r / DiffFew::kRows, row = r % DiffFew::kRows;
+    const int c0 = diff_first_taker(p, u);
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    float4 o[2][V4];
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int v = 0; v < V4; ++v) o[x][v] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = lo + warp; c < p.n_ctas && (c == lo || p.start[c].u == u); c += kMergeWarps) {
-        if (p.start[c].u == p.start[c + 1].u && p.start[c].t == p.start[c + 1].t) continue;  // nothing of the CTA's
-        const int64_t at = static_cast<int64_t>(u + c) * 128 + row;
+    DiffMerge<HD> a[2];
+    for (int c = c0 + warp; c < p.n_takers && (c == c0 || p.start[c].u == u); c += kMergeWarps) {
+        if (diff_takes_nothing(p, c)) continue;
+        const int64_t at = static_cast<int64_t>(u + c) * DiffFew::kSlotRows + row;
         float lse[2];
         float4 y[2][V4];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            lse[x] = __ldcg(p.part_lse + at + x * kDiffRows);
-            const float4 *src = reinterpret_cast<const float4 *>(p.part + (at + x * kDiffRows) * 2 * HD);
-#pragma unroll
-            for (int v = 0; v < V4; ++v) y[x][v] = __ldcg(src + v * 32 + lane);
+            lse[x] = __ldcg(p.part_lse + at + x * DiffFew::kRows);
+            diff_load<HD>(p.part + (at + x * DiffFew::kRows) * 2 * HD, lane, y[x]);
         }
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            if (lse[x] == -INFINITY) continue;  // (its row may hold anything)
-            const float mn = fmaxf(m[x], lse[x]);
-            const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - mn), g = ex2(lse[x] - mn);  // (NaN where lse is)
-            m[x] = mn;
-            l[x] = l[x] * f + g;
-#pragma unroll
-            for (int v = 0; v < V4; ++v)
-                o[x][v] = make_float4(o[x][v].x * f + y[x][v].x * g, o[x][v].y * f + y[x][v].y * g, o[x][v].z * f + y[x][v].z * g,
-                                      o[x][v].w * f + y[x][v].w * g);
-        }
+        for (int x = 0; x < 2; ++x) a[x].add(lse[x], y[x]);
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         if (lane == 0) {
-            s_m[x][warp] = m[x];
-            s_l[x][warp] = l[x];
+            s_m[x][warp] = a[x].m;
+            s_l[x][warp] = a[x].l;
         }
 #pragma unroll
-        for (int v = 0; v < V4; ++v) s_o[x][warp][v * 32 + lane] = o[x][v];
+        for (int v = 0; v < V4; ++v) s_o[x][warp][v * 32 + lane] = a[x].o[v];
     }
     __syncthreads();
     if (warp > 0) return;
     float4 y[V4];
-    float sum = 0.f;
 #pragma unroll
     for (int v = 0; v < V4; ++v) y[v] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -475,30 +416,59 @@ __global__ void __launch_bounds__(32 * kMergeWarps) diff_combine_kernel(const __
         const float part = (x ? -p.lambda[head] : 1.f) * (den == 0.f ? 0.f : 1.f / den);
 #pragma unroll
         for (int k = 0; k < kMergeWarps; ++k) {
-            const float g = f[k] * part;
-            if (f[k] == 0.f) continue;
+            float4 z[V4];
 #pragma unroll
-            for (int v = 0; v < V4; ++v) {
-                const float4 z = s_o[x][k][v * 32 + lane];
-                y[v] = make_float4(y[v].x + g * z.x, y[v].y + g * z.y, y[v].z + g * z.z, y[v].w + g * z.w);
-            }
+            for (int v = 0; v < V4; ++v) z[v] = s_o[x][k][v * 32 + lane];
+            diff_axpy<HD>(f[k] * part, z, f[k] != 0.f, y);
         }
     }
-    if (p.gain) {
-#pragma unroll
-        for (int v = 0; v < V4; ++v) sum += y[v].x * y[v].x + y[v].y * y[v].y + y[v].z * y[v].z + y[v].w * y[v].w;
-#pragma unroll
-        for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-        const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
-#pragma unroll
-        for (int v = 0; v < V4; ++v) {
-            const float4 g = __ldg(reinterpret_cast<const float4 *>(p.gain) + v * 32 + lane);
-            y[v] = make_float4(y[v].x * f * g.x, y[v].y * f * g.y, y[v].z * f * g.z, y[v].w * f * g.w);
-        }
+    diff_finish<HD>(p, static_cast<int64_t>(sq.q_row0 + qi) * heads + head, lane, y);
+}
+
+constexpr int kManyMergeWarps = 4;
+
+// A warp per output row and head: the pieces of its two maps' units.
+template <int HD>
+__global__ void __launch_bounds__(32 * kManyMergeWarps) diff_many_combine_kernel(const __grid_constant__ DiffParams p)
+{
+    constexpr int V4 = 2 * HD / 128;
+    const int lane = threadIdx.x & 31;
+    const int id = static_cast<int>(blockIdx.x) * kManyMergeWarps + (threadIdx.x >> 5);
+    ptx::griddep_launch_dependents();
+    if (id >= p.n_out) return;
+    int lo = 0, hi = p.n_seqs - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.seqs[mid].out0 <= id) lo = mid; else hi = mid - 1;
     }
-    uint2 *dst = reinterpret_cast<uint2 *>(p.out + (static_cast<int64_t>(sq.q_row0 + qi) * heads + head) * 2 * HD);
+    const DiffSeq &sq = p.seqs[lo];
+    const int heads = p.hq / 2, local = id - sq.out0, qi = local / heads, head = local - qi * heads;
+    const int pair = head / p.group, r = qi * p.group + head - pair * p.group;
+    const int row = r % DiffMany::kRows;
+    int u[2], c0[2];
 #pragma unroll
-    for (int v = 0; v < V4; ++v) dst[v * 32 + lane] = make_uint2(pack_bf16(y[v].x, y[v].y), pack_bf16(y[v].z, y[v].w));
+    for (int x = 0; x < 2; ++x) {
+        u[x] = sq.unit0 + (2 * pair + x) * sq.n_blocks + r / DiffMany::kRows;
+        c0[x] = diff_first_taker(p, u[x]);
+    }
+    ptx::griddep_wait();
+    DiffMerge<HD> a[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        for (int c = c0[x]; c < p.n_takers && (c == c0[x] || p.start[c].u == u[x]); ++c) {
+            if (diff_takes_nothing(p, c)) continue;
+            const int64_t at = static_cast<int64_t>(u[x] + c) * DiffMany::kSlotRows + row;
+            const float lse = __ldcg(p.part_lse + at);
+            float4 y[V4];
+            diff_load<HD>(p.part + at * 2 * HD, lane, y);
+            a[x].add(lse, y);
+        }
+    float4 y[V4];
+#pragma unroll
+    for (int v = 0; v < V4; ++v) y[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) diff_axpy<HD>((x ? -p.lambda[head] : 1.f) * (a[x].l == 0.f ? 0.f : 1.f / a[x].l), a[x].o, a[x].l != 0.f, y);
+    diff_finish<HD>(p, static_cast<int64_t>(sq.q_row0 + qi) * heads + head, lane, y);
 }
 
 cudaLaunchConfig_t diff_config(int blocks, int threads, int smem, cudaStream_t st, cudaLaunchAttribute *attr)
@@ -522,7 +492,7 @@ cudaError_t launch_diff_t(const CUtensorMap &k, const CUtensorMap &v, const Diff
     cudaError_t e = set_dyn_smem_once(diff_attn_kernel<HD>, DiffCfg<HD>::kDynSmem, configured);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = diff_config(p.n_ctas, kDiffThreads, DiffCfg<HD>::kDynSmem, st, &attr);
+    const cudaLaunchConfig_t cfg = diff_config(p.n_takers, kDiffThreads, DiffCfg<HD>::kDynSmem, st, &attr);
     return cudaLaunchKernelEx(&cfg, diff_attn_kernel<HD>, k, v, p);
 }
 
@@ -530,14 +500,19 @@ cudaError_t launch_diff_t(const CUtensorMap &k, const CUtensorMap &v, const Diff
 
 cudaError_t launch_diff_attn(int head_dim, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const DiffParams &p, cudaStream_t st)
 {
-    if (p.n_ctas <= 0) return cudaSuccess;
+    if (p.n_takers <= 0) return cudaSuccess;
     return head_dim == 128 ? launch_diff_t<128>(tm_k, tm_v, p, st) : launch_diff_t<64>(tm_k, tm_v, p, st);
 }
 
-cudaError_t launch_diff_combine(int head_dim, const DiffParams &p, cudaStream_t st)
+cudaError_t launch_diff_combine(int head_dim, bool many, const DiffParams &p, cudaStream_t st)
 {
     if (p.n_out <= 0) return cudaSuccess;
     cudaLaunchAttribute attr;
+    if (many) {
+        const cudaLaunchConfig_t cfg = diff_config((p.n_out + kManyMergeWarps - 1) / kManyMergeWarps, 32 * kManyMergeWarps, 0, st, &attr);
+        return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<128>, p)
+                               : cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<64>, p);
+    }
     const cudaLaunchConfig_t cfg = diff_config(p.n_out, 32 * kMergeWarps, 0, st, &attr);
     return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_combine_kernel<128>, p) : cudaLaunchKernelEx(&cfg, diff_combine_kernel<64>, p);
 }

@@ -2292,18 +2292,20 @@ struct DiffItem {
     int32_t q_row0, n_q, n_keys;
 };
 
-int64_t diff_slot_bytes(const pe_cache *c) { return 128 * (2 * static_cast<int64_t>(c->cfg.head_dim) + 1) * 4; }
+// Rows (n_q x group) up to which a sequence takes the kernel of few rows.
+constexpr int64_t kDiffFewRows = 64;
 
 // A unit's cost besides its tiles, in tiles.
 constexpr int64_t kDiffUnitCost = 1;
 
 // One launch over the items, at most kMaxSegs: fills p's sequences and stretches.
-void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t max_ctas, DiffParams &p)
+template <typename Shape>
+void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t max_takers, DiffParams &p)
 {
     p.n_seqs = p.n_out = 0;
     int64_t work = 0, tiles = 0;
     int32_t units = 0;
-    const int pairs = p.hkv / 2;
+    const int per_block = p.hkv / 2 * Shape::kMaps;  // units
     for (const DiffItem &it : items) {
         DiffSeq &q = p.seqs[p.n_seqs++];
         q.table_row = it.seq * c->cfg.max_pages_per_seq;
@@ -2311,27 +2313,26 @@ void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t ma
         q.q_row0 = it.q_row0;
         q.n_q = it.n_q;
         q.n_keys = it.n_keys;
-        q.n_blocks = static_cast<int32_t>(ceil_div(static_cast<int64_t>(it.n_q) * p.group, kDiffRows));
+        q.n_blocks = static_cast<int32_t>(ceil_div(static_cast<int64_t>(it.n_q) * p.group, Shape::kRows));
         q.unit0 = units;
         q.out0 = p.n_out;
-        units += q.n_blocks * pairs;
+        units += q.n_blocks * per_block;
         p.n_out += it.n_q * (p.hq / 2);
         int64_t one = 0;
-        for (int b = 0; b < q.n_blocks; ++b) one += diff_tiles(q, p.group, b);
-        tiles += one * pairs;
-        work += (one + q.n_blocks * kDiffUnitCost) * pairs;
+        for (int b = 0; b < q.n_blocks; ++b) one += diff_tiles<Shape>(q, p.group, b);
+        tiles += one * per_block;
+        work += (one + q.n_blocks * kDiffUnitCost) * per_block;
     }
-    // equal stretches of work; CTA c's begins at work * c / n
-    const int64_t n = std::min(tiles, max_ctas);
-    p.n_ctas = static_cast<int32_t>(n);
-    int64_t at = 0;  // work before the unit
-    int32_t u = 0, s = 0;
-    int64_t next = 0;  // the next CTA
-    for (s = 0; s < p.n_seqs; ++s) {
+    // equal stretches of work: taker c's begins at work * c / n
+    const int64_t n = std::min(tiles, max_takers);
+    p.n_takers = static_cast<int32_t>(n);
+    int64_t at = 0, next = 0;  // work before the unit; the next taker
+    int32_t u = 0;
+    for (int32_t s = 0; s < p.n_seqs; ++s) {
         const DiffSeq &q = p.seqs[s];
-        for (int j = 0; j < pairs; ++j)
+        for (int j = 0; j < per_block; ++j)
             for (int b = 0; b < q.n_blocks; ++b, ++u) {
-                const int64_t w = diff_tiles(q, p.group, b) + kDiffUnitCost;
+                const int64_t w = diff_tiles<Shape>(q, p.group, b) + kDiffUnitCost;
                 for (; next < n && work * next / n < at + w; ++next) {
                     const int64_t t = work * next / n - at - kDiffUnitCost;
                     p.start[next] = DiffStart{u, static_cast<int32_t>(std::max<int64_t>(0, t))};
@@ -2340,6 +2341,53 @@ void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t ma
             }
     }
     for (; next <= n; ++next) p.start[next] = DiffStart{u, 0};
+}
+
+// The items with one of the two kernels, in launches of as many rows as their partials fit.
+template <typename Shape>
+pe_status launch_diff(pe_cache *c, const std::vector<DiffItem> &all, DiffParams &p, cudaStream_t st)
+{
+    constexpr bool kMany = Shape::kMaps == 2;
+    const int64_t slots = c->ws_bytes / (Shape::kSlotRows * (2 * static_cast<int64_t>(c->cfg.head_dim) + 1) * 4);
+    const int64_t sms = std::min<int64_t>(c->num_sms, kMaxSkCtas);
+    const int64_t takers = std::max<int64_t>(1, std::min<int64_t>(kMany ? sms / 2 : sms, slots / 2));
+    const int64_t room = (slots - takers) / (p.hkv / 2 * Shape::kMaps);  // blocks; besides, a slot a taker
+    std::vector<DiffItem> items;
+    int64_t used = 0;
+    auto flush = [&]() -> pe_status {
+        if (items.empty()) return PE_OK;
+        plan_diff<Shape>(c, items, takers, p);
+        p.part = c->d_ws;
+        p.part_lse = c->d_ws + slots * Shape::kSlotRows * 2 * c->cfg.head_dim;
+        if (injected_failure(c)) return launch_fault("differential attention");
+        cudaError_t e = kMany ? launch_diff_attn_many(c->cfg.head_dim, c->tm_kd, c->tm_vd, p, st)
+                              : launch_diff_attn(c->cfg.head_dim, c->tm_kd, c->tm_vd, p, st);
+        if (e != cudaSuccess) return cuda_fail(e, "differential attention launch");
+        c->launches++;
+        if (injected_failure(c)) return launch_fault("differential attention's merge");
+        e = launch_diff_combine(c->cfg.head_dim, kMany, p, st);
+        if (e != cudaSuccess) return cuda_fail(e, "differential attention's merge launch");
+        c->launches++;
+        items.clear();
+        used = 0;
+        return PE_OK;
+    };
+    for (const DiffItem &it : all) {
+        const int32_t before = it.n_keys - it.n_q;
+        for (int32_t done = 0; done < it.n_q;) {
+            const int64_t fit = (room - used) * Shape::kRows / p.group;  // whole queries
+            if (fit < 1 || items.size() == kMaxSegs) {
+                if (items.empty()) return fail(PE_ERR_RANGE, "the workspace has no room for a launch's partials");
+                if (pe_status s = flush()) return s;
+                continue;
+            }
+            const int32_t take = static_cast<int32_t>(std::min<int64_t>(fit, it.n_q - done));
+            items.push_back(DiffItem{it.seq, it.q_row0 + done, take, before + done + take});
+            used += ceil_div(static_cast<int64_t>(take) * p.group, Shape::kRows);
+            done += take;
+        }
+    }
+    return flush();
 }
 
 pe_status run_diff(pe_cache *c, const std::vector<AttnItem> &all, int32_t layer, const void *Q, void *out, int32_t hq, float scale,
@@ -2363,47 +2411,14 @@ pe_status run_diff(pe_cache *c, const std::vector<AttnItem> &all, int32_t layer,
     p.oob_row = static_cast<int32_t>(c->pool_rows);
     p.scale_log2 = scale * 1.4426950408889634f;
     p.eps = eps;
-    // units that a launch's partials have room for, besides a slot a CTA
-    const int64_t slots = c->ws_bytes / diff_slot_bytes(c), pairs = p.hkv / 2;
-    const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>({c->num_sms, kMaxSkCtas, slots / 2}));
-    const int64_t room = (slots - ctas) / pairs;  // blocks
-    if (room < 1) return fail(PE_ERR_RANGE, "the workspace has no room for a launch's partials");
-    std::vector<DiffItem> items;
-    int64_t used = 0;
-    auto flush = [&]() -> pe_status {
-        if (items.empty()) return PE_OK;
-        plan_diff(c, items, ctas, p);
-        p.part = c->d_ws;
-        p.part_lse = c->d_ws + slots * 128 * 2 * c->cfg.head_dim;
-        if (injected_failure(c)) return launch_fault("differential attention");
-        cudaError_t e = launch_diff_attn(c->cfg.head_dim, c->tm_kd, c->tm_vd, p, st);
-        if (e != cudaSuccess) return cuda_fail(e, "differential attention launch");
-        c->launches++;
-        if (injected_failure(c)) return launch_fault("differential attention's merge");
-        e = launch_diff_combine(c->cfg.head_dim, p, st);
-        if (e != cudaSuccess) return cuda_fail(e, "differential attention's merge launch");
-        c->launches++;
-        items.clear();
-        used = 0;
-        return PE_OK;
-    };
+    std::vector<DiffItem> few, many;
     for (const AttnItem &it : all) {
-        const int32_t before = static_cast<int32_t>(c->len[it.seq]) - it.n_q;  // keys that the first query's see besides its own
-        for (int32_t done = 0; done < it.n_q;) {
-            // (whole queries; a block of them may be shared with none of the next piece's)
-            const int64_t fit = (room - used) * kDiffRows / p.group;
-            if (fit < 1 || items.size() == kMaxSegs) {
-                if (items.empty()) return fail(PE_ERR_RANGE, "the workspace has no room for a launch's partials");
-                if (pe_status s = flush()) return s;
-                continue;
-            }
-            const int32_t take = static_cast<int32_t>(std::min<int64_t>(fit, it.n_q - done));
-            items.push_back(DiffItem{it.seq, it.q_row0 + done, take, before + done + take});
-            used += ceil_div(static_cast<int64_t>(take) * p.group, kDiffRows);
-            done += take;
-        }
+        if (it.n_q <= 0) continue;
+        const int64_t rows = static_cast<int64_t>(it.n_q) * p.group;
+        (rows <= kDiffFewRows ? few : many).push_back(DiffItem{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq])});
     }
-    return flush();
+    if (pe_status s = launch_diff<DiffFew>(c, few, p, st)) return s;
+    return launch_diff<DiffMany>(c, many, p, st);
 }
 
 }  // namespace

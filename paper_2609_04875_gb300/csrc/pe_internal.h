@@ -98,12 +98,23 @@ struct RotateParams {
 };
 
 // ---------------------------------------------------------------- differential attention
-// Work units are (sequence, pair of kv-heads, block of kDiffRows query rows), numbered sequence by sequence, blocks fastest;
-// a unit's tiles are of kDiffKeys keys, up to what its last query sees.  CTA c takes the stretch from tile start[c].t of unit
-// start[c].u up to start[c + 1]; the piece of unit u that it computes is slot u + c of the partials (of two pieces in the
-// order of the stretches, the later one has the larger unit, the larger CTA, or both, so no two share a slot).
-constexpr int kDiffRows = 64;          // of each map; query * group + head-in-group
-constexpr int kDiffKeys = 64;
+// Two kernels.  Few rows: a unit is (sequence, pair of kv-heads, block of 64 query rows), both maps; its tiles are of 64 keys;
+// a CTA takes a stretch.  Many rows: a unit is (sequence, pair, map, block of 256 rows), its tiles are of 128 keys; a pair of
+// CTAs takes a stretch.  Rows are query * group + head-in-group.
+//
+// Units are numbered sequence by sequence, blocks fastest; a unit's tiles go up to what its last query sees.  Taker c has the
+// stretch from tile start[c].t of unit start[c].u up to start[c + 1]; the piece of unit u that it computes is slot u + c of
+// the partials (of two pieces in the order of the stretches, the later one has the larger unit, the larger taker, or both, so
+// no two share a slot).
+template <int ROWS, int KEYS, int SPLIT_MAPS, int SLOT_ROWS>
+struct DiffShape {
+    static constexpr int kRows = ROWS;          // of a block
+    static constexpr int kKeys = KEYS;          // of a tile
+    static constexpr int kMaps = SPLIT_MAPS;    // units of a (pair, block): 1, or 2 where a unit is one map
+    static constexpr int kSlotRows = SLOT_ROWS; // partial rows of a piece: both maps' block, or one's
+};
+using DiffFew = DiffShape<64, 64, 1, 128>;
+using DiffMany = DiffShape<256, 128, 2, 256>;
 
 struct DiffSeq {
     int32_t table_row;     // seq * max_pages_per_seq
@@ -125,12 +136,12 @@ struct DiffParams {
     __nv_bfloat16 *out;          // bf16 [rows][Hq / 2][2 d]
     const float *lambda;         // [Hq / 2]
     const float *gain;           // [2 d], or null: no norm
-    float *part;                 // partials: O / l fp32 [slots][128][2 d] (a map's kDiffRows rows, then the other's)
-    float *part_lse;             // [slots][128], log2 units
+    float *part;                 // partials: O / l fp32 [slots][kSlotRows][2 d] (few rows: a map's 64, then the other's)
+    float *part_lse;             // [slots][kSlotRows], log2 units
     int32_t *status;
     int32_t n_seqs, hq, hkv, group, layer, num_pages, ps, log_ps;
     int32_t oob_row;             // a pool row past the end: boxes there read zeros
-    int32_t n_ctas, n_out;
+    int32_t n_takers, n_out;
     float scale_log2;            // softmax_scale * log2(e)
     float eps;
     DiffSeq seqs[kMaxSegs];
@@ -138,10 +149,11 @@ struct DiffParams {
 };
 
 // Key tiles of a block's unit.
+template <typename Shape>
 __host__ __device__ inline int diff_tiles(const DiffSeq &q, int group, int block)
 {
-    const int rows = q.n_q * group, last = (block + 1) * kDiffRows < rows ? (block + 1) * kDiffRows - 1 : rows - 1;
-    return (q.n_keys - q.n_q + last / group + kDiffKeys) / kDiffKeys;
+    const int rows = q.n_q * group, last = (block + 1) * Shape::kRows < rows ? (block + 1) * Shape::kRows - 1 : rows - 1;
+    return (q.n_keys - q.n_q + last / group + Shape::kKeys) / Shape::kKeys;
 }
 
 // ---------------------------------------------------------------- copy-on-write
@@ -505,7 +517,8 @@ cudaError_t launch_append_rope(bool q8, int head_dim, const AppendParams &p, con
 cudaError_t launch_rotate(int head_dim, const RotateParams &p, cudaStream_t st);
 // tm_k / tm_v: the pools as 2-D maps with 64 x min(ps, 64) boxes, 128-byte swizzle.
 cudaError_t launch_diff_attn(int head_dim, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const DiffParams &p, cudaStream_t st);
-cudaError_t launch_diff_combine(int head_dim, const DiffParams &p, cudaStream_t st);
+cudaError_t launch_diff_attn_many(int head_dim, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const DiffParams &p, cudaStream_t st);
+cudaError_t launch_diff_combine(int head_dim, bool many, const DiffParams &p, cudaStream_t st);
 cudaError_t launch_unpack_q8(const UnpackParams &p, int pages, cudaStream_t st);
 cudaError_t launch_save_pages(const SaveParams &p, cudaStream_t st);
 cudaError_t launch_read_kv(bool q8, const ReadParams &p, cudaStream_t st);

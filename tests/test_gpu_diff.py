@@ -194,7 +194,9 @@ def test_debug_poison_and_rows_behind():
     s.cache.crop(s.seqs[0], 251)
     q, lam, gain = s.inputs([40], 4)
     base = torch.full((60, 2, 128), 7.0, dtype=torch.bfloat16, device="cuda")
-    out = s.cache.diff_attn(s.seqs[0], 0, q, lam, gain=gain, out=base[10:50])
+    wide = torch.full((131,), 3.0, device="cuda")  # lambda and gain where a vector load may not begin
+    wide[1:129], lam2 = gain, torch.cat([lam[:1], lam])[1:]
+    out = s.cache.diff_attn(s.seqs[0], 0, q, lam2, gain=wide[1:129], out=base[10:50])
     s.check(out, s.seqs, q, [0, 40], lam, gain)
     assert (base[:10] == 7).all() and (base[50:] == 7).all()
 
