@@ -62,6 +62,13 @@ __device__ __forceinline__ void arrive_cluster(uint32_t cluster_addr)
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
+// The same after writes to tensor memory alone (tcgen05.wait::st, tcgen05.fence): nothing else is handed over, and the release
+// of all memory at cluster scope, which a warp waits for, is not needed.
+__device__ __forceinline__ void arrive_cluster_tmem(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
 __device__ __forceinline__ void or_cluster(uint32_t cluster_addr, uint32_t bits)
 {
     asm volatile("red.relaxed.cluster.shared::cluster.or.b32 [%0], %1;" ::"r"(cluster_addr), "r"(bits) : "memory");
@@ -258,7 +265,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
         const uint64_t q_desc = ptx::smem_desc_sw128(sbase, 16, 1024);
         const uint64_t k_desc = ptx::smem_desc_sw128(sbase + C::kOffK, 16, 1024);
         const uint64_t v_desc = ptx::smem_desc_sw128(sbase + C::kOffV, C::kVRegion, 1024);
-        auto full = [&](uint32_t bar, int j) { return wait_cluster_warp(bar + 8 * (j % C::kStages), (j / C::kStages) & 1, wctx); };
+        auto full = [&](uint32_t bar, int j) { return wait_bar_warp(bar + 8 * (j % C::kStages), (j / C::kStages) & 1, wctx); };
         auto issue_s = [&](int j) {
             if (!full(b_k_full, j)) return false;
             ptx::tc_fence_after();
@@ -277,7 +284,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
             if (!wait_cluster_warp(b_q_full, piece & 1, wctx)) break;
             ok = issue_s(i) && (n < 2 || issue_s(i + 1));
             for (int k = 0; ok && k < n; ++k, ++i) {
-                if (!full(b_v_full, i) || !wait_cluster_warp(b_p_full + 8 * (i & 1), (i >> 1) & 1, wctx)) { ok = false; break; }
+                if (!full(b_v_full, i) || !wait_bar_warp(b_p_full + 8 * (i & 1), (i >> 1) & 1, wctx)) { ok = false; break; }
                 ptx::tc_fence_after();
                 const uint64_t vd = v_desc + (i % C::kStages) * (C::kVBytes >> 4);
 #pragma unroll
@@ -460,7 +467,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
                 ptx::tmem_wait_st();
                 ptx::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) arrive_cluster(p_full + 8 * (i & 1));
+                if (lane == 0) arrive_cluster_tmem(p_full + 8 * (i & 1));
             }
             if (!ok || !wait_bar_warp(b_o_done + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, wctx)) break;
             ptx::tc_fence_after();
