@@ -425,50 +425,85 @@ __global__ void __launch_bounds__(32 * kMergeWarps) diff_combine_kernel(const __
     diff_finish<HD>(p, static_cast<int64_t>(sq.q_row0 + qi) * heads + head, lane, y);
 }
 
-constexpr int kManyMergeWarps = 4;
+constexpr int kManyMergeWarps = 8;
 
-// A warp per output row and head: the pieces of its two maps' units.
+// A block per 32 consecutive rows of a pair of kv-heads, lane t on row t, a warp per eighth of the columns (the partials' layout:
+// part_chunk).
 template <int HD>
 __global__ void __launch_bounds__(32 * kManyMergeWarps) diff_many_combine_kernel(const __grid_constant__ DiffParams p)
 {
-    constexpr int V4 = 2 * HD / 128;
-    const int lane = threadIdx.x & 31;
-    const int id = static_cast<int>(blockIdx.x) * kManyMergeWarps + (threadIdx.x >> 5);
-    ptx::griddep_launch_dependents();
-    if (id >= p.n_out) return;
+    constexpr int N = 2 * HD / 4 / kManyMergeWarps;  // 16-byte chunks of a warp
+    __shared__ float s_sum[kManyMergeWarps][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int lo = 0, hi = p.n_seqs - 1;
+    const int id = static_cast<int>(blockIdx.x);
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (p.seqs[mid].out0 <= id) lo = mid; else hi = mid - 1;
     }
     const DiffSeq &sq = p.seqs[lo];
-    const int heads = p.hq / 2, local = id - sq.out0, qi = local / heads, head = local - qi * heads;
-    const int pair = head / p.group, r = qi * p.group + head - pair * p.group;
-    const int row = r % DiffMany::kRows;
+    const int groups = (sq.n_q * p.group + 31) / 32, pair = (id - sq.out0) / groups, r0 = ((id - sq.out0) - pair * groups) * 32;
+    const int r = r0 + lane, qi = r / p.group, head = pair * p.group + r - qi * p.group;
     int u[2], c0[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-        u[x] = sq.unit0 + (2 * pair + x) * sq.n_blocks + r / DiffMany::kRows;
+        u[x] = sq.unit0 + (2 * pair + x) * sq.n_blocks + r0 / DiffMany::kRows;
         c0[x] = diff_first_taker(p, u[x]);
     }
+    ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    DiffMerge<HD> a[2];
+    const bool valid = qi < sq.n_q;
+    float4 y[N];
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int k = 0; k < N; ++k) y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        float m = -INFINITY, l = 0.f;
+        float4 o[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int c = c0[x]; c < p.n_takers && (c == c0[x] || p.start[c].u == u[x]); ++c) {
             if (diff_takes_nothing(p, c)) continue;
-            const int64_t at = static_cast<int64_t>(u[x] + c) * DiffMany::kSlotRows + row;
-            const float lse = __ldcg(p.part_lse + at);
-            float4 y[V4];
-            diff_load<HD>(p.part + at * 2 * HD, lane, y);
-            a[x].add(lse, y);
+            const int64_t at = static_cast<int64_t>(u[x] + c) * DiffMany::kSlotRows + r % DiffMany::kRows;
+            const float lse = valid ? __ldcg(p.part_lse + at) : -INFINITY;
+            float4 z[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) z[k] = __ldcg(part_chunk<2 * HD>(p.part, at, warp * N + k));
+            if (lse == -INFINITY) continue;  // (no key seen, or no row; what it holds is anything)
+            const float mn = fmaxf(m, lse), f = m == -INFINITY ? 0.f : ex2(m - mn), g = ex2(lse - mn);  // (NaN where lse is)
+            m = mn;
+            l = l * f + g;
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                o[k] = make_float4(o[k].x * f + z[k].x * g, o[k].y * f + z[k].y * g, o[k].z * f + z[k].z * g, o[k].w * f + z[k].w * g);
         }
-    float4 y[V4];
+        if (l == 0.f) continue;
+        const float g = (x ? -__ldg(p.lambda + head) : 1.f) / l;
 #pragma unroll
-    for (int v = 0; v < V4; ++v) y[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < N; ++k) y[k] = make_float4(y[k].x + g * o[k].x, y[k].y + g * o[k].y, y[k].z + g * o[k].z, y[k].w + g * o[k].w);
+    }
+    if (p.gain) {
+        float sum = 0.f;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) diff_axpy<HD>((x ? -p.lambda[head] : 1.f) * (a[x].l == 0.f ? 0.f : 1.f / a[x].l), a[x].o, a[x].l != 0.f, y);
-    diff_finish<HD>(p, static_cast<int64_t>(sq.q_row0 + qi) * heads + head, lane, y);
+        for (int k = 0; k < N; ++k) sum += y[k].x * y[k].x + y[k].y * y[k].y + y[k].z * y[k].z + y[k].w * y[k].w;
+        s_sum[warp][lane] = sum;
+        __syncthreads();
+        sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < kManyMergeWarps; ++k) sum += s_sum[k][lane];
+        const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float *g = p.gain + (warp * N + k) * 4;
+            y[k] = make_float4(y[k].x * f * __ldg(g), y[k].y * f * __ldg(g + 1), y[k].z * f * __ldg(g + 2), y[k].w * f * __ldg(g + 3));
+        }
+    }
+    if (!valid) return;
+    uint4 *dst = reinterpret_cast<uint4 *>(p.out + (static_cast<int64_t>(sq.q_row0 + qi) * (p.hq / 2) + head) * 2 * HD + warp * N * 4);
+#pragma unroll
+    for (int k = 0; k < N; k += 2)
+        dst[k / 2] = make_uint4(pack_bf16(y[k].x, y[k].y), pack_bf16(y[k].z, y[k].w), pack_bf16(y[k + 1].x, y[k + 1].y),
+                                pack_bf16(y[k + 1].z, y[k + 1].w));
 }
 
 cudaLaunchConfig_t diff_config(int blocks, int threads, int smem, cudaStream_t st, cudaLaunchAttribute *attr)
@@ -509,7 +544,7 @@ cudaError_t launch_diff_combine(int head_dim, bool many, const DiffParams &p, cu
     if (p.n_out <= 0) return cudaSuccess;
     cudaLaunchAttribute attr;
     if (many) {
-        const cudaLaunchConfig_t cfg = diff_config((p.n_out + kManyMergeWarps - 1) / kManyMergeWarps, 32 * kManyMergeWarps, 0, st, &attr);
+        const cudaLaunchConfig_t cfg = diff_config(p.n_out, 32 * kManyMergeWarps, 0, st, &attr);
         return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<128>, p)
                                : cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<64>, p);
     }

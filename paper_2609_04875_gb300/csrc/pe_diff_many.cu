@@ -39,8 +39,8 @@ struct ManyCfg {
     static constexpr int kOffMax = kOffV + kStages * kVBytes; // float [2][128]: the halves' maxima, or sums
     static constexpr int kOffNeed = kOffMax + 2 * 128 * 4;    // bool [2][128]: whose reference has to move
     static constexpr int kOffBar = kOffNeed + 2 * 128;
-    // k_full, k_empty, v_full, v_empty [stages]; q_full, meet, edge; s_full, p_full, o_done [2]
-    static constexpr int kNumBars = 4 * kStages + 3 + 6;
+    // k_full, k_empty, v_full, v_empty, v_peer [stages]; q_full, meet, edge; s_full, p_full, o_done [2]
+    static constexpr int kNumBars = 5 * kStages + 3 + 6;
     static constexpr int kOffMisc = kOffBar + kNumBars * 8;   // tmem slot, abort, votes [2], keys not finite [4]
     static constexpr int kDynSmem = kOffMisc + 32 + 1024;
     static constexpr int kTmemO = 256;                        // S at 0 and 128
@@ -62,9 +62,10 @@ __device__ __forceinline__ void arrive_cluster(uint32_t cluster_addr)
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
-// The same after writes to tensor memory alone (tcgen05.wait::st, tcgen05.fence): nothing else is handed over, and the release
-// of all memory at cluster scope, which a warp waits for, is not needed.
-__device__ __forceinline__ void arrive_cluster_tmem(uint32_t cluster_addr)
+// The same where no generic memory is handed over: what was written is tensor memory (tcgen05.wait::st, tcgen05.fence) or this
+// CTA's shared memory for its own tensor core (fence.proxy.async).  The release of all memory at cluster scope makes a warp wait
+// for its stores: at every tile it took 1.8 of 3.4 thousand cycles.
+__device__ __forceinline__ void arrive_peer(uint32_t cluster_addr)
 {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
@@ -166,7 +167,8 @@ __global__ void __launch_bounds__(kManyThreads, 1)
     const uint32_t b_k_empty = b_k_full + 8 * C::kStages;
     const uint32_t b_v_full = b_k_empty + 8 * C::kStages;
     const uint32_t b_v_empty = b_v_full + 8 * C::kStages;
-    const uint32_t b_q_full = b_v_empty + 8 * C::kStages;  // (the first CTA's: the softmax warps of both)
+    const uint32_t b_v_peer = b_v_empty + 8 * C::kStages;  // (the first CTA's: the other's V is there)
+    const uint32_t b_q_full = b_v_peer + 8 * C::kStages;   // (the first CTA's: the softmax warps of both)
     const uint32_t b_meet = b_q_full + 8;                  // this CTA's softmax warps among themselves
     const uint32_t b_edge = b_meet + 8;                    // the softmax warps of both
     const uint32_t b_s_full = b_edge + 8;                  // [2]
@@ -184,6 +186,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
             ptx::mbar_init(b_k_empty + 8 * s, 1);
             ptx::mbar_init(b_v_full + 8 * s, 1);
             ptx::mbar_init(b_v_empty + 8 * s, 1);
+            ptx::mbar_init(b_v_peer + 8 * s, 1);
         }
         ptx::mbar_init(b_q_full, 2 * kSoftWarps);
         ptx::mbar_init(b_meet, kSoftWarps);
@@ -221,7 +224,8 @@ __global__ void __launch_bounds__(kManyThreads, 1)
         const bool is_v = warp == 9;
         const CUtensorMap *map = is_v ? &tm_v : &tm_k;
         const uint32_t b_full = is_v ? b_v_full : b_k_full, b_empty = is_v ? b_v_empty : b_k_empty;
-        const uint32_t b_count = peer_addr(b_full, 0);
+        const bool both = !is_v;  // K's loads of both CTAs are counted in the first; V's each in its own, whose softmax waits too
+        const uint32_t b_count = peer_addr(b_full, both ? 0 : rank);
         const int rows = min(p.ps, 64), keys = is_v ? 128 : 64;
         const int n_ops = keys / rows * C::kRegions;  // <= 32
         const int op_page = lane / C::kRegions, op_reg = lane % C::kRegions;
@@ -242,7 +246,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
             for (int k = 0; k < w.n; ++k, ++i) {
                 const int next = k + 1 < w.n ? row_of(k + 1) : 0, s = i % C::kStages;
                 if (i >= C::kStages && !wait_bar_warp(b_empty + 8 * s, ((i / C::kStages) - 1) & 1, wctx)) { ok = false; break; }
-                if (rank == 0 && lane == 0) ptx::mbar_arrive_expect_tx(b_full + 8 * s, 2 * bytes);
+                if (lane == 0 && (!both || rank == 0)) ptx::mbar_arrive_expect_tx(b_full + 8 * s, both ? 2 * bytes : bytes);
                 __syncwarp();
                 if (on) tma_load_pair(base + s * bytes, map, op_reg * 64, y, b_count + 8 * s);
                 y = next;
@@ -252,7 +256,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
         for (int k = max(0, i - C::kStages); ok && k < i; ++k)
             ok = wait_bar_warp(b_empty + 8 * (k % C::kStages), (k / C::kStages) & 1, wctx);
         __syncwarp();
-        if (*abort_flag && lane == 0 && rank == 0) {  // a bounded chance for copies in flight to land, of both CTAs
+        if (*abort_flag && lane == 0 && (!both || rank == 0)) {  // a bounded chance for copies in flight to land
             const uint64_t g0 = ptx::globaltimer();
             for (int k = max(0, i - C::kStages); k < i; ++k)
                 while (!ptx::mbar_try_wait(b_full + 8 * (k % C::kStages), (k / C::kStages) & 1) && ptx::globaltimer() - g0 < 4000000ull) {}
@@ -278,13 +282,19 @@ __global__ void __launch_bounds__(kManyThreads, 1)
             commit_pair(b_k_empty + 8 * (j % C::kStages));
             return true;
         };
+        if (rank == 1) {  // tells the first CTA that this one's V is there
+            const uint32_t peer = peer_addr(b_v_peer, 0);
+            for (bool ok = true; ok && w.next();)
+                for (int k = 0; ok && k < w.n; ++k, ++i)
+                    if ((ok = full(b_v_full, i)) && lane == 0) arrive_peer(peer + 8 * (i % C::kStages));
+        }
         bool ok = rank == 0;
         for (int piece = 0; ok && w.next(); ++piece) {
             const int n = __shfl_sync(0xffffffffu, w.n, 0);
             if (!wait_cluster_warp(b_q_full, piece & 1, wctx)) break;
             ok = issue_s(i) && (n < 2 || issue_s(i + 1));
             for (int k = 0; ok && k < n; ++k, ++i) {
-                if (!full(b_v_full, i) || !wait_bar_warp(b_p_full + 8 * (i & 1), (i >> 1) & 1, wctx)) { ok = false; break; }
+                if (!full(b_v_full, i) || !full(b_v_peer, i) || !wait_bar_warp(b_p_full + 8 * (i & 1), (i >> 1) & 1, wctx)) { ok = false; break; }
                 ptx::tc_fence_after();
                 const uint64_t vd = v_desc + (i % C::kStages) * (C::kVBytes >> 4);
 #pragma unroll
@@ -313,22 +323,32 @@ __global__ void __launch_bounds__(kManyThreads, 1)
             if (lane == 0) ptx::mbar_arrive(b_meet);
             return wait_bar_warp(b_meet, met++ & 1, wctx);
         };
-        auto meet_pair = [&]() {
+        auto meet_pair = [&](bool tells) {  // tells: this warp wrote to the other CTA
             __syncwarp();
             if (lane == 0) {
-                arrive_cluster(edge0);
-                arrive_cluster(edge1);
+                if (tells) {
+                    arrive_cluster(edge0);
+                    arrive_cluster(edge1);
+                } else {
+                    arrive_peer(edge0);
+                    arrive_peer(edge1);
+                }
             }
             return wait_cluster_warp(b_edge, edges++ & 1, wctx);
         };
-        while (ok && w.next()) {
+        // The next piece: its row, and Q's into shared memory, each half half of it (the S products of the piece before are done)
+        int pos, pos_first;
+        bool valid, any;
+        auto begin = [&]() {
+            if (!w.next()) return false;
             const DiffSeq &sq = p.seqs[w.si];
             const int r = w.block * DiffMany::kRows + static_cast<int>(rank) * 128 + row;
             const int qi = r / p.group, head = 2 * (w.pair * p.group + r - qi * p.group) + w.map;
-            const bool valid = qi < sq.n_q, any = __any_sync(0xffffffffu, valid);
-            const int pos = sq.n_keys - sq.n_q + qi;
-            const int pos_first = sq.n_keys - sq.n_q + w.block * DiffMany::kRows / p.group;  // of the pair's rows
-            if (valid) {  // Q's row into shared memory, each half half of it (the S products of the piece before are done)
+            valid = qi < sq.n_q;
+            any = __any_sync(0xffffffffu, valid);
+            pos = sq.n_keys - sq.n_q + qi;
+            pos_first = sq.n_keys - sq.n_q + w.block * DiffMany::kRows / p.group;  // of the pair's rows
+            if (valid) {
                 const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (static_cast<int64_t>(sq.q_row0 + qi) * p.hq + head) * HD);
 #pragma unroll
                 for (int c0 = 0; c0 < HD / 16; ++c0) {
@@ -339,16 +359,19 @@ __global__ void __launch_bounds__(kManyThreads, 1)
             }
             ptx::fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) arrive_cluster(q_full);
+            if (lane == 0) arrive_peer(q_full);
+            return true;
+        };
+        for (bool more = begin(); ok && more;) {
             float m_ref = -INFINITY, l = 0.f;
-            for (int k = 0; k < w.n; ++k, ++i) {
-                const int kbase = (w.t0 + k) * 128;
+            const int n = w.n, t0 = w.t0;
+            for (int k = 0; k < n; ++k, ++i) {
+                const int kbase = (t0 + k) * 128;
                 const uint32_t tS = tmem + 128 * (i & 1) + 64 * half + lane_off;
                 const bool edge = kbase + 127 > pos_first;  // a row of the pair does not see some key of the tile
                 if (edge) {
                     // V of such keys (pe_diff.cu): each CTA looks through the kv-head that it holds, for both
-                    if (rank == 0 && !wait_bar_warp(b_v_full + 8 * (i % C::kStages), (i / C::kStages) & 1, wctx)) { ok = false; break; }
-                    if (!meet_pair()) { ok = false; break; }  // (the first CTA's barrier counts both CTAs' loads)
+                    if (!wait_bar_warp(b_v_full + 8 * (i % C::kStages), (i / C::kStages) & 1, wctx)) { ok = false; break; }
                     const int key = threadIdx.x & 127, c0 = half * (HD / 16);
                     uint8_t *v = smem + C::kOffV + (i % C::kStages) * C::kVBytes + key * 128;
                     uint32_t odd = 0;
@@ -360,7 +383,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
                         or_cluster(odd0 + 4 * (key >> 5), 1u << (key & 31));
                         or_cluster(odd1 + 4 * (key >> 5), 1u << (key & 31));
                     }
-                    if (!meet_pair()) { ok = false; break; }
+                    if (!meet_pair(__any_sync(0xffffffffu, is_odd))) { ok = false; break; }
                     uint32_t mask[4];
 #pragma unroll
                     for (int x = 0; x < 4; ++x) mask[x] = odd_keys[x];
@@ -374,9 +397,9 @@ __global__ void __launch_bounds__(kManyThreads, 1)
                             const int sees = pos - kbase - 32 * x + 1;  // of this word's keys
                             if (sees > 0 && (mask[x] & (sees >= 32 ? ~0u : (1u << sees) - 1))) l = NAN;
                         }
-                        if (!meet_pair()) { ok = false; break; }  // the mask is read
+                        if (!meet_pair(false)) { ok = false; break; }  // the mask is read
                         if (threadIdx.x < 4) odd_keys[threadIdx.x] = 0;
-                        if (!meet_pair()) { ok = false; break; }  // and cleared
+                        if (!meet_pair(true)) { ok = false; break; }   // and cleared
                     }
                 }
                 if (!wait_bar_warp(b_s_full + 8 * (i & 1), (i >> 1) & 1, wctx)) { ok = false; break; }
@@ -467,28 +490,32 @@ __global__ void __launch_bounds__(kManyThreads, 1)
                 ptx::tmem_wait_st();
                 ptx::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) arrive_cluster_tmem(p_full + 8 * (i & 1));
+                if (lane == 0) arrive_peer(p_full + 8 * (i & 1));
             }
-            if (!ok || !wait_bar_warp(b_o_done + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, wctx)) break;
+            if (!ok) break;
+            const bool had = valid, had_any = any;
+            const int64_t at = static_cast<int64_t>(w.slot) * DiffMany::kSlotRows + rank * 128 + row;
+            more = begin();  // its first S products run during what follows
+            if (!wait_bar_warp(b_o_done + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, wctx)) break;
             ptx::tc_fence_after();
-            s_max[half * 128 + row] = l;  // (the maxima of a tile are read before any thread is here)
+            s_max[half * 128 + row] = l;  // (P V waited for every warp: no maxima of the last tile are read any more)
             if (!meet()) break;
             l += s_max[(half ^ 1) * 128 + row];
-            if (any) {
+            if (!meet()) break;           // (of use again in the next piece's first tile)
+            if (had_any) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
-                const int64_t at = static_cast<int64_t>(w.slot) * DiffMany::kSlotRows + rank * 128 + row;
-                float4 *dst = reinterpret_cast<float4 *>(p.part + at * 2 * HD) + half * (HD / 4);
 #pragma unroll 1
                 for (int ch = 0; ch < HD / 32; ++ch) {
                     float o[32];
                     ptx::tmem_ld32(tmem + C::kTmemO + half * HD + lane_off + ch * 32, o);
                     ptx::tmem_wait_ld();
-                    if (valid && l != 0.f)
+                    if (had && l != 0.f)
 #pragma unroll
                         for (int x = 0; x < 8; ++x)
-                            dst[ch * 8 + x] = make_float4(o[4 * x] * inv, o[4 * x + 1] * inv, o[4 * x + 2] * inv, o[4 * x + 3] * inv);
+                            *part_chunk<2 * HD>(p.part, at, half * (HD / 4) + ch * 8 + x) =
+                                make_float4(o[4 * x] * inv, o[4 * x + 1] * inv, o[4 * x + 2] * inv, o[4 * x + 3] * inv);
                 }
-                if (valid && half == 0) p.part_lse[at] = l == 0.f ? -INFINITY : m_ref + __log2f(l);
+                if (had && half == 0) p.part_lse[at] = l == 0.f ? -INFINITY : m_ref + __log2f(l);
             }
             ptx::tc_fence_before();
         }

@@ -2317,7 +2317,8 @@ void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t ma
         q.unit0 = units;
         q.out0 = p.n_out;
         units += q.n_blocks * per_block;
-        p.n_out += it.n_q * (p.hq / 2);
+        // blocks of the merge: an output row and head, or 32 rows of a pair
+        p.n_out += Shape::kMaps == 1 ? it.n_q * (p.hq / 2) : static_cast<int32_t>(ceil_div(static_cast<int64_t>(it.n_q) * p.group, 32)) * (p.hkv / 2);
         int64_t one = 0;
         for (int b = 0; b < q.n_blocks; ++b) one += diff_tiles<Shape>(q, p.group, b);
         tiles += one * per_block;

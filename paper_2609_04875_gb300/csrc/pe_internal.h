@@ -123,7 +123,7 @@ struct DiffSeq {
     int32_t n_keys;        // the last query sees all of them
     int32_t n_blocks;
     int32_t unit0;
-    int32_t out0;          // first output of the launch: out0 + query * Hq / 2 + head
+    int32_t out0;          // first block of the merge: out0 + query * Hq / 2 + head; many rows: out0 + (pair, 32 rows)
 };
 
 struct DiffStart {
@@ -136,7 +136,8 @@ struct DiffParams {
     __nv_bfloat16 *out;          // bf16 [rows][Hq / 2][2 d]
     const float *lambda;         // [Hq / 2]
     const float *gain;           // [2 d], or null: no norm
-    float *part;                 // partials: O / l fp32 [slots][kSlotRows][2 d] (few rows: a map's 64, then the other's)
+    float *part;                 // partials: O / l fp32 [slots][kSlotRows] rows of 2 d (few rows: a map's 64, then the other's;
+                                 // many: in part_chunk's order)
     float *part_lse;             // [slots][kSlotRows], log2 units
     int32_t *status;
     int32_t n_seqs, hq, hkv, group, layer, num_pages, ps, log_ps;
