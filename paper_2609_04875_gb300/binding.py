@@ -78,7 +78,7 @@ _sigs = {
     "pe_seq_create": [_P, _I32P],
     "pe_seq_release": [_P, _I32, _P],
     "pe_crop": [_P, _I32, _I64, _I32P, _I32, _I32P, _P],
-    "pe_crop_batch": [_P, _I32, _I32P, _I64P, _P],
+    "pe_crop_batch": [_P, _I32, _P, _P, _P],
     "pe_append_kv": [_P, _I32, _P, _P, _I32, _P],
     "pe_append_kv_batch": [_P, _I32, _I32P, _P, _P, _I32P, _P],
     "pe_replay_attn": [_P, _I32, _I32, _P, _P, _I32, _I32, ctypes.c_float, _P],
@@ -115,9 +115,9 @@ _sigs = {
     "pe_read_kv_batch": [_P, _I32, _I32P, _I64P, _I32P, _P, _P, _P],
     "pe_replay_attn_weights_batch": [_P, _I32, _I32P, _I32, _P, _I32P, _P, _I32, ctypes.c_float, _P, _I64, _P],
     "pe_evict_batch": [_P, _I32, _I32P, _I32P, _I32, _I32, _P, _I64, _P, _I64, _P],
-    "pe_append_kv_rope_batch": [_P, _I32, _I32P, _P, _P, _I32P, ctypes.POINTER(_Rope), _P, _P, _P, _I32, _P],
-    "pe_rotate_batch": [_P, _I32, _I32P, _P, _I32P, _P, _I32, _I32, ctypes.POINTER(_Rope), _P, _P],
-    "pe_diff_attn_batch": [_P, _I32, _I32P, _I32, _P, _I32P, _P, _I32, ctypes.c_float, _P, _P, ctypes.c_float, _P],
+    "pe_append_kv_rope_batch": [_P, _I32, _P, _P, _P, _P, ctypes.POINTER(_Rope), _P, _P, _P, _I32, _P],
+    "pe_rotate_batch": [_P, _I32, _P, _P, _P, _P, _I32, _I32, ctypes.POINTER(_Rope), _P, _P],
+    "pe_diff_attn_batch": [_P, _I32, _P, _I32, _P, _P, _P, _I32, ctypes.c_float, _P, _P, ctypes.c_float, _P],
     "pe_attn_plan_launches": [_P, _I32, _I32P, _I32P, _I32, _I32, _I64P, _I64, _I64P],
 }
 for _name, _args in _sigs.items():
@@ -188,6 +188,19 @@ def i64_array(vals):
 
 
 _i32_array, _i64_array = i32_array, i64_array
+
+
+def _ints(vals, ctype=ctypes.c_int32):
+    """(what holds them, its address) of a host array for one call, in fewer steps than a ctypes array takes: the latter
+    cost a call of two such arrays 1.7 us more."""
+    if type(vals) is list:
+        try:
+            a = array.array(_ARRAY_CODES[ctype], vals)
+            return a, a.buffer_info()[0]
+        except (TypeError, OverflowError):  # entries that only int() converts
+            pass
+    a = _int_array(vals, ctype, _i32_types if ctype is ctypes.c_int32 else _i64_types)
+    return a, ctypes.addressof(a)
 
 
 def replay_schedule(agents_turns, policy):
@@ -442,7 +455,11 @@ class PagedKVCache:
 
     def crop_batch(self, seqs, taus, stream=None):
         _covers(seqs, taus, "taus", 0)
-        _check(_lib.pe_crop_batch(self._h, len(seqs), _i32_array(seqs), _i64_array(taus), self._s(stream)))
+        ids, ids_at = _ints(seqs)
+        at, taus_at = _ints(taus, ctypes.c_int64)
+        rc = _lib.pe_crop_batch(self._h, len(seqs), ids_at, taus_at, self._s(stream))
+        if rc:
+            _check(rc)
 
     # -- append (prefill write) ------------------------------------------------
     def append_kv(self, seq, K=None, V=None, n_tokens=None, stream=None):
@@ -485,14 +502,13 @@ class PagedKVCache:
         (``Q_out``: the tensor to write, Q itself among them).  ``positions``: CUDA int32 [axes][cu_tokens[-1]] (or
         [cu_tokens[-1]] for one axis); by default those that the tokens get in their sequences."""
         _covers(seqs, cu_tokens, "cu_tokens")
-        cu = _i32_array(cu_tokens)
         if not isinstance(rope, Rope):
             raise TypeError("rope must be a Rope")
         if K is None:
             if not self.host_only:
                 raise ValueError("K and V are required")
-            _check(_lib.pe_append_kv_rope_batch(self._h, len(seqs), _i32_array(seqs), None, None, cu, rope._ref, None, None,
-                                                None, 0, self._s(stream)))
+            _check(_lib.pe_append_kv_rope_batch(self._h, len(seqs), _i32_array(seqs), None, None, _i32_array(cu_tokens),
+                                                rope._ref, None, None, None, 0, self._s(stream)))
             return None
         self._check_kv(K, V)
         total = K.shape[1]
@@ -510,9 +526,12 @@ class PagedKVCache:
             q, q_out, heads = self._ptr(Q, "Q"), self._ptr(Q_out, "Q_out"), shape[2]
         elif Q_out is not None:
             raise ValueError("Q_out without Q")
-        _check(_lib.pe_append_kv_rope_batch(self._h, len(seqs), _i32_array(seqs), self._ptr(K, "K"), self._ptr(V, "V"), cu,
-                                            rope._ref, self._positions(positions, rope, total), q, q_out, heads,
-                                            self._s(stream)))
+        ids, ids_at = _ints(seqs)
+        cu, cu_at = _ints(cu_tokens)
+        rc = _lib.pe_append_kv_rope_batch(self._h, len(seqs), ids_at, self._ptr(K, "K"), self._ptr(V, "V"), cu_at, rope._ref,
+                                          self._positions(positions, rope, total), q, q_out, heads, self._s(stream))
+        if rc:
+            _check(rc)
         return Q_out
 
     def append_kv_rope(self, seq, K, V, rope, Q=None, positions=None, Q_out=None, stream=None):
@@ -532,9 +551,13 @@ class PagedKVCache:
         _same_shape(out, X, "out", "X")
         if out is None:
             out = self._output_like(X, stream)
-        _check(_lib.pe_rotate_batch(self._h, len(seqs), _i32_array(seqs), self._ptr(X, "X"), _i32_array(cu_tokens),
-                                    self._ptr(out, "out"), shape[0] if len(shape) == 4 else 1, shape[-2], rope._ref,
-                                    self._positions(positions, rope, shape[-3]), self._s(stream)))
+        ids, ids_at = _ints(seqs)
+        cu, cu_at = _ints(cu_tokens)
+        rc = _lib.pe_rotate_batch(self._h, len(seqs), ids_at, self._ptr(X, "X"), cu_at, self._ptr(out, "out"),
+                                  shape[0] if len(shape) == 4 else 1, shape[-2], rope._ref,
+                                  self._positions(positions, rope, shape[-3]), self._s(stream))
+        if rc:
+            _check(rc)
         return out
 
     def rotate(self, seq, X, rope, positions=None, out=None, stream=None):
@@ -626,10 +649,14 @@ class PagedKVCache:
         elif tuple(out.shape) != want:
             raise ValueError(f"out has shape {tuple(out.shape)}, it must be {want}")
         scale = self._default_scale if softmax_scale is None else float(softmax_scale)
-        _check(_lib.pe_diff_attn_batch(self._h, len(seqs), _i32_array(seqs), layer, self._ptr(Q, "Q"), _i32_array(cu_q),
-                                       self._ptr(out, "out"), shape[1], scale, self._vec(lam, "lam", shape[1] // 2),
-                                       None if gain is None else self._vec(gain, "gain", 2 * shape[2]), float(eps),
-                                       self._s(stream)))
+        ids, ids_at = _ints(seqs)
+        cu, cu_at = _ints(cu_q)
+        rc = _lib.pe_diff_attn_batch(self._h, len(seqs), ids_at, layer, self._ptr(Q, "Q"), cu_at, self._ptr(out, "out"), shape[1],
+                                     scale, self._vec(lam, "lam", shape[1] // 2),
+                                     None if gain is None else self._vec(gain, "gain", 2 * shape[2]), float(eps),
+                                     self._s(stream))
+        if rc:
+            _check(rc)
         return out
 
     def diff_attn(self, seq, layer, Q, lam, gain=None, eps=1e-5, out=None, softmax_scale=None, stream=None):

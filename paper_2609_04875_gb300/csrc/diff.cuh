@@ -66,67 +66,4 @@ __device__ __forceinline__ bool diff_takes_nothing(const DiffParams &p, int c)
     return p.start[c].u == p.start[c + 1].u && p.start[c].t == p.start[c + 1].t;
 }
 
-// A partial row's columns 4 lane .. + 3 of every 128.
-template <int HD>
-__device__ __forceinline__ void diff_load(const float *row, int lane, float4 (&y)[2 * HD / 128])
-{
-#pragma unroll
-    for (int v = 0; v < 2 * HD / 128; ++v) y[v] = __ldcg(reinterpret_cast<const float4 *>(row) + v * 32 + lane);
-}
-
-// Pieces of one row and map: o = sum 2^(lse - m) O, l = sum 2^(lse - m).
-template <int HD>
-struct DiffMerge {
-    float m = -INFINITY, l = 0.f;
-    float4 o[2 * HD / 128];
-    __device__ __forceinline__ DiffMerge()
-    {
-#pragma unroll
-        for (int v = 0; v < 2 * HD / 128; ++v) o[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    __device__ __forceinline__ void add(float lse, const float4 (&y)[2 * HD / 128])
-    {
-        if (lse == -INFINITY) return;  // (no key seen; its row may hold anything)
-        const float mn = fmaxf(m, lse);
-        const float f = m == -INFINITY ? 0.f : ex2(m - mn), g = ex2(lse - mn);  // (NaN where lse is)
-        m = mn;
-        l = l * f + g;
-#pragma unroll
-        for (int v = 0; v < 2 * HD / 128; ++v)
-            o[v] = make_float4(o[v].x * f + y[v].x * g, o[v].y * f + y[v].y * g, o[v].z * f + y[v].z * g, o[v].w * f + y[v].w * g);
-    }
-};
-
-template <int HD>
-__device__ __forceinline__ void diff_axpy(float g, const float4 (&z)[2 * HD / 128], bool on, float4 (&y)[2 * HD / 128])
-{
-    if (!on) return;
-#pragma unroll
-    for (int v = 0; v < 2 * HD / 128; ++v)
-        y[v] = make_float4(y[v].x + g * z[v].x, y[v].y + g * z[v].y, y[v].z + g * z[v].z, y[v].w + g * z[v].w);
-}
-
-// The norm over a head's 2d columns, held by a warp, and the output row.
-template <int HD>
-__device__ __forceinline__ void diff_finish(const DiffParams &p, int64_t out_row, int lane, float4 (&y)[2 * HD / 128])
-{
-    constexpr int V4 = 2 * HD / 128;
-    if (p.gain) {
-        float sum = 0.f;
-#pragma unroll
-        for (int v = 0; v < V4; ++v) sum += y[v].x * y[v].x + y[v].y * y[v].y + y[v].z * y[v].z + y[v].w * y[v].w;
-#pragma unroll
-        for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-        const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
-#pragma unroll
-        for (int v = 0; v < V4; ++v) {
-            const float *g = p.gain + v * 128 + lane * 4;  // (a vector of any alignment)
-            y[v] = make_float4(y[v].x * f * __ldg(g), y[v].y * f * __ldg(g + 1), y[v].z * f * __ldg(g + 2), y[v].w * f * __ldg(g + 3));
-        }
-    }
-    uint2 *dst = reinterpret_cast<uint2 *>(p.out + out_row * 2 * HD);
-#pragma unroll
-    for (int v = 0; v < V4; ++v) dst[v * 32 + lane] = make_uint2(pack_bf16(y[v].x, y[v].y), pack_bf16(y[v].z, y[v].w));
-}
-
 }  // namespace pe

@@ -351,17 +351,18 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
     }
 }
 
-constexpr int kMergeWarps = 4;
+constexpr int kMergeWarps = 8;
 
-// A block per output row and head: warp x joins pieces x, x + 4, ... of both maps, lane t the columns 4t .. + 3 of every 128;
-// then the first warp the four.
+// A block per output row and head, a warp per eighth of its columns, in each warp groups of lanes with every fourth (d = 64:
+// eighth) piece.  Hardly any shared memory, so that a block is resident, waiting, while the attention still runs.
 template <int HD>
 __global__ void __launch_bounds__(32 * kMergeWarps) diff_combine_kernel(const __grid_constant__ DiffParams p)
 {
-    constexpr int V4 = 2 * HD / 128;  // float4 a lane
-    __shared__ float s_m[2][kMergeWarps], s_l[2][kMergeWarps];
-    __shared__ float4 s_o[2][kMergeWarps][2 * HD / 4];
+    constexpr int kLanes = 2 * HD / kMergeWarps / 4;  // of a group: a float4 each
+    constexpr int kGroups = 32 / kLanes;
+    __shared__ float s_sum[kMergeWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int col = warp * kLanes + lane % kLanes;    // in float4
     int lo = 0, hi = p.n_seqs - 1;
     const int id = static_cast<int>(blockIdx.x);
     while (lo < hi) {
@@ -375,54 +376,64 @@ __global__ void __launch_bounds__(32 * kMergeWarps) diff_combine_kernel(const __
     const int c0 = diff_first_taker(p, u);
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    DiffMerge<HD> a[2];
-    for (int c = c0 + warp; c < p.n_takers && (c == c0 || p.start[c].u == u); c += kMergeWarps) {
-        if (diff_takes_nothing(p, c)) continue;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 2
+    for (int c = c0 + lane / kLanes; c < p.n_takers && (c == c0 || p.start[c].u == u); c += kGroups) {
         const int64_t at = static_cast<int64_t>(u + c) * DiffFew::kSlotRows + row;
         float lse[2];
-        float4 y[2][V4];
+        float4 y[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             lse[x] = __ldcg(p.part_lse + at + x * DiffFew::kRows);
-            diff_load<HD>(p.part + (at + x * DiffFew::kRows) * 2 * HD, lane, y[x]);
+            y[x] = __ldcg(reinterpret_cast<const float4 *>(p.part + (at + x * DiffFew::kRows) * 2 * HD) + col);
         }
+        if (diff_takes_nothing(p, c)) continue;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) a[x].add(lse[x], y[x]);
+        for (int x = 0; x < 2; ++x) {
+            if (lse[x] == -INFINITY) continue;  // (no key seen; its row may hold anything)
+            const float mn = fmaxf(m[x], lse[x]);
+            const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - mn), g = ex2(lse[x] - mn);  // (NaN where lse is)
+            m[x] = mn;
+            l[x] = l[x] * f + g;
+            o[x] = make_float4(o[x].x * f + y[x].x * g, o[x].y * f + y[x].y * g, o[x].z * f + y[x].z * g, o[x].w * f + y[x].w * g);
+        }
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-        if (lane == 0) {
-            s_m[x][warp] = a[x].m;
-            s_l[x][warp] = a[x].l;
-        }
+        float mx = m[x];
 #pragma unroll
-        for (int v = 0; v < V4; ++v) s_o[x][warp][v * 32 + lane] = a[x].o[v];
-    }
-    __syncthreads();
-    if (warp > 0) return;
-    float4 y[V4];
+        for (int k = kLanes; k < 32; k <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
+        const float f = l[x] == 0.f ? 0.f : ex2(m[x] - mx);
+        l[x] *= f;
+        o[x] = make_float4(o[x].x * f, o[x].y * f, o[x].z * f, o[x].w * f);
 #pragma unroll
-    for (int v = 0; v < V4; ++v) y[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        float mx = -INFINITY, den = 0.f, f[kMergeWarps];
-#pragma unroll
-        for (int k = 0; k < kMergeWarps; ++k) mx = fmaxf(mx, s_m[x][k]);
-#pragma unroll
-        for (int k = 0; k < kMergeWarps; ++k) {
-            f[k] = s_l[x][k] == 0.f ? 0.f : ex2(s_m[x][k] - mx);
-            den += f[k] * s_l[x][k];
-        }
-        const float part = (x ? -p.lambda[head] : 1.f) * (den == 0.f ? 0.f : 1.f / den);
-#pragma unroll
-        for (int k = 0; k < kMergeWarps; ++k) {
-            float4 z[V4];
-#pragma unroll
-            for (int v = 0; v < V4; ++v) z[v] = s_o[x][k][v * 32 + lane];
-            diff_axpy<HD>(f[k] * part, z, f[k] != 0.f, y);
+        for (int k = kLanes; k < 32; k <<= 1) {
+            l[x] += __shfl_xor_sync(0xffffffffu, l[x], k);
+            o[x].x += __shfl_xor_sync(0xffffffffu, o[x].x, k);
+            o[x].y += __shfl_xor_sync(0xffffffffu, o[x].y, k);
+            o[x].z += __shfl_xor_sync(0xffffffffu, o[x].z, k);
+            o[x].w += __shfl_xor_sync(0xffffffffu, o[x].w, k);
         }
     }
-    diff_finish<HD>(p, static_cast<int64_t>(sq.q_row0 + qi) * heads + head, lane, y);
+    const float g0 = l[0] == 0.f ? 0.f : 1.f / l[0], g1 = l[1] == 0.f ? 0.f : -__ldg(p.lambda + head) / l[1];
+    float4 y = make_float4(g0 * o[0].x + g1 * o[1].x, g0 * o[0].y + g1 * o[1].y, g0 * o[0].z + g1 * o[1].z, g0 * o[0].w + g1 * o[1].w);
+    if (p.gain) {
+        float sum = y.x * y.x + y.y * y.y + y.z * y.z + y.w * y.w;
+#pragma unroll
+        for (int k = 1; k < kLanes; k <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        if (lane == 0) s_sum[warp] = sum;
+        __syncthreads();
+        sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < kMergeWarps; ++k) sum += s_sum[k];
+        const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
+        const float *g = p.gain + col * 4;  // (a vector of any alignment)
+        y = make_float4(y.x * f * __ldg(g), y.y * f * __ldg(g + 1), y.z * f * __ldg(g + 2), y.w * f * __ldg(g + 3));
+    }
+    if (lane < kLanes)
+        reinterpret_cast<uint2 *>(p.out + (static_cast<int64_t>(sq.q_row0 + qi) * heads + head) * 2 * HD)[col] =
+            make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
 }
 
 constexpr int kManyMergeWarps = 8;

@@ -63,33 +63,6 @@ __device__ __forceinline__ void rope_chunk(const RopeParams &r, const uint4 *row
     }
 }
 
-// The same where n_pairs is a multiple of 8: the other half of each of the chunk's pairs is one chunk, or this one.
-__device__ __forceinline__ void rope_chunk_whole(const RopeParams &r, const uint4 *row, int chunk, int64_t tok, int pos, float (&y)[8])
-{
-    const int whole = r.n_pairs / 8;
-    unpack8(__ldg(row + chunk), y);
-    if (chunk >= 2 * whole) return;
-    if (r.interleaved) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 t = rope_turn(r, 4 * chunk + k, tok, pos);
-            const float p = y[2 * k], q = y[2 * k + 1];
-            y[2 * k] = p * t.x - q * t.y;
-            y[2 * k + 1] = q * t.x + p * t.y;
-        }
-        return;
-    }
-    const bool second = chunk >= whole;
-    float z[8];
-    unpack8(__ldg(row + (second ? chunk - whole : chunk + whole)), z);
-    const float sign = second ? 1.f : -1.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const float2 t = rope_turn(r, 8 * (second ? chunk - whole : chunk) + k, tok, pos);
-        y[k] = y[k] * t.x + z[k] * (sign * t.y);
-    }
-}
-
 // A thread's share of every row of a token: two chunks of eight columns, a and b, which are either copied or eight whole
 // pairs, whose angles it keeps.  In halves those are chunks c and c + n_pairs / 8, of neighbours 2c and 2c + 1.
 template <int CPR>
@@ -295,11 +268,61 @@ cudaLaunchConfig_t serial_config(int64_t blocks, unsigned threads, cudaStream_t 
     return cfg;
 }
 
-// Page by page (append_q8_kernel): the new rows of K rotated in 32 bits, so that a value is rounded once, to its code.
-template <typename Params, int CPR, int NC, bool WHOLE>
-__global__ void __launch_bounds__(kQ8Block) append_rope_q8_kernel(const __grid_constant__ Params p, int threads, int page_blocks, int tokens,
-                                                                  int head_blocks, int head_block)
+// (cos, sin) of a page's new rows, in shared memory.  Where n_pairs is a multiple of 8, pair 8c + k of a row stands at k *
+// (n_pairs / 8) + c, so that lanes on neighbouring chunks read neighbouring entries.
+template <bool WHOLE>
+__device__ __forceinline__ int turn_at(int n_pairs, int i)
 {
+    return WHOLE ? (i & 7) * (n_pairs >> 3) + (i >> 3) : i;
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ void rope_chunk_table(const RopeParams &r, const float2 *turns, const uint4 *row, int chunk, float (&y)[8])
+{
+    const int n = r.n_pairs;
+    unpack8(__ldg(row + chunk), y);
+    if (chunk * 8 >= 2 * n) return;
+    if (r.interleaved) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (!WHOLE && 4 * chunk + k >= n) break;
+            const float2 t = turns[turn_at<WHOLE>(n, 4 * chunk + k)];
+            const float a = y[2 * k], b = y[2 * k + 1];
+            y[2 * k] = a * t.x - b * t.y;
+            y[2 * k + 1] = b * t.x + a * t.y;
+        }
+    } else if (WHOLE) {
+        const int whole = n >> 3, c = chunk < whole ? chunk : chunk - whole;
+        const float sign = chunk < whole ? -1.f : 1.f;
+        float z[8];
+        unpack8(__ldg(row + (chunk < whole ? chunk + whole : c)), z);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float2 t = turns[k * whole + c];
+            y[k] = y[k] * t.x + z[k] * (sign * t.y);
+        }
+    } else {
+        const __nv_bfloat16 *x = reinterpret_cast<const __nv_bfloat16 *>(row);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int col = chunk * 8 + k;
+            if (col >= 2 * n) break;
+            const bool second = col >= n;
+            const float2 t = turns[second ? col - n : col];
+            const float z = __bfloat162float(x[second ? col - n : col + n]);
+            y[k] = y[k] * t.x + (second ? z : -z) * t.y;
+        }
+    }
+}
+
+// A block per page and layer (append_q8_kernel works head by head), heads [h0, h1) of it one group after another: the angles
+// of the page's new rows are computed once.  K's new rows turn in 32 bits, so that a value is rounded once, to its code.
+// (With the angles computed where a chunk is read, 8 times unrolled: 16 agents x 32 layers, one token, 27 us.)
+template <typename Params, int CPR, int NC, bool WHOLE>
+__global__ void __launch_bounds__(kQ8Block, NC == 8 ? 1 : 3) append_rope_q8_kernel(const __grid_constant__ Params p, int threads, int page_blocks, int parts,
+                                                                  int tokens, int head_blocks, int head_block)
+{
+    extern __shared__ float2 turns[];
     __shared__ uint32_t s_max[kQ8Block / 32];
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
@@ -318,12 +341,10 @@ __global__ void __launch_bounds__(kQ8Block) append_rope_q8_kernel(const __grid_c
         return;
     }
     if (blockIdx.x == 0) enter_pages(a);
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kQ8Block / threads) + threadIdx.x / threads;
-    const bool on = unit < static_cast<int64_t>(a.L) * a.seg_tokens * a.hkv;
-    const int64_t u = on ? unit : 0;
-    const int h = static_cast<int>(u % a.hkv);
-    const int64_t r = u / a.hkv;
-    const int pg = static_cast<int>(r % a.seg_tokens);
+    int r = static_cast<int>(blockIdx.x);
+    const int part = r % parts;
+    r /= parts;
+    const int pg = r % a.seg_tokens;
     const int64_t l = r / a.seg_tokens;
     const AppendSeg &sg = a.segs[find_seg(a.segs, a.n_segs, pg)];
     const int lp = sg.len0 / a.ps + (pg - sg.cum0);
@@ -331,32 +352,41 @@ __global__ void __launch_bounds__(kQ8Block) append_rope_q8_kernel(const __grid_c
     const int pos0 = lp * a.ps;
     const int old = max(0, sg.len0 - pos0);
     const int rows = min(a.ps, sg.len0 + sg.n_tokens - pos0);
-    const int64_t head = (l * a.num_pages + page) * a.hkv + h;
-    uint8_t *kp = reinterpret_cast<uint8_t *>(a.k_pool) + head * a.ps * HD;
-    uint8_t *vp = reinterpret_cast<uint8_t *>(a.v_pool) + head * a.ps * HD;
-    int8_t *ex = a.exps + head * 2;
-    int ke0 = 0, ve0 = 0;
-    if (on && old > 0) {
-        ke0 = ex[0];
-        ve0 = ex[1];
-    }
-    const float kes = pow2i(ke0), ves = pow2i(ve0);
     const int64_t tok0 = sg.tok0 + (pos0 - sg.len0);  // of the page's row 0
-    if (threads <= 32) __syncwarp();
-    else __syncthreads();  // the old exponents are read before they are written
-    q8_write_page_f32<CPR, NC>(on, threadIdx.x % threads, threads, rows, old, ke0, ve0, kp, vp, ex, s_max,
-                               [&](int row, int col8, float (&k)[8], uint4 &v) {
-                                   if (row < old) {
-                                       q8_to_float(*reinterpret_cast<const uint2 *>(kp + row * HD + col8 * 8), kes, k);
-                                       v = q8_to_bf16(*reinterpret_cast<const uint2 *>(vp + row * HD + col8 * 8), ves);
-                                   } else {
-                                       const int64_t tok = tok0 + row;
-                                       const int64_t s = ((l * a.n_total + tok) * a.hkv + h) * CPR;
-                                       if constexpr (WHOLE) rope_chunk_whole(p.c.r, a.K + s, col8, tok, pos0 + row, k);
-                                       else rope_chunk(p.c.r, a.K + s, col8, tok, pos0 + row, k);
-                                       v = a.V[s + col8];
-                                   }
-                               });
+    const int n = p.c.r.n_pairs;
+    for (int x = threadIdx.x; x < (rows - old) * n; x += kQ8Block) {
+        const int row = x / n, i = x - row * n;
+        turns[row * n + turn_at<WHOLE>(n, i)] = rope_turn(p.c.r, i, tok0 + old + row, pos0 + old + row);
+    }
+    __syncthreads();
+    const int groups = kQ8Block / threads, share = (a.hkv + parts - 1) / parts, h1 = min(a.hkv, (part + 1) * share);
+    for (int hb = part * share; hb < h1; hb += groups) {
+        const int h = hb + threadIdx.x / threads;
+        const bool on = h < h1;
+        const int64_t head = (l * a.num_pages + page) * a.hkv + (on ? h : 0);
+        uint8_t *kp = reinterpret_cast<uint8_t *>(a.k_pool) + head * a.ps * HD;
+        uint8_t *vp = reinterpret_cast<uint8_t *>(a.v_pool) + head * a.ps * HD;
+        int8_t *ex = a.exps + head * 2;
+        int ke0 = 0, ve0 = 0;
+        if (on && old > 0) {
+            ke0 = ex[0];
+            ve0 = ex[1];
+        }
+        const float kes = pow2i(ke0), ves = pow2i(ve0);
+        if (threads <= 32) __syncwarp();
+        else __syncthreads();  // the old exponents are read before they are written
+        q8_write_page_f32<CPR, NC>(on, threadIdx.x % threads, threads, rows, old, ke0, ve0, kp, vp, ex, s_max,
+                                   [&](int row, int col8, float (&k)[8], uint4 &v) {
+                                       if (row < old) {
+                                           q8_to_float(*reinterpret_cast<const uint2 *>(kp + row * HD + col8 * 8), kes, k);
+                                           v = q8_to_bf16(*reinterpret_cast<const uint2 *>(vp + row * HD + col8 * 8), ves);
+                                       } else {
+                                           const int64_t s = ((l * a.n_total + tok0 + row) * a.hkv + h) * CPR;
+                                           v = __ldg(a.V + s + col8);
+                                           rope_chunk_table<WHOLE>(p.c.r, turns + (row - old) * n, a.K + s, col8, k);
+                                       }
+                                   });
+    }
 }
 
 constexpr int kSmallSegs = 16, kSmallPages = 128;  // the small parameter block (as in pe_kv.cu)
@@ -384,17 +414,29 @@ cudaError_t launch_append_rope_t(bool q8, const Params &p, cudaStream_t st)
         const cudaLaunchConfig_t cfg = serial_config(blocks, kRowThreads, st, &attr);
         return cudaLaunchKernelEx(&cfg, append_rope_kernel<Params, CPR, WHOLE>, p, nb, hb);
     }
-    const int elems = p.a.ps * CPR * 8, threads = q8_unit_threads(elems), nc = q8_unit_chunks(elems);
-    const int64_t units = static_cast<int64_t>(p.a.L) * p.a.seg_tokens * p.a.hkv;
-    const int64_t page_blocks = (units * threads + kQ8Block - 1) / kQ8Block;
-    const int64_t blocks = page_blocks + (lt * nb + kQ8Block / 32 - 1) / (kQ8Block / 32);
+    // threads that share a page of one kv-head: half as many chunks each as append_q8_kernel's, for K takes twice the registers
+    const int elems = p.a.ps * CPR * 8, threads = std::max(32, std::min(kQ8Block, elems / 32)), nc = elems / 8 / threads;
+    // a page's heads over as many blocks as there are groups of them, while the blocks are few
+    const int64_t pages = static_cast<int64_t>(p.a.L) * p.a.seg_tokens;
+    const int groups = kQ8Block / threads, most = (p.a.hkv + groups - 1) / groups;
+    int parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, 8 * 152 / std::max<int64_t>(1, pages))));
+    parts = (most + (most + parts - 1) / parts - 1) / ((most + parts - 1) / parts);  // (none without a group)
+    int64_t longest = 0;
+    for (int i = 0; i < p.a.n_segs; ++i) longest = std::max<int64_t>(longest, p.a.segs[i].n_tokens);
+    const int64_t page_blocks = pages * parts, blocks = page_blocks + (lt * nb + kQ8Block / 32 - 1) / (kQ8Block / 32);
     if (blocks > INT32_MAX) return cudaErrorInvalidValue;
-    const cudaLaunchConfig_t cfg = serial_config(blocks, kQ8Block, st, &attr);
+    cudaLaunchConfig_t cfg = serial_config(blocks, kQ8Block, st, &attr);
+    cfg.dynamicSmemBytes = static_cast<size_t>(std::min<int64_t>(p.a.ps, longest)) * p.c.r.n_pairs * sizeof(float2);
     const int pb = static_cast<int>(page_blocks), n = static_cast<int>(tokens);
-    if (nc == 8) return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, CPR, 8, WHOLE>, p, threads, pb, n, std::max(1, nb), hb);
-    if (CPR == 16 || nc == 4)
-        return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, CPR, 4, WHOLE>, p, threads, pb, n, std::max(1, nb), hb);
-    return cudaLaunchKernelEx(&cfg, append_rope_q8_kernel<Params, CPR, 2, WHOLE>, p, threads, pb, n, std::max(1, nb), hb);
+    auto launch = [&](auto kernel, std::atomic<uint64_t> &configured) {
+        if (cudaError_t e = set_dyn_smem_once(kernel, 128 * kRopeMaxPairs * static_cast<int>(sizeof(float2)), configured); e != cudaSuccess)
+            return e;
+        return cudaLaunchKernelEx(&cfg, kernel, p, threads, pb, parts, n, std::max(1, nb), hb);
+    };
+    static std::atomic<uint64_t> done[3];
+    if (nc == 8) return launch(append_rope_q8_kernel<Params, CPR, 8, WHOLE>, done[0]);
+    if (CPR == 16 || nc == 4) return launch(append_rope_q8_kernel<Params, CPR, 4, WHOLE>, done[1]);
+    return launch(append_rope_q8_kernel<Params, CPR, 2, WHOLE>, done[2]);
 }
 
 template <int SEGS, int PAGES>
