@@ -61,9 +61,15 @@ __device__ __forceinline__ int diff_first_taker(const DiffParams &p, int u)
     return lo;
 }
 
-__device__ __forceinline__ bool diff_takes_nothing(const DiffParams &p, int c)
+// And the one that holds its last.
+__device__ __forceinline__ int diff_last_taker(const DiffParams &p, int u)
 {
-    return p.start[c].u == p.start[c + 1].u && p.start[c].t == p.start[c + 1].t;
+    int lo = 0, hi = p.n_takers - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.start[mid].u <= u) lo = mid; else hi = mid - 1;
+    }
+    return lo;
 }
 
 }  // namespace pe

@@ -351,12 +351,12 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
     }
 }
 
-constexpr int kMergeWarps = 8;
+constexpr int kMergeWarps = 8, kMergeBatch = 4;  // pieces in flight
 
 // A block per output row and head, a warp per eighth of its columns, in each warp groups of lanes with every fourth (d = 64:
 // eighth) piece.  Hardly any shared memory, so that a block is resident, waiting, while the attention still runs.
 template <int HD>
-__global__ void __launch_bounds__(32 * kMergeWarps) diff_combine_kernel(const __grid_constant__ DiffParams p)
+__global__ void __launch_bounds__(32 * kMergeWarps, 4) diff_combine_kernel(const __grid_constant__ DiffParams p)
 {
     constexpr int kLanes = 2 * HD / kMergeWarps / 4;  // of a group: a float4 each
     constexpr int kGroups = 32 / kLanes;
@@ -373,31 +373,36 @@ __global__ void __launch_bounds__(32 * kMergeWarps) diff_combine_kernel(const __
     const int heads = p.hq / 2, local = id - sq.out0, qi = local / heads, head = local - qi * heads;
     const int pair = head / p.group, r = qi * p.group + head - pair * p.group;
     const int u = sq.unit0 + pair * sq.n_blocks + r / DiffFew::kRows, row = r % DiffFew::kRows;
-    const int c0 = diff_first_taker(p, u);
+    const int c0 = diff_first_taker(p, u), c1 = diff_last_taker(p, u);
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-#pragma unroll 2
-    for (int c = c0 + lane / kLanes; c < p.n_takers && (c == c0 || p.start[c].u == u); c += kGroups) {
-        const int64_t at = static_cast<int64_t>(u + c) * DiffFew::kSlotRows + row;
-        float lse[2];
-        float4 y[2];
+    for (int cb = c0 + lane / kLanes; cb <= c1; cb += kMergeBatch * kGroups) {
+        float lse[kMergeBatch][2];
+        float4 y[kMergeBatch][2];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            lse[x] = __ldcg(p.part_lse + at + x * DiffFew::kRows);
-            y[x] = __ldcg(reinterpret_cast<const float4 *>(p.part + (at + x * DiffFew::kRows) * 2 * HD) + col);
-        }
-        if (diff_takes_nothing(p, c)) continue;
+        for (int b = 0; b < kMergeBatch; ++b) {
+            const int c = min(cb + b * kGroups, c1);
+            const int64_t at = static_cast<int64_t>(u + c) * DiffFew::kSlotRows + row;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            if (lse[x] == -INFINITY) continue;  // (no key seen; its row may hold anything)
-            const float mn = fmaxf(m[x], lse[x]);
-            const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - mn), g = ex2(lse[x] - mn);  // (NaN where lse is)
-            m[x] = mn;
-            l[x] = l[x] * f + g;
-            o[x] = make_float4(o[x].x * f + y[x].x * g, o[x].y * f + y[x].y * g, o[x].z * f + y[x].z * g, o[x].w * f + y[x].w * g);
+            for (int x = 0; x < 2; ++x) {
+                lse[b][x] = __ldcg(p.part_lse + at + x * DiffFew::kRows);
+                y[b][x] = __ldcg(reinterpret_cast<const float4 *>(p.part + (at + x * DiffFew::kRows) * 2 * HD) + col);
+            }
         }
+#pragma unroll
+        for (int b = 0; b < kMergeBatch; ++b)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (cb + b * kGroups > c1 || lse[b][x] == -INFINITY) continue;  // (no key seen: its row may hold anything)
+                const float mn = fmaxf(m[x], lse[b][x]);
+                const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - mn), g = ex2(lse[b][x] - mn);  // (NaN where lse is)
+                const float4 z = y[b][x];
+                m[x] = mn;
+                l[x] = l[x] * f + g;
+                o[x] = make_float4(o[x].x * f + z.x * g, o[x].y * f + z.y * g, o[x].z * f + z.z * g, o[x].w * f + z.w * g);
+            }
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -436,6 +441,87 @@ __global__ void __launch_bounds__(32 * kMergeWarps) diff_combine_kernel(const __
             make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
 }
 
+constexpr int kRowMergeWarps = 4;
+
+// A warp per output row and head, two pieces of both maps in flight.
+template <int HD>
+__global__ void __launch_bounds__(32 * kRowMergeWarps) diff_row_combine_kernel(const __grid_constant__ DiffParams p)
+{
+    constexpr int V4 = 2 * HD / 128;  // float4 a lane
+    const int lane = threadIdx.x & 31, id = static_cast<int>(blockIdx.x) * kRowMergeWarps + (threadIdx.x >> 5);
+    ptx::griddep_launch_dependents();
+    if (id >= p.n_out) return;
+    int lo = 0, hi = p.n_seqs - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.seqs[mid].out0 <= id) lo = mid; else hi = mid - 1;
+    }
+    const DiffSeq &sq = p.seqs[lo];
+    const int heads = p.hq / 2, local = id - sq.out0, qi = local / heads, head = local - qi * heads;
+    const int pair = head / p.group, r = qi * p.group + head - pair * p.group;
+    const int u = sq.unit0 + pair * sq.n_blocks + r / DiffFew::kRows, row = r % DiffFew::kRows;
+    const int c0 = diff_first_taker(p, u), c1 = diff_last_taker(p, u);
+    ptx::griddep_wait();
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float4 o[2][V4];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int v = 0; v < V4; ++v) o[x][v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = c0; c <= c1; c += 2) {
+        float lse[2][2];
+        float4 y[2][2][V4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            if (c + b <= c1) {
+                const int64_t at = static_cast<int64_t>(u + c + b) * DiffFew::kSlotRows + row;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    lse[b][x] = __ldcg(p.part_lse + at + x * DiffFew::kRows);
+#pragma unroll
+                    for (int v = 0; v < V4; ++v)
+                        y[b][x][v] = __ldcg(reinterpret_cast<const float4 *>(p.part + (at + x * DiffFew::kRows) * 2 * HD) + v * 32 + lane);
+                }
+            }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (c + b > c1 || lse[b][x] == -INFINITY) continue;  // (no key seen: its row may hold anything)
+                const float mn = fmaxf(m[x], lse[b][x]);
+                const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - mn), g = ex2(lse[b][x] - mn);  // (NaN where lse is)
+                m[x] = mn;
+                l[x] = l[x] * f + g;
+#pragma unroll
+                for (int v = 0; v < V4; ++v) {
+                    const float4 z = y[b][x][v];
+                    o[x][v] = make_float4(o[x][v].x * f + z.x * g, o[x][v].y * f + z.y * g, o[x][v].z * f + z.z * g, o[x][v].w * f + z.w * g);
+                }
+            }
+    }
+    const float g0 = l[0] == 0.f ? 0.f : 1.f / l[0], g1 = l[1] == 0.f ? 0.f : -__ldg(p.lambda + head) / l[1];
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < V4; ++v) {
+        const float4 a = o[0][v], b = o[1][v];
+        o[0][v] = make_float4(g0 * a.x + g1 * b.x, g0 * a.y + g1 * b.y, g0 * a.z + g1 * b.z, g0 * a.w + g1 * b.w);
+        sum += o[0][v].x * o[0][v].x + o[0][v].y * o[0][v].y + o[0][v].z * o[0][v].z + o[0][v].w * o[0][v].w;
+    }
+    if (p.gain) {
+#pragma unroll
+        for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
+#pragma unroll
+        for (int v = 0; v < V4; ++v) {
+            const float *g = p.gain + v * 128 + lane * 4;  // (a vector of any alignment)
+            o[0][v] = make_float4(o[0][v].x * f * __ldg(g), o[0][v].y * f * __ldg(g + 1), o[0][v].z * f * __ldg(g + 2), o[0][v].w * f * __ldg(g + 3));
+        }
+    }
+    uint2 *dst = reinterpret_cast<uint2 *>(p.out + (static_cast<int64_t>(sq.q_row0 + qi) * heads + head) * 2 * HD);
+#pragma unroll
+    for (int v = 0; v < V4; ++v) dst[v * 32 + lane] = make_uint2(pack_bf16(o[0][v].x, o[0][v].y), pack_bf16(o[0][v].z, o[0][v].w));
+}
+
 constexpr int kManyMergeWarps = 8;
 
 // A block per 32 consecutive rows of a pair of kv-heads, lane t on row t, a warp per eighth of the columns (the partials' layout:
@@ -455,11 +541,12 @@ __global__ void __launch_bounds__(32 * kManyMergeWarps) diff_many_combine_kernel
     const DiffSeq &sq = p.seqs[lo];
     const int groups = (sq.n_q * p.group + 31) / 32, pair = (id - sq.out0) / groups, r0 = ((id - sq.out0) - pair * groups) * 32;
     const int r = r0 + lane, qi = r / p.group, head = pair * p.group + r - qi * p.group;
-    int u[2], c0[2];
+    int u[2], c0[2], c1[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         u[x] = sq.unit0 + (2 * pair + x) * sq.n_blocks + r0 / DiffMany::kRows;
         c0[x] = diff_first_taker(p, u[x]);
+        c1[x] = diff_last_taker(p, u[x]);
     }
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
@@ -473,8 +560,7 @@ __global__ void __launch_bounds__(32 * kManyMergeWarps) diff_many_combine_kernel
         float4 o[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c = c0[x]; c < p.n_takers && (c == c0[x] || p.start[c].u == u[x]); ++c) {
-            if (diff_takes_nothing(p, c)) continue;
+        for (int c = c0[x]; c <= c1[x]; ++c) {
             const int64_t at = static_cast<int64_t>(u[x] + c) * DiffMany::kSlotRows + r % DiffMany::kRows;
             const float lse = valid ? __ldcg(p.part_lse + at) : -INFINITY;
             float4 z[N];
@@ -558,6 +644,14 @@ cudaError_t launch_diff_combine(int head_dim, bool many, const DiffParams &p, cu
         const cudaLaunchConfig_t cfg = diff_config(p.n_out, 32 * kManyMergeWarps, 0, st, &attr);
         return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<128>, p)
                                : cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<64>, p);
+    }
+    // Few pieces of many rows go a warp a row: 8 agents of 32k keys and 16 queries (6 pieces of 4096 rows and heads) 183 us, by
+    // blocks 188; one agent of 120k keys (39 pieces of 32) by blocks 85.8, 3000 keys of 4 heads 9.6.
+    const DiffSeq &last = p.seqs[p.n_seqs - 1];
+    if (p.n_takers <= 8 * (last.unit0 + last.n_blocks * (p.hkv / 2)) && p.n_out >= 1024) {
+        const cudaLaunchConfig_t cfg = diff_config((p.n_out + kRowMergeWarps - 1) / kRowMergeWarps, 32 * kRowMergeWarps, 0, st, &attr);
+        return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_row_combine_kernel<128>, p)
+                               : cudaLaunchKernelEx(&cfg, diff_row_combine_kernel<64>, p);
     }
     const cudaLaunchConfig_t cfg = diff_config(p.n_out, 32 * kMergeWarps, 0, st, &attr);
     return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_combine_kernel<128>, p) : cudaLaunchKernelEx(&cfg, diff_combine_kernel<64>, p);

@@ -2329,7 +2329,6 @@ void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t ma
     }
     // equal stretches of work: taker c's begins at work * c / n
     const int64_t n = std::min(tiles, max_takers);
-    p.n_takers = static_cast<int32_t>(n);
     int64_t at = 0, next = 0;  // work before the unit; the next taker
     int32_t u = 0;
     for (int32_t s = 0; s < p.n_seqs; ++s) {
@@ -2344,7 +2343,13 @@ void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t ma
                 at += w;
             }
     }
-    for (; next <= n; ++next) p.start[next] = DiffStart{u, 0};
+    p.start[n] = DiffStart{u, 0};
+    // stretches without a tile (all unit cost) go
+    int32_t kept = 0;
+    for (int32_t c = 0; c < n; ++c)
+        if (p.start[c].u != p.start[c + 1].u || p.start[c].t != p.start[c + 1].t) p.start[kept++] = p.start[c];
+    p.start[kept] = p.start[n];
+    p.n_takers = kept;
 }
 
 // The items with one of the two kernels, in launches of as many rows as their partials fit.
