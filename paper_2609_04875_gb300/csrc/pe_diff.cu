@@ -351,17 +351,21 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
     }
 }
 
-constexpr int kMergeWarps = 8, kMergeBatch = 4;  // pieces in flight
+constexpr int kMergeWarps = 8, kMergeBatch = 4;  // warps of a row's columns; pieces that a group of lanes has in flight
 
-// A block per output row and head, a warp per eighth of its columns, in each warp groups of lanes with every fourth (d = 64:
-// eighth) piece.  Hardly any shared memory, so that a block is resident, waiting, while the attention still runs.
-template <int HD>
-__global__ void __launch_bounds__(32 * kMergeWarps, 4) diff_combine_kernel(const __grid_constant__ DiffParams p)
+// A block per output row and head, a warp per eighth of its columns (SETS of eight warps), in each warp groups of lanes with
+// every fourth (d = 64: eighth) of the set's pieces.  A round of loads takes about a microsecond, so that pieces are taken
+// 16 (d = 64: 32) a set at a time: 39 of 32 rows and heads, 9 us with one set.
+// With one set it has registers and shared memory enough to be resident, waiting, while the attention still runs.
+template <int HD, int SETS>
+__global__ void __launch_bounds__(32 * kMergeWarps * SETS, SETS == 1 ? 4 : 1) diff_combine_kernel(const __grid_constant__ DiffParams p)
 {
     constexpr int kLanes = 2 * HD / kMergeWarps / 4;  // of a group: a float4 each
     constexpr int kGroups = 32 / kLanes;
     __shared__ float s_sum[kMergeWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __shared__ float s_m[SETS][2], s_l[SETS][2];
+    __shared__ float4 s_o[SETS > 1 ? SETS : 1][SETS > 1 ? 2 * HD / 2 : 1];  // [set][map, column]
+    const int set = threadIdx.x / (32 * kMergeWarps), warp = (threadIdx.x >> 5) % kMergeWarps, lane = threadIdx.x & 31;
     const int col = warp * kLanes + lane % kLanes;    // in float4
     int lo = 0, hi = p.n_seqs - 1;
     const int id = static_cast<int>(blockIdx.x);
@@ -378,7 +382,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 4) diff_combine_kernel(const
     ptx::griddep_wait();
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-    for (int cb = c0 + lane / kLanes; cb <= c1; cb += kMergeBatch * kGroups) {
+    for (int cb = c0 + set * kMergeBatch * kGroups + lane / kLanes; cb <= c1; cb += SETS * kMergeBatch * kGroups) {
         float lse[kMergeBatch][2];
         float4 y[kMergeBatch][2];
 #pragma unroll
@@ -410,6 +414,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 4) diff_combine_kernel(const
 #pragma unroll
         for (int k = kLanes; k < 32; k <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
         const float f = l[x] == 0.f ? 0.f : ex2(m[x] - mx);
+        m[x] = mx;
         l[x] *= f;
         o[x] = make_float4(o[x].x * f, o[x].y * f, o[x].z * f, o[x].w * f);
 #pragma unroll
@@ -421,6 +426,36 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 4) diff_combine_kernel(const
             o[x].w += __shfl_xor_sync(0xffffffffu, o[x].w, k);
         }
     }
+    if constexpr (SETS > 1) {  // the sets' sums, joined by the first
+        if (lane < kLanes) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) s_o[set][x * (2 * HD / 4) + col] = o[x];
+        }
+        if (warp == 0 && lane == 0) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                s_m[set][x] = m[x];
+                s_l[set][x] = l[x];
+            }
+        }
+        __syncthreads();
+        if (set > 0) return;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < SETS; ++k) mx = fmaxf(mx, s_m[k][x]);
+            l[x] = 0.f;
+            o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < SETS; ++k) {
+                const float f = s_l[k][x] == 0.f ? 0.f : ex2(s_m[k][x] - mx);
+                const float4 z = s_o[k][x * (2 * HD / 4) + col];
+                l[x] += s_l[k][x] * f;
+                o[x] = make_float4(o[x].x + z.x * f, o[x].y + z.y * f, o[x].z + z.z * f, o[x].w + z.w * f);
+            }
+        }
+    }
     const float g0 = l[0] == 0.f ? 0.f : 1.f / l[0], g1 = l[1] == 0.f ? 0.f : -__ldg(p.lambda + head) / l[1];
     float4 y = make_float4(g0 * o[0].x + g1 * o[1].x, g0 * o[0].y + g1 * o[1].y, g0 * o[0].z + g1 * o[1].z, g0 * o[0].w + g1 * o[1].w);
     if (p.gain) {
@@ -428,7 +463,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps, 4) diff_combine_kernel(const
 #pragma unroll
         for (int k = 1; k < kLanes; k <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
         if (lane == 0) s_sum[warp] = sum;
-        __syncthreads();
+        ptx::bar_sync(1, 32 * kMergeWarps);  // (the first set's)
         sum = 0.f;
 #pragma unroll
         for (int k = 0; k < kMergeWarps; ++k) sum += s_sum[k];
@@ -653,8 +688,10 @@ cudaError_t launch_diff_combine(int head_dim, bool many, const DiffParams &p, cu
         return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_row_combine_kernel<128>, p)
                                : cudaLaunchKernelEx(&cfg, diff_row_combine_kernel<64>, p);
     }
-    const cudaLaunchConfig_t cfg = diff_config(p.n_out, 32 * kMergeWarps, 0, st, &attr);
-    return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_combine_kernel<128>, p) : cudaLaunchKernelEx(&cfg, diff_combine_kernel<64>, p);
+    const bool sets = p.n_takers > 16 * (last.unit0 + last.n_blocks * (p.hkv / 2)) && p.n_out <= 512;
+    const cudaLaunchConfig_t cfg = diff_config(p.n_out, 32 * kMergeWarps * (sets ? 3 : 1), 0, st, &attr);
+    if (head_dim == 128) return sets ? cudaLaunchKernelEx(&cfg, diff_combine_kernel<128, 3>, p) : cudaLaunchKernelEx(&cfg, diff_combine_kernel<128, 1>, p);
+    return sets ? cudaLaunchKernelEx(&cfg, diff_combine_kernel<64, 3>, p) : cudaLaunchKernelEx(&cfg, diff_combine_kernel<64, 1>, p);
 }
 
 }  // namespace pe
