@@ -381,7 +381,7 @@ class PagedKVCache:
         """make(): the tensor that a call writes on ``stream``.  Not the current stream's memory then: the allocator may
         give out a block whose last use there is still to come.  And not reused before what the current stream has been
         given to do with it by the time it is freed."""
-        if stream is None or self.host_only:
+        if stream is None or self.host_only:  # (the calls do this themselves where it is their usual case)
             return make()
         torch = self._torch
         if not isinstance(stream, torch.cuda.Stream):
@@ -522,7 +522,7 @@ class PagedKVCache:
                 raise ValueError("Q must be [L][cu_tokens[-1]][Hq][d]")
             _same_shape(Q_out, Q, "Q_out")
             if Q_out is None:
-                Q_out = self._output_like(Q, stream)
+                Q_out = self._torch.empty_like(Q) if stream is None else self._output_like(Q, stream)
             q, q_out, heads = self._ptr(Q, "Q"), self._ptr(Q_out, "Q_out"), shape[2]
         elif Q_out is not None:
             raise ValueError("Q_out without Q")
@@ -550,7 +550,7 @@ class PagedKVCache:
             raise ValueError("X must be [layers][cu_tokens[-1]][H][d]")
         _same_shape(out, X, "out", "X")
         if out is None:
-            out = self._output_like(X, stream)
+            out = self._torch.empty_like(X) if stream is None and self._torch is not None else self._output_like(X, stream)
         ids, ids_at = _ints(seqs)
         cu, cu_at = _ints(cu_tokens)
         rc = _lib.pe_rotate_batch(self._h, len(seqs), ids_at, self._ptr(X, "X"), cu_at, self._ptr(out, "out"),
@@ -645,7 +645,9 @@ class PagedKVCache:
             raise ValueError("Q must have pairs of heads")
         want = (shape[0], shape[1] // 2, 2 * shape[2])
         if out is None:
-            out = self._output(lambda: self._torch.empty(want, dtype=self._bf16, device=self._torch_device), stream)
+            empty = self._torch.empty
+            out = (empty(want, dtype=self._bf16, device=self._torch_device) if stream is None
+                   else self._output(lambda: empty(want, dtype=self._bf16, device=self._torch_device), stream))
         elif tuple(out.shape) != want:
             raise ValueError(f"out has shape {tuple(out.shape)}, it must be {want}")
         scale = self._default_scale if softmax_scale is None else float(softmax_scale)

@@ -45,6 +45,72 @@ struct DiffCfg {
     static_assert(kDynSmem <= 232448, "shared memory budget");
 };
 
+// One row of a unit and its head, joined by a warp, two pieces of both maps in flight: lane t has the columns 4t .. + 3 of every
+// 128.  c0, c1: the unit's first and last taker.
+template <int HD>
+__device__ __forceinline__ void diff_merge_row(const DiffParams &p, int u, int row, int c0, int c1, int64_t q_row, int head, int lane)
+{
+    constexpr int V4 = 2 * HD / 128;  // float4 a lane
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float4 o[2][V4];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int v = 0; v < V4; ++v) o[x][v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = c0; c <= c1; c += 2) {
+        float lse[2][2];
+        float4 y[2][2][V4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            if (c + b <= c1) {
+                const int64_t at = static_cast<int64_t>(u + c + b) * DiffFew::kSlotRows + row;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    lse[b][x] = __ldcg(p.part_lse + at + x * DiffFew::kRows);
+#pragma unroll
+                    for (int v = 0; v < V4; ++v)
+                        y[b][x][v] = __ldcg(reinterpret_cast<const float4 *>(p.part + (at + x * DiffFew::kRows) * 2 * HD) + v * 32 + lane);
+                }
+            }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (c + b > c1 || lse[b][x] == -INFINITY) continue;  // (no key seen: its row may hold anything)
+                const float mn = fmaxf(m[x], lse[b][x]);
+                const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - mn), g = ex2(lse[b][x] - mn);  // (NaN where lse is)
+                m[x] = mn;
+                l[x] = l[x] * f + g;
+#pragma unroll
+                for (int v = 0; v < V4; ++v) {
+                    const float4 z = y[b][x][v];
+                    o[x][v] = make_float4(o[x][v].x * f + z.x * g, o[x][v].y * f + z.y * g, o[x][v].z * f + z.z * g, o[x][v].w * f + z.w * g);
+                }
+            }
+    }
+    const float g0 = l[0] == 0.f ? 0.f : 1.f / l[0], g1 = l[1] == 0.f ? 0.f : -__ldg(p.lambda + head) / l[1];
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < V4; ++v) {
+        const float4 a = o[0][v], b = o[1][v];
+        o[0][v] = make_float4(g0 * a.x + g1 * b.x, g0 * a.y + g1 * b.y, g0 * a.z + g1 * b.z, g0 * a.w + g1 * b.w);
+        sum += o[0][v].x * o[0][v].x + o[0][v].y * o[0][v].y + o[0][v].z * o[0][v].z + o[0][v].w * o[0][v].w;
+    }
+    if (p.gain) {
+#pragma unroll
+        for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
+#pragma unroll
+        for (int v = 0; v < V4; ++v) {
+            const float *g = p.gain + v * 128 + lane * 4;  // (a vector of any alignment)
+            o[0][v] = make_float4(o[0][v].x * f * __ldg(g), o[0][v].y * f * __ldg(g + 1), o[0][v].z * f * __ldg(g + 2), o[0][v].w * f * __ldg(g + 3));
+        }
+    }
+    uint2 *dst = reinterpret_cast<uint2 *>(p.out + (q_row * (p.hq / 2) + head) * 2 * HD);
+#pragma unroll
+    for (int v = 0; v < V4; ++v) dst[v * 32 + lane] = make_uint2(pack_bf16(o[0][v].x, o[0][v].y), pack_bf16(o[0][v].z, o[0][v].w));
+}
+
 template <int HD>
 __global__ void __launch_bounds__(kDiffThreads, 1)
     diff_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -341,6 +407,14 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                 if (valid) p.part_lse[at] = l == 0.f ? -INFINITY : m_ref + __log2f(l);
             }
             ptx::tc_fence_before();
+            if (p.whole) {  // the unit's only piece: its rows here, a warp each
+                if (!meet()) break;
+                const int r0 = w.block * DiffFew::kRows, rows = min(DiffFew::kRows, sq.n_q * p.group - r0), u = w.slot - cta;
+                for (int x = warp; x < rows; x += 4) {
+                    const int q = (r0 + x) / p.group;
+                    diff_merge_row<HD>(p, u, x, cta, cta, sq.q_row0 + q, w.pair * p.group + r0 + x - q * p.group, lane);
+                }
+            }
         }
     }
     ptx::tc_fence_before();
@@ -478,11 +552,10 @@ __global__ void __launch_bounds__(32 * kMergeWarps * SETS, SETS == 1 ? 4 : 1) di
 
 constexpr int kRowMergeWarps = 4;
 
-// A warp per output row and head, two pieces of both maps in flight.
+// A warp per output row and head.
 template <int HD>
 __global__ void __launch_bounds__(32 * kRowMergeWarps) diff_row_combine_kernel(const __grid_constant__ DiffParams p)
 {
-    constexpr int V4 = 2 * HD / 128;  // float4 a lane
     const int lane = threadIdx.x & 31, id = static_cast<int>(blockIdx.x) * kRowMergeWarps + (threadIdx.x >> 5);
     ptx::griddep_launch_dependents();
     if (id >= p.n_out) return;
@@ -497,64 +570,7 @@ __global__ void __launch_bounds__(32 * kRowMergeWarps) diff_row_combine_kernel(c
     const int u = sq.unit0 + pair * sq.n_blocks + r / DiffFew::kRows, row = r % DiffFew::kRows;
     const int c0 = diff_first_taker(p, u), c1 = diff_last_taker(p, u);
     ptx::griddep_wait();
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    float4 o[2][V4];
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int v = 0; v < V4; ++v) o[x][v] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = c0; c <= c1; c += 2) {
-        float lse[2][2];
-        float4 y[2][2][V4];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-            if (c + b <= c1) {
-                const int64_t at = static_cast<int64_t>(u + c + b) * DiffFew::kSlotRows + row;
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    lse[b][x] = __ldcg(p.part_lse + at + x * DiffFew::kRows);
-#pragma unroll
-                    for (int v = 0; v < V4; ++v)
-                        y[b][x][v] = __ldcg(reinterpret_cast<const float4 *>(p.part + (at + x * DiffFew::kRows) * 2 * HD) + v * 32 + lane);
-                }
-            }
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                if (c + b > c1 || lse[b][x] == -INFINITY) continue;  // (no key seen: its row may hold anything)
-                const float mn = fmaxf(m[x], lse[b][x]);
-                const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - mn), g = ex2(lse[b][x] - mn);  // (NaN where lse is)
-                m[x] = mn;
-                l[x] = l[x] * f + g;
-#pragma unroll
-                for (int v = 0; v < V4; ++v) {
-                    const float4 z = y[b][x][v];
-                    o[x][v] = make_float4(o[x][v].x * f + z.x * g, o[x][v].y * f + z.y * g, o[x][v].z * f + z.z * g, o[x][v].w * f + z.w * g);
-                }
-            }
-    }
-    const float g0 = l[0] == 0.f ? 0.f : 1.f / l[0], g1 = l[1] == 0.f ? 0.f : -__ldg(p.lambda + head) / l[1];
-    float sum = 0.f;
-#pragma unroll
-    for (int v = 0; v < V4; ++v) {
-        const float4 a = o[0][v], b = o[1][v];
-        o[0][v] = make_float4(g0 * a.x + g1 * b.x, g0 * a.y + g1 * b.y, g0 * a.z + g1 * b.z, g0 * a.w + g1 * b.w);
-        sum += o[0][v].x * o[0][v].x + o[0][v].y * o[0][v].y + o[0][v].z * o[0][v].z + o[0][v].w * o[0][v].w;
-    }
-    if (p.gain) {
-#pragma unroll
-        for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-        const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
-#pragma unroll
-        for (int v = 0; v < V4; ++v) {
-            const float *g = p.gain + v * 128 + lane * 4;  // (a vector of any alignment)
-            o[0][v] = make_float4(o[0][v].x * f * __ldg(g), o[0][v].y * f * __ldg(g + 1), o[0][v].z * f * __ldg(g + 2), o[0][v].w * f * __ldg(g + 3));
-        }
-    }
-    uint2 *dst = reinterpret_cast<uint2 *>(p.out + (static_cast<int64_t>(sq.q_row0 + qi) * heads + head) * 2 * HD);
-#pragma unroll
-    for (int v = 0; v < V4; ++v) dst[v * 32 + lane] = make_uint2(pack_bf16(o[0][v].x, o[0][v].y), pack_bf16(o[0][v].z, o[0][v].w));
+    diff_merge_row<HD>(p, u, row, c0, c1, sq.q_row0 + qi, head, lane);
 }
 
 constexpr int kManyMergeWarps = 8;

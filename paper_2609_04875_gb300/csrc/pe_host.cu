@@ -2302,11 +2302,17 @@ template <typename Shape>
 constexpr int64_t kDiffUnitCost = Shape::kMaps == 2 ? 6 : 3;
 
 // One launch over the items, at most kMaxSegs: fills p's sequences and stretches.
+// Few rows on few keys: a CTA a whole unit, which then finishes its rows itself, in place of cutting every unit and merging the
+// pieces in a second launch.  A tile takes 0.75 us, four rows 0.7.  A call of one query, with its output allocated (host and
+// GPU), whole / cut: 8 heads of d = 64 on 640 keys 12.3 / 16.4 us, 32 of d = 128 on 300 12.2 / 16.4, 16 on 900 16.8 / 16.6, on
+// 1300 21 / 16; 54 rows on 283 20.0 / 16.3.
+constexpr int64_t kDiffWhole = 48;  // 4 x tiles + rows
+
 template <typename Shape>
 void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t max_takers, DiffParams &p)
 {
     p.n_seqs = p.n_out = 0;
-    int64_t work = 0, tiles = 0;
+    int64_t work = 0, tiles = 0, longest = 0, rows = 0;
     int32_t units = 0;
     const int per_block = p.hkv / 2 * Shape::kMaps;  // units
     for (const DiffItem &it : items) {
@@ -2324,9 +2330,18 @@ void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t ma
         p.n_out += Shape::kMaps == 1 ? it.n_q * (p.hq / 2) : static_cast<int32_t>(ceil_div(static_cast<int64_t>(it.n_q) * p.group, 32)) * (p.hkv / 2);
         int64_t one = 0;
         for (int b = 0; b < q.n_blocks; ++b) one += diff_tiles<Shape>(q, p.group, b);
+        longest = std::max<int64_t>(longest, diff_tiles<Shape>(q, p.group, q.n_blocks - 1));
+        rows = std::max(rows, std::min<int64_t>(Shape::kRows, static_cast<int64_t>(it.n_q) * p.group));
         tiles += one * per_block;
         work += (one + q.n_blocks * kDiffUnitCost<Shape>) * per_block;
     }
+    if (Shape::kMaps == 1 && units <= max_takers && 4 * longest + rows <= kDiffWhole) {
+        p.whole = 1;
+        p.n_takers = units;
+        for (int32_t u = 0; u <= units; ++u) p.start[u] = DiffStart{u, 0};
+        return;
+    }
+    p.whole = 0;
     // equal stretches of work: taker c's begins at work * c / n
     const int64_t n = std::min(tiles, max_takers);
     int64_t at = 0, next = 0;  // work before the unit; the next taker
@@ -2373,10 +2388,12 @@ pe_status launch_diff(pe_cache *c, const std::vector<DiffItem> &all, DiffParams 
                               : launch_diff_attn(c->cfg.head_dim, c->tm_kd, c->tm_vd, p, st);
         if (e != cudaSuccess) return cuda_fail(e, "differential attention launch");
         c->launches++;
-        if (injected_failure(c)) return launch_fault("differential attention's merge");
-        e = launch_diff_combine(c->cfg.head_dim, kMany, p, st);
-        if (e != cudaSuccess) return cuda_fail(e, "differential attention's merge launch");
-        c->launches++;
+        if (!p.whole) {
+            if (injected_failure(c)) return launch_fault("differential attention's merge");
+            e = launch_diff_combine(c->cfg.head_dim, kMany, p, st);
+            if (e != cudaSuccess) return cuda_fail(e, "differential attention's merge launch");
+            c->launches++;
+        }
         items.clear();
         used = 0;
         return PE_OK;
