@@ -573,15 +573,13 @@ __global__ void __launch_bounds__(32 * kRowMergeWarps) diff_row_combine_kernel(c
     diff_merge_row<HD>(p, u, row, c0, c1, sq.q_row0 + qi, head, lane);
 }
 
-constexpr int kManyMergeWarps = 8;
-
-// A block per 32 consecutive rows of a pair of kv-heads, lane t on row t, a warp per eighth of the columns (the partials' layout:
-// part_chunk).
-template <int HD>
-__global__ void __launch_bounds__(32 * kManyMergeWarps) diff_many_combine_kernel(const __grid_constant__ DiffParams p)
+// A block per 32 consecutive rows of a pair of kv-heads, lane t on row t, the columns over WARPS warps (the partials' layout:
+// part_chunk), BATCH pieces in flight.
+template <int HD, int WARPS, int BATCH>
+__global__ void __launch_bounds__(32 * WARPS) diff_many_combine_kernel(const __grid_constant__ DiffParams p)
 {
-    constexpr int N = 2 * HD / 4 / kManyMergeWarps;  // 16-byte chunks of a warp
-    __shared__ float s_sum[kManyMergeWarps][32];
+    constexpr int N = 2 * HD / 4 / WARPS;  // 16-byte chunks of a warp
+    __shared__ float s_sum[WARPS][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int lo = 0, hi = p.n_seqs - 1;
     const int id = static_cast<int>(blockIdx.x);
@@ -611,19 +609,29 @@ __global__ void __launch_bounds__(32 * kManyMergeWarps) diff_many_combine_kernel
         float4 o[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c = c0[x]; c <= c1[x]; ++c) {
-            const int64_t at = static_cast<int64_t>(u[x] + c) * DiffMany::kSlotRows + r % DiffMany::kRows;
-            const float lse = valid ? __ldcg(p.part_lse + at) : -INFINITY;
-            float4 z[N];
+        for (int cb = c0[x]; cb <= c1[x]; cb += BATCH) {
+            float lse[BATCH];
+            float4 z[BATCH][N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) z[k] = __ldcg(part_chunk<2 * HD>(p.part, at, warp * N + k));
-            if (lse == -INFINITY) continue;  // (no key seen, or no row; what it holds is anything)
-            const float mn = fmaxf(m, lse), f = m == -INFINITY ? 0.f : ex2(m - mn), g = ex2(lse - mn);  // (NaN where lse is)
-            m = mn;
-            l = l * f + g;
+            for (int b = 0; b < BATCH; ++b) {
+                const int64_t at = static_cast<int64_t>(u[x] + cb + b) * DiffMany::kSlotRows + r % DiffMany::kRows;
+                const bool in = valid && cb + b <= c1[x];
+                lse[b] = in ? __ldcg(p.part_lse + at) : -INFINITY;
 #pragma unroll
-            for (int k = 0; k < N; ++k)
-                o[k] = make_float4(o[k].x * f + z[k].x * g, o[k].y * f + z[k].y * g, o[k].z * f + z[k].z * g, o[k].w * f + z[k].w * g);
+                for (int k = 0; k < N; ++k)
+                    z[b][k] = in ? __ldcg(part_chunk<2 * HD>(p.part, at, warp * N + k)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                if (lse[b] == -INFINITY) continue;  // (no key seen, or no row; what it holds is anything)
+                const float mn = fmaxf(m, lse[b]), f = m == -INFINITY ? 0.f : ex2(m - mn), g = ex2(lse[b] - mn);  // (NaN where lse is)
+                m = mn;
+                l = l * f + g;
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    o[k] = make_float4(o[k].x * f + z[b][k].x * g, o[k].y * f + z[b][k].y * g, o[k].z * f + z[b][k].z * g,
+                                       o[k].w * f + z[b][k].w * g);
+            }
         }
         if (l == 0.f) continue;
         const float g = (x ? -__ldg(p.lambda + head) : 1.f) / l;
@@ -638,7 +646,7 @@ __global__ void __launch_bounds__(32 * kManyMergeWarps) diff_many_combine_kernel
         __syncthreads();
         sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < kManyMergeWarps; ++k) sum += s_sum[k][lane];
+        for (int k = 0; k < WARPS; ++k) sum += s_sum[k][lane];
         const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
@@ -692,9 +700,15 @@ cudaError_t launch_diff_combine(int head_dim, bool many, const DiffParams &p, cu
     if (p.n_out <= 0) return cudaSuccess;
     cudaLaunchAttribute attr;
     if (many) {
-        const cudaLaunchConfig_t cfg = diff_config(p.n_out, 32 * kManyMergeWarps, 0, st, &attr);
-        return head_dim == 128 ? cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<128>, p)
-                               : cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<64>, p);
+        const DiffSeq &last = p.seqs[p.n_seqs - 1];
+        const bool pieces = p.n_takers > 2 * (last.unit0 + last.n_blocks * p.hkv);  // more than two or three of a unit
+        const int warps = pieces ? head_dim / 4 : head_dim / 8;
+        const cudaLaunchConfig_t cfg = diff_config(p.n_out, 32 * warps, 0, st, &attr);
+        if (head_dim == 128)
+            return pieces ? cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<128, 32, 3>, p)
+                          : cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<128, 16, 1>, p);
+        return pieces ? cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<64, 16, 4>, p)
+                      : cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<64, 8, 1>, p);
     }
     // Few pieces of many rows go a warp a row: 8 agents of 32k keys and 16 queries (6 pieces of 4096 rows and heads) 183 us, by
     // blocks 188; one agent of 120k keys (39 pieces of 32) by blocks 85.8, 3000 keys of 4 heads 9.6.

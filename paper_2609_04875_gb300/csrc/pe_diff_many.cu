@@ -12,7 +12,8 @@
 // share its reference: it moves only when a tile's sum passes 2^64 (pe_attn.cu), so per tile they exchange one vote, and the
 // maxima only then and at a piece's first tile.
 //
-// Roles (352 threads): warps 0-3 and 4-7 softmax, 8 K producer, 9 V producer, 10 MMA (the pair's first CTA issues).
+// Roles (352 threads): warps 0-3 and 4-7 softmax, 8 producer of Q and K, 9 of V, 10 MMA (the pair's first CTA issues).  A piece's Q
+// is loaded as soon as the S products of the piece before are done, so that it is there when that one's outputs are written.
 #include <algorithm>
 
 #include "diff.cuh"
@@ -39,8 +40,8 @@ struct ManyCfg {
     static constexpr int kOffMax = kOffV + kStages * kVBytes; // float [2][128]: the halves' maxima, or sums
     static constexpr int kOffNeed = kOffMax + 2 * 128 * 4;    // bool [2][128]: whose reference has to move
     static constexpr int kOffBar = kOffNeed + 2 * 128;
-    // k_full, k_empty, v_full, v_empty, v_peer [stages]; q_full, meet, edge; s_full, p_full, o_done [2]
-    static constexpr int kNumBars = 5 * kStages + 3 + 6;
+    // k_full, k_empty, v_full, v_empty, v_peer [stages]; q_full, q_empty, meet, edge; s_full, p_full, o_done [2]
+    static constexpr int kNumBars = 5 * kStages + 4 + 6;
     static constexpr int kOffMisc = kOffBar + kNumBars * 8;   // tmem slot, abort, votes [2], keys not finite [4]
     static constexpr int kDynSmem = kOffMisc + 32 + 1024;
     static constexpr int kTmemO = 256;                        // S at 0 and 128
@@ -117,6 +118,16 @@ __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *m
         : "memory");
 }
 
+__device__ __forceinline__ void tma_load_pair_4d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, int32_t w,
+                                                 uint32_t cluster_bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(cluster_bar)
+        : "memory");
+}
+
 __device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
@@ -152,8 +163,8 @@ __device__ __forceinline__ void commit_pair(uint32_t bar)
 
 template <int HD>
 __global__ void __launch_bounds__(kManyThreads, 1)
-    diff_many_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                     const __grid_constant__ DiffParams p)
+    diff_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ DiffParams p)
 {
     using C = ManyCfg<HD>;
     extern __shared__ uint8_t smem_raw[];
@@ -168,8 +179,9 @@ __global__ void __launch_bounds__(kManyThreads, 1)
     const uint32_t b_v_full = b_k_empty + 8 * C::kStages;
     const uint32_t b_v_empty = b_v_full + 8 * C::kStages;
     const uint32_t b_v_peer = b_v_empty + 8 * C::kStages;  // (the first CTA's: the other's V is there)
-    const uint32_t b_q_full = b_v_peer + 8 * C::kStages;   // (the first CTA's: the softmax warps of both)
-    const uint32_t b_meet = b_q_full + 8;                  // this CTA's softmax warps among themselves
+    const uint32_t b_q_full = b_v_peer + 8 * C::kStages;   // (the first CTA's counts the loads of both)
+    const uint32_t b_q_empty = b_q_full + 8;
+    const uint32_t b_meet = b_q_empty + 8;                 // this CTA's softmax warps among themselves
     const uint32_t b_edge = b_meet + 8;                    // the softmax warps of both
     const uint32_t b_s_full = b_edge + 8;                  // [2]
     const uint32_t b_p_full = b_s_full + 16;               // [2] (the first CTA's: the softmax warps of both)
@@ -188,7 +200,8 @@ __global__ void __launch_bounds__(kManyThreads, 1)
             ptx::mbar_init(b_v_empty + 8 * s, 1);
             ptx::mbar_init(b_v_peer + 8 * s, 1);
         }
-        ptx::mbar_init(b_q_full, 2 * kSoftWarps);
+        ptx::mbar_init(b_q_full, 1);
+        ptx::mbar_init(b_q_empty, 1);
         ptx::mbar_init(b_meet, kSoftWarps);
         ptx::mbar_init(b_edge, 2 * kSoftWarps);
         for (int s = 0; s < 2; ++s) {
@@ -201,6 +214,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
         for (int k = 0; k < 4; ++k) odd_keys[k] = 0;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
+        ptx::prefetch_tensormap(&tm_q);
         ptx::prefetch_tensormap(&tm_k);
         ptx::prefetch_tensormap(&tm_v);
     }
@@ -220,7 +234,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
     DiffWalk<DiffMany> w(p, static_cast<int>(blockIdx.x >> 1));
     int i = 0;  // tiles of the pieces before
     if (warp == 8 || warp == 9) {
-        // =================================================== producers: 64 keys of K, or one kv-head's V of 128
+        // =================================================== producers: Q's 128 rows and 64 keys of K, or one kv-head's V of 128
         const bool is_v = warp == 9;
         const CUtensorMap *map = is_v ? &tm_v : &tm_k;
         const uint32_t b_full = is_v ? b_v_full : b_k_full, b_empty = is_v ? b_v_empty : b_k_empty;
@@ -232,9 +246,22 @@ __global__ void __launch_bounds__(kManyThreads, 1)
         const bool on = lane < n_ops;
         const uint32_t bytes = is_v ? C::kVBytes : C::kKBytes;
         const uint32_t base = sbase + (is_v ? C::kOffV + op_reg * C::kVRegion : C::kOffK + op_reg * C::kKRegion) + op_page * rows * 128;
+        const uint32_t q_count = peer_addr(b_q_full, 0);
         bool ok = true;
-        while (ok && w.next()) {
+        int pieces = 0;
+        for (; ok && w.next(); ++pieces) {
             const DiffSeq &sq = p.seqs[w.si];
+            if (!is_v) {
+                if (pieces > 0 && !wait_bar_warp(b_q_empty, (pieces - 1) & 1, wctx)) { ok = false; break; }
+                if (lane == 0) {
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(b_q_full, 2 * C::kQBytes);
+                    // (rows past the sequence's last are others', or zeros)
+                    const int q0 = sq.q_row0 + (w.block * DiffMany::kRows + static_cast<int>(rank) * 128) / p.group;
+                    for (int r = 0; r < C::kRegions; ++r)
+                        tma_load_pair_4d(sbase + r * (128 * 128), &tm_q, r * 64, w.map, w.pair * p.group, q0, q_count);
+                }
+                __syncwarp();
+            }
             const int kvh = 2 * w.pair + (is_v ? static_cast<int>(rank) : w.map);
             auto row_of = [&](int k) -> int {  // of the pool, of this lane's box of tile k
                 const int key = (w.t0 + k) * 128 + (is_v ? 0 : 64 * static_cast<int>(rank)) + op_page * rows, lp = key >> p.log_ps;
@@ -253,11 +280,14 @@ __global__ void __launch_bounds__(kManyThreads, 1)
             }
         }
         // what the pair's first CTA still sends to this CTA's barriers is waited for: they have to be there
+        if (ok && !is_v && pieces > 0) ok = wait_bar_warp(b_q_empty, (pieces - 1) & 1, wctx);
         for (int k = max(0, i - C::kStages); ok && k < i; ++k)
             ok = wait_bar_warp(b_empty + 8 * (k % C::kStages), (k / C::kStages) & 1, wctx);
         __syncwarp();
         if (*abort_flag && lane == 0 && (!both || rank == 0)) {  // a bounded chance for copies in flight to land
             const uint64_t g0 = ptx::globaltimer();
+            if (!is_v && pieces > 0)
+                while (!ptx::mbar_try_wait(b_q_full, (pieces - 1) & 1) && ptx::globaltimer() - g0 < 4000000ull) {}
             for (int k = max(0, i - C::kStages); k < i; ++k)
                 while (!ptx::mbar_try_wait(b_full + 8 * (k % C::kStages), (k / C::kStages) & 1) && ptx::globaltimer() - g0 < 4000000ull) {}
         }
@@ -291,8 +321,9 @@ __global__ void __launch_bounds__(kManyThreads, 1)
         bool ok = rank == 0;
         for (int piece = 0; ok && w.next(); ++piece) {
             const int n = __shfl_sync(0xffffffffu, w.n, 0);
-            if (!wait_cluster_warp(b_q_full, piece & 1, wctx)) break;
+            if (!wait_bar_warp(b_q_full, piece & 1, wctx)) break;
             ok = issue_s(i) && (n < 2 || issue_s(i + 1));
+            if (n <= 2) commit_pair(b_q_empty);
             for (int k = 0; ok && k < n; ++k, ++i) {
                 if (!full(b_v_full, i) || !full(b_v_peer, i) || !wait_bar_warp(b_p_full + 8 * (i & 1), (i >> 1) & 1, wctx)) { ok = false; break; }
                 ptx::tc_fence_after();
@@ -303,14 +334,17 @@ __global__ void __launch_bounds__(kManyThreads, 1)
                                 (k > 0 || kk > 0) ? 1u : 0u);
                 commit_pair(b_o_done + 8 * (i & 1));
                 commit_pair(b_v_empty + 8 * (i % C::kStages));
-                if (k + 2 < n) ok = issue_s(i + 2);  // (P(i), over S(i), is read by then)
+                if (k + 2 < n) {
+                    ok = issue_s(i + 2);  // (P(i), over S(i), is read by then)
+                    if (k + 3 == n) commit_pair(b_q_empty);
+                }
             }
         }
     } else if (warp < kSoftWarps) {
         // =================================================== softmax: thread (half, row) owns 64 of a tile's keys
         const int row = threadIdx.x & 127, half = warp >> 2;
         const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t q_full = peer_addr(b_q_full, 0), p_full = peer_addr(b_p_full, 0);
+        const uint32_t p_full = peer_addr(b_p_full, 0);
         const uint32_t edge0 = peer_addr(b_edge, 0), edge1 = peer_addr(b_edge, 1);
         const uint32_t odd0 = peer_addr(sbase + C::kOffMisc + 16, 0), odd1 = peer_addr(sbase + C::kOffMisc + 16, 1);
         float *s_max = reinterpret_cast<float *>(smem + C::kOffMax);
@@ -336,30 +370,16 @@ __global__ void __launch_bounds__(kManyThreads, 1)
             }
             return wait_cluster_warp(b_edge, edges++ & 1, wctx);
         };
-        // The next piece: its row, and Q's into shared memory, each half half of it (the S products of the piece before are done)
         int pos, pos_first;
         bool valid, any;
-        auto begin = [&]() {
+        auto begin = [&]() {  // the next piece's row
             if (!w.next()) return false;
             const DiffSeq &sq = p.seqs[w.si];
-            const int r = w.block * DiffMany::kRows + static_cast<int>(rank) * 128 + row;
-            const int qi = r / p.group, head = 2 * (w.pair * p.group + r - qi * p.group) + w.map;
+            const int qi = (w.block * DiffMany::kRows + static_cast<int>(rank) * 128 + row) / p.group;
             valid = qi < sq.n_q;
             any = __any_sync(0xffffffffu, valid);
             pos = sq.n_keys - sq.n_q + qi;
             pos_first = sq.n_keys - sq.n_q + w.block * DiffMany::kRows / p.group;  // of the pair's rows
-            if (valid) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (static_cast<int64_t>(sq.q_row0 + qi) * p.hq + head) * HD);
-#pragma unroll
-                for (int c0 = 0; c0 < HD / 16; ++c0) {
-                    const int c = half * (HD / 16) + c0;
-                    const uint4 v = __ldg(src + c);
-                    *reinterpret_cast<uint4 *>(smem + (c >> 3) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
-                }
-            }
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) arrive_peer(q_full);
             return true;
         };
         for (bool more = begin(); ok && more;) {
@@ -495,7 +515,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
             if (!ok) break;
             const bool had = valid, had_any = any;
             const int64_t at = static_cast<int64_t>(w.slot) * DiffMany::kSlotRows + rank * 128 + row;
-            more = begin();  // its first S products run during what follows
+            more = begin();
             if (!wait_bar_warp(b_o_done + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, wctx)) break;
             ptx::tc_fence_after();
             s_max[half * 128 + row] = l;  // (P V waited for every warp: no maxima of the last tile are read any more)
@@ -531,7 +551,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
 }
 
 template <int HD>
-cudaError_t launch_many_t(const CUtensorMap &k, const CUtensorMap &v, const DiffParams &p, cudaStream_t st)
+cudaError_t launch_many_t(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const DiffParams &p, cudaStream_t st)
 {
     static std::atomic<uint64_t> configured{0};
     cudaError_t e = set_dyn_smem_once(diff_many_kernel<HD>, ManyCfg<HD>::kDynSmem, configured);
@@ -549,15 +569,16 @@ cudaError_t launch_many_t(const CUtensorMap &k, const CUtensorMap &v, const Diff
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, diff_many_kernel<HD>, k, v, p);
+    return cudaLaunchKernelEx(&cfg, diff_many_kernel<HD>, q, k, v, p);
 }
 
 }  // namespace
 
-cudaError_t launch_diff_attn_many(int head_dim, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const DiffParams &p, cudaStream_t st)
+cudaError_t launch_diff_attn_many(int head_dim, const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
+                                  const DiffParams &p, cudaStream_t st)
 {
     if (p.n_takers <= 0) return cudaSuccess;
-    return head_dim == 128 ? launch_many_t<128>(tm_k, tm_v, p, st) : launch_many_t<64>(tm_k, tm_v, p, st);
+    return head_dim == 128 ? launch_many_t<128>(tm_q, tm_k, tm_v, p, st) : launch_many_t<64>(tm_q, tm_k, tm_v, p, st);
 }
 
 }  // namespace pe

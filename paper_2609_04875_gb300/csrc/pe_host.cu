@@ -390,6 +390,22 @@ pe_status encode_q(CUtensorMap *m, const void *q, int64_t rows, int hq, int d, i
     return PE_OK;
 }
 
+// The same with pairs of heads apart, [rows][Hq / 2][2][d]: box (64, 1, g, 128/g), one map's heads.
+pe_status encode_q_map(CUtensorMap *m, const void *q, int64_t rows, int hq, int d, int g)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return fail(PE_ERR_CUDA, "cuTensorMapEncodeTiled unavailable");
+    cuuint64_t dims[4] = {static_cast<cuuint64_t>(d), 2, static_cast<cuuint64_t>(hq / 2), static_cast<cuuint64_t>(rows)};
+    cuuint64_t strides[3] = {static_cast<cuuint64_t>(d) * 2, static_cast<cuuint64_t>(d) * 4, static_cast<cuuint64_t>(hq) * d * 2};
+    cuuint32_t box[4] = {64, 1, static_cast<cuuint32_t>(g), static_cast<cuuint32_t>(kBM / g)};
+    cuuint32_t es[4] = {1, 1, 1, 1};
+    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(q), dims, strides, box, es,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(PE_ERR_CUDA, "cuTensorMapEncodeTiled (q maps) failed: %d", static_cast<int>(r));
+    return PE_OK;
+}
+
 void free_device(pe_cache *c)
 {
     if (c->own_pools) {
@@ -2369,9 +2385,13 @@ void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t ma
 
 // The items with one of the two kernels, in launches of as many rows as their partials fit.
 template <typename Shape>
-pe_status launch_diff(pe_cache *c, const std::vector<DiffItem> &all, DiffParams &p, cudaStream_t st)
+pe_status launch_diff(pe_cache *c, const std::vector<DiffItem> &all, int64_t q_rows, DiffParams &p, cudaStream_t st)
 {
     constexpr bool kMany = Shape::kMaps == 2;
+    if (all.empty()) return PE_OK;
+    CUtensorMap tm_q;
+    if (kMany)
+        if (pe_status s = encode_q_map(&tm_q, p.q, q_rows, p.hq, c->cfg.head_dim, p.group)) return s;
     const int64_t slots = c->ws_bytes / (Shape::kSlotRows * (2 * static_cast<int64_t>(c->cfg.head_dim) + 1) * 4);
     const int64_t sms = std::min<int64_t>(c->num_sms, kMaxSkCtas);
     const int64_t takers = std::max<int64_t>(1, std::min<int64_t>(kMany ? sms / 2 : sms, slots / 2));
@@ -2384,7 +2404,7 @@ pe_status launch_diff(pe_cache *c, const std::vector<DiffItem> &all, DiffParams 
         p.part = c->d_ws;
         p.part_lse = c->d_ws + slots * Shape::kSlotRows * 2 * c->cfg.head_dim;
         if (injected_failure(c)) return launch_fault("differential attention");
-        cudaError_t e = kMany ? launch_diff_attn_many(c->cfg.head_dim, c->tm_kd, c->tm_vd, p, st)
+        cudaError_t e = kMany ? launch_diff_attn_many(c->cfg.head_dim, tm_q, c->tm_kd, c->tm_vd, p, st)
                               : launch_diff_attn(c->cfg.head_dim, c->tm_kd, c->tm_vd, p, st);
         if (e != cudaSuccess) return cuda_fail(e, "differential attention launch");
         c->launches++;
@@ -2416,7 +2436,7 @@ pe_status launch_diff(pe_cache *c, const std::vector<DiffItem> &all, DiffParams 
     return flush();
 }
 
-pe_status run_diff(pe_cache *c, const std::vector<AttnItem> &all, int32_t layer, const void *Q, void *out, int32_t hq, float scale,
+pe_status run_diff(pe_cache *c, const std::vector<AttnItem> &all, int32_t layer, const void *Q, int64_t q_rows, void *out, int32_t hq, float scale,
                    const float *lambda, const float *gain, float eps, cudaStream_t st)
 {
     DiffParams p;
@@ -2443,8 +2463,8 @@ pe_status run_diff(pe_cache *c, const std::vector<AttnItem> &all, int32_t layer,
         const int64_t rows = static_cast<int64_t>(it.n_q) * p.group;
         (rows <= kDiffFewRows ? few : many).push_back(DiffItem{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq])});
     }
-    if (pe_status s = launch_diff<DiffFew>(c, few, p, st)) return s;
-    return launch_diff<DiffMany>(c, many, p, st);
+    if (pe_status s = launch_diff<DiffFew>(c, few, q_rows, p, st)) return s;
+    return launch_diff<DiffMany>(c, many, q_rows, p, st);
 }
 
 }  // namespace
@@ -2920,7 +2940,7 @@ static pe_status diff_attn_batch(pe_cache *c, int32_t n, const int32_t *seqs, in
         if ((s = unpack_layer(c, items.data(), items.size(), layer, st)) != PE_OK) return s;
         layer = 0;
     }
-    return run_diff(c, items, layer, Q, out, hq, scale, lambda, gain, eps, st);
+    return run_diff(c, items, layer, Q, cu_q[n], out, hq, scale, lambda, gain, eps, st);
 }
 
 pe_status pe_diff_attn_batch(pe_cache *c, int32_t n, const int32_t *seqs, int32_t layer, const void *Q_packed,
