@@ -112,7 +112,7 @@ _sigs = {
                                 _I32P, _I32],
     "pe_cache_create_q8": [ctypes.POINTER(_Config), ctypes.POINTER(_P)],
     "pe_cache_scales": [_P, ctypes.POINTER(_P)],
-    "pe_read_kv_batch": [_P, _I32, _I32P, _I64P, _I32P, _P, _P, _P],
+    "pe_read_kv_batch": [_P, _I32, _P, _P, _P, _P, _P, _P],
     "pe_replay_attn_weights_batch": [_P, _I32, _I32P, _I32, _P, _I32P, _P, _I32, ctypes.c_float, _P, _I64, _P],
     "pe_evict_batch": [_P, _I32, _I32P, _I32P, _I32, _I32, _P, _I64, _P, _I64, _P],
     "pe_append_kv_rope_batch": [_P, _I32, _P, _P, _P, _P, ctypes.POINTER(_Rope), _P, _P, _P, _I32, _P],
@@ -710,10 +710,17 @@ class PagedKVCache:
         if self.host_only:
             raise ValueError("a host-only cache holds no K and V")
         shape = (self.num_layers, cu_tokens[-1], self.num_kv_heads, self.head_dim)
-        K, V = [self._output(lambda: self._torch.empty(shape, dtype=self._bf16, device=self._torch_device), stream)
-                for _ in range(2)]
-        _check(_lib.pe_read_kv_batch(self._h, len(seqs), _i32_array(seqs), _i64_array(begins), _i32_array(cu_tokens),
-                                     K.data_ptr(), V.data_ptr(), self._s(stream)))
+        if stream is None:
+            K, V = [self._torch.empty(shape, dtype=self._bf16, device=self._torch_device) for _ in range(2)]
+        else:
+            K, V = [self._output(lambda: self._torch.empty(shape, dtype=self._bf16, device=self._torch_device), stream)
+                    for _ in range(2)]
+        ids, ids_at = _ints(seqs)
+        first, first_at = _ints(begins, ctypes.c_int64)
+        cu, cu_at = _ints(cu_tokens)
+        rc = _lib.pe_read_kv_batch(self._h, len(seqs), ids_at, first_at, cu_at, K.data_ptr(), V.data_ptr(), self._s(stream))
+        if rc:
+            _check(rc)
         return K, V
 
     def read_kv(self, seq, begin=0, n=None, stream=None):

@@ -13,8 +13,10 @@ struct DiffWalk {
     const DiffParams &p;
     int u, t, u1, t1;  // next piece, end of the stretch
     int taker;
+    int rank, ranks;   // of the CTAs that share a piece, and their number
     int si, pair, map, block, t0, n, slot;
-    __device__ __forceinline__ DiffWalk(const DiffParams &p_, int cta) : p(p_), taker(cta), map(0)
+    __device__ __forceinline__ DiffWalk(const DiffParams &p_, int cta, int rank_ = 0, int ranks_ = 1)
+        : p(p_), taker(cta), rank(rank_), ranks(ranks_), map(0)
     {
         u = p.start[cta].u;
         t = p.start[cta].t;
@@ -43,6 +45,11 @@ struct DiffWalk {
             n = (u == u1 ? t1 : diff_tiles<Shape>(p.seqs[si], p.group, block)) - t;
             ++u;
             t = 0;
+            if (ranks > 1) {
+                const int all = n;
+                t0 += all * rank / ranks;
+                n = all * (rank + 1) / ranks - all * rank / ranks;
+            }
             if (n > 0) return true;
         }
         return false;

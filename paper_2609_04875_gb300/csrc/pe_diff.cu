@@ -39,76 +39,79 @@ struct DiffCfg {
     // k_full, k_empty, v_full, v_empty [stages]; q_full, edge; s_full, p_full, o_done [2]
     static constexpr int kNumBars = 4 * kStages + 2 + 6;
     static constexpr int kOffMisc = kOffBar + kNumBars * 8;   // tmem slot, abort flag, keys not finite [2]
-    static constexpr int kDynSmem = kOffMisc + 16 + 1024;
+    static constexpr int kOffLse = kOffMisc + 16;             // float [128]: whole units
+    static constexpr int kRowFloats = 2 * HD + 4;             // of a row's O there, in the stages' memory: 16 bytes past a multiple of 128
+    static constexpr int kDynSmem = kOffLse + 128 * 4 + 1024;
     static constexpr int kTmemO = 256;                        // S at 0 and 128, P over S
     static constexpr uint32_t kTmemCols = 512;
     static_assert(kDynSmem <= 232448, "shared memory budget");
+    static_assert(128 * kRowFloats * 4 <= kOffBar - kOffK, "rows of a whole unit");
 };
 
-// One row of a unit and its head, joined by a warp, two pieces of both maps in flight: lane t has the columns 4t .. + 3 of every
-// 128.  c0, c1: the unit's first and last taker.
+// One row of a head, joined from its pieces by a warp: lane t has the columns 4t .. + 3 of every 128.
 template <int HD>
-__device__ __forceinline__ void diff_merge_row(const DiffParams &p, int u, int row, int c0, int c1, int64_t q_row, int head, int lane)
-{
-    constexpr int V4 = 2 * HD / 128;  // float4 a lane
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+struct DiffRow {
+    static constexpr int V4 = 2 * HD / 128;  // float4 a lane
+    float m[2], l[2];
     float4 o[2][V4];
+    __device__ __forceinline__ DiffRow()
+    {
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 2; ++x) {
+            m[x] = -INFINITY;
+            l[x] = 0.f;
 #pragma unroll
-        for (int v = 0; v < V4; ++v) o[x][v] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = c0; c <= c1; c += 2) {
-        float lse[2][2];
-        float4 y[2][2][V4];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-            if (c + b <= c1) {
-                const int64_t at = static_cast<int64_t>(u + c + b) * DiffFew::kSlotRows + row;
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    lse[b][x] = __ldcg(p.part_lse + at + x * DiffFew::kRows);
-#pragma unroll
-                    for (int v = 0; v < V4; ++v)
-                        y[b][x][v] = __ldcg(reinterpret_cast<const float4 *>(p.part + (at + x * DiffFew::kRows) * 2 * HD) + v * 32 + lane);
-                }
-            }
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                if (c + b > c1 || lse[b][x] == -INFINITY) continue;  // (no key seen: its row may hold anything)
-                const float mn = fmaxf(m[x], lse[b][x]);
-                const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - mn), g = ex2(lse[b][x] - mn);  // (NaN where lse is)
-                m[x] = mn;
-                l[x] = l[x] * f + g;
-#pragma unroll
-                for (int v = 0; v < V4; ++v) {
-                    const float4 z = y[b][x][v];
-                    o[x][v] = make_float4(o[x][v].x * f + z.x * g, o[x][v].y * f + z.y * g, o[x][v].z * f + z.z * g, o[x][v].w * f + z.w * g);
-                }
-            }
-    }
-    const float g0 = l[0] == 0.f ? 0.f : 1.f / l[0], g1 = l[1] == 0.f ? 0.f : -__ldg(p.lambda + head) / l[1];
-    float sum = 0.f;
-#pragma unroll
-    for (int v = 0; v < V4; ++v) {
-        const float4 a = o[0][v], b = o[1][v];
-        o[0][v] = make_float4(g0 * a.x + g1 * b.x, g0 * a.y + g1 * b.y, g0 * a.z + g1 * b.z, g0 * a.w + g1 * b.w);
-        sum += o[0][v].x * o[0][v].x + o[0][v].y * o[0][v].y + o[0][v].z * o[0][v].z + o[0][v].w * o[0][v].w;
-    }
-    if (p.gain) {
-#pragma unroll
-        for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-        const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
-#pragma unroll
-        for (int v = 0; v < V4; ++v) {
-            const float *g = p.gain + v * 128 + lane * 4;  // (a vector of any alignment)
-            o[0][v] = make_float4(o[0][v].x * f * __ldg(g), o[0][v].y * f * __ldg(g + 1), o[0][v].z * f * __ldg(g + 2), o[0][v].w * f * __ldg(g + 3));
+            for (int v = 0; v < V4; ++v) o[x][v] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
-    uint2 *dst = reinterpret_cast<uint2 *>(p.out + (q_row * (p.hq / 2) + head) * 2 * HD);
+    // A piece of map x: O / l and log-sum-exp.
+    __device__ __forceinline__ void add(int x, float lse, const float4 (&z)[V4])
+    {
+        if (lse == -INFINITY) return;  // (no key seen: its row may hold anything)
+        const float mn = fmaxf(m[x], lse);
+        const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - mn), g = ex2(lse - mn);  // (NaN where lse is)
+        m[x] = mn;
+        l[x] = l[x] * f + g;
 #pragma unroll
-    for (int v = 0; v < V4; ++v) dst[v * 32 + lane] = make_uint2(pack_bf16(o[0][v].x, o[0][v].y), pack_bf16(o[0][v].z, o[0][v].w));
+        for (int v = 0; v < V4; ++v)
+            o[x][v] = make_float4(o[x][v].x * f + z[v].x * g, o[x][v].y * f + z[v].y * g, o[x][v].z * f + z[v].z * g, o[x][v].w * f + z[v].w * g);
+    }
+    // The difference of the maps, the norm, and the output row.
+    __device__ __forceinline__ void finish(const DiffParams &p, int64_t q_row, int head, int lane)
+    {
+        const float g0 = l[0] == 0.f ? 0.f : 1.f / l[0], g1 = l[1] == 0.f ? 0.f : -__ldg(p.lambda + head) / l[1];
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < V4; ++v) {
+            const float4 a = o[0][v], b = o[1][v];
+            o[0][v] = make_float4(g0 * a.x + g1 * b.x, g0 * a.y + g1 * b.y, g0 * a.z + g1 * b.z, g0 * a.w + g1 * b.w);
+            sum += o[0][v].x * o[0][v].x + o[0][v].y * o[0][v].y + o[0][v].z * o[0][v].z + o[0][v].w * o[0][v].w;
+        }
+        if (p.gain) {
+#pragma unroll
+            for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+            const float f = 1.f / sqrtf(sum / (2 * HD) + p.eps);
+#pragma unroll
+            for (int v = 0; v < V4; ++v) {
+                const float *g = p.gain + v * 128 + lane * 4;  // (a vector of any alignment)
+                o[0][v] = make_float4(o[0][v].x * f * __ldg(g), o[0][v].y * f * __ldg(g + 1), o[0][v].z * f * __ldg(g + 2), o[0][v].w * f * __ldg(g + 3));
+            }
+        }
+        uint2 *dst = reinterpret_cast<uint2 *>(p.out + (q_row * (p.hq / 2) + head) * 2 * HD);
+#pragma unroll
+        for (int v = 0; v < V4; ++v) dst[v * 32 + lane] = make_uint2(pack_bf16(o[0][v].x, o[0][v].y), pack_bf16(o[0][v].z, o[0][v].w));
+    }
+};
+
+// ld_cluster_f32 (ptx.cuh), four
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr, uint32_t rank)
+{
+    float4 v;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(addr), "r"(rank)
+                 : "memory");
+    return v;
 }
 
 template <int HD>
@@ -122,7 +125,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
     const uint32_t sbase = (raw + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (sbase - raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cta = static_cast<int>(blockIdx.x);
+    const int ranks = max(1, p.whole), rank = static_cast<int>(blockIdx.x) % ranks, taker = static_cast<int>(blockIdx.x) / ranks;
 
     const uint32_t b_k_full = sbase + C::kOffBar;
     const uint32_t b_k_empty = b_k_full + 8 * C::kStages;
@@ -136,8 +139,10 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::kOffMisc + 4);
     uint32_t *odd_keys = reinterpret_cast<uint32_t *>(smem + C::kOffMisc + 8);  // [2]
+    float *s_rows = reinterpret_cast<float *>(smem + C::kOffK), *s_lse = reinterpret_cast<float *>(smem + C::kOffLse);
     const WaitCtx wctx{abort_flag, p.status};
 
+    if (threadIdx.x < 128) s_lse[threadIdx.x] = -INFINITY;  // (a CTA may have no tile of its cluster's unit)
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kStages; ++s) {
             ptx::mbar_init(b_k_full + 8 * s, 2);
@@ -171,7 +176,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
 
-    DiffWalk<DiffFew> w(p, cta);
+    DiffWalk<DiffFew> w(p, taker, rank, ranks);
     int i = 0;  // tiles of the pieces before
     if (warp >= 4 && warp < 8) {
         // =================================================== producers: K of a map, or V of a kv-head
@@ -393,7 +398,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
             if (any) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
                 const int64_t at = static_cast<int64_t>(w.slot) * 128 + row;
-                float4 *dst = reinterpret_cast<float4 *>(p.part + at * 2 * HD);
+                float4 *dst = reinterpret_cast<float4 *>(p.whole ? s_rows + row * C::kRowFloats : p.part + at * 2 * HD);
 #pragma unroll 1
                 for (int ch = 0; ch < 2 * HD / 32; ++ch) {
                     float o[32];
@@ -404,17 +409,9 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                         for (int x = 0; x < 8; ++x)
                             dst[ch * 8 + x] = make_float4(o[4 * x] * inv, o[4 * x + 1] * inv, o[4 * x + 2] * inv, o[4 * x + 3] * inv);
                 }
-                if (valid) p.part_lse[at] = l == 0.f ? -INFINITY : m_ref + __log2f(l);
+                if (valid) (p.whole ? s_lse[row] : p.part_lse[at]) = l == 0.f ? -INFINITY : m_ref + __log2f(l);
             }
             ptx::tc_fence_before();
-            if (p.whole) {  // the unit's only piece: its rows here, a warp each
-                if (!meet()) break;
-                const int r0 = w.block * DiffFew::kRows, rows = min(DiffFew::kRows, sq.n_q * p.group - r0), u = w.slot - cta;
-                for (int x = warp; x < rows; x += 4) {
-                    const int q = (r0 + x) / p.group;
-                    diff_merge_row<HD>(p, u, x, cta, cta, sq.q_row0 + q, w.pair * p.group + r0 + x - q * p.group, lane);
-                }
-            }
         }
     }
     ptx::tc_fence_before();
@@ -422,6 +419,36 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
     if (warp == 8) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, C::kTmemCols);
+    }
+    if (p.whole) {  // the cluster's parts of its unit, a warp a row
+        __syncwarp();
+        ptx::cluster_sync();
+        DiffWalk<DiffFew> unit(p, taker);
+        if (unit.next()) {
+            const DiffSeq &sq = p.seqs[unit.si];
+            const int r0 = unit.block * DiffFew::kRows, rows = min(DiffFew::kRows, sq.n_q * p.group - r0);
+            for (int x = rank + warp * ranks; x < rows; x += ranks * (kDiffThreads / 32)) {
+                const int q = (r0 + x) / p.group, head = unit.pair * p.group + r0 + x - q * p.group;
+                DiffRow<HD> a;
+#pragma unroll 2
+                for (int c = 0; c < ranks; ++c) {
+                    float lse[2];
+                    float4 z[2][2 * HD / 128];
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        lse[m] = ptx::ld_cluster_f32(ptx::smem_addr(s_lse + m * DiffFew::kRows + x), c);
+#pragma unroll
+                        for (int v = 0; v < 2 * HD / 128; ++v)
+                            z[m][v] = ld_cluster_f32x4(ptx::smem_addr(s_rows + (m * DiffFew::kRows + x) * C::kRowFloats + v * 128 + lane * 4), c);
+                    }
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) a.add(m, lse[m], z[m]);
+                }
+                a.finish(p, sq.q_row0 + q, head, lane);
+            }
+        }
+        __syncwarp();
+        ptx::cluster_sync();  // the others have read this CTA's rows
     }
 }
 
@@ -552,7 +579,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps * SETS, SETS == 1 ? 4 : 1) di
 
 constexpr int kRowMergeWarps = 4;
 
-// A warp per output row and head.
+// A warp per output row and head, two pieces of both maps in flight.
 template <int HD>
 __global__ void __launch_bounds__(32 * kRowMergeWarps) diff_row_combine_kernel(const __grid_constant__ DiffParams p)
 {
@@ -570,7 +597,27 @@ __global__ void __launch_bounds__(32 * kRowMergeWarps) diff_row_combine_kernel(c
     const int u = sq.unit0 + pair * sq.n_blocks + r / DiffFew::kRows, row = r % DiffFew::kRows;
     const int c0 = diff_first_taker(p, u), c1 = diff_last_taker(p, u);
     ptx::griddep_wait();
-    diff_merge_row<HD>(p, u, row, c0, c1, sq.q_row0 + qi, head, lane);
+    DiffRow<HD> a;
+    for (int c = c0; c <= c1; c += 2) {
+        float lse[2][2];
+        float4 z[2][2][DiffRow<HD>::V4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                lse[b][x] = -INFINITY;
+                if (c + b > c1) continue;
+                const int64_t at = static_cast<int64_t>(u + c + b) * DiffFew::kSlotRows + x * DiffFew::kRows + row;
+                lse[b][x] = __ldcg(p.part_lse + at);
+#pragma unroll
+                for (int v = 0; v < DiffRow<HD>::V4; ++v) z[b][x][v] = __ldcg(reinterpret_cast<const float4 *>(p.part + at * 2 * HD) + v * 32 + lane);
+            }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) a.add(x, lse[b][x], z[b][x]);
+    }
+    a.finish(p, sq.q_row0 + qi, head, lane);
 }
 
 // A block per 32 consecutive rows of a pair of kv-heads, lane t on row t, the columns over WARPS warps (the partials' layout:
@@ -682,8 +729,15 @@ cudaError_t launch_diff_t(const CUtensorMap &k, const CUtensorMap &v, const Diff
     static std::atomic<uint64_t> configured{0};
     cudaError_t e = set_dyn_smem_once(diff_attn_kernel<HD>, DiffCfg<HD>::kDynSmem, configured);
     if (e != cudaSuccess) return e;
-    cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = diff_config(p.n_takers, kDiffThreads, DiffCfg<HD>::kDynSmem, st, &attr);
+    cudaLaunchAttribute attr[2];
+    const int ranks = std::max(1, p.whole);
+    cudaLaunchConfig_t cfg = diff_config(p.n_takers * ranks, kDiffThreads, DiffCfg<HD>::kDynSmem, st, attr);
+    if (ranks > 1) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = static_cast<unsigned>(ranks);
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
     return cudaLaunchKernelEx(&cfg, diff_attn_kernel<HD>, k, v, p);
 }
 

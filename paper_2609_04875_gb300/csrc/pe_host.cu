@@ -2318,11 +2318,14 @@ template <typename Shape>
 constexpr int64_t kDiffUnitCost = Shape::kMaps == 2 ? 6 : 3;
 
 // One launch over the items, at most kMaxSegs: fills p's sequences and stretches.
-// Few rows on few keys: a CTA a whole unit, which then finishes its rows itself, in place of cutting every unit and merging the
-// pieces in a second launch.  A tile takes 0.75 us, four rows 0.7.  A call of one query, with its output allocated (host and
-// GPU), whole / cut: 8 heads of d = 64 on 640 keys 12.3 / 16.4 us, 32 of d = 128 on 300 12.2 / 16.4, 16 on 900 16.8 / 16.6, on
-// 1300 21 / 16; 54 rows on 283 20.0 / 16.3.
-constexpr int64_t kDiffWhole = 48;  // 4 x tiles + rows
+// Few rows on few keys: a cluster of 1 to 8 CTAs a whole unit, at most kDiffWholeTiles tiles each where there are SMs enough, whose
+// rows it joins itself, in place of cutting every unit and merging the pieces in a second launch.  A tile takes 0.75 us, a
+// row of each of nine warps about as much.  A call of one query, with its output allocated (host and GPU), whole / cut: 8
+// heads of d = 64 on 640 keys 10.9 / 15.2 us, on 3000 12.6 / 16.0, 16 of d = 128 on 2 x 2000 12.9 / 15.2, 32 on 7 x 1700 14.5 /
+// 15.9; on 5000 (10 tiles a CTA) 16.8 / 15.8.
+constexpr int64_t kDiffWhole = 8;       // tiles and rounds of rows of a CTA
+constexpr int64_t kDiffWholeTiles = 4;  // (10 tiles over 1, 2, 4 CTAs: 11.1, 9.7, 9.0 us; 5 over 1, 2: 9.6, 9.8)
+constexpr int64_t kDiffWholeRanks = 8;
 
 template <typename Shape>
 void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t max_takers, DiffParams &p)
@@ -2351,13 +2354,17 @@ void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t ma
         tiles += one * per_block;
         work += (one + q.n_blocks * kDiffUnitCost<Shape>) * per_block;
     }
-    if (Shape::kMaps == 1 && units <= max_takers && 4 * longest + rows <= kDiffWhole) {
-        p.whole = 1;
-        p.n_takers = units;
-        for (int32_t u = 0; u <= units; ++u) p.start[u] = DiffStart{u, 0};
-        return;
-    }
     p.whole = 0;
+    if (Shape::kMaps == 1 && units <= max_takers) {
+        int64_t ranks = 1;
+        while (ranks < kDiffWholeRanks && longest > kDiffWholeTiles * ranks && 2 * ranks * units <= max_takers) ranks *= 2;
+        if (ceil_div(longest, ranks) + ceil_div(rows, 9 * ranks) <= kDiffWhole) {
+            p.whole = static_cast<int32_t>(ranks);
+            p.n_takers = units;
+            for (int32_t u = 0; u <= units; ++u) p.start[u] = DiffStart{u, 0};
+            return;
+        }
+    }
     // equal stretches of work: taker c's begins at work * c / n
     const int64_t n = std::min(tiles, max_takers);
     int64_t at = 0, next = 0;  // work before the unit; the next taker

@@ -143,7 +143,8 @@ struct DiffParams {
     int32_t n_seqs, hq, hkv, group, layer, num_pages, ps, log_ps;
     int32_t oob_row;             // a pool row past the end: boxes there read zeros
     int32_t n_takers, n_out;
-    int32_t whole;               // few rows: every taker has one whole unit, whose rows it finishes itself (no merge)
+    int32_t whole;               // few rows: 0, or every taker is a cluster of that many CTAs with one whole unit, whose rows it
+                                 // finishes itself (no merge)
     float scale_log2;            // softmax_scale * log2(e)
     float eps;
     DiffSeq seqs[kMaxSegs];
