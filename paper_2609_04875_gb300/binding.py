@@ -835,6 +835,75 @@ class PagedKVCache:
             return keep
         return call
 
+    def prepare_append_kv_rope_batch(self, seqs, K, V, cu_tokens, rope, Q=None, positions=None, Q_out=None, stream=None):
+        _covers(seqs, cu_tokens, "cu_tokens")
+        self._check_kv(K, V)
+        total = K.shape[1]
+        if total != cu_tokens[-1]:
+            raise ValueError("K token count does not match cu_tokens")
+        if not isinstance(rope, Rope):
+            raise TypeError("rope must be a Rope")
+        if (Q is None) != (Q_out is None):
+            raise ValueError("give both Q and Q_out or neither")
+        if Q is not None and (Q.dim() != 4 or Q.shape[0] != self.num_layers or Q.shape[1] != total or Q.shape[3] != self.head_dim
+                              or Q_out.shape != Q.shape):
+            raise ValueError("Q and Q_out must be [L][cu_tokens[-1]][Hq][d]")
+        ids, cu = _ints(seqs), _ints(cu_tokens)
+        keep = (K, V, Q, Q_out, positions, rope, ids, cu)
+        args = (self._h, len(seqs), ids[1], self._ptr(K, "K"), self._ptr(V, "V"), cu[1], rope._ref,
+                self._positions(positions, rope, total), None if Q is None else self._ptr(Q, "Q"),
+                None if Q is None else self._ptr(Q_out, "Q_out"), 0 if Q is None else Q.shape[2], self._s(stream))
+        fn = _lib.pe_append_kv_rope_batch
+
+        def call():
+            rc = fn(*args)
+            if rc:
+                _check(rc)
+            return keep
+        return call
+
+    def prepare_rotate_batch(self, seqs, X, cu_tokens, rope, out, positions=None, stream=None):
+        _covers(seqs, cu_tokens, "cu_tokens")
+        if not isinstance(rope, Rope):
+            raise TypeError("rope must be a Rope")
+        shape = X.shape
+        if len(shape) not in (3, 4) or shape[-1] != self.head_dim or shape[-3] != cu_tokens[-1] or out.shape != shape:
+            raise ValueError("X and out must be [layers][cu_tokens[-1]][H][d]")
+        ids, cu = _ints(seqs), _ints(cu_tokens)
+        keep = (X, out, positions, rope, ids, cu)
+        args = (self._h, len(seqs), ids[1], self._ptr(X, "X"), cu[1], self._ptr(out, "out"), shape[0] if len(shape) == 4 else 1,
+                shape[-2], rope._ref, self._positions(positions, rope, shape[-3]), self._s(stream))
+        fn = _lib.pe_rotate_batch
+
+        def call():
+            rc = fn(*args)
+            if rc:
+                _check(rc)
+            return keep
+        return call
+
+    def prepare_diff_attn_batch(self, seqs, layer, Q, cu_q, lam, out, gain=None, eps=1e-5, softmax_scale=None, stream=None):
+        _covers(seqs, cu_q, "cu_q")
+        shape = Q.shape
+        if len(shape) != 3 or shape[2] != self.head_dim or shape[0] != cu_q[-1] or shape[1] % 2:
+            raise ValueError("Q must be [cu_q[-1]][Hq][d], with pairs of heads")
+        if tuple(out.shape) != (shape[0], shape[1] // 2, 2 * shape[2]):
+            raise ValueError("out must be [cu_q[-1]][Hq / 2][2 d]")
+        scale = self._default_scale if softmax_scale is None else float(softmax_scale)
+        ids, cu = _ints(seqs), _ints(cu_q)
+        keep = (Q, out, lam, gain, ids, cu)
+        args = (self._h, len(seqs), ids[1], int(layer), self._ptr(Q, "Q"), cu[1], self._ptr(out, "out"), shape[1],
+                ctypes.c_float(scale), self._vec(lam, "lam", shape[1] // 2),
+                None if gain is None else self._vec(gain, "gain", 2 * shape[2]), ctypes.c_float(eps), self._s(stream))
+        fn = _lib.pe_diff_attn_batch
+
+        def call():
+            rc = fn(*args)
+            if rc:
+                _check(rc)
+            return keep
+        return call
+
     def replay_attn_static_scratch(self, seq, layer, Q, out=None, softmax_scale=None, stream=None):
         """pe_replay_attn_static_scratch: split-KV replay attention whose partials
         live in the library's fixed device array (the call allocates nothing)."""

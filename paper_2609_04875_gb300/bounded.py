@@ -17,11 +17,14 @@ from __future__ import annotations
 
 import torch
 
-from .binding import PagedKVCache
+from .binding import PagedKVCache, Rope
 
 
 class BoundedAgents:
-    def __init__(self, agents, layers, hq, hkv, d, budget, slack=256, sinks=4, recent=64, page_size=16, longest_prompt=None):
+    def __init__(self, agents, layers, hq, hkv, d, budget, slack=256, sinks=4, recent=64, page_size=16, longest_prompt=None,
+                 rope=None):
+        """``rope`` (binding.Rope): K and Q come unrotated, and turn by each token's position in its whole session (on every
+        axis), which eviction does not change."""
         if sinks + recent > budget:
             raise ValueError("sinks + recent exceed the budget")
         self.layers, self.hq, self.budget, self.slack, self.sinks, self.recent = layers, hq, budget, slack, sinks, recent
@@ -35,6 +38,7 @@ class BoundedAgents:
         # origin[i][j]: the position in agent i's whole session of the token its cache holds at position j
         self.origin = torch.full((agents, self.columns), -1, dtype=torch.int32, device="cuda")
         self.seen = [0] * agents
+        self.rope = rope
 
     def lengths(self):
         return [self.cache.seq_info(s)[0] for s in self.seqs]
@@ -48,18 +52,25 @@ class BoundedAgents:
         lens = self.lengths()
         if max(a + n for a, n in zip(lens, counts)) > self.columns:
             raise ValueError("more tokens than a session may hold at once")
-        self.cache.append_kv_batch(self.seqs, K, V, cu)
         # where the new tokens are held, and their positions in the whole sessions
         new = [(i, a + j, seen + j) for i, (a, n, seen) in enumerate(zip(lens, counts, self.seen)) for j in range(n)]
+        rows, at, pos = torch.tensor(new, dtype=torch.int64, device="cuda").reshape(-1, 3).t()
+        pos = pos.int()
+        if self.rope is None:
+            self.cache.append_kv_batch(self.seqs, K, V, cu)
+        else:
+            Q = self.cache.append_kv_rope_batch(self.seqs, K, V, cu, self.rope, Q=Q, positions=self._on_axes(pos))
         if new:
-            rows, at, pos = torch.tensor(new, device="cuda").t()
-            self.origin[rows, at] = pos.int()
+            self.origin[rows, at] = pos
         self.seen = [a + n for a, n in zip(self.seen, counts)]
         out = torch.empty_like(Q)
         for layer in range(self.layers):
             self.cache.replay_attn_weights_batch(self.seqs, layer, Q[layer], cu, self.weights, out=out[layer])
         self._evict()
         return out
+
+    def _on_axes(self, pos):
+        return pos.expand(self.rope.n_axes, -1).contiguous()
 
     def _evict(self):
         over = [i for i, n in enumerate(self.lengths()) if n > self.budget + self.slack]
@@ -93,13 +104,16 @@ class BoundedAgents:
         if tuple(Q.shape) != (self.layers, held, self.hq, self.cache.head_dim):
             raise ValueError(f"Q must be [{self.layers}][{held}][{self.hq}][{self.cache.head_dim}]")
         self.weights[agent] = 0
+        if self.rope is not None:
+            Q = self.cache.rotate(self.seqs[agent], Q, self.rope, positions=self._on_axes(self.origin[agent, :held]))
         for layer in range(self.layers if held else 0):
             self.cache.replay_attn_weights_batch([self.seqs[agent]], layer, Q[layer], [0, held], self.weights[agent: agent + 1])
 
 
 def main():
     agents, layers, hq, hkv, d = 8, 2, 32, 8, 128
-    b = BoundedAgents(agents, layers, hq, hkv, d, budget=1024, slack=128, longest_prompt=3000)
+    rope = Rope([10000.0 ** (-i / (d // 2)) for i in range(d // 2)])
+    b = BoundedAgents(agents, layers, hq, hkv, d, budget=1024, slack=128, longest_prompt=3000, rope=rope)
     g = torch.Generator("cuda").manual_seed(1)
 
     def tokens(counts):

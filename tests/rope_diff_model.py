@@ -15,12 +15,13 @@ def rotated(x, pos, freq, axis=None, interleaved=False, scale=1.0):
     x, n = x.double(), len(freq)
     axis = axis or [0] * n
     f = torch.tensor(freq, dtype=torch.float64, device=x.device)
+    far = pos.abs().max().item() if pos.numel() else 0
     angle = (pos.double()[axis].t() * f)[:, None]           # [N][1][pairs]
     one, two = (slice(0, 2 * n, 2), slice(1, 2 * n, 2)) if interleaved else (slice(0, n), slice(n, 2 * n))
     a, b, c, s = x[..., one], x[..., two], angle.cos(), angle.sin()
     y, e = x.clone(), torch.zeros_like(x)
     y[..., one], y[..., two] = scale * (a * c - b * s), scale * (b * c + a * s)
-    e[..., one] = e[..., two] = abs(scale) * (a.abs() + b.abs()) * (2.0 ** -20 + 1e-15 * pos.abs().max().item())
+    e[..., one] = e[..., two] = abs(scale) * (a.abs() + b.abs()) * (2.0 ** -20 + 1e-15 * far)
     return y, e
 
 

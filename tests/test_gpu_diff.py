@@ -272,6 +272,31 @@ def test_a_step_as_a_model_makes_it(bits):
             s.cache.replay_attn_batch(s.seqs, layer, rq[layer], cu)
 
 
+def test_prepared_calls_are_the_plain_ones():
+    s = Setup([300, 90], 4, 64, 16, seed=11, slack=20)
+    q, lam, gain = s.inputs([2, 2], 8)
+    cu, rope = [0, 2, 4], pe.Rope(freqs(32))
+    K, V = randn(s.g, 1, 4, 4, 64), randn(s.g, 1, 4, 4, 64)
+    rq, out, x = torch.empty_like(q)[None], torch.empty((4, 4, 128), dtype=torch.bfloat16, device="cuda"), torch.empty_like(q)
+    append = s.cache.prepare_append_kv_rope_batch(s.seqs, K, V, cu, rope, Q=q[None], Q_out=rq)
+    rotate = s.cache.prepare_rotate_batch(s.seqs, q, cu, rope, x)
+    attend = s.cache.prepare_diff_attn_batch(s.seqs, 0, rq[0], cu, lam, out, gain=gain)
+    for _ in range(2):
+        append()
+        rotate()
+        attend()
+        assert torch.equal(x, rq[0]) and torch.equal(x, s.cache.rotate_batch(s.seqs, q, cu, rope))
+        assert torch.equal(out, s.cache.diff_attn_batch(s.seqs, 0, rq[0], cu, lam, gain=gain))
+    assert [s.cache.seq_info(i)[0] for i in s.seqs] == [304, 94]
+    s.check(out, s.seqs, rq[0], cu, lam, gain)
+    for call, args, kw in [(s.cache.prepare_append_kv_rope_batch, (s.seqs, K, V, cu, rope), {"Q": q[None]}),
+                           (s.cache.prepare_rotate_batch, (s.seqs, q, cu, rope, x[:3]), {}),
+                           (s.cache.prepare_rotate_batch, (s.seqs, q, cu, rope, x), {"positions": torch.zeros((2, 4), dtype=torch.int32, device="cuda")}),
+                           (s.cache.prepare_diff_attn_batch, (s.seqs, 0, q, cu, lam, x), {})]:
+        with pytest.raises(ValueError):
+            call(*args, **kw)
+
+
 def test_a_failed_launch():
     s = Setup([600], 4, 64, 16, seed=9)
     q, lam, gain = s.inputs([80], 8)
