@@ -336,5 +336,8 @@ def test_refusals():
     tiny = pe.PagedKVCache(1, 2, 64, 16, 8, 1, 8, workspace_bytes=1024)
     y = tiny.seq_create()
     tiny.append_kv(y, randn(s.g, 1, 5, 2, 64), randn(s.g, 1, 5, 2, 64))
+    for n in (1, 5):
+        with pytest.raises(pe.PEError, match="workspace"):
+            tiny.diff_attn(y, 0, randn(s.g, n, 2 if n == 1 else 64, 64), torch.zeros(1 if n == 1 else 32, device="cuda"))
     none = s.cache.diff_attn_batch(seqs, 0, q[:0], [0, 0, 0], lam)
     assert none.shape == (0, 2, 128)
