@@ -2308,14 +2308,16 @@ struct DiffItem {
     int32_t q_row0, n_q, n_keys;
 };
 
-// Rows (n_q x group) up to which a sequence takes the kernel of few rows.
+// Rows (n_q x group) up to which a sequence takes the kernel of few rows.  More of them would go through it in blocks of 64, each
+// with the keys again: 128 rows on 3000 keys 20.6 us (many rows' kernel: 20.1), on 20000 41.7 (35.9), on 8 x 8000 101 (72), on
+// 500 14.5 (15.4); 68 rows on 20000 31.1 (34.5); d = 64, 128 rows on 8 x 8000 52 (63), on 20000 31.4 (28.7).
 constexpr int64_t kDiffFewRows = 64;
 
 // A unit's cost besides its tiles, in tiles: queries fetched, a first tile whose products wait for its softmax, outputs written.
-// 2000 queries on 2000 keys, 32 / 8 heads, d = 128 (256 units of 8 tiles): 0 123 us, 2 100, 4 89, 6 83, 8 84; 16 agents of 1000
-// keys, one query: 0 17.3, 1 16.5, 3 15.9, 6 16.4.
+// Many rows, 2000 queries on 2000 keys, 32 / 8 heads, d = 128 (256 units of 8 tiles): 2 81 us, 4 73, 6 71.5, 8 74; few rows, 5
+// agents of 9000 keys, 3 queries: 1 21.1, 3 19.5, 4 18.9, 6 18.4; 16 of 1500, one query: 21.5, 20.3, 19.5, 19.7.
 template <typename Shape>
-constexpr int64_t kDiffUnitCost = Shape::kMaps == 2 ? 6 : 3;
+constexpr int64_t kDiffUnitCost = Shape::kMaps == 2 ? 6 : 5;
 
 // One launch over the items, at most kMaxSegs: fills p's sequences and stretches.
 // Few rows on few keys: a cluster of 1 to 8 CTAs a whole unit, at most kDiffWholeTiles tiles each where there are SMs enough, whose
