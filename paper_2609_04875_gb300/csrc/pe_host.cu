@@ -2844,6 +2844,8 @@ static pe_status append_batch(pe_cache *c, int32_t n, const int32_t *seqs, const
             if (!ra->Q_out) return fail(PE_ERR_INVALID, "null Q_out");
             if (!aligned16(ra->Q) || !aligned16(ra->Q_out)) return fail(PE_ERR_INVALID, "Q and Q_out must be 16-byte aligned");
             if (ra->hq <= 0) return fail(PE_ERR_INVALID, "num_q_heads must be positive");
+            if (static_cast<int64_t>(c->cfg.num_layers) * ra->hq > INT32_MAX / 2)
+                return fail(PE_ERR_RANGE, "%d layers of %d heads are too many rows of a token", c->cfg.num_layers, ra->hq);
             const int64_t row = static_cast<int64_t>(c->cfg.num_layers) * total * c->cfg.head_dim * 2;
             const int64_t kv_bytes = row * c->cfg.num_kv_heads, q_bytes = row * ra->hq;
             if (ra->Q != ra->Q_out && !apart(ra->Q, q_bytes, ra->Q_out, q_bytes)) return fail(PE_ERR_INVALID, "Q_out overlaps Q");
@@ -2882,6 +2884,8 @@ pe_status pe_rotate_batch(pe_cache *c, int32_t n, const int32_t *seqs, const voi
     if (n < 0 || (n > 0 && (!seqs || !cu_tokens))) return fail(PE_ERR_INVALID, "bad batch arguments");
     if (n > 0 && cu_tokens[0] != 0) return fail(PE_ERR_INVALID, "cu_tokens[0] must be 0");
     if (num_layers < 0 || num_heads < 1) return fail(PE_ERR_INVALID, "%d layers of %d heads", num_layers, num_heads);
+    if (static_cast<int64_t>(num_layers) * num_heads > INT32_MAX / 2)
+        return fail(PE_ERR_RANGE, "%d layers of %d heads are too many rows of a token", num_layers, num_heads);
     for (int32_t i = 0; i < n; ++i) {
         if (pe_status s = check_seq(c, seqs[i])) return s;
         const int32_t cnt = cu_tokens[i + 1] - cu_tokens[i];

@@ -5,9 +5,9 @@
 //     a' = scale (a cos - b sin),  b' = scale (b cos + a sin)
 // in 32 bits, rounded once.  Columns past the pairs are copied.
 //
-// Bound by memory: every row is read once and written once, and an angle, a token's for all heads of a layer, costs a sine and
-// a cosine for each pair.  A thread keeps the angles of the same eight pairs (16 registers) and goes through the heads, four
-// rows of 32 bytes in flight; a warp reads and writes whole rows.  1638 tokens of 32 layers, 32 query heads and 8 kv-heads of
+// Bound by memory: every row is read once and written once, and an angle, a token's for all its rows, costs a sine and
+// a cosine for each pair.  A thread keeps the angles of the same eight pairs (16 registers) and goes through the rows of a token,
+// layer by layer and head by head, four of 32 bytes in flight; a warp reads and writes whole rows.  1638 tokens of 32 layers, 32 query heads and 8 kv-heads of
 // 128: 189 us, 6.8 TB/s (a thread per chunk that computes its own angles: 713); the queries of 4 x 1500 tokens of 8 layers 117
 // us, 6.7 TB/s (696).  Small calls are bound by their launch: 16 tokens of one layer 2.9 us on the GPU.
 #include <algorithm>
@@ -125,63 +125,75 @@ __device__ __forceinline__ uint4 ld_once(const uint4 *p)
     return v;
 }
 
-// Rows [0, n) of one token, a warp: row h from src + h * CPR to dst + h * dst_stride.
-template <int CPR, bool WHOLE>
-__device__ __forceinline__ void rotate_rows(const RopeParams &r, const uint4 *src, uint4 *dst, int64_t dst_stride, int n, int64_t tok, int pos)
+// Rows [r0, r1) of one token, a warp, numbered layer by layer and head by head: at(l, h) is a row's offset in chunks, of src and
+// of dst; with V it is copied alike (v_src, v_dst).
+template <int CPR, bool WHOLE, bool V, typename From, typename To>
+__device__ __forceinline__ void rotate_rows(const RopeParams &r, const uint4 *src, uint4 *dst, const uint4 *v_src, uint4 *v_dst, int heads,
+                                            int r0, int r1, int64_t tok, int pos, const From &from, const To &to)
 {
-    constexpr int CP = CPR / 2, RPW = 32 / CP, U = 4;
+    constexpr int CP = CPR / 2, RPW = 32 / CP, U = V ? 2 : 4;
     const int lane = threadIdx.x & 31, c = lane % CP;
     if constexpr (WHOLE) {
         const PairOfChunks<CPR> pc(r, c, tok, pos);
-        for (int h0 = lane / CP; h0 < n; h0 += U * RPW) {
-            uint4 a[U], b[U];
+        for (int x0 = r0 + lane / CP; x0 < r1; x0 += U * RPW) {
+            uint4 a[U], b[U], va[U], vb[U];
+            int64_t at[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (h0 + u * RPW < n) {
-                    const uint4 *row = src + static_cast<int64_t>(h0 + u * RPW) * CPR;
-                    a[u] = ld_once(row + pc.a);
-                    b[u] = ld_once(row + pc.b);
+            for (int u = 0; u < U; ++u) {
+                const int x = x0 + u * RPW, l = x / heads, h = x - l * heads;
+                if (x >= r1) continue;
+                const int64_t f = from(l, h);
+                at[u] = to(l, h);
+                a[u] = ld_once(src + f + pc.a);
+                b[u] = ld_once(src + f + pc.b);
+                if constexpr (V) {
+                    va[u] = ld_once(v_src + f + pc.a);
+                    vb[u] = ld_once(v_src + f + pc.b);
                 }
+            }
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (h0 + u * RPW < n) {
-                    pc.turn(a[u], b[u]);
-                    uint4 *row = dst + (h0 + u * RPW) * dst_stride;
-                    row[pc.a] = a[u];
-                    row[pc.b] = b[u];
+            for (int u = 0; u < U; ++u) {
+                if (x0 + u * RPW >= r1) continue;
+                pc.turn(a[u], b[u]);
+                dst[at[u] + pc.a] = a[u];
+                dst[at[u] + pc.b] = b[u];
+                if constexpr (V) {
+                    v_dst[at[u] + pc.a] = va[u];
+                    v_dst[at[u] + pc.b] = vb[u];
                 }
+            }
         }
     } else {
-        for (int h0 = 0; h0 < n; h0 += RPW) {
-            const int h = h0 + lane / CP;
-            float x[8], y[8];
-            if (h < n) {
-                rope_chunk(r, src + static_cast<int64_t>(h) * CPR, 2 * c, tok, pos, x);
-                rope_chunk(r, src + static_cast<int64_t>(h) * CPR, 2 * c + 1, tok, pos, y);
+        for (int x0 = r0; x0 < r1; x0 += RPW) {
+            const int x = x0 + lane / CP, l = x / heads, h = x - l * heads;
+            float y[8], z[8];
+            int64_t f = 0;
+            if (x < r1) {
+                f = from(l, h);
+                rope_chunk(r, src + f, 2 * c, tok, pos, y);
+                rope_chunk(r, src + f, 2 * c + 1, tok, pos, z);
             }
             __syncwarp();
-            if (h < n) {
-                dst[h * dst_stride + 2 * c] = pack8(x);
-                dst[h * dst_stride + 2 * c + 1] = pack8(y);
+            if (x < r1) {
+                const int64_t t = to(l, h);
+                dst[t + 2 * c] = pack8(y);
+                dst[t + 2 * c + 1] = pack8(z);
+                if constexpr (V) {
+                    v_dst[t + 2 * c] = v_src[f + 2 * c];
+                    v_dst[t + 2 * c + 1] = v_src[f + 2 * c + 1];
+                }
             }
         }
     }
 }
 
-template <int CPR>
-__device__ __forceinline__ void copy_rows(const uint4 *src, uint4 *dst, int64_t dst_stride, int n)
+// The queries of token tok: a part of part_rows rows.
+template <int CPR, bool WHOLE>
+__device__ __forceinline__ void rotate_part(const RopeParams &r, const uint4 *X, uint4 *out, int layers, int64_t n_total, int heads, int part,
+                                            int part_rows, int64_t tok, int pos)
 {
-    constexpr int RPW = 32 / CPR, U = 4;
-    const int lane = threadIdx.x & 31;
-    for (int h0 = lane / CPR; h0 < n; h0 += U * RPW) {
-        uint4 a[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (h0 + u * RPW < n) a[u] = ld_once(src + static_cast<int64_t>(h0 + u * RPW) * CPR + lane % CPR);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (h0 + u * RPW < n) dst[(h0 + u * RPW) * dst_stride + lane % CPR] = a[u];
-    }
+    const auto at = [&](int l, int h) { return ((l * n_total + tok) * heads + h) * CPR; };
+    rotate_rows<CPR, WHOLE, false>(r, X, out, nullptr, nullptr, heads, part * part_rows, min((part + 1) * part_rows, layers * heads), tok, pos, at, at);
 }
 
 template <typename Segs>
@@ -197,26 +209,21 @@ __device__ __forceinline__ int find_seg(const Segs &segs, int n, int t)
 
 constexpr int kRowThreads = 128;  // of a block of rows: 4 tasks, a warp each
 
-// A warp per token, layer and block of head_block heads.
+// A warp per token and part of its rows (tokens fastest: neighbouring warps read neighbouring rows).
 template <int CPR, bool WHOLE>
-__global__ void __launch_bounds__(kRowThreads) rotate_kernel(const __grid_constant__ RotateParams p, int head_blocks, int head_block)
+__global__ void __launch_bounds__(kRowThreads) rotate_kernel(const __grid_constant__ RotateParams p, int parts, int part_rows)
 {
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    int64_t r = static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5);
-    const int h0 = static_cast<int>(r % head_blocks) * head_block;
-    r /= head_blocks;
-    const int tok = p.tok0 + static_cast<int>(r % p.n_tokens);
-    const int64_t l = r / p.n_tokens;
-    if (l >= p.layers) return;
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5);
+    const int part = static_cast<int>(id / p.n_tokens), tok = p.tok0 + static_cast<int>(id - static_cast<int64_t>(part) * p.n_tokens);
+    if (part >= parts) return;
     int lo = 0, hi = p.n_segs - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (p.segs[mid].tok0 <= tok) lo = mid; else hi = mid - 1;
     }
-    const int64_t row = (l * p.n_total + tok) * p.heads + h0;
-    rotate_rows<CPR, WHOLE>(p.r, p.X + row * CPR, p.out + row * CPR, CPR, min(head_block, p.heads - h0), tok,
-                            p.segs[lo].pos0 + tok - p.segs[lo].tok0);
+    rotate_part<CPR, WHOLE>(p.r, p.X, p.out, p.layers, p.n_total, p.heads, part, part_rows, tok, p.segs[lo].pos0 + tok - p.segs[lo].tok0);
 }
 
 template <typename Block>
@@ -230,35 +237,30 @@ __device__ __forceinline__ void enter_pages(const Block &a)
     }
 }
 
-// A warp per token, layer and one of: K's rows and V's, into their slots, or head_block of Q's.
+// A warp per token and part: of K's rows and V's, into their slots, or of Q's.
 template <typename Params, int CPR, bool WHOLE>
-__global__ void __launch_bounds__(kRowThreads) append_rope_kernel(const __grid_constant__ Params p, int head_blocks, int head_block)
+__global__ void __launch_bounds__(kRowThreads) append_rope_kernel(const __grid_constant__ Params p, int kv_parts, int kv_rows, int q_parts, int q_rows)
 {
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     const auto &a = p.a;
     if (blockIdx.x == 0) enter_pages(a);
-    int64_t r = static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5);
-    const int part = static_cast<int>(r % (1 + head_blocks));
-    r /= 1 + head_blocks;
-    const int t = static_cast<int>(r % a.seg_tokens);
-    const int64_t l = r / a.seg_tokens;
-    if (l >= a.L) return;
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5);
+    const int part = static_cast<int>(id / a.seg_tokens), t = static_cast<int>(id - static_cast<int64_t>(part) * a.seg_tokens);
+    if (part >= kv_parts + q_parts) return;
     const AppendSeg &sg = a.segs[find_seg(a.segs, a.n_segs, t)];
     const int local = t - sg.cum0, pos = sg.len0 + local;
-    const int64_t tok = sg.tok0 + local, lt = l * a.n_total + tok;
-    if (part > 0) {
-        const int h0 = (part - 1) * head_block;
-        const int64_t at = (lt * p.c.hq + h0) * CPR;
-        rotate_rows<CPR, WHOLE>(p.c.r, p.c.Q + at, p.c.Q_out + at, CPR, min(head_block, p.c.hq - h0), tok, pos);
+    const int64_t tok = sg.tok0 + local;
+    if (part >= kv_parts) {
+        rotate_part<CPR, WHOLE>(p.c.r, p.c.Q, p.c.Q_out, a.L, a.n_total, p.c.hq, part - kv_parts, q_rows, tok, pos);
         return;
     }
-    const int lp = pos / a.ps;
-    const int page = lp < sg.first_new_lp ? sg.last_page : a.new_pages[sg.new0 + (lp - sg.first_new_lp)];
-    const int64_t src = lt * a.hkv * CPR, stride = static_cast<int64_t>(a.ps) * CPR;  // between a slot's heads
-    const int64_t dst = ((l * a.num_pages + page) * a.hkv * a.ps + (pos - lp * a.ps)) * CPR;
-    copy_rows<CPR>(a.V + src, a.v_pool + dst, stride, a.hkv);
-    rotate_rows<CPR, WHOLE>(p.c.r, a.K + src, a.k_pool + dst, stride, a.hkv, tok, pos);
+    const int lp = pos / a.ps, slot = pos - lp * a.ps;
+    const int64_t page = lp < sg.first_new_lp ? sg.last_page : a.new_pages[sg.new0 + (lp - sg.first_new_lp)];
+    rotate_rows<CPR, WHOLE, true>(
+        p.c.r, a.K, a.k_pool, a.V, a.v_pool, a.hkv, part * kv_rows, min((part + 1) * kv_rows, a.L * a.hkv), tok, pos,
+        [&](int l, int h) { return ((l * static_cast<int64_t>(a.n_total) + tok) * a.hkv + h) * CPR; },
+        [&](int l, int h) { return (((static_cast<int64_t>(l) * a.num_pages + page) * a.hkv + h) * a.ps + slot) * CPR; });
 }
 
 cudaLaunchConfig_t serial_config(int64_t blocks, unsigned threads, cudaStream_t st, cudaLaunchAttribute *attr)
@@ -327,7 +329,7 @@ __device__ __forceinline__ void rope_chunk_table(const RopeParams &r, const floa
 // (with the angles computed where a chunk is read, 8 times unrolled: 27), 8 agents' 333 tokens of 2 layers 12 us (20).
 template <typename Params, int CPR, int NC, bool WHOLE>
 __global__ void __launch_bounds__(kQ8Block, NC == 8 ? 1 : 3) append_rope_q8_kernel(const __grid_constant__ Params p, int threads, int page_blocks, int parts,
-                                                                  int tokens, int head_blocks, int head_block)
+                                                                  int tokens, int q_parts, int q_rows)
 {
     extern __shared__ float2 turns[];
     __shared__ uint32_t s_max[kQ8Block / 32];
@@ -335,16 +337,13 @@ __global__ void __launch_bounds__(kQ8Block, NC == 8 ? 1 : 3) append_rope_q8_kern
     ptx::griddep_wait();
     const auto &a = p.a;
     constexpr int HD = CPR * 8;
-    if (static_cast<int>(blockIdx.x) >= page_blocks) {  // Q's rows, a warp per token, layer and block of heads
-        int64_t r = static_cast<int64_t>(blockIdx.x - page_blocks) * (kQ8Block / 32) + (threadIdx.x >> 5);
-        const int h0 = static_cast<int>(r % head_blocks) * head_block;
-        r /= head_blocks;
-        int t = static_cast<int>(r % tokens), s = 0;
-        const int64_t l = r / tokens;
-        if (l >= a.L) return;
+    if (static_cast<int>(blockIdx.x) >= page_blocks) {  // Q's rows, a warp per token and part
+        const int64_t id = static_cast<int64_t>(blockIdx.x - page_blocks) * (kQ8Block / 32) + (threadIdx.x >> 5);
+        const int q_part = static_cast<int>(id / tokens);
+        if (q_part >= q_parts) return;
+        int t = static_cast<int>(id - static_cast<int64_t>(q_part) * tokens), s = 0;
         for (; t >= a.segs[s].n_tokens; ++s) t -= a.segs[s].n_tokens;
-        const int64_t tok = a.segs[s].tok0 + t, at = ((l * a.n_total + tok) * p.c.hq + h0) * CPR;
-        rotate_rows<CPR, WHOLE>(p.c.r, p.c.Q + at, p.c.Q_out + at, CPR, min(head_block, p.c.hq - h0), tok, a.segs[s].len0 + t);
+        rotate_part<CPR, WHOLE>(p.c.r, p.c.Q, p.c.Q_out, a.L, a.n_total, p.c.hq, q_part, q_rows, a.segs[s].tok0 + t, a.segs[s].len0 + t);
         return;
     }
     if (blockIdx.x == 0) enter_pages(a);
@@ -398,13 +397,15 @@ __global__ void __launch_bounds__(kQ8Block, NC == 8 ? 1 : 3) append_rope_q8_kern
 
 constexpr int kSmallSegs = 16, kSmallPages = 128;  // the small parameter block (as in pe_kv.cu)
 
-// Heads of a block of rows: all, or fewer (a multiple of what a warp reads at once) until the warps are 16 an SM.
-int block_of_heads(int64_t token_layers, int heads, int cpr)
+// Rows of a part: eight steps of a warp's rows, or fewer (a whole number of steps) until the warps are 16 an SM.  A part's rows
+// share their angles, whose eight sines and cosines take a thread longer than a step does.  A warp per token and layer / parts, 3890
+// tokens of 10 layers, 16 heads of Q and 2 of K of 128: 98 / 65 us; 3509 tokens of 21 layers, 8 and 8 of 64: 137 / 74.
+int part_of_rows(int64_t tokens, int rows, int cpr)
 {
-    const int least = 64 / cpr;  // rows of a warp
-    int hb = (heads + least - 1) / least * least;
-    while (hb > least && token_layers * ((heads + hb - 1) / hb) < 152 * 16) hb = (hb / 2 + least - 1) / least * least;
-    return hb;
+    const int step = 64 / cpr;  // rows of a warp
+    int n = 8;
+    while (n > 1 && (tokens * ((rows + n * step - 1) / (n * step)) < 152 * 16 || (n / 2) * step >= rows)) n /= 2;
+    return n * step;
 }
 
 template <typename Params, int CPR, bool WHOLE>
@@ -413,13 +414,13 @@ cudaError_t launch_append_rope_t(bool q8, const Params &p, cudaStream_t st)
     cudaLaunchAttribute attr;
     int64_t tokens = 0;
     for (int i = 0; i < p.a.n_segs; ++i) tokens += p.a.segs[i].n_tokens;
-    const int64_t lt = p.a.L * tokens;
-    const int hb = p.c.Q ? block_of_heads(lt, p.c.hq, CPR) : 1, nb = p.c.Q ? (p.c.hq + hb - 1) / hb : 0;
+    const int q_all = p.c.Q ? p.a.L * p.c.hq : 0, q_rows = part_of_rows(tokens, std::max(1, q_all), CPR), q_parts = (q_all + q_rows - 1) / q_rows;
     if (!q8) {
-        const int64_t blocks = (lt * (1 + nb) + kRowThreads / 32 - 1) / (kRowThreads / 32);
+        const int kv_all = p.a.L * p.a.hkv, kv_rows = part_of_rows(tokens, kv_all, CPR), kv_parts = (kv_all + kv_rows - 1) / kv_rows;
+        const int64_t blocks = (tokens * (kv_parts + q_parts) + kRowThreads / 32 - 1) / (kRowThreads / 32);
         if (blocks > INT32_MAX) return cudaErrorInvalidValue;
         const cudaLaunchConfig_t cfg = serial_config(blocks, kRowThreads, st, &attr);
-        return cudaLaunchKernelEx(&cfg, append_rope_kernel<Params, CPR, WHOLE>, p, nb, hb);
+        return cudaLaunchKernelEx(&cfg, append_rope_kernel<Params, CPR, WHOLE>, p, kv_parts, kv_rows, q_parts, q_rows);
     }
     // threads that share a page of one kv-head: half as many chunks each as append_q8_kernel's, for K takes twice the registers
     const int elems = p.a.ps * CPR * 8, threads = std::max(32, std::min(kQ8Block, elems / 32)), nc = elems / 8 / threads;
@@ -430,7 +431,7 @@ cudaError_t launch_append_rope_t(bool q8, const Params &p, cudaStream_t st)
     parts = (most + (most + parts - 1) / parts - 1) / ((most + parts - 1) / parts);  // (none without a group)
     int64_t longest = 0;
     for (int i = 0; i < p.a.n_segs; ++i) longest = std::max<int64_t>(longest, p.a.segs[i].n_tokens);
-    const int64_t page_blocks = pages * parts, blocks = page_blocks + (lt * nb + kQ8Block / 32 - 1) / (kQ8Block / 32);
+    const int64_t page_blocks = pages * parts, blocks = page_blocks + (tokens * q_parts + kQ8Block / 32 - 1) / (kQ8Block / 32);
     if (blocks > INT32_MAX) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = serial_config(blocks, kQ8Block, st, &attr);
     cfg.dynamicSmemBytes = static_cast<size_t>(std::min<int64_t>(p.a.ps, longest)) * p.c.r.n_pairs * sizeof(float2);
@@ -438,7 +439,7 @@ cudaError_t launch_append_rope_t(bool q8, const Params &p, cudaStream_t st)
     auto launch = [&](auto kernel, std::atomic<uint64_t> &configured) {
         if (cudaError_t e = set_dyn_smem_once(kernel, 128 * kRopeMaxPairs * static_cast<int>(sizeof(float2)), configured); e != cudaSuccess)
             return e;
-        return cudaLaunchKernelEx(&cfg, kernel, p, threads, pb, parts, n, std::max(1, nb), hb);
+        return cudaLaunchKernelEx(&cfg, kernel, p, threads, pb, parts, n, q_parts, q_rows);
     };
     static std::atomic<uint64_t> done[3];
     if (nc == 8) return launch(append_rope_q8_kernel<Params, CPR, 8, WHOLE>, done[0]);
@@ -473,15 +474,15 @@ cudaError_t launch_append_rope(bool q8, int head_dim, const AppendParams &a, con
 template <int CPR>
 static cudaError_t launch_rotate_t(const RotateParams &p, cudaStream_t st)
 {
-    const int64_t lt = static_cast<int64_t>(p.layers) * p.n_tokens;
-    if (lt <= 0) return cudaSuccess;
-    const int hb = block_of_heads(lt, p.heads, CPR), nb = (p.heads + hb - 1) / hb;
-    const int64_t blocks = (lt * nb + kRowThreads / 32 - 1) / (kRowThreads / 32);
+    const int rows = p.layers * p.heads;
+    if (p.n_tokens <= 0 || rows <= 0) return cudaSuccess;
+    const int part_rows = part_of_rows(p.n_tokens, rows, CPR), parts = (rows + part_rows - 1) / part_rows;
+    const int64_t blocks = (static_cast<int64_t>(p.n_tokens) * parts + kRowThreads / 32 - 1) / (kRowThreads / 32);
     if (blocks > INT32_MAX) return cudaErrorInvalidValue;
     cudaLaunchAttribute attr;
     const cudaLaunchConfig_t cfg = serial_config(blocks, kRowThreads, st, &attr);
-    return p.r.n_pairs % 8 == 0 ? cudaLaunchKernelEx(&cfg, rotate_kernel<CPR, true>, p, nb, hb)
-                                : cudaLaunchKernelEx(&cfg, rotate_kernel<CPR, false>, p, nb, hb);
+    return p.r.n_pairs % 8 == 0 ? cudaLaunchKernelEx(&cfg, rotate_kernel<CPR, true>, p, parts, part_rows)
+                                : cudaLaunchKernelEx(&cfg, rotate_kernel<CPR, false>, p, parts, part_rows);
 }
 
 cudaError_t launch_rotate(int head_dim, const RotateParams &p, cudaStream_t st)
