@@ -207,8 +207,10 @@ typedef struct {
  * What the cache holds does not turn again: a sequence whose positions change
  * (eviction, crops of middle parts) goes on with positions of the caller's.
  * On a host-only cache only the bookkeeping runs (tensors unused).
- * Errors: those of pe_append_kv_batch; INVALID (a bad rotation, null or
- * misaligned Q_out or positions, Q_out that overlaps K, V or a part of Q). */
+ * Errors: those of pe_append_kv_batch (after CUDA, Q_out may hold a part of the
+ * rotated queries: a call that rotates Q in place is not repeated on it);
+ * INVALID (a bad rotation, null or misaligned Q_out or positions, Q_out that
+ * overlaps K, V, the positions or a part of Q). */
 pe_status pe_append_kv_rope_batch(pe_cache *cache, int32_t n, const int32_t *seqs, const void *K_packed,
                                   const void *V_packed, const int32_t *cu_tokens, const pe_rope *rope,
                                   const int32_t *positions, const void *Q_packed, void *Q_out, int32_t num_q_heads,

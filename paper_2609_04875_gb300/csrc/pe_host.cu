@@ -2851,6 +2851,8 @@ static pe_status append_batch(pe_cache *c, int32_t n, const int32_t *seqs, const
             if (ra->Q != ra->Q_out && !apart(ra->Q, q_bytes, ra->Q_out, q_bytes)) return fail(PE_ERR_INVALID, "Q_out overlaps Q");
             if (!apart(ra->Q_out, q_bytes, K, kv_bytes) || !apart(ra->Q_out, q_bytes, V, kv_bytes))
                 return fail(PE_ERR_INVALID, "Q_out overlaps K or V");
+            if (ra->positions && !apart(ra->Q_out, q_bytes, ra->positions, total * ra->rope->n_axes * 4))
+                return fail(PE_ERR_INVALID, "Q_out overlaps the positions");
         }
     }
     CallTxn tx(c, static_cast<cudaStream_t>(stream));
@@ -2903,6 +2905,7 @@ pe_status pe_rotate_batch(pe_cache *c, int32_t n, const int32_t *seqs, const voi
     if (!aligned16(X) || !aligned16(out)) return fail(PE_ERR_INVALID, "X and out must be 16-byte aligned");
     const int64_t bytes = static_cast<int64_t>(num_layers) * total * num_heads * c->cfg.head_dim * 2;
     if (X != out && !apart(X, bytes, out, bytes)) return fail(PE_ERR_INVALID, "out overlaps X");
+    if (positions && !apart(out, bytes, positions, total * rope->n_axes * 4)) return fail(PE_ERR_INVALID, "out overlaps the positions");
     p.X = static_cast<const uint4 *>(X);
     p.out = static_cast<uint4 *>(out);
     p.layers = num_layers;

@@ -346,3 +346,22 @@ def test_refusals():
         cache.rotate(s, x[:, :, ::2].repeat(1, 1, 2)[:, ::1].transpose(0, 1), rope)
     with pytest.raises(ValueError):
         pe.Rope([1.0, 2.0], axis=[0])
+
+
+def test_refuses_outputs_over_positions():
+    g = gen(14)
+    cache, (s,), _, _ = filled(1, 2, 64, 16, [5], [40], g=g)
+    rope = pe.Rope(freqs(32), axis=[0] * 16 + [1] * 16)
+    K = randn(g, 1, 4, 2, 64)
+    both = torch.zeros(512 + 16, dtype=torch.bfloat16, device="cuda")
+    X, pos = both[:512].view(1, 4, 2, 64), both[512:].view(torch.int32).view(2, 4)
+    inside = both[496:512].view(torch.int32).view(2, 4)   # the last 32 bytes of X
+    state = cache.seq_info(s), cache.free_list()
+    with pytest.raises(pe.PEError, match="positions"):
+        cache.append_kv_rope(s, K, K.clone(), rope, Q=X, Q_out=X, positions=inside)
+    with pytest.raises(pe.PEError, match="positions"):
+        cache.rotate(s, X, rope, positions=inside, out=X)
+    assert (cache.seq_info(s), cache.free_list()) == state
+    cache.rotate(s, X, rope, positions=pos, out=X)         # side by side
+    cache.append_kv_rope(s, K, K.clone(), rope, Q=X, Q_out=X, positions=pos)
+    assert cache.seq_info(s)[0] == 9
