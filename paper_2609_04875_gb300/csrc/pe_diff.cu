@@ -45,8 +45,8 @@ struct DiffCfg {
     static constexpr int kOffBar = kOffV + kStages * kVBytes;
     // k_full, k_empty, v_full, v_empty [stages]; q_full, edge; s_full, p_full, o_done [2]
     static constexpr int kNumBars = 4 * kStages + 2 + 6;
-    static constexpr int kOffMisc = kOffBar + kNumBars * 8;   // tmem slot, abort flag, keys not finite [2]
-    static constexpr int kOffLse = kOffMisc + 16;             // float [128]: whole units
+    static constexpr int kOffMisc = kOffBar + kNumBars * 8;   // tmem slot, abort flag, keys not finite [2][2]
+    static constexpr int kOffLse = kOffMisc + 24;             // float [128]: whole units
     static constexpr int kRowFloats = 2 * HD + 4;             // of a row's O there, in the stages' memory: 16 bytes past a multiple of 128
     static constexpr int kDynSmem = kOffLse + 128 * 4 + 1024;
     static constexpr int kTmemO = 256;                        // S at 0 and 128, P over S
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
     const uint32_t b_o_done = b_p_full + 16;   // [2]
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::kOffMisc + 4);
-    uint32_t *odd_keys = reinterpret_cast<uint32_t *>(smem + C::kOffMisc + 8);  // [2]
+    uint32_t *odd_keys = reinterpret_cast<uint32_t *>(smem + C::kOffMisc + 8);  // [2][2]
     float *s_rows = reinterpret_cast<float *>(smem + C::kOffK), *s_lse = reinterpret_cast<float *>(smem + C::kOffLse);
     const WaitCtx wctx{abort_flag, p.status};
 
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
             ptx::mbar_init(b_o_done + 8 * s, 1);
         }
         *abort_flag = 0;
-        odd_keys[0] = odd_keys[1] = 0;
+        for (int k = 0; k < 4; ++k) odd_keys[k] = 0;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
         ptx::prefetch_tensormap(&tm_k);
@@ -307,9 +307,13 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                     for (int c = 0; c < HD / 8; ++c)
                         odd = max(odd, bf16x8_absmax(*reinterpret_cast<const uint4 *>(v + (c >> 3) * C::kVRegion + (((c & 7) ^ (key & 7)) << 4))));
                     const bool is_odd = odd >= 0x7f80u;
-                    if (is_odd) atomicOr(&odd_keys[key >> 5], 1u << (key & 31));
+                    // Two sets of words in turn (a tile has one meeting or three, so their parity tells it from the next):
+                    // a thread that is ahead may mark the next tile's keys before all have read this one's, but not those
+                    // of the tile after, which is past the next one's meeting.
+                    volatile uint32_t *odd_set = odd_keys + 2 * (met & 1);
+                    if (is_odd) atomicOr(const_cast<uint32_t *>(odd_set) + (key >> 5), 1u << (key & 31));
                     if (!meet()) { ok = false; break; }
-                    const uint64_t odd_mask = odd_keys[0] | static_cast<uint64_t>(odd_keys[1]) << 32;
+                    const uint64_t odd_mask = odd_set[0] | static_cast<uint64_t>(odd_set[1]) << 32;
                     if (odd_mask) {
                         if (is_odd)
                             for (int c = 0; c < HD / 8; ++c)
@@ -318,7 +322,7 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                         const int sees = pos - kbase + 1;  // keys of the tile
                         if (sees > 0 && (odd_mask & (sees >= 64 ? ~0ull : (1ull << sees) - 1))) l = NAN;
                         if (!meet()) { ok = false; break; }  // the mask is read
-                        if (row < 2) odd_keys[row] = 0;
+                        if (row < 2) odd_set[row] = 0;
                         if (!meet()) { ok = false; break; }  // and cleared
                     }
                 }

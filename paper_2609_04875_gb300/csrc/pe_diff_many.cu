@@ -48,8 +48,8 @@ struct ManyCfg {
     static constexpr int kOffBar = kOffNeed + 2 * 128;
     // k_full, k_empty, v_full, v_empty, v_peer [stages]; q_full, q_empty, meet, edge; s_full, p_full, o_done [2]
     static constexpr int kNumBars = 5 * kStages + 4 + 6;
-    static constexpr int kOffMisc = kOffBar + kNumBars * 8;   // tmem slot, abort, votes [2], keys not finite [4]
-    static constexpr int kDynSmem = kOffMisc + 32 + 1024;
+    static constexpr int kOffMisc = kOffBar + kNumBars * 8;   // tmem slot, abort, votes [2], keys not finite [2][4]
+    static constexpr int kDynSmem = kOffMisc + 48 + 1024;
     static constexpr int kTmemO = 256;                        // S at 0 and 128
     static constexpr uint32_t kTmemCols = 512;
     static_assert(kDynSmem <= 232448, "shared memory budget");
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::kOffMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::kOffMisc + 4);
     volatile uint32_t *votes = reinterpret_cast<volatile uint32_t *>(smem + C::kOffMisc + 8);      // [2]
-    volatile uint32_t *odd_keys = reinterpret_cast<volatile uint32_t *>(smem + C::kOffMisc + 16);  // [4]
+    volatile uint32_t *odd_keys = reinterpret_cast<volatile uint32_t *>(smem + C::kOffMisc + 16);  // [2][4]
     const WaitCtx wctx{abort_flag, p.status};
 
     if (threadIdx.x == 0) {
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
         }
         *abort_flag = 0;
         votes[0] = votes[1] = 0;
-        for (int k = 0; k < 4; ++k) odd_keys[k] = 0;
+        for (int k = 0; k < 8; ++k) odd_keys[k] = 0;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
         ptx::prefetch_tensormap(&tm_q);
@@ -405,14 +405,16 @@ __global__ void __launch_bounds__(kManyThreads, 1)
                     for (int c = 0; c < HD / 16; ++c)
                         odd = max(odd, bf16x8_absmax(*reinterpret_cast<const uint4 *>(v + ((c0 + c) >> 3) * C::kVRegion + (((c0 + c) & 7) << 4))));
                     const bool is_odd = odd >= 0x7f80u;
+                    // two sets of words in turn, by the meetings' parity (pe_diff.cu): the other CTA may be a tile ahead
+                    const int odd_set = 4 * (edges & 1);
                     if (is_odd) {
-                        or_cluster(odd0 + 4 * (key >> 5), 1u << (key & 31));
-                        or_cluster(odd1 + 4 * (key >> 5), 1u << (key & 31));
+                        or_cluster(odd0 + 4 * (odd_set + (key >> 5)), 1u << (key & 31));
+                        or_cluster(odd1 + 4 * (odd_set + (key >> 5)), 1u << (key & 31));
                     }
                     if (!meet_pair(__any_sync(0xffffffffu, is_odd))) { ok = false; break; }
                     uint32_t mask[4];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) mask[x] = odd_keys[x];
+                    for (int x = 0; x < 4; ++x) mask[x] = odd_keys[odd_set + x];
                     if (mask[0] | mask[1] | mask[2] | mask[3]) {
                         if (mask[key >> 5] >> (key & 31) & 1u)
                             for (int c = 0; c < HD / 16; ++c)
@@ -424,7 +426,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
                             if (sees > 0 && (mask[x] & (sees >= 32 ? ~0u : (1u << sees) - 1))) l = NAN;
                         }
                         if (!meet_pair(false)) { ok = false; break; }  // the mask is read
-                        if (threadIdx.x < 4) odd_keys[threadIdx.x] = 0;
+                        if (threadIdx.x < 4) odd_keys[odd_set + threadIdx.x] = 0;
                         if (!meet_pair(true)) { ok = false; break; }   // and cleared
                     }
                 }
