@@ -275,8 +275,8 @@ pe_status pe_replay_attn_weights_batch(pe_cache *cache, int32_t n, const int32_t
  * multiplies the norm by, 1 - lambda_init included), or NULL: out = O.  eps >= 0.
  * Q: device bf16 [cu_q[n]][Hq][d]; out: device bf16 [cu_q[n]][Hq / 2][2d], which
  * must not overlap Q, lambda or gain.  Sums, maxima and the norm in 32 bits, in
- * an order that does not depend on timing; weights rounded to bf16, as in
- * pe_replay_attn_batch.  A map none of whose scores is above -infinity counts as
+ * an order that does not depend on timing; a weight as two bf16 parts, off by
+ * 2^-16 of itself, so that maps which nearly cancel lose no more.  A map none of whose scores is above -infinity counts as
  * zero.  Keys that a row does not see do not reach it, whatever they hold; an
  * infinity or NaN among those it sees makes outputs infinite or NaN.
  * 8-bit caches attend by way of the unpacked layer.

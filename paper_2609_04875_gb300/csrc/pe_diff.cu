@@ -6,9 +6,9 @@
 // One pass over keys and values for both maps: the M side of the products holds 64 rows of each map, the maps of the same
 // queries.  Per tile of 64 keys
 //     S [128 x 128]  = Q [128 x d] . [K_2j ; K_2j+1]^T        (a row uses the 64 columns of its own map)
-//     O [128 x 2d]  += P [128 x 64] . [V_2j | V_2j+1]         (A = P from TMEM)
+//     O [128 x 2d]  += P [128 x 64] . [V_2j | V_2j+1]         (A = P from TMEM, in two parts: two_parts)
 // so half of S is not used, and where there are few rows most of M is not; both cost less than the keys' way from memory
-// (64 keys, d = 128: 64 KB, 2800 cycles of an SM's share of HBM; its MMAs 1024).
+// (64 keys, d = 128: 64 KB, 2800 cycles of an SM's share of HBM; its MMAs 1536).
 //
 // Work is cut into equal stretches of tiles, a CTA each (pe_internal.h); every piece writes O / l and its log-sum-exp, and
 // the merge joins a row's pieces of both maps, subtracts and norms.  Where keys are few a cluster takes a whole unit and joins
@@ -254,8 +254,8 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                 ptx::tc_fence_after();
                 const uint64_t vd = v_desc + (i % C::kStages) * (C::kVBytes >> 4);
 #pragma unroll
-                for (int kk = 0; kk < DiffFew::kKeys / 16; ++kk)
-                    mma_bf16_ts_warp(tm + C::kTmemO, tm + 128 * (i & 1) + kk * 8, vd + (kk * 16 * 128 >> 4), kIdescO,
+                for (int kk = 0; kk < 2 * DiffFew::kKeys / 16; ++kk)  // the weights' upper parts, then their lower ones
+                    mma_bf16_ts_warp(tm + C::kTmemO, tm + 128 * (i & 1) + kk * 8, vd + ((kk & 3) * 16 * 128 >> 4), kIdescO,
                                      (k > 0 || kk > 0) ? 1u : 0u);
                 mma_commit_warp(b_o_done + 8 * (i & 1));
                 mma_commit_warp(b_v_empty + 8 * (i % C::kStages));
@@ -342,22 +342,23 @@ __global__ void __launch_bounds__(kDiffThreads, 1)
                         for (int c = 0; c < DiffFew::kKeys; ++c)
                             if (kbase + c > pos) s[c] = -INFINITY;
                     }
-                    // weights against the row's reference, which moves only when a tile's sum passes 2^64 (pe_attn.cu); the
-                    // row is divided by the sum of its weights as rounded
+                    // weights against the row's reference, which moves only when a tile's sum passes 2^64 (pe_attn.cu)
                     auto exp_tile = [&](float ref) -> float {
                         const float2 nref = make_float2(-ref, -ref);
                         float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                         for (int ch = 0; ch < DiffFew::kKeys / 32; ++ch) {
-                            uint32_t pk[16];
+                            uint32_t pk[16], lo[16];
 #pragma unroll
                             for (int x = 0; x < 16; ++x) {
                                 const int c = ch * 32 + 2 * x;
                                 const float2 y = fma2(make_float2(s[c], s[c + 1]), sl2, nref);
-                                pk[x] = pack_bf16(ex2(y.x), ex2(y.y));
-                                acc[x & 3] = add2(acc[x & 3], unpack_bf16(pk[x]));
+                                const float2 e = make_float2(ex2(y.x), ex2(y.y));
+                                pk[x] = two_parts(e, lo[x]);
+                                acc[x & 3] = add2(acc[x & 3], e);
                             }
                             tmem_st16(tS + ch * 16, pk);
+                            tmem_st16(tS + DiffFew::kKeys / 2 + ch * 16, lo);
                         }
                         const float2 a = add2(add2(acc[0], acc[1]), add2(acc[2], acc[3]));
                         return a.x + a.y;

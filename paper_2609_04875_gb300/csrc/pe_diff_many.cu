@@ -4,8 +4,8 @@
 // units of their own.  Per tile of 128 keys, by tcgen05 over a pair of CTAs (128 rows each)
 //     S [256 x 128] = Q [256 x d] . K_2j+m^T            (each CTA's shared memory holds 64 of the keys)
 //     O [256 x 2d] += P [256 x 128] . [V_2j | V_2j+1]   (A = P from TMEM; each CTA's shared memory holds one kv-head's V)
-// so a CTA loads half of a tile: 48 KB (d = 128) for 1536 cycles of MMAs, 32 bytes a cycle, where the whole would be 64 and
-// as much as an SM takes in.
+// P goes to the second product as two bf16 parts (two_parts, diff.cuh), which take the columns of S that they come from.
+// So a CTA loads half of a tile: 48 KB (d = 128) for 2560 cycles of MMAs.
 //
 // Bound by the tensor cores.  S(j + 1) is computed before P(j) is waited for, so a tile's softmax has the time of a tile's
 // MMAs; it is spread over two warpgroups, each with half of the tile's keys (64 exponentials a thread).  The halves of a row
@@ -335,8 +335,8 @@ __global__ void __launch_bounds__(kManyThreads, 1)
                 ptx::tc_fence_after();
                 const uint64_t vd = v_desc + (i % C::kStages) * (C::kVBytes >> 4);
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk)  // P's halves over S's
-                    mma_pair_ts(tm + C::kTmemO, tm + 128 * (i & 1) + (kk >> 2) * 64 + (kk & 3) * 8, vd + (kk * 16 * 128 >> 4), kIdescO,
+                for (int kk = 0; kk < 16; ++kk)  // P's halves over S's: of each the weights' upper parts, then their lower ones
+                    mma_pair_ts(tm + C::kTmemO, tm + 128 * (i & 1) + kk * 8, vd + (((kk >> 3) * 4 + (kk & 3)) * 16 * 128 >> 4), kIdescO,
                                 (k > 0 || kk > 0) ? 1u : 0u);
                 commit_pair(b_o_done + 8 * (i & 1));
                 commit_pair(b_v_empty + 8 * (i % C::kStages));
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(kManyThreads, 1)
 #pragma unroll
                     for (int x = 0; x < 4; ++x) mask[x] = odd_keys[odd_set + x];
                     if (mask[0] | mask[1] | mask[2] | mask[3]) {
-                        if (mask[key >> 5] >> (key & 31) & 1u)
+                        if (odd_keys[odd_set + (key >> 5)] >> (key & 31) & 1u)
                             for (int c = 0; c < HD / 16; ++c)
                                 *reinterpret_cast<uint4 *>(v + ((c0 + c) >> 3) * C::kVRegion + (((c0 + c) & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
                         ptx::fence_proxy_async_smem();
@@ -450,15 +450,17 @@ __global__ void __launch_bounds__(kManyThreads, 1)
                     float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                     for (int ch = 0; ch < 2; ++ch) {
-                        uint32_t pk[16];
+                        uint32_t pk[16], lo[16];
 #pragma unroll
                         for (int x = 0; x < 16; ++x) {
                             const int c = ch * 32 + 2 * x;
                             const float2 y = fma2(make_float2(s[c], s[c + 1]), sl2, nref);
-                            pk[x] = pack_bf16(ex2(y.x), ex2(y.y));
-                            acc[x & 3] = add2(acc[x & 3], unpack_bf16(pk[x]));
+                            const float2 e = make_float2(ex2(y.x), ex2(y.y));
+                            pk[x] = two_parts(e, lo[x]);
+                            acc[x & 3] = add2(acc[x & 3], e);
                         }
                         tmem_st16(tS + ch * 16, pk);
+                        tmem_st16(tS + 32 + ch * 16, lo);
                     }
                     const float2 a = add2(add2(acc[0], acc[1]), add2(acc[2], acc[3]));
                     return a.x + a.y;
