@@ -2308,16 +2308,19 @@ struct DiffItem {
     int32_t q_row0, n_q, n_keys;
 };
 
-// Rows (n_q x group) up to which a sequence takes the kernel of few rows.  More of them would go through it in blocks of 64, each
-// with the keys again: 128 rows on 3000 keys 20.6 us (many rows' kernel: 20.1), on 20000 41.7 (35.9), on 8 x 8000 101 (72), on
-// 500 14.5 (15.4); 68 rows on 20000 31.1 (34.5); d = 64, 128 rows on 8 x 8000 52 (63), on 20000 31.4 (28.7).
-constexpr int64_t kDiffFewRows = 64;
+// Rows (n_q x group) up to which a sequence takes the kernel of few rows, in blocks of 64, each with the keys again.  Many rows'
+// kernel leaves half of its 256 rows empty at 128, and reads V for each map; at d = 64 it is bound by its softmax besides.  us, few
+// (many): d = 64, 128 rows on 3000 keys 16.0 (17.8), on 20000 33.8 (31.4), on 8 x 8000 53 (71); 68 rows 26 (31) and 49 (70); 256
+// rows on 8 x 8000 93 (78).  d = 128, 128 rows on 500 keys 16.5 (15.7), on 8000 33.6 (30.7), on 20000 45 (44), on 60000 79 (89),
+// on 8 x 8000 103 (97); 68 rows 16.5 (14.4) on 500, 36 (42) on 20000, 95 (94) on 8 x 8000.
+constexpr int64_t diff_few_rows(int head_dim) { return head_dim == 64 ? 128 : 64; }
 
 // A unit's cost besides its tiles, in tiles: queries fetched, a first tile whose products wait for its softmax, outputs written.
-// Many rows, 2000 queries on 2000 keys, 32 / 8 heads, d = 128 (256 units of 8 tiles): 2 81 us, 4 73, 6 71.5, 8 74; few rows, 5
-// agents of 9000 keys, 3 queries: 1 21.1, 3 19.5, 4 18.9, 6 18.4; 16 of 1500, one query: 21.5, 20.3, 19.5, 19.7.
+// Many rows, 2000 queries on 2000 keys, 32 / 8 heads, d = 128 (256 units of 8 tiles): 2 92.7 us, 3 88.7, 4 89.0, 6 90.8, 8 94.7; 500
+// on 1000: 29.0, 27.9, 27.6, 27.6, 27.7.  Few rows, 8 sequences of 1000 keys, 128 rows: 3 31.6, 4 31.4, 5 30.3, 7 29.5; 16 of 1500,
+// one query: 23.4, 22.9, 23.8, 25.3.
 template <typename Shape>
-constexpr int64_t kDiffUnitCost = Shape::kMaps == 2 ? 6 : 5;
+constexpr int64_t kDiffUnitCost = Shape::kMaps == 2 ? 4 : 5;
 
 // One launch over the items, at most kMaxSegs: fills p's sequences and stretches.
 // Few rows on few keys: a cluster of 1 to 8 CTAs a whole unit, at most kDiffWholeTiles tiles each where there are SMs enough, whose
@@ -2470,7 +2473,7 @@ pe_status run_diff(pe_cache *c, const std::vector<AttnItem> &all, int32_t layer,
     for (const AttnItem &it : all) {
         if (it.n_q <= 0) continue;
         const int64_t rows = static_cast<int64_t>(it.n_q) * p.group;
-        (rows <= kDiffFewRows ? few : many).push_back(DiffItem{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq])});
+        (rows <= diff_few_rows(c->cfg.head_dim) ? few : many).push_back(DiffItem{it.seq, it.q_row0, it.n_q, static_cast<int32_t>(c->len[it.seq])});
     }
     if (pe_status s = launch_diff<DiffFew>(c, few, q_rows, p, st)) return s;
     return launch_diff<DiffMany>(c, many, q_rows, p, st);

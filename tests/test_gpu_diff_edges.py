@@ -65,6 +65,14 @@ def test_few_rows_of_many_units(T, n, hq):
     check(Setup(lens, 16, 64, 16, seed=T + n), [n] * 12, hq, [T - 90, T - 40, T - 5])
 
 
+# 65 to 128 rows: two blocks of 64, each with its own edge; one query's 128 heads in both
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T,n,hq,bad", [(700, 128, 2, [650, 699]), (5000, 100, 2, [4990]), (2000, 32, 8, [1985]), (130, 65, 2, [64, 129]),
+                                        (300, 1, 256, [299]), (200, 128, 2, [100])])
+def test_two_blocks(T, n, hq, bad, d):
+    check(Setup([T], 2, d, 16, seed=T + n + hq), [n], hq, bad)
+
+
 # tiles of 128 keys: a block of 256 rows has two or three on the edge, a whole prompt all of them
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("T,n,bad", [(700, 300, [690]), (700, 300, [450, 690]), (700, 700, [5]), (700, 700, [140, 300, 520]), (700, 700, [260, 699]),
