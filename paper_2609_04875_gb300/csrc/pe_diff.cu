@@ -735,22 +735,37 @@ cudaLaunchConfig_t diff_config(int blocks, int threads, int smem, cudaStream_t s
     return cfg;
 }
 
+// n clusters of `ranks` CTAs.
 template <int HD>
-cudaError_t launch_diff_t(const CUtensorMap &k, const CUtensorMap &v, const DiffParams &p, cudaStream_t st)
+cudaError_t diff_attn_config(int n, int ranks, cudaStream_t st, cudaLaunchAttribute (&attr)[2], cudaLaunchConfig_t &cfg)
 {
     static std::atomic<uint64_t> configured{0};
-    cudaError_t e = set_dyn_smem_once(diff_attn_kernel<HD>, DiffCfg<HD>::kDynSmem, configured);
-    if (e != cudaSuccess) return e;
-    cudaLaunchAttribute attr[2];
-    const int ranks = std::max(1, p.whole);
-    cudaLaunchConfig_t cfg = diff_config(p.n_takers * ranks, kDiffThreads, DiffCfg<HD>::kDynSmem, st, attr);
+    cfg = diff_config(n * ranks, kDiffThreads, DiffCfg<HD>::kDynSmem, st, attr);
     if (ranks > 1) {
         attr[1].id = cudaLaunchAttributeClusterDimension;
         attr[1].val.clusterDim.x = static_cast<unsigned>(ranks);
         attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
         cfg.numAttrs = 2;
     }
+    return set_dyn_smem_once(diff_attn_kernel<HD>, DiffCfg<HD>::kDynSmem, configured);
+}
+
+template <int HD>
+cudaError_t launch_diff_t(const CUtensorMap &k, const CUtensorMap &v, const DiffParams &p, cudaStream_t st)
+{
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg;
+    if (cudaError_t e = diff_attn_config<HD>(p.n_takers, std::max(1, p.whole), st, attr, cfg); e != cudaSuccess) return e;
     return cudaLaunchKernelEx(&cfg, diff_attn_kernel<HD>, k, v, p);
+}
+
+template <int HD>
+cudaError_t diff_clusters_t(int ranks, int *n)
+{
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg;
+    if (cudaError_t e = diff_attn_config<HD>(1, ranks, nullptr, attr, cfg); e != cudaSuccess) return e;
+    return cudaOccupancyMaxActiveClusters(n, diff_attn_kernel<HD>, &cfg);
 }
 
 }  // namespace
@@ -759,6 +774,11 @@ cudaError_t launch_diff_attn(int head_dim, const CUtensorMap &tm_k, const CUtens
 {
     if (p.n_takers <= 0) return cudaSuccess;
     return head_dim == 128 ? launch_diff_t<128>(tm_k, tm_v, p, st) : launch_diff_t<64>(tm_k, tm_v, p, st);
+}
+
+cudaError_t diff_resident_clusters(int head_dim, int ranks, int *n)
+{
+    return head_dim == 128 ? diff_clusters_t<128>(ranks, n) : diff_clusters_t<64>(ranks, n);
 }
 
 cudaError_t launch_diff_combine(int head_dim, bool many, const DiffParams &p, cudaStream_t st)

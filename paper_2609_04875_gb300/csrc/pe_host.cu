@@ -115,6 +115,7 @@ struct pe_cache {
     // device state
     int device = 0;
     int num_sms = 148;
+    int diff_clusters[3] = {};         // of 2, 4 and 8 CTAs that the device holds at once (differential attention; 0: not asked yet)
     void *k_pool = nullptr, *v_pool = nullptr;  // bf16, what the attention kernels read.  8-bit cache: one layer only,
                                                 // the called layer's pages unpacked at their page ids
     bool q8 = false;              // K and V held in 8 bits (q8.cuh)
@@ -2322,16 +2323,17 @@ constexpr int64_t diff_few_rows(int head_dim) { return head_dim == 64 ? 128 : 64
 template <typename Shape>
 constexpr int64_t kDiffUnitCost = Shape::kMaps == 2 ? 4 : 5;
 
-// One launch over the items, at most kMaxSegs: fills p's sequences and stretches.
 // Few rows on few keys: a cluster of 1 to 8 CTAs a whole unit, at most kDiffWholeTiles tiles each where there are SMs enough, whose
 // rows it joins itself, in place of cutting every unit and merging the pieces in a second launch.  A tile takes 0.75 us, a
 // row of each of nine warps about as much.  A call of one query, with its output allocated (host and GPU), whole / cut: 8
 // heads of d = 64 on 640 keys 10.9 / 15.2 us, on 3000 12.6 / 16.0, 16 of d = 128 on 2 x 2000 12.9 / 15.2, 32 on 7 x 1700 14.5 /
-// 15.9; on 5000 (10 tiles a CTA) 16.8 / 15.8.
+// 15.9; on 5000 (10 tiles a CTA) 16.8 / 15.8.  Only clusters that the device holds all at once: of 8 CTAs the card has room for
+// 15, not 19, and a sixteenth waits for another to end (16 units of 2000 keys 26.8 us, cut 13.9).
 constexpr int64_t kDiffWhole = 8;       // tiles and rounds of rows of a CTA
 constexpr int64_t kDiffWholeTiles = 4;  // (10 tiles over 1, 2, 4 CTAs: 11.1, 9.7, 9.0 us; 5 over 1, 2: 9.6, 9.8)
 constexpr int64_t kDiffWholeRanks = 8;
 
+// One launch over the items, at most kMaxSegs: fills p's sequences and stretches.
 template <typename Shape>
 void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t max_takers, DiffParams &p)
 {
@@ -2362,7 +2364,7 @@ void plan_diff(const pe_cache *c, const std::vector<DiffItem> &items, int64_t ma
     p.whole = 0;
     if (Shape::kMaps == 1 && units <= max_takers) {
         int64_t ranks = 1;
-        while (ranks < kDiffWholeRanks && longest > kDiffWholeTiles * ranks && 2 * ranks * units <= max_takers) ranks *= 2;
+        for (int x = 0; ranks < kDiffWholeRanks && longest > kDiffWholeTiles * ranks && units <= c->diff_clusters[x]; ++x) ranks *= 2;
         if (ceil_div(longest, ranks) + ceil_div(rows, 9 * ranks) <= kDiffWhole) {
             p.whole = static_cast<int32_t>(ranks);
             p.n_takers = units;
@@ -2408,6 +2410,10 @@ pe_status launch_diff(pe_cache *c, const std::vector<DiffItem> &all, int64_t q_r
     const int64_t sms = std::min<int64_t>(c->num_sms, kMaxSkCtas);
     const int64_t takers = std::max<int64_t>(1, std::min<int64_t>(kMany ? sms / 2 : sms, slots / 2));
     const int64_t room = (slots - takers) / (p.hkv / 2 * Shape::kMaps);  // blocks; besides, a slot a taker
+    if (!kMany && c->diff_clusters[0] == 0)
+        for (int x = 0; x < 3; ++x)
+            if (cudaError_t e = diff_resident_clusters(c->cfg.head_dim, 2 << x, &c->diff_clusters[x]); e != cudaSuccess)
+                return cuda_fail(e, "differential attention's clusters");
     std::vector<DiffItem> items;
     int64_t used = 0;
     auto flush = [&]() -> pe_status {

@@ -520,6 +520,8 @@ cudaError_t launch_append_rope(bool q8, int head_dim, const AppendParams &p, con
 cudaError_t launch_rotate(int head_dim, const RotateParams &p, cudaStream_t st);
 // tm_k / tm_v: the pools as 2-D maps with 64 x min(ps, 64) boxes, 128-byte swizzle.
 cudaError_t launch_diff_attn(int head_dim, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const DiffParams &p, cudaStream_t st);
+// Clusters of `ranks` CTAs of it that the current device holds at once.
+cudaError_t diff_resident_clusters(int head_dim, int ranks, int *n);
 // tm_q: Q as {d, 2, Hq / 2, rows} with boxes of 64 columns, one map and 128 rows of a pair.
 cudaError_t launch_diff_attn_many(int head_dim, const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
                                   const DiffParams &p, cudaStream_t st);
