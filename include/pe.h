@@ -185,8 +185,10 @@ pe_status pe_append_kv_batch(pe_cache *cache, int32_t n, const int32_t *seqs, co
  *   a' = scale (a cos - b sin),  b' = scale (b cos + a sin)
  * in 32 bits, rounded once.  Columns from 2 n_pairs on stay as they are.  The
  * position is the token's on axis axis[i] (time, height, width, ...).  Angles
- * are taken modulo a full turn in 64-bit integers, so far positions lose no
- * precision.  Kept by the caller; read inside the call only. */
+ * are taken modulo a full turn in 64-bit integers: besides the 32 bits of the
+ * sine and cosine, an angle is off by no more than |position| times the rounding
+ * of freq[i] / 2 pi in 64 bits (|freq| up to 1: 2^-21 radian at 2^31 positions).
+ * Kept by the caller; read inside the call only. */
 typedef struct {
     int32_t n_pairs;            /* 1 .. head_dim / 2 */
     int32_t interleaved;        /* 0: pairs (i, i + n_pairs); 1: neighbours */
@@ -274,11 +276,12 @@ pe_status pe_replay_attn_weights_batch(pe_cache *cache, int32_t n, const int32_t
  * lambda: device fp32 [Hq / 2].  gain: device fp32 [2d] (what the model
  * multiplies the norm by, 1 - lambda_init included), or NULL: out = O.  eps >= 0.
  * Q: device bf16 [cu_q[n]][Hq][d]; out: device bf16 [cu_q[n]][Hq / 2][2d], which
- * must not overlap Q, lambda or gain.  Sums, maxima and the norm in 32 bits, in
- * an order that does not depend on timing; a weight as two bf16 parts, off by
- * 2^-16 of itself, so that maps which nearly cancel lose no more.  A map none of whose scores is above -infinity counts as
- * zero.  Keys that a row does not see do not reach it, whatever they hold; an
- * infinity or NaN among those it sees makes outputs infinite or NaN.
+ * must not overlap Q, lambda or gain.  Sums, maxima and the norm in 32 bits
+ * (whose squares hold |O| below 2^59), in an order that does not depend on
+ * timing; a weight as two bf16 parts, off by 2^-16 of itself, so that maps which
+ * nearly cancel lose no more.  A map none of whose scores is above -infinity
+ * counts as zero.  Keys that a row does not see do not reach it, whatever they
+ * hold; an infinity or NaN among those it sees makes outputs infinite or NaN.
  * 8-bit caches attend by way of the unpacked layer.
  * Errors: those of pe_replay_attn_batch; UNSUPPORTED (an odd number of
  * kv-heads), INVALID (null or misaligned lambda, misaligned gain, eps negative

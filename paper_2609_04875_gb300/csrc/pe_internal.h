@@ -58,7 +58,8 @@ constexpr int kRopeMaxPairs = 64;      // head_dim / 2
 constexpr int kRopeMaxAxes = 8;
 
 // Pair i of a head's columns turns by turn[i] 2^-64 of a full turn a position.  The product with a position, modulo 2^64,
-// is the angle modulo a full turn, exactly: however far the position, the angle errs by no more than turn[i]'s own rounding.
+// is the angle of that fraction modulo a full turn, exactly: what is off is the fraction, by 2^-52 of |frequency| / 2 pi (a
+// division in double) and 2^-64, so the angle by |position| times that (|frequency| up to 1: 2^-21 radian at 2^31 positions).
 struct RopeParams {
     uint64_t turn[kRopeMaxPairs];
     uint8_t axis[kRopeMaxPairs];
