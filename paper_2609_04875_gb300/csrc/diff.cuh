@@ -9,7 +9,7 @@ constexpr float kDiffSumLimit = 1.8446744e19f;  // 2^64: larger tile sums move a
 
 // A pair of weights as two bf16 parts each: their upper ones, and in `lo` what those leave over, so that a weight is off by
 // 2^-16 of itself.  One part is not enough here: what the maps share cancels, and the errors of both maps' weights stay while the
-// difference shrinks (maps 2 % apart, lambda 0.95: 2e-2 to 4e-2 off in the 2-norm with one part, 1.7e-3 with two, which is the
+// difference shrinks (maps 2 % apart, lambda 0.95: up to 3.6e-2 off in the 2-norm with one part, 1.7e-3 with two, which is the
 // output's own rounding).
 __device__ __forceinline__ uint32_t two_parts(float2 e, uint32_t &lo)
 {

@@ -14,8 +14,8 @@
 // the merge joins a row's pieces of both maps, subtracts and norms.  Where keys are few a cluster takes a whole unit and joins
 // its parts through shared memory (plan_diff, pe_host.cu).
 //
-// Bound by HBM, and by what does not shrink with the bytes.  16 agents of 2k to 8k keys, 32 / 8 heads, d = 128: 57 us (5.9
-// TB/s); 64 query heads on 120k keys 80 us (6.1); 8 agents of 32k keys and 16 queries (64 rows) 178 us (6.0).  Of the 80: first
+// Bound by HBM, and by what does not shrink with the bytes.  16 agents of 2k to 8k keys, 32 / 8 heads, d = 128: 60 us (5.6
+// TB/s); 64 query heads on 120k keys 82 us (6.0); 8 agents of 32k keys and 16 queries (64 rows) 180 us (6.0).  Of the 82: first
 // scores 3.6 us after the launch before ends; the SMs finish over 16 us, for some groups of eight take their bytes 13 % slower
 // than others; 1 us to the merge and 4 in it.  (Equal shares of bytes; shares taken as the SMs come free would need pieces
 // short enough that the merge, or the pieces' own starts, cost what they save.)
@@ -796,8 +796,9 @@ cudaError_t launch_diff_combine(int head_dim, bool many, const DiffParams &p, cu
         return pieces ? cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<64, 16, 4>, p)
                       : cudaLaunchKernelEx(&cfg, diff_many_combine_kernel<64, 8, 1>, p);
     }
-    // Few pieces of many rows go a warp a row: 8 agents of 32k keys and 16 queries (6 pieces of 4096 rows and heads) 183 us, by
-    // blocks 188; one agent of 120k keys (39 pieces of 32) by blocks 85.8, 3000 keys of 4 heads 9.6.
+    // Few pieces of many rows go a warp a row: 8 agents of 32k keys and 16 queries, normed (6 pieces of 4096 rows and heads) 189
+    // us, by blocks 197.  Very many pieces of few rows take three sets of warps: one agent of 120k keys (39 pieces of 32) 82.6 us,
+    // with one set 89.5.
     const DiffSeq &last = p.seqs[p.n_seqs - 1];
     if (p.n_takers <= 8 * (last.unit0 + last.n_blocks * (p.hkv / 2)) && p.n_out >= 1024) {
         const cudaLaunchConfig_t cfg = diff_config((p.n_out + kRowMergeWarps - 1) / kRowMergeWarps, 32 * kRowMergeWarps, 0, st, &attr);

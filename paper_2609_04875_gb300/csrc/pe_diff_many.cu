@@ -12,9 +12,10 @@
 // share its reference: it moves only when a tile's sum passes 2^64 (pe_attn.cu), so per tile they exchange one vote, and the
 // maxima only then and at a piece's first tile.
 //
-// Measured: 1638 queries on 16k keys, 32 / 8 heads, d = 128: 370 to 395 us (1.6 to 1.7 PFLOP/s; the card's power limit), 400
-// queries 108 us; d = 64, whose softmax has half the MMAs' time to hide in, 309 us (1.0 PFLOP/s).  With the vote left out 283 at d
-// = 64, with sums before rounding 281 (d = 128: 1 to 4 %).  Not kept: P in columns of its own at d = 64, so that S(j + 2) need
+// Measured: 1638 queries on 16k keys, 32 / 8 heads, d = 128: 542 to 578 us (1.8 to 1.9 PFLOP/s of products, P's two parts counted;
+// tensor cores 90 % busy, the card's power limit), 400 queries 150 us; d = 64, whose softmax has half the MMAs' time to hide in,
+// 360 to 374 us.  Weights in one part took 378 and 309 and were not accurate enough (two_parts).  Not kept, all measured with one
+// part (309, 395, 24.4 and 71 us): P in columns of its own at d = 64, so that S(j + 2) need
 // not wait for P V(j), 362 us; four warpgroups with a quarter of the keys each 341 (d = 128 406); both maps of a block in a
 // cluster of four that finishes its rows itself: 500 queries on 1000 keys 26.6 us against 24.4, 2000 on 2000 97 against 71.
 //

@@ -2324,13 +2324,13 @@ template <typename Shape>
 constexpr int64_t kDiffUnitCost = Shape::kMaps == 2 ? 4 : 5;
 
 // Few rows on few keys: a cluster of 1 to 8 CTAs a whole unit, at most kDiffWholeTiles tiles each where there are SMs enough, whose
-// rows it joins itself, in place of cutting every unit and merging the pieces in a second launch.  A tile takes 0.75 us, a
-// row of each of nine warps about as much.  A call of one query, with its output allocated (host and GPU), whole / cut: 8
-// heads of d = 64 on 640 keys 10.9 / 15.2 us, on 3000 12.6 / 16.0, 16 of d = 128 on 2 x 2000 12.9 / 15.2, 32 on 7 x 1700 14.5 /
-// 15.9; on 5000 (10 tiles a CTA) 16.8 / 15.8.  Only clusters that the device holds all at once: of 8 CTAs the card has room for
+// rows it joins itself, in place of cutting every unit and merging the pieces in a second launch.  A tile takes 0.95 us (d = 64:
+// 0.6), a row of each of nine warps 0.9.  A call of one query, with its output allocated (host and GPU), whole / cut: 8 heads of
+// d = 64 on 640 keys 11.3 / 15.9 us, on 3000 13.3 / 16.1, 16 of d = 128 on 2 x 2000 13.7 / 15.8, 32 on 7 x 1700 16.7 / 16.8; on
+// 5000 (10 tiles a CTA) 19.5 / 15.8.  (Prepared calls back to back, where the merge's launch hides: 640 keys 9.9 / 8.6.)  Only clusters that the device holds all at once: of 8 CTAs the card has room for
 // 15, not 19, and a sixteenth waits for another to end (16 units of 2000 keys 26.8 us, cut 13.9).
 constexpr int64_t kDiffWhole = 8;       // tiles and rounds of rows of a CTA
-constexpr int64_t kDiffWholeTiles = 4;  // (10 tiles over 1, 2, 4 CTAs: 11.1, 9.7, 9.0 us; 5 over 1, 2: 9.6, 9.8)
+constexpr int64_t kDiffWholeTiles = 4;  // (10 tiles over 1, 2, 4 CTAs: 12.2, 10.6, 9.9 us; 5 over 1, 2: 9.1, 9.4)
 constexpr int64_t kDiffWholeRanks = 8;
 
 // One launch over the items, at most kMaxSegs: fills p's sequences and stretches.

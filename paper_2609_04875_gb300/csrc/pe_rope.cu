@@ -71,7 +71,6 @@ __device__ __forceinline__ void rope_chunk(const RopeParams &r, const uint4 *row
 
 // A thread's share of every row of a token: two chunks of eight columns, a and b, which are either copied or eight whole
 // pairs, whose angles it keeps.  In halves those are chunks c and c + n_pairs / 8, of neighbours 2c and 2c + 1.
-template <int CPR>
 struct PairOfChunks {
     int a, b;
     bool turns, interleaved;
@@ -134,7 +133,7 @@ __device__ __forceinline__ void rotate_rows(const RopeParams &r, const uint4 *sr
     constexpr int CP = CPR / 2, RPW = 32 / CP, U = V ? 2 : 4;
     const int lane = threadIdx.x & 31, c = lane % CP;
     if constexpr (WHOLE) {
-        const PairOfChunks<CPR> pc(r, c, tok, pos);
+        const PairOfChunks pc(r, c, tok, pos);
         for (int x0 = r0 + lane / CP; x0 < r1; x0 += U * RPW) {
             uint4 a[U], b[U], va[U], vb[U];
             int64_t at[U];
